@@ -52,7 +52,8 @@ typedef enum {
     RTN_ERR_VALUE = 4,          /* a weight code outside {-1,0,+1}, or a bad enum value        */
     RTN_ERR_UNSUPPORTED = 5,    /* the requested variant cannot run this shape                 */
     RTN_ERR_CUDA = 6,           /* a CUDA runtime call failed (launch, attribute, copy)        */
-    RTN_ERR_DEVICE_TIMEOUT = 7  /* a bounded device-side wait gave up (see last_device_status) */
+    RTN_ERR_DEVICE_TIMEOUT = 7, /* a bounded device-side wait gave up (see last_device_status) */
+    RTN_ERR_DEVICE_INDEX = 8    /* an index read on the device was out of range (see last_device_status) */
 } rtn_status;
 
 /* Treatment of filter taps that fall outside the image.  The paper never mentions padding; the
@@ -223,6 +224,88 @@ rtn_status rtn_pack_quaternary(const uint8_t* q_values, int64_t rows, int64_t K,
 rtn_status rtn_quaternary_gemm(const void* a_packed, const void* w_packed, int64_t M, int64_t N, int64_t K,
                                int32_t* out, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators of a ternary language-model layer around the packed products (the paper has no counterpart).
+ * Common to them: fp32, bf16 and fp16 tensors (arithmetic, norms, sums and states in fp32, one rounding at the
+ * end); strides count elements; a call with no tokens (M, T or B of 0) returns RTN_OK and launches nothing; calls
+ * only enqueue and can be captured in a graph (after a first call that sets kernel attributes).
+ * ---------------------------------------------------------------------------------------------- */
+typedef enum { RTN_F32 = 0, RTN_BF16 = 1, RTN_F16 = 2 } rtn_dtype;
+typedef enum { RTN_ACT_NONE = 0, RTN_ACT_RELU = 1, RTN_ACT_GELU = 2 /* erf */, RTN_ACT_GELU_TANH = 3, RTN_ACT_SILU = 4 } rtn_activation;
+typedef enum { RTN_ROTARY_HALF = 0 /* pairs (i, i + R/2) */, RTN_ROTARY_INTERLEAVED = 1 /* pairs (2i, 2i + 1) */ } rtn_rotary_layout;
+typedef enum { RTN_ROTARY_SCALE_NONE = 0, RTN_ROTARY_SCALE_LINEAR = 1, RTN_ROTARY_SCALE_BASE = 2, RTN_ROTARY_SCALE_PARTS = 3 } rtn_rotary_scaling;
+
+/* Ternary linear layer: the packed product with bias, activation and residual in its epilogue.
+ *     out[m][n] = act( sum_k (a_s x[m][k] + a_o)(w_s w[n][k] + w_o) + bias[n] ) + residual[m][n]
+ *   a_packed ... n_wparam   as in rtn_ternary_gemm
+ *   bias        NULL, or fp32 [N]
+ *   residual    NULL, or [M][N] of `dtype`, rows residual_stride elements apart; may be `out` itself (same stride), to
+ *               add a layer to a residual stream in place; no other overlap
+ *   out         [M][N] of `dtype`, rows out_stride >= N elements apart
+ * Up to 8 rows (16 where the columns are few) run on a bit-plane kernel that streams the weights once, more rows
+ * on the tensor cores with the launches of rtn_gemm_kernel_launches. */
+rtn_status rtn_ternary_linear(const void* a_packed, const int32_t* a_sum,
+                              const void* w_packed, const int32_t* w_sum,
+                              int64_t M, int64_t N, int64_t K,
+                              const float* a_scale, const float* a_offset, int64_t n_aparam,
+                              const float* w_scale, const float* w_offset, int64_t n_wparam,
+                              const float* bias, rtn_activation act, const void* residual, int64_t residual_stride,
+                              void* out, int64_t out_stride, rtn_dtype dtype, void* stream);
+
+/* Table of a rotation: fp32 [rows][R], row p = cos(p f_i), i < R/2, then sin(p f_i), each times `amplitude`.
+ * R even, >= 2.  f_i = base^(-2i/R) and, for contexts longer than the one a model was trained on,
+ *   LINEAR  f_i / factor
+ *   BASE    base * factor^(R/(R-2)) in place of base (R > 2)
+ *   PARTS   f_i where it makes at least `high` turns over `original_context` positions, f_i / factor where it makes at
+ *           most `low`, a linear ramp in the turns between (high > low)
+ * Angles are computed in double.  factor, original_context, low, high are read by the kinds that name them. */
+rtn_status rtn_rotary_table(float* table, int64_t rows, int64_t R, double base, rtn_rotary_scaling scaling, double factor,
+                            double original_context, double low, double high, double amplitude, void* stream);
+
+/* Norms of the query and key heads and their rotation by position, in one pass:
+ *     y = x w / sqrt(mean(x^2) + eps);   the first R of the D elements rotated by row positions[t] of the table
+ *   q, k        [T][Hq][D] and [T][Hk][D] of `dtype`: token t, head h starts at t*token + h*head, elements adjacent
+ *   out_q,out_k same shapes with strides of their own; out_q == q with q's strides (in place) is allowed, also
+ *               for k, no other overlap
+ *   q_weight, k_weight   fp32 [D], or both NULL: no norm, the rotation alone
+ *   table       fp32 [table_rows][R] (rtn_rotary_table), 4-byte aligned; NULL with R = 0: the norms alone
+ *   positions   int64 [T], or NULL: token t is at position t
+ * Hk = 0 (k NULL) is allowed.  D <= 1024, R even, R <= D.  A position outside the table makes the token's heads NaN, and
+ * rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once. */
+rtn_status rtn_qk_norm_rotary(const void* q, int64_t q_token, int64_t q_head, const void* k, int64_t k_token, int64_t k_head,
+                              void* out_q, int64_t oq_token, int64_t oq_head, void* out_k, int64_t ok_token, int64_t ok_head,
+                              int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t R, rtn_rotary_layout layout,
+                              const float* q_weight, const float* k_weight, float eps,
+                              const float* table, int64_t table_rows, const int64_t* positions, rtn_dtype dtype, void* stream);
+
+/* Linear attention with a decay for each head, over whole prompts of different lengths.  Per sequence and head h:
+ *     S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,      out_t = scale q_t^T S_t
+ *   q           [total][H][Dk], k [total][Hk][Dk], v [total][Hk][Dv] of `dtype` with token and head strides, elements
+ *               adjacent; H a multiple of Hk, query head h reads key head h / (H/Hk)
+ *   out         [total][H][Dv] of `dtype`, strides of its own, no overlap with the inputs
+ *   log_decay   fp32 [H], natural logarithm, <= 0 in every intended use
+ *   start       int32 [B+1], on the device: sequence b has tokens start[b] .. start[b+1]-1; lengths of 0 are allowed
+ *   max_len     at least the longest length (sizes the grid)
+ *   state       fp32 [n_slots][H][Dk][Dv] holding S before the first token, or NULL: zero
+ *   state_out   same shape, receives S after the last token; may be `state` (in place).  Required.
+ *   slots       int32 [B] (on the device): sequence b's state is slots[b]; the live slots are distinct; a negative slot
+ *               is a padding entry: its out rows become zero and no state is read or written.  NULL: slot b
+ * Dk, Dv <= 256.  Bounds that do not fit (a decreasing start, a length over max_len, a slot >= n_slots) make the kernel
+ * skip the sequence (its rows of out are not written), and rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once. */
+rtn_status rtn_decay_attention(const void* q, int64_t q_token, int64_t q_head, const void* k, int64_t k_token, int64_t k_head,
+                               const void* v, int64_t v_token, int64_t v_head, void* out, int64_t o_token, int64_t o_head,
+                               int64_t total, int64_t B, const int32_t* start, int64_t max_len,
+                               int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, const float* log_decay, float scale,
+                               const float* state, float* state_out, const int32_t* slots, int64_t n_slots,
+                               rtn_dtype dtype, void* stream);
+
+/* The same for one new token of each of B sequences (token b belongs to sequence b). */
+rtn_status rtn_decay_attention_step(const void* q, int64_t q_token, int64_t q_head, const void* k, int64_t k_token, int64_t k_head,
+                                    const void* v, int64_t v_token, int64_t v_head, void* out, int64_t o_token, int64_t o_head,
+                                    int64_t B, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, const float* log_decay, float scale,
+                                    const float* state, float* state_out, const int32_t* slots, int64_t n_slots,
+                                    rtn_dtype dtype, void* stream);
+
 /* The variant RTN_VARIANT_AUTO resolves to for a shape (never AUTO). */
 rtn_variant rtn_choose_gemm_variant(int64_t M, int64_t N, int64_t K);
 /* Slices of K that RTN_VARIANT_AUTO cuts a GEMM shape into (1 = none).  A linear layer with few rows and
@@ -251,7 +334,8 @@ int64_t rtn_conv_next_kernel_launches(int64_t B, int64_t C, int64_t H, int64_t W
 
 /* Synchronises `stream`, then reads and clears the device status word of the current device.
  * RTN_OK, or RTN_ERR_DEVICE_TIMEOUT if a kernel's bounded wait (on an mbarrier of the
- * tensor-core pipeline) ran out since the last call; that kernel's output is then invalid. */
+ * tensor-core pipeline) ran out since the last call; that kernel's output is then invalid.  Else
+ * RTN_ERR_DEVICE_INDEX if a layer operator met a position, slot or sequence bound out of range. */
 rtn_status rtn_last_device_status(void* stream);
 
 /* Self-test of the bounded waits (the safety net behind RTN_ERR_DEVICE_TIMEOUT): launches one small kernel

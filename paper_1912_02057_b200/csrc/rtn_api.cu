@@ -99,6 +99,7 @@ const char* rtn_status_string(rtn_status s)
         case RTN_ERR_UNSUPPORTED: return "RTN_ERR_UNSUPPORTED: variant cannot run this shape";
         case RTN_ERR_CUDA: return "RTN_ERR_CUDA: CUDA runtime call failed";
         case RTN_ERR_DEVICE_TIMEOUT: return "RTN_ERR_DEVICE_TIMEOUT: bounded device wait gave up";
+        case RTN_ERR_DEVICE_INDEX: return "RTN_ERR_DEVICE_INDEX: an index read on the device was out of range";
     }
     return "unknown rtn_status";
 }
@@ -450,7 +451,8 @@ rtn_status rtn_last_device_status(void* stream)
         if (cudaMemsetAsync(st, 0, sizeof(unsigned), s) != cudaSuccess) return RTN_ERR_CUDA;
         if (cudaStreamSynchronize(s) != cudaSuccess) return RTN_ERR_CUDA;
     }
-    return (h & rtn::kStatusWaitTimeout) ? RTN_ERR_DEVICE_TIMEOUT : RTN_OK;
+    if (h & rtn::kStatusWaitTimeout) return RTN_ERR_DEVICE_TIMEOUT;
+    return (h & rtn::kStatusBadIndex) ? RTN_ERR_DEVICE_INDEX : RTN_OK;
 }
 
 }  // extern "C"

@@ -21,6 +21,9 @@
 #include "rtn_tcgen05.cuh"
 #include "rtn_timeline.cuh"
 #include "rtn_tensormap.cuh"
+#include "rtn_epilogue.cuh"
+
+#include <type_traits>
 
 // Timeline slots (instrumented build only): 0 kernel entry, 1 set-up done (expanded operands visible), 4 kernel end;
 // per tile i < 8 of the CTA: 40+2i first stage of the tile ready for the tensor core, 41+2i accumulators committed,
@@ -69,6 +72,7 @@ struct GemmI8Plan {
     uint32_t stage_bytes, off_stage, off_c, off_bar, off_misc, off_t;
     size_t smem_bytes;
     int tma_out;            // the epilogue writes the output with TMA stores (set by the launcher)
+    int res_vec;            // the residual's rows are 16-byte aligned (set by the launcher)
 };
 
 bool make_gemm_plan(int64_t M, int64_t N, int64_t K, GemmI8Plan& p, int sms)
@@ -111,6 +115,7 @@ bool make_gemm_plan(int64_t M, int64_t N, int64_t K, GemmI8Plan& p, int sms)
     o += kMaxEpiWarps * kStageWarp > 1024 + kTmaWarpsPre * kTmaStageWarp ? kMaxEpiWarps * kStageWarp
                                                                            : 1024 + kTmaWarpsPre * kTmaStageWarp;
     p.tma_out = 0;
+    p.res_vec = 0;
     o = (o + 127) / 128 * 128;
     p.off_stage = o;
     int ns = (int)((kSmemLimit - o) / p.stage_bytes);
@@ -161,15 +166,96 @@ gemm_expand_operands_kernel(const GemmArgs g, const __grid_constant__ GemmI8Plan
     dst[7 * R] = make_uint4(o[4], o[5], o[6], o[7]);
 }
 
+template <typename T> struct LinearTOf { using type = T; };
+template <> struct LinearTOf<void> { using type = float; };
+template <typename T> using LinearT = typename LinearTOf<T>::type;
+
+// Epilogue of rtn_ternary_linear for one warp's 32 rows and the columns c_begin .. c_end of a tile: blocks of 64 bytes of each row
+// (16 fp32 or 32 half-precision columns).  The residual's block is asked for before the accumulators are read; the results
+// leave as in the plain epilogue, staged and handed to the copy engine, or row by row where the output's rows are not
+// 16-byte aligned.
+template <typename T>
+__device__ __forceinline__ void linear_rows_out(const GemmArgs& g, const LinearArgs& l, const GemmI8Plan& p, const CUtensorMap& omap,
+                                                const float4* sC, uint32_t trow, int64_t m, int64_t mbase, int64_t n0,
+                                                int c_begin, int c_end, bool row_ok, bool alive, float a_s, float a_o, float s_x,
+                                                int lane, uint32_t tma_stage)
+{
+    constexpr int V = Vec16<T>::N, kCols = 4 * V;                      // columns of 16 and of 64 bytes
+    const T* res = static_cast<const T*>(l.residual);
+    for (int c0 = c_begin; c0 < c_end; c0 += kCols) {
+        uint4 rv[4];
+        // 16-byte reads of the residual: rows on 16-byte boundaries (the launcher checked), whole vectors inside the row
+        const bool res_vec = l.residual != nullptr && p.res_vec && row_ok && n0 + c0 + kCols <= g.N;
+        if (res_vec) {
+            #pragma unroll
+            for (int i = 0; i < 4; ++i) rv[i] = *reinterpret_cast<const uint4*>(res + m * l.res_stride + n0 + c0 + i * V);
+        }
+        float r[kCols];
+        #pragma unroll
+        for (int h = 0; h < kCols; h += 16) {
+            uint32_t v[16];
+            tc::tmem_ld16(trow + (uint32_t)(c0 + h < p.BN ? c0 + h : 0), v);       // past the tile: columns past N, never stored
+            tc::tmem_ld_wait();
+            #pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float4 c = sC[c0 + h < p.BN ? c0 + h + j : 0];
+                r[h + j] = activate(fmaf(a_s, fmaf(c.x, (float)(int)v[j], c.y * s_x), a_o * c.z) + c.w, l.act);
+            }
+        }
+        if (l.residual != nullptr) {
+            if (res_vec) {
+                #pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float f[V];
+                    Vec16<T>::unpack(rv[i], f);
+                    #pragma unroll
+                    for (int e = 0; e < V; ++e) r[i * V + e] += f[e];
+                }
+            } else if (row_ok) {
+                #pragma unroll
+                for (int j = 0; j < kCols; ++j)
+                    if (c0 + j < p.BN && n0 + c0 + j < g.N) r[j] += to_f32(res[m * l.res_stride + n0 + c0 + j]);
+            }
+        }
+        if (p.tma_out) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
+            #pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float f[V];
+                #pragma unroll
+                for (int e = 0; e < V; ++e) f[e] = r[i * V + e];
+                const uint4 u = Vec16<T>::pack(f);
+                const uint32_t dst = tma_stage + (uint32_t)lane * 64u + (uint32_t)((i ^ ((lane >> 1) & 3)) << 4);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
+            }
+            tc::fence_smem_to_async_proxy();
+            __syncwarp();
+            if (lane == 0 && alive && mbase < g.M && n0 + c0 < g.N) {
+                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                             ::"l"(reinterpret_cast<uint64_t>(&omap)), "r"((int)(n0 + c0)), "r"((int)mbase), "r"(tma_stage) : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+        } else if (row_ok) {
+            T* orow = static_cast<T*>(l.out) + m * l.out_stride + n0 + c0;
+            #pragma unroll
+            for (int j = 0; j < kCols; ++j)
+                if (c0 + j < p.BN && n0 + c0 + j < g.N) orow[j] = from_f32<T>(r[j]);
+        }
+    }
+}
+
 // kPreW: the weight part of every stage comes from the scratch buffer gemm_expand_operands_kernel wrote (one
 // bulk asynchronous copy per stage, issued by a thread of warp 1), so the expander warps expand only the
 // activation rows: half of the integer work that paces the kernel.  kPreA (only with kPreW): the activation
 // part too; the expander warps then have nothing to do and the ring is paced by the copies and the MMAs.
-template <bool kPreW, bool kPreA>
+// OutT = void: rtn_ternary_gemm.  Otherwise the epilogue of rtn_ternary_linear (LinearArgs) with OutT outputs.
+template <bool kPreW, bool kPreA, typename OutT>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_i8_kernel(const GemmArgs g, const __grid_constant__ GemmI8Plan p, const uint4* __restrict__ wexp,
-               const uint4* __restrict__ aexp, const __grid_constant__ CUtensorMap omap)
+               const uint4* __restrict__ aexp, const __grid_constant__ CUtensorMap omap, const LinearArgs l)
 {
+    constexpr bool kLinear = !std::is_void<OutT>::value;
     extern __shared__ __align__(128) uint8_t smem[];
     float4* sC = reinterpret_cast<float4*>(smem + p.off_c);
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + p.off_bar);
@@ -361,20 +447,22 @@ gemm_i8_kernel(const GemmArgs g, const __grid_constant__ GemmI8Plan p, const uin
             asm volatile("bar.sync %0, %1;" ::"r"(kEpiBarrier), "r"(nEpiThreads) : "memory");
             for (int j = etid; j < p.BN; j += nEpiThreads) {
                 const int64_t n = n0 + j;
-                float p1 = 0.f, p2 = 0.f, p3 = 0.f;
+                float p1 = 0.f, p2 = 0.f, p3 = 0.f, p4 = 0.f;
                 if (n < g.N) {
+                    if constexpr (kLinear) { if (l.bias != nullptr) p4 = l.bias[n]; }
                     const double ws = g.ep.w_scale[g.ep.n_wparam == 1 ? 0 : n];
                     const double wo = g.ep.w_offset[g.ep.n_wparam == 1 ? 0 : n];
                     p1 = (float)ws; p2 = (float)wo;
                     p3 = (float)(ws * (double)g.w_sum[n] + (double)g.K * wo);
                 }
-                sC[j] = make_float4(p1, p2, p3, 0.f);
+                sC[j] = make_float4(p1, p2, p3, p4);
             }
             asm volatile("bar.sync %0, %1;" ::"r"(kEpiBarrier), "r"(nEpiThreads) : "memory");
             const bool alive = wait_or_die(&acc_full[acc], acc_ph, g.status, dead);
             tc::tc_fence_after_sync();
             if (etid == 0 && tc_ < 8) RTN_TL(gemm_i8, 56 + 2 * (int)tc_);
-            const int per = ((p.BN + parts_used - 1) / parts_used + 15) / 16 * 16;     // columns per range, whole blocks of 16
+            constexpr int kBlk = kLinear && sizeof(LinearT<OutT>) == 2 ? 32 : 16;      // columns of a staged block (64 bytes of a row)
+            const int per = ((p.BN + parts_used - 1) / parts_used + kBlk - 1) / kBlk * kBlk;     // columns per range, whole blocks
             const int c_begin = part * per < p.BN ? part * per : p.BN;
             const int c_end = c_begin + per < p.BN ? c_begin + per : p.BN;
             for (int tm = 0; tm < p.TM; ++tm) {
@@ -390,6 +478,10 @@ gemm_i8_kernel(const GemmArgs g, const __grid_constant__ GemmI8Plan p, const uin
                 const int64_t mbase = m0 + tm * 128 + q * 32;
                 // write-out of a staged block: lane -> rows rr and rr + 16, 16-byte chunk ch
                 const int rr = (lane & 7) + 8 * (lane >> 4), ch = (lane >> 3) & 1;
+                if constexpr (kLinear) {
+                    linear_rows_out<OutT>(g, l, p, omap, sC, trow, m, mbase, n0, c_begin, c_end, row_ok, alive, a_s, a_o, s_x,
+                                          lane, tma_stage);
+                } else
                 for (int c0 = c_begin; c0 < c_end; c0 += 16) {
                     uint32_t v[16];
                     tc::tmem_ld16(trow + (uint32_t)c0, v);
@@ -499,30 +591,31 @@ int gemm_i8_launches(int64_t M, int64_t N, int64_t K)
     return gemm_pre_mode(p, K) == 0 ? 1 : 2;
 }
 
-cudaError_t launch_gemm_i8(const GemmArgs& g, cudaStream_t s)
+// Output as a 2-D tensor for the epilogue's TMA stores: boxes of 32 rows x 64 bytes, 64-byte swizzle.  Needs rows on 16-byte
+// boundaries and at least one box of columns.
+static bool encode_output(CUtensorMap* omap, void* out, int64_t M, int64_t N, int64_t stride, int dtype)
 {
-    GemmI8Plan p;
-    if (!make_gemm_plan(g.M, g.N, g.K, p, device_sm_count())) return cudaErrorInvalidConfiguration;
+    const int e = dtype_bytes(dtype);
+    if ((N * e & 15) != 0 || (stride * e & 15) != 0 || N * e < 64 || (reinterpret_cast<uintptr_t>(out) & 15) != 0) return false;
+    EncodeTiledFn enc = encode_tiled_fn();
+    const cuuint64_t dims[2] = {(cuuint64_t)N, (cuuint64_t)M};
+    const cuuint64_t strides[1] = {(cuuint64_t)(stride * e)};
+    const cuuint32_t box[2] = {(cuuint32_t)(64 / e), 32};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUtensorMapDataType type = dtype == RTN_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == RTN_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return enc != nullptr && enc(omap, type, 2, out, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+                                 CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename OutT>
+static cudaError_t launch_gemm_i8_typed(const GemmArgs& g, const LinearArgs& l, GemmI8Plan& p, const CUtensorMap& omap, cudaStream_t s)
+{
     const int mode = gemm_pre_mode(p, g.K);
-    // Output as a 2-D tensor for the epilogue's TMA stores: rows of N floats, boxes of 32 rows x 16 columns,
-    // 64-byte swizzle.  Needs 16-byte aligned rows; the debug output keeps the store-instruction epilogue.
-    CUtensorMap omap;
-    memset(&omap, 0, sizeof(omap));
-    if (g.dbg_acc == nullptr && (g.N & 3) == 0 && g.N >= kTmaCols && (reinterpret_cast<uintptr_t>(g.out) & 15) == 0) {
-        EncodeTiledFn enc = encode_tiled_fn();
-        const cuuint64_t dims[2] = {(cuuint64_t)g.N, (cuuint64_t)g.M};
-        const cuuint64_t strides[1] = {(cuuint64_t)g.N * 4};
-        const cuuint32_t box[2] = {(cuuint32_t)kTmaCols, 32};
-        const cuuint32_t estr[2] = {1, 1};
-        if (enc != nullptr &&
-            enc(&omap, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, g.out, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS)
-            p.tma_out = 1;
-    }
     if (mode == 0) {
-        cudaError_t e = cudaFuncSetAttribute(gemm_i8_kernel<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
+        cudaError_t e = cudaFuncSetAttribute(gemm_i8_kernel<false, false, OutT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
         if (e != cudaSuccess) return e;
-        gemm_i8_kernel<false, false><<<(unsigned)p.grid, kThreads, p.smem_bytes, s>>>(g, p, nullptr, nullptr, omap);
+        gemm_i8_kernel<false, false, OutT><<<(unsigned)p.grid, kThreads, p.smem_bytes, s>>>(g, p, nullptr, nullptr, omap, l);
         return cudaGetLastError();
     }
     // scratch from the stream-ordered allocator: N (and M) rounded up to tiles, times K rounded up to blocks, bytes
@@ -536,18 +629,40 @@ cudaError_t launch_gemm_i8(const GemmArgs& g, cudaStream_t s)
     gemm_expand_operands_kernel<<<(unsigned)((items_w + items_a + 255) / 256), 256, 0, s>>>(g, p, wexp, aexp);
     e = cudaGetLastError();
     if (e == cudaSuccess && mode == 1) {
-        e = cudaFuncSetAttribute(gemm_i8_kernel<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
+        e = cudaFuncSetAttribute(gemm_i8_kernel<true, false, OutT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
         if (e == cudaSuccess)
-            e = launch_pdl(gemm_i8_kernel<true, false>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, g, p,
-                           (const uint4*)wexp, (const uint4*)aexp, omap);
+            e = launch_pdl(gemm_i8_kernel<true, false, OutT>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, g, p,
+                           (const uint4*)wexp, (const uint4*)aexp, omap, l);
     } else if (e == cudaSuccess) {
-        e = cudaFuncSetAttribute(gemm_i8_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
+        e = cudaFuncSetAttribute(gemm_i8_kernel<true, true, OutT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
         if (e == cudaSuccess)
-            e = launch_pdl(gemm_i8_kernel<true, true>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, g, p,
-                           (const uint4*)wexp, (const uint4*)aexp, omap);
+            e = launch_pdl(gemm_i8_kernel<true, true, OutT>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, g, p,
+                           (const uint4*)wexp, (const uint4*)aexp, omap, l);
     }
     const cudaError_t e2 = cudaFreeAsync(scratch, s);
     return e != cudaSuccess ? e : e2;
+}
+
+cudaError_t launch_gemm_i8(const GemmArgs& g, cudaStream_t s)
+{
+    GemmI8Plan p;
+    if (!make_gemm_plan(g.M, g.N, g.K, p, device_sm_count())) return cudaErrorInvalidConfiguration;
+    CUtensorMap omap;
+    memset(&omap, 0, sizeof(omap));
+    // the debug output keeps the store-instruction epilogue
+    if (g.dbg_acc == nullptr && encode_output(&omap, g.out, g.M, g.N, g.N, RTN_F32)) p.tma_out = 1;
+    return launch_gemm_i8_typed<void>(g, LinearArgs{}, p, omap, s);
+}
+
+cudaError_t launch_gemm_i8_linear(const GemmArgs& g, const LinearArgs& l, cudaStream_t s)
+{
+    GemmI8Plan p;
+    if (!make_gemm_plan(g.M, g.N, g.K, p, device_sm_count())) return cudaErrorInvalidConfiguration;
+    CUtensorMap omap;
+    memset(&omap, 0, sizeof(omap));
+    if (encode_output(&omap, l.out, g.M, g.N, l.out_stride, l.dtype)) p.tma_out = 1;
+    p.res_vec = l.residual != nullptr && (reinterpret_cast<uintptr_t>(l.residual) & 15) == 0 && l.res_stride * dtype_bytes(l.dtype) % 16 == 0;
+    return with_dtype(l.dtype, [&](auto t) { return launch_gemm_i8_typed<decltype(t)>(g, l, p, omap, s); });
 }
 
 }  // namespace rtn

@@ -10,6 +10,7 @@ namespace rtn {
 // Bits of the device status word.
 constexpr unsigned kStatusBadWeightCode = 1u;   // rtn_pack_weights met a code outside {-1,0,+1}
 constexpr unsigned kStatusWaitTimeout   = 2u;   // a bounded mbarrier wait gave up
+constexpr unsigned kStatusBadIndex      = 4u;   // a position, slot or sequence bound read on the device is out of range
 
 // Packed format: 128 codes per 32-byte block (16 B plane 1 "non-zero", 16 B plane 2 "sign").
 constexpr int kBlockCodes = 128;
@@ -72,6 +73,54 @@ struct NextLayerArgs {
     uint8_t* out_packed;    // [B*Ho*Wo] packed rows of N codes
 };
 
+// What the ternary product does after the affine form (rtn_ternary_linear):
+//   out = act(affine + bias[n]) + residual, rounded once to dtype.
+struct LinearArgs {
+    const float* bias;          // [N] or NULL
+    int act;                    // rtn_activation
+    const void* residual;       // [M][N] of dtype, rows res_stride elements apart, or NULL
+    int64_t res_stride;
+    void* out;                  // [M][N] of dtype, rows out_stride elements apart
+    int64_t out_stride;
+    int dtype;                  // rtn_dtype
+};
+
+constexpr int kRotaryMaxDim = 1024;
+struct RotaryArgs {
+    const void *q, *k;
+    int64_t q_token, q_head, k_token, k_head;           // strides in elements
+    void *out_q, *out_k;
+    int64_t oq_token, oq_head, ok_token, ok_head;
+    const float *q_weight, *k_weight;                   // [D] or NULL (no norm)
+    float eps;
+    const float* table;                                 // [table_rows][R]: R/2 cosines, R/2 sines
+    int64_t table_rows;
+    const int64_t* positions;                           // [T] or NULL (token t is at position t)
+    int64_t T;
+    int Hq, Hk, D, R, layout, dtype;
+    unsigned* status;
+};
+
+constexpr int kDecayMaxDim = 256;
+struct DecayArgs {
+    const void *q, *k, *v;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head;      // strides in elements
+    void* out;
+    int64_t o_token, o_head;
+    const float* log_decay;                             // [H]
+    const float* state;                                 // [slots][H][Dk][Dv] or NULL (zero)
+    float* state_out;                                   // same shape
+    const int32_t* slot;                                // [B] or NULL (sequence b has slot b)
+    int64_t n_slots;
+    const int32_t* start;                               // [B + 1] first tokens (NULL in the single-token form)
+    int64_t total;                                      // tokens in q, k, v, out
+    int64_t max_len;
+    int64_t B;
+    int H, Hk, Dk, Dv, dtype;
+    float scale;
+    unsigned* status;
+};
+
 // Multiprocessors of the current device, asked once per device.  Plans, *_supported answers, launch counts,
 // scratch sizes and the launchers all size their grids with this number, so they agree on any part.  Without a
 // usable device (a host-only query) the answer is a B200's 148.
@@ -110,6 +159,16 @@ cudaError_t launch_pack_quaternary(const uint8_t* q, int64_t rows, int64_t K, ui
                                    cudaStream_t s);
 cudaError_t launch_gemm_quaternary(const uint8_t* a, const uint8_t* w, int64_t M, int64_t N, int64_t K, int32_t* out,
                                    cudaStream_t s);
+
+// Operators of a ternary language-model layer.
+cudaError_t launch_linear(const GemmArgs& g, const LinearArgs& l, cudaStream_t s);
+bool linear_rows_path(int64_t M, int64_t N, int64_t K);       // few rows: the bit-plane kernel, else the tensor cores
+cudaError_t launch_gemm_i8_linear(const GemmArgs& g, const LinearArgs& l, cudaStream_t s);
+cudaError_t launch_qk_norm_rotary(const RotaryArgs& g, cudaStream_t s);
+cudaError_t launch_rotary_table(float* table, int64_t rows, int R, double base, int kind, double factor, double original,
+                                double low, double high, double amplitude, cudaStream_t s);
+cudaError_t launch_decay_attention(const DecayArgs& g, cudaStream_t s);
+cudaError_t launch_decay_attention_step(const DecayArgs& g, cudaStream_t s);
 
 // Tensor-core (tcgen05 kind::i8) variants; *_supported say whether a shape can run there.
 bool gemm_i8_supported(int64_t M, int64_t N, int64_t K);

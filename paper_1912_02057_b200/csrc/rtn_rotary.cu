@@ -1,0 +1,258 @@
+// Root-mean-square norms of the query and key heads and the rotation by position, one pass over both tensors:
+//
+//   y = x * w / sqrt(mean(x^2) + eps)            (w == NULL: y = x)
+//   (y_a, y_b) <- (y_a c - y_b s, y_b c + y_a s)   for the R/2 pairs (a, b) of the head's first R elements,
+//                                                  (c, s) = row positions[t] of the table
+//
+// with pairs (i, i + R/2) in the half layout and (2i, 2i + 1) in the interleaved one.
+//
+// Bound: DRAM, each element read and written once.  A group of lanes (a power of two, at most a warp) owns one head: a lane
+// holds 16 bytes of it in registers, the sum of squares is a shuffle tree over the group, and in the half layout the
+// lane reads its partner's 16 bytes as well (the line its own group just brought in: one load instead of a shuffle
+// per element).  The cosines, sines and weights of a lane's elements are the same for every head of a token, so a group
+// takes several heads of one token and reads them once.
+#include "rtn_internal.cuh"
+#include "rtn_types.cuh"
+
+namespace rtn {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kGenericWarps = 4;
+
+__device__ __forceinline__ bool token_position(const RotaryArgs& g, int64_t t, int64_t& pos)
+{
+    pos = g.positions != nullptr ? g.positions[t] : t;
+    return pos >= 0 && pos < g.table_rows;
+}
+
+// HP heads of one token per group of G lanes; CH 16-byte chunks per lane (head dimension up to 32 CH chunks).
+template <typename T, int CH, int HP>
+__global__ void __launch_bounds__(kThreads)
+qk_norm_rotary_kernel(const RotaryArgs g, int G, int groups_q, int groups_k)
+{
+    constexpr int V = Vec16<T>::N;
+    const int lane_g = threadIdx.x & (G - 1);
+    const int64_t item = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+    const int per_token = groups_q + groups_k;
+    const int64_t t = item / per_token;
+    const bool live = t < g.T;                       // groups past the end stay for the warp's shuffles
+    const int gi = (int)(item - t * per_token);
+    const bool is_q = gi < groups_q;
+    const int h0 = (is_q ? gi : gi - groups_q) * HP;
+    const int H = is_q ? g.Hq : g.Hk;
+    const T* src = static_cast<const T*>(is_q ? g.q : g.k) + (live ? t : 0) * (is_q ? g.q_token : g.k_token);
+    T* dst = static_cast<T*>(is_q ? g.out_q : g.out_k) + (live ? t : 0) * (is_q ? g.oq_token : g.ok_token);
+    const int64_t s_head = is_q ? g.q_head : g.k_head, d_head = is_q ? g.oq_head : g.ok_head;
+    const float* w = is_q ? g.q_weight : g.k_weight;
+    const int nch = g.D / V, hch = g.R / 2 / V;      // chunks of a head, of half its rotated part
+
+    // the heads' elements (and, in the half layout, the partners') first: everything below waits for them
+    uint4 own[HP][CH], other[HP][CH];
+    #pragma unroll
+    for (int p = 0; p < HP; ++p)
+        #pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int ch = lane_g + c * 32;
+            own[p][c] = other[p][c] = make_uint4(0, 0, 0, 0);
+            if (live && h0 + p < H && ch < nch) {
+                const uint4* row = reinterpret_cast<const uint4*>(src + (h0 + p) * s_head);
+                own[p][c] = row[ch];
+                if (g.layout == RTN_ROTARY_HALF && ch < 2 * hch) other[p][c] = row[ch < hch ? ch + hch : ch - hch];
+            }
+        }
+
+    int64_t pos = 0;
+    const bool pos_ok = !live || g.R == 0 || token_position(g, t, pos);
+    if (!pos_ok && lane_g == 0) atomicOr(g.status, kStatusBadIndex);
+    float cs[CH][V], sn[CH][V], wo[CH][V], wp[CH][V];        // per element: cosine, signed sine, weight, partner's weight
+    #pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int ch = lane_g + c * 32;
+        const bool rot = live && ch < 2 * hch && pos_ok;
+        const float* row = g.table + pos * g.R;
+        const int pch = ch < hch ? ch + hch : ch - hch;
+        #pragma unroll
+        for (int e = 0; e < V; ++e) { cs[c][e] = 1.f; sn[c][e] = 0.f; wo[c][e] = 1.f; wp[c][e] = 1.f; }
+        if (rot) {
+            #pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const bool half = g.layout == RTN_ROTARY_HALF;
+                const int f = half ? (ch < hch ? ch : ch - hch) * V + e : ch * (V / 2) + e / 2;
+                const bool second = half ? ch >= hch : (e & 1);
+                cs[c][e] = __ldg(row + f);
+                const float s = __ldg(row + g.R / 2 + f);
+                sn[c][e] = second ? s : -s;
+            }
+        }
+        if (w != nullptr && ch < nch) {
+            #pragma unroll
+            for (int e = 0; e < V; ++e) wo[c][e] = __ldg(w + ch * V + e);
+            if (g.layout == RTN_ROTARY_HALF && ch < 2 * hch) {
+                #pragma unroll
+                for (int e = 0; e < V; ++e) wp[c][e] = __ldg(w + pch * V + e);
+            }
+        }
+    }
+    #pragma unroll
+    for (int p = 0; p < HP; ++p) {
+        float x[CH][V];
+        float ss = 0.f;
+        #pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            Vec16<T>::unpack(own[p][c], x[c]);
+            #pragma unroll
+            for (int e = 0; e < V; ++e) ss = fmaf(x[c][e], x[c][e], ss);
+        }
+        float r = 1.f;
+        if (w != nullptr) {
+            for (int d = G / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+            r = 1.f / sqrtf(ss / (float)g.D + g.eps);
+        }
+        if (!pos_ok) r = __int_as_float(0x7fffffff);             // a position outside the table: NaN, never a wrong angle
+        #pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int ch = lane_g + c * 32;
+            if (!live || h0 + p >= H || ch >= nch) continue;
+            float o[V], y[V];
+            if (g.layout == RTN_ROTARY_HALF) {
+                Vec16<T>::unpack(other[p][c], o);
+                #pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = fmaf(x[c][e] * wo[c][e], cs[c][e], o[e] * wp[c][e] * sn[c][e]) * r;
+            } else {
+                const bool rot = ch < 2 * hch;           // past the rotated part the neighbour's value stays out of it
+                #pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float o = rot ? x[c][e ^ 1] * wo[c][e ^ 1] : 0.f;
+                    y[e] = fmaf(x[c][e] * wo[c][e], cs[c][e], o * sn[c][e]) * r;
+                }
+            }
+            reinterpret_cast<uint4*>(dst + (h0 + p) * d_head)[ch] = Vec16<T>::pack(y);
+        }
+    }
+}
+
+// Any head dimension, stride and alignment: a warp per (token, head), the head staged in shared memory as fp32.
+template <typename T>
+__global__ void __launch_bounds__(kGenericWarps * 32)
+qk_norm_rotary_generic_kernel(const RotaryArgs g)
+{
+    __shared__ float stage[kGenericWarps][kRotaryMaxDim];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float* x = stage[warp];
+    const int heads = g.Hq + g.Hk, half = g.R / 2;
+    const int64_t item = (int64_t)blockIdx.x * kGenericWarps + warp;
+    if (item >= g.T * heads) return;
+    const int64_t t = item / heads;
+    int h = (int)(item - t * heads);
+    const bool is_q = h < g.Hq;
+    if (!is_q) h -= g.Hq;
+    const T* src = static_cast<const T*>(is_q ? g.q : g.k) + t * (is_q ? g.q_token : g.k_token) + h * (is_q ? g.q_head : g.k_head);
+    T* dst = static_cast<T*>(is_q ? g.out_q : g.out_k) + t * (is_q ? g.oq_token : g.ok_token) + h * (is_q ? g.oq_head : g.ok_head);
+    const float* w = is_q ? g.q_weight : g.k_weight;
+    float ss = 0.f;
+    for (int e = lane; e < g.D; e += 32) {
+        const float v = to_f32(src[e]);
+        x[e] = v;
+        ss = fmaf(v, v, ss);
+    }
+    #pragma unroll
+    for (int d = 16; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);      // also orders the stores to x before the reads
+    __syncwarp();
+    int64_t pos = 0;
+    const bool pos_ok = g.R == 0 || token_position(g, t, pos);
+    if (!pos_ok && lane == 0) atomicOr(g.status, kStatusBadIndex);
+    float r = w != nullptr ? 1.f / sqrtf(ss / (float)g.D + g.eps) : 1.f;
+    if (!pos_ok) r = __int_as_float(0x7fffffff);
+    const float* row = g.table + (pos_ok ? pos : 0) * g.R;
+    for (int e = lane; e < g.D; e += 32) {
+        float y = x[e] * (w != nullptr ? w[e] : 1.f);
+        if (e < g.R && pos_ok) {
+            const bool is_half = g.layout == RTN_ROTARY_HALF;
+            const int f = is_half ? (e < half ? e : e - half) : e >> 1;
+            const bool second = is_half ? e >= half : (e & 1);
+            const int pe = is_half ? (second ? e - half : e + half) : e ^ 1;
+            const float o = x[pe] * (w != nullptr ? w[pe] : 1.f);
+            const float s = row[half + f];
+            y = fmaf(y, row[f], second ? o * s : -o * s);
+        }
+        dst[e] = from_f32<T>(y * r);
+    }
+}
+
+// Row p of the table: cos(p f_i) and sin(p f_i), i < R/2, times the amplitude; angles in double (p f_i passes 2^24).
+//   f_i = base^(-2i/R);  LINEAR: f_i / factor;  BASE: base * factor^(R/(R-2)) in place of base;
+//   PARTS: by the turns f_i makes over the original context, f_i above `high`, f_i / factor below `low`, a ramp between
+__global__ void rotary_table_kernel(float* __restrict__ table, int64_t rows, int R, double base, int kind, double factor,
+                                    double original, double low, double high, double amplitude)
+{
+    const int half = R / 2;
+    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= rows * half) return;
+    const int64_t p = i / half;
+    const int j = (int)(i - p * half);
+    if (kind == RTN_ROTARY_SCALE_BASE) base *= pow(factor, (double)R / (double)(R - 2));
+    double f = exp2(-2.0 * (double)j / (double)R * log2(base));
+    if (kind == RTN_ROTARY_SCALE_LINEAR) f /= factor;
+    if (kind == RTN_ROTARY_SCALE_PARTS) {
+        const double turns = original * f / 6.283185307179586476925;
+        double keep = (turns - low) / (high - low);
+        keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+        f = f * (keep + (1.0 - keep) / factor);
+    }
+    double s, c;
+    sincos((double)p * f, &s, &c);
+    table[p * R + j] = (float)(amplitude * c);
+    table[p * R + half + j] = (float)(amplitude * s);
+}
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+template <typename T, int CH, int HP>
+cudaError_t launch_vec(const RotaryArgs& g, int G, cudaStream_t s)
+{
+    const int gq = (g.Hq + HP - 1) / HP, gk = (g.Hk + HP - 1) / HP;
+    const int64_t items = g.T * (gq + gk), per_cta = kThreads / G;
+    qk_norm_rotary_kernel<T, CH, HP><<<(unsigned)((items + per_cta - 1) / per_cta), kThreads, 0, s>>>(g, G, gq, gk);
+    return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_typed(const RotaryArgs& g, cudaStream_t s)
+{
+    constexpr int V = Vec16<T>::N;
+    // 16-byte path: whole chunks in the head and in each half of its rotated part, every row on a 16-byte boundary
+    const int64_t strides = g.q_token | g.q_head | g.k_token | g.k_head | g.oq_token | g.oq_head | g.ok_token | g.ok_head;
+    const bool vec = g.D % V == 0 && (g.R / 2) % V == 0 && strides % V == 0 && g.D / V <= 64 && aligned16(g.q) &&
+                     aligned16(g.k) && aligned16(g.out_q) && aligned16(g.out_k);
+    if (!vec) {
+        const int64_t items = g.T * (g.Hq + g.Hk);
+        qk_norm_rotary_generic_kernel<T><<<(unsigned)((items + kGenericWarps - 1) / kGenericWarps), kGenericWarps * 32, 0, s>>>(g);
+        return cudaGetLastError();
+    }
+    const int nch = g.D / V;
+    int G = 1;
+    while (G < nch && G < 32) G *= 2;
+    if (nch > 32) return launch_vec<T, 2, 1>(g, G, s);
+    // several heads per group once one head each would fill the machine many times over
+    const int64_t warps = g.T * (g.Hq + g.Hk) * G / 32;
+    return warps > (int64_t)device_sm_count() * 128 ? launch_vec<T, 1, 4>(g, G, s) : launch_vec<T, 1, 1>(g, G, s);
+}
+
+}  // namespace
+
+cudaError_t launch_qk_norm_rotary(const RotaryArgs& g, cudaStream_t s)
+{
+    return with_dtype(g.dtype, [&](auto t) { return launch_typed<decltype(t)>(g, s); });
+}
+
+cudaError_t launch_rotary_table(float* table, int64_t rows, int R, double base, int kind, double factor, double original,
+                                double low, double high, double amplitude, cudaStream_t s)
+{
+    const int64_t n = rows * (R / 2);
+    rotary_table_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(table, rows, R, base, kind, factor, original, low, high, amplitude);
+    return cudaGetLastError();
+}
+
+}  // namespace rtn

@@ -1,0 +1,478 @@
+"""The layer operators on the GPU against their plain forms in double: types, layouts, odd sizes, strides, refusals."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1912_02057_b200 as rtn
+import layer_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+ids = lambda v: str(v).replace("torch.", "").replace(" ", "")  # noqa: E731
+
+
+def cuda(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+# ---------------------------------------------------------------------------------------------- linear
+
+def linear_case(M, N, K, seed, per_row=True):
+    g = np.random.default_rng(seed)
+    x, w = (g.choice(np.array([-1, 0, 1], np.int8), size=s, p=[0.3, 0.4, 0.3]) for s in ((M, K), (N, K)))
+    na, nw = (M, N) if per_row else (1, 1)
+    d = dict(x=x, w=w, a_scale=g.uniform(0.5, 1.5, na).astype(np.float32), a_offset=g.uniform(-0.1, 0.1, na).astype(np.float32),
+             w_scale=(g.uniform(0.5, 1.5, nw) / np.sqrt(K)).astype(np.float32),
+             w_offset=(g.uniform(-0.1, 0.1, nw) / np.sqrt(K)).astype(np.float32),
+             bias=g.normal(size=N).astype(np.float32), residual=g.normal(size=(M, N)).astype(np.float32))
+    return d
+
+
+def packed(d):
+    one = torch.tensor([0.5], device="cuda")
+    xp, xs = rtn.rtn_ternarize_pack_act(cuda(d["x"]).float(), -one, one)
+    wp, ws = rtn.rtn_pack_weights(cuda(d["w"]))
+    return (xp, xs, wp, ws[0].contiguous(), d["x"].shape[0], d["w"].shape[0], d["x"].shape[1],
+            *(cuda(d[n]) for n in ("a_scale", "a_offset", "w_scale", "w_offset")))
+
+
+# fp32 roundings: four terms of the affine form (each a product or two and a sum), the bias, the activation (its slope is
+# at most 1.13, its own error a few units), the residual
+LINEAR_C = 24
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("shape", [(1, 1, 1), (1, 64, 64), (1, 4096, 4096), (1, 100, 129), (2, 33, 640), (3, 257, 127), (5, 130, 4100),
+                                   (8, 1000, 512), (9, 70, 300), (9, 24, 4224), (17, 16, 128), (33, 520, 257), (130, 1000, 512),
+                                   (257, 300, 384), (300, 77, 1000), (520, 640, 256), (1100, 528, 130)], ids=ids)
+def test_linear_matches_the_plain_form(shape, dtype):
+    M, N, K = shape
+    for n, (kind, bias, residual, per_row) in enumerate([(0, False, False, True), (1, True, True, False), (2, True, False, True),
+                                                         (3, False, True, True), (4, True, True, True)]):
+        d = linear_case(M, N, K, 100 + n, per_row)
+        r = cuda(d["residual"], dtype) if residual else None
+        out = rtn.rtn_ternary_linear(*packed(d), bias=cuda(d["bias"]) if bias else None, activation=kind, residual=r, dtype=dtype)
+        want, mag = ref.linear(d["x"], d["w"], d["a_scale"], d["a_offset"], d["w_scale"], d["w_offset"],
+                               d["bias"] if bias else None, kind, ref.f64(r) if residual else None)
+        assert out.dtype == dtype
+        ref.assert_close(out, want, mag, LINEAR_C, f"{shape} act {kind}")
+    assert rtn.rtn_last_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("shape", [(3, 70, 200), (200, 304, 200), (150, 77, 130)], ids=ids)
+def test_linear_strided_unaligned_and_in_place(shape, dtype):
+    M, N, K = shape
+    d = linear_case(M, N, K, 7)
+    args = packed(d)
+    for offset, stride in ((0, N + 5), (1, N + 3), (0, (N + 63) // 32 * 32)):
+        wide = torch.full((M * stride + 8,), 7.0, dtype=dtype, device="cuda")
+        out = wide[offset:offset + M * stride].view(M, stride)[:, :N]
+        out.copy_(cuda(d["residual"]))
+        want, mag = ref.linear(d["x"], d["w"], d["a_scale"], d["a_offset"], d["w_scale"], d["w_offset"], d["bias"], 4, ref.f64(out))
+        got = rtn.rtn_ternary_linear(*args, bias=cuda(d["bias"]), activation=rtn.ACT_SILU, residual=out, out=out)
+        assert got is out
+        ref.assert_close(out, want, mag, LINEAR_C, f"in place, offset {offset}, stride {stride}")
+        rest = wide.clone()
+        rest[offset:offset + M * stride].view(M, stride)[:, :N] = 7.0
+        assert bool((rest == 7.0).all()), "wrote outside its rows"
+    # one row of a residual for all rows (stride 0)
+    row = cuda(d["residual"][:1], dtype)
+    got = rtn.rtn_ternary_linear(*args, residual=row.expand(M, N), dtype=dtype)
+    want, mag = ref.linear(d["x"], d["w"], d["a_scale"], d["a_offset"], d["w_scale"], d["w_offset"], None, 0, ref.f64(row))
+    ref.assert_close(got, want, mag, LINEAR_C, "broadcast residual")
+
+
+@pytest.mark.parametrize("shape", [(64, 64, 576), (300, 200, 700), (600, 520, 256)], ids=ids)
+def test_linear_without_extras_is_the_gemm(shape):
+    d = linear_case(*shape, 3)
+    args = packed(d)
+    a = rtn.rtn_ternary_linear(*args)
+    b = rtn.rtn_ternary_gemm(*args, variant=rtn.VARIANT_I8)
+    assert torch.equal(a, b)
+
+
+def test_linear_special_values_pass_through():
+    d = linear_case(4, 40, 64, 5)
+    bias = d["bias"].copy()
+    bias[:4] = [np.inf, -np.inf, np.nan, 0]
+    for M in (4, 40):
+        d = linear_case(M, 40, 64, 5)
+        for kind in range(5):
+            y = rtn.rtn_ternary_linear(*packed(d), bias=cuda(bias), activation=kind).cpu().numpy()
+            assert np.all(y[:, 0] == np.inf) and np.isnan(y[:, 2]).all() and np.isfinite(y[:, 3:]).all(), kind
+            assert np.all(y[:, 1] == (-np.inf if kind == 0 else 0)) or kind in (2, 3, 4), kind
+
+
+# ---------------------------------------------------------------------------------------------- norm and rotation
+
+# fp32 roundings: the sum of squares (a tree over at most 64 partial sums of 8 or 16, halved by the root), the root, the quotient, weight
+# and rotation
+ROTARY_C = 40
+
+
+def rotary_run(T, Hq, Hk, D, R, layout, norm, dtype, seed=0, positions=True, view=lambda q, k: (q, k), in_place=False):
+    g = np.random.default_rng(seed)
+    P = 500
+    q0, k0 = g.normal(size=(T, Hq, D)) * 2, g.normal(size=(T, max(Hk, 1), D))
+    q, k = view(cuda(q0.astype(np.float32), dtype), cuda(k0.astype(np.float32), dtype))
+    k = k if Hk else None
+    table = rtn.rtn_rotary_table(P, R, 500.0) if R else None
+    pos = g.integers(0, P, T) if positions else np.arange(T)
+    qw, kw = (g.normal(1, 0.3, D).astype(np.float32), g.normal(1, 0.3, D).astype(np.float32)) if norm else (None, None)
+    tab = None if table is None else ref.f64(table)
+    wants = [ref.rotary(ref.f64(x), pos, tab, w, 1e-5, layout) if x is not None else None for x, w in ((q, qw), (k, kw))]
+    outs = rtn.rtn_qk_norm_rotary(q, k, cuda(pos) if positions else None, table, q_weight=None if qw is None else cuda(qw),
+                                  k_weight=None if kw is None or k is None else cuda(kw), eps=1e-5, layout=layout,
+                                  out_q=q if in_place else None, out_k=k if in_place else None)
+    assert not in_place or (outs[0] is q and outs[1] is k)
+    for name, got, want in zip("qk", outs, wants):
+        if want is not None:
+            ref.assert_close(got, *want, ROTARY_C, name)
+    assert rtn.rtn_last_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("layout", [rtn.ROTARY_HALF, rtn.ROTARY_INTERLEAVED], ids=["half", "interleaved"])
+@pytest.mark.parametrize("dims", [(1, 1, 1, 64, 64), (7, 8, 2, 128, 128), (33, 5, 3, 128, 64), (3, 4, 4, 256, 256), (5, 3, 1, 96, 96),
+                                  (4, 2, 2, 80, 48), (6, 3, 2, 50, 50), (2, 2, 1, 7, 6), (3, 2, 0, 128, 32), (2, 1, 1, 1000, 16),
+                                  (2500, 32, 8, 128, 128)], ids=ids)
+@pytest.mark.parametrize("norm", [True, False], ids=["norm", "plain"])
+def test_norm_and_rotation_match_the_plain_form(dims, layout, norm, dtype):
+    rotary_run(*dims, layout, norm, dtype, positions=dims[0] > 3 or dims[0] == 1)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("D", [128, 37])
+def test_norm_alone(D, dtype):
+    rotary_run(9, 3, 2, D, 0, rtn.ROTARY_HALF, True, dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("D,R,extra", [(128, 128, 0), (128, 64, 0), (64, 64, 3), (128, 128, 1)])
+@pytest.mark.parametrize("layout", [rtn.ROTARY_HALF, rtn.ROTARY_INTERLEAVED], ids=["half", "interleaved"])
+def test_rotation_in_place_on_columns_of_a_projection(D, R, extra, layout, dtype):
+    def view(q, k):
+        T, Hq, _ = q.shape
+        Hk = k.shape[1]
+        wide = torch.zeros(T, (Hq + 2 * Hk) * D + extra, dtype=dtype, device="cuda")
+        a, b = wide[:, extra:extra + Hq * D].unflatten(1, (Hq, D)), wide[:, extra + Hq * D:extra + (Hq + Hk) * D].unflatten(1, (Hk, D))
+        a.copy_(q), b.copy_(k)
+        return a, b
+    rotary_run(70, 6, 2, D, R, layout, True, dtype, view=view, in_place=True)
+    head_major = lambda q, k: (q.transpose(0, 1).contiguous().transpose(0, 1), k.transpose(0, 1).contiguous().transpose(0, 1))  # noqa: E731
+    rotary_run(70, 6, 2, D, R, layout, False, dtype, view=head_major, in_place=True)
+
+
+def test_rotation_keeps_what_lies_past_it():
+    """A non-finite value past the rotated part, or in another pair, stays where it is."""
+    for layout in (rtn.ROTARY_HALF, rtn.ROTARY_INTERLEAVED):
+        for D, R in ((128, 64), (20, 12)):
+            q = torch.randn(3, 2, D, device="cuda")
+            q[1, 1, R + 1], q[2, 0, R + 2] = float("inf"), float("nan")
+            out, _ = rtn.rtn_qk_norm_rotary(q, None, None, rtn.rtn_rotary_table(8, R), layout=layout)
+            bad = ~torch.isfinite(out)
+            assert bad.sum() == 2 and bool(bad[1, 1, R + 1]) and bool(bad[2, 0, R + 2])
+
+
+def test_a_position_outside_the_table_is_reported():
+    for D, T in ((64, 4), (30, 4)):
+        q = torch.ones(T, 2, D, device="cuda")
+        table = rtn.rtn_rotary_table(10, D)
+        for wrong in (10, -1, 1 << 40):
+            pos = torch.tensor([3, wrong, 9, 0], device="cuda")
+            out, _ = rtn.rtn_qk_norm_rotary(q, None, pos, table)
+            assert torch.isnan(out[1]).all() and torch.isfinite(out[[0, 2, 3]]).all()
+            assert rtn.rtn_last_device_status() == 8 and rtn.rtn_last_device_status() == 0
+
+
+@pytest.mark.parametrize("kind", [rtn.ROTARY_SCALE_NONE, rtn.ROTARY_SCALE_LINEAR, rtn.ROTARY_SCALE_BASE, rtn.ROTARY_SCALE_PARTS])
+def test_rotary_table(kind):
+    R, base, factor, context, low, high, amplitude = 64, 10000.0, 8.0, 4096.0, 1.0, 32.0, 1.2
+    rows = 70001
+    got = ref.f64(rtn.rtn_rotary_table(rows, R, base, kind, factor, context, low, high, amplitude))
+    i = np.arange(R // 2)
+    f = base ** (-2.0 * i / R)
+    if kind == rtn.ROTARY_SCALE_LINEAR:
+        f = f / factor
+    if kind == rtn.ROTARY_SCALE_BASE:
+        f = (base * factor ** (R / (R - 2))) ** (-2.0 * i / R)
+    if kind == rtn.ROTARY_SCALE_PARTS:
+        keep = np.clip((context * f / (2 * np.pi) - low) / (high - low), 0, 1)
+        f = f * (keep + (1 - keep) / factor)
+    angle = np.arange(rows)[:, None] * f
+    want = amplitude * np.concatenate([np.cos(angle), np.sin(angle)], 1)
+    # angles in double: a few units of 2^-53 times up to 70001 turns of argument, then one rounding to fp32
+    assert np.abs(got - want).max() <= amplitude * (2.0 ** -24 + 70001 * 16 * 2.0 ** -53)
+
+
+# ---------------------------------------------------------------------------------------------- decay attention
+
+def decay_case(lens, H, Hk, Dk, Dv, dtype, seed=0, gap=0, log_decay=None):
+    g = np.random.default_rng(seed)
+    T = sum(lens)
+    make = lambda h, d: cuda(g.normal(size=(T, h, d)).astype(np.float32), dtype)  # noqa: E731
+    q, k, v = make(H, Dk), make(Hk, Dk), make(Hk, Dv)
+    if log_decay is None:
+        log_decay = np.log1p(-np.exp2(-2.0 - 6.0 * np.arange(H) / H)).astype(np.float32)
+    start = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    return q, k, v, log_decay, start
+
+
+def decay_check(lens, H, Hk, Dk, Dv, dtype, fresh, seed=0, log_decay=None, scale=None, view=lambda *x: x):
+    q, k, v, log_decay, start = decay_case(lens, H, Hk, Dk, Dv, dtype, seed, log_decay=log_decay)
+    q, k, v = view(q, k, v)
+    g = np.random.default_rng(seed + 1)
+    state = None if fresh else g.normal(size=(len(lens), H, Dk, Dv)).astype(np.float32)
+    s = Dk ** -0.5 if scale is None else scale
+    want, mag, end, mag_end = ref.decay(ref.f64(q), ref.f64(k), ref.f64(v), log_decay, start, state, s)
+    out, got = rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), max(lens), state=None if fresh else cuda(state), scale=scale)
+    c = ref.decay_roundings(log_decay, max(lens), Dk)
+    # the tensor-core form rounds scores and states to pairs of bf16 (2^-17 relative) on their way to an output
+    ref.assert_close(out, want, mag, c, "out", extra=2.0 ** -15 if dtype == torch.bfloat16 else 0.0)
+    ref.assert_close(got, end, mag_end, c, "state")
+    assert rtn.rtn_last_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("fresh", [True, False], ids=["fresh", "state"])
+@pytest.mark.parametrize("lens,H,Hk,Dk,Dv", [
+    ([1], 1, 1, 64, 64), ([0, 5, 0], 2, 1, 64, 64), ([127, 1, 128, 129], 2, 2, 64, 64), ([300, 17], 4, 2, 128, 128),
+    ([256], 3, 1, 128, 128), ([640], 2, 2, 128, 128), ([65, 2], 2, 1, 128, 64), ([140], 2, 2, 64, 128), ([33, 64], 2, 2, 96, 80),
+    ([20], 3, 3, 7, 5), ([40, 3], 2, 1, 256, 256), ([130], 1, 1, 32, 200)], ids=ids)
+def test_decay_attention_matches_the_recurrence(lens, H, Hk, Dk, Dv, fresh, dtype):
+    decay_check(lens, H, Hk, Dk, Dv, dtype, fresh)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids)
+@pytest.mark.parametrize("D", [64, 128])
+def test_one_long_prompt(D, dtype):
+    decay_check([5001], 2, 1, D, D, dtype, False)
+
+
+@pytest.mark.parametrize("value", [0.0, -1e-4, -3.0, -60.0, -400.0, -np.inf])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids)
+def test_decays_from_none_to_all(value, dtype):
+    decay_check([200, 31], 2, 2, 64, 64, dtype, False, log_decay=np.array([value, -0.01], np.float32), scale=0.3)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids)
+def test_strided_inputs(dtype):
+    def columns(q, k, v):
+        wide = torch.cat([x.flatten(1) for x in (q, k, v)], 1).contiguous()
+        a, b, c = wide.split([x[0].numel() for x in (q, k, v)], 1)
+        return a.unflatten(1, q.shape[1:]), b.unflatten(1, k.shape[1:]), c.unflatten(1, v.shape[1:])
+    head_major = lambda *x: tuple(t.transpose(0, 1).contiguous().transpose(0, 1) for t in x)  # noqa: E731
+    odd = lambda *x: tuple(torch.cat([t.flatten(1), t.flatten(1)[:, :1]], 1)[:, 1:].unflatten(1, t.shape[1:]).copy_(t) for t in x)  # noqa: E731
+    for view in (columns, head_major, odd):
+        decay_check([150, 70], 4, 2, 64, 64, dtype, False, view=view)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids)
+def test_sequences_do_not_reach_each_other(dtype):
+    """NaN and infinities in a neighbour's tokens and state, before and after, change nothing."""
+    lens = [70, 60, 200]
+    q, k, v, log_decay, start = decay_case(lens, 2, 1, 64, 64, dtype)
+    state = torch.randn(3, 2, 64, 64, device="cuda")
+    clean = rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), 200, state=state, state_out=torch.empty_like(state))
+    for x in (q, k, v):
+        x[:70], x[130:] = float("nan"), float("inf")
+    state[0], state[2] = float("nan"), float("inf")
+    out, got = rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), 200, state=state, state_out=torch.empty_like(state))
+    assert torch.equal(out[70:130], clean[0][70:130]) and torch.equal(got[1], clean[1][1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("B,H,Hk,Dk,Dv", [(1, 1, 1, 64, 64), (3, 4, 2, 128, 128), (40, 16, 4, 128, 128), (2, 2, 2, 7, 5), (5, 3, 1, 96, 200),
+                                          (2, 2, 1, 256, 256), (300, 2, 2, 64, 64)], ids=ids)
+def test_step_matches_the_recurrence(B, H, Hk, Dk, Dv, dtype):
+    q, k, v, log_decay, start = decay_case([1] * B, H, Hk, Dk, Dv, dtype)
+    g = np.random.default_rng(9)
+    pool = B + 3
+    slots = g.permutation(pool)[:B].astype(np.int32)
+    state = g.normal(size=(pool, H, Dk, Dv)).astype(np.float32)
+    want, mag, end, mag_end = ref.decay(ref.f64(q), ref.f64(k), ref.f64(v), log_decay, start, state[slots], Dk ** -0.5)
+    c = ref.decay_roundings(log_decay, 1, Dk)
+    device = cuda(state)
+    out, got = rtn.rtn_decay_attention_step(q, k, v, cuda(log_decay), device, slots=cuda(slots))          # in place
+    assert got is device
+    ref.assert_close(out, want, mag, c, "out")
+    ref.assert_close(got[torch.from_numpy(slots).long().cuda()], end, mag_end, c, "state")
+    others = np.setdiff1d(np.arange(pool), slots)
+    assert np.array_equal(got.cpu().numpy()[others], state[others])
+    # no state yet, states in order
+    want, mag, end, mag_end = ref.decay(ref.f64(q), ref.f64(k), ref.f64(v), log_decay, start, None, Dk ** -0.5)
+    out, got = rtn.rtn_decay_attention_step(q, k, v, cuda(log_decay), None)
+    ref.assert_close(out, want, mag, c, "out, fresh")
+    ref.assert_close(got, end, mag_end, c, "state, fresh")
+    assert rtn.rtn_last_device_status() == 0
+
+
+def test_padding_entries_and_bad_slots():
+    B, H, D = 4, 2, 64
+    for dtype in (torch.float32, torch.bfloat16):
+        q, k, v, log_decay, start = decay_case([1] * B, H, H, D, D, dtype)
+        state = torch.randn(6, H, D, D, device="cuda")
+        keep = state.clone()
+        for call in ("step", "prompt"):
+            run = (lambda slots, out: rtn.rtn_decay_attention_step(q, k, v, cuda(log_decay), state, slots=slots, out=out)) if call == "step" else \
+                (lambda slots, out: rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), 1, state=state, slots=slots, out=out))
+            state.copy_(keep)
+            out = torch.full((B, H, D), 5.0, dtype=dtype, device="cuda")
+            run(torch.tensor([2, -1, 5, -7], dtype=torch.int32, device="cuda"), out)
+            assert bool((out[[1, 3]] == 0).all()) and bool((out[[0, 2]] != 5).any())
+            assert torch.equal(state[[0, 1, 3, 4]], keep[[0, 1, 3, 4]]) and not torch.equal(state[2], keep[2])
+            assert rtn.rtn_last_device_status() == 0
+            state.copy_(keep)
+            run(torch.tensor([2, 6, 0, 1], dtype=torch.int32, device="cuda"), out)
+            assert rtn.rtn_last_device_status() == 8
+            assert torch.equal(state[[3, 4, 5]], keep[[3, 4, 5]])
+
+
+def test_bad_sequence_bounds_are_reported_and_skipped():
+    for dtype, D in ((torch.float32, 64), (torch.bfloat16, 64), (torch.bfloat16, 128)):
+        q, k, v, log_decay, _ = decay_case([100], 2, 2, D, D, dtype)
+        for start, longest in (([0, 50, 30], 60), ([0, 50, 120], 80), ([0, 90], 80), ([-3, 40], 80)):
+            out, _ = rtn.rtn_decay_attention(q, k, v, cuda(log_decay), torch.tensor(start, dtype=torch.int32, device="cuda"), longest)
+            assert rtn.rtn_last_device_status() == 8, (start, longest)
+        rtn.rtn_decay_attention(q, k, v, cuda(log_decay), torch.tensor([0, 100], dtype=torch.int32, device="cuda"), 100)
+        assert rtn.rtn_last_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids)
+def test_prompt_then_steps_is_the_longer_prompt(dtype):
+    lens, more = [130, 5], 3
+    H, Hk, D = 4, 2, 64
+    q, k, v, log_decay, start = decay_case([n + more for n in lens], H, Hk, D, D, dtype)
+    whole, end = rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), max(lens) + more)
+    head = torch.cat([torch.arange(s, s + n) for s, n in zip(start, lens)]).cuda()
+    first = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    out, state = rtn.rtn_decay_attention(q[head], k[head], v[head], cuda(log_decay), cuda(first), max(lens))
+    tol = 2e-2 if dtype == torch.bfloat16 else 1e-4      # two roundings to the type of values of about 10
+    assert torch.allclose(out.float(), whole[head].float(), rtol=tol, atol=tol)
+    for i in range(more):
+        at = torch.tensor([s + n + i for s, n in zip(start, lens)], device="cuda")
+        out, state = rtn.rtn_decay_attention_step(q[at], k[at], v[at], cuda(log_decay), state)
+        assert torch.allclose(out.float(), whole[at].float(), rtol=tol, atol=tol)
+    assert torch.allclose(state, end, rtol=1e-4, atol=1e-3)
+
+
+def test_state_pool_past_32_bits():
+    H, D = 16, 128
+    slots_n = (1 << 31) // (H * D * D) + 8                 # element offsets pass 2^31
+    pool = torch.empty((slots_n, H, D, D), device="cuda")
+    slots = torch.tensor([slots_n - 1, 3, slots_n - 5], dtype=torch.int32, device="cuda")
+    pool[slots.long()] = torch.randn(3, H, D, D, device="cuda")
+    state = pool[slots.long()].cpu().numpy()
+    q, k, v, log_decay, start = decay_case([1] * 3, H, H, D, D, torch.bfloat16)
+    want, mag, end, mag_end = ref.decay(ref.f64(q), ref.f64(k), ref.f64(v), log_decay, start, state, D ** -0.5)
+    out, _ = rtn.rtn_decay_attention_step(q, k, v, cuda(log_decay), pool, slots=slots)
+    c = ref.decay_roundings(log_decay, 1, D)
+    ref.assert_close(out, want, mag, c, "step")
+    ref.assert_close(pool[slots.long()], end, mag_end, c, "step's state")
+    want, mag, end, mag_end = ref.decay(ref.f64(q), ref.f64(k), ref.f64(v), log_decay, start, pool[slots.long()].cpu().numpy(), D ** -0.5)
+    out, _ = rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), 1, state=pool, slots=slots)
+    ref.assert_close(out, want, mag, c, "prompt", extra=2.0 ** -15)
+    ref.assert_close(pool[slots.long()], end, mag_end, c, "prompt's state")
+
+
+# ---------------------------------------------------------------------------------------------- all of them
+
+def every_operator():
+    """(name, call) of each operator on its own inputs; a call returns its tensors."""
+    d = linear_case(5, 256, 256, 1)
+    small, args = packed(d), packed(linear_case(300, 256, 256, 2))
+    q, k, v, log_decay, start = decay_case([140, 9], 4, 2, 64, 64, torch.bfloat16)
+    table, g, s = rtn.rtn_rotary_table(64, 64), cuda(log_decay), cuda(start)
+    pos = torch.arange(149, device="cuda") % 64
+    w = torch.ones(64, device="cuda")
+    state = torch.randn(149, 4, 64, 64, device="cuda")
+    new = torch.zeros_like(state)
+    return [("linear rows", lambda: [rtn.rtn_ternary_linear(*small, activation=rtn.ACT_GELU, dtype=torch.bfloat16)]),
+            ("linear", lambda: [rtn.rtn_ternary_linear(*args, dtype=torch.bfloat16)]),
+            ("rotary", lambda: list(rtn.rtn_qk_norm_rotary(q, k, pos, table, w, w))),
+            ("prompt", lambda: list(rtn.rtn_decay_attention(q, k, v, g, s, 140))),
+            ("step", lambda: list(rtn.rtn_decay_attention_step(q, k, v, g, state, state_out=new)))]
+
+
+def test_other_streams_and_repeats_give_the_same_bits():
+    for name, call in every_operator():
+        first = [t.clone() for t in call()]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            again = call()
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, again)), name
+
+
+def test_graph_capture():
+    for name, call in every_operator():
+        want = [t.clone() for t in call()]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = call()
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got)), name
+
+
+def test_nothing_to_do():
+    d = linear_case(1, 64, 64, 1)
+    args = list(packed(d))
+    args[0], args[1], args[4] = args[0][:0], args[1][:0], 0
+    args[7], args[8] = args[7][:0], args[8][:0]
+    assert rtn.rtn_ternary_linear(*args, dtype=torch.bfloat16).shape == (0, 64)
+    q = torch.empty(0, 2, 64, device="cuda")
+    out, _ = rtn.rtn_qk_norm_rotary(q, q, None, rtn.rtn_rotary_table(4, 64))
+    assert out.shape == (0, 2, 64)
+    g = torch.zeros(2, device="cuda")
+    out, state = rtn.rtn_decay_attention(q, q, q, g, torch.zeros(1, dtype=torch.int32, device="cuda"), 0)
+    assert out.shape == (0, 2, 64) and state.shape == (0, 2, 64, 64)
+    state = torch.randn(3, 2, 64, 64, device="cuda")
+    want = state.clone()
+    rtn.rtn_decay_attention(q, q, q, g, torch.zeros(4, dtype=torch.int32, device="cuda"), 0, state=state)
+    assert torch.equal(state, want)
+    rtn.rtn_decay_attention_step(q, q, q, g, state[:0])
+    torch.cuda.synchronize()
+    assert rtn.rtn_last_device_status() == 0
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    q = torch.zeros(4, 2, 64, device="cuda")
+    g, start = torch.zeros(2, device="cuda"), torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    table = rtn.rtn_rotary_table(8, 64)
+    for wrong in (lambda: rtn.rtn_qk_norm_rotary(q.double(), q.double(), None, table),
+                  lambda: rtn.rtn_qk_norm_rotary(q, q.half(), None, table),
+                  lambda: rtn.rtn_qk_norm_rotary(q, q, torch.zeros(4, dtype=torch.int32, device="cuda"), table),
+                  lambda: rtn.rtn_qk_norm_rotary(q.cpu(), None, None, table),
+                  lambda: rtn.rtn_qk_norm_rotary(q, None, None, table, q_weight=torch.ones(63, device="cuda")),
+                  lambda: rtn.rtn_qk_norm_rotary(q.transpose(1, 2), None, None, table),
+                  lambda: rtn.rtn_decay_attention(q, q[:3], q, g, start, 4),
+                  lambda: rtn.rtn_decay_attention(q, q, q, g, start.long(), 4),
+                  lambda: rtn.rtn_decay_attention(q, q, q, g[:1], start, 4),
+                  lambda: rtn.rtn_decay_attention(q, q, q, g, start, 4, state=torch.zeros(1, 2, 64, 64, device="cuda").half()),
+                  lambda: rtn.rtn_decay_attention_step(q, q, q, g, torch.zeros(4, 2, 64, 63, device="cuda")),
+                  lambda: rtn.rtn_decay_attention_step(q, q, q, g, None, slots=torch.zeros(4, dtype=torch.int32, device="cuda"))):
+        with pytest.raises(ValueError):
+            wrong()
+    for wrong, code in ((lambda: rtn.rtn_qk_norm_rotary(q, None, None, rtn.rtn_rotary_table(8, 66)), 2),
+                        (lambda: rtn.rtn_rotary_table(8, 63), 2),
+                        (lambda: rtn.rtn_decay_attention(q, q.repeat(1, 2, 1)[:, :3], q.repeat(1, 2, 1)[:, :3], g, start, 4), 2),
+                        (lambda: rtn.rtn_decay_attention_step(q, q, q, g, torch.zeros(3, 2, 64, 64, device="cuda")), 2),
+                        (lambda: rtn.rtn_qk_norm_rotary(q, q, None, table, q_weight=torch.ones(64, device="cuda")), 1)):
+        with pytest.raises(rtn.RtnError) as e:
+            wrong()
+        assert e.value.code == code
+    d = packed(linear_case(4, 64, 64, 1))
+    with pytest.raises(ValueError):
+        rtn.rtn_ternary_linear(*d, out=torch.empty(4, 63, device="cuda"))
+    with pytest.raises(ValueError):
+        rtn.rtn_ternary_linear(*d, bias=torch.zeros(63, device="cuda"))
+    with pytest.raises(rtn.RtnError):
+        rtn.rtn_ternary_linear(*d, activation=9)
