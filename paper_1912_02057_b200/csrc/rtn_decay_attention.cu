@@ -9,6 +9,7 @@
 //   stride.  Bound: the FMA pipe (two FMAs and a product per state element and token).
 #include "rtn_internal.cuh"
 #include "rtn_types.cuh"
+#include "rtn_decay.cuh"
 
 namespace rtn {
 
@@ -111,15 +112,6 @@ constexpr int kRecCols = 32;            // state columns of a CTA, one per lane
 constexpr int kRecWarps = 4;            // each holds a quarter of the rows
 constexpr int kRecTile = 16;            // tokens staged at a time
 
-// First token and length of sequence b; false (with the status bit) where the bounds do not fit.
-__device__ __forceinline__ bool sequence_bounds(const DecayArgs& g, int64_t b, int64_t& first, int64_t& len, int64_t& slot)
-{
-    first = g.start[b];
-    len = (int64_t)g.start[b + 1] - first;
-    slot = g.slot != nullptr ? g.slot[b] : b;
-    return first >= 0 && len >= 0 && len <= g.max_len && first + len <= g.total && slot < g.n_slots;
-}
-
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(kRecCols * kRecWarps)
 decay_recurrent_kernel(const DecayArgs g)
@@ -208,6 +200,11 @@ cudaError_t launch_recurrent_typed(const DecayArgs& g, cudaStream_t s)
 
 cudaError_t launch_decay_attention(const DecayArgs& g, cudaStream_t s)
 {
+    if (decay_chunk_supported(g)) {
+        bool taken = false;
+        const cudaError_t e = launch_decay_chunk(g, s, taken);
+        if (taken) return e;
+    }
     return with_dtype(g.dtype, [&](auto t) { return launch_recurrent_typed<decltype(t)>(g, s); });
 }
 
