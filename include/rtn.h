@@ -228,7 +228,9 @@ rtn_status rtn_quaternary_gemm(const void* a_packed, const void* w_packed, int64
  * Operators of a ternary language-model layer around the packed products (the paper has no counterpart).
  * Common to them: fp32, bf16 and fp16 tensors (arithmetic, norms, sums and states in fp32, one rounding at the
  * end); strides count elements; a call with no tokens (M, T or B of 0) returns RTN_OK and launches nothing; calls
- * only enqueue and can be captured in a graph (after a first call that sets kernel attributes).
+ * only enqueue and can be captured in a graph (after a first call that sets kernel attributes).  Scratch (the operands of a
+ * tensor-core linear layer, the segment states of a long prompt) comes, stream-ordered, from a memory pool per device that the library
+ * makes at the first use and that keeps its memory from call to call.
  * ---------------------------------------------------------------------------------------------- */
 typedef enum { RTN_F32 = 0, RTN_BF16 = 1, RTN_F16 = 2 } rtn_dtype;
 typedef enum { RTN_ACT_NONE = 0, RTN_ACT_RELU = 1, RTN_ACT_GELU = 2 /* erf */, RTN_ACT_GELU_TANH = 3, RTN_ACT_SILU = 4 } rtn_activation;

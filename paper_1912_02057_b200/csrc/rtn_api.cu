@@ -2,6 +2,7 @@
 #include "rtn_internal.cuh"
 #include "rtn_tcgen05.cuh"
 
+#include <atomic>
 #include <limits.h>
 
 namespace {
@@ -58,6 +59,34 @@ rtn_status check_params(const float* s, const float* o, int64_t n, int64_t full)
 
 namespace rtn {
 unsigned* device_status_word() { return status_word(); }
+
+cudaError_t scratch_alloc(void** p, size_t bytes, cudaStream_t s)
+{
+    static std::atomic<cudaMemPool_t> pools[kMaxDevices];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    cudaMemPool_t pool = pools[dev].load(std::memory_order_acquire);
+    if (pool == nullptr) {
+        cudaMemPoolProps props;
+        memset(&props, 0, sizeof(props));
+        props.allocType = cudaMemAllocationTypePinned;
+        props.location.type = cudaMemLocationTypeDevice;
+        props.location.id = dev;
+        e = cudaMemPoolCreate(&pool, &props);
+        if (e != cudaSuccess) return e;
+        uint64_t keep = UINT64_MAX;
+        e = cudaMemPoolSetAttribute(pool, cudaMemPoolAttrReleaseThreshold, &keep);
+        cudaMemPool_t expected = nullptr;
+        if (e != cudaSuccess || !pools[dev].compare_exchange_strong(expected, pool, std::memory_order_acq_rel)) {
+            cudaMemPoolDestroy(pool);               // another thread was first
+            if (e != cudaSuccess) return e;
+            pool = expected;
+        }
+    }
+    return cudaMallocFromPoolAsync(p, bytes, pool, s);
+}
 }
 
 extern "C" {

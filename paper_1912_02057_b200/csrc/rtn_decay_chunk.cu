@@ -9,15 +9,20 @@
 // from memory (Q, K, V) are exact in bf16.  What the kernel computes on the way to a product is split into bf16 terms that
 // are multiplied one after the other into the same accumulator: P and S into two (2^-17 relative, far below the bf16
 // output's own rounding), the decayed V into three (2^-25), because the state it enters is kept and returned in fp32.
+// The tensor core's accumulation rounds towards zero, so what a chunk adds to the state gets an accumulator of its own and is
+// added in registers: accumulated onto the state itself, its 24 products a chunk bent the state by 1.3e-6.
 //
 // A CTA walks the chunks of one (sequence, query head, segment).  Warp roles, coupled by mbarriers:
-//   P   (4 warps)  scores -> P terms, in place in tensor memory (A operand of P V); scales Q S by l^(i+1) before P V adds to it
-//   S   (4 warps)  S^T -> bf16 terms in shared memory (B operand of Q S); scales S^T by l^C; initial and final state
-//   V   (4 warps)  V tile -> decayed, transposed V terms in tensor memory (A operand of the state update), 32 tokens at a time
-//   O   (4 warps)  O -> output rows
-//   one thread loads the K, Q and V tiles by TMA into a ring, one issues every MMA in the order Q S, state, P V, next Q K^T:
+//   P   (8 warps)  scores -> P terms, in place in tensor memory (A operand of P V); scales Q S by l^(i+1) before P V adds to it;
+//                  O -> bf16 rows, staged in the V tile's slot and stored by TMA
+//   S   (8 warps)  the state, in registers (a row of S^T per pair of threads): decays it, adds the chunk's part, writes its terms
+//                  to shared memory (B operand of Q S); initial and final state
+//   V   (8 warps)  V tile -> decayed, transposed V terms in tensor memory (A operand of the state update), 32 tokens at a time
+//   three threads load the Q, K and V tiles by TMA into a ring each, one warp issues every MMA in the order Q S, state, P V, next Q K^T:
 //   the scores' conversion then runs beside Q S and the state update, the state's beside P V and the next scores.
-// Tensor memory (512 columns): S^T | scores, then P | O | two entries of V terms.
+// The conversions are what the kernel spends its issue slots on, with a chain of dependent instructions per value: two warps per
+// role and scheduler hide what one could not.  The state's 64 registers a thread come from the other roles' shares (setmaxnreg).
+// Tensor memory (512 columns): state update | scores, then P | O | two entries of V terms.
 //
 // Rows past a sequence's end belong to its neighbour: K and V rows are zeroed in shared memory before a product reads
 // them (0 * NaN), scores are masked by selection.  Inside a sequence a non-finite value can reach the outputs of up to 127
@@ -32,39 +37,45 @@
 #include "rtn_tensormap.cuh"
 #include "rtn_timeline.cuh"
 
+// Timeline slots (instrumented build only): 0 kernel entry, 1 set-up done, 4 kernel end; chunk c in 4 .. 7 of a CTA, from
+// slot 8 + 20 (c - 4): 0 state update begins, 1 / 2 Q S begins / issued, 3 state update issued, 4 P ready, 5 P V issued,
+// 6 next scores issued (MMA thread); 7 scores ready, 8 P written, 9 Q S ready, 10 Q S scaled; 11 state updated, 12 state
+// terms written; 13 V tile landed, 14 V terms written; 15 O complete, 16 O read, 17 rows stored.
 RTN_TL_DEFINE(decay_chunk)
-#include "rtn_conv_i8_common.cuh"
+#define CHUNK_TL(k) RTN_TL(decay_chunk, c >= 4 && c < 8 ? 8 + 20 * (c - 4) + (k) : -1)
 
 namespace rtn {
 
 namespace {
 
-using conv_detail::wait_or_die;
-
 constexpr int kC = 128;                     // tokens of a chunk
 constexpr int kEntry = 32;                  // tokens of an entry of V terms
-constexpr int kThreads = 18 * 32;
-constexpr int kWarpS = 4, kWarpV = 8, kWarpO = 12, kWarpLoad = 16, kWarpMma = 17;
+constexpr int kThreads = 28 * 32;
+constexpr int kWarpLoadQ = 0, kWarpMma = 1, kWarpLoadK = 2 /* V: 3 */, kWarpS = 4, kWarpP = 12, kWarpV = 20;
+// registers a thread: 72 at launch; 40 + 2 x (96 + 72 + 56) = 488 <= 7 x 72 per warp group of 128
+constexpr int kRegsRest = 40, kRegsS = 96, kRegsP = 72, kRegsV = 56;
 constexpr uint32_t kColS = 0, kColP = 128, kColO = 256, kColV = 384, kTmemCols = 512;
-constexpr int kMaxSlots = 9;
 
 template <int D> struct Layout {
-    static constexpr int kSlots = D == 128 ? 5 : 9;             // ring of K, Q, V tiles
+    // Slots of the three rings.  A Q tile lives from its scores to Q S, a K tile to the end of the state update, a V tile from its
+    // conversion to the store of the rows that are staged in its slot.
+    static constexpr int kSlotsQ = D == 128 ? 1 : 3, kSlotsK = D == 128 ? 2 : 3, kSlotsV = D == 128 ? 2 : 3;
+    static constexpr int kSlots = kSlotsQ + kSlotsK + kSlotsV;
     static constexpr uint32_t kTile = kC * D * 2;
     static constexpr uint32_t kHalf = kC * 128;                 // 64 columns of a tile
     static constexpr uint32_t kState = D * D * 2;               // one bf16 term of S^T
     static constexpr uint32_t off_state = kSlots * kTile;
     static constexpr uint32_t off_table = off_state + 2 * kState;
-    static constexpr uint32_t off_bar = off_table + kC * 4;
+    static constexpr uint32_t off_bar = off_table + (kC + 32 + kC) * 4;
     static constexpr uint32_t kBytes = off_bar + 512 + 1024;    // and room to start on a 1024-byte boundary
 };
 
 struct Bars {
-    uint64_t full[kMaxSlots], empty[kMaxSlots];     // tiles: load -> users, MMA -> load
+    uint64_t full[9], empty[9];                     // tiles: load -> users, last user -> load
     uint64_t sc_full, p_full, qs_done;              // scores ready; P ready and Q S scaled; Q S in the accumulator
-    uint64_t s_full, kv_done;                       // state terms ready and S^T scaled; state updated
+    uint64_t s_full, kv_done, d_free;               // state terms ready; a chunk's addition to the state complete; read
     uint64_t vt_full[2], vt_empty[2];               // V terms
-    uint64_t o_full, o_empty;                       // O complete; O read
+    uint64_t o_full, o_empty, o_staged;             // O complete; O read; rows staged
     uint64_t fixed;                                 // rows past the end zeroed
     uint32_t tmem_slot;
     int dead;
@@ -76,6 +87,8 @@ struct ChunkPlan {
     int segments;           // of the longest sequence
     float* local;           // [B][H][segments - 1][D][D]: what a segment adds to the state
 };
+
+constexpr uint32_t kTries = 1u << 22;       // of a wait before it gives up
 
 // l^n from log2 l; n = 0 gives 1 for every l (log2 l may be -inf).
 __device__ __forceinline__ float decay_pow(float g2, float n) { return n == 0.f ? 1.f : exp2f(n * g2); }
@@ -89,17 +102,74 @@ __device__ __forceinline__ void tma_load_tile(uint32_t dst, const CUtensorMap* m
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c), "r"(head), "r"(token), "r"(tc::smem_addr(bar)) : "memory");
 }
 
+__device__ __forceinline__ void tma_store_tile(const CUtensorMap* map, uint32_t src, int c, int head, int token)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c), "r"(head), "r"(token), "r"(src) : "memory");
+}
+
+// Pairs of fp32 values in one 64-bit register: one instruction for both.
+typedef unsigned long long pair_t;
+__device__ __forceinline__ pair_t make_pair(float a, float b)
+{
+    pair_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void take_pair(pair_t p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ pair_t mul_pair(pair_t a, pair_t b)
+{
+    pair_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ pair_t fma_pair(pair_t a, pair_t b, pair_t c)
+{
+    pair_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// The pair rounded to bf16 (packed low / high) and what is left of it.
+__device__ __forceinline__ pair_t split_term(pair_t y, uint32_t& term)
+{
+    float a, b;
+    take_pair(y, a, b);
+    term = pack2<__nv_bfloat16>(a, b);
+    return fma_pair(make_pair(bf16_low(term), bf16_high(term)), make_pair(-1.f, -1.f), y);
+}
+__device__ __forceinline__ uint32_t round_pair(pair_t y)
+{
+    float a, b;
+    take_pair(y, a, b);
+    return pack2<__nv_bfloat16>(a, b);
+}
+// Two bf16 terms of each (16 bits), three (24 bits).
+__device__ __forceinline__ void split2(pair_t y, uint32_t& hi, uint32_t& lo) { lo = round_pair(split_term(y, hi)); }
+__device__ __forceinline__ void split3(pair_t y, uint32_t& hi, uint32_t& mid, uint32_t& lo)
+{
+    lo = round_pair(split_term(split_term(y, hi), mid));
+}
+__device__ __forceinline__ float value(const uint8_t* p) { return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16); }
+__device__ __forceinline__ pair_t as_pair(uint32_t a, uint32_t b) { return make_pair(__uint_as_float(a), __uint_as_float(b)); }
+
+template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
 template <int D, bool kStates>
 __global__ void __launch_bounds__(kThreads, 1)
 decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__ CUtensorMap map_q,
-                   const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
+                   const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                   const __grid_constant__ CUtensorMap map_o)
 {
     using L = Layout<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    float* table = reinterpret_cast<float*>(smem + L::off_table);            // l^(C-1-j)
+    float* table = reinterpret_cast<float*>(smem + L::off_table);            // l^(C-1-j), then 32 zeros, then the last chunk's
     Bars& bar = *reinterpret_cast<Bars*>(smem + L::off_bar);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = warp & 3;
+    // the warp's number by a shuffle: the branches on it are then known to be uniform, and what the MMA warp computes for its
+    // instructions stays in uniform registers
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, quad = warp & 3;
 
     // ---- what this CTA works on
     const int segs = kStates ? p.segments - 1 : p.segments;
@@ -128,347 +198,424 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
     const float g2 = g.log_decay[h] * 1.4426950408889634f;
 
     // ---- set-up
+    RTN_TL_INIT(decay_chunk)
+    if (threadIdx.x == 0) RTN_TL(decay_chunk, 0);
     if (warp == kWarpMma) tc::tmem_alloc(&bar.tmem_slot, kTmemCols);
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kMaxSlots; ++i) { tc::mbar_init(&bar.full[i], 1); tc::mbar_init(&bar.empty[i], 1); }
-        tc::mbar_init(&bar.sc_full, 1); tc::mbar_init(&bar.p_full, 128); tc::mbar_init(&bar.qs_done, 1);
-        tc::mbar_init(&bar.s_full, D); tc::mbar_init(&bar.kv_done, 1);
+        for (int i = 0; i < L::kSlots; ++i) { tc::mbar_init(&bar.full[i], 1); tc::mbar_init(&bar.empty[i], 1); }
+        tc::mbar_init(&bar.sc_full, 1); tc::mbar_init(&bar.p_full, 256); tc::mbar_init(&bar.qs_done, 1);
+        tc::mbar_init(&bar.s_full, 2 * D); tc::mbar_init(&bar.kv_done, 1); tc::mbar_init(&bar.d_free, 2 * D);
         for (int i = 0; i < 2; ++i) { tc::mbar_init(&bar.vt_full[i], D); tc::mbar_init(&bar.vt_empty[i], 1); }
-        tc::mbar_init(&bar.o_full, 1); tc::mbar_init(&bar.o_empty, 128); tc::mbar_init(&bar.fixed, D);
+        tc::mbar_init(&bar.o_full, 1); tc::mbar_init(&bar.o_empty, 256); tc::mbar_init(&bar.o_staged, 256); tc::mbar_init(&bar.fixed, 2 * D);
         tc::mbar_init_fence();
         bar.dead = 0;
     }
-    if (threadIdx.x < kC) table[threadIdx.x] = decay_pow(g2, (float)(kC - 1 - threadIdx.x));
+    if (threadIdx.x < kC) table[kC - 1 - threadIdx.x] = decay_pow(g2, (float)threadIdx.x);
+    else if (threadIdx.x < kC + 32) table[threadIdx.x] = 0.f;
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
-    const uint32_t tmem = bar.tmem_slot;
+    constexpr uint32_t tmem = 0;                // all 512 columns are this CTA's: they begin at 0
+    if (bar.tmem_slot != tmem && threadIdx.x == 0) bar.dead = 1;
+    if (threadIdx.x == 0) RTN_TL(decay_chunk, 1);
     const uint32_t base = tc::smem_addr(smem);
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     volatile int* dead = &bar.dead;
-    auto wait = [&](uint64_t* m, int phase) { return wait_or_die(m, (uint32_t)phase & 1u, g.status, dead); };
-    // whole warps wait together and give up together: what follows is warp-collective
-    auto warp_wait = [&](uint64_t* m, int phase) { return __all_sync(0xffffffffu, wait(m, phase)) != 0; };
-    // tiles in the order K, Q, V of each chunk (K, V where only states are wanted)
-    constexpr int kPer = kStates ? 2 : 3;
-    auto tile_slot = [&](int c, int which) { return (c * kPer + which) % L::kSlots; };
-    auto tile_phase = [&](int c, int which) { return (c * kPer + which) / L::kSlots; };
-    constexpr int kTileK = 0, kTileQ = 1, kTileV = kStates ? 1 : 2;
+    // Bounded waits: one that runs out marks the CTA, which reports it at its end.  Whole warps wait together and give up together
+    // (what follows is warp-collective).
+    auto wait = [&](uint64_t* m, int phase) {
+        const bool ok = tc::mbar_wait_tries(m, (uint32_t)phase & 1u, kTries);
+        if (!ok) *dead = 1;
+        return ok;
+    };
+    auto warp_wait = [&](uint64_t* m, int phase) {
+        const bool ok = __all_sync(0xffffffffu, tc::mbar_wait_tries(m, (uint32_t)phase & 1u, kTries)) != 0;
+        if (!ok) *dead = 1;
+        return ok;
+    };
+    // rings: Q, then K, then V slots
+    enum { kTileQ, kTileK, kTileV };
+    auto slots_of = [](int which) { return which == kTileQ ? L::kSlotsQ : which == kTileK ? L::kSlotsK : L::kSlotsV; };
+    auto tile_slot = [&](int c, int which) {
+        return (which == kTileQ ? 0 : which == kTileK ? L::kSlotsQ : L::kSlotsQ + L::kSlotsK) + c % slots_of(which);
+    };
+    auto tile_phase = [&](int c, int which) { return c / slots_of(which); };
 
-    if (warp == kWarpLoad) {
-        // ------------------------------------------------------------ tiles (one thread)
-        if (lane == 0) {
-            int t = 0;
-            for (; t < chunks * kPer; ++t) {
-                const int s = t % L::kSlots, c = t / kPer, which = t % kPer;
-                if (!wait(&bar.empty[s], t / L::kSlots + 1)) break;
-                const CUtensorMap* map = which == kTileK ? &map_k : which == kTileV ? &map_v : &map_q;
+    if (warp < kWarpS) {
+      regs_down<kRegsRest>();
+      if (warp == kWarpLoadK && lane == 1) {
+        // ------------------------------------------------------------ rows out (one thread)
+        if constexpr (!kStates) {
+            const int stores = tail == kC ? chunks : chunks - 1;              // the last rows of a sequence are stored by their threads
+            for (int c = 0; c < stores; ++c) {
+                const int sv = tile_slot(c, kTileV);
+                if (!wait(&bar.o_staged, c)) break;
+                for (int x = 0; x < D / 64; ++x) tma_store_tile(&map_o, base + sv * L::kTile + x * L::kHalf, x * 64, h, (int)row0 + c * kC);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                tc::mbar_arrive(&bar.empty[sv]);
+            }
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        }
+      } else if (warp != kWarpMma) {
+        // ------------------------------------------------------------ tiles (one thread per ring)
+        const int which = warp == kWarpLoadQ ? kTileQ : warp == kWarpLoadK ? kTileK : kTileV;
+        if (lane == 0 && !(kStates && which == kTileQ)) {
+            const CUtensorMap* map = which == kTileK ? &map_k : which == kTileV ? &map_v : &map_q;
+            int c = 0;
+            for (; c < chunks; ++c) {
+                const int s = tile_slot(c, which);
+                if (!wait(&bar.empty[s], tile_phase(c, which) + 1)) break;
                 tc::mbar_arrive_expect_tx(&bar.full[s], L::kTile);
                 for (int half = 0; half < D / 64; ++half)
-                    tma_load_tile(base + s * L::kTile + half * L::kHalf, map, half * 64, !kStates && which == kTileQ ? h : hk,
+                    tma_load_tile(base + s * L::kTile + half * L::kHalf, map, half * 64, which == kTileQ ? h : hk,
                                   (int)row0 + c * kC, &bar.full[s]);
             }
             // every copy has landed before the CTA ends, also when a wait gave up
-            for (int u = t > L::kSlots ? t - L::kSlots : 0; u < t; ++u) tc::mbar_wait(&bar.full[u % L::kSlots], (uint32_t)(u / L::kSlots) & 1u, g.status);
+            for (int u = c > slots_of(which) ? c - slots_of(which) : 0; u < c; ++u)
+                tc::mbar_wait(&bar.full[tile_slot(u, which)], (uint32_t)tile_phase(u, which) & 1u, g.status);
         }
-    } else if (warp == kWarpMma) {
-        // ------------------------------------------------------------ every MMA (one thread)
-        if (lane == 0) {
+      } else {
+        // ------------------------------------------------------------ every MMA
+        {
+            const uint32_t elected = tc::elect_one();
+            auto commit = [&](uint64_t* m) { if (elected) tc::mma_commit(m); __syncwarp(); };
             constexpr uint32_t id_kk = tc::idesc_bf16(128, kC, false);           // scores
             constexpr uint32_t id_s = tc::idesc_bf16(128, D, false), id_mn = tc::idesc_bf16(128, D, true);
-            auto kmajor = [&](uint32_t tile, uint32_t half_bytes, int step) {
-                return tc::smem_desc_sw128(tile + (uint32_t)(step >> 2) * half_bytes + (uint32_t)(step & 3) * 32u, 16);
+            // descriptors: a tile's own, and constant steps along k on top (addresses count 16 bytes, and stay below 2^14)
+            auto tile_desc = [&](int slot_) { return tc::smem_desc_sw128(base + (uint32_t)slot_ * L::kTile, L::kHalf); };
+            auto kmajor = [](uint64_t desc, uint32_t half_bytes, int step) {
+                return desc + (((uint32_t)(step >> 2) * half_bytes + (uint32_t)(step & 3) * 32u) >> 4);
             };
-            auto mnmajor = [&](uint32_t tile, int step) { return tc::smem_desc_sw128(tile + (uint32_t)step * 2048u, L::kHalf); };
+            auto mnmajor = [](uint64_t desc, int step) { return desc + (((uint32_t)step * 2048u) >> 4); };
+            const uint64_t state_desc = tc::smem_desc_sw128(base + L::off_state, 16);
             auto scores = [&](int c) {
                 const int sk = tile_slot(c, kTileK), sq = tile_slot(c, kTileQ);
-                if (!wait(&bar.full[sk], tile_phase(c, kTileK)) || !wait(&bar.full[sq], tile_phase(c, kTileQ))) return false;
+                if (!warp_wait(&bar.full[sk], tile_phase(c, kTileK)) || !warp_wait(&bar.full[sq], tile_phase(c, kTileQ))) return false;
                 tc::tc_fence_after_sync();
+                const uint64_t dq = tile_desc(sq), dk = tile_desc(sk);
                 #pragma unroll
                 for (int s = 0; s < D / 16; ++s)
-                    tc::mma_f16_ss(tmem + kColP, kmajor(base + sq * L::kTile, L::kHalf, s), kmajor(base + sk * L::kTile, L::kHalf, s), id_kk, s > 0);
-                tc::mma_commit(&bar.sc_full);
+                    tc::mma_f16_ss(elected, tmem + kColP, kmajor(dq, L::kHalf, s), kmajor(dk, L::kHalf, s), id_kk, s > 0);
+                commit(&bar.sc_full);
                 return true;
             };
-            bool alive = chunks == 0 || kStates || scores(0);
+            bool alive = true;
+            if constexpr (!kStates) alive = chunks == 0 || scores(0);
             for (int c = 0; c < chunks && alive; ++c) {
-                const int sk = tile_slot(c, kTileK), sq = tile_slot(c, kTileQ), sv = tile_slot(c, kTileV);
-                if constexpr (!kStates) {
-                    alive = wait(&bar.s_full, c) && (c == 0 || wait(&bar.o_empty, c - 1));
-                    if (!alive) break;
-                    tc::tc_fence_after_sync();
-                    #pragma unroll
-                    for (int term = 0; term < 2; ++term)
-                        #pragma unroll
-                        for (int s = 0; s < D / 16; ++s)
-                            tc::mma_f16_ss(tmem + kColO, kmajor(base + sq * L::kTile, L::kHalf, s),
-                                           kmajor(base + L::off_state + term * L::kState, D * 128, s), id_s, term + s > 0);
-                    tc::mma_commit(&bar.qs_done);
-                    tc::mma_commit(&bar.empty[sq]);
-                } else {
-                    alive = wait(&bar.full[sk], tile_phase(c, kTileK));
-                    if (!alive) break;
-                }
+                const int sk = tile_slot(c, kTileK), sq = kStates ? 0 : tile_slot(c, kTileQ), sv = tile_slot(c, kTileV);
+                const uint64_t dq = tile_desc(sq), dk = tile_desc(sk), dv = tile_desc(sv);
+                if constexpr (kStates) { if (!(alive = warp_wait(&bar.full[sk], tile_phase(c, kTileK)))) break; }
+                if (c > 0 && !(alive = warp_wait(&bar.d_free, c - 1))) break;
                 // the last chunk's rows past the end are zero before a product reads them
-                if (c == chunks - 1 && tail < kC && !(alive = wait(&bar.fixed, 0))) break;
+                if (c == chunks - 1 && tail < kC && !(alive = warp_wait(&bar.fixed, 0))) break;
+                CHUNK_TL(0);
+                // state update by entries; Q S between the second and the third: its own terms may come late, and the V warps
+                // are two entries ahead at most
+                #pragma unroll 1
                 for (int e = 0; e < kC / kEntry && alive; ++e) {
+                    if constexpr (!kStates) {
+                        if (e == 2) {
+                            alive = warp_wait(&bar.s_full, c) && (c == 0 || warp_wait(&bar.o_empty, c - 1));
+                            if (!alive) break;
+                            tc::tc_fence_after_sync();
+                            CHUNK_TL(1);
+                            #pragma unroll 1
+                            for (int term = 0; term < 2; ++term)
+                                #pragma unroll
+                                for (int s = 0; s < D / 16; ++s)
+                                    tc::mma_f16_ss(elected, tmem + kColO, kmajor(dq, L::kHalf, s),
+                                                   kmajor(state_desc + (term * L::kState >> 4), D * 128, s), id_s, term + s > 0);
+                            commit(&bar.qs_done);
+                            commit(&bar.empty[sq]);
+                            CHUNK_TL(2);
+                        }
+                    }
                     const int ve = c * (kC / kEntry) + e;
-                    if (!(alive = wait(&bar.vt_full[ve & 1], ve >> 1))) break;
+                    if (!(alive = warp_wait(&bar.vt_full[ve & 1], ve >> 1))) break;
                     tc::tc_fence_after_sync();
-                    #pragma unroll
+                    #pragma unroll 1
                     for (int term = 0; term < 3; ++term)
                         #pragma unroll
                         for (int s = 0; s < kEntry / 16; ++s)
-                            tc::mma_f16_ts(tmem + kColS, tmem + kColV + (uint32_t)((ve & 1) * 64 + term * 16 + s * 8),
-                                           mnmajor(base + sk * L::kTile, e * (kEntry / 16) + s), id_mn, !kStates || ve + term + s > 0);
-                    tc::mma_commit(&bar.vt_empty[ve & 1]);
+                            tc::mma_f16_ts(elected, tmem + kColS, tmem + kColV + (uint32_t)((ve & 1) * 64 + term * 16 + s * 8),
+                                           mnmajor(dk, e * (kEntry / 16) + s), id_mn, e + term + s > 0);
+                    commit(&bar.vt_empty[ve & 1]);
                 }
                 if (!alive) break;
-                if (!kStates || c == chunks - 1) tc::mma_commit(&bar.kv_done);       // states only: nobody follows the chunks
-                tc::mma_commit(&bar.empty[sk]);
+                CHUNK_TL(3);
+                commit(&bar.kv_done);
+                commit(&bar.empty[sk]);
                 if constexpr (!kStates) {
-                    if (!(alive = wait(&bar.p_full, c))) break;
+                    if (!(alive = warp_wait(&bar.p_full, c))) break;
+                    CHUNK_TL(4);
                     tc::tc_fence_after_sync();
-                    #pragma unroll
+                    #pragma unroll 1
                     for (int term = 0; term < 2; ++term)
                         #pragma unroll
                         for (int s = 0; s < kC / 16; ++s)
-                            tc::mma_f16_ts(tmem + kColO, tmem + kColP + (uint32_t)((s >> 1) * 32 + term * 16 + (s & 1) * 8),
-                                           mnmajor(base + sv * L::kTile, s), id_mn, true);
-                    tc::mma_commit(&bar.o_full);
+                            tc::mma_f16_ts(elected, tmem + kColO, tmem + kColP + (uint32_t)(s * 16 + term * 8),
+                                           mnmajor(dv, s), id_mn, true);
+                    commit(&bar.o_full);
+                    CHUNK_TL(5);
                 }
-                tc::mma_commit(&bar.empty[sv]);
-                if constexpr (!kStates) {
+                if constexpr (kStates) {
+                    commit(&bar.empty[sv]);
+                } else {
                     if (c + 1 < chunks) alive = scores(c + 1);
+                    CHUNK_TL(6);
                 }
             }
         }
-    } else if (warp < kWarpS) {
-        // ------------------------------------------------------------ P: row i of the chunk per thread
+      }
+    } else if (warp >= kWarpP && warp < kWarpV) {
+        // ------------------------------------------------------------ P: row i of the chunk, half of the keys, per thread
         if constexpr (!kStates) {
-            const int i = quad * 32 + lane;
-            float near[16];                                                   // l^(15 - jj)
+            const int i = quad * 32 + lane, half = (warp >> 2) & 1;
+            pair_t near[8];                                                   // l^(15 - x), by pairs
             #pragma unroll
-            for (int jj = 0; jj < 16; ++jj) near[jj] = decay_pow(g2, (float)(15 - jj));
+            for (int x = 0; x < 8; ++x) near[x] = make_pair(table[kC - 16 + 2 * x], table[kC - 15 + 2 * x]);
             const float own = decay_pow(g2, (float)(i + 1));
             for (int c = 0; c < chunks; ++c) {
                 if (!warp_wait(&bar.sc_full, c)) break;
+                if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(7);
                 tc::tc_fence_after_sync();
                 #pragma unroll 1
-                for (int kb = 0; kb < kC / 32; ++kb) {
-                    const uint32_t at = tmem + lanes + kColP + (uint32_t)(kb * 32);
-                    uint32_t v[32], t[32];                                    // t: sixteen words of high terms, sixteen of low
-                    if (kb > quad) {                                          // keys after every row of the warp
+                for (int kb = half * 4; kb < half * 4 + 4; ++kb) {            // 16 keys: eight words of high terms, eight of low
+                    const uint32_t at = tmem + lanes + kColP + (uint32_t)(kb * 16);
+                    const float* w = table + (kC - 1 - i + kb * 16);          // l^(i - key), zero past the diagonal
+                    uint32_t t[16];
+                    if (kb * 16 >= quad * 32 + 32) {                          // keys after every row of the warp
                         #pragma unroll
-                        for (int x = 0; x < 32; ++x) t[x] = 0;
+                        for (int x = 0; x < 16; ++x) t[x] = 0;
                     } else {
-                        tc::tmem_ld32(at, v);
-                        float f0 = 0.f, f1 = 0.f;
-                        if (kb < quad) { f0 = decay_pow(g2, (float)(i - kb * 32 - 15)); f1 = decay_pow(g2, (float)(i - kb * 32 - 31)); }
-                        tc::tmem_ld_wait();
-                        #pragma unroll
-                        for (int x = 0; x < 32; x += 2) {
-                            float y0, y1;
-                            if (kb < quad) {
-                                const float f = x < 16 ? f0 : f1;
-                                y0 = __uint_as_float(v[x]) * (f * near[x & 15]);
-                                y1 = __uint_as_float(v[x + 1]) * (f * near[(x & 15) + 1]);
-                            } else {                                          // the diagonal block: row lane, key x
-                                y0 = x <= lane ? __uint_as_float(v[x]) * decay_pow(g2, (float)(lane - x)) : 0.f;
-                                y1 = x + 1 <= lane ? __uint_as_float(v[x + 1]) * decay_pow(g2, (float)(lane - x - 1)) : 0.f;
+                        uint32_t v[16];
+                        tc::tmem_ld16(at, v);
+                        if (kb * 16 + 16 <= quad * 32) {                      // keys before every row of the warp
+                            const pair_t f = make_pair(w[15], w[15]);
+                            tc::tmem_ld_wait();
+                            #pragma unroll
+                            for (int x = 0; x < 16; x += 2)
+                                split2(mul_pair(as_pair(v[x], v[x + 1]), mul_pair(f, near[x >> 1])), t[x >> 1], t[8 + (x >> 1)]);
+                        } else {                                              // masked by selection: scores there may be anything
+                            const int n = i - kb * 16;
+                            tc::tmem_ld_wait();
+                            #pragma unroll
+                            for (int x = 0; x < 16; x += 2) {
+                                const float y0 = x > n ? 0.f : __uint_as_float(v[x]), y1 = x + 1 > n ? 0.f : __uint_as_float(v[x + 1]);
+                                split2(mul_pair(make_pair(y0, y1), make_pair(w[x], w[x + 1])), t[x >> 1], t[8 + (x >> 1)]);
                             }
-                            const uint32_t hi = pack2<__nv_bfloat16>(y0, y1);
-                            t[x >> 1] = hi;
-                            t[16 + (x >> 1)] = pack2<__nv_bfloat16>(y0 - bf16_low(hi), y1 - bf16_high(hi));
                         }
                     }
-                    tc::tmem_st32(at, t);
+                    tc::tmem_st16(at, t);
                 }
                 tc::tmem_st_wait();
+                if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(8);
                 if (!warp_wait(&bar.qs_done, c)) break;
+                if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(9);
                 tc::tc_fence_after_sync();
                 #pragma unroll 1
-                for (int x0 = 0; x0 < D; x0 += 32) {
-                    uint32_t v[32];
-                    tc::tmem_ld32(tmem + lanes + kColO + (uint32_t)x0, v);
+                for (int x0 = half * (D / 2); x0 < (half + 1) * (D / 2); x0 += 16) {
+                    uint32_t v[16];
+                    tc::tmem_ld16(tmem + lanes + kColO + (uint32_t)x0, v);
                     tc::tmem_ld_wait();
                     #pragma unroll
-                    for (int x = 0; x < 32; ++x) v[x] = __float_as_uint(__uint_as_float(v[x]) * own);
-                    tc::tmem_st32(tmem + lanes + kColO + (uint32_t)x0, v);
+                    for (int x = 0; x < 16; x += 2) {
+                        float a, b2;
+                        take_pair(mul_pair(as_pair(v[x], v[x + 1]), make_pair(own, own)), a, b2);
+                        v[x] = __float_as_uint(a); v[x + 1] = __float_as_uint(b2);
+                    }
+                    tc::tmem_st16(tmem + lanes + kColO + (uint32_t)x0, v);
                 }
                 tc::tmem_st_wait();
                 tc::tc_fence_before_sync();
                 tc::mbar_arrive(&bar.p_full);
+                if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(10);
+
+                // the chunk's rows
+                if (!warp_wait(&bar.o_full, c)) break;
+                if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(15);
+                tc::tc_fence_after_sync();
+                const int sv = tile_slot(c, kTileV);
+                const bool whole = c < chunks - 1 || tail == kC;              // a store of 128 rows stays inside the sequence
+                uint8_t* row = smem + sv * L::kTile + i * 128;                // P V has read the slot's V tile
+                __nv_bfloat16* orow = out + (int64_t)(c * kC + i) * g.o_token;
+                const bool mine = c * kC + i < n_tok;
+                #pragma unroll 1
+                for (int x0 = half * (D / 2); x0 < (half + 1) * (D / 2); x0 += 16) {
+                    uint32_t v[16];
+                    tc::tmem_ld16(tmem + lanes + kColO + (uint32_t)x0, v);
+                    tc::tmem_ld_wait();
+                    uint8_t* dst = row + (x0 >> 6) * L::kHalf;
+                    #pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        uint32_t w[4];
+                        #pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            w[x] = round_pair(mul_pair(as_pair(v[y * 8 + 2 * x], v[y * 8 + 2 * x + 1]), make_pair(g.scale, g.scale)));
+                        const uint4 u = make_uint4(w[0], w[1], w[2], w[3]);
+                        if (whole) *reinterpret_cast<uint4*>(dst + (((((x0 & 63) >> 3) + y) ^ (i & 7)) << 4)) = u;
+                        else if (mine) *reinterpret_cast<uint4*>(orow + x0 + y * 8) = u;
+                    }
+                }
+                tc::tc_fence_before_sync();
+                tc::mbar_arrive(&bar.o_empty);
+                if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(16);
+                if (whole) {
+                    tc::fence_smem_to_async_proxy();
+                    tc::mbar_arrive(&bar.o_staged);
+                }
             }
         }
-    } else if (warp < kWarpV) {
-        // ------------------------------------------------------------ S: state column (row of S^T) d per thread
-        const int d = quad * 32 + lane;
+    } else if (warp >= kWarpS && warp < kWarpP) {
+        // ------------------------------------------------------------ S: row d of S^T, half of its columns, per thread
+        regs_up<kRegsS>();
+        const int d = quad * 32 + lane, half = (warp >> 2) & 1;
         if (d < D) {
-            const int64_t at = (slot * g.H + h) * (int64_t)D * D + d;
-            const float* local = p.local + ((b * g.H + h) * (int64_t)(p.segments - 1)) * D * D + d;
-            // 32 rows of the state before the segment: the given one and what the segments before this one added
-            auto initial = [&](int r0, float (&v)[32]) {
+            constexpr int N = D / 2;
+            const int r0 = half * N;
+            const int64_t at = ((slot * g.H + h) * (int64_t)D + r0) * D + d;
+            pair_t S[N / 2];                                // S^T row d, columns r0 .. r0 + N - 1
+            {
+                float v[N];
+                // the given state, and what the segments before this one added
                 const float w0 = decay_pow(g2, (float)s0);
+                const bool given = !kStates && g.state != nullptr && w0 != 0.f;
                 #pragma unroll
-                for (int x = 0; x < 32; ++x) v[x] = g.state != nullptr && w0 != 0.f ? w0 * g.state[at + (int64_t)(r0 + x) * D] : 0.f;
-                for (int s = 0; s < seg; ++s) {
-                    const float w = decay_pow(g2, (float)((int64_t)(seg - 1 - s) * p.seg_len));
-                    if (w == 0.f) continue;
-                    #pragma unroll
-                    for (int x = 0; x < 32; ++x) v[x] = fmaf(w, local[((int64_t)s * D + r0 + x) * D], v[x]);
+                for (int x = 0; x < N; ++x) v[x] = given ? w0 * g.state[at + (int64_t)x * D] : 0.f;
+                if constexpr (!kStates) {
+                    const float* local = p.local + (((b * g.H + h) * (int64_t)(p.segments - 1)) * D + r0) * D + d;
+                    for (int s = 0; s < seg; ++s) {
+                        const float w = decay_pow(g2, (float)((int64_t)(seg - 1 - s) * p.seg_len));
+                        if (w == 0.f) continue;
+                        #pragma unroll
+                        for (int x = 0; x < N; ++x) v[x] = fmaf(w, local[((int64_t)s * D + x) * D], v[x]);
+                    }
                 }
+                #pragma unroll
+                for (int x = 0; x < N; x += 2) S[x >> 1] = make_pair(v[x], v[x + 1]);
+                __syncwarp();
+            }
+            const float keep = decay_pow(g2, (float)kC);
+            const uint32_t col = tmem + lanes + kColS + (uint32_t)r0;
+            auto add = [&](float l) {                       // S <- l S + the chunk's part
+                #pragma unroll
+                for (int x0 = 0; x0 < N; x0 += 32) {
+                    uint32_t u[2][16];
+                    tc::tmem_ld16(col + (uint32_t)x0, u[0]);
+                    tc::tmem_ld16(col + (uint32_t)(x0 + 16), u[1]);
+                    tc::tmem_ld_wait();
+                    #pragma unroll
+                    for (int x = 0; x < 32; x += 2)
+                        S[(x0 + x) >> 1] = fma_pair(make_pair(l, l), S[(x0 + x) >> 1], as_pair(u[x >> 4][x & 15], u[x >> 4][(x & 15) + 1]));
+                }
+                tc::tc_fence_before_sync();
             };
             bool alive = true;
-            if constexpr (!kStates) {
-                for (int c = 0; c < chunks; ++c) {
-                    if (c > 0 && !(alive = warp_wait(&bar.kv_done, c - 1))) break;
+            for (int c = 0; c < chunks; ++c) {
+                if (c > 0) {
+                    if (!(alive = warp_wait(&bar.kv_done, c - 1))) break;
+                    if (threadIdx.x == (kWarpS + (D / 32 - 1)) * 32) CHUNK_TL(11);
                     tc::tc_fence_after_sync();
-                    const float keep = decay_pow(g2, (float)(c == chunks - 1 ? tail : kC));
+                    add(keep);
+                    tc::mbar_arrive(&bar.d_free);
+                }
+                if constexpr (!kStates) {
+                    if (c > 0 && !(alive = warp_wait(&bar.qs_done, c - 1))) break;      // the terms of the chunk before have been read
                     uint8_t* terms = smem + L::off_state + d * 128;
-                    #pragma unroll 1
-                    for (int r0 = 0; r0 < D; r0 += 32) {
-                        const uint32_t col = tmem + lanes + kColS + (uint32_t)r0;
-                        uint32_t u[32];
-                        if (c == 0) {
-                            float v[32];
-                            initial(r0, v);
-                            #pragma unroll
-                            for (int x = 0; x < 32; ++x) u[x] = __float_as_uint(v[x]);
-                            __syncwarp();
-                        } else {
-                            tc::tmem_ld32(col, u);
-                            tc::tmem_ld_wait();
-                        }
+                    #pragma unroll
+                    for (int x = 0; x < N; x += 8) {
+                        uint32_t hi[4], lo[4];
                         #pragma unroll
-                        for (int x = 0; x < 32; x += 8) {
-                            uint32_t hi[4], lo[4];
-                            #pragma unroll
-                            for (int y = 0; y < 4; ++y) {
-                                const float a = __uint_as_float(u[x + 2 * y]), bb = __uint_as_float(u[x + 2 * y + 1]);
-                                hi[y] = pack2<__nv_bfloat16>(a, bb);
-                                lo[y] = pack2<__nv_bfloat16>(a - bf16_low(hi[y]), bb - bf16_high(hi[y]));
-                            }
-                            const int r = r0 + x;
-                            const uint32_t o = (uint32_t)(r >> 6) * (D * 128) + ((uint32_t)(((r & 63) >> 3) ^ (d & 7)) << 4);
-                            *reinterpret_cast<uint4*>(terms + o) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                            *reinterpret_cast<uint4*>(terms + L::kState + o) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                        }
-                        #pragma unroll
-                        for (int x = 0; x < 32; ++x) u[x] = __float_as_uint(__uint_as_float(u[x]) * keep);
-                        tc::tmem_st32(col, u);
+                        for (int y = 0; y < 4; ++y) split2(S[(x >> 1) + y], hi[y], lo[y]);
+                        const int r = r0 + x;
+                        const uint32_t o = (uint32_t)(r >> 6) * (D * 128) + ((uint32_t)(((r & 63) >> 3) ^ (d & 7)) << 4);
+                        *reinterpret_cast<uint4*>(terms + o) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                        *reinterpret_cast<uint4*>(terms + L::kState + o) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                     }
-                    tc::tmem_st_wait();
                     tc::fence_smem_to_async_proxy();
-                    tc::tc_fence_before_sync();
                     tc::mbar_arrive(&bar.s_full);
+                    if (threadIdx.x == (kWarpS + (D / 32 - 1)) * 32) CHUNK_TL(12);
                 }
             }
             // the state after the segment
-            if ((kStates || last_seg) && alive && (chunks == 0 || warp_wait(&bar.kv_done, kStates ? 0 : chunks - 1))) {
+            if ((kStates || last_seg) && alive && (chunks == 0 || warp_wait(&bar.kv_done, chunks - 1))) {
                 tc::tc_fence_after_sync();
-                float* dst = kStates ? p.local + (((b * g.H + h) * (int64_t)(p.segments - 1)) + seg) * D * D + d : g.state_out + at;
-                #pragma unroll 1
-                for (int r0 = 0; r0 < D; r0 += 32) {
-                    uint32_t u[32];
-                    if (chunks > 0) {
-                        tc::tmem_ld32(tmem + lanes + kColS + (uint32_t)r0, u);
-                        tc::tmem_ld_wait();
-                    } else {
-                        float v[32];
-                        initial(r0, v);
-                        #pragma unroll
-                        for (int x = 0; x < 32; ++x) u[x] = __float_as_uint(v[x]);
-                    }
-                    #pragma unroll
-                    for (int x = 0; x < 32; ++x) dst[(int64_t)(r0 + x) * D] = __uint_as_float(u[x]);
+                if (chunks > 0) add(decay_pow(g2, (float)tail));
+                float* dst = kStates ? p.local + ((((b * g.H + h) * (int64_t)(p.segments - 1)) + seg) * D + r0) * D + d : g.state_out + at;
+                #pragma unroll
+                for (int x = 0; x < N; x += 2) {
+                    float a, b2;
+                    take_pair(S[x >> 1], a, b2);
+                    dst[(int64_t)x * D] = a; dst[(int64_t)(x + 1) * D] = b2;
                 }
             }
         }
-    } else if (warp < kWarpO) {
-        // ------------------------------------------------------------ V: column d of the V tile per thread
-        const int d = quad * 32 + lane;
+    } else {
+        // ------------------------------------------------------------ V: column d of the V tile, every other entry, per thread
+        regs_down<kRegsV>();
+        const int d = quad * 32 + lane, half = (warp >> 2) & 1;
         if (d < D) {
-            const uint32_t v_col = (uint32_t)(d >> 6) * L::kHalf + (uint32_t)(d & 7) * 2u;
-            const uint32_t chunk16 = (uint32_t)((d & 63) >> 3);
+            uint32_t v_at[8];                               // where column d of token row j lies, for j & 7 (1024 bytes to the next 8)
+            #pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v_at[j] = (uint32_t)(d >> 6) * L::kHalf + (uint32_t)(d & 7) * 2u + (uint32_t)j * 128u + ((uint32_t)(((d & 63) >> 3) ^ j) << 4);
+            const uint32_t col = tmem + lanes + kColV + (uint32_t)(half * 64);
             for (int c = 0; c < chunks; ++c) {
                 const int sv = tile_slot(c, kTileV);
                 if (!warp_wait(&bar.full[sv], tile_phase(c, kTileV))) break;
+                if (threadIdx.x == (kWarpV + (D / 32 - 1)) * 32) CHUNK_TL(13);
                 const int n = c == chunks - 1 ? tail : kC;
                 uint8_t* tile = smem + sv * L::kTile;
                 if (n < kC) {
                     const int sk = tile_slot(c, kTileK);
                     if (!warp_wait(&bar.full[sk], tile_phase(c, kTileK))) break;
-                    // 16-byte pieces of the rows n .. C-1 of both tiles (every half)
+                    // 16-byte pieces of the rows n .. C-1 of both tiles (every 64 columns)
                     const int pieces = (kC - n) * 8;
-                    for (int x = d; x < pieces * (D / 64); x += D) {
+                    for (int x = half * D + d; x < pieces * (D / 64); x += 2 * D) {
                         const uint32_t o = (uint32_t)(x / pieces) * L::kHalf + (uint32_t)n * 128u + (uint32_t)(x % pieces) * 16u;
                         *reinterpret_cast<uint4*>(tile + o) = make_uint4(0, 0, 0, 0);
                         *reinterpret_cast<uint4*>(smem + sk * L::kTile + o) = make_uint4(0, 0, 0, 0);
                     }
+                    for (int j = half * D + d; j < kC; j += 2 * D) table[kC + 32 + j] = j < n ? table[j + kC - n] : 0.f;
                     tc::fence_smem_to_async_proxy();
                     tc::mbar_arrive(&bar.fixed);
+                    if (!warp_wait(&bar.fixed, 0)) break;
                 }
-                // only states: the weight runs on to the end of the segment
-                const float run = kStates ? decay_pow(g2, (float)(n_tok - (c * kC + n))) : 1.f;
+                const float* weight = n < kC ? table + kC + 32 : table;       // l^(n - 1 - j)
                 bool alive = true;
                 #pragma unroll 1
-                for (int e = 0; e < kC / kEntry; ++e) {
-                    const int ve = c * (kC / kEntry) + e;
-                    uint32_t hi[16], mid[16], lo[16];
-                    #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        float y[2];
+                for (int e = half; e < kC / kEntry; e += 2) {
+                    #pragma unroll 1
+                    for (int sub = 0; sub < kEntry / 16; ++sub) {
+                        uint32_t hi[8], mid[8], lo[8];
+                        const int j0 = e * kEntry + sub * 16;
+                        const uint8_t* rows = tile + j0 * 128;
+                        float v[16];
                         #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const int j = e * kEntry + 2 * x + k;
-                            const uint32_t o = v_col + (uint32_t)j * 128u + ((chunk16 ^ (uint32_t)(j & 7)) << 4);
-                            const float v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(tile + o) << 16);
-                            const float w = table[j + kC - n < kC ? j + kC - n : 0];
-                            y[k] = j < n ? v * (kStates ? w * run : w) : 0.f;
+                        for (int x = 0; x < 16; ++x) v[x] = value(rows + v_at[x & 7] + (x >> 3) * 1024);
+                        #pragma unroll
+                        for (int x = 0; x < 16; x += 4) {
+                            const float4 w = *reinterpret_cast<const float4*>(weight + j0 + x);
+                            const int k = x >> 1;
+                            split3(mul_pair(make_pair(v[x], v[x + 1]), make_pair(w.x, w.y)), hi[k], mid[k], lo[k]);
+                            split3(mul_pair(make_pair(v[x + 2], v[x + 3]), make_pair(w.z, w.w)), hi[k + 1], mid[k + 1], lo[k + 1]);
                         }
-                        hi[x] = pack2<__nv_bfloat16>(y[0], y[1]);
-                        y[0] -= bf16_low(hi[x]); y[1] -= bf16_high(hi[x]);
-                        mid[x] = pack2<__nv_bfloat16>(y[0], y[1]);
-                        lo[x] = pack2<__nv_bfloat16>(y[0] - bf16_low(mid[x]), y[1] - bf16_high(mid[x]));
+                        if (sub == 0) {
+                            if (!(alive = warp_wait(&bar.vt_empty[half], 2 * c + (e >> 1) + 1))) break;
+                            tc::tc_fence_after_sync();
+                        }
+                        tc::tmem_st8(col + (uint32_t)(sub * 8), hi);
+                        tc::tmem_st8(col + (uint32_t)(16 + sub * 8), mid);
+                        tc::tmem_st8(col + (uint32_t)(32 + sub * 8), lo);
                     }
-                    if (!(alive = warp_wait(&bar.vt_empty[ve & 1], (ve >> 1) + 1))) break;
-                    tc::tc_fence_after_sync();
-                    const uint32_t col = tmem + lanes + kColV + (uint32_t)((ve & 1) * 64);
-                    tc::tmem_st16(col, hi);
-                    tc::tmem_st16(col + 16, mid);
-                    tc::tmem_st16(col + 32, lo);
+                    if (!alive) break;
                     tc::tmem_st_wait();
                     tc::tc_fence_before_sync();
-                    tc::mbar_arrive(&bar.vt_full[ve & 1]);
+                    tc::mbar_arrive(&bar.vt_full[half]);
                 }
                 if (!alive) break;
-            }
-        }
-    } else {
-        // ------------------------------------------------------------ O: row i of the chunk per thread
-        if constexpr (!kStates) {
-            const int i = quad * 32 + lane;
-            for (int c = 0; c < chunks; ++c) {
-                if (!warp_wait(&bar.o_full, c)) break;
-                tc::tc_fence_after_sync();
-                uint32_t w[D / 2];
-                #pragma unroll
-                for (int x0 = 0; x0 < D; x0 += 32) {
-                    uint32_t v[32];
-                    tc::tmem_ld32(tmem + lanes + kColO + (uint32_t)x0, v);
-                    tc::tmem_ld_wait();
-                    #pragma unroll
-                    for (int x = 0; x < 32; x += 2)
-                        w[(x0 + x) / 2] = pack2<__nv_bfloat16>(g.scale * __uint_as_float(v[x]), g.scale * __uint_as_float(v[x + 1]));
-                }
-                tc::tc_fence_before_sync();
-                tc::mbar_arrive(&bar.o_empty);
-                if (c * kC + i < n_tok) {
-                    uint4* dst = reinterpret_cast<uint4*>(out + (int64_t)(c * kC + i) * g.o_token);
-                    #pragma unroll
-                    for (int x = 0; x < D / 8; ++x) dst[x] = make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]);
-                }
+                if (threadIdx.x == (kWarpV + (D / 32 - 1)) * 32) CHUNK_TL(14);
             }
         }
     }
@@ -476,6 +623,8 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
     __syncthreads();
     tc::tc_fence_after_sync();
     if (warp == kWarpMma) tc::tmem_dealloc(tmem, kTmemCols);
+    if (threadIdx.x == 0 && *dead) atomicOr(g.status, kStatusWaitTimeout);
+    if (threadIdx.x == 0) RTN_TL(decay_chunk, 4);
 }
 
 // [tokens][heads][D] bf16 tensor in boxes of 128 tokens x 64 elements of one head, rows under the 128-byte swizzle.
@@ -512,7 +661,8 @@ ChunkPlan make_plan(const DecayArgs& g)
 }
 
 template <int D>
-cudaError_t launch_typed(const DecayArgs& g, cudaStream_t s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v)
+cudaError_t launch_typed(const DecayArgs& g, cudaStream_t s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+                         const CUtensorMap& o)
 {
     constexpr int bytes = (int)Layout<D>::kBytes;
     ChunkPlan p = make_plan(g);
@@ -522,14 +672,14 @@ cudaError_t launch_typed(const DecayArgs& g, cudaStream_t s, const CUtensorMap& 
     if (p.segments > 1) {
         e = cudaFuncSetAttribute(decay_chunk_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != cudaSuccess) return e;
-        e = cudaMallocAsync(&scratch, (size_t)g.B * g.H * (p.segments - 1) * D * D * sizeof(float), s);
+        e = scratch_alloc(&scratch, (size_t)g.B * g.H * (p.segments - 1) * D * D * sizeof(float), s);
         if (e != cudaSuccess) return e;
         p.local = static_cast<float*>(scratch);
-        decay_chunk_kernel<D, true><<<(unsigned)(g.B * g.H * (p.segments - 1)), kThreads, bytes, s>>>(g, p, q, k, v);
+        decay_chunk_kernel<D, true><<<(unsigned)(g.B * g.H * (p.segments - 1)), kThreads, bytes, s>>>(g, p, q, k, v, o);
         e = cudaGetLastError();
     }
     if (e == cudaSuccess) {
-        decay_chunk_kernel<D, false><<<(unsigned)(g.B * g.H * p.segments), kThreads, bytes, s>>>(g, p, q, k, v);
+        decay_chunk_kernel<D, false><<<(unsigned)(g.B * g.H * p.segments), kThreads, bytes, s>>>(g, p, q, k, v, o);
         e = cudaGetLastError();
     }
     if (scratch != nullptr) {
@@ -549,11 +699,11 @@ bool decay_chunk_supported(const DecayArgs& g)
 
 cudaError_t launch_decay_chunk(const DecayArgs& g, cudaStream_t s, bool& taken)
 {
-    CUtensorMap q, k, v;
+    CUtensorMap q, k, v, o;
     taken = encode_heads(&q, g.q, g.total, g.H, g.Dk, g.q_token, g.q_head) && encode_heads(&k, g.k, g.total, g.Hk, g.Dk, g.k_token, g.k_head) &&
-            encode_heads(&v, g.v, g.total, g.Hk, g.Dv, g.v_token, g.v_head);
+            encode_heads(&v, g.v, g.total, g.Hk, g.Dv, g.v_token, g.v_head) && encode_heads(&o, g.out, g.total, g.H, g.Dv, g.o_token, g.o_head);
     if (!taken) return cudaSuccess;
-    return g.Dk == 64 ? launch_typed<64>(g, s, q, k, v) : launch_typed<128>(g, s, q, k, v);
+    return g.Dk == 64 ? launch_typed<64>(g, s, q, k, v, o) : launch_typed<128>(g, s, q, k, v, o);
 }
 
 }  // namespace rtn

@@ -622,7 +622,8 @@ static cudaError_t launch_gemm_i8_typed(const GemmArgs& g, const LinearArgs& l, 
     const int64_t nblk = (g.K + kBlockCodes - 1) / kBlockCodes;
     const int64_t items_w = p.tiles_n * nblk * p.BN, items_a = mode == 2 ? p.tiles_m * nblk * p.TM * 128 : 0;
     void* scratch = nullptr;
-    cudaError_t e = cudaMallocAsync(&scratch, (size_t)(items_w + items_a) * 128, s);
+    const size_t scratch_bytes = (size_t)(items_w + items_a) * 128;
+    cudaError_t e = std::is_void<OutT>::value ? cudaMallocAsync(&scratch, scratch_bytes, s) : scratch_alloc(&scratch, scratch_bytes, s);
     if (e != cudaSuccess) return e;
     uint4* wexp = reinterpret_cast<uint4*>(scratch);
     uint4* aexp = mode == 2 ? wexp + items_w * 8 : nullptr;
