@@ -17,7 +17,6 @@ VARIANT_AUTO, VARIANT_POPC, VARIANT_I8 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 ROTARY_SCALE_NONE, ROTARY_SCALE_LINEAR, ROTARY_SCALE_BASE, ROTARY_SCALE_PARTS = 0, 1, 2, 3
-_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 _STATUS = {0: "RTN_OK", 1: "RTN_ERR_NULL", 2: "RTN_ERR_SHAPE", 3: "RTN_ERR_ALIGN",
            4: "RTN_ERR_VALUE", 5: "RTN_ERR_UNSUPPORTED", 6: "RTN_ERR_CUDA",
@@ -381,92 +380,42 @@ def rtn_probe_copy(src, dst, stream=None):
 
 
 # ---------------------------------------------------------------------------------------------- layer operators
+# Their arguments are checked and marshalled by _rtn_torch.so (csrc/rtn_torch.cpp), which calls the same C entry points.
 
-def _dense(name, t, dtype, device, shape=None):
-    """Address of a contiguous tensor of this type on the call's device (None stays None)."""
-    if t is None:
-        return None
-    if t.dtype != dtype:
-        raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name}: on {t.device}, the call is on {device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous tensor")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t.data_ptr()
+_torch_side = None
 
 
-def _heads(name, t, dtype, device, shape):
-    """Address, token stride and head stride of a [tokens, heads, D] tensor with adjacent elements."""
-    if t.shape != shape:
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name}: on {t.device}, the call is on {device}")
-    token, head, one = t.stride()
-    if one != 1 and shape[2] > 1 and t.numel():
-        raise ValueError(f"{name}: the elements of a head have to be adjacent")
-    return t.data_ptr(), token, head
-
-
-def _call_device(t, dtype):
-    """The device of a call, which has to be the current CUDA device, and the raw current stream."""
-    if not t.is_cuda:
-        raise ValueError("expected a CUDA tensor")
-    if dtype not in _DTYPE:
-        raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
-    index = t.device.index
-    if index != torch.cuda.current_device():
-        raise ValueError(f"tensors on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
-    return t.device, torch._C._cuda_getCurrentRawStream(index)
-
-
-def _params(name, scale, offset, full, device):
-    n = scale.numel()
-    if n not in (1, full) or offset.numel() != n:
-        raise ValueError(f"{name} scale and offset: expected 1 or {full} values each, got {n} and {offset.numel()}")
-    return _dense(name + "_scale", scale, torch.float32, device), _dense(name + "_offset", offset, torch.float32, device), n
+def _load_torch_side():
+    global _torch_side
+    try:
+        from . import _rtn_torch as native
+    except ImportError as e:
+        raise RuntimeError("_rtn_torch.so is missing or was built for another torch: build it with "
+                           "`python -m paper_1912_02057_b200.build`.  There is no fallback.") from e
+    at = lambda f: C.cast(f, C.c_void_p).value
+    L = lib()
+    native.bind(at(L.rtn_ternary_linear), at(L.rtn_qk_norm_rotary), at(L.rtn_decay_attention), at(L.rtn_decay_attention_step),
+                at(L.rtn_packed_row_bytes), RtnError)
+    _torch_side = native
+    return native
 
 
 def rtn_ternary_linear(a_packed, a_sum, w_packed, w_sum, M, N, K, a_scale, a_offset, w_scale, w_offset, bias=None,
                        activation=ACT_NONE, residual=None, out=None, dtype=None, stream=None):
     """act(packed ternary product + affine form + bias) + residual -> [M,N] of ``dtype`` (default: the type of ``out`` or
     ``residual``, else fp32).  ``out`` may be ``residual``; rows of either may be strided."""
-    if dtype is None:
-        dtype = out.dtype if out is not None else residual.dtype if residual is not None else torch.float32
-    device, raw = _call_device(a_packed, dtype)
-    if out is None:
-        out = torch.empty((M, N), dtype=dtype, device=device)
-    row = rtn_packed_row_bytes(K)
-    if a_packed.numel() < M * row or w_packed.numel() < N * row or a_sum.numel() < M or w_sum.numel() < N:
-        raise ValueError(f"operands too small for M={M}, N={N}, K={K}")
-    ends = []
-    for name, t in (("residual", residual), ("out", out)):
-        if t is None:
-            ends += [None, 0]
-            continue
-        if t.shape != (M, N) or t.dtype != dtype or t.device != device or (t.stride(1) != 1 and N > 1):
-            raise ValueError(f"{name}: expected {dtype} [{M}, {N}] on {device} with adjacent columns, got {t.dtype} {tuple(t.shape)} "
-                             f"on {t.device} with strides {t.stride()}")
-        ends += [t.data_ptr(), t.stride(0) if M > 1 else max(N, t.stride(0))]
-    _check(lib().rtn_ternary_linear(
-        _dense("a_packed", a_packed, torch.uint8, device), _dense("a_sum", a_sum, torch.int32, device),
-        _dense("w_packed", w_packed, torch.uint8, device), _dense("w_sum", w_sum, torch.int32, device), M, N, K,
-        *_params("a", a_scale, a_offset, M, device), *_params("w", w_scale, w_offset, N, device),
-        _dense("bias", bias, torch.float32, device, (N,)), int(activation), *ends, _DTYPE[dtype],
-        raw if stream is None else stream.cuda_stream), "rtn_ternary_linear")
-    return out
+    return (_torch_side or _load_torch_side()).linear(a_packed, a_sum, w_packed, w_sum, M, N, K, a_scale, a_offset, w_scale, w_offset,
+                                                      bias, activation, residual, out, dtype, stream and stream.cuda_stream)
 
 
 def rtn_rotary_table(rows, R, base=10000.0, scaling=ROTARY_SCALE_NONE, factor=1.0, original_context=0.0, low=1.0, high=32.0,
                      amplitude=1.0, device=None, stream=None):
-    """fp32 [rows, R]: the cosines, then the sines of the positions' angles."""
+    """fp32 [rows, R]: the cosines, then the sines of the positions' angles.  ``device``: the current CUDA device."""
     table = torch.empty((rows, R), dtype=torch.float32, device=device or "cuda")
-    _, raw = _call_device(table, torch.float32)
-    _check(lib().rtn_rotary_table(table.data_ptr(), rows, R, base, int(scaling), factor, original_context, low, high, amplitude,
-                                  raw if stream is None else stream.cuda_stream), "rtn_rotary_table")
+    if not table.is_cuda or table.device.index != torch.cuda.current_device():
+        raise ValueError(f"device: expected the current CUDA device, got {table.device}")
+    _check(lib().rtn_rotary_table(_ptr(table), rows, R, base, int(scaling), factor, original_context, low, high, amplitude,
+                                  _stream(stream)), "rtn_rotary_table")
     return table
 
 
@@ -474,75 +423,19 @@ def rtn_qk_norm_rotary(q, k, positions, table, q_weight=None, k_weight=None, eps
                        stream=None):
     """Norms (where weights are given) and rotation of q [T,Hq,D] and k [T,Hk,D] (or None) by the rows ``positions`` (int64 [T],
     or None: 0, 1, ...) of ``table`` [P,R] (or None: no rotation).  ``out_q`` / ``out_k`` may be the inputs.  Returns both."""
-    if q.dim() != 3:
-        raise ValueError("q: expected [tokens, heads, D]")
-    device, raw = _call_device(q, q.dtype)
-    T, Hq, D = q.shape
-    if out_q is None:
-        out_q = torch.empty((T, Hq, D), dtype=q.dtype, device=device)
-    ends = [*_heads("q", q, q.dtype, device, (T, Hq, D))]
-    oq = _heads("out_q", out_q, q.dtype, device, (T, Hq, D))
-    Hk = 0
-    if k is not None:
-        Hk = k.shape[1] if k.dim() == 3 else 0
-        if out_k is None:
-            out_k = torch.empty((T, Hk, D), dtype=q.dtype, device=device)
-        ends += [*_heads("k", k, q.dtype, device, (T, Hk, D)), *oq, *_heads("out_k", out_k, q.dtype, device, (T, Hk, D))]
-    else:
-        ends += [None, 0, 0, *oq, None, 0, 0]
-    P, R = table.shape if table is not None else (0, 0)
-    _check(lib().rtn_qk_norm_rotary(
-        *ends, T, Hq, Hk, D, R, int(layout), _dense("q_weight", q_weight, torch.float32, device, (D,)),
-        _dense("k_weight", k_weight, torch.float32, device, (D,)), eps, _dense("table", table, torch.float32, device), P,
-        _dense("positions", positions, torch.int64, device, (T,)), _DTYPE[q.dtype],
-        raw if stream is None else stream.cuda_stream), "rtn_qk_norm_rotary")
-    return out_q, out_k
-
-
-def _decay_args(q, k, v, log_decay, state, state_out, slots, B, scale, out, device):
-    T, H, Dk = q.shape
-    if k.dim() != 3 or v.dim() != 3:
-        raise ValueError("k, v: expected [tokens, heads, D]")
-    Hk, Dv = k.shape[1], v.shape[2]
-    dtype = q.dtype
-    if out is None:
-        out = torch.empty((T, H, Dv), dtype=dtype, device=device)
-    if state_out is None:
-        if state is None and slots is not None:
-            raise ValueError("slots without a state: state_out is required")
-        state_out = state if state is not None else torch.empty((B, H, Dk, Dv), dtype=torch.float32, device=device)
-    if state_out.dim() != 4:
-        raise ValueError("state_out: expected [slots, H, Dk, Dv]")
-    shape = (state_out.shape[0], H, Dk, Dv)
-    ends = (*_heads("q", q, dtype, device, (T, H, Dk)), *_heads("k", k, dtype, device, (T, Hk, Dk)),
-            *_heads("v", v, dtype, device, (T, Hk, Dv)), *_heads("out", out, dtype, device, (T, H, Dv)))
-    tail = (H, Hk, Dk, Dv, _dense("log_decay", log_decay, torch.float32, device, (H,)), Dk ** -0.5 if scale is None else scale,
-            _dense("state", state, torch.float32, device, shape), _dense("state_out", state_out, torch.float32, device, shape),
-            _dense("slots", slots, torch.int32, device, (B,)), shape[0], _DTYPE[dtype])
-    return ends, tail, out, state_out
+    return (_torch_side or _load_torch_side()).rotary(q, k, positions, table, q_weight, k_weight, eps, layout, out_q, out_k,
+                                                      stream and stream.cuda_stream)
 
 
 def rtn_decay_attention(q, k, v, log_decay, start, max_len, state=None, state_out=None, slots=None, scale=None, out=None, stream=None):
     """Linear attention with a decay per head over prompts laid end to end: q [total,H,Dk], k [total,Hk,Dk], v [total,Hk,Dv],
     ``start`` int32 [B+1].  ``state`` fp32 [slots,H,Dk,Dv] (None: zero), ``state_out`` (default: ``state`` itself, or a new one)
     receives the states after the last tokens.  ``scale`` defaults to Dk**-0.5.  Returns (out [total,H,Dv], state_out)."""
-    if q.dim() != 3 or start.dim() != 1 or start.numel() < 1:
-        raise ValueError("q: expected [tokens, heads, Dk]; start: expected [B + 1]")
-    device, raw = _call_device(q, q.dtype)
-    B = start.numel() - 1
-    ends, tail, out, state_out = _decay_args(q, k, v, log_decay, state, state_out, slots, B, scale, out, device)
-    _check(lib().rtn_decay_attention(*ends, q.shape[0], B, _dense("start", start, torch.int32, device), max_len, *tail,
-                                     raw if stream is None else stream.cuda_stream), "rtn_decay_attention")
-    return out, state_out
+    return (_torch_side or _load_torch_side()).decay(q, k, v, log_decay, start, max_len, state, state_out, slots, scale, out,
+                                                     stream and stream.cuda_stream)
 
 
 def rtn_decay_attention_step(q, k, v, log_decay, state, state_out=None, slots=None, scale=None, out=None, stream=None):
     """One new token for each of B sequences: q [B,H,Dk], k [B,Hk,Dk], v [B,Hk,Dv]; ``state`` (None: zero) and ``state_out``
     (default: in place) fp32 [slots,H,Dk,Dv], ``slots`` int32 [B] (negative: a padding entry).  Returns (out [B,H,Dv], state_out)."""
-    if q.dim() != 3:
-        raise ValueError("q: expected [B, heads, Dk]")
-    device, raw = _call_device(q, q.dtype)
-    B = q.shape[0]
-    ends, tail, out, state_out = _decay_args(q, k, v, log_decay, state, state_out, slots, B, scale, out, device)
-    _check(lib().rtn_decay_attention_step(*ends, B, *tail, raw if stream is None else stream.cuda_stream), "rtn_decay_attention_step")
-    return out, state_out
+    return (_torch_side or _load_torch_side()).step(q, k, v, log_decay, state, state_out, slots, scale, out, stream and stream.cuda_stream)

@@ -1,4 +1,4 @@
-"""Builds librtn_b200.so in-tree with nvcc for sm_100a.
+"""Builds librtn_b200.so in-tree with nvcc for sm_100a, and _rtn_torch.so, the torch side of the layer operators, with g++.
 
 Usage: python -m paper_1912_02057_b200.build [--force] [--verbose] [--timeline]
 
@@ -34,7 +34,32 @@ LIB_TIMELINE = os.path.join(HERE, "librtn_b200_timeline.so")
 def build(force=False, verbose=False, timeline=False):
     if timeline:
         return _build(os.path.join(HERE, "_build_timeline"), LIB_TIMELINE, ["-DRTN_TIMELINE"], force, verbose)
-    return _build(OBJ, LIB, [], force, verbose)
+    lib = _build(OBJ, LIB, [], force, verbose)
+    _build_torch(force, verbose)
+    return lib
+
+
+LIB_TORCH = os.path.join(HERE, "_rtn_torch.so")
+
+
+def _build_torch(force, verbose):
+    src = os.path.join(CSRC, "rtn_torch.cpp")
+    if not force and _newer(LIB_TORCH, [src, os.path.join(ROOT, "include", "rtn.h")]):
+        return
+    import sysconfig
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    libs = library_paths()
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"),
+           *(x for i in include_paths() for x in ("-isystem", i)), src, "-o", LIB_TORCH,
+           *(x for l in libs for x in ("-L" + l, "-Wl,-rpath," + l)), "-lc10", "-ltorch", "-ltorch_cpu", "-ltorch_python", "-lc10_cuda", "-ltorch_cuda"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if verbose or r.returncode != 0:
+        sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed on rtn_torch.cpp")
 
 
 def _build(OBJ, LIB, extra, force, verbose):

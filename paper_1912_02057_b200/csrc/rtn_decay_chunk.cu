@@ -108,28 +108,6 @@ __device__ __forceinline__ void tma_store_tile(const CUtensorMap* map, uint32_t 
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c), "r"(head), "r"(token), "r"(src) : "memory");
 }
 
-// Pairs of fp32 values in one 64-bit register: one instruction for both.
-typedef unsigned long long pair_t;
-__device__ __forceinline__ pair_t make_pair(float a, float b)
-{
-    pair_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void take_pair(pair_t p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
-__device__ __forceinline__ pair_t mul_pair(pair_t a, pair_t b)
-{
-    pair_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ pair_t fma_pair(pair_t a, pair_t b, pair_t c)
-{
-    pair_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-
 // The pair rounded to bf16 (packed low / high) and what is left of it.
 __device__ __forceinline__ pair_t split_term(pair_t y, uint32_t& term)
 {

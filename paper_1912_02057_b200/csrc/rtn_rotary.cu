@@ -18,7 +18,7 @@ namespace rtn {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 64;
 constexpr int kGenericWarps = 4;
 
 __device__ __forceinline__ bool token_position(const RotaryArgs& g, int64_t t, int64_t& pos)
@@ -27,109 +27,167 @@ __device__ __forceinline__ bool token_position(const RotaryArgs& g, int64_t t, i
     return pos >= 0 && pos < g.table_rows;
 }
 
-// HP heads of one token per group of G lanes; CH 16-byte chunks per lane (head dimension up to 32 CH chunks).
-template <typename T, int CH, int HP>
+// N consecutive floats, on a boundary of their own size (16 bytes at most).
+template <int N>
+__device__ __forceinline__ void load_floats(const float* p, float (&f)[N])
+{
+    if constexpr (N >= 4) {
+        #pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const float4 v = __ldg(reinterpret_cast<const float4*>(p + i));
+            f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+        }
+    } else {
+        const float2 v = __ldg(reinterpret_cast<const float2*>(p));
+        f[0] = v.x; f[1] = v.y;
+    }
+}
+
+// `per_group` heads of one token per group of G lanes, HP at a time with the next ones' loads in flight; CH 16-byte chunks per lane
+// (head dimension up to 32 CH chunks).
+template <typename T, int CH, int HP, bool kHalf>
 __global__ void __launch_bounds__(kThreads)
-qk_norm_rotary_kernel(const RotaryArgs g, int G, int groups_q, int groups_k)
+qk_norm_rotary_kernel(const RotaryArgs g, int G, int per_group, int groups_q, int groups_k)
 {
     constexpr int V = Vec16<T>::N;
     const int lane_g = threadIdx.x & (G - 1);
-    const int64_t item = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
-    const int per_token = groups_q + groups_k;
-    const int64_t t = item / per_token;
-    const bool live = t < g.T;                       // groups past the end stay for the warp's shuffles
+    const unsigned item = blockIdx.x * (unsigned)(kThreads / G) + threadIdx.x / G;
+    const unsigned per_token = groups_q + groups_k;
+    const unsigned t = item / per_token;            // (32 bits hold it: the entry point bounds T (Hq + Hk))
+    const bool live = t < g.T;                      // groups past the end stay for the warp's shuffles
     const int gi = (int)(item - t * per_token);
     const bool is_q = gi < groups_q;
-    const int h0 = (is_q ? gi : gi - groups_q) * HP;
     const int H = is_q ? g.Hq : g.Hk;
-    const T* src = static_cast<const T*>(is_q ? g.q : g.k) + (live ? t : 0) * (is_q ? g.q_token : g.k_token);
-    T* dst = static_cast<T*>(is_q ? g.out_q : g.out_k) + (live ? t : 0) * (is_q ? g.oq_token : g.ok_token);
+    const int h0 = (is_q ? gi : gi - groups_q) * per_group;
+    const int h1 = !live ? h0 : h0 + per_group < H ? h0 + per_group : H;
+    const T* src = static_cast<const T*>(is_q ? g.q : g.k) + (int64_t)(live ? t : 0) * (is_q ? g.q_token : g.k_token);
+    T* dst = static_cast<T*>(is_q ? g.out_q : g.out_k) + (int64_t)(live ? t : 0) * (is_q ? g.oq_token : g.ok_token);
     const int64_t s_head = is_q ? g.q_head : g.k_head, d_head = is_q ? g.oq_head : g.ok_head;
     const float* w = is_q ? g.q_weight : g.k_weight;
-    const int nch = g.D / V, hch = g.R / 2 / V;      // chunks of a head, of half its rotated part
+    const int nch = g.D / V, hch = g.R / 2 / V;     // chunks of a head, of half its rotated part
 
-    // the heads' elements (and, in the half layout, the partners') first: everything below waits for them
-    uint4 own[HP][CH], other[HP][CH];
-    #pragma unroll
-    for (int p = 0; p < HP; ++p)
+    // the first heads' elements (and, in the half layout, the partners'): everything below waits for them
+    uint4 own[HP][CH], other[HP][kHalf ? CH : 1];
+    const T* at = src + h0 * s_head + lane_g * V;
+    T* to = dst + h0 * d_head + lane_g * V;
+    auto load = [&](int h) {                        // heads h .. h + HP - 1, `at` on the first
         #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int ch = lane_g + c * 32;
-            own[p][c] = other[p][c] = make_uint4(0, 0, 0, 0);
-            if (live && h0 + p < H && ch < nch) {
-                const uint4* row = reinterpret_cast<const uint4*>(src + (h0 + p) * s_head);
-                own[p][c] = row[ch];
-                if (g.layout == RTN_ROTARY_HALF && ch < 2 * hch) other[p][c] = row[ch < hch ? ch + hch : ch - hch];
+        for (int p = 0; p < HP; ++p)
+            #pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int ch = lane_g + c * 32;
+                own[p][c] = make_uint4(0, 0, 0, 0);
+                if constexpr (kHalf) other[p][c] = make_uint4(0, 0, 0, 0);
+                if (h + p < h1 && ch < nch) {
+                    const uint4* row = reinterpret_cast<const uint4*>(at + p * s_head) + c * 32;
+                    own[p][c] = *row;
+                    if constexpr (kHalf) { if (ch < 2 * hch) other[p][c] = row[ch < hch ? hch : -hch]; }
+                }
             }
-        }
+    };
+    load(h0);
 
     int64_t pos = 0;
     const bool pos_ok = !live || g.R == 0 || token_position(g, t, pos);
     if (!pos_ok && lane_g == 0) atomicOr(g.status, kStatusBadIndex);
-    float cs[CH][V], sn[CH][V], wo[CH][V], wp[CH][V];        // per element: cosine, signed sine, weight, partner's weight
+    // y_e = (x_e A_e + o_e B_e) / rms with o the partner element: A = w cos, B = (partner's w) (-sin or sin), the same for every head
+    float A[CH][V], B[CH][V];
     #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int ch = lane_g + c * 32;
-        const bool rot = live && ch < 2 * hch && pos_ok;
-        const float* row = g.table + pos * g.R;
-        const int pch = ch < hch ? ch + hch : ch - hch;
+        const bool rot = ch < 2 * hch && pos_ok, second = ch >= hch;
         #pragma unroll
-        for (int e = 0; e < V; ++e) { cs[c][e] = 1.f; sn[c][e] = 0.f; wo[c][e] = 1.f; wp[c][e] = 1.f; }
+        for (int e = 0; e < V; ++e) { A[c][e] = 1.f; B[c][e] = 0.f; }
         if (rot) {
-            #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const bool half = g.layout == RTN_ROTARY_HALF;
-                const int f = half ? (ch < hch ? ch : ch - hch) * V + e : ch * (V / 2) + e / 2;
-                const bool second = half ? ch >= hch : (e & 1);
-                cs[c][e] = __ldg(row + f);
-                const float s = __ldg(row + g.R / 2 + f);
-                sn[c][e] = second ? s : -s;
+            const float* row = g.table + pos * g.R;
+            if constexpr (kHalf) {
+                const int f = (second ? ch - hch : ch) * V;
+                load_floats<V>(row + f, A[c]);
+                load_floats<V>(row + g.R / 2 + f, B[c]);
+                #pragma unroll
+                for (int e = 0; e < V; ++e) B[c][e] = second ? B[c][e] : -B[c][e];
+            } else {
+                float cs[V / 2], sn[V / 2];
+                load_floats<V / 2>(row + ch * (V / 2), cs);
+                load_floats<V / 2>(row + g.R / 2 + ch * (V / 2), sn);
+                #pragma unroll
+                for (int e = 0; e < V; ++e) { A[c][e] = cs[e / 2]; B[c][e] = (e & 1) ? sn[e / 2] : -sn[e / 2]; }
             }
         }
         if (w != nullptr && ch < nch) {
+            float f[V];
+            load_floats<V>(w + ch * V, f);
             #pragma unroll
-            for (int e = 0; e < V; ++e) wo[c][e] = __ldg(w + ch * V + e);
-            if (g.layout == RTN_ROTARY_HALF && ch < 2 * hch) {
+            for (int e = 0; e < V; ++e) A[c][e] *= f[e];
+            if (rot) {
+                if constexpr (kHalf) load_floats<V>(w + (second ? ch - hch : ch + hch) * V, f);
                 #pragma unroll
-                for (int e = 0; e < V; ++e) wp[c][e] = __ldg(w + pch * V + e);
+                for (int e = 0; e < V; ++e) B[c][e] *= kHalf ? f[e] : f[e ^ 1];
             }
         }
     }
+    pair_t A2[CH][V / 2], B2[CH][V / 2];
     #pragma unroll
-    for (int p = 0; p < HP; ++p) {
-        float x[CH][V];
-        float ss = 0.f;
+    for (int c = 0; c < CH; ++c)
         #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            Vec16<T>::unpack(own[p][c], x[c]);
+        for (int e = 0; e < V / 2; ++e) {
+            A2[c][e] = make_pair(A[c][2 * e], A[c][2 * e + 1]);
+            B2[c][e] = make_pair(B[c][2 * e], B[c][2 * e + 1]);
+        }
+    const float inv_d = 1.f / (float)g.D;
+    const int trips = per_group;                    // the same for every lane: they shuffle together
+    for (int done = 0; done < trips; done += HP) {
+        const int h = h0 + done;
+        pair_t y[HP][CH][V / 2];
+        float r[HP];
+        #pragma unroll
+        for (int p = 0; p < HP; ++p) {
+            pair_t ss = make_pair(0.f, 0.f);
             #pragma unroll
-            for (int e = 0; e < V; ++e) ss = fmaf(x[c][e], x[c][e], ss);
-        }
-        float r = 1.f;
-        if (w != nullptr) {
-            for (int d = G / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-            r = 1.f / sqrtf(ss / (float)g.D + g.eps);
-        }
-        if (!pos_ok) r = __int_as_float(0x7fffffff);             // a position outside the table: NaN, never a wrong angle
-        #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int ch = lane_g + c * 32;
-            if (!live || h0 + p >= H || ch >= nch) continue;
-            float o[V], y[V];
-            if (g.layout == RTN_ROTARY_HALF) {
-                Vec16<T>::unpack(other[p][c], o);
+            for (int c = 0; c < CH; ++c) {
+                pair_t x[V / 2], o[V / 2];
+                Pairs16<T>::unpack(own[p][c], x);
+                if constexpr (kHalf) {
+                    Pairs16<T>::unpack(other[p][c], o);              // zero past the rotated part
+                } else {
+                    const bool rot = lane_g + c * 32 < 2 * hch;      // past it the neighbour's value stays out
+                    #pragma unroll
+                    for (int e = 0; e < V / 2; ++e) {
+                        float a, b;
+                        take_pair(x[e], a, b);
+                        o[e] = make_pair(rot ? b : 0.f, rot ? a : 0.f);
+                    }
+                }
                 #pragma unroll
-                for (int e = 0; e < V; ++e) y[e] = fmaf(x[c][e] * wo[c][e], cs[c][e], o[e] * wp[c][e] * sn[c][e]) * r;
-            } else {
-                const bool rot = ch < 2 * hch;           // past the rotated part the neighbour's value stays out of it
-                #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float o = rot ? x[c][e ^ 1] * wo[c][e ^ 1] : 0.f;
-                    y[e] = fmaf(x[c][e] * wo[c][e], cs[c][e], o * sn[c][e]) * r;
+                for (int e = 0; e < V / 2; ++e) {
+                    ss = fma_pair(x[e], x[e], ss);
+                    y[p][c][e] = fma_pair(x[e], A2[c][e], mul_pair(o[e], B2[c][e]));
                 }
             }
-            reinterpret_cast<uint4*>(dst + (h0 + p) * d_head)[ch] = Vec16<T>::pack(y);
+            float a, b;
+            take_pair(ss, a, b);
+            r[p] = a + b;
         }
+        at += HP * s_head;
+        if (done + HP < trips) load(h + HP);
+        if (w != nullptr) {
+            for (int d = G / 2; d > 0; d >>= 1)
+                #pragma unroll
+                for (int p = 0; p < HP; ++p) r[p] += __shfl_xor_sync(0xffffffffu, r[p], d);
+        }
+        #pragma unroll
+        for (int p = 0; p < HP; ++p) {
+            float s = w != nullptr ? rsqrtf(fmaf(r[p], inv_d, g.eps)) : 1.f;
+            if (!pos_ok) s = __int_as_float(0x7fffffff);             // a position outside the table: NaN, never a wrong angle
+            #pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                if (h + p >= h1 || lane_g + c * 32 >= nch) continue;
+                #pragma unroll
+                for (int e = 0; e < V / 2; ++e) y[p][c][e] = mul_pair(y[p][c][e], make_pair(s, s));
+                reinterpret_cast<uint4*>(to + p * d_head)[c * 32] = Pairs16<T>::pack(y[p][c]);
+            }
+        }
+        to += HP * d_head;
     }
 }
 
@@ -163,7 +221,7 @@ qk_norm_rotary_generic_kernel(const RotaryArgs g)
     int64_t pos = 0;
     const bool pos_ok = g.R == 0 || token_position(g, t, pos);
     if (!pos_ok && lane == 0) atomicOr(g.status, kStatusBadIndex);
-    float r = w != nullptr ? 1.f / sqrtf(ss / (float)g.D + g.eps) : 1.f;
+    float r = w != nullptr ? rsqrtf(ss / (float)g.D + g.eps) : 1.f;
     if (!pos_ok) r = __int_as_float(0x7fffffff);
     const float* row = g.table + (pos_ok ? pos : 0) * g.R;
     for (int e = lane; e < g.D; e += 32) {
@@ -210,11 +268,13 @@ __global__ void rotary_table_kernel(float* __restrict__ table, int64_t rows, int
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 template <typename T, int CH, int HP>
-cudaError_t launch_vec(const RotaryArgs& g, int G, cudaStream_t s)
+cudaError_t launch_vec(const RotaryArgs& g, int G, int per_group, cudaStream_t s)
 {
-    const int gq = (g.Hq + HP - 1) / HP, gk = (g.Hk + HP - 1) / HP;
+    const int gq = (g.Hq + per_group - 1) / per_group, gk = (g.Hk + per_group - 1) / per_group;
     const int64_t items = g.T * (gq + gk), per_cta = kThreads / G;
-    qk_norm_rotary_kernel<T, CH, HP><<<(unsigned)((items + per_cta - 1) / per_cta), kThreads, 0, s>>>(g, G, gq, gk);
+    const unsigned grid = (unsigned)((items + per_cta - 1) / per_cta);
+    if (g.layout == RTN_ROTARY_HALF) qk_norm_rotary_kernel<T, CH, HP, true><<<grid, kThreads, 0, s>>>(g, G, per_group, gq, gk);
+    else qk_norm_rotary_kernel<T, CH, HP, false><<<grid, kThreads, 0, s>>>(g, G, per_group, gq, gk);
     return cudaGetLastError();
 }
 
@@ -225,7 +285,8 @@ cudaError_t launch_typed(const RotaryArgs& g, cudaStream_t s)
     // 16-byte path: whole chunks in the head and in each half of its rotated part, every row on a 16-byte boundary
     const int64_t strides = g.q_token | g.q_head | g.k_token | g.k_head | g.oq_token | g.oq_head | g.ok_token | g.ok_head;
     const bool vec = g.D % V == 0 && (g.R / 2) % V == 0 && strides % V == 0 && g.D / V <= 64 && aligned16(g.q) &&
-                     aligned16(g.k) && aligned16(g.out_q) && aligned16(g.out_k);
+                     aligned16(g.k) && aligned16(g.out_q) && aligned16(g.out_k) && aligned16(g.table) &&
+                     aligned16(g.q_weight) && aligned16(g.k_weight);
     if (!vec) {
         const int64_t items = g.T * (g.Hq + g.Hk);
         qk_norm_rotary_generic_kernel<T><<<(unsigned)((items + kGenericWarps - 1) / kGenericWarps), kGenericWarps * 32, 0, s>>>(g);
@@ -234,10 +295,11 @@ cudaError_t launch_typed(const RotaryArgs& g, cudaStream_t s)
     const int nch = g.D / V;
     int G = 1;
     while (G < nch && G < 32) G *= 2;
-    if (nch > 32) return launch_vec<T, 2, 1>(g, G, s);
-    // several heads per group once one head each would fill the machine many times over
+    // Few tokens: a head per group, for the most groups; many: eight, for the fewest table and weight reads.
     const int64_t warps = g.T * (g.Hq + g.Hk) * G / 32;
-    return warps > (int64_t)device_sm_count() * 128 ? launch_vec<T, 1, 4>(g, G, s) : launch_vec<T, 1, 1>(g, G, s);
+    const int per_group = warps > (int64_t)device_sm_count() * 128 ? 8 : warps > (int64_t)device_sm_count() * 32 ? 2 : 1;
+    if (nch > 32) return launch_vec<T, 2, 1>(g, G, per_group, s);
+    return per_group == 1 ? launch_vec<T, 1, 1>(g, G, 1, s) : launch_vec<T, 1, 2>(g, G, per_group, s);
 }
 
 }  // namespace

@@ -54,6 +54,50 @@ template <typename T> struct Vec16 {
     }
 };
 
+// Pairs of fp32 values in one 64-bit register: one instruction for both.
+typedef unsigned long long pair_t;
+__device__ __forceinline__ pair_t make_pair(float a, float b)
+{
+    pair_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void take_pair(pair_t p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ pair_t mul_pair(pair_t a, pair_t b)
+{
+    pair_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ pair_t fma_pair(pair_t a, pair_t b, pair_t c)
+{
+    pair_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// The elements of T in 16 bytes as fp32 pairs and back.
+template <typename T> struct Pairs16 {
+    static constexpr int N = Vec16<T>::N / 2;
+    static __device__ __forceinline__ void unpack(const uint4& u, pair_t (&f)[N])
+    {
+        float v[2 * N];
+        Vec16<T>::unpack(u, v);
+        #pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = make_pair(v[2 * i], v[2 * i + 1]);
+    }
+    static __device__ __forceinline__ uint4 pack(const pair_t (&f)[N])
+    {
+        float v[2 * N];
+        #pragma unroll
+        for (int i = 0; i < N; ++i) take_pair(f[i], v[2 * i], v[2 * i + 1]);
+        if constexpr (sizeof(T) == 4)
+            return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        else
+            return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[2 * N - 4], v[2 * N - 3]), pack2<T>(v[2 * N - 2], v[2 * N - 1]));
+    }
+};
+
 // Calls f(T{}) with the C++ type of `dtype`.
 template <typename F>
 inline cudaError_t with_dtype(int dtype, F&& f)
