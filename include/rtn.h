@@ -244,8 +244,8 @@ typedef enum { RTN_ROTARY_SCALE_NONE = 0, RTN_ROTARY_SCALE_LINEAR = 1, RTN_ROTAR
  *   residual    NULL, or [M][N] of `dtype`, rows residual_stride elements apart; may be `out` itself (same stride), to
  *               add a layer to a residual stream in place; no other overlap
  *   out         [M][N] of `dtype`, rows out_stride >= N elements apart
- * Up to 8 rows (16 where the columns are few) run on a bit-plane kernel that streams the weights once, more rows
- * on the tensor cores with the launches of rtn_gemm_kernel_launches. */
+ * Few rows (up to 8, more where the product is small) run on a bit-plane kernel that streams the weights, some rows on a tensor-core
+ * kernel that expands its own operands, both one launch; larger products take the launches of rtn_gemm_kernel_launches. */
 rtn_status rtn_ternary_linear(const void* a_packed, const int32_t* a_sum,
                               const void* w_packed, const int32_t* w_sum,
                               int64_t M, int64_t N, int64_t K,

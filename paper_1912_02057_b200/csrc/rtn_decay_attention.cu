@@ -6,7 +6,7 @@
 // decay_step_kernel: one token per sequence.  Bound: DRAM, the fp32 state read and written once (8 Dk Dv bytes per head
 //   against 4 Dk Dv operations).
 // decay_recurrent_kernel: whole prompts token by token with the state in registers; any type, head dimension and
-//   stride.  Bound: the FMA pipe (two FMAs and a product per state element and token).
+//   stride.  Bound: the FMA pipe (two FMAs per state element and token).
 #include "rtn_internal.cuh"
 #include "rtn_types.cuh"
 #include "rtn_decay.cuh"
@@ -108,92 +108,247 @@ cudaError_t launch_step_typed(const DecayArgs& g, cudaStream_t s)
 
 // ------------------------------------------------------------------------------------------------ prompts, token by token
 
-constexpr int kRecCols = 32;            // state columns of a CTA, one per lane
-constexpr int kRecWarps = 4;            // each holds a quarter of the rows
-constexpr int kRecTile = 16;            // tokens staged at a time
+constexpr int kRecWarps = 4;            // each holds a quarter of the state's rows
+constexpr int kRecThreads = kRecWarps * 32;
+constexpr int kRecTile = 16;            // tokens staged at a time, at most
 
-template <typename T, int ROWS>
-__global__ void __launch_bounds__(kRecCols * kRecWarps)
-decay_recurrent_kernel(const DecayArgs g)
+struct RecPlan {
+    int64_t seg_len;        // tokens of a segment
+    int segments;           // of the longest sequence
+    float* local;           // [B][H][segments - 1][Dk][Dv]: what a segment adds to the state
+};
+
+// l^n from log2 l; n = 0 gives 1 for every l.
+__device__ __forceinline__ float power(float g2, float n) { return n == 0.f ? 1.f : exp2f(n * g2); }
+
+// Column(s) of the state in the lanes of four warps, rows in registers by pairs.  Within a tile of tokens i = 0, 1, ... the state is kept
+// relative to the tile's first token,
+//   S_i = l^i S'_i,   S'_i = S'_(i-1) + (l^-i k_i) v_i^T,   o_i = (l^i q_i)^T S'_i,
+// which leaves one FMA per element for the update and one for the output, two elements to an instruction.  A tile ends before
+// l^-i passes e^60; at l = 0 it is one token.
+template <typename T, int ROWS, int COLS, bool kStates>
+__global__ void __launch_bounds__(kRecThreads)
+decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
 {
-    constexpr int DK = ROWS * kRecWarps;
-    __shared__ __align__(16) float sq[kRecTile][DK], sk[kRecTile][DK];
-    __shared__ float sv[kRecTile][kRecCols], so[kRecTile][kRecWarps][kRecCols];
+    constexpr int DK = ROWS * kRecWarps, DV = COLS * 32;
+    __shared__ __align__(16) float sq[kStates ? 1 : kRecTile][DK], sk[kRecTile][DK];
+    __shared__ float sv[kRecTile][DV], so[kStates ? 1 : kRecTile][kRecWarps][DV], grow[kRecTile], shrink[kRecTile];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int h = blockIdx.y, hk = h / (g.H / g.Hk), c0 = blockIdx.z * kRecCols;
+    const int h = blockIdx.y, hk = h / (g.H / g.Hk);
+    const int slices = (g.Dv + DV - 1) / DV;
+    const int c0 = (int)(blockIdx.z % slices) * DV, seg = (int)(blockIdx.z / slices);
     const int64_t b = blockIdx.x;
     int64_t first, len, slot;
     if (!sequence_bounds(g, b, first, len, slot)) {
-        if (threadIdx.x == 0) atomicOr(g.status, kStatusBadIndex);
+        if (!kStates && threadIdx.x == 0 && seg == 0) atomicOr(g.status, kStatusBadIndex);
         return;
     }
-    const int cols = g.Dv - c0 < kRecCols ? g.Dv - c0 : kRecCols;
+    const int64_t s0 = (int64_t)seg * p.seg_len;
+    if (seg > 0 && s0 >= len) return;
+    const bool last_seg = s0 + p.seg_len >= len;
+    if (kStates && (last_seg || slot < 0)) return;
+    const int64_t n_tok = last_seg ? len - s0 : p.seg_len;
+    first += s0;
+    const int cols = g.Dv - c0 < DV ? g.Dv - c0 : DV;
     T* out = static_cast<T*>(g.out) + first * g.o_token + h * g.o_head + c0;
     if (slot < 0) {
-        for (int64_t i = threadIdx.x; i < len * cols; i += blockDim.x) out[(i / cols) * g.o_token + i % cols] = from_f32<T>(0.f);
+        for (int64_t i = threadIdx.x; i < n_tok * cols; i += kRecThreads) out[(i / cols) * g.o_token + i % cols] = from_f32<T>(0.f);
         return;
     }
     const T* q = static_cast<const T*>(g.q) + first * g.q_token + h * g.q_head;
     const T* k = static_cast<const T*>(g.k) + first * g.k_token + hk * g.k_head;
     const T* v = static_cast<const T*>(g.v) + first * g.v_token + hk * g.v_head + c0;
-    const float l = expf(g.log_decay[h]);
+    const float g2 = g.log_decay[h] * 1.4426950408889634f;
+    const float reach = 86.f / fmaxf(fabsf(g2), 1e-6f);                     // steps until |log2| passes 86 (about e^60)
+    const int tile = reach >= (float)(kRecTile - 1) ? kRecTile : 1 + (int)reach;
     const int64_t base = (slot * g.H + h) * (int64_t)g.Dk * g.Dv + c0 + lane;
-    float S[ROWS];
-    #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int r = warp * ROWS + i;
-        S[i] = g.state != nullptr && r < g.Dk && lane < cols ? g.state[base + (int64_t)r * g.Dv] : 0.f;
+    const int64_t local_base = ((b * g.H + h) * (int64_t)(p.segments - 1)) * g.Dk * g.Dv + c0 + lane;
+    pair_t S[COLS][ROWS / 2];
+    {
+        // the given state and what the segments before this one added, one whole slice after the other (every load of a slice in flight)
+        #pragma unroll
+        for (int c = 0; c < COLS; ++c)
+            #pragma unroll
+            for (int i = 0; i < ROWS / 2; ++i) S[c][i] = make_pair(0.f, 0.f);
+        auto add = [&](const float* src, float w) {
+            float x[COLS][ROWS];
+            #pragma unroll
+            for (int c = 0; c < COLS; ++c)
+                #pragma unroll
+                for (int i = 0; i < ROWS; ++i)
+                    x[c][i] = warp * ROWS + i < g.Dk && lane + 32 * c < cols ? src[(int64_t)(warp * ROWS + i) * g.Dv + 32 * c] : 0.f;
+            #pragma unroll
+            for (int c = 0; c < COLS; ++c)
+                #pragma unroll
+                for (int i = 0; i < ROWS; i += 2) S[c][i / 2] = fma_pair(make_pair(w, w), make_pair(x[c][i], x[c][i + 1]), S[c][i / 2]);
+        };
+        if constexpr (!kStates) {
+            const float w0 = power(g2, (float)s0);
+            if (g.state != nullptr && w0 != 0.f) add(g.state + base, w0);
+            for (int x = 0; x < seg; ++x) {
+                const float w = power(g2, (float)((int64_t)(seg - 1 - x) * p.seg_len));
+                if (w != 0.f) add(p.local + local_base + (int64_t)x * g.Dk * g.Dv, w);
+            }
+        }
     }
-    for (int64_t t0 = 0; t0 < len; t0 += kRecTile) {
-        const int n = len - t0 < kRecTile ? (int)(len - t0) : kRecTile;
-        for (int i = threadIdx.x; i < n * DK; i += blockDim.x) {
-            const int t = i / DK, d = i % DK;
-            sq[t][d] = d < g.Dk ? to_f32(q[(t0 + t) * g.q_token + d]) : 0.f;
-            sk[t][d] = d < g.Dk ? to_f32(k[(t0 + t) * g.k_token + d]) : 0.f;
+    auto decay = [&](float l) {
+        #pragma unroll
+        for (int c = 0; c < COLS; ++c)
+            #pragma unroll
+            for (int i = 0; i < ROWS / 2; ++i) S[c][i] = mul_pair(S[c][i], make_pair(l, l));
+    };
+    if (threadIdx.x < kRecTile) {
+        grow[threadIdx.x] = power(g2, -(float)threadIdx.x);             // (past the tile's length: not looked at)
+        shrink[threadIdx.x] = power(g2, (float)threadIdx.x);
+    }
+    __syncthreads();
+    // A tile's values on their way in registers while the tile before it is worked on: item i of a thread is token (128 i + thread) / DK,
+    // element (128 i + thread) mod DK.
+    constexpr int kPer = DK * kRecTile / kRecThreads, kPerV = DV * kRecTile / kRecThreads;
+    T rq[kStates ? 1 : kPer], rk[kPer], rv[kPerV];
+    auto fetch = [&](int64_t at, int n) {
+        const T *qt = q + at * g.q_token, *kt = k + at * g.k_token, *vt = v + at * g.v_token;
+        #pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int t = (i * kRecThreads + threadIdx.x) / DK, d = (i * kRecThreads + threadIdx.x) % DK;
+            const bool ok = t < n && d < g.Dk;
+            if constexpr (!kStates) rq[i] = ok ? qt[t * g.q_token + d] : from_f32<T>(0.f);
+            rk[i] = ok ? kt[t * g.k_token + d] : from_f32<T>(0.f);
         }
-        for (int i = threadIdx.x; i < n * kRecCols; i += blockDim.x) {
-            const int t = i / kRecCols, c = i % kRecCols;
-            sv[t][c] = c < cols ? to_f32(v[(t0 + t) * g.v_token + c]) : 0.f;
+        #pragma unroll
+        for (int i = 0; i < kPerV; ++i) {
+            const int t = (i * kRecThreads + threadIdx.x) / DV, c = (i * kRecThreads + threadIdx.x) % DV;
+            rv[i] = t < n && c < cols ? vt[t * g.v_token + c] : from_f32<T>(0.f);
         }
+    };
+    int64_t t0 = 0;
+    fetch(0, n_tok < tile ? (int)n_tok : tile);
+    while (t0 < n_tok) {
+        const int n = n_tok - t0 < tile ? (int)(n_tok - t0) : tile;
+        #pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int t = (i * kRecThreads + threadIdx.x) / DK, d = (i * kRecThreads + threadIdx.x) % DK;
+            if (t < n) {
+                if constexpr (!kStates) sq[t][d] = to_f32(rq[i]) * shrink[t];
+                sk[t][d] = to_f32(rk[i]) * grow[t];
+            }
+        }
+        #pragma unroll
+        for (int i = 0; i < kPerV; ++i) {
+            const int t = (i * kRecThreads + threadIdx.x) / DV, c = (i * kRecThreads + threadIdx.x) % DV;
+            if (t < n) sv[t][c] = to_f32(rv[i]);
+        }
+        const int64_t t1 = t0 + n;
+        fetch(t1, n_tok - t1 < tile ? (int)(n_tok - t1) : tile);
+        decay(power(g2, t0 == 0 ? 1.f : (float)tile));
         __syncthreads();
         for (int t = 0; t < n; ++t) {
-            const float vt = sv[t][lane];
+            pair_t vt[COLS], o[COLS];
+            #pragma unroll
+            for (int c = 0; c < COLS; ++c) {
+                const float x = sv[t][lane + 32 * c];
+                vt[c] = make_pair(x, x);
+                o[c] = make_pair(0.f, 0.f);
+            }
             const float4* k4 = reinterpret_cast<const float4*>(&sk[t][warp * ROWS]);
-            const float4* q4 = reinterpret_cast<const float4*>(&sq[t][warp * ROWS]);
-            float o0 = 0.f, o1 = 0.f;
+            const float4* q4 = reinterpret_cast<const float4*>(&sq[kStates ? 0 : t][warp * ROWS]);
             #pragma unroll
             for (int i = 0; i < ROWS / 4; ++i) {
-                const float4 kk = k4[i], qq = q4[i];
-                S[4 * i] = fmaf(l, S[4 * i], kk.x * vt);             o0 = fmaf(qq.x, S[4 * i], o0);
-                S[4 * i + 1] = fmaf(l, S[4 * i + 1], kk.y * vt);     o1 = fmaf(qq.y, S[4 * i + 1], o1);
-                S[4 * i + 2] = fmaf(l, S[4 * i + 2], kk.z * vt);     o0 = fmaf(qq.z, S[4 * i + 2], o0);
-                S[4 * i + 3] = fmaf(l, S[4 * i + 3], kk.w * vt);     o1 = fmaf(qq.w, S[4 * i + 3], o1);
+                const float4 kk = k4[i];
+                const pair_t ka = make_pair(kk.x, kk.y), kb = make_pair(kk.z, kk.w);
+                #pragma unroll
+                for (int c = 0; c < COLS; ++c) {
+                    S[c][2 * i] = fma_pair(ka, vt[c], S[c][2 * i]);
+                    S[c][2 * i + 1] = fma_pair(kb, vt[c], S[c][2 * i + 1]);
+                }
+                if constexpr (!kStates) {
+                    const float4 qq = q4[i];
+                    const pair_t qa = make_pair(qq.x, qq.y), qb = make_pair(qq.z, qq.w);
+                    #pragma unroll
+                    for (int c = 0; c < COLS; ++c) {
+                        o[c] = fma_pair(qa, S[c][2 * i], o[c]);
+                        o[c] = fma_pair(qb, S[c][2 * i + 1], o[c]);
+                    }
+                }
             }
-            so[t][warp][lane] = o0 + o1;
+            if constexpr (!kStates) {
+                #pragma unroll
+                for (int c = 0; c < COLS; ++c) {
+                    float a, b2;
+                    take_pair(o[c], a, b2);
+                    so[t][warp][lane + 32 * c] = a + b2;
+                }
+            }
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < n * cols; i += blockDim.x) {
-            const int t = i / cols, c = i % cols;
-            const float o = (so[t][0][c] + so[t][1][c]) + (so[t][2][c] + so[t][3][c]);
-            out[(t0 + t) * g.o_token + c] = from_f32<T>(g.scale * o);
+        if constexpr (!kStates) {
+            for (int i = threadIdx.x; i < n * cols; i += kRecThreads) {
+                const int t = i / cols, c = i % cols;
+                const float o = (so[t][0][c] + so[t][1][c]) + (so[t][2][c] + so[t][3][c]);
+                out[(t0 + t) * g.o_token + c] = from_f32<T>(g.scale * o);
+            }
         }
-        __syncthreads();
+        t0 += n;
+        if (t0 >= n_tok) decay(power(g2, (float)(n - 1)));
     }
+    if (!kStates && !last_seg) return;
+    float* dst = kStates ? p.local + local_base + (int64_t)seg * g.Dk * g.Dv : g.state_out + base;
     #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int r = warp * ROWS + i;
-        if (r < g.Dk && lane < cols) g.state_out[base + (int64_t)r * g.Dv] = S[i];
+    for (int i = 0; i < ROWS; i += 2)
+        #pragma unroll
+        for (int c = 0; c < COLS; ++c) {
+            float s[2];
+            take_pair(S[c][i / 2], s[0], s[1]);
+            #pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = warp * ROWS + i + e;
+                if (r < g.Dk && lane + 32 * c < cols) dst[(int64_t)r * g.Dv + 32 * c] = s[e];
+            }
+        }
+}
+
+template <typename T, int ROWS, int COLS>
+cudaError_t launch_recurrent_rows(const DecayArgs& g, cudaStream_t s)
+{
+    const int slices = (g.Dv + COLS * 32 - 1) / (COLS * 32);
+    // Few heads and long prompts: segments, until about four CTAs per SM walk a share of the tokens each; one launch finds what
+    // each adds to the state, the next starts each from the decayed sum of what came before it.
+    RecPlan p{};
+    const int64_t ctas = g.B * g.H * slices;
+    int64_t segs = 4 * (int64_t)device_sm_count() / ctas;
+    if (segs > g.max_len / 128) segs = g.max_len / 128;
+    if (segs > 16) segs = 16;
+    if (segs < 1) segs = 1;
+    p.seg_len = (g.max_len + segs - 1) / segs;
+    if (p.seg_len < 1) p.seg_len = 1;
+    p.segments = (int)((g.max_len + p.seg_len - 1) / p.seg_len);
+    if (p.segments < 1) p.segments = 1;
+    cudaError_t e = cudaSuccess;
+    void* scratch = nullptr;
+    if (p.segments > 1) {
+        e = scratch_alloc(&scratch, (size_t)g.B * g.H * (p.segments - 1) * g.Dk * g.Dv * sizeof(float), s);
+        if (e != cudaSuccess) return e;
+        p.local = static_cast<float*>(scratch);
+        decay_recurrent_kernel<T, ROWS, COLS, true><<<dim3((unsigned)g.B, (unsigned)g.H, (unsigned)(slices * (p.segments - 1))), kRecThreads, 0, s>>>(g, p);
+        e = cudaGetLastError();
     }
+    if (e == cudaSuccess) {
+        decay_recurrent_kernel<T, ROWS, COLS, false><<<dim3((unsigned)g.B, (unsigned)g.H, (unsigned)(slices * p.segments)), kRecThreads, 0, s>>>(g, p);
+        e = cudaGetLastError();
+    }
+    if (scratch != nullptr) {
+        const cudaError_t e2 = cudaFreeAsync(scratch, s);
+        if (e == cudaSuccess) e = e2;
+    }
+    return e;
 }
 
 template <typename T>
 cudaError_t launch_recurrent_typed(const DecayArgs& g, cudaStream_t s)
 {
-    const dim3 grid((unsigned)g.B, (unsigned)g.H, (unsigned)((g.Dv + kRecCols - 1) / kRecCols));
-    if (g.Dk <= 64) decay_recurrent_kernel<T, 16><<<grid, kRecCols * kRecWarps, 0, s>>>(g);
-    else if (g.Dk <= 128) decay_recurrent_kernel<T, 32><<<grid, kRecCols * kRecWarps, 0, s>>>(g);
-    else decay_recurrent_kernel<T, 64><<<grid, kRecCols * kRecWarps, 0, s>>>(g);
-    return cudaGetLastError();
+    if (g.Dk <= 64) return launch_recurrent_rows<T, 16, 2>(g, s);
+    if (g.Dk <= 128) return launch_recurrent_rows<T, 32, 2>(g, s);
+    return launch_recurrent_rows<T, 64, 1>(g, s);
 }
 
 }  // namespace

@@ -7,16 +7,18 @@ namespace rtn {
 
 #ifdef __CUDACC__
 
-__device__ __forceinline__ float activate(float y, int act)
+// One copy of the code, called: inlined at every unrolled output it was most of a kernel's instructions, and a short kernel's time is
+// made of fetching them.
+static __device__ __noinline__ float activation(float y, int act)
 {
     switch (act) {
         case RTN_ACT_RELU: return y < 0.f ? 0.f : y;                                     // a NaN stays one
         case RTN_ACT_GELU: return 0.5f * y * (1.f + erff(y * 0.70710678118654752f));
         case RTN_ACT_GELU_TANH: return 0.5f * y * (1.f + tanhf(0.79788456080286536f * fmaf(0.044715f * y * y, y, y)));
-        case RTN_ACT_SILU: return y / (1.f + expf(-y));
-        default: return y;
+        default: return y / (1.f + expf(-y));
     }
 }
+__device__ __forceinline__ float activate(float y, int act) { return act == RTN_ACT_NONE ? y : activation(y, act); }
 
 __device__ __forceinline__ float load_as_f32(const void* p, int64_t i, int dtype)
 {

@@ -7,6 +7,7 @@
 // counter pair per activation row and column, and one shuffle tree joins the group.  CPG columns at once keep that many loads in flight.
 #include "rtn_internal.cuh"
 #include "rtn_epilogue.cuh"
+#include "rtn_tcgen05.cuh"
 
 namespace rtn {
 
@@ -19,6 +20,7 @@ template <int MT, int CPG>
 __global__ void __launch_bounds__(kThreads)
 linear_rows_kernel(const GemmArgs g, const LinearArgs p, int GL)
 {
+    constexpr int kOut = MT * CPG;
     const int gl = threadIdx.x & (GL - 1);
     const int64_t group = (int64_t)blockIdx.x * (kThreads / GL) + threadIdx.x / GL;
     const int64_t n0 = group * CPG;
@@ -26,11 +28,29 @@ linear_rows_kernel(const GemmArgs g, const LinearArgs p, int GL)
     const int64_t nblk = (g.K + kBlockCodes - 1) / kBlockCodes;
     const uint4* __restrict__ A = reinterpret_cast<const uint4*>(g.a_packed);
     const uint4* __restrict__ W = reinterpret_cast<const uint4*>(g.w_packed);
-    int cnt[MT][CPG];
+    int cnt[kOut];
     #pragma unroll
-    for (int i = 0; i < MT; ++i)
-        #pragma unroll
-        for (int j = 0; j < CPG; ++j) cnt[i][j] = 0;
+    for (int i = 0; i < kOut; ++i) cnt[i] = 0;
+    // Lane o of the group finishes outputs o, o + GL, ... of its MT x CPG; the operands of the first are on their way during the loop
+    // (fetched after it, one output after the other, they were most of the time of a small call).
+    struct Params { float as, ao, ws, wo, bias, res; int sx, sw; bool ok; };
+    auto fetch = [&](int o) {
+        Params q;
+        const int64_t m = m0 + o / CPG, n = n0 + o % CPG;
+        q.ok = o < kOut && m < g.M && n < g.N;
+        q.as = q.ao = q.ws = q.wo = q.bias = q.res = 0.f;
+        q.sx = q.sw = 0;
+        if (q.ok) {
+            const EpilogueParams& ep = g.ep;
+            const int64_t ia = ep.n_aparam == 1 ? 0 : m, iw = ep.n_wparam == 1 ? 0 : n;
+            q.as = ep.a_scale[ia]; q.ao = ep.a_offset[ia]; q.ws = ep.w_scale[iw]; q.wo = ep.w_offset[iw];
+            q.sx = g.a_sum[m]; q.sw = g.w_sum[n];
+            if (p.bias != nullptr) q.bias = p.bias[n];
+            if (p.residual != nullptr) q.res = load_as_f32(p.residual, m * p.res_stride + n, p.dtype);
+        }
+        return q;
+    };
+    Params first = fetch(gl);
     for (int64_t kb = gl; kb < nblk; kb += GL) {
         uint4 w1[CPG], w2[CPG];
         #pragma unroll
@@ -48,34 +68,315 @@ linear_rows_kernel(const GemmArgs g, const LinearArgs p, int GL)
             #pragma unroll
             for (int j = 0; j < CPG; ++j) {
                 const uint32_t c0 = a1.x & w1[j].x, c1 = a1.y & w1[j].y, c2 = a1.z & w1[j].z, c3 = a1.w & w1[j].w;
-                cnt[i][j] += (__popc(c0) + __popc(c1)) + (__popc(c2) + __popc(c3))
-                           - 2 * ((__popc((a2.x ^ w2[j].x) & c0) + __popc((a2.y ^ w2[j].y) & c1)) +
-                                  (__popc((a2.z ^ w2[j].z) & c2) + __popc((a2.w ^ w2[j].w) & c3)));
+                cnt[i * CPG + j] += (__popc(c0) + __popc(c1)) + (__popc(c2) + __popc(c3))
+                                  - 2 * ((__popc((a2.x ^ w2[j].x) & c0) + __popc((a2.y ^ w2[j].y) & c1)) +
+                                         (__popc((a2.z ^ w2[j].z) & c2) + __popc((a2.w ^ w2[j].w) & c3)));
             }
         }
     }
     for (int d = GL / 2; d > 0; d >>= 1) {
         #pragma unroll
-        for (int i = 0; i < MT; ++i)
-            #pragma unroll
-            for (int j = 0; j < CPG; ++j) cnt[i][j] += __shfl_xor_sync(0xffffffffu, cnt[i][j], d);
+        for (int i = 0; i < kOut; ++i) cnt[i] += __shfl_xor_sync(0xffffffffu, cnt[i], d);
     }
-    // lane j of the group finishes outputs j, j + GL, ... of its MT x CPG
-    #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int o = gl; o < kOut; o += GL) {
+        const Params q = o == gl ? first : fetch(o);
+        int s = 0;
         #pragma unroll
-        for (int j = 0; j < CPG; ++j) {
-            const int64_t m = m0 + i, n = n0 + j;
-            if (((i * CPG + j) & (GL - 1)) != gl || m >= g.M || n >= g.N) continue;
-            const EpilogueParams& ep = g.ep;
-            const int64_t ia = ep.n_aparam == 1 ? 0 : m, iw = ep.n_wparam == 1 ? 0 : n;
-            float y = epilogue_f64(cnt[i][j], g.a_sum[m], g.w_sum[n], (double)g.K, ep.a_scale[ia], ep.a_offset[ia],
-                                   ep.w_scale[iw], ep.w_offset[iw]);
-            if (p.bias != nullptr) y += p.bias[n];
-            y = activate(y, p.act);
-            if (p.residual != nullptr) y += load_as_f32(p.residual, m * p.res_stride + n, p.dtype);
-            store_from_f32(p.out, m * p.out_stride + n, p.dtype, y);
+        for (int i = 0; i < kOut; ++i) s = o == i ? cnt[i] : s;
+        if (!q.ok) continue;
+        // the arithmetic of the tensor-core forms, so that a row's result does not depend on how many rows it comes with
+        const float p3 = (float)((double)q.ws * (double)q.sw + (double)g.K * (double)q.wo);
+        const float y = activate(fmaf(q.as, fmaf(q.ws, (float)s, q.wo * (float)q.sx), q.ao * p3) + q.bias, p.act) + q.res;
+        store_from_f32(p.out, (m0 + o / CPG) * p.out_stride + n0 + o % CPG, p.dtype, y);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ some to many rows, small products
+
+// linear_tiles_kernel: 128 weight rows (the MMA's M, lanes of tensor memory) by BT tokens (its N), tcgen05.mma kind::i8.  Sixteen
+// warps expand the bit planes of both operands into a ring of 4, 8 or 16 stages, a team of 4, 2 or 1 warps to a stage and a whole
+// K = 128 block at a time (several rows per lane in flight, and no team waits for another); a seventeenth issues the MMAs; then the
+// sixteen write out.  A lane is one output column: its scale, offset, code sum and bias live in registers, and a warp's
+// store is 32 adjacent columns of a token, with no staging.
+// Bound: the integer pipe (about 100 instructions per row and block to expand) while the weights stream by; the epilogue for short K.
+// Few tiles and a long K: the K blocks are dealt to the CTAs of a cluster, which leave their int32 sums in shared memory and
+// each finish a share of the tokens from all of them (exact whatever the order).
+constexpr int kTileWarps = 16;
+constexpr int kTileThreads = (kTileWarps + 1) * 32;
+constexpr int kTileRing = 192 * 1024;           // bytes of stages
+constexpr int kTileMaxStages = 16;
+constexpr int kTileMaxTokens = 256;
+constexpr uint32_t kTileTries = 1u << 20;
+
+struct TilePlan {
+    int BT;                 // tokens of a tile, a multiple of 16
+    int tiles_n, tiles_m;
+    int slices;             // CTAs of a cluster, along K
+    int stages;
+    uint32_t tmem_cols;
+    uint32_t smem_bytes;
+};
+
+struct TileBars {
+    uint64_t full[kTileMaxStages], empty[kTileMaxStages], acc;
+    uint32_t tmem_slot;
+    int dead;
+};
+
+// One packed 128-code block of a row, expanded to eight 16-byte chunks `ld` rows apart.
+__device__ __forceinline__ void expand_block(const uint4& nz, const uint4& sg, uint4* dst, int ld)
+{
+    uint32_t o[8];
+    tc::unpack32(nz.x, sg.x, o);
+    dst[0 * ld] = make_uint4(o[0], o[1], o[2], o[3]); dst[1 * ld] = make_uint4(o[4], o[5], o[6], o[7]);
+    tc::unpack32(nz.y, sg.y, o);
+    dst[2 * ld] = make_uint4(o[0], o[1], o[2], o[3]); dst[3 * ld] = make_uint4(o[4], o[5], o[6], o[7]);
+    tc::unpack32(nz.z, sg.z, o);
+    dst[4 * ld] = make_uint4(o[0], o[1], o[2], o[3]); dst[5 * ld] = make_uint4(o[4], o[5], o[6], o[7]);
+    tc::unpack32(nz.w, sg.w, o);
+    dst[6 * ld] = make_uint4(o[0], o[1], o[2], o[3]); dst[7 * ld] = make_uint4(o[4], o[5], o[6], o[7]);
+}
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kTileThreads, 1)
+linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
+{
+    extern __shared__ __align__(128) uint8_t smem[];
+    TileBars& bar = *reinterpret_cast<TileBars*>(smem);
+    float4* token = reinterpret_cast<float4*>(smem + 512);                  // {a_s, a_o, S_x, -} of the tile's tokens
+    uint8_t* ring = smem + 512 + kTileMaxTokens * 16;
+    static_assert(sizeof(TileBars) <= 512, "barriers");
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int rank = (int)(blockIdx.x % p.slices);
+    const int tile = (int)(blockIdx.x / p.slices);
+    const int64_t n0 = (int64_t)(tile / p.tiles_m) * 128, m0 = (int64_t)(tile % p.tiles_m) * p.BT;
+    const int nblk = (int)((g.K + kBlockCodes - 1) / kBlockCodes);
+    const int kb0 = (int)((int64_t)nblk * rank / p.slices), kb1 = (int)((int64_t)nblk * (rank + 1) / p.slices);
+    const uint32_t stage_bytes = (uint32_t)(128 + p.BT) * 128u;
+    volatile int* dead = &bar.dead;
+
+    if (warp == kTileWarps) tc::tmem_alloc(&bar.tmem_slot, p.tmem_cols);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < p.stages; ++i) { tc::mbar_init(&bar.full[i], kTileWarps / p.stages); tc::mbar_init(&bar.empty[i], 1); }
+        tc::mbar_init(&bar.acc, 1);
+        tc::mbar_init_fence();
+        bar.dead = 0;
+    }
+    // the epilogue's operands, asked for now and looked at after the loop: a token's (one per thread), a column's
+    const int quad = warp & 3;
+    const int64_t n = n0 + quad * 32 + lane;
+    const bool col_ok = n < g.N && warp < kTileWarps;
+    float t_s = 0.f, t_o = 0.f, w_s = 0.f, w_o = 0.f, bias = 0.f;
+    int t_x = 0, w_x = 0;
+    if (threadIdx.x < p.BT && m0 + threadIdx.x < g.M) {
+        const int64_t m = m0 + threadIdx.x;
+        t_s = g.ep.a_scale[g.ep.n_aparam == 1 ? 0 : m]; t_o = g.ep.a_offset[g.ep.n_aparam == 1 ? 0 : m]; t_x = g.a_sum[m];
+    }
+    if (col_ok) {
+        w_s = g.ep.w_scale[g.ep.n_wparam == 1 ? 0 : n]; w_o = g.ep.w_offset[g.ep.n_wparam == 1 ? 0 : n]; w_x = g.w_sum[n];
+        if (l.bias != nullptr) bias = l.bias[n];
+    }
+    tc::tc_fence_before_sync();
+    __syncthreads();
+    tc::tc_fence_after_sync();
+    const uint32_t tmem = bar.tmem_slot;
+    auto warp_wait = [&](uint64_t* m, uint32_t parity) {
+        const bool ok = __all_sync(0xffffffffu, tc::mbar_wait_tries(m, parity & 1u, kTileTries)) != 0;
+        if (!ok) *dead = 1;
+        return ok;
+    };
+
+    if (warp < kTileWarps) {
+        // ------------------------------------------------------------ expand: the warps of a team own one stage, so that a stage's
+        // phases follow each other in one program order; a team's warps take 32-row groups of the block in turn
+        const uint4* __restrict__ W = reinterpret_cast<const uint4*>(g.w_packed);
+        const uint4* __restrict__ X = reinterpret_cast<const uint4*>(g.a_packed);
+        const int team_warps = kTileWarps / p.stages, s = warp / team_warps, member = warp % team_warps;
+        const int row_groups = 4 + (p.BT + 31) / 32;
+        uint4* dst = reinterpret_cast<uint4*>(ring + s * stage_bytes);
+        // Items: block i, row groups first, first + team_warps, ... (four at most); the next item's planes are on their way while this
+        // one's are expanded.
+        uint4 nz[4], sg[4];
+        auto load = [&](int i, int first) {
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int rg = first + k * team_warps;
+                const bool isW = rg < 4;
+                const int r = (isW ? rg : rg - 4) * 32 + lane;
+                const int64_t row = (isW ? n0 : m0) + r;
+                const bool ok = i < kb1 - kb0 && rg < row_groups && (isW || r < p.BT) && row < (isW ? g.N : g.M);
+                nz[k] = sg[k] = make_uint4(0, 0, 0, 0);
+                if (ok) { const uint4* q = (isW ? W : X) + (row * nblk + kb0 + i) * 2; nz[k] = __ldg(q); sg[k] = __ldg(q + 1); }
+            }
+        };
+        int i = s, first = member;
+        load(i, first);
+        while (i < kb1 - kb0) {
+            if (first == member && !warp_wait(&bar.empty[s], (uint32_t)(i / p.stages) + 1)) break;
+            uint4 cnz[4], csg[4];
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) { cnz[k] = nz[k]; csg[k] = sg[k]; }
+            const int now = first;
+            first += 4 * team_warps;
+            const bool last = first >= row_groups;
+            if (last) { first = member; i += p.stages; }
+            load(i, first);
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int rg = now + k * team_warps;
+                if (rg < 4) expand_block(cnz[k], csg[k], dst + rg * 32 + lane, 128);
+                else if (rg < row_groups && (rg - 4) * 32 + lane < p.BT) expand_block(cnz[k], csg[k], dst + 128 * 8 + (rg - 4) * 32 + lane, p.BT);
+            }
+            if (last) {
+                tc::fence_smem_to_async_proxy();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&bar.full[s]);
+            }
         }
+        if (threadIdx.x < p.BT) token[threadIdx.x] = make_float4(t_s, t_o, (float)t_x, 0.f);
+        asm volatile("bar.sync 1, %0;" ::"n"(kTileWarps * 32) : "memory");
+    } else {
+        // ------------------------------------------------------------ MMA
+        const uint32_t elected = tc::elect_one();
+        const uint32_t idesc = tc::idesc_i8(128, (uint32_t)p.BT);
+        const uint32_t at = tc::smem_addr(ring);
+        const uint64_t desc_w = tc::smem_desc_kmajor(at, 2048, 128), desc_x = tc::smem_desc_kmajor(at + 128u * 128u, (uint32_t)p.BT * 16u, 128);
+        bool alive = true;
+        for (int i = 0; i < kb1 - kb0; ++i) {
+            const int s = i & (p.stages - 1);
+            if (!(alive = warp_wait(&bar.full[s], (uint32_t)(i / p.stages)))) break;
+            tc::tc_fence_after_sync();
+            const uint64_t step = (uint64_t)(s * (stage_bytes >> 4));          // descriptors count 16 bytes
+            #pragma unroll
+            for (int j = 0; j < 4; ++j)                             // K = 32: chunks 2j and 2j + 1
+                tc::mma_i8_ss(elected, tmem, desc_w + step + (uint64_t)(j * 256), desc_x + step + (uint64_t)(j * 2 * p.BT), idesc, i > 0 || j > 0);
+            if (elected) tc::mma_commit(&bar.empty[s]);
+            __syncwarp();
+        }
+        if (elected && alive) tc::mma_commit(&bar.acc);
+        __syncwarp();
+    }
+
+    // ---------------------------------------------------------------- write out: column n0 + 32 (warp mod 4) + lane, every fourth
+    // group of 8 tokens of the CTA's share
+    const bool done = warp_wait(&bar.acc, 0);
+    tc::tc_fence_after_sync();
+    const int groups = p.BT / 8;
+    int* part = reinterpret_cast<int*>(ring);                        // [token][128]
+    if (p.slices > 1) {
+        if (warp < kTileWarps && done) {
+            for (int q = warp >> 2; q < groups; q += kTileWarps / 4) {
+                uint32_t v[8];
+                tc::tmem_ld8(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(q * 8), v);
+                tc::tmem_ld_wait();
+                #pragma unroll
+                for (int x = 0; x < 8; ++x) part[(q * 8 + x) * 128 + quad * 32 + lane] = (int)v[x];
+            }
+        }
+        cluster_sync();
+    }
+    if (warp < kTileWarps && done && !(p.slices > 1 && *dead)) {
+        const float p3 = (float)((double)w_s * (double)w_x + (double)g.K * (double)w_o);
+        const T* res = static_cast<const T*>(l.residual);
+        T* out = static_cast<T*>(l.out);
+        for (int q = (warp >> 2) * p.slices + rank; q < groups; q += kTileWarps / 4 * p.slices) {
+            uint32_t v[8];
+            if (p.slices == 1) {
+                tc::tmem_ld8(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(q * 8), v);
+            } else {
+                #pragma unroll
+                for (int x = 0; x < 8; ++x) v[x] = 0;
+                for (int r = 0; r < p.slices; ++r) {
+                    const uint32_t mine = tc::smem_addr(part + q * 8 * 128 + quad * 32 + lane);
+                    uint32_t at;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(mine), "r"(r));
+                    #pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        uint32_t y;
+                        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(y) : "r"(at + (uint32_t)x * 512u) : "memory");
+                        v[x] += y;
+                    }
+                }
+            }
+            float add[8];
+            #pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const int64_t m = m0 + q * 8 + x;
+                add[x] = res != nullptr && col_ok && m < g.M ? to_f32(res[m * l.res_stride + n]) : 0.f;
+            }
+            if (p.slices == 1) tc::tmem_ld_wait();
+            #pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const int64_t m = m0 + q * 8 + x;
+                const float4 t = token[q * 8 + x];
+                const float y = activate(fmaf(t.x, fmaf(w_s, (float)(int)v[x], w_o * t.z), t.y * p3) + bias, l.act) + add[x];
+                if (col_ok && m < g.M) out[m * l.out_stride + n] = from_f32<T>(y);
+            }
+        }
+    }
+    if (p.slices > 1) cluster_sync();            // nobody leaves while its sums are read
+    if (threadIdx.x == 0 && *dead) atomicOr(g.status, kStatusWaitTimeout);
+    tc::tc_fence_before_sync();
+    __syncthreads();
+    tc::tc_fence_after_sync();
+    if (warp == kTileWarps) tc::tmem_dealloc(tmem, p.tmem_cols);
+}
+
+TilePlan make_tile_plan(int64_t M, int64_t N, int64_t K)
+{
+    TilePlan p{};
+    const int sms = device_sm_count();
+    const int nblk = (int)((K + kBlockCodes - 1) / kBlockCodes);
+    p.tiles_n = (int)((N + 127) / 128);
+    // Tokens of a tile: what makes rounds of CTAs times a tile's time least.  Per block the slower of expanding 128 + BT rows (1.6
+    // clocks each) and the MMAs (2 BT); 30 clocks per token for the epilogue; 4000 to start and end.
+    double best = 0.0;
+    const int most = M >= kTileMaxTokens ? kTileMaxTokens : (int)((M + 15) / 16 * 16);
+    for (int bt = 16; bt <= most; bt += 16) {
+        if (bt > 128 && bt % 32 != 0 && bt != most) continue;
+        const int64_t tiles = (int64_t)p.tiles_n * ((M + bt - 1) / bt);
+        const double block = 1.6 * (128 + bt) > 2.0 * bt ? 1.6 * (128 + bt) : 2.0 * bt;
+        const double cost = (double)((tiles + sms - 1) / sms) * (4000.0 + nblk * block + 30.0 * bt);
+        if (p.BT == 0 || cost < best) { best = cost; p.BT = bt; }
+    }
+    p.tiles_m = (int)((M + p.BT - 1) / p.BT);
+    // K over a cluster while it leaves a CTA at least four blocks and the machine has the SMs
+    p.slices = 1;
+    while (p.slices < 8 && (int64_t)p.tiles_n * p.tiles_m * p.slices * 2 <= sms && nblk >= p.slices * 8) p.slices *= 2;
+    const int stage = (128 + p.BT) * 128;
+    p.stages = kTileMaxStages;                  // a power of two: a team of warps for each
+    while (p.stages * stage > kTileRing) p.stages /= 2;
+    p.tmem_cols = 32;
+    while (p.tmem_cols < (uint32_t)p.BT) p.tmem_cols *= 2;
+    p.smem_bytes = 512 + kTileMaxTokens * 16 + (uint32_t)(p.stages * stage);
+    return p;
+}
+
+cudaError_t launch_tiles(const GemmArgs& g, const LinearArgs& l, const TilePlan& p, cudaStream_t s)
+{
+    return with_dtype(l.dtype, [&](auto t) {
+        auto kernel = linear_tiles_kernel<decltype(t)>;
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
+        if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cfg.gridDim = dim3((unsigned)(p.tiles_n * p.tiles_m * p.slices));
+        cfg.blockDim = dim3(kTileThreads);
+        cfg.dynamicSmemBytes = p.smem_bytes;
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)p.slices;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, kernel, g, l, p);
+    });
 }
 
 template <int MT, int CPG>
@@ -92,15 +393,29 @@ cudaError_t launch_rows(const GemmArgs& g, const LinearArgs& l, cudaStream_t s)
 
 }  // namespace
 
-// Few rows: the weights are streamed once through the bit-plane kernel.
+// Which of the three forms a shape takes; times in a graph on one B200 (bf16 out, us):
+//                      M   N     K      rows   tiles  two launches
+//   rows              16  4096  4096     9.8   12.0   26.5
+//                     48  1000   512     5.0    8.4    8.9
+//   tiles             24  4096  4096    13.5   14.3   26.5        16  4096 16384  24.2  19.1  85.9
+//                    256  4096  4096           21.4   23.1
+//   two launches     512  4096  4096           26.2   23.0       256 16384  4096        44.0  36.4
+// rows: the weights are streamed once per eight rows and the POPC rate binds, 2.9 us per million rows x columns x blocks, on top of 4; tiles
+// start at 8 and never under 0.3 us per block of K.  Over 64 tokens a tile, or over one round of tiles, the weights' planes are
+// better expanded once, by a launch of their own.
 bool linear_rows_path(int64_t M, int64_t N, int64_t K)
 {
-    return M <= kMaxRows || !gemm_i8_supported(M, N, K);
+    return M <= kMaxRows || (double)M * (double)N * (double)((K + kBlockCodes - 1) / kBlockCodes) <= 2.5e6 || !gemm_i8_supported(M, N, K);
 }
 
 cudaError_t launch_linear(const GemmArgs& g, const LinearArgs& l, cudaStream_t s)
 {
-    if (!linear_rows_path(g.M, g.N, g.K)) return launch_gemm_i8_linear(g, l, s);
+    if (!linear_rows_path(g.M, g.N, g.K)) {
+        if ((g.N + 127) / 128 > device_sm_count()) return launch_gemm_i8_linear(g, l, s);
+        const TilePlan p = make_tile_plan(g.M, g.N, g.K);
+        const bool one_round = (int64_t)p.tiles_n * p.tiles_m <= device_sm_count();
+        return one_round && p.BT <= 64 ? launch_tiles(g, l, p, s) : launch_gemm_i8_linear(g, l, s);
+    }
     if (g.M == 1) return launch_rows<1, 4>(g, l, s);
     if (g.M == 2) return launch_rows<2, 4>(g, l, s);
     if (g.M <= 4) return launch_rows<4, 4>(g, l, s);
