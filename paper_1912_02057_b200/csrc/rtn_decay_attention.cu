@@ -115,7 +115,7 @@ constexpr int kRecTile = 16;            // tokens staged at a time, at most
 struct RecPlan {
     int64_t seg_len;        // tokens of a segment
     int segments;           // of the longest sequence
-    float* local;           // [B][H][segments - 1][Dk][Dv]: what a segment adds to the state
+    float* local;           // [B][H][segments][Dk][Dv]: the state before the first segment, then what each but the last adds to it
 };
 
 // l^n from log2 l; n = 0 gives 1 for every l.
@@ -162,8 +162,22 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
     const float reach = 86.f / fmaxf(fabsf(g2), 1e-6f);                     // steps until |log2| passes 86 (about e^60)
     const int tile = reach >= (float)(kRecTile - 1) ? kRecTile : 1 + (int)reach;
     const int64_t base = (slot * g.H + h) * (int64_t)g.Dk * g.Dv + c0 + lane;
-    const int64_t local_base = ((b * g.H + h) * (int64_t)(p.segments - 1)) * g.Dk * g.Dv + c0 + lane;
+    const int64_t slice = (int64_t)g.Dk * g.Dv, local_base = (b * g.H + h) * (int64_t)p.segments * slice + c0 + lane;
     pair_t S[COLS][ROWS / 2];
+    auto store = [&](float* dst) {
+        #pragma unroll
+        for (int i = 0; i < ROWS; i += 2)
+            #pragma unroll
+            for (int c = 0; c < COLS; ++c) {
+                float s[2];
+                take_pair(S[c][i / 2], s[0], s[1]);
+                #pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = warp * ROWS + i + e;
+                    if (r < g.Dk && lane + 32 * c < cols) dst[(int64_t)r * g.Dv + 32 * c] = s[e];
+                }
+            }
+    };
     {
         // the given state and what the segments before this one added, one whole slice after the other (every load of a slice in flight)
         #pragma unroll
@@ -182,12 +196,23 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
                 #pragma unroll
                 for (int i = 0; i < ROWS; i += 2) S[c][i / 2] = fma_pair(make_pair(w, w), make_pair(x[c][i], x[c][i + 1]), S[c][i / 2]);
         };
-        if constexpr (!kStates) {
+        if constexpr (kStates) {
+            // The last segment's CTA writes state_out, which may be the state itself, while other segments may not have begun: they take
+            // the given state from the scratch.
+            if (seg == 0 && g.state != nullptr) {
+                add(g.state + base, 1.f);
+                store(p.local + local_base);
+                #pragma unroll
+                for (int c = 0; c < COLS; ++c)
+                    #pragma unroll
+                    for (int i = 0; i < ROWS / 2; ++i) S[c][i] = make_pair(0.f, 0.f);
+            }
+        } else {
             const float w0 = power(g2, (float)s0);
-            if (g.state != nullptr && w0 != 0.f) add(g.state + base, w0);
+            if (g.state != nullptr && w0 != 0.f) add(seg == 0 && last_seg ? g.state + base : p.local + local_base, w0);
             for (int x = 0; x < seg; ++x) {
                 const float w = power(g2, (float)((int64_t)(seg - 1 - x) * p.seg_len));
-                if (w != 0.f) add(p.local + local_base + (int64_t)x * g.Dk * g.Dv, w);
+                if (w != 0.f) add(p.local + local_base + (x + 1) * slice, w);
             }
         }
     }
@@ -291,20 +316,8 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
         t0 += n;
         if (t0 >= n_tok) decay(power(g2, (float)(n - 1)));
     }
-    if (!kStates && !last_seg) return;
-    float* dst = kStates ? p.local + local_base + (int64_t)seg * g.Dk * g.Dv : g.state_out + base;
-    #pragma unroll
-    for (int i = 0; i < ROWS; i += 2)
-        #pragma unroll
-        for (int c = 0; c < COLS; ++c) {
-            float s[2];
-            take_pair(S[c][i / 2], s[0], s[1]);
-            #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = warp * ROWS + i + e;
-                if (r < g.Dk && lane + 32 * c < cols) dst[(int64_t)r * g.Dv + 32 * c] = s[e];
-            }
-        }
+    if (kStates) store(p.local + local_base + (seg + 1) * slice);
+    else if (last_seg) store(g.state_out + base);
 }
 
 template <typename T, int ROWS, int COLS>
@@ -326,7 +339,7 @@ cudaError_t launch_recurrent_rows(const DecayArgs& g, cudaStream_t s)
     cudaError_t e = cudaSuccess;
     void* scratch = nullptr;
     if (p.segments > 1) {
-        e = scratch_alloc(&scratch, (size_t)g.B * g.H * (p.segments - 1) * g.Dk * g.Dv * sizeof(float), s);
+        e = scratch_alloc(&scratch, (size_t)g.B * g.H * p.segments * g.Dk * g.Dv * sizeof(float), s);
         if (e != cudaSuccess) return e;
         p.local = static_cast<float*>(scratch);
         decay_recurrent_kernel<T, ROWS, COLS, true><<<dim3((unsigned)g.B, (unsigned)g.H, (unsigned)(slices * (p.segments - 1))), kRecThreads, 0, s>>>(g, p);

@@ -85,7 +85,7 @@ static_assert(sizeof(Bars) <= 512, "barriers");
 struct ChunkPlan {
     int64_t seg_len;        // tokens of a segment, a multiple of kC
     int segments;           // of the longest sequence
-    float* local;           // [B][H][segments - 1][D][D]: what a segment adds to the state
+    float* local;           // [B][H][segments][D][D]: the state before the first segment, then what each but the last adds to it
 };
 
 constexpr uint32_t kTries = 1u << 22;       // of a wait before it gives up
@@ -454,20 +454,32 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
             const int r0 = half * N;
             const int64_t at = ((slot * g.H + h) * (int64_t)D + r0) * D + d;
             pair_t S[N / 2];                                // S^T row d, columns r0 .. r0 + N - 1
+            float* local = p.local + ((b * g.H + h) * (int64_t)p.segments * D + r0) * D + d;
             {
                 float v[N];
-                // the given state, and what the segments before this one added
-                const float w0 = decay_pow(g2, (float)s0);
-                const bool given = !kStates && g.state != nullptr && w0 != 0.f;
-                #pragma unroll
-                for (int x = 0; x < N; ++x) v[x] = given ? w0 * g.state[at + (int64_t)x * D] : 0.f;
-                if constexpr (!kStates) {
-                    const float* local = p.local + (((b * g.H + h) * (int64_t)(p.segments - 1)) * D + r0) * D + d;
+                if constexpr (kStates) {
+                    // The last segment's CTA writes state_out, which may be the state itself, while other segments may not have begun:
+                    // they take the given state from here.
+                    if (seg == 0 && g.state != nullptr) {
+                        #pragma unroll
+                        for (int x = 0; x < N; ++x) v[x] = g.state[at + (int64_t)x * D];
+                        #pragma unroll
+                        for (int x = 0; x < N; ++x) local[(int64_t)x * D] = v[x];
+                    }
+                    #pragma unroll
+                    for (int x = 0; x < N; ++x) v[x] = 0.f;
+                } else {
+                    // the given state (a sequence of one segment: read and written by this CTA alone), and what the segments before added
+                    const float w0 = decay_pow(g2, (float)s0);
+                    const float* given = seg == 0 && last_seg ? g.state + at : local;
+                    const bool any = g.state != nullptr && w0 != 0.f;
+                    #pragma unroll
+                    for (int x = 0; x < N; ++x) v[x] = any ? w0 * given[(int64_t)x * D] : 0.f;
                     for (int s = 0; s < seg; ++s) {
                         const float w = decay_pow(g2, (float)((int64_t)(seg - 1 - s) * p.seg_len));
                         if (w == 0.f) continue;
                         #pragma unroll
-                        for (int x = 0; x < N; ++x) v[x] = fmaf(w, local[((int64_t)s * D + x) * D], v[x]);
+                        for (int x = 0; x < N; ++x) v[x] = fmaf(w, local[((int64_t)(s + 1) * D + x) * D], v[x]);
                     }
                 }
                 #pragma unroll
@@ -520,7 +532,7 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
             if ((kStates || last_seg) && alive && (chunks == 0 || warp_wait(&bar.kv_done, chunks - 1))) {
                 tc::tc_fence_after_sync();
                 if (chunks > 0) add(decay_pow(g2, (float)tail));
-                float* dst = kStates ? p.local + ((((b * g.H + h) * (int64_t)(p.segments - 1)) + seg) * D + r0) * D + d : g.state_out + at;
+                float* dst = kStates ? local + (int64_t)(seg + 1) * D * D : g.state_out + at;
                 #pragma unroll
                 for (int x = 0; x < N; x += 2) {
                     float a, b2;
@@ -650,7 +662,7 @@ cudaError_t launch_typed(const DecayArgs& g, cudaStream_t s, const CUtensorMap& 
     if (p.segments > 1) {
         e = cudaFuncSetAttribute(decay_chunk_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != cudaSuccess) return e;
-        e = scratch_alloc(&scratch, (size_t)g.B * g.H * (p.segments - 1) * D * D * sizeof(float), s);
+        e = scratch_alloc(&scratch, (size_t)g.B * g.H * p.segments * D * D * sizeof(float), s);
         if (e != cudaSuccess) return e;
         p.local = static_cast<float*>(scratch);
         decay_chunk_kernel<D, true><<<(unsigned)(g.B * g.H * (p.segments - 1)), kThreads, bytes, s>>>(g, p, q, k, v, o);

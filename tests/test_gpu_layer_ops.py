@@ -476,3 +476,78 @@ def test_the_binding_refuses_what_does_not_fit():
         rtn.rtn_ternary_linear(*d, bias=torch.zeros(63, device="cuda"))
     with pytest.raises(rtn.RtnError):
         rtn.rtn_ternary_linear(*d, activation=9)
+
+
+# ---------------------------------------------------------------------------------------------- long prompts in segments
+
+@pytest.mark.parametrize("dtype,D", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64), (torch.float16, 128), (torch.float32, 200)],
+                         ids=ids)
+def test_long_prompts_update_their_states_in_place(dtype, D):
+    """Sequences of one and of many segments, states in slots of a pool, read and written in place: the same bits as with states
+    of their own, whatever else is in the pool; a padding entry among them."""
+    lens, H, Hk = [2100, 3, 900, 130, 0], 2, 1
+    q, k, v, log_decay, start = decay_case(lens, H, Hk, D, D, dtype)
+    pool = torch.randn(9, H, D, D, generator=torch.Generator().manual_seed(4)).cuda()
+    keep = pool.clone()
+    slots = torch.tensor([8, 2, 0, -1, 5], dtype=torch.int32, device="cuda")
+    live = [0, 1, 2, 4]
+    apart = torch.zeros_like(pool)
+    out1, _ = rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), 2100, state=pool, state_out=apart, slots=slots)
+    assert torch.equal(pool, keep)
+    out2, _ = rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), 2100, state=pool, slots=slots)
+    at = slots[live].long()
+    assert torch.equal(out1, out2) and torch.equal(pool[at], apart[at])
+    others = [i for i in range(9) if i not in at.tolist()]
+    assert torch.equal(pool[others], keep[others]) and bool((apart[others] == 0).all())
+    assert bool((out1[start[3]:start[4]] == 0).all())
+    want, mag, end, mag_end = ref.decay(ref.f64(q), ref.f64(k), ref.f64(v), log_decay, start, keep[slots.clamp_min(0).long()].cpu().numpy(), D ** -0.5)
+    c = ref.decay_roundings(log_decay, max(lens), D)
+    rows = np.r_[0:start[3], start[4]:start[5]]
+    ref.assert_close(out1[torch.from_numpy(rows).cuda()], want[rows], mag[rows], c, "out", extra=2.0 ** -15 if dtype == torch.bfloat16 else 0.0)
+    ref.assert_close(pool[at], end[live], mag_end[live], c, "state")
+    assert rtn.rtn_last_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=ids)
+def test_bad_slots_among_long_prompts(dtype):
+    lens, H, D = [300, 200, 100], 2, 64
+    q, k, v, log_decay, start = decay_case(lens, H, H, D, D, dtype)
+    pool = torch.randn(4, H, D, D, device="cuda")
+    keep = pool.clone()
+    rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), 300, state=pool, slots=torch.tensor([1, 4, 3], dtype=torch.int32, device="cuda"))
+    assert rtn.rtn_last_device_status() == 8
+    assert torch.equal(pool[[0, 2]], keep[[0, 2]]) and not torch.equal(pool[[1, 3]], keep[[1, 3]])
+
+
+def test_graph_capture_with_scratch():
+    """The forms that take scratch memory: a large linear layer, long prompts in segments (both kernels)."""
+    calls = []
+    args = packed(linear_case(700, 1500, 1024, 2))
+    calls.append(lambda: [rtn.rtn_ternary_linear(*args, dtype=torch.bfloat16)])
+    for dtype in (torch.bfloat16, torch.float16):
+        q, k, v, log_decay, start = decay_case([3000], 2, 1, 64, 64, dtype)
+        calls.append(lambda q=q, k=k, v=v, g=cuda(log_decay), s=cuda(start): list(rtn.rtn_decay_attention(q, k, v, g, s, 3000)))
+    for call in calls:
+        want = [t.clone() for t in call()]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = call()
+        for _ in range(2):
+            for t in got:
+                t.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("K", [512, 4096])
+def test_a_rows_result_does_not_depend_on_how_many_come_with_it(K):
+    """One row, a few (bit planes), some (one launch) and many (two launches): the same bits."""
+    d = linear_case(1100, 640, K, 12)
+    big = packed(d)
+    bias = cuda(d["bias"])
+    whole = rtn.rtn_ternary_linear(*big, bias=bias, activation=rtn.ACT_GELU)
+    for M in (1, 3, 8, 20, 100, 300, 600):
+        part = (big[0][:M], big[1][:M], *big[2:4], M, *big[5:7], big[7][:M], big[8][:M], *big[9:])
+        assert torch.equal(rtn.rtn_ternary_linear(*part, bias=bias, activation=rtn.ACT_GELU), whole[:M]), M
+    assert rtn.rtn_last_device_status() == 0
