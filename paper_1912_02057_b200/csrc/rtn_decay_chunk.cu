@@ -22,7 +22,7 @@
 //   the scores' conversion then runs beside Q S and the state update, the state's beside P V and the next scores.
 // The conversions are what the kernel spends its issue slots on, with a chain of dependent instructions per value: two warps per
 // role and scheduler hide what one could not.  The state's 64 registers a thread come from the other roles' shares (setmaxnreg).
-// Tensor memory (512 columns): state update | scores, then P | O | two entries of V terms.
+// Tensor memory (512 columns): state update | scores, then P | O | two entries of V terms (what is left of each 128 columns, too).
 //
 // Rows past a sequence's end belong to its neighbour: K and V rows are zeroed in shared memory before a product reads
 // them (0 * NaN), scores are masked by selection.  Inside a sequence a non-finite value can reach the outputs of up to 127
@@ -49,12 +49,12 @@ namespace rtn {
 namespace {
 
 constexpr int kC = 128;                     // tokens of a chunk
-constexpr int kEntry = 32;                  // tokens of an entry of V terms
 constexpr int kThreads = 28 * 32;
 constexpr int kWarpLoadQ = 0, kWarpMma = 1, kWarpLoadK = 2 /* V: 3 */, kWarpS = 4, kWarpP = 12, kWarpV = 20;
-// registers a thread: 72 at launch; 40 + 2 x (96 + 72 + 56) = 488 <= 7 x 72 per warp group of 128
-constexpr int kRegsRest = 40, kRegsS = 96, kRegsP = 72, kRegsV = 56;
-constexpr uint32_t kColS = 0, kColP = 128, kColO = 256, kColV = 384, kTmemCols = 512;
+// registers a thread: 72 at launch (V keeps them); 40 + 2 x (96 + 64 + 72) = 504 = 7 x 72 per warp group of 128
+constexpr int kRegsRest = 40, kRegsS = 96, kRegsP = 64;
+
+constexpr uint32_t kColS = 0, kColP = 128, kColO = 256, kTmemCols = 512;
 
 template <int D> struct Layout {
     // Slots of the three rings.  A Q tile lives from its scores to Q S, a K tile to the end of the state update, a V tile from its
@@ -62,6 +62,14 @@ template <int D> struct Layout {
     static constexpr int kSlotsQ = D == 128 ? 1 : 3, kSlotsK = D == 128 ? 2 : 3, kSlotsV = D == 128 ? 2 : 3;
     static constexpr int kSlots = kSlotsQ + kSlotsK + kSlotsV;
     static constexpr uint32_t kTile = kC * D * 2;
+    // Tokens of an entry of V terms (the MMA warp waits and commits once per entry); two entries in tensor memory, a column to two tokens
+    // of each of the three terms, where S^T, scores and O leave room.
+    static constexpr int kEntry = D == 64 ? 64 : 32;
+    static constexpr int kEntries = kC / kEntry;                // of a chunk
+    static __host__ __device__ constexpr uint32_t term_col(int place, int term)
+    {
+        return D == 64 ? (place == 0 ? 384 + 32 * term : term == 0 ? 480 : 32 + 32 * term) : 384 + 64 * place + 16 * term;
+    }
     static constexpr uint32_t kHalf = kC * 128;                 // 64 columns of a tile
     static constexpr uint32_t kState = D * D * 2;               // one bf16 term of S^T
     static constexpr uint32_t off_state = kSlots * kTile;
@@ -291,9 +299,9 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                 // state update by entries; Q S between the second and the third: its own terms may come late, and the V warps
                 // are two entries ahead at most
                 #pragma unroll 1
-                for (int e = 0; e < kC / kEntry && alive; ++e) {
+                for (int e = 0; e < L::kEntries && alive; ++e) {
                     if constexpr (!kStates) {
-                        if (e == 2) {
+                        if (e == L::kEntries / 2) {
                             alive = warp_wait(&bar.s_full, c) && (c == 0 || warp_wait(&bar.o_empty, c - 1));
                             if (!alive) break;
                             tc::tc_fence_after_sync();
@@ -305,25 +313,23 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                                     tc::mma_f16_ss(elected, tmem + kColO, kmajor(dq, L::kHalf, s),
                                                    kmajor(state_desc + (term * L::kState >> 4), D * 128, s), id_s, term + s > 0);
                             commit(&bar.qs_done);
-                            commit(&bar.empty[sq]);
                             CHUNK_TL(2);
                         }
                     }
-                    const int ve = c * (kC / kEntry) + e;
+                    const int ve = c * L::kEntries + e;
                     if (!(alive = warp_wait(&bar.vt_full[ve & 1], ve >> 1))) break;
                     tc::tc_fence_after_sync();
-                    #pragma unroll 1
+                    #pragma unroll
                     for (int term = 0; term < 3; ++term)
                         #pragma unroll
-                        for (int s = 0; s < kEntry / 16; ++s)
-                            tc::mma_f16_ts(elected, tmem + kColS, tmem + kColV + (uint32_t)((ve & 1) * 64 + term * 16 + s * 8),
-                                           mnmajor(dk, e * (kEntry / 16) + s), id_mn, e + term + s > 0);
+                        for (int s = 0; s < L::kEntry / 16; ++s)
+                            tc::mma_f16_ts(elected, tmem + kColS, tmem + ((e & 1) ? L::term_col(1, term) : L::term_col(0, term)) + (uint32_t)(s * 8),
+                                           mnmajor(dk, e * (L::kEntry / 16) + s), id_mn, e + term + s > 0);
                     commit(&bar.vt_empty[ve & 1]);
                 }
                 if (!alive) break;
                 CHUNK_TL(3);
                 commit(&bar.kv_done);
-                commit(&bar.empty[sk]);
                 if constexpr (!kStates) {
                     if (!(alive = warp_wait(&bar.p_full, c))) break;
                     CHUNK_TL(4);
@@ -337,9 +343,7 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                     commit(&bar.o_full);
                     CHUNK_TL(5);
                 }
-                if constexpr (kStates) {
-                    commit(&bar.empty[sv]);
-                } else {
+                if constexpr (!kStates) {
                     if (c + 1 < chunks) alive = scores(c + 1);
                     CHUNK_TL(6);
                 }
@@ -348,6 +352,7 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
       }
     } else if (warp >= kWarpP && warp < kWarpV) {
         // ------------------------------------------------------------ P: row i of the chunk, half of the keys, per thread
+        regs_down<kRegsP>();
         if constexpr (!kStates) {
             const int i = quad * 32 + lane, half = (warp >> 2) & 1;
             pair_t near[8];                                                   // l^(15 - x), by pairs
@@ -390,7 +395,9 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                 tc::tmem_st_wait();
                 if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(8);
                 if (!warp_wait(&bar.qs_done, c)) break;
+                if (threadIdx.x == kWarpP * 32) tc::mbar_arrive(&bar.empty[tile_slot(c, kTileQ)]);       // Q S was the tile's last use
                 if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(9);
+                __syncwarp();
                 tc::tc_fence_after_sync();
                 #pragma unroll 1
                 for (int x0 = half * (D / 2); x0 < (half + 1) * (D / 2); x0 += 16) {
@@ -505,6 +512,11 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
             for (int c = 0; c < chunks; ++c) {
                 if (c > 0) {
                     if (!(alive = warp_wait(&bar.kv_done, c - 1))) break;
+                    if (threadIdx.x == kWarpS * 32) {                         // the update was the K tile's last use (states only: V's, too)
+                        tc::mbar_arrive(&bar.empty[tile_slot(c - 1, kTileK)]);
+                        if constexpr (kStates) tc::mbar_arrive(&bar.empty[tile_slot(c - 1, kTileV)]);
+                    }
+                    __syncwarp();
                     if (threadIdx.x == (kWarpS + (D / 32 - 1)) * 32) CHUNK_TL(11);
                     tc::tc_fence_after_sync();
                     add(keep);
@@ -543,14 +555,15 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
         }
     } else {
         // ------------------------------------------------------------ V: column d of the V tile, every other entry, per thread
-        regs_down<kRegsV>();
         const int d = quad * 32 + lane, half = (warp >> 2) & 1;
         if (d < D) {
             uint32_t v_at[8];                               // where column d of token row j lies, for j & 7 (1024 bytes to the next 8)
             #pragma unroll
             for (int j = 0; j < 8; ++j)
                 v_at[j] = (uint32_t)(d >> 6) * L::kHalf + (uint32_t)(d & 7) * 2u + (uint32_t)j * 128u + ((uint32_t)(((d & 63) >> 3) ^ j) << 4);
-            const uint32_t col = tmem + lanes + kColV + (uint32_t)(half * 64);
+            const uint32_t col_hi = tmem + lanes + (half ? L::term_col(1, 0) : L::term_col(0, 0));
+            const uint32_t col_mid = tmem + lanes + (half ? L::term_col(1, 1) : L::term_col(0, 1));
+            const uint32_t col_lo = tmem + lanes + (half ? L::term_col(1, 2) : L::term_col(0, 2));
             for (int c = 0; c < chunks; ++c) {
                 const int sv = tile_slot(c, kTileV);
                 if (!warp_wait(&bar.full[sv], tile_phase(c, kTileV))) break;
@@ -575,11 +588,11 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                 const float* weight = n < kC ? table + kC + 32 : table;       // l^(n - 1 - j)
                 bool alive = true;
                 #pragma unroll 1
-                for (int e = half; e < kC / kEntry; e += 2) {
-                    #pragma unroll 1
-                    for (int sub = 0; sub < kEntry / 16; ++sub) {
+                for (int e = half; e < L::kEntries; e += 2) {
+                    #pragma unroll 2                    // (two register sets: a store to tensor memory is slow to let go of its own)
+                    for (int sub = 0; sub < L::kEntry / 16; ++sub) {
                         uint32_t hi[8], mid[8], lo[8];
-                        const int j0 = e * kEntry + sub * 16;
+                        const int j0 = e * L::kEntry + sub * 16;
                         const uint8_t* rows = tile + j0 * 128;
                         float v[16];
                         #pragma unroll
@@ -592,12 +605,12 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                             split3(mul_pair(make_pair(v[x + 2], v[x + 3]), make_pair(w.z, w.w)), hi[k + 1], mid[k + 1], lo[k + 1]);
                         }
                         if (sub == 0) {
-                            if (!(alive = warp_wait(&bar.vt_empty[half], 2 * c + (e >> 1) + 1))) break;
+                            if (!(alive = warp_wait(&bar.vt_empty[half], ((c * L::kEntries + e) >> 1) + 1))) break;
                             tc::tc_fence_after_sync();
                         }
-                        tc::tmem_st8(col + (uint32_t)(sub * 8), hi);
-                        tc::tmem_st8(col + (uint32_t)(16 + sub * 8), mid);
-                        tc::tmem_st8(col + (uint32_t)(32 + sub * 8), lo);
+                        tc::tmem_st8(col_hi + (uint32_t)(sub * 8), hi);
+                        tc::tmem_st8(col_mid + (uint32_t)(sub * 8), mid);
+                        tc::tmem_st8(col_lo + (uint32_t)(sub * 8), lo);
                     }
                     if (!alive) break;
                     tc::tmem_st_wait();

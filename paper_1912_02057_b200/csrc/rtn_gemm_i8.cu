@@ -199,7 +199,14 @@ __device__ __forceinline__ void linear_rows_out(const GemmArgs& g, const LinearA
             #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 const float4 c = sC[c0 + h < p.BN ? c0 + h + j : 0];
-                r[h + j] = activate(fmaf(a_s, fmaf(c.x, (float)(int)v[j], c.y * s_x), a_o * c.z) + c.w, l.act);
+                r[h + j] = fmaf(a_s, fmaf(c.x, (float)(int)v[j], c.y * s_x), a_o * c.z) + c.w;
+            }
+        }
+        if (l.act != RTN_ACT_NONE) {
+            #pragma unroll
+            for (int j = 0; j < kCols; j += 4) {
+                const float4 y = activation4(make_float4(r[j], r[j + 1], r[j + 2], r[j + 3]), l.act);
+                r[j] = y.x; r[j + 1] = y.y; r[j + 2] = y.z; r[j + 3] = y.w;
             }
         }
         if (l.residual != nullptr) {

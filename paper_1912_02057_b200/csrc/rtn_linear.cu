@@ -181,6 +181,27 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
         w_s = g.ep.w_scale[g.ep.n_wparam == 1 ? 0 : n]; w_o = g.ep.w_offset[g.ep.n_wparam == 1 ? 0 : n]; w_x = g.w_sum[n];
         if (l.bias != nullptr) bias = l.bias[n];
     }
+    const uint4* __restrict__ W = reinterpret_cast<const uint4*>(g.w_packed);
+    const uint4* __restrict__ X = reinterpret_cast<const uint4*>(g.a_packed);
+    const int team_warps = kTileWarps / p.stages, s = (warp < kTileWarps ? warp : 0) / team_warps, member = warp % team_warps;
+    const int row_groups = 4 + (p.BT + 31) / 32;
+    uint4* dst = reinterpret_cast<uint4*>(ring + s * stage_bytes);
+    // Items: block i, row groups first, first + team_warps, ... (four at most); the next item's planes are on their way while this
+    // one's are expanded.
+    uint4 nz[4], sg[4];
+    auto load = [&](int i, int first) {
+        #pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int rg = first + k * team_warps;
+            const bool isW = rg < 4;
+            const int r = (isW ? rg : rg - 4) * 32 + lane;
+            const int64_t row = (isW ? n0 : m0) + r;
+            const bool ok = i < kb1 - kb0 && rg < row_groups && (isW || r < p.BT) && row < (isW ? g.N : g.M);
+            nz[k] = sg[k] = make_uint4(0, 0, 0, 0);
+            if (ok) { const uint4* q = (isW ? W : X) + (row * nblk + kb0 + i) * 2; nz[k] = __ldg(q); sg[k] = __ldg(q + 1); }
+        }
+    };
+    if (warp < kTileWarps) load(s, member);
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
@@ -194,28 +215,7 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
     if (warp < kTileWarps) {
         // ------------------------------------------------------------ expand: the warps of a team own one stage, so that a stage's
         // phases follow each other in one program order; a team's warps take 32-row groups of the block in turn
-        const uint4* __restrict__ W = reinterpret_cast<const uint4*>(g.w_packed);
-        const uint4* __restrict__ X = reinterpret_cast<const uint4*>(g.a_packed);
-        const int team_warps = kTileWarps / p.stages, s = warp / team_warps, member = warp % team_warps;
-        const int row_groups = 4 + (p.BT + 31) / 32;
-        uint4* dst = reinterpret_cast<uint4*>(ring + s * stage_bytes);
-        // Items: block i, row groups first, first + team_warps, ... (four at most); the next item's planes are on their way while this
-        // one's are expanded.
-        uint4 nz[4], sg[4];
-        auto load = [&](int i, int first) {
-            #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int rg = first + k * team_warps;
-                const bool isW = rg < 4;
-                const int r = (isW ? rg : rg - 4) * 32 + lane;
-                const int64_t row = (isW ? n0 : m0) + r;
-                const bool ok = i < kb1 - kb0 && rg < row_groups && (isW || r < p.BT) && row < (isW ? g.N : g.M);
-                nz[k] = sg[k] = make_uint4(0, 0, 0, 0);
-                if (ok) { const uint4* q = (isW ? W : X) + (row * nblk + kb0 + i) * 2; nz[k] = __ldg(q); sg[k] = __ldg(q + 1); }
-            }
-        };
         int i = s, first = member;
-        load(i, first);
         while (i < kb1 - kb0) {
             if (first == member && !warp_wait(&bar.empty[s], (uint32_t)(i / p.stages) + 1)) break;
             uint4 cnz[4], csg[4];
@@ -263,19 +263,19 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
     }
 
     // ---------------------------------------------------------------- write out: column n0 + 32 (warp mod 4) + lane, every fourth
-    // group of 8 tokens of the CTA's share
+    // group of 4 tokens of the CTA's share
     const bool done = warp_wait(&bar.acc, 0);
     tc::tc_fence_after_sync();
-    const int groups = p.BT / 8;
+    const int groups = p.BT / 4;
     int* part = reinterpret_cast<int*>(ring);                        // [token][128]
     if (p.slices > 1) {
         if (warp < kTileWarps && done) {
             for (int q = warp >> 2; q < groups; q += kTileWarps / 4) {
-                uint32_t v[8];
-                tc::tmem_ld8(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(q * 8), v);
+                uint32_t v[4];
+                tc::tmem_ld4(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(q * 4), v);
                 tc::tmem_ld_wait();
                 #pragma unroll
-                for (int x = 0; x < 8; ++x) part[(q * 8 + x) * 128 + quad * 32 + lane] = (int)v[x];
+                for (int x = 0; x < 4; ++x) part[(q * 4 + x) * 128 + quad * 32 + lane] = (int)v[x];
             }
         }
         cluster_sync();
@@ -285,38 +285,46 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
         const T* res = static_cast<const T*>(l.residual);
         T* out = static_cast<T*>(l.out);
         for (int q = (warp >> 2) * p.slices + rank; q < groups; q += kTileWarps / 4 * p.slices) {
-            uint32_t v[8];
+            uint32_t v[4];
             if (p.slices == 1) {
-                tc::tmem_ld8(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(q * 8), v);
+                tc::tmem_ld4(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(q * 4), v);
             } else {
                 #pragma unroll
-                for (int x = 0; x < 8; ++x) v[x] = 0;
+                for (int x = 0; x < 4; ++x) v[x] = 0;
+                const uint32_t mine = tc::smem_addr(part + q * 4 * 128 + quad * 32 + lane);
                 for (int r = 0; r < p.slices; ++r) {
-                    const uint32_t mine = tc::smem_addr(part + q * 8 * 128 + quad * 32 + lane);
                     uint32_t at;
                     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(mine), "r"(r));
                     #pragma unroll
-                    for (int x = 0; x < 8; ++x) {
+                    for (int x = 0; x < 4; ++x) {
                         uint32_t y;
                         asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(y) : "r"(at + (uint32_t)x * 512u) : "memory");
                         v[x] += y;
                     }
                 }
             }
-            float add[8];
-            #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const int64_t m = m0 + q * 8 + x;
-                add[x] = res != nullptr && col_ok && m < g.M ? to_f32(res[m * l.res_stride + n]) : 0.f;
+            const int64_t m = m0 + q * 4;
+            const int rows = !col_ok || m >= g.M ? 0 : g.M - m < 4 ? (int)(g.M - m) : 4;
+            float add[4] = {0.f, 0.f, 0.f, 0.f};
+            if (res != nullptr) {
+                const T* r = res + m * l.res_stride + n;
+                #pragma unroll
+                for (int x = 0; x < 4; ++x) { if (x < rows) add[x] = to_f32(*r); r += l.res_stride; }
             }
             if (p.slices == 1) tc::tmem_ld_wait();
+            float y[4];
             #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const int64_t m = m0 + q * 8 + x;
-                const float4 t = token[q * 8 + x];
-                const float y = activate(fmaf(t.x, fmaf(w_s, (float)(int)v[x], w_o * t.z), t.y * p3) + bias, l.act) + add[x];
-                if (col_ok && m < g.M) out[m * l.out_stride + n] = from_f32<T>(y);
+            for (int x = 0; x < 4; ++x) {
+                const float4 t = token[q * 4 + x];
+                y[x] = fmaf(t.x, fmaf(w_s, (float)(int)v[x], w_o * t.z), t.y * p3) + bias;
             }
+            if (l.act != RTN_ACT_NONE) {
+                const float4 a = activation4(make_float4(y[0], y[1], y[2], y[3]), l.act);
+                y[0] = a.x; y[1] = a.y; y[2] = a.z; y[3] = a.w;
+            }
+            T* o = out + m * l.out_stride + n;
+            #pragma unroll
+            for (int x = 0; x < 4; ++x) { if (x < rows) *o = from_f32<T>(y[x] + add[x]); o += l.out_stride; }
         }
     }
     if (p.slices > 1) cluster_sync();            // nobody leaves while its sums are read
