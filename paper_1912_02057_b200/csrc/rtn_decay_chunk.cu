@@ -150,7 +150,8 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
 {
     using L = Layout<D>;
     extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    // (an offset, not a rounded address: through an integer the compiler loses that it is shared memory, and every access becomes generic)
+    uint8_t* smem = smem_raw + ((1024u - (tc::smem_addr(smem_raw) & 1023u)) & 1023u);
     float* table = reinterpret_cast<float*>(smem + L::off_table);            // l^(C-1-j), then 32 zeros, then the last chunk's
     Bars& bar = *reinterpret_cast<Bars*>(smem + L::off_bar);
     // the warp's number by a shuffle: the branches on it are then known to be uniform, and what the MMA warp computes for its
