@@ -14,7 +14,7 @@
 //
 // A CTA walks the chunks of one (sequence, query head, segment).  Warp roles, coupled by mbarriers:
 //   P   (8 warps)  scores -> P terms, in place in tensor memory (A operand of P V); scales Q S by l^(i+1) before P V adds to it;
-//                  O -> bf16 rows, staged in the V tile's slot and stored by TMA
+//                  O -> bf16 rows, staged in the K tile's slot and stored by TMA
 //   S   (8 warps)  the state, in registers (a row of S^T per pair of threads): decays it, adds the chunk's part, writes its terms
 //                  to shared memory (B operand of Q S); initial and final state
 //   V   (8 warps)  V tile -> decayed, transposed V terms in tensor memory (A operand of the state update), 32 tokens at a time
@@ -56,10 +56,13 @@ constexpr int kRegsRest = 40, kRegsS = 96, kRegsP = 64;
 
 constexpr uint32_t kColS = 0, kColP = 128, kColO = 256, kTmemCols = 512;
 
-template <int D> struct Layout {
-    // Slots of the three rings.  A Q tile lives from its scores to Q S, a K tile to the end of the state update, a V tile from its
-    // conversion to the store of the rows that are staged in its slot.
-    static constexpr int kSlotsQ = D == 128 ? 1 : 3, kSlotsK = D == 128 ? 2 : 3, kSlotsV = D == 128 ? 2 : 3;
+template <int D, bool kStates> struct Layout {
+    // Slots of the three rings.  A Q tile lives from its scores to Q S, a V tile from its conversion to P V, a K tile from its scores to the
+    // store of the rows that are staged in its slot after the state update.  Where only states are wanted the slots of Q and the
+    // state's terms go to K and V.
+    static constexpr int kSlotsQ = kStates ? 0 : D == 128 ? 1 : 3;
+    static constexpr int kSlotsK = kStates ? (D == 128 ? 3 : 4) : D == 128 ? 2 : 3;
+    static constexpr int kSlotsV = kStates ? (D == 128 ? 4 : 5) : D == 128 ? 2 : 3;
     static constexpr int kSlots = kSlotsQ + kSlotsK + kSlotsV;
     static constexpr uint32_t kTile = kC * D * 2;
     // Tokens of an entry of V terms (the MMA warp waits and commits once per entry); two entries in tensor memory, a column to two tokens
@@ -73,7 +76,7 @@ template <int D> struct Layout {
     static constexpr uint32_t kHalf = kC * 128;                 // 64 columns of a tile
     static constexpr uint32_t kState = D * D * 2;               // one bf16 term of S^T
     static constexpr uint32_t off_state = kSlots * kTile;
-    static constexpr uint32_t off_table = off_state + 2 * kState;
+    static constexpr uint32_t off_table = off_state + (kStates ? 0 : 2 * kState);
     static constexpr uint32_t off_bar = off_table + (kC + 32 + kC) * 4;
     static constexpr uint32_t kBytes = off_bar + 512 + 1024;    // and room to start on a 1024-byte boundary
 };
@@ -148,7 +151,7 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                    const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                    const __grid_constant__ CUtensorMap map_o)
 {
-    using L = Layout<D>;
+    using L = Layout<D, kStates>;
     extern __shared__ uint8_t smem_raw[];
     // (an offset, not a rounded address: through an integer the compiler loses that it is shared memory, and every access becomes generic)
     uint8_t* smem = smem_raw + ((1024u - (tc::smem_addr(smem_raw) & 1023u)) & 1023u);
@@ -235,12 +238,12 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
         if constexpr (!kStates) {
             const int stores = tail == kC ? chunks : chunks - 1;              // the last rows of a sequence are stored by their threads
             for (int c = 0; c < stores; ++c) {
-                const int sv = tile_slot(c, kTileV);
+                const int sk = tile_slot(c, kTileK);
                 if (!wait(&bar.o_staged, c)) break;
-                for (int x = 0; x < D / 64; ++x) tma_store_tile(&map_o, base + sv * L::kTile + x * L::kHalf, x * 64, h, (int)row0 + c * kC);
+                for (int x = 0; x < D / 64; ++x) tma_store_tile(&map_o, base + sk * L::kTile + x * L::kHalf, x * 64, h, (int)row0 + c * kC);
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                tc::mbar_arrive(&bar.empty[sv]);
+                tc::mbar_arrive(&bar.empty[sk]);
             }
             asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         }
@@ -422,9 +425,10 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                 if (!warp_wait(&bar.o_full, c)) break;
                 if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(15);
                 tc::tc_fence_after_sync();
-                const int sv = tile_slot(c, kTileV);
+                if (threadIdx.x == kWarpP * 32) tc::mbar_arrive(&bar.empty[tile_slot(c, kTileV)]);       // P V was the V tile's last use
+                __syncwarp();
                 const bool whole = c < chunks - 1 || tail == kC;              // a store of 128 rows stays inside the sequence
-                uint8_t* row = smem + sv * L::kTile + i * 128;                // P V has read the slot's V tile
+                uint8_t* row = smem + tile_slot(c, kTileK) * L::kTile + i * 128;        // the state update has read the slot's K tile
                 __nv_bfloat16* orow = out + (int64_t)(c * kC + i) * g.o_token;
                 const bool mine = c * kC + i < n_tok;
                 #pragma unroll 1
@@ -513,11 +517,13 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
             for (int c = 0; c < chunks; ++c) {
                 if (c > 0) {
                     if (!(alive = warp_wait(&bar.kv_done, c - 1))) break;
-                    if (threadIdx.x == kWarpS * 32) {                         // the update was the K tile's last use (states only: V's, too)
-                        tc::mbar_arrive(&bar.empty[tile_slot(c - 1, kTileK)]);
-                        if constexpr (kStates) tc::mbar_arrive(&bar.empty[tile_slot(c - 1, kTileV)]);
+                    if constexpr (kStates) {                                  // the update was both tiles' last use
+                        if (threadIdx.x == kWarpS * 32) {
+                            tc::mbar_arrive(&bar.empty[tile_slot(c - 1, kTileK)]);
+                            tc::mbar_arrive(&bar.empty[tile_slot(c - 1, kTileV)]);
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
                     if (threadIdx.x == (kWarpS + (D / 32 - 1)) * 32) CHUNK_TL(11);
                     tc::tc_fence_after_sync();
                     add(keep);
@@ -668,18 +674,18 @@ template <int D>
 cudaError_t launch_typed(const DecayArgs& g, cudaStream_t s, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                          const CUtensorMap& o)
 {
-    constexpr int bytes = (int)Layout<D>::kBytes;
+    constexpr int bytes = (int)Layout<D, false>::kBytes, bytes_states = (int)Layout<D, true>::kBytes;
     ChunkPlan p = make_plan(g);
     cudaError_t e = cudaFuncSetAttribute(decay_chunk_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
     void* scratch = nullptr;
     if (p.segments > 1) {
-        e = cudaFuncSetAttribute(decay_chunk_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        e = cudaFuncSetAttribute(decay_chunk_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes_states);
         if (e != cudaSuccess) return e;
         e = scratch_alloc(&scratch, (size_t)g.B * g.H * p.segments * D * D * sizeof(float), s);
         if (e != cudaSuccess) return e;
         p.local = static_cast<float*>(scratch);
-        decay_chunk_kernel<D, true><<<(unsigned)(g.B * g.H * (p.segments - 1)), kThreads, bytes, s>>>(g, p, q, k, v, o);
+        decay_chunk_kernel<D, true><<<(unsigned)(g.B * g.H * (p.segments - 1)), kThreads, bytes_states, s>>>(g, p, q, k, v, o);
         e = cudaGetLastError();
     }
     if (e == cudaSuccess) {
