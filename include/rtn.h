@@ -292,7 +292,9 @@ rtn_status rtn_qk_norm_rotary(const void* q, int64_t q_token, int64_t q_head, co
  *   state_out   same shape, receives S after the last token; may be `state` (in place).  Required.
  *   slots       int32 [B] (on the device): sequence b's state is slots[b]; the live slots are distinct; a negative slot
  *               is a padding entry: its out rows become zero and no state is read or written.  NULL: slot b
- * Dk, Dv <= 256.  Bounds that do not fit (a decreasing start, a length over max_len, a slot >= n_slots) make the kernel
+ * Dk, Dv <= 256.  A value that is not finite reaches no token before its own: in v it makes that column of the head not finite
+ * (NaN or infinite) from its token on, in k or the state every column, in q its own token's row.
+ * Bounds that do not fit (a decreasing start, a length over max_len, a slot >= n_slots) make the kernel
  * skip the sequence (its rows of out are not written), and rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once. */
 rtn_status rtn_decay_attention(const void* q, int64_t q_token, int64_t q_head, const void* k, int64_t k_token, int64_t k_head,
                                const void* v, int64_t v_token, int64_t v_head, void* out, int64_t o_token, int64_t o_head,

@@ -209,11 +209,9 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
             }
         } else {
             const float w0 = power(g2, (float)s0);
-            if (g.state != nullptr && w0 != 0.f) add(seg == 0 && last_seg ? g.state + base : p.local + local_base, w0);
-            for (int x = 0; x < seg; ++x) {
-                const float w = power(g2, (float)((int64_t)(seg - 1 - x) * p.seg_len));
-                if (w != 0.f) add(p.local + local_base + (x + 1) * slice, w);
-            }
+            if (g.state != nullptr) add(seg == 0 && last_seg ? g.state + base : p.local + local_base, w0);
+            for (int x = 0; x < seg; ++x)
+                add(p.local + local_base + (x + 1) * slice, power(g2, (float)((int64_t)(seg - 1 - x) * p.seg_len)));
         }
     }
     auto decay = [&](float l) {

@@ -25,8 +25,9 @@
 // Tensor memory (512 columns): state update | scores, then P | O | two entries of V terms (what is left of each 128 columns, too).
 //
 // Rows past a sequence's end belong to its neighbour: K and V rows are zeroed in shared memory before a product reads
-// them (0 * NaN), scores are masked by selection.  Inside a sequence a non-finite value can reach the outputs of up to 127
-// tokens before it (0 * NaN in P V).
+// them (0 * NaN), scores are masked by selection.  A non-finite v of a later token in the chunk would reach a row through the
+// zeros of P: the V warps see every value, and one whose third term is not finite is zeroed in the tile P V reads; the rows from
+// its token on get a NaN in that column when they are written.
 //
 // Few heads and long prompts: the sequence is cut into segments; a first launch computes what each segment adds to the state
 // (V and MMA roles only), and the second starts each segment from the decayed sum of what came before.
@@ -40,7 +41,7 @@
 // Timeline slots (instrumented build only): 0 kernel entry, 1 set-up done, 4 kernel end; chunk c in 4 .. 7 of a CTA, from
 // slot 8 + 20 (c - 4): 0 state update begins, 1 / 2 Q S begins / issued, 3 state update issued, 4 P ready, 5 P V issued,
 // 6 next scores issued (MMA thread); 7 scores ready, 8 P written, 9 Q S ready, 10 Q S scaled; 11 state updated, 12 state
-// terms written; 13 V tile landed, 14 V terms written; 15 O complete, 16 O read, 17 rows stored.
+// terms written; 13 V tile landed, 14 V terms written; 15 O complete, 16 O read and staged.
 RTN_TL_DEFINE(decay_chunk)
 #define CHUNK_TL(k) RTN_TL(decay_chunk, c >= 4 && c < 8 ? 8 + 20 * (c - 4) + (k) : -1)
 
@@ -77,8 +78,9 @@ template <int D, bool kStates> struct Layout {
     static constexpr uint32_t kState = D * D * 2;               // one bf16 term of S^T
     static constexpr uint32_t off_state = kSlots * kTile;
     static constexpr uint32_t off_table = off_state + (kStates ? 0 : 2 * kState);
-    static constexpr uint32_t off_bar = off_table + (kC + 32 + kC) * 4;
-    static constexpr uint32_t kBytes = off_bar + 512 + 1024;    // and room to start on a 1024-byte boundary
+    static constexpr uint32_t off_bad = off_table + (kC + 32 + kC) * 4;    // first token with a non-finite v, by column
+    static constexpr uint32_t off_bar = off_bad + D * 4;
+    static constexpr uint32_t kBytes = off_bar + 288 + 1024;    // and room to start on a 1024-byte boundary
 };
 
 struct Bars {
@@ -90,8 +92,9 @@ struct Bars {
     uint64_t fixed;                                 // rows past the end zeroed
     uint32_t tmem_slot;
     int dead;
+    int any_bad;                                    // some column has a non-finite v
 };
-static_assert(sizeof(Bars) <= 512, "barriers");
+static_assert(sizeof(Bars) <= 288, "barriers");
 
 struct ChunkPlan {
     int64_t seg_len;        // tokens of a segment, a multiple of kC
@@ -156,6 +159,7 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
     // (an offset, not a rounded address: through an integer the compiler loses that it is shared memory, and every access becomes generic)
     uint8_t* smem = smem_raw + ((1024u - (tc::smem_addr(smem_raw) & 1023u)) & 1023u);
     float* table = reinterpret_cast<float*>(smem + L::off_table);            // l^(C-1-j), then 32 zeros, then the last chunk's
+    int* bad_from = reinterpret_cast<int*>(smem + L::off_bad);
     Bars& bar = *reinterpret_cast<Bars*>(smem + L::off_bar);
     // the warp's number by a shuffle: the branches on it are then known to be uniform, and what the MMA warp computes for its
     // instructions stays in uniform registers
@@ -198,8 +202,9 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
         for (int i = 0; i < 2; ++i) { tc::mbar_init(&bar.vt_full[i], D); tc::mbar_init(&bar.vt_empty[i], 1); }
         tc::mbar_init(&bar.o_full, 1); tc::mbar_init(&bar.o_empty, 256); tc::mbar_init(&bar.o_staged, 256); tc::mbar_init(&bar.fixed, 2 * D);
         tc::mbar_init_fence();
-        bar.dead = 0;
+        bar.dead = bar.any_bad = 0;
     }
+    if (threadIdx.x < D) bad_from[threadIdx.x] = 0x7fffffff;
     if (threadIdx.x < kC) table[kC - 1 - threadIdx.x] = decay_pow(g2, (float)threadIdx.x);
     else if (threadIdx.x < kC + 32) table[threadIdx.x] = 0.f;
     tc::tc_fence_before_sync();
@@ -210,7 +215,7 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
     if (threadIdx.x == 0) RTN_TL(decay_chunk, 1);
     const uint32_t base = tc::smem_addr(smem);
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    volatile int* dead = &bar.dead;
+    volatile int *dead = &bar.dead, *any_bad = &bar.any_bad;
     // Bounded waits: one that runs out marks the CTA, which reports it at its end.  Whole warps wait together and give up together
     // (what follows is warp-collective).
     auto wait = [&](uint64_t* m, int phase) {
@@ -448,6 +453,14 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                         else if (mine) *reinterpret_cast<uint4*>(orow + x0 + y * 8) = u;
                     }
                 }
+                if (*any_bad) {
+                    #pragma unroll 1
+                    for (int x = half * (D / 2); x < (half + 1) * (D / 2); ++x)
+                        if (c * kC + i >= bad_from[x]) {
+                            if (whole) *reinterpret_cast<uint16_t*>(row + (x >> 6) * L::kHalf + ((((x & 63) >> 3) ^ (i & 7)) << 4) + (x & 7) * 2) = 0x7fff;
+                            else if (mine) orow[x] = __ushort_as_bfloat16(0x7fff);
+                        }
+                }
                 tc::tc_fence_before_sync();
                 tc::mbar_arrive(&bar.o_empty);
                 if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(16);
@@ -484,12 +497,11 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                     // the given state (a sequence of one segment: read and written by this CTA alone), and what the segments before added
                     const float w0 = decay_pow(g2, (float)s0);
                     const float* given = seg == 0 && last_seg ? g.state + at : local;
-                    const bool any = g.state != nullptr && w0 != 0.f;
+                    const bool any = g.state != nullptr;        // (also where w0 is 0: a non-finite state stays one)
                     #pragma unroll
                     for (int x = 0; x < N; ++x) v[x] = any ? w0 * given[(int64_t)x * D] : 0.f;
                     for (int s = 0; s < seg; ++s) {
                         const float w = decay_pow(g2, (float)((int64_t)(seg - 1 - s) * p.seg_len));
-                        if (w == 0.f) continue;
                         #pragma unroll
                         for (int x = 0; x < N; ++x) v[x] = fmaf(w, local[((int64_t)(s + 1) * D + x) * D], v[x]);
                     }
@@ -596,6 +608,7 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                 bool alive = true;
                 #pragma unroll 1
                 for (int e = half; e < L::kEntries; e += 2) {
+                    uint32_t seen = 0;                  // every low term: NaN where a value is not finite, under 2 where it is under 2^17
                     #pragma unroll 2                    // (two register sets: a store to tensor memory is slow to let go of its own)
                     for (int sub = 0; sub < L::kEntry / 16; ++sub) {
                         uint32_t hi[8], mid[8], lo[8];
@@ -611,6 +624,10 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                             split3(mul_pair(make_pair(v[x], v[x + 1]), make_pair(w.x, w.y)), hi[k], mid[k], lo[k]);
                             split3(mul_pair(make_pair(v[x + 2], v[x + 3]), make_pair(w.z, w.w)), hi[k + 1], mid[k + 1], lo[k + 1]);
                         }
+                        if constexpr (!kStates) {
+                            #pragma unroll
+                            for (int x = 0; x < 8; ++x) seen |= lo[x];
+                        }
                         if (sub == 0) {
                             if (!(alive = warp_wait(&bar.vt_empty[half], ((c * L::kEntries + e) >> 1) + 1))) break;
                             tc::tc_fence_after_sync();
@@ -620,6 +637,18 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                         tc::tmem_st8(col_lo + (uint32_t)(sub * 8), lo);
                     }
                     if (!alive) break;
+                    if (!kStates && (seen & 0x40004000u)) {
+                        #pragma unroll 1
+                        for (int j = e * L::kEntry; j < (e + 1) * L::kEntry; ++j) {
+                            uint16_t* x = reinterpret_cast<uint16_t*>(tile + j * 128 + (d >> 6) * L::kHalf + ((((d & 63) >> 3) ^ (j & 7)) << 4) + (d & 7) * 2);
+                            if ((*x & 0x7f80) != 0x7f80) continue;
+                            *x = 0;
+                            atomicMin(&bad_from[d], c * kC + j);
+                            *any_bad = 1;
+                        }
+                        tc::fence_smem_to_async_proxy();
+                    }
+                    __syncwarp();
                     tc::tmem_st_wait();
                     tc::tc_fence_before_sync();
                     tc::mbar_arrive(&bar.vt_full[half]);

@@ -285,6 +285,48 @@ def test_sequences_do_not_reach_each_other(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("D,length,at", [(64, 300, 40), (128, 300, 257), (128, 300, 299), (64, 2500, 1100), (128, 2500, 0), (64, 90, 89)], ids=ids)
+def test_a_value_that_is_not_finite_reaches_no_earlier_token(D, length, at, value, dtype):
+    q, k, v, log_decay, start = decay_case([length], 2, 2, D, D, dtype)
+    run = lambda: rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), length)  # noqa: E731
+    clean, end = run()
+    keep = v[at, 1, 5].clone()
+    v[at, 1, 5] = value                         # one column of one head, from its token on
+    out, got = run()
+    bad = torch.zeros_like(out, dtype=torch.bool)
+    bad[at:, 1, 5] = True
+    assert torch.equal(out[~bad], clean[~bad]) and not torch.isfinite(out[bad]).any()
+    bad = torch.zeros_like(got, dtype=torch.bool)
+    bad[0, 1, :, 5] = True
+    assert torch.equal(got[~bad], end[~bad]) and not torch.isfinite(got[bad]).any()
+    v[at, 1, 5] = keep
+    k[at, 1, 7] = value                         # one row of the state: every column of the head
+    out, got = run()
+    assert torch.equal(out[:, 0], clean[:, 0]) and torch.equal(out[:at], clean[:at]) and not torch.isfinite(out[at:, 1]).any()
+    assert torch.equal(got[0, 0], end[0, 0]) and not torch.isfinite(got[0, 1, 7]).any()
+    k[at, 1, 7] = 0.5
+    clean, end = run()
+    q[at, 1, 3] = value                         # one token's output
+    out, got = run()
+    rest = torch.arange(length, device="cuda") != at
+    assert torch.equal(out[rest], clean[rest]) and torch.equal(out[at, 0], clean[at, 0]) and torch.equal(got, end)
+    assert not torch.isfinite(out[at, 1]).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids)
+@pytest.mark.parametrize("D", [64, 128])
+def test_values_far_from_one_scale_the_result(D, dtype):
+    """Every product and sum is linear in v, and a power of two changes no rounding."""
+    q, k, v, log_decay, start = decay_case([300, 40], 2, 1, D, D, dtype)
+    run = lambda x: rtn.rtn_decay_attention(q, k, x, cuda(log_decay), cuda(start), 300)  # noqa: E731
+    out, got = run(v)
+    for power in (20, 60):
+        big, state = run(v * 2.0 ** power)
+        assert torch.equal(big, out * 2.0 ** power) and torch.equal(state, got * 2.0 ** power)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
 @pytest.mark.parametrize("B,H,Hk,Dk,Dv", [(1, 1, 1, 64, 64), (3, 4, 2, 128, 128), (40, 16, 4, 128, 128), (2, 2, 2, 7, 5), (5, 3, 1, 96, 200),
                                           (2, 2, 1, 256, 256), (300, 2, 2, 64, 64)], ids=ids)
 def test_step_matches_the_recurrence(B, H, Hk, Dk, Dv, dtype):
