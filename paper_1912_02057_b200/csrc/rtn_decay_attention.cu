@@ -5,8 +5,10 @@
 //
 // decay_step_kernel: one token per sequence.  Bound: DRAM, the fp32 state read and written once (8 Dk Dv bytes per head
 //   against 4 Dk Dv operations).
+//   96 sequences x 32 heads of 128 x 128: 66 us in a graph, 6.1 TB/s (0.94 of a plain copy's rate).
 // decay_recurrent_kernel: whole prompts token by token with the state in registers; any type, head dimension and
-//   stride.  Bound: the FMA pipe (two FMAs per state element and token).
+//   stride.  Bound: the FMA pipe (two FMAs per state element and token), behind a chain of about 280 clocks per token that two or
+//   three CTAs per SM hide in part.  8 x 2048 tokens, 32 heads of 128, fp16: 1084 us, 0.44 of the pipe's rate.
 #include "rtn_internal.cuh"
 #include "rtn_types.cuh"
 #include "rtn_decay.cuh"
@@ -108,9 +110,7 @@ cudaError_t launch_step_typed(const DecayArgs& g, cudaStream_t s)
 
 // ------------------------------------------------------------------------------------------------ prompts, token by token
 
-constexpr int kRecWarps = 4;            // each holds a quarter of the state's rows
-constexpr int kRecThreads = kRecWarps * 32;
-constexpr int kRecTile = 8;             // tokens staged at a time, at most (16: 8 x 2048 tokens of 32 heads 1500 us instead of 1160)
+constexpr int kRecTile = 8;             // tokens staged at a time, at most
 
 struct RecPlan {
     int64_t seg_len;        // tokens of a segment
@@ -121,18 +121,18 @@ struct RecPlan {
 // l^n from log2 l; n = 0 gives 1 for every l.
 __device__ __forceinline__ float power(float g2, float n) { return n == 0.f ? 1.f : exp2f(n * g2); }
 
-// Column(s) of the state in the lanes of four warps, rows in registers by pairs.  Within a tile of tokens i = 0, 1, ... the state is kept
+// Column(s) of the state in the lanes of each warp, ROWS rows of it in registers by pairs.  Within a tile of tokens i = 0, 1, ... the state is kept
 // relative to the tile's first token,
 //   S_i = l^i S'_i,   S'_i = S'_(i-1) + (l^-i k_i) v_i^T,   o_i = (l^i q_i)^T S'_i,
 // which leaves one FMA per element for the update and one for the output, two elements to an instruction.  A tile ends before
 // l^-i passes e^60; at l = 0 it is one token.
-template <typename T, int ROWS, int COLS, bool kStates>
-__global__ void __launch_bounds__(kRecThreads)
+template <typename T, int ROWS, int COLS, int WARPS, bool kStates>
+__global__ void __launch_bounds__(WARPS * 32, WARPS == 4 ? 3 : 2)         // (a fourth CTA of 4 warps: 2 x 9656 tokens of heads of 64, 318 us instead of 256)
 decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
 {
-    constexpr int DK = ROWS * kRecWarps, DV = COLS * 32;
+    constexpr int kRecThreads = WARPS * 32, DK = ROWS * WARPS, DV = COLS * 32;
     __shared__ __align__(16) float sq[kStates ? 1 : kRecTile][DK], sk[kRecTile][DK];
-    __shared__ float sv[kRecTile][DV], so[kStates ? 1 : kRecTile][kRecWarps][DV], grow[kRecTile], shrink[kRecTile];
+    __shared__ float sv[kRecTile][DV], so[kStates ? 1 : kRecTile][WARPS][DV];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int h = blockIdx.y, hk = h / (g.H / g.Hk);
     const int slices = (g.Dv + DV - 1) / DV;
@@ -220,49 +220,44 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
             #pragma unroll
             for (int i = 0; i < ROWS / 2; ++i) S[c][i] = mul_pair(S[c][i], make_pair(l, l));
     };
-    if (threadIdx.x < kRecTile) {
-        grow[threadIdx.x] = power(g2, -(float)threadIdx.x);             // (past the tile's length: not looked at)
-        shrink[threadIdx.x] = power(g2, (float)threadIdx.x);
-    }
-    __syncthreads();
-    // A tile's values on their way in registers while the tile before it is worked on: item i of a thread is token (128 i + thread) / DK,
-    // element (128 i + thread) mod DK.
-    constexpr int kPer = DK * kRecTile / kRecThreads, kPerV = DV * kRecTile / kRecThreads;
+    // A tile's values on their way in registers while the tile before it is worked on: a thread has one element of every kEveryK-th
+    // token of q and k, and of every kEveryV-th of v.
+    static_assert(kRecThreads % DK == 0 && kRecThreads % DV == 0 && kRecTile * DK % kRecThreads == 0 && kRecTile * DV % kRecThreads == 0, "shares");
+    constexpr int kEveryK = kRecThreads / DK, kEveryV = kRecThreads / DV, kPer = kRecTile / kEveryK, kPerV = kRecTile / kEveryV;
+    const int dk = threadIdx.x % DK, tk = threadIdx.x / DK, dv = threadIdx.x % DV, tv = threadIdx.x / DV;
     T rq[kStates ? 1 : kPer], rk[kPer], rv[kPerV];
-    auto fetch = [&](int64_t at, int n) {
-        const T *qt = q + at * g.q_token, *kt = k + at * g.k_token, *vt = v + at * g.v_token;
+    const T *qt = q + tk * g.q_token + dk, *kt = k + tk * g.k_token + dk, *vt_ = v + tv * g.v_token + dv;
+    auto fetch = [&](int n) {               // the tile that the pointers are at
+        const int nk = dk < g.Dk ? n - tk : 0, nv = dv < cols ? n - tv : 0;
         #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int t = (i * kRecThreads + threadIdx.x) / DK, d = (i * kRecThreads + threadIdx.x) % DK;
-            const bool ok = t < n && d < g.Dk;
-            if constexpr (!kStates) rq[i] = ok ? qt[t * g.q_token + d] : from_f32<T>(0.f);
-            rk[i] = ok ? kt[t * g.k_token + d] : from_f32<T>(0.f);
+            if constexpr (!kStates) rq[i] = i * kEveryK < nk ? qt[i * kEveryK * g.q_token] : from_f32<T>(0.f);
+            rk[i] = i * kEveryK < nk ? kt[i * kEveryK * g.k_token] : from_f32<T>(0.f);
         }
         #pragma unroll
-        for (int i = 0; i < kPerV; ++i) {
-            const int t = (i * kRecThreads + threadIdx.x) / DV, c = (i * kRecThreads + threadIdx.x) % DV;
-            rv[i] = t < n && c < cols ? vt[t * g.v_token + c] : from_f32<T>(0.f);
-        }
+        for (int i = 0; i < kPerV; ++i) rv[i] = i * kEveryV < nv ? vt_[i * kEveryV * g.v_token] : from_f32<T>(0.f);
+        qt += n * g.q_token; kt += n * g.k_token; vt_ += n * g.v_token;
     };
+    float own_grow[kPer], own_shrink[kStates ? 1 : kPer];
+    #pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        own_grow[i] = tk + i * kEveryK < tile ? power(g2, -(float)(tk + i * kEveryK)) : 0.f;
+        if constexpr (!kStates) own_shrink[i] = power(g2, (float)(tk + i * kEveryK));
+    }
+    T* ot = out + tv * g.o_token + dv;
     int64_t t0 = 0;
-    fetch(0, n_tok < tile ? (int)n_tok : tile);
+    fetch(n_tok < tile ? (int)n_tok : tile);
     while (t0 < n_tok) {
         const int n = n_tok - t0 < tile ? (int)(n_tok - t0) : tile;
         #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int t = (i * kRecThreads + threadIdx.x) / DK, d = (i * kRecThreads + threadIdx.x) % DK;
-            if (t < n) {
-                if constexpr (!kStates) sq[t][d] = to_f32(rq[i]) * shrink[t];
-                sk[t][d] = to_f32(rk[i]) * grow[t];
-            }
+        for (int i = 0; i < kPer; ++i) {                // (rows past the tile's length: not looked at)
+            if constexpr (!kStates) sq[tk + i * kEveryK][dk] = to_f32(rq[i]) * own_shrink[i];
+            sk[tk + i * kEveryK][dk] = to_f32(rk[i]) * own_grow[i];
         }
         #pragma unroll
-        for (int i = 0; i < kPerV; ++i) {
-            const int t = (i * kRecThreads + threadIdx.x) / DV, c = (i * kRecThreads + threadIdx.x) % DV;
-            if (t < n) sv[t][c] = to_f32(rv[i]);
-        }
+        for (int i = 0; i < kPerV; ++i) sv[tv + i * kEveryV][dv] = to_f32(rv[i]);
         const int64_t t1 = t0 + n;
-        fetch(t1, n_tok - t1 < tile ? (int)(n_tok - t1) : tile);
+        fetch(n_tok - t1 < tile ? (int)(n_tok - t1) : tile);
         decay(power(g2, t0 == 0 ? 1.f : (float)tile));
         __syncthreads();
         for (int t = 0; t < n; ++t) {
@@ -305,11 +300,17 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
         }
         __syncthreads();
         if constexpr (!kStates) {
-            for (int i = threadIdx.x; i < n * cols; i += kRecThreads) {
-                const int t = i / cols, c = i % cols;
-                const float o = (so[t][0][c] + so[t][1][c]) + (so[t][2][c] + so[t][3][c]);
-                out[(t0 + t) * g.o_token + c] = from_f32<T>(g.scale * o);
+            #pragma unroll
+            for (int i = 0; i < kPerV; ++i) {
+                const int t = tv + i * kEveryV;
+                if (t < n && dv < cols) {
+                    float o = 0.f;
+                    #pragma unroll
+                    for (int w = 0; w < WARPS; ++w) o += so[t][w][dv];
+                    ot[i * kEveryV * g.o_token] = from_f32<T>(g.scale * o);
+                }
             }
+            ot += n * g.o_token;
         }
         t0 += n;
         if (t0 >= n_tok) decay(power(g2, (float)(n - 1)));
@@ -318,18 +319,19 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
     else if (last_seg) store(g.state_out + base);
 }
 
-template <typename T, int ROWS, int COLS>
+template <typename T, int ROWS, int COLS, int WARPS>
 cudaError_t launch_recurrent_rows(const DecayArgs& g, cudaStream_t s)
 {
     const int slices = (g.Dv + COLS * 32 - 1) / (COLS * 32);
-    // Few heads and long prompts: segments, until about four CTAs per SM walk a share of the tokens each; one launch finds what
-    // each adds to the state, the next starts each from the decayed sum of what came before it.
+    // Few heads and long prompts: segments, until about sixteen warps per SM walk a share of the tokens each; one launch finds what
+    // each adds to the state (half of the work once more), the next starts each from the decayed sum of what came before it.  Two
+    // segments do not make up for that where one CTA per head already has an SM (4 x 4096 tokens of 16 heads of 128: 805 us, in two 861).
     RecPlan p{};
     const int64_t ctas = g.B * g.H * slices;
-    int64_t segs = 4 * (int64_t)device_sm_count() / ctas;
+    int64_t segs = (16 / WARPS) * (int64_t)device_sm_count() / ctas;
     if (segs > g.max_len / 128) segs = g.max_len / 128;
     if (segs > 16) segs = 16;
-    if (segs < 1) segs = 1;
+    if (segs < 1 || (segs == 2 && 2 * ctas > device_sm_count())) segs = 1;
     p.seg_len = (g.max_len + segs - 1) / segs;
     if (p.seg_len < 1) p.seg_len = 1;
     p.segments = (int)((g.max_len + p.seg_len - 1) / p.seg_len);
@@ -340,11 +342,11 @@ cudaError_t launch_recurrent_rows(const DecayArgs& g, cudaStream_t s)
         e = scratch_alloc(&scratch, (size_t)g.B * g.H * p.segments * g.Dk * g.Dv * sizeof(float), s);
         if (e != cudaSuccess) return e;
         p.local = static_cast<float*>(scratch);
-        decay_recurrent_kernel<T, ROWS, COLS, true><<<dim3((unsigned)g.B, (unsigned)g.H, (unsigned)(slices * (p.segments - 1))), kRecThreads, 0, s>>>(g, p);
+        decay_recurrent_kernel<T, ROWS, COLS, WARPS, true><<<dim3((unsigned)g.B, (unsigned)g.H, (unsigned)(slices * (p.segments - 1))), WARPS * 32, 0, s>>>(g, p);
         e = cudaGetLastError();
     }
     if (e == cudaSuccess) {
-        decay_recurrent_kernel<T, ROWS, COLS, false><<<dim3((unsigned)g.B, (unsigned)g.H, (unsigned)(slices * p.segments)), kRecThreads, 0, s>>>(g, p);
+        decay_recurrent_kernel<T, ROWS, COLS, WARPS, false><<<dim3((unsigned)g.B, (unsigned)g.H, (unsigned)(slices * p.segments)), WARPS * 32, 0, s>>>(g, p);
         e = cudaGetLastError();
     }
     if (scratch != nullptr) {
@@ -357,9 +359,10 @@ cudaError_t launch_recurrent_rows(const DecayArgs& g, cudaStream_t s)
 template <typename T>
 cudaError_t launch_recurrent_typed(const DecayArgs& g, cudaStream_t s)
 {
-    if (g.Dk <= 64) return launch_recurrent_rows<T, 16, 2>(g, s);
-    if (g.Dk <= 128) return launch_recurrent_rows<T, 32, 2>(g, s);
-    return launch_recurrent_rows<T, 64, 1>(g, s);
+    // 8 warps of 16 rows rather than 4 of 32: 128 registers hold them, 2594 -> 1739 us for 32768 tokens of 16 heads of 128
+    if (g.Dk <= 64) return launch_recurrent_rows<T, 16, 2, 4>(g, s);
+    if (g.Dk <= 128) return launch_recurrent_rows<T, 16, 2, 8>(g, s);
+    return launch_recurrent_rows<T, 32, 2, 8>(g, s);
 }
 
 }  // namespace
