@@ -6,7 +6,8 @@
 //
 // with pairs (i, i + R/2) in the half layout and (2i, 2i + 1) in the interleaved one.
 //
-// Bound: DRAM, each element read and written once.  A group of lanes (a power of two, at most a warp) owns one head: a lane
+// Bound: DRAM, each element read and written once: 59 us at the size below are 5.7 TB/s, 0.88 of a plain copy's rate; small calls are
+// bound by their launch (32 tokens: 2.4 us in a graph).  A group of lanes (a power of two, at most a warp) owns one head: a lane
 // holds 16 bytes of it in registers, the sum of squares is a shuffle tree over the group, and in the half layout the
 // lane reads its partner's 16 bytes as well (the line its own group just brought in: one load instead of a shuffle
 // per element).  The cosines, sines and weights of a lane's elements are the same for every head of a token, so a group
@@ -43,12 +44,21 @@ __device__ __forceinline__ void load_floats(const float* p, float (&f)[N])
     }
 }
 
-// `per_group` heads of one token per group of G lanes, HP at a time with the next ones' loads in flight; CH 16-byte chunks per lane
-// (head dimension up to 32 CH chunks).
-template <typename T, int CH, int HP, bool kHalf>
-__global__ void __launch_bounds__(kThreads)
-qk_norm_rotary_kernel(const RotaryArgs g, int G, int per_group, int groups_q, int groups_k)
+__device__ __forceinline__ void copy16_async(uint32_t dst, const void* src, bool real)       // zeros unless `real`
 {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// PG heads of one token per group of G lanes, HP at a time; CH 16-byte chunks per lane (head dimension up to 32 CH chunks).  Many
+// heads are all asked for at once, into shared memory: it holds more of them in flight than registers do (16384 tokens of 32 + 8 heads
+// of 128, bf16: 63 us instead of 74; with 18 CTAs per SM instead of 15, for a few spilled words of the weights, 59).
+template <typename T, int CH, int HP, int PG, bool kHalf>
+__global__ void __launch_bounds__(kThreads, PG > 2 && CH == 1 ? 18 : 1)
+qk_norm_rotary_kernel(const RotaryArgs g, int G, int groups_q, int groups_k)
+{
+    constexpr bool kStage = PG > 2 && CH == 1;
+    __shared__ uint4 stage[kStage ? PG : 1][kStage ? kThreads : 1];
     constexpr int V = Vec16<T>::N;
     const int lane_g = threadIdx.x & (G - 1);
     const unsigned item = blockIdx.x * (unsigned)(kThreads / G) + threadIdx.x / G;
@@ -58,8 +68,8 @@ qk_norm_rotary_kernel(const RotaryArgs g, int G, int per_group, int groups_q, in
     const int gi = (int)(item - t * per_token);
     const bool is_q = gi < groups_q;
     const int H = is_q ? g.Hq : g.Hk;
-    const int h0 = (is_q ? gi : gi - groups_q) * per_group;
-    const int h1 = !live ? h0 : h0 + per_group < H ? h0 + per_group : H;
+    const int h0 = (is_q ? gi : gi - groups_q) * PG;
+    const int h1 = !live ? h0 : h0 + PG < H ? h0 + PG : H;
     const T* src = static_cast<const T*>(is_q ? g.q : g.k) + (int64_t)(live ? t : 0) * (is_q ? g.q_token : g.k_token);
     T* dst = static_cast<T*>(is_q ? g.out_q : g.out_k) + (int64_t)(live ? t : 0) * (is_q ? g.oq_token : g.ok_token);
     const int64_t s_head = is_q ? g.q_head : g.k_head, d_head = is_q ? g.oq_head : g.ok_head;
@@ -85,7 +95,14 @@ qk_norm_rotary_kernel(const RotaryArgs g, int G, int per_group, int groups_q, in
                 }
             }
     };
-    load(h0);
+    if constexpr (kStage) {
+        #pragma unroll
+        for (int p = 0; p < PG; ++p) {
+            const bool real = h0 + p < h1 && lane_g < nch;
+            copy16_async((uint32_t)__cvta_generic_to_shared(&stage[p][threadIdx.x]), real ? at + p * s_head : src, real);
+            if (p % HP == HP - 1) asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    } else load(h0);
 
     int64_t pos = 0;
     const bool pos_ok = !live || g.R == 0 || token_position(g, t, pos);
@@ -97,7 +114,10 @@ qk_norm_rotary_kernel(const RotaryArgs g, int G, int per_group, int groups_q, in
         const int ch = lane_g + c * 32;
         const bool rot = ch < 2 * hch && pos_ok, second = ch >= hch;
         #pragma unroll
-        for (int e = 0; e < V; ++e) { A[c][e] = 1.f; B[c][e] = 0.f; }
+        for (int e = 0; e < V; ++e) {
+            A[c][e] = pos_ok ? 1.f : __int_as_float(0x7fffffff);     // a position outside the table: NaN, never a wrong angle
+            B[c][e] = 0.f;
+        }
         if (rot) {
             const float* row = g.table + pos * g.R;
             if constexpr (kHalf) {
@@ -135,9 +155,25 @@ qk_norm_rotary_kernel(const RotaryArgs g, int G, int per_group, int groups_q, in
             B2[c][e] = make_pair(B[c][2 * e], B[c][2 * e + 1]);
         }
     const float inv_d = 1.f / (float)g.D;
-    const int trips = per_group;                    // the same for every lane: they shuffle together
-    for (int done = 0; done < trips; done += HP) {
+    #pragma unroll (kStage ? PG / HP : 1)
+    for (int done = 0; done < PG; done += HP) {     // (the same for every lane: they shuffle together)
         const int h = h0 + done;
+        if constexpr (kStage) {
+            // (the count of groups still on their way has to be a constant)
+            if (done == 0) copies_wait<PG / HP - 1>();
+            else if (done == HP) copies_wait<PG / HP - 2>();
+            else if (done == 2 * HP) copies_wait<PG / HP - 3>();
+            else copies_wait<0>();
+            __syncwarp();
+            #pragma unroll
+            for (int p = 0; p < HP; ++p) {
+                own[p][0] = stage[done + p][threadIdx.x];
+                if constexpr (kHalf) {
+                    other[p][0] = make_uint4(0, 0, 0, 0);
+                    if (lane_g < 2 * hch) other[p][0] = stage[done + p][threadIdx.x + (lane_g < hch ? hch : -hch)];
+                }
+            }
+        }
         pair_t y[HP][CH][V / 2];
         float r[HP];
         #pragma unroll
@@ -169,16 +205,18 @@ qk_norm_rotary_kernel(const RotaryArgs g, int G, int per_group, int groups_q, in
             r[p] = a + b;
         }
         at += HP * s_head;
-        if (done + HP < trips) load(h + HP);
+        if (!kStage && done + HP < PG) load(h + HP);
         if (w != nullptr) {
-            for (int d = G / 2; d > 0; d >>= 1)
-                #pragma unroll
-                for (int p = 0; p < HP; ++p) r[p] += __shfl_xor_sync(0xffffffffu, r[p], d);
+            #pragma unroll
+            for (int d = 16; d > 0; d >>= 1)
+                if (d < G) {
+                    #pragma unroll
+                    for (int p = 0; p < HP; ++p) r[p] += __shfl_xor_sync(0xffffffffu, r[p], d);
+                }
         }
         #pragma unroll
         for (int p = 0; p < HP; ++p) {
-            float s = w != nullptr ? rsqrtf(fmaf(r[p], inv_d, g.eps)) : 1.f;
-            if (!pos_ok) s = __int_as_float(0x7fffffff);             // a position outside the table: NaN, never a wrong angle
+            const float s = w != nullptr ? rsqrtf(fmaf(r[p], inv_d, g.eps)) : 1.f;
             #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 if (h + p >= h1 || lane_g + c * 32 >= nch) continue;
@@ -267,14 +305,14 @@ __global__ void rotary_table_kernel(float* __restrict__ table, int64_t rows, int
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-template <typename T, int CH, int HP>
-cudaError_t launch_vec(const RotaryArgs& g, int G, int per_group, cudaStream_t s)
+template <typename T, int CH, int HP, int PG>
+cudaError_t launch_vec(const RotaryArgs& g, int G, cudaStream_t s)
 {
-    const int gq = (g.Hq + per_group - 1) / per_group, gk = (g.Hk + per_group - 1) / per_group;
+    const int gq = (g.Hq + PG - 1) / PG, gk = (g.Hk + PG - 1) / PG;
     const int64_t items = g.T * (gq + gk), per_cta = kThreads / G;
     const unsigned grid = (unsigned)((items + per_cta - 1) / per_cta);
-    if (g.layout == RTN_ROTARY_HALF) qk_norm_rotary_kernel<T, CH, HP, true><<<grid, kThreads, 0, s>>>(g, G, per_group, gq, gk);
-    else qk_norm_rotary_kernel<T, CH, HP, false><<<grid, kThreads, 0, s>>>(g, G, per_group, gq, gk);
+    if (g.layout == RTN_ROTARY_HALF) qk_norm_rotary_kernel<T, CH, HP, PG, true><<<grid, kThreads, 0, s>>>(g, G, gq, gk);
+    else qk_norm_rotary_kernel<T, CH, HP, PG, false><<<grid, kThreads, 0, s>>>(g, G, gq, gk);
     return cudaGetLastError();
 }
 
@@ -298,8 +336,8 @@ cudaError_t launch_typed(const RotaryArgs& g, cudaStream_t s)
     // Few tokens: a head per group, for the most groups; many: eight, for the fewest table and weight reads.
     const int64_t warps = g.T * (g.Hq + g.Hk) * G / 32;
     const int per_group = warps > (int64_t)device_sm_count() * 128 ? 8 : warps > (int64_t)device_sm_count() * 32 ? 2 : 1;
-    if (nch > 32) return launch_vec<T, 2, 1>(g, G, per_group, s);
-    return per_group == 1 ? launch_vec<T, 1, 1>(g, G, 1, s) : launch_vec<T, 1, 2>(g, G, per_group, s);
+    if (nch > 32) return per_group == 1 ? launch_vec<T, 2, 1, 1>(g, G, s) : launch_vec<T, 2, 1, 8>(g, G, s);
+    return per_group == 1 ? launch_vec<T, 1, 1, 1>(g, G, s) : per_group == 2 ? launch_vec<T, 1, 2, 2>(g, G, s) : launch_vec<T, 1, 2, 8>(g, G, s);
 }
 
 }  // namespace
