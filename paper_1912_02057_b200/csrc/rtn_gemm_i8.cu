@@ -75,7 +75,8 @@ struct GemmI8Plan {
     int res_vec;            // the residual's rows are 16-byte aligned (set by the launcher)
 };
 
-bool make_gemm_plan(int64_t M, int64_t N, int64_t K, GemmI8Plan& p, int sms)
+// `epilogue`: cycles per output and SM of a linear layer's epilogue (0: rtn_ternary_gemm).
+bool make_gemm_plan(int64_t M, int64_t N, int64_t K, GemmI8Plan& p, int sms, double epilogue = 0.0)
 {
     if (M < 1 || N < 1 || K < 1) return false;
     // Tile shape by a cost model: a K = 128 stage costs the slower of its MMAs (2 TM BN cycles) and of
@@ -90,7 +91,17 @@ bool make_gemm_plan(int64_t M, int64_t N, int64_t K, GemmI8Plan& p, int sms)
             const int64_t nt = ((M + 128 * tm - 1) / (128 * tm)) * ((N + bn - 1) / bn);
             const int64_t rounds = (nt + sms - 1) / sms;
             const double mma = 2.0 * tm * bn, expand = 4.0 * (128 * tm + bn);
-            const double cost = (double)rounds * (mma > expand ? mma : expand);
+            double cost = (double)rounds * (mma > expand ? mma : expand);
+            if (epilogue > 0.0) {
+                // Both operands come expanded (two cycles per row and stage; an MMA of 128 columns takes 430, a stage 700 at least) and the
+                // epilogue counts: under the next tile's products where tensor memory holds two accumulators, after its own where it holds
+                // one.  4096 x 4096 x 4096 with GELU and residual, bf16: 128 x 256 tiles 94 us, 256 x 256 tiles 105; without either 74 and 66.
+                double stage = tm * (2.0 * bn > 430.0 ? 2.0 * bn : 430.0);
+                if (stage < expand / 2) stage = expand / 2;
+                if (stage < 700.0) stage = 700.0;
+                const double main = (double)((K + kBlockCodes - 1) / kBlockCodes) * stage + 1500.0, epi = epilogue * 128 * tm * bn + 3800.0;
+                cost = 2 * tm * bn <= 512 ? (double)(rounds - 1) * (main > epi ? main : epi) + main + epi : (double)rounds * (main + epi);
+            }
             if (best == 0.0 || cost < best) { best = cost; p.TM = tm; p.BN = bn; }
             if (bn <= 128) break;
         }
@@ -723,7 +734,9 @@ cudaError_t launch_gemm_i8(const GemmArgs& g, cudaStream_t s)
 cudaError_t launch_gemm_i8_linear(const GemmArgs& g, const LinearArgs& l, cudaStream_t s)
 {
     GemmI8Plan p;
-    if (!make_gemm_plan(g.M, g.N, g.K, p, device_sm_count())) return cudaErrorInvalidConfiguration;
+    // (from the times of 256 x 256 tiles with and without each)
+    const double epilogue = 0.2 + (l.act != RTN_ACT_NONE ? 0.3 : 0.0) + (l.residual == nullptr ? 0.0 : l.dtype == RTN_F32 ? 0.45 : 0.27);
+    if (!make_gemm_plan(g.M, g.N, g.K, p, device_sm_count(), epilogue)) return cudaErrorInvalidConfiguration;
     CUtensorMap omap;
     memset(&omap, 0, sizeof(omap));
     if (encode_output(&omap, l.out, g.M, g.N, l.out_stride, l.dtype)) p.tma_out = 1;
