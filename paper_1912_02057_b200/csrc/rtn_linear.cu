@@ -5,6 +5,8 @@
 // the POPC rate binds).  A group of GL lanes (a power of two, at most a warp) owns CPG weight rows at a time: lane i takes
 // the 128-code blocks i, i + GL, ... of each (32 adjacent bytes, so a group reads whole lines), keeps a
 // counter pair per activation row and column, and one shuffle tree joins the group.  CPG columns at once keep that many loads in flight.
+// 1 x 4096 x 4096 (4.3 MB of planes): 2.9 us in a graph, 0.2 of a plain copy's rate: the latency of a launch and of two loads one after
+// the other; 48 x 1000 x 512: 5.0 us.
 #include "rtn_internal.cuh"
 #include "rtn_epilogue.cuh"
 #include "rtn_tcgen05.cuh"
@@ -99,6 +101,8 @@ linear_rows_kernel(const GemmArgs g, const LinearArgs p, int GL)
 // sixteen write out.  A lane is one output column: its scale, offset, code sum and bias live in registers, and a warp's
 // store is 32 adjacent columns of a token, with no staging.
 // Bound: the integer pipe (about 100 instructions per row and block to expand) while the weights stream by; the epilogue for short K.
+// 48 x 16384 x 4096 with bias and GELU: 19.6 us in a graph, of which an instruction of 64 columns, its wait and commit are about 430 clocks
+// per block of K (32 blocks: 7 us) and the expansion about as much beside it; 777 x 1000 x 512: 9.9 us.
 // Few tiles and a long K: the K blocks are dealt to the CTAs of a cluster, which leave their int32 sums in shared memory and
 // each finish a share of the tokens from all of them (exact whatever the order).
 constexpr int kTileWarps = 16;

@@ -1,9 +1,10 @@
 """Role timelines of the tensor-core kernels from in-kernel clock stamps.
 
-    python -m paper_1912_02057_b200.timeline [--workload cfg2|layer2|layer3|layer4|cfg3a|cfg3b|gemm2048|gemm4096|gemm8192] [--batch B] [--io fp32|packed]
+    python -m paper_1912_02057_b200.timeline [--workload cfg2|layer2|layer3|layer4|cfg3a|cfg3b|gemm2048|gemm4096|gemm8192|decay64|decay128] [--batch B] [--io fp32|packed]
 
 Builds librtn_b200_timeline.so (the library with -DRTN_TIMELINE, see csrc/rtn_timeline.cuh), runs the workload's
-layer (conv_i8_kernel for cfg2 / layer2, conv_i8s_kernel for cfg3a and cfg3b, gemm_i8_kernel for the square GEMMs) on it a few
+layer (conv_i8_kernel for cfg2 / layer2, conv_i8s_kernel for cfg3a and cfg3b, gemm_i8_kernel for the square GEMMs,
+decay_chunk_kernel with heads of 64 or 128 for decay64 / decay128: 148 heads of 2048 tokens, chunks 4 to 7) on it a few
 times (the last run is reported; earlier ones warm the caches and overlap each launch's
 set-up with the previous kernel's tail as in a stream of layers) and prints, for four CTAs spread over the grid,
 the microseconds after the CTA's entry at which each role began and ended each tile.  The stamps are SM cycle
@@ -27,7 +28,35 @@ SLOTS = {"conv_i8": {"entry": 0, "set-up done": 1, "filters expanded": 2, "epilo
          "gemm_i8": {"entry": 0, "set-up done": 1, "end": 4, "roles": {"mma": 40, "epilogue": 56}, "tiles": 8}}
 # workload -> (instrumented kernel, how to build the case)
 WORKLOADS = {"layer3": "conv_i8r", "layer4": "conv_i8r", "cfg2": "conv_i8", "layer2": "conv_i8", "cfg3a": "conv_i8s", "cfg3b": "conv_i8s",
-             "gemm4096": "gemm_i8", "gemm2048": "gemm_i8", "gemm8192": "gemm_i8"}
+             "gemm4096": "gemm_i8", "gemm2048": "gemm_i8", "gemm8192": "gemm_i8", "decay64": "decay_chunk", "decay128": "decay_chunk"}
+
+# decay_chunk_kernel's stamps of a chunk, in slot order
+DECAY = ("state update begins", "Q S begins", "Q S issued", "state update issued", "P ready", "P V issued", "next scores issued",
+         "scores ready", "P written", "Q S ready", "Q S scaled", "state updated", "state terms written", "V tile landed", "V terms written",
+         "O complete", "O read and staged")
+
+
+def decay_chunks(D, runs, rtn, torch, np, read):
+    """Runs one prompt of 2048 tokens over 148 heads of D and prints chunks 4 to 7 of the recorded CTAs, from each chunk's first stamp."""
+    T, H = 2048, 148
+    q, k, v = (torch.randn(T, H, D, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    log_decay = torch.full((H,), -0.01, device="cuda")
+    start = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    for _ in range(runs):
+        rtn.rtn_decay_attention(q, k, v, log_decay, start, T)
+    torch.cuda.synchronize()
+    assert rtn.rtn_last_device_status() == 0
+    st = read()
+    print(f"one prompt of {T} tokens, {H} heads of {D}, bf16 (decay_chunk kernel): SM clocks of the last of {runs} launches")
+    for c in range(4):
+        if st[c, 0] == 0:
+            continue
+        print(f"CTA {c} of 4 recorded: set-up {st[c, 1] - st[c, 0]}, end {st[c, 4] - st[c, 0]}")
+        for chunk in range(4):
+            at = 8 + 20 * chunk
+            first = st[c, at]
+            print(f"    chunk {chunk + 4} at {first - st[c, 0]}: " +
+                  ", ".join(f"{n} {st[c, at + i] - first}" for i, n in enumerate(DECAY) if i and st[c, at + i]))
 
 
 def main():
@@ -49,6 +78,15 @@ def main():
     L = rtn.lib()
     reader = getattr(L, f"rtn_timeline_read_{tag}")
     reader.argtypes = [ctypes.c_void_p, ctypes.c_int]
+    if a.workload.startswith("decay"):
+        assert reader(None, 1) == 0
+
+        def read():
+            buf = (ctypes.c_longlong * (4 * 96))()
+            assert reader(buf, 0) == 0
+            return np.array(buf, dtype=np.int64).reshape(4, 96)
+        decay_chunks(int(a.workload[5:]), a.runs, rtn, torch, np, read)
+        return 0
     if a.workload.startswith("gemm"):
         case = inputs.config5(int(a.workload[4:]))
         M, N, K = case.M, case.N, case.K
