@@ -360,7 +360,8 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
         }
       }
     } else if (warp >= kWarpP && warp < kWarpV) {
-        // ------------------------------------------------------------ P: row i of the chunk, half of the keys, per thread
+        // ------------------------------------------------------------ P: row i of the chunk, every other 16 keys, per thread
+        // (each of the two warps of 32 rows then has one of the two blocks on the diagonal, which take twice as long as the others)
         regs_down<kRegsP>();
         if constexpr (!kStates) {
             const int i = quad * 32 + lane, half = (warp >> 2) & 1;
@@ -373,7 +374,7 @@ decay_chunk_kernel(const DecayArgs g, const ChunkPlan p, const __grid_constant__
                 if (threadIdx.x == (kWarpP + 3) * 32) CHUNK_TL(7);
                 tc::tc_fence_after_sync();
                 #pragma unroll 1
-                for (int kb = half * 4; kb < half * 4 + 4; ++kb) {            // 16 keys: eight words of high terms, eight of low
+                for (int kb = half; kb < 8; kb += 2) {                        // 16 keys: eight words of high terms, eight of low
                     const uint32_t at = tmem + lanes + kColP + (uint32_t)(kb * 16);
                     const float* w = table + (kC - 1 - i + kb * 16);          // l^(i - key), zero past the diagonal
                     uint32_t t[16];
