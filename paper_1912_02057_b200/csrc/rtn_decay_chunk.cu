@@ -51,7 +51,9 @@ namespace {
 
 constexpr int kC = 128;                     // tokens of a chunk
 constexpr int kThreads = 28 * 32;
-constexpr int kWarpLoadQ = 0, kWarpMma = 1, kWarpLoadK = 2 /* V: 3 */, kWarpS = 4, kWarpP = 12, kWarpV = 20;
+// (the MMA warp on the scheduler with the fewest conversions: heads of 64 have 64 rows of states and values, in the lanes of warps 0 and 1
+// modulo 4; on that of warp 1 a prompt of 32768 tokens of 16 such heads takes 127 us instead of 119)
+constexpr int kWarpLoadQ = 0, kWarpMma = 2, kWarpLoadK = 1 /* V: 3 */, kWarpS = 4, kWarpP = 12, kWarpV = 20;
 // registers a thread: 72 at launch (V keeps them); 40 + 2 x (96 + 64 + 72) = 504 = 7 x 72 per warp group of 128
 constexpr int kRegsRest = 40, kRegsS = 96, kRegsP = 64;
 
@@ -688,11 +690,15 @@ ChunkPlan make_plan(const DecayArgs& g)
 {
     ChunkPlan p{};
     const int64_t chunks = (g.max_len + kC - 1) / kC, ctas = g.B * g.H, sms = device_sm_count();
+    // Times in chunks of the main pass: a segment's chunks in both passes (0.4 in the first), four for another launch, and a sixth for each
+    // segment's part that the last one adds up.  16 heads of 128: 512 tokens 21 us in one segment, 28 in two; 1024 tokens 34 in one, 31 in
+    // four; 2048 tokens 58 in one, 42 in four, 36 in eight.
     int64_t segs = 1;
-    if (ctas < sms) segs = sms / ctas;
-    if (segs > chunks / 4) segs = chunks / 4;
-    if (segs > 16) segs = 16;
-    if (segs < 1) segs = 1;
+    double best = (double)chunks;
+    for (int64_t n = 2; n * ctas <= sms && 2 * n <= chunks; ++n) {
+        const double cost = 1.4 * (double)((chunks + n - 1) / n) + 4.0 + (double)n / 6.0;
+        if (cost < best) { best = cost; segs = n; }
+    }
     p.seg_len = (chunks + segs - 1) / segs * kC;
     if (p.seg_len < kC) p.seg_len = kC;
     p.segments = (int)((chunks * kC + p.seg_len - 1) / p.seg_len);
