@@ -5,7 +5,7 @@
 //
 // decay_step_kernel: one token per sequence.  Bound: DRAM, the fp32 state read and written once (8 Dk Dv bytes per head
 //   against 4 Dk Dv operations).
-//   96 sequences x 32 heads of 128 x 128: 66 us in a graph, 6.1 TB/s (0.94 of a plain copy's rate).
+//   96 sequences x 32 heads of 128 x 128: 62 us in a graph, 6.5 TB/s, a plain copy's rate.
 // decay_recurrent_kernel: whole prompts token by token with the state in registers; any type, head dimension and
 //   stride.  Bound: the FMA pipe (two FMAs per state element and token), behind a chain of about 280 clocks per token that two or
 //   three CTAs per SM hide in part.  8 x 2048 tokens, 32 heads of 128, fp16: 1084 us, 0.44 of the pipe's rate.
@@ -19,12 +19,11 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------ single tokens
 
-constexpr int kStepThreads = 256;
 constexpr int kStepBatch = 8;           // state vectors a thread has in flight
 
 // CTA = (sequence, head, slice of VW-element column groups).  Thread (r, c) owns columns VW c .. of the rows r, r + nr, ...:
 // a warp reads whole sectors of consecutive rows, and every state element is touched once.
-template <typename T, int VW>
+template <typename T, int VW, int kStepThreads>
 __global__ void __launch_bounds__(kStepThreads)
 decay_step_kernel(const DecayArgs g, int slice, int slices)
 {
@@ -49,20 +48,14 @@ decay_step_kernel(const DecayArgs g, int slice, int slices)
     const int c = threadIdx.x % cw, r0 = threadIdx.x / cw;
     const int64_t base = (slot * g.H + h) * (int64_t)g.Dk * g.Dv + c0 + c * VW;
     const bool mine = r0 < nr;
-    for (int i = threadIdx.x; i < g.Dk; i += kStepThreads) { sq[i] = to_f32(q[i]); sk[i] = to_f32(k[i]); }
-    float vv[VW], acc[VW];
-    #pragma unroll
-    for (int e = 0; e < VW; ++e) { vv[e] = mine ? to_f32(v[c * VW + e]) : 0.f; acc[e] = 0.f; }
-    const float l = expf(g.log_decay[h]);
-    __syncthreads();
-    for (int r = r0; mine && r < g.Dk; r += kStepBatch * nr) {
-        float s[kStepBatch][VW];
+    float s[kStepBatch][VW];
+    auto load = [&](int r) {                // the rows r, r + nr, ... of a batch
         #pragma unroll
         for (int i = 0; i < kStepBatch; ++i) {
             const int row = r + i * nr;
             #pragma unroll
             for (int e = 0; e < VW; ++e) s[i][e] = 0.f;
-            if (g.state != nullptr && row < g.Dk) {
+            if (mine && g.state != nullptr && row < g.Dk) {
                 const float* p = g.state + base + (int64_t)row * g.Dv;
                 if constexpr (VW == 4) {
                     const float4 f = *reinterpret_cast<const float4*>(p);
@@ -70,6 +63,15 @@ decay_step_kernel(const DecayArgs g, int slice, int slices)
                 } else s[i][0] = *p;
             }
         }
+    };
+    load(r0);                               // (on its way while q and k are: 238 sequences x 8 heads of 64: 16.3 us instead of 18.6)
+    for (int i = threadIdx.x; i < g.Dk; i += kStepThreads) { sq[i] = to_f32(q[i]); sk[i] = to_f32(k[i]); }
+    float vv[VW], acc[VW];
+    #pragma unroll
+    for (int e = 0; e < VW; ++e) { vv[e] = mine ? to_f32(v[c * VW + e]) : 0.f; acc[e] = 0.f; }
+    const float l = expf(g.log_decay[h]);
+    __syncthreads();
+    for (int r = r0; mine && r < g.Dk; r += kStepBatch * nr) {
         #pragma unroll
         for (int i = 0; i < kStepBatch; ++i) {
             const int row = r + i * nr;
@@ -84,6 +86,7 @@ decay_step_kernel(const DecayArgs g, int slice, int slices)
             if constexpr (VW == 4) *reinterpret_cast<float4*>(p) = make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
             else *p = s[i][0];
         }
+        if (r + kStepBatch * nr < g.Dk) load(r + kStepBatch * nr);
     }
     #pragma unroll
     for (int e = 0; e < VW; ++e) red[threadIdx.x * VW + e] = acc[e];
@@ -99,12 +102,17 @@ template <typename T>
 cudaError_t launch_step_typed(const DecayArgs& g, cudaStream_t s)
 {
     const bool vec = g.Dv % 4 == 0 && (reinterpret_cast<uintptr_t>(g.state) & 15) == 0 && (reinterpret_cast<uintptr_t>(g.state_out) & 15) == 0;
-    // few heads in all: 32 columns (whole 128-byte rows) per CTA, so that more SMs pull on the memory
-    const int slice = g.B * g.H < 2 * device_sm_count() ? 32 : kDecayMaxDim;
+    // As many columns (whole 128-byte rows) per CTA as make one batch of 128 threads, fewer where there are few heads and SMs are left: 15
+    // sequences x 32 heads of 128 in slices of 32 columns 13.2 us, 128 at once 14.7; 131 x 16 of 64 in slices of 32 15.8 us, 64 at once 13.0
+    const int fit = 128 * kStepBatch * 4 / g.Dk / 32 * 32;
+    const int slice = g.B * g.H < 2 * device_sm_count() || fit < 32 ? 32 : fit < kDecayMaxDim ? fit : kDecayMaxDim;
     const int slices = (g.Dv + slice - 1) / slice;
     const unsigned grid = (unsigned)(g.B * g.H * slices);
-    if (vec) decay_step_kernel<T, 4><<<grid, kStepThreads, 0, s>>>(g, slice, slices);
-    else decay_step_kernel<T, 1><<<grid, kStepThreads, 0, s>>>(g, slice, slices);
+    // 64 x 64 states are one batch of 128 threads, larger ones take 256 (238 sequences x 8 heads of 64: 12.4 us instead of 16.3)
+    const bool small = (int64_t)g.Dk * (g.Dv < slice ? g.Dv : slice) <= 128 * kStepBatch * 4;
+    if (vec && small) decay_step_kernel<T, 4, 128><<<grid, 128, 0, s>>>(g, slice, slices);
+    else if (vec) decay_step_kernel<T, 4, 256><<<grid, 256, 0, s>>>(g, slice, slices);
+    else decay_step_kernel<T, 1, 256><<<grid, 256, 0, s>>>(g, slice, slices);
     return cudaGetLastError();
 }
 
