@@ -408,16 +408,19 @@ cudaError_t launch_rows(const GemmArgs& g, const LinearArgs& l, cudaStream_t s)
 // Which of the three forms a shape takes; times in a graph on one B200 (bf16 out, us):
 //                      M   N     K      rows   tiles  two launches
 //   rows              16  4096  4096     9.8   12.0   26.5
-//                     48  1000   512     5.0    8.4    8.9
+//                     64  2048   512     4.7    7.0             1000   100   300   4.8    6.5
 //   tiles             24  4096  4096    13.5   14.3   26.5        16  4096 16384  24.2  19.1  85.9
-//                    256  4096  4096           21.4   23.1
+//                    256  4096  4096           21.4   23.1       643   809   247  10.4    6.3
 //   two launches     512  4096  4096           26.2   23.0       256 16384  4096        44.0  36.4
-// rows: the weights are streamed once per eight rows and the POPC rate binds, 2.9 us per million rows x columns x blocks, on top of 4; tiles
-// start at 8 and never under 0.3 us per block of K.  Over 64 tokens a tile, or over one round of tiles, the weights' planes are
+// rows: the weights are streamed once per eight rows and the POPC rate binds, 2.9 us per million rows x columns x blocks, on top of 4 (with
+// one or two blocks of K the lanes of a group are too few for the outputs: 100 x 1000 x 128 8.0 us, in tiles 5.7); tiles start at 7 and take
+// 0.11 us and more per block of K.  Over 64 tokens a tile, or over one round of tiles, the weights' planes are
 // better expanded once, by a launch of their own.
 bool linear_rows_path(int64_t M, int64_t N, int64_t K)
 {
-    return M <= kMaxRows || (double)M * (double)N * (double)((K + kBlockCodes - 1) / kBlockCodes) <= 2.5e6 || !gemm_i8_supported(M, N, K);
+    const double nblk = (double)((K + kBlockCodes - 1) / kBlockCodes);
+    const bool rows_win = nblk > 2 && 2.9e-6 * (double)M * (double)N * nblk <= 3.0 + 0.11 * nblk;
+    return M <= kMaxRows || rows_win || !gemm_i8_supported(M, N, K);
 }
 
 cudaError_t launch_linear(const GemmArgs& g, const LinearArgs& l, cudaStream_t s)
