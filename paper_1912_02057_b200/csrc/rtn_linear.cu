@@ -345,21 +345,21 @@ TilePlan make_tile_plan(int64_t M, int64_t N, int64_t K)
     const int sms = device_sm_count();
     const int nblk = (int)((K + kBlockCodes - 1) / kBlockCodes);
     p.tiles_n = (int)((N + 127) / 128);
-    // Tokens of a tile: what makes rounds of CTAs times a tile's time least.  Per block the slower of expanding 128 + BT rows (1.6
-    // clocks each) and the MMAs (2 BT); 30 clocks per token for the epilogue; 4000 to start and end.
+    // Tokens of a tile, and CTAs of a cluster that share its K (while one keeps at least four blocks and the machine has the SMs): what
+    // makes rounds of CTAs times a tile's time least.  Per block the slower of expanding 128 + BT rows (1.6 clocks each) and the MMAs (2 BT);
+    // 30 clocks per token for the epilogue, shared by a cluster, which takes 2000 to meet; 4000 to start and end.  Clusters of eight fill
+    // three quarters of the machine at most (more of them wait for a place: 64 x 1024 x 16384 26 us, in clusters of four 16).
     double best = 0.0;
     const int most = M >= kTileMaxTokens ? kTileMaxTokens : (int)((M + 15) / 16 * 16);
     for (int bt = 16; bt <= most; bt += 16) {
         if (bt > 128 && bt % 32 != 0 && bt != most) continue;
-        const int64_t tiles = (int64_t)p.tiles_n * ((M + bt - 1) / bt);
+        const int64_t tiles_m = (M + bt - 1) / bt, tiles = (int64_t)p.tiles_n * tiles_m;
+        int slices = 1;
+        while (slices < 8 && bt <= 64 && tiles * slices * 2 <= (slices < 4 ? sms : sms * 3 / 4) && nblk >= slices * 8) slices *= 2;
         const double block = 1.6 * (128 + bt) > 2.0 * bt ? 1.6 * (128 + bt) : 2.0 * bt;
-        const double cost = (double)((tiles + sms - 1) / sms) * (4000.0 + nblk * block + 30.0 * bt);
-        if (p.BT == 0 || cost < best) { best = cost; p.BT = bt; }
+        const double cost = (double)((tiles + sms - 1) / sms) * (4000.0 + (nblk + slices - 1) / slices * block + 30.0 * bt / slices + (slices > 1 ? 2000.0 : 0.0));
+        if (p.BT == 0 || cost < best) { best = cost; p.BT = bt; p.slices = slices; p.tiles_m = (int)tiles_m; }
     }
-    p.tiles_m = (int)((M + p.BT - 1) / p.BT);
-    // K over a cluster while it leaves a CTA at least four blocks and the machine has the SMs
-    p.slices = 1;
-    while (p.slices < 8 && (int64_t)p.tiles_n * p.tiles_m * p.slices * 2 <= sms && nblk >= p.slices * 8) p.slices *= 2;
     const int stage = (128 + p.BT) * 128;
     p.stages = kTileMaxStages;                  // a power of two: a team of warps for each
     while (p.stages * stage > kTileRing) p.stages /= 2;
@@ -407,10 +407,10 @@ cudaError_t launch_rows(const GemmArgs& g, const LinearArgs& l, cudaStream_t s)
 
 // Which of the three forms a shape takes; times in a graph on one B200 (bf16 out, us):
 //                      M   N     K      rows   tiles  two launches
-//   rows              16  4096  4096     9.8   12.0   26.5
+//   rows               9  4096  4096     9.3   10.5
 //                     64  2048   512     4.7    7.0             1000   100   300   4.8    6.5
-//   tiles             24  4096  4096    13.5   14.3   26.5        16  4096 16384  24.2  19.1  85.9
-//                    256  4096  4096           21.4   23.1       643   809   247  10.4    6.3
+//   tiles             24  4096  4096    13.5   10.9   26.5        16  4096 16384  24.2  18.9  85.9
+//                    256  4096  4096           20.6   23.1       643   809   247  10.4    6.3
 //   two launches     512  4096  4096           26.2   23.0       256 16384  4096        44.0  36.4
 // rows: the weights are streamed once per eight rows and the POPC rate binds, 2.9 us per million rows x columns x blocks, on top of 4 (with
 // one or two blocks of K the lanes of a group are too few for the outputs: 100 x 1000 x 128 8.0 us, in tiles 5.7); tiles start at 7 and take
