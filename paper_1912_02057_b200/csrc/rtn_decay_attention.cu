@@ -8,7 +8,7 @@
 //   96 sequences x 32 heads of 128 x 128: 62 us in a graph, 6.5 TB/s, a plain copy's rate.
 // decay_recurrent_kernel: whole prompts token by token with the state in registers; any type, head dimension and
 //   stride.  Bound: the FMA pipe (two FMAs per state element and token), behind a chain of about 280 clocks per token that two or
-//   three CTAs per SM hide in part.  8 x 2048 tokens, 32 heads of 128, fp16: 1084 us, 0.44 of the pipe's rate.
+//   three CTAs per SM hide in part.  8 x 2048 tokens, 32 heads of 128, fp16: 1091 us, 0.44 of the pipe's rate.
 #include "rtn_internal.cuh"
 #include "rtn_types.cuh"
 #include "rtn_decay.cuh"

@@ -22,6 +22,9 @@
 //   the scores' conversion then runs beside Q S and the state update, the state's beside P V and the next scores.
 // The conversions are what the kernel spends its issue slots on, with a chain of dependent instructions per value: two warps per
 // role and scheduler hide what one could not.  The state's 64 registers a thread come from the other roles' shares (setmaxnreg).
+// Bound: at D = 128 a chunk's products are 4100 clocks of the tensor pipe (terms counted), the hand-overs between them and the
+// conversions make them 5900; the conversions use 0.59 of the issue slots.  148 heads of 2048 tokens: D = 128 73 us, 0.67 of a plain copy
+// of the same bytes, D = 64 44 us, 0.54.
 // Tensor memory (512 columns): state update | scores, then P | O | two entries of V terms (what is left of each 128 columns, too).
 //
 // Rows past a sequence's end belong to its neighbour: K and V rows are zeroed in shared memory before a product reads

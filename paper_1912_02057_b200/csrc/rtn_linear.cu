@@ -101,8 +101,8 @@ linear_rows_kernel(const GemmArgs g, const LinearArgs p, int GL)
 // sixteen write out.  A lane is one output column: its scale, offset, code sum and bias live in registers, and a warp's
 // store is 32 adjacent columns of a token, with no staging.
 // Bound: the integer pipe (about 100 instructions per row and block to expand) while the weights stream by; the epilogue for short K.
-// 48 x 16384 x 4096 with bias and GELU: 19.6 us in a graph, of which an instruction of 64 columns, its wait and commit are about 430 clocks
-// per block of K (32 blocks: 7 us) and the expansion about as much beside it; 777 x 1000 x 512: 9.9 us.
+// 48 x 16384 x 4096 with bias and GELU: 20 us in a graph, of which an instruction of 64 columns, its wait and commit are about 430 clocks
+// per block of K (32 blocks: 7 us) and the expansion about as much beside it; 777 x 1000 x 512 with bias and SiLU: 10 us.
 // Few tiles and a long K: the K blocks are dealt to the CTAs of a cluster, which leave their int32 sums in shared memory and
 // each finish a share of the tokens from all of them (exact whatever the order).
 constexpr int kTileWarps = 16;
