@@ -8,7 +8,7 @@
 //   96 sequences x 32 heads of 128 x 128: 62 us in a graph, 6.5 TB/s, a plain copy's rate.
 // decay_recurrent_kernel: whole prompts token by token with the state in registers; any type, head dimension and
 //   stride.  Bound: the FMA pipe (two FMAs per state element and token), behind a chain of about 280 clocks per token that two or
-//   three CTAs per SM hide in part.  8 x 2048 tokens, 32 heads of 128, fp16: 1091 us, 0.44 of the pipe's rate.
+//   three CTAs per SM hide in part.  8 prompts of 2048 tokens, 32 heads of 128, fp16: 1310 us, 0.35 of that rate.
 #include "rtn_internal.cuh"
 #include "rtn_types.cuh"
 #include "rtn_decay.cuh"
@@ -129,11 +129,13 @@ struct RecPlan {
 // l^n from log2 l; n = 0 gives 1 for every l.
 __device__ __forceinline__ float power(float g2, float n) { return n == 0.f ? 1.f : exp2f(n * g2); }
 
-// Column(s) of the state in the lanes of each warp, ROWS rows of it in registers by pairs.  Within a tile of tokens i = 0, 1, ... the state is kept
-// relative to the tile's first token,
+// Column(s) of the state in the lanes of each warp, ROWS rows of it in registers by pairs.  Within a run of tokens i = 0, 1, ... the state is kept
+// relative to the run's first token,
 //   S_i = l^i S'_i,   S'_i = S'_(i-1) + (l^-i k_i) v_i^T,   o_i = (l^i q_i)^T S'_i,
-// which leaves one FMA per element for the update and one for the output, two elements to an instruction.  A tile ends before
-// l^-i passes e^60; at l = 0 it is one token.
+// which leaves one FMA per element for the update and one for the output, two elements to an instruction.  A run is a tile or a half,
+// a quarter, an eighth of one, the longest whose l^-i stay at 2^8 or below: the range of k v and of q is then fp32's own but for eight
+// powers of two.  What the steeper heads' extra products cost: 1310 us for 8 x 2048 tokens of 32 heads of 128, fp16, at log decays down to
+// -0.79, 1342 at -1, 1390 at -3, 1477 at -8.
 template <typename T, int ROWS, int COLS, int WARPS, bool kStates>
 __global__ void __launch_bounds__(WARPS * 32, WARPS == 4 ? 3 : 2)         // (a fourth CTA of 4 warps: 2 x 9656 tokens of heads of 64, 318 us instead of 256)
 decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
@@ -167,8 +169,9 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
     const T* k = static_cast<const T*>(g.k) + first * g.k_token + hk * g.k_head;
     const T* v = static_cast<const T*>(g.v) + first * g.v_token + hk * g.v_head + c0;
     const float g2 = g.log_decay[h] * 1.4426950408889634f;
-    const float reach = 86.f / fmaxf(fabsf(g2), 1e-6f);                     // steps until |log2| passes 86 (about e^60)
-    const int tile = reach >= (float)(kRecTile - 1) ? kRecTile : 1 + (int)reach;
+    const float steep = fabsf(g2);
+    const int run = steep <= 8.f / 7.f ? 8 : steep <= 8.f / 3.f ? 4 : steep <= 8.f ? 2 : 1;
+    static_assert(kRecTile == 8, "runs");
     const int64_t base = (slot * g.H + h) * (int64_t)g.Dk * g.Dv + c0 + lane;
     const int64_t slice = (int64_t)g.Dk * g.Dv, local_base = (b * g.H + h) * (int64_t)p.segments * slice + c0 + lane;
     pair_t S[COLS][ROWS / 2];
@@ -222,6 +225,7 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
                 add(p.local + local_base + (x + 1) * slice, power(g2, (float)((int64_t)(seg - 1 - x) * p.seg_len)));
         }
     }
+    const float run_decay = power(g2, (float)run);
     auto decay = [&](float l) {
         #pragma unroll
         for (int c = 0; c < COLS; ++c)
@@ -249,14 +253,15 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
     float own_grow[kPer], own_shrink[kStates ? 1 : kPer];
     #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        own_grow[i] = tk + i * kEveryK < tile ? power(g2, -(float)(tk + i * kEveryK)) : 0.f;
-        if constexpr (!kStates) own_shrink[i] = power(g2, (float)(tk + i * kEveryK));
+        const float place = (float)((tk + i * kEveryK) & (run - 1));
+        own_grow[i] = power(g2, -place);
+        if constexpr (!kStates) own_shrink[i] = power(g2, place);
     }
     T* ot = out + tv * g.o_token + dv;
     int64_t t0 = 0;
-    fetch(n_tok < tile ? (int)n_tok : tile);
+    fetch(n_tok < kRecTile ? (int)n_tok : kRecTile);
     while (t0 < n_tok) {
-        const int n = n_tok - t0 < tile ? (int)(n_tok - t0) : tile;
+        const int n = n_tok - t0 < kRecTile ? (int)(n_tok - t0) : kRecTile;
         #pragma unroll
         for (int i = 0; i < kPer; ++i) {                // (rows past the tile's length: not looked at)
             if constexpr (!kStates) sq[tk + i * kEveryK][dk] = to_f32(rq[i]) * own_shrink[i];
@@ -265,10 +270,10 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
         #pragma unroll
         for (int i = 0; i < kPerV; ++i) sv[tv + i * kEveryV][dv] = to_f32(rv[i]);
         const int64_t t1 = t0 + n;
-        fetch(n_tok - t1 < tile ? (int)(n_tok - t1) : tile);
-        decay(power(g2, t0 == 0 ? 1.f : (float)tile));
+        fetch(n_tok - t1 < kRecTile ? (int)(n_tok - t1) : kRecTile);
+        decay(t0 == 0 ? power(g2, 1.f) : run_decay);
         __syncthreads();
-        for (int t = 0; t < n; ++t) {
+        auto token = [&](int t) {
             pair_t vt[COLS], o[COLS];
             #pragma unroll
             for (int c = 0; c < COLS; ++c) {
@@ -305,6 +310,15 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
                     so[t][warp][lane + 32 * c] = a + b2;
                 }
             }
+        };
+        if (run == kRecTile) {                          // (with the test in one loop for both: 1472 us instead of 1310, 8 x 2048 tokens of 32 heads of 128)
+            for (int t = 0; t < n; ++t) token(t);
+        } else {
+            #pragma unroll 1
+            for (int t = 0; t < n; ++t) {
+                if (t > 0 && (t & (run - 1)) == 0) decay(run_decay);
+                token(t);
+            }
         }
         __syncthreads();
         if constexpr (!kStates) {
@@ -321,7 +335,7 @@ decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
             ot += n * g.o_token;
         }
         t0 += n;
-        if (t0 >= n_tok) decay(power(g2, (float)(n - 1)));
+        if (t0 >= n_tok) decay(power(g2, (float)((n - 1) & (run - 1))));
     }
     if (kStates) store(p.local + local_base + (seg + 1) * slice);
     else if (last_seg) store(g.state_out + base);
@@ -367,7 +381,7 @@ cudaError_t launch_recurrent_rows(const DecayArgs& g, cudaStream_t s)
 template <typename T>
 cudaError_t launch_recurrent_typed(const DecayArgs& g, cudaStream_t s)
 {
-    // 8 warps of 16 rows rather than 4 of 32: 128 registers hold them, 2594 -> 1739 us for 32768 tokens of 16 heads of 128
+    // 8 warps of 16 rows rather than 4 of 32: 128 registers hold them, 2594 -> 1743 us for 32768 tokens of 16 heads of 128
     if (g.Dk <= 64) return launch_recurrent_rows<T, 16, 2, 4>(g, s);
     if (g.Dk <= 128) return launch_recurrent_rows<T, 16, 2, 8>(g, s);
     return launch_recurrent_rows<T, 32, 2, 8>(g, s);

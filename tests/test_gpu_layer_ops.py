@@ -593,3 +593,31 @@ def test_a_rows_result_does_not_depend_on_how_many_come_with_it(K):
         part = (big[0][:M], big[1][:M], *big[2:4], M, *big[5:7], big[7][:M], big[8][:M], *big[9:])
         assert torch.equal(rtn.rtn_ternary_linear(*part, bias=bias, activation=rtn.ACT_GELU), whole[:M]), M
     assert rtn.rtn_last_device_status() == 0
+
+
+# ---------------------------------------------------------------------------------------------- steep decays, values far from one
+
+@pytest.mark.parametrize("log_decay", [-0.3, -0.6, -3.0, -5.0, -8.0, -8.5, -10.0, -20.0])
+@pytest.mark.parametrize("dtype,D,longest", [(torch.float32, 64, 70), (torch.float32, 128, 30), (torch.bfloat16, 96, 40), (torch.bfloat16, 64, 15),
+                                             (torch.bfloat16, 64, 200)], ids=ids)
+@pytest.mark.parametrize("q_power,v_power", [(0, 60), (0, 100), (0, -60), (-60, 60), (60, -60), (-100, 0), (100, 0)])
+def test_steep_decays_of_values_far_from_one(log_decay, dtype, D, longest, q_power, v_power):
+    """Finite inputs with a finite result give it, whatever the decay: no factor on the way is far from one."""
+    lens, H = [longest, 3], 2
+    q, k, v, g, start = decay_case(lens, H, 1, D, D, dtype, log_decay=np.array([log_decay, -0.01], np.float32))
+    q, v = q * 2.0 ** q_power, v * 2.0 ** v_power
+    state = (np.random.default_rng(3).normal(size=(2, H, D, D)) * 2.0 ** v_power).astype(np.float32)
+    want, mag, end, mag_end = ref.decay(ref.f64(q), ref.f64(k), ref.f64(v), g, start, state, D ** -0.5)
+    out, got = rtn.rtn_decay_attention(q, k, v, cuda(g), cuda(start), longest, state=cuda(state))
+    c = ref.decay_roundings(g, longest, D)
+    ref.assert_close(out, want, mag, c, "out", extra=2.0 ** -15 if dtype == torch.bfloat16 else 0.0)
+    ref.assert_close(got, end, mag_end, c, "state")
+    # token by token through the other entry point
+    after = cuda(state)
+    for t in range(longest):
+        rows = [b for b, n in enumerate(lens) if t < n]
+        at = start[rows] + t
+        slots = torch.tensor(rows, dtype=torch.int32, device="cuda")
+        one, _ = rtn.rtn_decay_attention_step(*(x[cuda(at).long()] for x in (q, k, v)), cuda(g), after, slots=slots)
+        ref.assert_close(one, want[at], mag[at], c, "token")
+    ref.assert_close(after, end, mag_end, c, "tokens' state")
