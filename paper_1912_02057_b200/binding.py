@@ -3,7 +3,11 @@
 Argument marshalling only: torch supplies device memory and the current stream; every step of
 the path runs in the library's CUDA kernels.  There is no fallback: if the shared library is
 missing, the first call raises.
+
+``stream=S`` stands for ``with torch.cuda.stream(S)`` around the call: the results a call makes belong to S, and as there the
+caller sees to it that inputs made on another stream are complete, and stay, until S has used them.
 """
+import contextlib
 import ctypes as C
 import os
 
@@ -154,6 +158,22 @@ def _stream(stream):
     return C.c_void_p(stream.cuda_stream)
 
 
+def _on(stream):
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def _empty(shape, dtype, device, stream):
+    """A result of the stream that writes it: on the current one's memory it could take the place of a tensor whose last use
+    there is still to come."""
+    with _on(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _zeros(n, dtype, stream):
+    with _on(stream):
+        return torch.zeros((n,), dtype=dtype, device="cuda")
+
+
 def _check(code, where):
     if code != 0:
         raise RtnError(code, where)
@@ -183,8 +203,8 @@ def rtn_pack_weights(w_codes, stream=None):
     else:
         N, Cin, kh, kw = w_codes.shape
     Kc = rtn_conv_packed_k(Cin, kh, kw)
-    w_packed = torch.empty((N, rtn_packed_row_bytes(Kc)), dtype=torch.uint8, device=w_codes.device)
-    w_sum = torch.empty((1 + kh * kw, N), dtype=torch.int32, device=w_codes.device)
+    w_packed = _empty((N, rtn_packed_row_bytes(Kc)), torch.uint8, w_codes.device, stream)
+    w_sum = _empty((1 + kh * kw, N), torch.int32, w_codes.device, stream)
     _check(lib().rtn_pack_weights(_ptr(w_codes, torch.int8), N, Cin, kh, kw, _ptr(w_packed),
                                   _ptr(w_sum), _stream(stream)), "rtn_pack_weights")
     return w_packed, w_sum
@@ -193,10 +213,8 @@ def rtn_pack_weights(w_codes, stream=None):
 def rtn_ternarize_pack_act(a, t_lo, t_hi, want_sum=True, out=None, out_sum=None, stream=None):
     """fp32 [M,K] -> (a_packed uint8 [M, row_bytes], a_sum int32 [M] or None)."""
     M, K = a.shape
-    a_packed = out if out is not None else torch.empty((M, rtn_packed_row_bytes(K)),
-                                                       dtype=torch.uint8, device=a.device)
-    a_sum = out_sum if out_sum is not None else (
-        torch.empty((M,), dtype=torch.int32, device=a.device) if want_sum else None)
+    a_packed = out if out is not None else _empty((M, rtn_packed_row_bytes(K)), torch.uint8, a.device, stream)
+    a_sum = out_sum if out_sum is not None else (_empty((M,), torch.int32, a.device, stream) if want_sum else None)
     _check(lib().rtn_ternarize_pack_act(_ptr(a, torch.float32), M, K, _ptr(t_lo, torch.float32),
                                         _ptr(t_hi, torch.float32), t_lo.numel(), _ptr(a_packed),
                                         _ptr(a_sum, torch.int32, allow_none=True), _stream(stream)),
@@ -208,7 +226,7 @@ def rtn_ternary_gemm(a_packed, a_sum, w_packed, w_sum, M, N, K, a_scale, a_offse
                      w_offset, out=None, dbg_acc=None, variant=VARIANT_AUTO, stream=None):
     """Packed ternary GEMM + affine epilogue -> fp32 [M,N].  ``dbg_acc`` (int32 [M,N]) receives raw S_xw."""
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float32, device=a_packed.device)
+        out = _empty((M, N), torch.float32, a_packed.device, stream)
     _check(lib().rtn_ternary_gemm(
         _ptr(a_packed), _ptr(a_sum, torch.int32), _ptr(w_packed), _ptr(w_sum, torch.int32),
         M, N, K, _ptr(a_scale, torch.float32), _ptr(a_offset, torch.float32), a_scale.numel(),
@@ -225,7 +243,7 @@ def rtn_ternary_conv2d(x, t_lo, t_hi, w_packed, w_sum, N, kh, kw, stride, pad, p
     B, Cin, H, W = x.shape
     Ho, Wo = rtn_conv_out_dim(H, kh, stride, pad), rtn_conv_out_dim(W, kw, stride, pad)
     if out is None:
-        out = torch.empty((B, N, Ho, Wo), dtype=torch.float32, device=x.device)
+        out = _empty((B, N, Ho, Wo), torch.float32, x.device, stream)
     _check(lib().rtn_ternary_conv2d(
         _ptr(x, torch.float32), B, Cin, H, W, _ptr(t_lo, torch.float32), _ptr(t_hi, torch.float32),
         t_lo.numel(), _ptr(w_packed), _ptr(w_sum, torch.int32), N, kh, kw, stride, pad,
@@ -293,7 +311,7 @@ def rtn_ternary_conv2d_packed(x_packed, B, Cin, H, W, w_packed, w_sum, N, kh, kw
 def rtn_pack_quaternary(q_values, stream=None):
     """uint8 values [rows,K] in {0..3} on the device -> packed rows uint8 [rows, row_bytes]."""
     rows, K = q_values.shape
-    packed = torch.empty((rows, rtn_packed_row_bytes(K)), dtype=torch.uint8, device=q_values.device)
+    packed = _empty((rows, rtn_packed_row_bytes(K)), torch.uint8, q_values.device, stream)
     _check(lib().rtn_pack_quaternary(_ptr(q_values, torch.uint8), rows, K, _ptr(packed), _stream(stream)),
            "rtn_pack_quaternary")
     return packed
@@ -302,7 +320,7 @@ def rtn_pack_quaternary(q_values, stream=None):
 def rtn_quaternary_gemm(a_packed, w_packed, M, N, K, out=None, stream=None):
     """Packed 2-bit x 2-bit GEMM (the paper's comparison workload) -> exact int32 [M,N]."""
     if out is None:
-        out = torch.empty((M, N), dtype=torch.int32, device=a_packed.device)
+        out = _empty((M, N), torch.int32, a_packed.device, stream)
     _check(lib().rtn_quaternary_gemm(_ptr(a_packed), _ptr(w_packed), M, N, K, _ptr(out, torch.int32),
                                      _stream(stream)), "rtn_quaternary_gemm")
     return out
@@ -339,7 +357,7 @@ def rtn_last_device_status(stream=None):
 def rtn_selftest_wait_timeout(polls=1024, stream=None):
     """Runs the library's bounded wait on an mbarrier nothing arrives on.  Returns the device int32 tensor that
     receives 1 when the wait gave up; the next rtn_last_device_status then reports RTN_ERR_DEVICE_TIMEOUT once."""
-    gave_up = torch.zeros((1,), dtype=torch.int32, device="cuda")
+    gave_up = _zeros(1, torch.int32, stream)
     _check(lib().rtn_selftest_wait_timeout(int(polls), _ptr(gave_up, torch.int32), _stream(stream)),
            "rtn_selftest_wait_timeout")
     return gave_up
@@ -348,7 +366,7 @@ def rtn_selftest_wait_timeout(polls=1024, stream=None):
 def rtn_probe_peak_i8(n_mma, stream=None):
     """Launches the int8 tensor-pipe probe; returns (cycles int64 [CTAs] on the device, operations per CTA)."""
     ctas = int(lib().rtn_probe_ctas())
-    cycles = torch.zeros((ctas,), dtype=torch.int64, device="cuda")
+    cycles = _zeros(ctas, torch.int64, stream)
     _check(lib().rtn_probe_peak_i8(int(n_mma), _ptr(cycles, torch.int64), _stream(stream)), "rtn_probe_peak_i8")
     return cycles, int(n_mma) * int(lib().rtn_probe_i8_ops_per_mma())
 
@@ -357,7 +375,7 @@ def rtn_probe_i8_rate(n_cols, n_mma, stream=None):
     """The tensor-pipe probe with accumulators of n_cols columns; returns (cycles int64 [CTAs] on the device,
     operations per CTA)."""
     ctas = int(lib().rtn_probe_ctas())
-    cycles = torch.zeros((ctas,), dtype=torch.int64, device="cuda")
+    cycles = _zeros(ctas, torch.int64, stream)
     _check(lib().rtn_probe_i8_rate(int(n_cols), int(n_mma), _ptr(cycles, torch.int64), _stream(stream)), "rtn_probe_i8_rate")
     return cycles, int(n_mma) * 2 * 128 * int(n_cols) * 32
 
@@ -365,8 +383,8 @@ def rtn_probe_i8_rate(n_cols, n_mma, stream=None):
 def rtn_probe_peak_popc(rounds, stream=None):
     """Launches the AND / XOR / popcount probe; returns (cycles int64 [CTAs] on the device, operations per CTA)."""
     ctas = int(lib().rtn_probe_ctas())
-    cycles = torch.zeros((ctas,), dtype=torch.int64, device="cuda")
-    sink = torch.zeros((1,), dtype=torch.int32, device="cuda")
+    cycles = _zeros(ctas, torch.int64, stream)
+    sink = _zeros(1, torch.int32, stream)
     _check(lib().rtn_probe_peak_popc(int(rounds), _ptr(cycles, torch.int64), _ptr(sink, torch.int32), _stream(stream)),
            "rtn_probe_peak_popc")
     return cycles, int(rounds) * int(lib().rtn_probe_popc_ops_per_round())
@@ -411,7 +429,7 @@ def rtn_ternary_linear(a_packed, a_sum, w_packed, w_sum, M, N, K, a_scale, a_off
 def rtn_rotary_table(rows, R, base=10000.0, scaling=ROTARY_SCALE_NONE, factor=1.0, original_context=0.0, low=1.0, high=32.0,
                      amplitude=1.0, device=None, stream=None):
     """fp32 [rows, R]: the cosines, then the sines of the positions' angles.  ``device``: the current CUDA device."""
-    table = torch.empty((rows, R), dtype=torch.float32, device=device or "cuda")
+    table = _empty((rows, R), torch.float32, device or "cuda", stream)
     if not table.is_cuda or table.device.index != torch.cuda.current_device():
         raise ValueError(f"device: expected the current CUDA device, got {table.device}")
     _check(lib().rtn_rotary_table(_ptr(table), rows, R, base, int(scaling), factor, original_context, low, high, amplitude,

@@ -10,6 +10,7 @@
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include "rtn.h"
@@ -77,13 +78,13 @@ rtn_dtype type_of(at::ScalarType t)
 struct Call {
     c10::Device device;
     void* stream;
-    Call(const at::Tensor& first, PyObject* stream_or_none) : device(first.device())
+    bool given;                 // a stream of the caller's, not the current one
+    Call(const at::Tensor& first, PyObject* stream_or_none) : device(first.device()), given(stream_or_none != Py_None)
     {
         if (!first.is_cuda()) refuse("expected a CUDA tensor");
         const auto current = c10::cuda::current_device();
         if (device.index() != current) refuse("tensors on " + device.str() + ", but the current device is cuda:" + std::to_string(current));
-        stream = stream_or_none == Py_None ? c10::cuda::getCurrentCUDAStream(current).stream()
-                                           : reinterpret_cast<void*>(whole(stream_or_none, "stream"));
+        stream = given ? reinterpret_cast<void*>(whole(stream_or_none, "stream")) : c10::cuda::getCurrentCUDAStream(current).stream();
     }
     // A contiguous tensor of this type; None is NULL.
     template <typename T = void>
@@ -97,8 +98,12 @@ struct Call {
         }
         return static_cast<T*>(t->data_ptr());
     }
+    // A result of the stream that writes it: on the current one's memory it could take the place of a tensor whose last use there
+    // is still to come.
     at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const
     {
+        c10::cuda::OptionalCUDAStreamGuard on;
+        if (given) on.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), device.index()));
         return at::detail::empty_cuda(shape, type, device, std::nullopt);
     }
 };

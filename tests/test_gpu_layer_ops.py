@@ -621,3 +621,66 @@ def test_steep_decays_of_values_far_from_one(log_decay, dtype, D, longest, q_pow
         one, _ = rtn.rtn_decay_attention_step(*(x[cuda(at).long()] for x in (q, k, v)), cuda(g), after, slots=slots)
         ref.assert_close(one, want[at], mag[at], c, "token")
     ref.assert_close(after, end, mag_end, c, "tokens' state")
+
+
+# ---------------------------------------------------------------------------------------------- a stream of the caller's
+
+def calls_that_make_their_results():
+    """(name, call(stream)) of every entry point that makes its results."""
+    d = linear_case(40, 256, 256, 1)
+    x, w = cuda(d["x"]).float(), cuda(d["w"])
+    lo, hi = torch.tensor([-0.5], device="cuda"), torch.tensor([0.5], device="cuda")
+    args = packed(d)
+    four = torch.randint(0, 4, (40, 256), device="cuda").to(torch.uint8)
+    fp = rtn.rtn_pack_quaternary(four)
+    image = torch.randn(2, 64, 9, 9, device="cuda")
+    codes = torch.randint(-1, 2, (64, 64, 3, 3), device="cuda").to(torch.int8)
+    cp, cs = rtn.rtn_pack_weights(codes)
+    one = torch.ones(1, device="cuda")
+    q, k, v, log_decay, start = decay_case([140, 9], 4, 2, 64, 64, torch.bfloat16)
+    table, g, s = rtn.rtn_rotary_table(256, 64), cuda(log_decay), cuda(start)
+    state = torch.randn(149, 4, 64, 64, device="cuda")
+    return [("pack weights", lambda on: rtn.rtn_pack_weights(w, stream=on)),
+            ("ternarize", lambda on: rtn.rtn_ternarize_pack_act(x, lo, hi, stream=on)),
+            ("gemm", lambda on: [rtn.rtn_ternary_gemm(*args, stream=on)]),
+            ("conv", lambda on: [rtn.rtn_ternary_conv2d(image, lo, hi, cp, cs, 64, 3, 3, 1, 1, rtn.PAD_CODE_ZERO, 1.0, 0.0, one, one, stream=on)]),
+            ("pack quaternary", lambda on: [rtn.rtn_pack_quaternary(four, stream=on)]),
+            ("quaternary gemm", lambda on: [rtn.rtn_quaternary_gemm(fp, fp, 40, 40, 256, stream=on)]),
+            ("linear", lambda on: [rtn.rtn_ternary_linear(*args, dtype=torch.bfloat16, stream=on)]),
+            ("table", lambda on: [rtn.rtn_rotary_table(300, 64, stream=on)]),
+            ("rotary", lambda on: rtn.rtn_qk_norm_rotary(q, k, None, table, stream=on)),
+            ("prompt", lambda on: rtn.rtn_decay_attention(q, k, v, g, s, 140, stream=on)),
+            ("step", lambda on: rtn.rtn_decay_attention_step(q, k, v, g, None, stream=on))]
+
+
+def test_results_belong_to_the_stream_that_writes_them():
+    """With stream= a result never takes memory whose last use on the current stream is still to come."""
+    side = torch.cuda.Stream()
+    for name, call in calls_that_make_their_results():
+        want = [t.clone() for t in call(None)]
+        # tensors of the results' sizes, read late on the current stream and let go of at once
+        freed = [torch.full_like(t, 3) for t in want]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        late = [t.clone() for t in freed]
+        del freed
+        got = call(side)
+        side.synchronize()
+        at = {s["address"]: s for s in torch.cuda.memory_snapshot()}
+        for t in got:
+            segment = next(s for a, s in at.items() if a <= t.data_ptr() < a + s["total_size"])
+            assert segment["stream"] == side.cuda_stream, name
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got)), name
+        assert all(bool((t == 3).all()) for t in late), name
+    # the default stream, named, from within another one
+    default = torch.cuda.default_stream()
+    with torch.cuda.stream(side):
+        for name, call in calls_that_make_their_results():
+            side.synchronize()
+            got = call(default)
+            default.synchronize()
+            want = call(None)
+            side.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, got)), name
+    assert rtn.rtn_last_device_status() == 0
