@@ -205,7 +205,10 @@ qk_norm_rotary_kernel(const RotaryArgs g, int G, int groups_q, int groups_k)
             r[p] = a + b;
         }
         at += HP * s_head;
-        if (!kStage && done + HP < PG) load(h + HP);
+        if constexpr (!kStage) {
+            if (done + HP < PG) load(h + HP);
+            __syncwarp();                           // in place, a lane's elements are read by its partner before it writes them
+        }
         if (w != nullptr) {
             #pragma unroll
             for (int d = 16; d > 0; d >>= 1)

@@ -166,6 +166,19 @@ def test_rotation_in_place_on_columns_of_a_projection(D, R, extra, layout, dtype
     rotary_run(70, 6, 2, D, R, layout, False, dtype, view=head_major, in_place=True)
 
 
+# (T, Hq, Hk, D, type): one, two and eight heads to a group of lanes, heads of one and of two vectors to a lane
+@pytest.mark.parametrize("T,Hq,Hk,D,dtype", [(9, 3, 2, 128, torch.bfloat16), (300, 32, 8, 128, torch.bfloat16), (1000, 33, 7, 128, torch.float16),
+                                             (300, 16, 3, 128, torch.float32), (600, 32, 9, 128, torch.float32), (7, 3, 2, 256, torch.float32),
+                                             (500, 33, 7, 256, torch.float32), (7, 3, 2, 512, torch.float16), (500, 33, 7, 512, torch.bfloat16)],
+                         ids=ids)
+@pytest.mark.parametrize("layout", [rtn.ROTARY_HALF, rtn.ROTARY_INTERLEAVED], ids=["half", "interleaved"])
+@pytest.mark.parametrize("norm", [True, False], ids=["norm", "plain"])
+@pytest.mark.parametrize("part", [1, 2])
+def test_rotation_in_place_of_few_and_many_heads(T, Hq, Hk, D, dtype, layout, norm, part):
+    rotary_run(T, Hq, Hk, D, D // part, layout, norm, dtype, in_place=True)
+    rotary_run(T, Hq, Hk, D, D // part, layout, norm, dtype)
+
+
 def test_rotation_keeps_what_lies_past_it():
     """A non-finite value past the rotated part, or in another pair, stays where it is."""
     for layout in (rtn.ROTARY_HALF, rtn.ROTARY_INTERLEAVED):
