@@ -1188,18 +1188,15 @@ static cudaError_t launch_conv_i8_any_mode(const ConvArgs& c, const NextLayerArg
     }
     if (f != nullptr) {
         if (p.sk_stage) {
-            cudaError_t e = cudaFuncSetAttribute(conv_i8_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)p.smem_bytes);
+            cudaError_t e = allow_shared_memory(conv_i8_kernel<true, true>);
             if (e != cudaSuccess) return e;
             return launch_pdl(conv_i8_kernel<true, true>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, c, p, tmap, *f);
         }
-        cudaError_t e = cudaFuncSetAttribute(conv_i8_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)p.smem_bytes);
+        cudaError_t e = allow_shared_memory(conv_i8_kernel<true>);
         if (e != cudaSuccess) return e;
         return launch_pdl(conv_i8_kernel<true>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, c, p, tmap, *f);
     }
-    cudaError_t e = cudaFuncSetAttribute(conv_i8_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)p.smem_bytes);
+    cudaError_t e = allow_shared_memory(conv_i8_kernel<false>);
     if (e != cudaSuccess) return e;
     return launch_pdl(conv_i8_kernel<false>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, c, p, tmap,
                       NextLayerArgs{});

@@ -633,12 +633,12 @@ cudaError_t launch_with_scratch(const ConvArgs& c, const ConvI8RPlan& p, void* s
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     if (f != nullptr) {
-        e = cudaFuncSetAttribute(conv_i8r_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
+        e = allow_shared_memory(conv_i8r_kernel<true>);
         if (e != cudaSuccess) return e;
         return launch_pdl(conv_i8r_kernel<true>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, c, p,
                           (const uint4*)codes, (const int*)psum, *f);
     }
-    e = cudaFuncSetAttribute(conv_i8r_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
+    e = allow_shared_memory(conv_i8r_kernel<false>);
     if (e != cudaSuccess) return e;
     return launch_pdl(conv_i8r_kernel<false>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, c, p,
                       (const uint4*)codes, (const int*)psum, NextLayerArgs{});

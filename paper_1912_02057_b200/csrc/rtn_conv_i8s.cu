@@ -841,8 +841,7 @@ static cudaError_t launch_i8s_mode(const ConvArgs& c, const NextLayerArgs& f, cu
     ConvI8SPlan p;
     if (!make_plan_s(c, p, device_sm_count(), kNext)) return cudaErrorInvalidConfiguration;
     if (!pre_expand(p)) {
-        cudaError_t e = cudaFuncSetAttribute(conv_i8s_kernel<false, kNext>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)p.smem_bytes);
+        cudaError_t e = allow_shared_memory(conv_i8s_kernel<false, kNext>);
         if (e != cudaSuccess) return e;
         return launch_pdl(conv_i8s_kernel<false, kNext>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, c, p,
                           (const uint4*)nullptr, f);
@@ -857,8 +856,7 @@ static cudaError_t launch_i8s_mode(const ConvArgs& c, const NextLayerArgs& f, cu
     conv_expand_filters_kernel<<<(unsigned)((items + 255) / 256), 256, 0, s>>>(c, p, reinterpret_cast<uint4*>(scratch));
     e = cudaGetLastError();
     if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(conv_i8s_kernel<true, kNext>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)p.smem_bytes);
+        e = allow_shared_memory(conv_i8s_kernel<true, kNext>);
     if (e == cudaSuccess)
         e = launch_pdl(conv_i8s_kernel<true, kNext>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, c, p,
                        (const uint4*)scratch, f);

@@ -185,8 +185,7 @@ cudaError_t launch_conv_popc(const ConvArgs& c, cudaStream_t s)
     int PH, PW;
     const size_t smem = conv_popc_smem(c, PH, PW);
     if (!conv_popc_supported(c)) return cudaErrorInvalidConfiguration;
-    cudaError_t e = cudaFuncSetAttribute(conv_popc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)smem);
+    cudaError_t e = allow_shared_memory(conv_popc_kernel);
     if (e != cudaSuccess) return e;
     const int tiles = ((c.Ho + kTH - 1) / kTH) * ((c.Wo + kTW - 1) / kTW);
     dim3 grid((unsigned)tiles, (unsigned)((c.N + kNB - 1) / kNB), (unsigned)c.B);

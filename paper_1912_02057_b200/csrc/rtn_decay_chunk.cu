@@ -715,11 +715,11 @@ cudaError_t launch_typed(const DecayArgs& g, cudaStream_t s, const CUtensorMap& 
 {
     constexpr int bytes = (int)Layout<D, false>::kBytes, bytes_states = (int)Layout<D, true>::kBytes;
     ChunkPlan p = make_plan(g);
-    cudaError_t e = cudaFuncSetAttribute(decay_chunk_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    cudaError_t e = allow_shared_memory(decay_chunk_kernel<D, false>);
     if (e != cudaSuccess) return e;
     void* scratch = nullptr;
     if (p.segments > 1) {
-        e = cudaFuncSetAttribute(decay_chunk_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes_states);
+        e = allow_shared_memory(decay_chunk_kernel<D, true>);
         if (e != cudaSuccess) return e;
         e = scratch_alloc(&scratch, (size_t)g.B * g.H * p.segments * D * D * sizeof(float), s);
         if (e != cudaSuccess) return e;

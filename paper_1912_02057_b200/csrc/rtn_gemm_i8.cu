@@ -689,7 +689,7 @@ static cudaError_t launch_gemm_i8_typed(const GemmArgs& g, const LinearArgs& l, 
 {
     const int mode = gemm_pre_mode(p, g.K);
     if (mode == 0) {
-        cudaError_t e = cudaFuncSetAttribute(gemm_i8_kernel<false, false, OutT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
+        cudaError_t e = allow_shared_memory(gemm_i8_kernel<false, false, OutT>);
         if (e != cudaSuccess) return e;
         gemm_i8_kernel<false, false, OutT><<<(unsigned)p.grid, kThreads, p.smem_bytes, s>>>(g, p, nullptr, nullptr, omap, l);
         return cudaGetLastError();
@@ -706,12 +706,12 @@ static cudaError_t launch_gemm_i8_typed(const GemmArgs& g, const LinearArgs& l, 
     gemm_expand_operands_kernel<<<(unsigned)((items_w + items_a + 255) / 256), 256, 0, s>>>(g, p, wexp, aexp);
     e = cudaGetLastError();
     if (e == cudaSuccess && mode == 1) {
-        e = cudaFuncSetAttribute(gemm_i8_kernel<true, false, OutT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
+        e = allow_shared_memory(gemm_i8_kernel<true, false, OutT>);
         if (e == cudaSuccess)
             e = launch_pdl(gemm_i8_kernel<true, false, OutT>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, g, p,
                            (const uint4*)wexp, (const uint4*)aexp, omap, l);
     } else if (e == cudaSuccess) {
-        e = cudaFuncSetAttribute(gemm_i8_kernel<true, true, OutT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
+        e = allow_shared_memory(gemm_i8_kernel<true, true, OutT>);
         if (e == cudaSuccess)
             e = launch_pdl(gemm_i8_kernel<true, true, OutT>, dim3((unsigned)p.grid), dim3(kThreads), p.smem_bytes, s, g, p,
                            (const uint4*)wexp, (const uint4*)aexp, omap, l);

@@ -140,6 +140,14 @@ inline int device_sm_count()
     return sms;
 }
 
+// Lets a kernel be launched with any amount of dynamic shared memory the machine has (none of these kernels has static shared
+// memory).  The limit belongs to the process: set to what one launch needs, it could be lowered by another host thread before
+// that launch, which was then refused.
+template <typename... A> inline cudaError_t allow_shared_memory(void (*kernel)(A...))
+{
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+}
+
 // Scratch of the layer operators for the duration of a call, stream-ordered, from a memory pool of the library's own (one per
 // device, made at the first use) that keeps what it has: the device's default pool hands its memory back at every
 // synchronisation, and mapping it again cost 100 us (a 20 MB operand) to 1 ms at the next call.

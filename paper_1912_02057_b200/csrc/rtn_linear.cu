@@ -373,7 +373,7 @@ cudaError_t launch_tiles(const GemmArgs& g, const LinearArgs& l, const TilePlan&
 {
     return with_dtype(l.dtype, [&](auto t) {
         auto kernel = linear_tiles_kernel<decltype(t)>;
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem_bytes);
+        cudaError_t e = allow_shared_memory(kernel);
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg;
         memset(&cfg, 0, sizeof(cfg));

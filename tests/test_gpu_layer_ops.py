@@ -697,3 +697,39 @@ def test_results_belong_to_the_stream_that_writes_them():
             side.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(want, got)), name
     assert rtn.rtn_last_device_status() == 0
+
+
+# ---------------------------------------------------------------------------------------------- host threads
+
+@pytest.mark.parametrize("shapes", [((16, 16384, 1024), (64, 16384, 512)), ((1500, 1536, 512), (2000, 4096, 512))], ids=["tiles", "two launches"])
+def test_host_threads_with_products_of_different_sizes(shapes):
+    """Calls of one kernel with different amounts of shared memory, from several host threads at once: every launch goes through."""
+    import threading
+    calls, wants = [], []
+    for shape in shapes:
+        args = packed(linear_case(*shape, 3))
+        wants.append(rtn.rtn_ternary_linear(*args))
+        calls.append(args)
+    torch.cuda.synchronize()
+    bad, outs, streams = [], [torch.zeros_like(wants[i % 2]) for i in range(4)], [torch.cuda.Stream() for _ in range(4)]
+
+    def work(i):
+        ap, asum, wp, wsum, M, N, K, a_s, a_o, w_s, w_o = calls[i % 2]
+        p = [x.data_ptr() for x in (ap, asum, wp, wsum, a_s, a_o, w_s, w_o)]
+        f, out, on = rtn.lib().rtn_ternary_linear, outs[i].data_ptr(), streams[i].cuda_stream
+        for n in range(1500):
+            code = f(p[0], p[1], p[2], p[3], M, N, K, p[4], p[5], M, p[6], p[7], N, None, 0, None, 0, out, N, 0, on)
+            if code != 0:
+                bad.append(code)
+            if n % 100 == 99:
+                streams[i].synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not bad, f"{len(bad)} of 6000 calls refused: {bad[:3]}"
+    assert all(torch.equal(outs[i], wants[i % 2]) for i in range(4))
+    assert rtn.rtn_last_device_status() == 0
