@@ -19,7 +19,7 @@ bool written_strides_ok(int64_t tokens, int64_t heads, int64_t D, int64_t token,
 {
     if (!strides_ok(token, head)) return false;
     if (heads > 1 && head < D) return false;
-    return tokens <= 1 || token >= (heads - 1) * head + D || (head >= (tokens - 1) * token + D && token >= D);
+    return tokens <= 1 || token >= (heads - 1) * head + D || (head >= (__int128)(tokens - 1) * token + D && token >= D);
 }
 
 rtn_status as_status(cudaError_t e) { return e == cudaSuccess ? RTN_OK : RTN_ERR_CUDA; }
@@ -88,7 +88,7 @@ rtn_status rtn_rotary_table(float* table, int64_t rows, int64_t R, double base, 
                             double original_context, double low, double high, double amplitude, void* stream)
 {
     if (table == nullptr) return RTN_ERR_NULL;
-    if (rows <= 0 || R < 2 || R % 2 != 0 || R > rtn::kRotaryMaxDim || rows * (R / 2) >= (int64_t)INT_MAX * 256) return RTN_ERR_SHAPE;
+    if (rows <= 0 || rows >= (int64_t)INT_MAX * 256 || R < 2 || R % 2 != 0 || R > rtn::kRotaryMaxDim || rows * (R / 2) >= (int64_t)INT_MAX * 256) return RTN_ERR_SHAPE;
     if (!aligned(table, 4)) return RTN_ERR_ALIGN;
     if (!(base > 0.0) || !isfinite(base) || !isfinite(amplitude)) return RTN_ERR_VALUE;
     switch (scaling) {
@@ -112,7 +112,7 @@ rtn_status rtn_qk_norm_rotary(const void* q, int64_t q_token, int64_t q_head, co
                               const float* q_weight, const float* k_weight, float eps, const float* table, int64_t table_rows,
                               const int64_t* positions, rtn_dtype dtype, void* stream)
 {
-    if (T < 0 || Hq <= 0 || Hk < 0 || D <= 0 || R < 0 || R > D || R % 2 != 0 || D > rtn::kRotaryMaxDim || Hq > 65535 || Hk > 65535 ||
+    if (T < 0 || T >= kMaxDim || Hq <= 0 || Hk < 0 || D <= 0 || R < 0 || R > D || R % 2 != 0 || D > rtn::kRotaryMaxDim || Hq > 65535 || Hk > 65535 ||
         T * (Hq + Hk) >= (int64_t)INT_MAX || table_rows < 0) return RTN_ERR_SHAPE;
     if (T > 0 && (q == nullptr || out_q == nullptr || (Hk > 0 && (k == nullptr || out_k == nullptr)))) return RTN_ERR_NULL;
     if (R > 0 && (table == nullptr || table_rows == 0)) return RTN_ERR_NULL;
@@ -168,7 +168,7 @@ rtn_status rtn_decay_attention_step(const void* q, int64_t q_token, int64_t q_he
                                     const float* state, float* state_out, const int32_t* slots, int64_t n_slots, rtn_dtype dtype,
                                     void* stream)
 {
-    if (B < 0 || B * H >= (int64_t)INT_MAX / 8) return RTN_ERR_SHAPE;
+    if (B < 0 || B >= kMaxDim || H <= 0 || H > 65535 || B * H >= (int64_t)INT_MAX / 8) return RTN_ERR_SHAPE;
     rtn::DecayArgs g{};
     const rtn_status st = fill_decay(g, q, q_token, q_head, k, k_token, k_head, v, v_token, v_head, out, o_token, o_head, B, B, H, Hk,
                                      Dk, Dv, log_decay, scale, state, state_out, slots, n_slots, dtype);

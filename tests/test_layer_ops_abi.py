@@ -76,3 +76,15 @@ def test_decay_attention():
 def test_status_text():
     f = rtn.lib().rtn_status_string
     assert f(8).startswith(b"RTN_ERR_DEVICE_INDEX") and f(9).startswith(b"unknown")
+
+
+def test_sizes_whose_products_pass_64_bits():
+    """Refused, whatever their products are modulo 2^64."""
+    assert rotary(T=1 << 62) == SHAPE and rotary(T=(1 << 62) + 1) == SHAPE and rotary(T=1 << 31) == SHAPE
+    assert table(rows=1 << 62) == SHAPE and table(rows=(1 << 62) + 2) == SHAPE and table(rows=1 << 39, R=2) == SHAPE
+    many = dict(H=1 << 15, Hk=1 << 15, slots=P, os=(8 << 15, 8))
+    assert step(B=1 << 49, **many) == SHAPE and step(B=(1 << 49) + 1, **many) == SHAPE
+    assert step(H=1 << 62, Hk=1, B=4) == SHAPE and step(H=-(1 << 62), B=2) == SHAPE
+    # rows of out that meet: 2^31 - 2 tokens 2^33 elements apart are not between two heads 2^34 apart
+    assert decay(total=(1 << 31) - 1, os=(1 << 33, 1 << 34)) == SHAPE
+    assert rotary(T=(1 << 29) - 1, oqs=(1 << 35, 1 << 36)) == SHAPE
