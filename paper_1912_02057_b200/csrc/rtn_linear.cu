@@ -95,34 +95,34 @@ linear_rows_kernel(const GemmArgs g, const LinearArgs p, int GL)
 
 // ------------------------------------------------------------------------------------------------ some to many rows, small products
 
-// linear_tiles_kernel: 128 weight rows (the MMA's M, lanes of tensor memory) by BT tokens (its N), tcgen05.mma kind::i8.  Sixteen
-// warps expand the bit planes of both operands into a ring of 4, 8 or 16 stages, a team of 4, 2 or 1 warps to a stage and a whole
-// K = 128 block at a time (several rows per lane in flight, and no team waits for another); a seventeenth issues the MMAs; then the
+// linear_tiles_kernel: 128 weight rows (the MMA's M, lanes of tensor memory) by BT <= 64 tokens (its N), tcgen05.mma kind::i8.  Sixteen
+// warps expand the bit planes of both operands into a ring of eight stages, a team of two warps to a stage and a whole
+// K = 128 block at a time (three rows per lane in flight, and no team waits for another); a seventeenth issues the MMAs; then the
 // sixteen write out.  A lane is one output column: its scale, offset, code sum and bias live in registers, and a warp's
 // store is 32 adjacent columns of a token, with no staging.
-// Bound: the integer pipe (about 100 instructions per row and block to expand) while the weights stream by; the epilogue for short K.
-// 48 x 16384 x 4096 with bias and GELU: 20 us in a graph, of which an instruction of 64 columns, its wait and commit are about 430 clocks
-// per block of K (32 blocks: 7 us) and the expansion about as much beside it; 777 x 1000 x 512 with bias and SiLU: 10 us.
+// Bound: the expansion (280 warp instructions per 32 rows and block, epilogue included, with 0.42 of the issue slots used: the planes' loads are
+// waited for) while the weights stream by; the epilogue for short K.  48 x 16384 x 4096 with bias and GELU: 17.2 us in a graph, of which the
+// MMAs are 3 us (46 clocks each up to 48 columns, 48 at 64, by the probe; four to a block of K, 32 blocks); 777 x 1000 x 512 with bias and SiLU: 8.8 us.
 // Few tiles and a long K: the K blocks are dealt to the CTAs of a cluster, which leave their int32 sums in shared memory and
 // each finish a share of the tokens from all of them (exact whatever the order).
 constexpr int kTileWarps = 16;
 constexpr int kTileThreads = (kTileWarps + 1) * 32;
-constexpr int kTileRing = 192 * 1024;           // bytes of stages
-constexpr int kTileMaxStages = 16;
-constexpr int kTileMaxTokens = 256;
+constexpr int kTileStages = 8;                  // 18 to 24 KB each
+constexpr int kTeamWarps = kTileWarps / kTileStages;
+constexpr int kTileMaxTokens = 64;
+constexpr int kLaneRows = (4 + kTileMaxTokens / 32) / kTeamWarps;      // 32-row groups of a block to a warp
 constexpr uint32_t kTileTries = 1u << 20;
 
 struct TilePlan {
     int BT;                 // tokens of a tile, a multiple of 16
     int tiles_n, tiles_m;
     int slices;             // CTAs of a cluster, along K
-    int stages;
     uint32_t tmem_cols;
     uint32_t smem_bytes;
 };
 
 struct TileBars {
-    uint64_t full[kTileMaxStages], empty[kTileMaxStages], acc;
+    uint64_t full[kTileStages], empty[kTileStages], acc;
     uint32_t tmem_slot;
     int dead;
 };
@@ -166,7 +166,7 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
 
     if (warp == kTileWarps) tc::tmem_alloc(&bar.tmem_slot, p.tmem_cols);
     if (threadIdx.x == 0) {
-        for (int i = 0; i < p.stages; ++i) { tc::mbar_init(&bar.full[i], kTileWarps / p.stages); tc::mbar_init(&bar.empty[i], 1); }
+        for (int i = 0; i < kTileStages; ++i) { tc::mbar_init(&bar.full[i], kTeamWarps); tc::mbar_init(&bar.empty[i], 1); }
         tc::mbar_init(&bar.acc, 1);
         tc::mbar_init_fence();
         bar.dead = 0;
@@ -187,16 +187,16 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
     }
     const uint4* __restrict__ W = reinterpret_cast<const uint4*>(g.w_packed);
     const uint4* __restrict__ X = reinterpret_cast<const uint4*>(g.a_packed);
-    const int team_warps = kTileWarps / p.stages, s = (warp < kTileWarps ? warp : 0) / team_warps, member = warp % team_warps;
+    const int s = (warp < kTileWarps ? warp : 0) / kTeamWarps, member = warp % kTeamWarps;
     const int row_groups = 4 + (p.BT + 31) / 32;
     uint4* dst = reinterpret_cast<uint4*>(ring + s * stage_bytes);
-    // Items: block i, row groups first, first + team_warps, ... (four at most); the next item's planes are on their way while this
-    // one's are expanded.
-    uint4 nz[4], sg[4];
-    auto load = [&](int i, int first) {
+    // A warp's 32-row groups of a block: member, member + 2, member + 4.  The planes of its next block are on their way while this one's
+    // are expanded.
+    uint4 nz[kLaneRows], sg[kLaneRows];
+    auto load = [&](int i) {
         #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int rg = first + k * team_warps;
+        for (int k = 0; k < kLaneRows; ++k) {
+            const int rg = member + k * kTeamWarps;
             const bool isW = rg < 4;
             const int r = (isW ? rg : rg - 4) * 32 + lane;
             const int64_t row = (isW ? n0 : m0) + r;
@@ -205,7 +205,7 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
             if (ok) { const uint4* q = (isW ? W : X) + (row * nblk + kb0 + i) * 2; nz[k] = __ldg(q); sg[k] = __ldg(q + 1); }
         }
     };
-    if (warp < kTileWarps) load(s, member);
+    if (warp < kTileWarps) load(s);
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
@@ -218,29 +218,22 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
 
     if (warp < kTileWarps) {
         // ------------------------------------------------------------ expand: the warps of a team own one stage, so that a stage's
-        // phases follow each other in one program order; a team's warps take 32-row groups of the block in turn
-        int i = s, first = member;
-        while (i < kb1 - kb0) {
-            if (first == member && !warp_wait(&bar.empty[s], (uint32_t)(i / p.stages) + 1)) break;
-            uint4 cnz[4], csg[4];
+        // phases follow each other in one program order
+        for (int i = s; i < kb1 - kb0; i += kTileStages) {
+            if (!warp_wait(&bar.empty[s], (uint32_t)(i / kTileStages) + 1)) break;
+            uint4 cnz[kLaneRows], csg[kLaneRows];
             #pragma unroll
-            for (int k = 0; k < 4; ++k) { cnz[k] = nz[k]; csg[k] = sg[k]; }
-            const int now = first;
-            first += 4 * team_warps;
-            const bool last = first >= row_groups;
-            if (last) { first = member; i += p.stages; }
-            load(i, first);
+            for (int k = 0; k < kLaneRows; ++k) { cnz[k] = nz[k]; csg[k] = sg[k]; }
+            load(i + kTileStages);
             #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int rg = now + k * team_warps;
+            for (int k = 0; k < kLaneRows; ++k) {
+                const int rg = member + k * kTeamWarps;
                 if (rg < 4) expand_block(cnz[k], csg[k], dst + rg * 32 + lane, 128);
                 else if (rg < row_groups && (rg - 4) * 32 + lane < p.BT) expand_block(cnz[k], csg[k], dst + 128 * 8 + (rg - 4) * 32 + lane, p.BT);
             }
-            if (last) {
-                tc::fence_smem_to_async_proxy();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&bar.full[s]);
-            }
+            tc::fence_smem_to_async_proxy();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&bar.full[s]);
         }
         if (threadIdx.x < p.BT) token[threadIdx.x] = make_float4(t_s, t_o, (float)t_x, 0.f);
         asm volatile("bar.sync 1, %0;" ::"n"(kTileWarps * 32) : "memory");
@@ -252,8 +245,8 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
         const uint64_t desc_w = tc::smem_desc_kmajor(at, 2048, 128), desc_x = tc::smem_desc_kmajor(at + 128u * 128u, (uint32_t)p.BT * 16u, 128);
         bool alive = true;
         for (int i = 0; i < kb1 - kb0; ++i) {
-            const int s = i & (p.stages - 1);
-            if (!(alive = warp_wait(&bar.full[s], (uint32_t)(i / p.stages)))) break;
+            const int s = i % kTileStages;
+            if (!(alive = warp_wait(&bar.full[s], (uint32_t)(i / kTileStages)))) break;
             tc::tc_fence_after_sync();
             const uint64_t step = (uint64_t)(s * (stage_bytes >> 4));          // descriptors count 16 bytes
             #pragma unroll
@@ -339,34 +332,34 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
     if (warp == kTileWarps) tc::tmem_dealloc(tmem, p.tmem_cols);
 }
 
-TilePlan make_tile_plan(int64_t M, int64_t N, int64_t K)
+// False where two launches do better.
+bool make_tile_plan(int64_t M, int64_t N, int64_t K, TilePlan& p)
 {
-    TilePlan p{};
     const int sms = device_sm_count();
     const int nblk = (int)((K + kBlockCodes - 1) / kBlockCodes);
+    p = TilePlan{};
     p.tiles_n = (int)((N + 127) / 128);
+    if (p.tiles_n > sms) return false;
     // Tokens of a tile, and CTAs of a cluster that share its K (while one keeps at least four blocks and the machine has the SMs): what
     // makes rounds of CTAs times a tile's time least.  Per block the slower of expanding 128 + BT rows (1.6 clocks each) and the MMAs (2 BT);
     // 30 clocks per token for the epilogue, shared by a cluster, which takes 2000 to meet; 4000 to start and end.  Clusters of eight fill
-    // three quarters of the machine at most (more of them wait for a place: 64 x 1024 x 16384 26 us, in clusters of four 16).
+    // three quarters of the machine at most (more of them wait for a place: 64 x 1024 x 16384 26 us, in clusters of four 16).  Where more than 64
+    // tokens to a tile would do better, or one round of tiles is not enough, the operands are better expanded once, by a launch of their own.
     double best = 0.0;
-    const int most = M >= kTileMaxTokens ? kTileMaxTokens : (int)((M + 15) / 16 * 16);
+    const int most = M >= 256 ? 256 : (int)((M + 15) / 16 * 16);
     for (int bt = 16; bt <= most; bt += 16) {
         if (bt > 128 && bt % 32 != 0 && bt != most) continue;
         const int64_t tiles_m = (M + bt - 1) / bt, tiles = (int64_t)p.tiles_n * tiles_m;
         int slices = 1;
-        while (slices < 8 && bt <= 64 && tiles * slices * 2 <= (slices < 4 ? sms : sms * 3 / 4) && nblk >= slices * 8) slices *= 2;
+        while (slices < 8 && bt <= kTileMaxTokens && tiles * slices * 2 <= (slices < 4 ? sms : sms * 3 / 4) && nblk >= slices * 8) slices *= 2;
         const double block = 1.6 * (128 + bt) > 2.0 * bt ? 1.6 * (128 + bt) : 2.0 * bt;
         const double cost = (double)((tiles + sms - 1) / sms) * (4000.0 + (nblk + slices - 1) / slices * block + 30.0 * bt / slices + (slices > 1 ? 2000.0 : 0.0));
         if (p.BT == 0 || cost < best) { best = cost; p.BT = bt; p.slices = slices; p.tiles_m = (int)tiles_m; }
     }
-    const int stage = (128 + p.BT) * 128;
-    p.stages = kTileMaxStages;                  // a power of two: a team of warps for each
-    while (p.stages * stage > kTileRing) p.stages /= 2;
-    p.tmem_cols = 32;
-    while (p.tmem_cols < (uint32_t)p.BT) p.tmem_cols *= 2;
-    p.smem_bytes = 512 + kTileMaxTokens * 16 + (uint32_t)(p.stages * stage);
-    return p;
+    if (p.BT > kTileMaxTokens || (int64_t)p.tiles_n * p.tiles_m > sms) return false;
+    p.tmem_cols = p.BT <= 32 ? 32 : 64;
+    p.smem_bytes = 512 + kTileMaxTokens * 16 + (uint32_t)(kTileStages * (128 + p.BT) * 128);
+    return true;
 }
 
 cudaError_t launch_tiles(const GemmArgs& g, const LinearArgs& l, const TilePlan& p, cudaStream_t s)
@@ -407,29 +400,29 @@ cudaError_t launch_rows(const GemmArgs& g, const LinearArgs& l, cudaStream_t s)
 
 // Which of the three forms a shape takes; times in a graph on one B200 (bf16 out, us):
 //                      M   N     K      rows   tiles  two launches
-//   rows               9  4096  4096     9.3   10.5
-//                     64  2048   512     4.7    7.0             1000   100   300   4.8    6.5
-//   tiles             24  4096  4096    13.5   10.9   26.5        16  4096 16384  24.2  18.9  85.9
-//                    256  4096  4096           20.6   23.1       643   809   247  10.4    6.3
-//   two launches     512  4096  4096           26.2   23.0       256 16384  4096        44.0  36.4
+//   rows               1  4096  4096     2.7    8.3               5  4096  4096   5.5   8.4
+//                      8  4096  4096     5.7    8.6               8 11008  4096  11.4  14.6
+//                      8 16384  4096    15.3   14.8               4 16384 16384  27.0  41.1
+//                     64  2048   512     4.6    5.6    8.6     1000   100   300   4.6   5.2  11.5
+//   tiles             16  4096  4096     9.3    8.6   25.4       24  4096  4096  13.0   8.9  25.5
+//                     16  4096 16384    23.7   16.0   83.5      643   809   247  10.3   5.1  10.2
+//                    256  4096  4096           17.8   22.3      100  1000   128   7.9   4.5   6.5
+//   two launches     512  4096  4096           34.0   22.4      256 16384  4096        66.9  33.4
 // rows: the weights are streamed once per eight rows and the POPC rate binds, 2.9 us per million rows x columns x blocks, on top of 4 (with
-// one or two blocks of K the lanes of a group are too few for the outputs: 100 x 1000 x 128 8.0 us, in tiles 5.7); tiles start at 7 and take
-// 0.11 us and more per block of K.  Over 64 tokens a tile, or over one round of tiles, the weights' planes are
-// better expanded once, by a launch of their own.
+// one or two blocks of K the lanes of a group are too few for the outputs); tiles start at 5.3 and take 0.11 us and more per block of K.
+// Up to eight rows the weights are streamed once, and rows are within 4 % of tiles or ahead from three blocks of K on.
 bool linear_rows_path(int64_t M, int64_t N, int64_t K)
 {
     const double nblk = (double)((K + kBlockCodes - 1) / kBlockCodes);
-    const bool rows_win = nblk > 2 && 2.9e-6 * (double)M * (double)N * nblk <= 3.0 + 0.11 * nblk;
+    const bool rows_win = nblk > 2 && 2.9e-6 * (double)((M + 7) / 8 * 8) * (double)N * nblk <= 1.3 + 0.11 * nblk;
     return M <= kMaxRows || rows_win || !gemm_i8_supported(M, N, K);
 }
 
 cudaError_t launch_linear(const GemmArgs& g, const LinearArgs& l, cudaStream_t s)
 {
     if (!linear_rows_path(g.M, g.N, g.K)) {
-        if ((g.N + 127) / 128 > device_sm_count()) return launch_gemm_i8_linear(g, l, s);
-        const TilePlan p = make_tile_plan(g.M, g.N, g.K);
-        const bool one_round = (int64_t)p.tiles_n * p.tiles_m <= device_sm_count();
-        return one_round && p.BT <= 64 ? launch_tiles(g, l, p, s) : launch_gemm_i8_linear(g, l, s);
+        TilePlan p;
+        return make_tile_plan(g.M, g.N, g.K, p) ? launch_tiles(g, l, p, s) : launch_gemm_i8_linear(g, l, s);
     }
     if (g.M == 1) return launch_rows<1, 4>(g, l, s);
     if (g.M == 2) return launch_rows<2, 4>(g, l, s);

@@ -61,6 +61,33 @@ def test_linear_matches_the_plain_form(shape, dtype):
     assert rtn.rtn_last_device_status() == 0
 
 
+# one launch: tiles of 16, 32, 48 and 64 tokens, a K of its own, and shared by clusters of two, four and eight
+@pytest.mark.parametrize("shape", [(16, 6000, 1030), (17, 3000, 2050), (33, 2500, 4224), (33, 16300, 500), (40, 1200, 8200), (50, 3000, 700),
+                                   (64, 5000, 130), (63, 900, 4100), (200, 300, 4100), (250, 1000, 1000), (100, 300, 120)], ids=ids)
+def test_linear_tiles_and_clusters(shape):
+    linear_cases(shape)
+
+
+# more columns than one round of tiles holds, one row tile and several; several rounds of the largest tiles and a long K
+@pytest.mark.parametrize("shape", [(9, 20000, 300), (20, 18900, 300), (64, 20000, 260), (130, 19000, 200), (300, 20000, 130), (3000, 5000, 6000),
+                                   (2500, 7001, 1700)], ids=ids)
+def test_linear_many_columns_and_many_tiles(shape):
+    linear_cases(shape)
+
+
+def linear_cases(shape):
+    M, N, K = shape
+    for dtype, kind, bias, residual in ((torch.float32, 2, True, False), (torch.bfloat16, 4, True, True), (torch.float16, 0, False, True)):
+        d = linear_case(M, N, K, 100 + kind)
+        r = cuda(d["residual"], dtype) if residual else None
+        out = rtn.rtn_ternary_linear(*packed(d), bias=cuda(d["bias"]) if bias else None, activation=kind, residual=r, dtype=dtype)
+        at = np.linspace(0, M - 1, min(M, 200)).astype(np.int64)              # (rows of the double form)
+        want, mag = ref.linear(d["x"][at], d["w"], d["a_scale"][at], d["a_offset"][at], d["w_scale"], d["w_offset"],
+                               d["bias"] if bias else None, kind, ref.f64(r)[at] if residual else None)
+        ref.assert_close(out[cuda(at)], want, mag, LINEAR_C, f"{shape} {dtype} act {kind}")
+    assert rtn.rtn_last_device_status() == 0
+
+
 @pytest.mark.parametrize("dtype", DTYPES, ids=ids)
 @pytest.mark.parametrize("shape", [(3, 70, 200), (200, 304, 200), (150, 77, 130)], ids=ids)
 def test_linear_strided_unaligned_and_in_place(shape, dtype):
