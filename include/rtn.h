@@ -230,7 +230,8 @@ rtn_status rtn_quaternary_gemm(const void* a_packed, const void* w_packed, int64
  * end); strides count elements; a call with no tokens (M, T or B of 0) returns RTN_OK and launches nothing; calls
  * only enqueue and can be captured in a graph (after a first call that sets kernel attributes).  Scratch (the operands of a
  * tensor-core linear layer, the segment states of a long prompt) comes, stream-ordered, from a memory pool per device that the library
- * makes at the first use and that keeps its memory from call to call.
+ * makes at the first use and that keeps its memory from call to call, the most that was in use at once (a tensor-core linear layer
+ * takes up to 2 GiB for its expanded operands), until rtn_release_scratch.
  * ---------------------------------------------------------------------------------------------- */
 typedef enum { RTN_F32 = 0, RTN_BF16 = 1, RTN_F16 = 2 } rtn_dtype;
 typedef enum { RTN_ACT_NONE = 0, RTN_ACT_RELU = 1, RTN_ACT_GELU = 2 /* erf */, RTN_ACT_GELU_TANH = 3, RTN_ACT_SILU = 4 } rtn_activation;
@@ -341,6 +342,10 @@ int64_t rtn_conv_next_kernel_launches(int64_t B, int64_t C, int64_t H, int64_t W
  * tensor-core pipeline) ran out since the last call; that kernel's output is then invalid.  Else
  * RTN_ERR_DEVICE_INDEX if a layer operator met a position, slot or sequence bound out of range. */
 rtn_status rtn_last_device_status(void* stream);
+
+/* Synchronises `stream`, then gives back to the device what the current device's scratch pool keeps and no call in flight on
+ * another stream uses.  The next call that needs scratch maps memory again (100 us to 1 ms). */
+rtn_status rtn_release_scratch(void* stream);
 
 /* Self-test of the bounded waits (the safety net behind RTN_ERR_DEVICE_TIMEOUT): launches one small kernel
  * whose single waiting thread polls, `polls` times (1..4096, each poll parks the thread for up to about 2 us),

@@ -132,6 +132,8 @@ def lib():
         L.rtn_probe_copy.argtypes = [_vp, _vp, _i64, _vp]
         L.rtn_selftest_wait_timeout.restype = _int
         L.rtn_selftest_wait_timeout.argtypes = [_i64, _vp, _vp]
+        L.rtn_release_scratch.restype = _int
+        L.rtn_release_scratch.argtypes = [_vp]
         L.rtn_status_string.restype = C.c_char_p
         L.rtn_status_string.argtypes = [_int]
         _lib = L
@@ -352,6 +354,11 @@ def rtn_conv_next_kernel_launches(B, Cin, H, W, N, kh, kw, stride, pad):
 
 def rtn_last_device_status(stream=None):
     return int(lib().rtn_last_device_status(_stream(stream)))
+
+
+def rtn_release_scratch(stream=None):
+    """Gives the device back the scratch memory that the layer operators keep between calls (it lies outside torch's allocator)."""
+    _check(lib().rtn_release_scratch(_stream(stream)), "rtn_release_scratch")
 
 
 def rtn_selftest_wait_timeout(polls=1024, stream=None):

@@ -60,9 +60,10 @@ rtn_status check_params(const float* s, const float* o, int64_t n, int64_t full)
 namespace rtn {
 unsigned* device_status_word() { return status_word(); }
 
+static std::atomic<cudaMemPool_t> pools[kMaxDevices];      // of the layer operators' scratch
+
 cudaError_t scratch_alloc(void** p, size_t bytes, cudaStream_t s)
 {
-    static std::atomic<cudaMemPool_t> pools[kMaxDevices];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
@@ -86,6 +87,18 @@ cudaError_t scratch_alloc(void** p, size_t bytes, cudaStream_t s)
         }
     }
     return cudaMallocFromPoolAsync(p, bytes, pool, s);
+}
+
+cudaError_t scratch_release(cudaStream_t s)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    cudaMemPool_t pool = pools[dev].load(std::memory_order_acquire);
+    if (pool == nullptr) return cudaSuccess;
+    e = cudaStreamSynchronize(s);
+    return e != cudaSuccess ? e : cudaMemPoolTrimTo(pool, 0);
 }
 }
 
@@ -482,6 +495,11 @@ rtn_status rtn_last_device_status(void* stream)
     }
     if (h & rtn::kStatusWaitTimeout) return RTN_ERR_DEVICE_TIMEOUT;
     return (h & rtn::kStatusBadIndex) ? RTN_ERR_DEVICE_INDEX : RTN_OK;
+}
+
+rtn_status rtn_release_scratch(void* stream)
+{
+    return rtn::scratch_release(static_cast<cudaStream_t>(stream)) == cudaSuccess ? RTN_OK : RTN_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -152,6 +152,7 @@ template <typename... A> inline cudaError_t allow_shared_memory(void (*kernel)(A
 // device, made at the first use) that keeps what it has: the device's default pool hands its memory back at every
 // synchronisation, and mapping it again cost 100 us (a 20 MB operand) to 1 ms at the next call.
 cudaError_t scratch_alloc(void** p, size_t bytes, cudaStream_t s);      // released with cudaFreeAsync
+cudaError_t scratch_release(cudaStream_t s);    // waits for the stream and gives back what the current device's pool keeps
 
 // Device address of the current device's status word (NULL on failure); defined with the C ABI.
 unsigned* device_status_word();

@@ -760,3 +760,20 @@ def test_host_threads_with_products_of_different_sizes(shapes):
     assert not bad, f"{len(bad)} of 6000 calls refused: {bad[:3]}"
     assert all(torch.equal(outs[i], wants[i % 2]) for i in range(4))
     assert rtn.rtn_last_device_status() == 0
+
+
+def test_scratch_is_given_back():
+    args = packed(linear_case(4096, 4096, 1024, 2))
+    q, k, v, log_decay, start = decay_case([3000], 2, 1, 64, 64, torch.bfloat16)
+    want, states = rtn.rtn_ternary_linear(*args), rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), 3000)
+    torch.cuda.synchronize()
+    kept = torch.cuda.mem_get_info()[0]
+    rtn.rtn_release_scratch()
+    assert torch.cuda.mem_get_info()[0] >= kept + 2 * 4096 * 1024              # the expanded operands, a byte per code
+    rtn.rtn_release_scratch()
+    again, others = rtn.rtn_ternary_linear(*args), rtn.rtn_decay_attention(q, k, v, cuda(log_decay), cuda(start), 3000)
+    assert torch.equal(want, again) and all(torch.equal(a, b) for a, b in zip(states, others))
+    side = torch.cuda.Stream()
+    rtn.rtn_ternary_linear(*args, stream=side)
+    rtn.rtn_release_scratch(side)
+    assert rtn.rtn_last_device_status() == 0
