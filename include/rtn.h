@@ -227,7 +227,7 @@ rtn_status rtn_quaternary_gemm(const void* a_packed, const void* w_packed, int64
 /* ------------------------------------------------------------------------------------------------
  * Operators of a ternary language-model layer around the packed products (the paper has no counterpart).
  * Common to them: fp32, bf16 and fp16 tensors (arithmetic, norms, sums and states in fp32, one rounding at the
- * end); strides count elements; a call with no tokens (M, T or B of 0) returns RTN_OK and launches nothing; calls
+ * end; rtn_decay_attention's products on the tensor cores round their operands as it says there); strides count elements; a call with no tokens (M, T or B of 0) returns RTN_OK and launches nothing; calls
  * only enqueue and can be captured in a graph (after a first call that sets kernel attributes).  Scratch (the operands of a
  * tensor-core linear layer, the segment states of a long prompt) comes, stream-ordered, from a memory pool per device that the library
  * makes at the first use and that keeps its memory from call to call, the most that was in use at once (a tensor-core linear layer
@@ -246,7 +246,8 @@ typedef enum { RTN_ROTARY_SCALE_NONE = 0, RTN_ROTARY_SCALE_LINEAR = 1, RTN_ROTAR
  *               add a layer to a residual stream in place; no other overlap
  *   out         [M][N] of `dtype`, rows out_stride >= N elements apart
  * Few rows (up to 8, more where the product is small) run on a bit-plane kernel that streams the weights, some rows on a tensor-core
- * kernel that expands its own operands, both one launch; larger products take the launches of rtn_gemm_kernel_launches. */
+ * kernel that expands its own operands, both one launch; larger products take two where the operands are expanded ahead (at least two
+ * row tiles of 128 or 256), else one. */
 rtn_status rtn_ternary_linear(const void* a_packed, const int32_t* a_sum,
                               const void* w_packed, const int32_t* w_sum,
                               int64_t M, int64_t N, int64_t K,
@@ -293,7 +294,13 @@ rtn_status rtn_qk_norm_rotary(const void* q, int64_t q_token, int64_t q_head, co
  *   state_out   same shape, receives S after the last token; may be `state` (in place).  Required.
  *   slots       int32 [B] (on the device): sequence b's state is slots[b]; the live slots are distinct; a negative slot
  *               is a padding entry: its out rows become zero and no state is read or written.  NULL: slot b
- * Dk, Dv <= 256.  A value that is not finite reaches no token before its own: in v it makes that column of the head not finite
+ * Dk, Dv <= 256.  bf16 tensors with Dk = Dv = 64 or 128, 16-byte rows and prompts of more than 16 tokens run on the tensor cores in chunks of
+ * 128 tokens: there the weighted scores and the state in its product with q are rounded to 16 bits (two bf16 terms) and sums are the tensor
+ * core's (fp32, towards zero), so an output is off by up to 2^-15 of its terms' magnitudes beside its own rounding (0.24 % of outputs are not the
+ * bf16 value nearest to the exact one, 0.02 to 0.05 % where all is fp32); what is
+ * added to the state keeps 24 bits, and the state is fp32 throughout.  Everything else runs token by token in fp32, with k scaled by up to
+ * 2^8 and q by down to 2^-8 under steep decays.
+ * A value that is not finite reaches no token before its own: in v it makes that column of the head not finite
  * (NaN or infinite) from its token on, in k or the state every column, in q its own token's row.
  * Bounds that do not fit (a decreasing start, a length over max_len, a slot >= n_slots) make the kernel
  * skip the sequence (its rows of out are not written), and rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once. */
@@ -304,7 +311,8 @@ rtn_status rtn_decay_attention(const void* q, int64_t q_token, int64_t q_head, c
                                const float* state, float* state_out, const int32_t* slots, int64_t n_slots,
                                rtn_dtype dtype, void* stream);
 
-/* The same for one new token of each of B sequences (token b belongs to sequence b). */
+/* The same for one new token of each of B sequences (token b belongs to sequence b), in fp32.  A slot >= n_slots makes the token's rows of
+ * out NaN. */
 rtn_status rtn_decay_attention_step(const void* q, int64_t q_token, int64_t q_head, const void* k, int64_t k_token, int64_t k_head,
                                     const void* v, int64_t v_token, int64_t v_head, void* out, int64_t o_token, int64_t o_head,
                                     int64_t B, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, const float* log_decay, float scale,

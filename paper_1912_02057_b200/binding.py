@@ -455,7 +455,9 @@ def rtn_qk_norm_rotary(q, k, positions, table, q_weight=None, k_weight=None, eps
 def rtn_decay_attention(q, k, v, log_decay, start, max_len, state=None, state_out=None, slots=None, scale=None, out=None, stream=None):
     """Linear attention with a decay per head over prompts laid end to end: q [total,H,Dk], k [total,Hk,Dk], v [total,Hk,Dv],
     ``start`` int32 [B+1].  ``state`` fp32 [slots,H,Dk,Dv] (None: zero), ``state_out`` (default: ``state`` itself, or a new one)
-    receives the states after the last tokens.  ``scale`` defaults to Dk**-0.5.  Returns (out [total,H,Dv], state_out)."""
+    receives the states after the last tokens.  ``scale`` defaults to Dk**-0.5.  bf16 prompts of more than 16 tokens with heads of 64 or 128
+    run on the tensor cores, with scores and the state's part in an output held to 16 bits; states keep fp32's precision.  Returns
+    (out [total,H,Dv], state_out)."""
     return (_torch_side or _load_torch_side()).decay(q, k, v, log_decay, start, max_len, state, state_out, slots, scale, out,
                                                      stream and stream.cuda_stream)
 

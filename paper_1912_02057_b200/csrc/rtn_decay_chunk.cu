@@ -7,8 +7,9 @@
 //
 // Every product is a tcgen05.mma of kind::f16 with M = 128 and fp32 accumulators in tensor memory.  Operands that come
 // from memory (Q, K, V) are exact in bf16.  What the kernel computes on the way to a product is split into bf16 terms that
-// are multiplied one after the other into the same accumulator: P and S into two (2^-17 relative, far below the bf16
-// output's own rounding), the decayed V into three (2^-25), because the state it enters is kept and returned in fp32.
+// are multiplied one after the other into the same accumulator: P and S into two (2^-17 relative, against 2^-9 of the bf16
+// output: 0.24 % of the outputs are not the bf16 value nearest to the definition's in double, 0.05 % of the token-by-token kernel's; the
+// error in norm is the same 1.66e-3), the decayed V into three (2^-25), because the state it enters is kept and returned in fp32.
 // The tensor core's accumulation rounds towards zero, so what a chunk adds to the state gets an accumulator of its own and is
 // added in registers: accumulated onto the state itself, its 24 products a chunk bent the state by 1.3e-6.
 //

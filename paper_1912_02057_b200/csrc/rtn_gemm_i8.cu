@@ -93,8 +93,8 @@ bool make_gemm_plan(int64_t M, int64_t N, int64_t K, GemmI8Plan& p, int sms, dou
             const double mma = 2.0 * tm * bn, expand = 4.0 * (128 * tm + bn);
             double cost = (double)rounds * (mma > expand ? mma : expand);
             if (epilogue > 0.0) {
-                // Both operands come expanded (two cycles per row and stage; an MMA of 128 columns takes 430, a stage 700 at least) and the
-                // epilogue counts: under the next tile's products where tensor memory holds two accumulators, after its own where it holds
+                // Operands as they come expanded from a launch ahead (two cycles per row and stage; an MMA of 128 columns takes 430, a stage 700
+                // at least; one row tile, M <= 128 TM, expands in the kernel at twice the cycles, which is not counted) and the epilogue counts: under the next tile's products where tensor memory holds two accumulators, after its own where it holds
                 // one.  4096 x 4096 x 4096 with GELU and residual, bf16: 128 x 256 tiles 94 us, 256 x 256 tiles 105; without either 74 and 66.
                 double stage = tm * (2.0 * bn > 430.0 ? 2.0 * bn : 430.0);
                 if (stage < expand / 2) stage = expand / 2;

@@ -332,7 +332,7 @@ linear_tiles_kernel(const GemmArgs g, const LinearArgs l, const TilePlan p)
     if (warp == kTileWarps) tc::tmem_dealloc(tmem, p.tmem_cols);
 }
 
-// False where two launches do better.
+// False where gemm_i8_kernel does better.
 bool make_tile_plan(int64_t M, int64_t N, int64_t K, TilePlan& p)
 {
     const int sms = device_sm_count();
@@ -344,7 +344,7 @@ bool make_tile_plan(int64_t M, int64_t N, int64_t K, TilePlan& p)
     // makes rounds of CTAs times a tile's time least.  Per block the slower of expanding 128 + BT rows (1.6 clocks each) and the MMAs (2 BT);
     // 30 clocks per token for the epilogue, shared by a cluster, which takes 2000 to meet; 4000 to start and end.  Clusters of eight fill
     // three quarters of the machine at most (more of them wait for a place: 64 x 1024 x 16384 26 us, in clusters of four 16).  Where more than 64
-    // tokens to a tile would do better, or one round of tiles is not enough, the operands are better expanded once, by a launch of their own.
+    // tokens to a tile would do better, or one round of tiles is not enough, gemm_i8_kernel's larger tiles are ahead.
     double best = 0.0;
     const int most = M >= 256 ? 256 : (int)((M + 15) / 16 * 16);
     for (int bt = 16; bt <= most; bt += 16) {
