@@ -5,10 +5,11 @@ ResNet-18 images/s.
     python bench.py [--gpus N] [--steps K] [--warmup W] [--impl ours|reference]
                     [--workload NAME] [--variant auto|popc|i8] [--io fp32|packed]
 
-Without --workload the run covers every configuration of the workload list (SUITE) and prints ONE JSON line:
-the headline configuration's numbers at the top level and one entry per configuration under `per_config`
-(time, TOPS, roofline, end-to-end), plus the measured peaks of the int8 tensor pipe and of the AND / XOR /
-popcount pattern (`peaks`).  With --workload the line describes that configuration alone.
+Without --workload the run covers every configuration of the workload list (SUITE) and prints ONE JSON line of a few
+kilobytes: the headline configuration's numbers at the top level and one short entry per configuration under `per_config`
+(time, TOPS, roofline fraction, end-to-end), plus the measured peaks of the int8 tensor pipe and of the AND / XOR /
+popcount pattern (`peaks`).  With --workload the line describes that configuration alone.  Every configuration's whole record (timing
+regions, clocks, sources) goes to stderr ahead of it, one `# record {...}` line each.
 
 One step = one pass of the whole hot path over one batch of seeded synthetic input: for a conv workload a
 single rtn_ternary_conv2d call (ternarize in-kernel -> implicit-GEMM contraction -> affine epilogue); for a
@@ -1030,6 +1031,24 @@ def run_reference(args, name):
 
 
 # ------------------------------------------------------------------------------------------------
+def brief(entry):
+    """A configuration's record in a few numbers."""
+    roofline, e2e, clocks = entry.get("roofline") or {}, entry.get("e2e") or {}, entry.get("clocks") or {}
+    short = {k: entry[k] for k in ("workload", "ms_per_step", "value", "unit", "images_per_s", "body_images_per_s", "launches_per_step") if k in entry}
+    short.update(bound=roofline.get("bound"), frac=roofline.get("frac"), e2e=e2e.get("value"), sm_mhz=clocks.get("sm_mhz"), reasons=clocks.get("reasons"))
+    return {k: float(f"{v:.6g}") if isinstance(v, float) else v for k, v in short.items()}
+
+
+def report(line, entries):
+    """The JSON line on stdout, the entries' whole records on stderr (all of them in the line made it longer than a log's tail)."""
+    for e in entries:
+        print("# record " + json.dumps(e), file=sys.stderr)
+    sys.stderr.flush()
+    if len(entries) > 1:
+        line["per_config"] = [brief(e) for e in entries]
+    print(json.dumps(line), flush=True)
+
+
 def run_ours(args):
     import paper_1912_02057_b200 as rtn
     ctx = Ctx(args)
@@ -1067,11 +1086,7 @@ def run_ours(args):
             rate, dt, sample = oracle_sample(head_case, 12.0, args.io, fill_budget=True)
             line["cpu_baseline"] = {"value": rate / 1e12, "unit": "TOPS", "cores": oracle.threads(),
                                     "kind": "oracle", "sample": sample, "seconds": dt}
-        if len(entries) > 1:
-            line["per_config"] = entries
-        else:
-            line["detail"] = head
-        print(json.dumps(line))
+        report(line, entries)
     assert rtn.rtn_last_device_status() == 0
     ctx.close()
 
