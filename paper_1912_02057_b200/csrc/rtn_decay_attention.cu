@@ -137,7 +137,7 @@ __device__ __forceinline__ float power(float g2, float n) { return n == 0.f ? 1.
 // powers of two.  What the steeper heads' extra products cost: 1310 us for 8 x 2048 tokens of 32 heads of 128, fp16, at log decays down to
 // -0.79, 1342 at -1, 1390 at -3, 1477 at -8.
 template <typename T, int ROWS, int COLS, int WARPS, bool kStates>
-__global__ void __launch_bounds__(WARPS * 32, WARPS == 4 ? 3 : 2)         // (a fourth CTA of 4 warps: 2 x 9656 tokens of heads of 64, 318 us instead of 256)
+__global__ void __launch_bounds__(WARPS * 32, WARPS == 4 ? 3 : 2)         // (a fourth CTA of 4 warps: prompts of 9656 and 4828 tokens, heads of 64, 318 us instead of 256)
 decay_recurrent_kernel(const DecayArgs g, const RecPlan p)
 {
     constexpr int kRecThreads = WARPS * 32, DK = ROWS * WARPS, DV = COLS * 32;
@@ -347,7 +347,7 @@ cudaError_t launch_recurrent_rows(const DecayArgs& g, cudaStream_t s)
     const int slices = (g.Dv + COLS * 32 - 1) / (COLS * 32);
     // Few heads and long prompts: segments, until about sixteen warps per SM walk a share of the tokens each; one launch finds what
     // each adds to the state (half of the work once more), the next starts each from the decayed sum of what came before it.  Two
-    // segments do not make up for that where one CTA per head already has an SM (4 x 4096 tokens of 16 heads of 128: 805 us, in two 861).
+    // segments do not make up for that where one CTA per head already has an SM (four prompts of 2048 to 4096 tokens, 16 heads of 128: 805 us, in two 861).
     RecPlan p{};
     const int64_t ctas = g.B * g.H * slices;
     int64_t segs = (16 / WARPS) * (int64_t)device_sm_count() / ctas;
