@@ -319,6 +319,79 @@ rtn_status rtn_decay_attention_step(const void* q, int64_t q_token, int64_t q_he
                                     const float* state, float* state_out, const int32_t* slots, int64_t n_slots,
                                     rtn_dtype dtype, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * A layer of routed ternary experts: the choice of experts, their products, and the norms around a block.  What is said of the layer
+ * operators above holds for them as well.
+ * ---------------------------------------------------------------------------------------------- */
+typedef enum { RTN_SCORE_SOFTMAX = 0, RTN_SCORE_SIGMOID = 1 } rtn_score;
+typedef enum { RTN_GATE_LINEAR = 0, RTN_GATE_SIGMOID = 1, RTN_GATE_SILU = 2 } rtn_gate;
+
+/* Choice of top_k of E experts for each of T tokens, and the plan of the rows that the experts work on.
+ *     s = softmax or sigmoid of the token's logits;  c = s + bias;  out of the kept groups, the top_k largest c
+ *     weight = weight_scale * s   (each divided by the sum of the chosen ones' s where `renormalise`)
+ *   logits      [T][E] of `dtype`, rows logits_stride elements apart
+ *   bias        NULL, or fp32 [E]: moves the choice, not the weights
+ *   groups      E / groups consecutive experts each; a group's value is the sum of its group_top largest c; the kept_groups groups of the
+ *               largest values stay.  1 group: no such step
+ *   experts     int32 [T][top_k], in the order of c, largest first
+ *   weights     fp32 [T][top_k]
+ *   start, tokens, place   NULL (all three), or the plan: the T*top_k (token, choice) pairs as rows sorted by expert, within an expert by
+ *               token.  Expert e has rows start[e] .. start[e+1]-1 (int32 [E+1]); row r is of token tokens[r] (int32 [T*top_k]); choice j of
+ *               token t is row place[t][j] (int32 [T][top_k])
+ * Choices are those of exact arithmetic (a c that fp32 cannot tell from another is computed in double); of equal ones the lowest index
+ * comes first, for groups too.  A logit of -inf or NaN (or a bias of it) is never chosen, and +inf counts as the largest finite
+ * value; a token with fewer experts to choose has -1, weight 0 and place -1 in the rest, and the rows from start[E] on are not written.
+ * E <= 1024, groups <= 32 and a divisor of E, top_k <= 32 and <= the experts in the kept groups. */
+rtn_status rtn_route_experts(const void* logits, int64_t logits_stride, int64_t T, int64_t E, rtn_dtype dtype, rtn_score score,
+                             const float* bias, int64_t groups, int64_t kept_groups, int64_t group_top, int64_t top_k,
+                             int renormalise, float weight_scale, int32_t* experts, float* weights,
+                             int32_t* start, int32_t* tokens, int32_t* place, void* stream);
+
+/* The experts' ternary products.  Expert e has rows start[e] .. start[e+1]-1 of R, a row's input is packed row tokens[r]:
+ *     y[r][n] = sum_k (a_s x[tokens[r]][k] + a_o)(w_s w[e][n][k] + w_o) + bias[e][n]
+ *     out[r][i] = act(y[r][i])                   F = N outputs, or
+ *     out[r][i] = act(y[r][i]) * y[r][F + i]     F = N / 2 outputs where `gated`
+ *   a_packed, a_sum, a_scale, a_offset   as in rtn_ternary_gemm, for T input rows (n_aparam 1 or T)
+ *   tokens      int32 [R], or NULL: row r is input row r (R = T)
+ *   start       int32 [E+1], on the device (rtn_route_experts); rows outside every expert are left as they were
+ *   w_packed    E * N packed rows of K codes, w_sum int32 [E*N] (row 0 of rtn_pack_weights' w_sum); w_scale, w_offset: n_wparam 1 or E*N
+ *   bias        NULL, or fp32 [E][N]
+ *   out         NULL, or [R][F] of `dtype`, rows out_stride >= F elements apart
+ *   out_packed, out_sum   NULL (both), or the codes of the outputs against thresholds, R packed rows of F codes and their sums, as
+ *               rtn_ternarize_pack_act gives them: what the next product reads.  t_lo, t_hi: n_thr 1 or E.  They are the codes of the exact
+ *               output (one that fp32 cannot tell from a threshold is computed in double); out and out_packed may both be given
+ * Few rows run on a bit-plane kernel that streams the weights, others on the tensor cores.  Bounds that do not fit (a decreasing
+ * start, or one outside 0 .. R) leave the expert's rows as they were, a token out of range makes its row NaN (codes 0), and
+ * rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once. */
+rtn_status rtn_ternary_experts(const void* a_packed, const int32_t* a_sum, int64_t T, const int32_t* tokens, const int32_t* start, int64_t R,
+                               const void* w_packed, const int32_t* w_sum, int64_t E, int64_t N, int64_t K,
+                               const float* a_scale, const float* a_offset, int64_t n_aparam,
+                               const float* w_scale, const float* w_offset, int64_t n_wparam, const float* bias,
+                               rtn_activation act, int gated, void* out, int64_t out_stride, rtn_dtype dtype,
+                               const float* t_lo, const float* t_hi, int64_t n_thr, void* out_packed, int32_t* out_sum, void* stream);
+
+/* The norms after one block and before the next, with the block's gate and residual, in one pass over T tokens of W values:
+ *     y = branch[t],  or  sum_j weights[t][j] branch[place[t][j]]  (the experts' weighted sum; a negative place adds nothing)
+ *     u = y post_weight / sqrt(mean(y^2) + eps)                    (post_weight NULL: u = y)
+ *     h = residual + scale * g(gate) * u                           (each NULL: left out)
+ *     n = h norm_weight / sqrt(mean(h^2) + eps)                    (norm_weight NULL: n = h)
+ *   branch      [R][W] of `dtype`, or NULL: h = residual
+ *   place       int32 [T][k] with k <= 32, or NULL with k = 0: row t, R = T;  weights fp32 [T][k], or NULL: ones
+ *   gate        [T][W] of `dtype`, g by gate_kind: itself, sigmoid(z) or z sigmoid(z);  scale fp32, n_scale 1 or W values
+ *   residual    [T][W] of `stream_dtype`
+ *   stream_out  NULL, or h in `stream_dtype`; may be `residual` (same stride), no other overlap
+ *   normed      NULL, or n in `dtype` (n is computed from h before its rounding)
+ *   out_packed, out_sum   NULL (both), or n's codes, T packed rows of W codes and their sums (t_lo, t_hi: n_thr 1 or W); they are the codes of
+ *               the exact n
+ * Rows of every tensor are `*_stride` elements apart (0 repeats a row of an input).  W <= 16384.  A place >= R makes the token's row NaN
+ * (codes 0), and rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once. */
+rtn_status rtn_block_norm(const void* branch, int64_t branch_stride, int64_t R, const int32_t* place, const float* weights, int64_t k,
+                          const float* post_weight, const void* gate, int64_t gate_stride, rtn_gate gate_kind,
+                          const float* scale, int64_t n_scale, const void* residual, int64_t residual_stride,
+                          const float* norm_weight, float eps, int64_t T, int64_t W, void* stream_out, int64_t stream_stride,
+                          void* normed, int64_t normed_stride, const float* t_lo, const float* t_hi, int64_t n_thr,
+                          void* out_packed, int32_t* out_sum, rtn_dtype dtype, rtn_dtype stream_dtype, void* stream);
+
 /* The variant RTN_VARIANT_AUTO resolves to for a shape (never AUTO). */
 rtn_variant rtn_choose_gemm_variant(int64_t M, int64_t N, int64_t K);
 /* Slices of K that RTN_VARIANT_AUTO cuts a GEMM shape into (1 = none).  A linear layer with few rows and

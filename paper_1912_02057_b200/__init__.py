@@ -1,6 +1,6 @@
 """B200-native forward ternary-by-ternary contraction of the Reparameterized Ternary Network
 (arXiv 1912.02057): ternarize + pack, packed ternary GEMM / conv2d, affine epilogue; and the operators of a ternary
-language-model layer around it (linear layer, query / key norm and rotation, decay attention).
+language-model layer around it (linear layer, query / key norm and rotation, decay attention, routed experts, block norms).
 
 The compute lives in the CUDA shared library ``librtn_b200.so`` (C ABI declared in
 ``include/rtn.h``); :mod:`.binding` marshals torch tensors into it and fails loudly when the
@@ -14,6 +14,7 @@ from .binding import (  # noqa: F401
     rtn_ternary_conv2d_noalloc, rtn_ternary_conv2d_fused, rtn_ternary_conv2d_packed,
     rtn_last_device_status, rtn_release_scratch, rtn_selftest_wait_timeout, rtn_probe_peak_i8, rtn_probe_i8_rate, rtn_probe_peak_popc, rtn_probe_copy, rtn_choose_gemm_variant, rtn_gemm_k_slices, rtn_gemm_kernel_launches, rtn_choose_conv_variant, rtn_conv_kernel_launches, rtn_conv_next_kernel_launches,
     rtn_ternary_linear, rtn_rotary_table, rtn_qk_norm_rotary, rtn_decay_attention, rtn_decay_attention_step,
+    rtn_route_experts, rtn_ternary_experts, rtn_block_norm, Routing, Normed, SCORE_SOFTMAX, SCORE_SIGMOID, GATE_LINEAR, GATE_SIGMOID, GATE_SILU,
     ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU, ROTARY_HALF, ROTARY_INTERLEAVED,
     ROTARY_SCALE_NONE, ROTARY_SCALE_LINEAR, ROTARY_SCALE_BASE, ROTARY_SCALE_PARTS,
     PAD_CODE_ZERO, PAD_VALUE_ZERO, VARIANT_AUTO, VARIANT_POPC, VARIANT_I8,

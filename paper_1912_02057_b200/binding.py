@@ -7,6 +7,7 @@ missing, the first call raises.
 ``stream=S`` stands for ``with torch.cuda.stream(S)`` around the call: the results a call makes belong to S, and as there the
 caller sees to it that inputs made on another stream are complete, and stay, until S has used them.
 """
+import collections
 import contextlib
 import ctypes as C
 import os
@@ -21,6 +22,8 @@ VARIANT_AUTO, VARIANT_POPC, VARIANT_I8 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 ROTARY_SCALE_NONE, ROTARY_SCALE_LINEAR, ROTARY_SCALE_BASE, ROTARY_SCALE_PARTS = 0, 1, 2, 3
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GATE_LINEAR, GATE_SIGMOID, GATE_SILU = 0, 1, 2
 
 _STATUS = {0: "RTN_OK", 1: "RTN_ERR_NULL", 2: "RTN_ERR_SHAPE", 3: "RTN_ERR_ALIGN",
            4: "RTN_ERR_VALUE", 5: "RTN_ERR_UNSUPPORTED", 6: "RTN_ERR_CUDA",
@@ -102,6 +105,14 @@ def lib():
         L.rtn_decay_attention.argtypes = [_vp, _i64, _i64] * 4 + [_i64, _i64, _vp, _i64] + _states
         L.rtn_decay_attention_step.restype = _int
         L.rtn_decay_attention_step.argtypes = [_vp, _i64, _i64] * 4 + [_i64] + _states
+        L.rtn_route_experts.restype = _int
+        L.rtn_route_experts.argtypes = [_vp, _i64, _i64, _i64, _int, _int, _vp, _i64, _i64, _i64, _i64, _int, _f32] + [_vp] * 6
+        L.rtn_ternary_experts.restype = _int
+        L.rtn_ternary_experts.argtypes = [_vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp,
+                                          _int, _int, _vp, _i64, _int, _vp, _vp, _i64, _vp, _vp, _vp]
+        L.rtn_block_norm.restype = _int
+        L.rtn_block_norm.argtypes = [_vp, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _int, _vp, _i64, _vp, _i64, _vp, _f32, _i64, _i64,
+                                     _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _int, _int, _vp]
         L.rtn_choose_gemm_variant.restype = _int
         L.rtn_choose_gemm_variant.argtypes = [_i64] * 3
         L.rtn_gemm_kernel_launches.restype = _i64
@@ -420,7 +431,7 @@ def _load_torch_side():
     at = lambda f: C.cast(f, C.c_void_p).value
     L = lib()
     native.bind(at(L.rtn_ternary_linear), at(L.rtn_qk_norm_rotary), at(L.rtn_decay_attention), at(L.rtn_decay_attention_step),
-                at(L.rtn_packed_row_bytes), RtnError)
+                at(L.rtn_packed_row_bytes), at(L.rtn_route_experts), at(L.rtn_ternary_experts), at(L.rtn_block_norm), RtnError)
     _torch_side = native
     return native
 
@@ -466,3 +477,40 @@ def rtn_decay_attention_step(q, k, v, log_decay, state, state_out=None, slots=No
     """One new token for each of B sequences: q [B,H,Dk], k [B,Hk,Dk], v [B,Hk,Dv]; ``state`` (None: zero) and ``state_out``
     (default: in place) fp32 [slots,H,Dk,Dv], ``slots`` int32 [B] (negative: a padding entry).  Returns (out [B,H,Dv], state_out)."""
     return (_torch_side or _load_torch_side()).step(q, k, v, log_decay, state, state_out, slots, scale, out, stream and stream.cuda_stream)
+
+
+Routing = collections.namedtuple("Routing", "experts weights start tokens place")
+Normed = collections.namedtuple("Normed", "stream normed codes sums")
+
+
+def rtn_route_experts(logits, top_k, score=SCORE_SOFTMAX, bias=None, groups=1, kept_groups=None, group_top=1, renormalise=True, scale=1.0,
+                      plan=True, stream=None):
+    """Chooses ``top_k`` of the experts for each row of ``logits`` [T,E]: by softmax or sigmoid scores plus ``bias`` (fp32 [E], which moves the
+    choice only), out of the ``kept_groups`` of ``groups`` whose ``group_top`` largest sum up highest.  Returns Routing(experts int32 [T,top_k],
+    weights fp32 [T,top_k], start int32 [E+1], tokens int32 [T*top_k], place int32 [T,top_k]); the last three are the plan of the rows
+    that rtn_ternary_experts works on (``plan=False``: None).  Logits of -inf or NaN are never chosen (-1 where too few are left)."""
+    return Routing(*(_torch_side or _load_torch_side()).route(logits, top_k, score, bias, groups, kept_groups, group_top, renormalise, scale, plan,
+                                                              stream and stream.cuda_stream))
+
+
+def rtn_ternary_experts(a_packed, a_sum, tokens, start, w_packed, w_sum, N, K, a_scale, a_offset, w_scale, w_offset, bias=None,
+                        activation=ACT_NONE, gated=False, out=None, dtype=None, t_lo=None, t_hi=None, out_packed=None, out_sum=None, stream=None):
+    """Each expert's ternary product for its rows start[e] .. start[e+1]-1 (row r is input row tokens[r]; ``tokens=None``: r): act(y), or
+    act(y[:F]) * y[F:] where ``gated`` (F = N/2).  w_packed: E*N packed rows of K codes; w_sum, w_scale, w_offset, bias: E*N values (scale
+    and offset also 1).  Returns [R,F] of ``dtype`` (default: the type of ``out``, else fp32), or, given thresholds, the outputs' codes as
+    (packed rows, sums); an ``out`` given with thresholds is written too.  Rows outside every expert are left as they were."""
+    return (_torch_side or _load_torch_side()).experts(a_packed, a_sum, tokens, start, w_packed, w_sum, N, K, a_scale, a_offset, w_scale, w_offset,
+                                                       bias, activation, gated, out, dtype, t_lo, t_hi, out_packed, out_sum,
+                                                       stream and stream.cuda_stream)
+
+
+def rtn_block_norm(branch, residual=None, place=None, weights=None, post_weight=None, gate=None, gate_kind=GATE_LINEAR, scale=None,
+                   norm_weight=None, eps=1e-6, out=None, normed=False, t_lo=None, t_hi=None, out_packed=None, out_sum=None, dtype=None, stream=None):
+    """What stands between two blocks, in one pass: y = branch [T,W] (or the sum over j of weights[t,j] * branch[place[t,j]]), normed where
+    ``post_weight`` is given; h = residual + scale * g(gate) * y; n = h, normed where ``norm_weight`` is given.  Returns Normed(stream, normed,
+    codes, sums): h (in ``out``, which may be ``residual``), n where ``normed`` is True or a tensor, n's codes against t_lo and t_hi and their
+    sums.  h has the residual's type (without one ``out``'s, else ``dtype``, else the branch's), n the branch's (without one that of
+    ``normed``, else ``dtype``, else h's)."""
+    return Normed(*(_torch_side or _load_torch_side()).block_norm(branch, residual, place, weights, post_weight, gate, gate_kind, scale, norm_weight,
+                                                                  eps, out, normed, t_lo, t_hi, out_packed, out_sum, dtype,
+                                                                  stream and stream.cuda_stream))

@@ -1,0 +1,159 @@
+// The experts' ternary products for few rows (decoding): bit planes, AND / XOR / popcount (Eq. 9), act, gate and codes in the epilogue.
+//
+// experts_rows_kernel: a CTA has a tile of MT rows of one expert and a block of output columns.  A group of GL lanes owns CPG outputs at a time, that
+// is CPG weight rows or, gated, CPG pairs of them; lane i takes the 128-code blocks i, i + GL, ... of each (32 adjacent bytes), and one
+// shuffle tree joins the group.
+// Bound: DRAM, the packed weights of the experts that have rows, read once; from about four rows of an expert on the POPC rate.
+#include "rtn_experts.cuh"
+
+namespace rtn {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kOutputs = 4;             // of a group at a time: columns of a CTA = 256 / GL * 4, a multiple of 32
+
+template <int MT, bool kGated, bool kCodes>
+__global__ void __launch_bounds__(kThreads)
+experts_rows_kernel(const __grid_constant__ ExpertsArgs g, int GL, int col_blocks)
+{
+    constexpr int NR = kGated ? 2 * kOutputs : kOutputs;       // weight rows of a group
+    __shared__ uint32_t bits[kCodes ? MT : 1][2][kCodes ? kThreads * kOutputs / 32 : 1];
+    const int gl = threadIdx.x & (GL - 1), per_cta = kThreads / GL * kOutputs;
+    const int col = (int)(blockIdx.x % (unsigned)col_blocks);
+    const int64_t f0 = (int64_t)col * per_cta, n0 = f0 + threadIdx.x / GL * kOutputs;
+    const RowTile tile = find_tile(g.start, g.E, g.R, MT, (int)(blockIdx.x / (unsigned)col_blocks), g.status);
+    if (tile.e < 0) return;
+    const int64_t nblk = (g.K + kBlockCodes - 1) / kBlockCodes;
+    if constexpr (kCodes) {
+        for (int i = threadIdx.x; i < MT * 2 * per_cta / 32; i += kThreads)
+            bits[i / (2 * (per_cta / 32))][i / (per_cta / 32) % 2][i % (per_cta / 32)] = 0;
+        __syncthreads();
+    }
+    const uint4* __restrict__ W = reinterpret_cast<const uint4*>(g.w_packed) + (int64_t)tile.e * g.N * nblk * 2;
+    const uint4* A[MT];
+    #pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        A[i] = nullptr;
+        if (i < tile.rows) {
+            const int64_t m = g.tokens != nullptr ? g.tokens[tile.row + i] : tile.row + i;
+            if (m >= 0 && m < g.T) A[i] = reinterpret_cast<const uint4*>(g.a_packed) + m * nblk * 2;
+            else if (col == 0 && threadIdx.x == 0) atomicOr(g.status, kStatusBadIndex);
+        }
+    }
+    int cnt[MT][NR];
+    #pragma unroll
+    for (int i = 0; i < MT; ++i)
+        #pragma unroll
+        for (int j = 0; j < NR; ++j) cnt[i][j] = 0;
+    for (int64_t kb = gl; kb < nblk; kb += GL) {
+        uint4 w1[NR], w2[NR];
+        #pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            const int64_t n = n0 + j % kOutputs;
+            const bool ok = n < g.F;
+            const uint4* src = W + ((ok ? n + (j >= kOutputs ? g.F : 0) : 0) * nblk + kb) * 2;
+            w1[j] = ok ? __ldg(src) : make_uint4(0, 0, 0, 0);
+            w2[j] = ok ? __ldg(src + 1) : make_uint4(0, 0, 0, 0);
+        }
+        #pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            if (A[i] == nullptr) continue;
+            const uint4 a1 = __ldg(A[i] + kb * 2), a2 = __ldg(A[i] + kb * 2 + 1);
+            #pragma unroll
+            for (int j = 0; j < NR; ++j) {
+                const uint32_t c0 = a1.x & w1[j].x, c1 = a1.y & w1[j].y, c2 = a1.z & w1[j].z, c3 = a1.w & w1[j].w;
+                cnt[i][j] += (__popc(c0) + __popc(c1)) + (__popc(c2) + __popc(c3))
+                           - 2 * ((__popc((a2.x ^ w2[j].x) & c0) + __popc((a2.y ^ w2[j].y) & c1)) +
+                                  (__popc((a2.z ^ w2[j].z) & c2) + __popc((a2.w ^ w2[j].w) & c3)));
+            }
+        }
+    }
+    for (int d = GL / 2; d > 0; d >>= 1) {
+        #pragma unroll
+        for (int i = 0; i < MT; ++i)
+            #pragma unroll
+            for (int j = 0; j < NR; ++j) cnt[i][j] += __shfl_xor_sync(0xffffffffu, cnt[i][j], d);
+    }
+    float lo = 0.f, hi = 0.f;
+    if constexpr (kCodes) { lo = g.t_lo[g.n_thr == 1 ? 0 : tile.e]; hi = g.t_hi[g.n_thr == 1 ? 0 : tile.e]; }
+    for (int o = gl; o < MT * kOutputs; o += GL) {              // lane o of the group finishes outputs o, o + GL, ...
+        const int i = o / kOutputs, j = o % kOutputs;
+        int s = 0, s2 = 0;
+        #pragma unroll
+        for (int a = 0; a < MT; ++a)
+            #pragma unroll
+            for (int b = 0; b < kOutputs; ++b)
+                if (a * kOutputs + b == o) { s = cnt[a][b]; if constexpr (kGated) s2 = cnt[a][kOutputs + b]; }
+        const int64_t n = n0 + j;
+        if (i >= tile.rows || n >= g.F) continue;
+        const RowParams r = row_params(g, tile.row + i);
+        const ColParams c = col_params(g, tile.e, n), c2 = kGated ? col_params(g, tile.e, g.F + n) : c;
+        bool up = false, down = false;
+        const float v = output_of<kCodes>(g, r, tile.e, n, c, (float)s, c2, (float)s2, lo, hi, up, down);
+        if (g.out != nullptr) store_from_f32(g.out, (tile.row + i) * g.out_stride + n, g.dtype, v);
+        if constexpr (kCodes) {
+            const int at = (int)(n - f0);
+            if (up || down) atomicOr(&bits[i][0][at / 32], 1u << (at & 31));
+            if (up) atomicOr(&bits[i][1][at / 32], 1u << (at & 31));
+        }
+    }
+    if constexpr (kCodes) {
+        __syncthreads();
+        const int words = per_cta / 32;
+        const int64_t width = (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes;     // (a packed row's padding is written too)
+        for (int x = threadIdx.x; x < tile.rows * words; x += kThreads) {
+            const int i = x / words, w = x % words;
+            const int64_t c = f0 + w * 32;
+            if (c >= width) continue;
+            uint32_t* at = reinterpret_cast<uint32_t*>(g.out_packed + (tile.row + i) * (width / kBlockCodes * kBlockBytes) +
+                                                       c / kBlockCodes * kBlockBytes + c % kBlockCodes / 8);
+            const uint32_t nz = bits[i][0][w], pos = bits[i][1][w];
+            at[0] = nz;
+            at[4] = pos;
+            const int sum = 2 * __popc(pos) - __popc(nz);
+            if (sum != 0) atomicAdd(&g.out_sum[tile.row + i], sum);                     // (whole numbers: any order gives the same)
+        }
+    }
+}
+
+__global__ void __launch_bounds__(256)
+zero_sums_kernel(const ExpertsArgs g)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < g.R && i >= g.start[0] && i < g.start[g.E]) g.out_sum[i] = 0;
+}
+
+template <int MT>
+cudaError_t launch_rows(const ExpertsArgs& g, cudaStream_t s)
+{
+    const int64_t nblk = (g.K + kBlockCodes - 1) / kBlockCodes;
+    int GL = 1;
+    while (GL < nblk && GL < 32) GL *= 2;
+    const int per_cta = kThreads / GL * kOutputs;
+    const int64_t tiles = g.R / MT + (g.E < g.R ? g.E : g.R);           // at most: an expert has one tile that is not full
+    const int64_t width = g.out_packed != nullptr ? (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes : g.F;
+    const int64_t cols = (width + per_cta - 1) / per_cta;
+    if (cols * tiles > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    const unsigned grid = (unsigned)(cols * tiles);
+    if (g.out_packed != nullptr) {
+        zero_sums_kernel<<<(unsigned)((g.R + 255) / 256), 256, 0, s>>>(g);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        if (g.gated) experts_rows_kernel<MT, true, true><<<grid, kThreads, 0, s>>>(g, GL, (int)cols);
+        else experts_rows_kernel<MT, false, true><<<grid, kThreads, 0, s>>>(g, GL, (int)cols);
+    } else {
+        if (g.gated) experts_rows_kernel<MT, true, false><<<grid, kThreads, 0, s>>>(g, GL, (int)cols);
+        else experts_rows_kernel<MT, false, false><<<grid, kThreads, 0, s>>>(g, GL, (int)cols);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_ternary_experts(const ExpertsArgs& g, cudaStream_t s)
+{
+    return g.R <= g.E ? launch_rows<1>(g, s) : launch_rows<4>(g, s);
+}
+
+}  // namespace rtn

@@ -121,6 +121,75 @@ struct DecayArgs {
     unsigned* status;
 };
 
+constexpr int kMaxExperts = 1024;
+constexpr int kMaxChoices = 32;             // experts of a token, groups
+struct RouteArgs {
+    const void* logits;
+    int64_t stride, T;
+    int E, dtype, score;
+    const float* bias;                                  // [E] or NULL
+    int groups, kept, group_top, top_k, renormalise;
+    float scale;
+    int32_t* experts;                                   // [T][top_k]
+    float* weights;
+    int32_t *start, *tokens, *place;                    // the plan, or NULL
+};
+
+struct ExpertsArgs {
+    const uint8_t* a_packed;
+    const int32_t* a_sum;
+    int64_t T;
+    const int32_t* tokens;                              // [R] or NULL (row r is input row r)
+    const int32_t* start;                               // [E + 1]
+    int64_t R;
+    const uint8_t* w_packed;
+    const int32_t* w_sum;
+    int E;
+    int64_t N, K, F;                                    // F outputs of a row: N, or N / 2 where gated
+    EpilogueParams ep;
+    const float* bias;                                  // [E][N] or NULL
+    int act, gated;
+    void* out;
+    int64_t out_stride;
+    int dtype;
+    const float *t_lo, *t_hi;
+    int64_t n_thr;
+    uint8_t* out_packed;
+    int32_t* out_sum;
+    unsigned* status;
+};
+
+constexpr int kNormMaxWidth = 16384;
+struct NormArgs {
+    const void* branch;                                 // or NULL
+    int64_t branch_stride, R;
+    const int32_t* place;                               // [T][k] or NULL
+    const float* weights;
+    int k;
+    const float* post_weight;
+    const void* gate;
+    int64_t gate_stride;
+    int gate_kind;
+    const float* scale;
+    int n_scale;
+    const void* residual;
+    int64_t residual_stride;
+    const float* norm_weight;
+    float eps;
+    int64_t T;
+    int W;
+    void* stream_out;
+    int64_t stream_stride;
+    void* normed;
+    int64_t normed_stride;
+    const float *t_lo, *t_hi;
+    int n_thr;
+    uint8_t* out_packed;
+    int32_t* out_sum;
+    int dtype, stream_dtype;
+    unsigned* status;
+};
+
 // Multiprocessors of the current device, asked once per device.  Plans, *_supported answers, launch counts,
 // scratch sizes and the launchers all size their grids with this number, so they agree on any part.  Without a
 // usable device (a host-only query) the answer is a B200's 148.
@@ -183,6 +252,9 @@ cudaError_t launch_rotary_table(float* table, int64_t rows, int R, double base, 
                                 double low, double high, double amplitude, cudaStream_t s);
 cudaError_t launch_decay_attention(const DecayArgs& g, cudaStream_t s);
 cudaError_t launch_decay_attention_step(const DecayArgs& g, cudaStream_t s);
+cudaError_t launch_route_experts(const RouteArgs& g, cudaStream_t s);
+cudaError_t launch_ternary_experts(const ExpertsArgs& g, cudaStream_t s);
+cudaError_t launch_block_norm(const NormArgs& g, cudaStream_t s);
 
 // Tensor-core (tcgen05 kind::i8) variants; *_supported say whether a shape can run there.
 bool gemm_i8_supported(int64_t M, int64_t N, int64_t K);

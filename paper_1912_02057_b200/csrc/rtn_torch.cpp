@@ -22,6 +22,9 @@ decltype(&rtn_qk_norm_rotary) f_rotary;
 decltype(&rtn_decay_attention) f_decay;
 decltype(&rtn_decay_attention_step) f_step;
 decltype(&rtn_packed_row_bytes) f_row_bytes;
+decltype(&rtn_route_experts) f_route;
+decltype(&rtn_ternary_experts) f_experts;
+decltype(&rtn_block_norm) f_norm;
 PyObject* rtn_error;                // class RtnError(code, where)
 
 // Thrown with the Python error already set.
@@ -300,6 +303,173 @@ PyObject* step(PyObject* const* a)
     return pair_of(d.out, &d.state_out);
 }
 
+// Address and row stride of a [rows, width] tensor with adjacent columns.
+struct Rows {
+    void* p = nullptr;
+    int64_t stride = 0;
+    Rows() = default;
+    Rows(const at::Tensor& t, const char* name, at::ScalarType type, const Call& call, int64_t rows, int64_t width)
+    {
+        if (t.dim() != 2 || (rows >= 0 && t.size(0) != rows) || t.size(1) != width || t.scalar_type() != type || t.device() != call.device ||
+            (t.stride(1) != 1 && width > 1 && t.size(0) > 0))
+            refuse(std::string(name) + ": expected " + c10::toString(type) + " [" + (rows >= 0 ? std::to_string(rows) : "rows") + ", " +
+                   std::to_string(width) + "] with adjacent columns on " + call.device.str() + ", got " + text(t));
+        p = t.data_ptr();
+        stride = t.size(0) > 1 ? t.stride(0) : std::max(width, t.stride(0));
+    }
+};
+
+bool truth(PyObject* o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised{};
+    return v != 0;
+}
+
+at::ScalarType dtype_of(PyObject* o, at::ScalarType otherwise)
+{
+    if (o == Py_None) return otherwise;
+    if (!THPDtype_Check(o)) refuse("dtype: expected a torch.dtype");
+    return reinterpret_cast<THPDtype*>(o)->scalar_type;
+}
+
+PyObject* tuple_of(std::initializer_list<const at::Tensor*> ts)
+{
+    PyObject* r = PyTuple_New((Py_ssize_t)ts.size());
+    Py_ssize_t i = 0;
+    for (const at::Tensor* t : ts) {
+        PyObject* x = t != nullptr && t->defined() ? THPVariable_Wrap(*t) : Py_NewRef(Py_None);
+        if (r == nullptr || x == nullptr) { Py_XDECREF(r); Py_XDECREF(x); return nullptr; }
+        PyTuple_SET_ITEM(r, i++, x);
+    }
+    return r;
+}
+
+// Thresholds and the places of the codes: none, or all of them.
+struct Codes {
+    const float *lo = nullptr, *hi = nullptr;
+    int64_t n = 1;
+    at::Tensor packed, sums;
+    void* p = nullptr;
+    int32_t* s = nullptr;
+    Codes(const Call& call, PyObject* t_lo, PyObject* t_hi, PyObject* out_packed, PyObject* out_sum, int64_t rows, int64_t width, int64_t full)
+    {
+        const at::Tensor *a = tensor_or_none(t_lo, "t_lo"), *b = tensor_or_none(t_hi, "t_hi");
+        const at::Tensor *gp = tensor_or_none(out_packed, "out_packed"), *gs = tensor_or_none(out_sum, "out_sum");
+        if (a == nullptr && b == nullptr) {
+            if (gp != nullptr || gs != nullptr) refuse("out_packed and out_sum: codes need t_lo and t_hi");
+            return;
+        }
+        if (a == nullptr || b == nullptr) refuse("t_lo and t_hi: both, or neither");
+        n = a->numel();
+        if ((n != 1 && n != full) || b->numel() != n)
+            refuse("t_lo and t_hi: expected 1 or " + std::to_string(full) + " values each, got " + std::to_string(n) + " and " + std::to_string(b->numel()));
+        lo = call.dense<float>(a, "t_lo", at::kFloat);
+        hi = call.dense<float>(b, "t_hi", at::kFloat);
+        const int64_t row = (int64_t)f_row_bytes(width);
+        packed = gp != nullptr ? *gp : call.empty({rows, row}, at::kByte);
+        sums = gs != nullptr ? *gs : call.empty({rows}, at::kInt);
+        p = call.dense(&packed, "out_packed", at::kByte, {rows, row});
+        s = call.dense<int32_t>(&sums, "out_sum", at::kInt, {rows});
+    }
+};
+
+// logits, top_k, score, bias, groups, kept_groups, group_top, renormalise, scale, plan, stream
+PyObject* route(PyObject* const* a)
+{
+    const at::Tensor& logits = tensor(a[0], "logits");
+    if (logits.dim() != 2) refuse("logits: expected [tokens, experts], got " + text(logits));
+    const rtn_dtype dtype = type_of(logits.scalar_type());
+    const Call call(logits, a[10]);
+    const int64_t T = logits.size(0), E = logits.size(1), k = whole(a[1], "top_k"), groups = whole(a[4], "groups");
+    if (k < 1 || k > 32) refuse("top_k: expected 1 to 32, got " + std::to_string(k));
+    const Rows x(logits, "logits", logits.scalar_type(), call, T, E);
+    const at::Tensor experts = call.empty({T, k}, at::kInt), weights = call.empty({T, k}, at::kFloat);
+    at::Tensor start, tokens, place;
+    const bool plan = truth(a[9]);
+    if (plan) { start = call.empty({E + 1}, at::kInt); tokens = call.empty({T * k}, at::kInt); place = call.empty({T, k}, at::kInt); }
+    auto at_ = [](const at::Tensor& t) { return t.defined() ? static_cast<int32_t*>(t.data_ptr()) : nullptr; };
+    check(f_route(x.p, x.stride, T, E, dtype, (rtn_score)whole(a[2], "score"), call.dense<float>(tensor_or_none(a[3], "bias"), "bias", at::kFloat, {E}),
+                  groups, a[5] == Py_None ? groups : whole(a[5], "kept_groups"), whole(a[6], "group_top"), k, truth(a[7]), (float)real(a[8]),
+                  at_(experts), static_cast<float*>(weights.data_ptr()), at_(start), at_(tokens), at_(place), call.stream), "rtn_route_experts");
+    return tuple_of({&experts, &weights, &start, &tokens, &place});
+}
+
+// a_packed, a_sum, tokens, start, w_packed, w_sum, N, K, a_scale, a_offset, w_scale, w_offset, bias, activation, gated, out, dtype, t_lo, t_hi,
+// out_packed, out_sum, stream
+PyObject* experts(PyObject* const* a)
+{
+    const at::Tensor &ap = tensor(a[0], "a_packed"), &as = tensor(a[1], "a_sum"), &start = tensor(a[3], "start");
+    const at::Tensor &wp = tensor(a[4], "w_packed"), &ws = tensor(a[5], "w_sum");
+    const at::Tensor *tokens = tensor_or_none(a[2], "tokens"), *bias = tensor_or_none(a[12], "bias"), *given = tensor_or_none(a[15], "out");
+    const int64_t N = whole(a[6], "N"), K = whole(a[7], "K");
+    const Call call(ap, a[21]);
+    const bool gated = truth(a[14]);
+    if (start.dim() != 1 || start.numel() < 2) refuse("start: expected [E + 1], got " + text(start));
+    const int64_t E = start.numel() - 1, T = as.numel(), R = tokens != nullptr ? tokens->numel() : T, row = (int64_t)f_row_bytes(K);
+    if (N <= 0 || K <= 0 || (gated && N % 2 != 0)) refuse("N and K: expected positive sizes (N even where gated), got " + std::to_string(N) + " and " + std::to_string(K));
+    if (N > (INT64_C(1) << 31) / E || ap.numel() != T * row || wp.numel() != E * N * row || ws.numel() != E * N)
+        refuse("operands do not fit E=" + std::to_string(E) + ", N=" + std::to_string(N) + ", K=" + std::to_string(K) + " and " + std::to_string(T) + " input rows");
+    const int64_t F = gated ? N / 2 : N;
+    const Codes codes(call, a[17], a[18], a[19], a[20], R, F, E);
+    const at::ScalarType type = dtype_of(a[16], given != nullptr ? given->scalar_type() : at::kFloat);
+    const rtn_dtype dtype = type_of(type);
+    at::Tensor out;
+    Rows o;
+    if (given != nullptr || codes.p == nullptr) {
+        out = given != nullptr ? *given : call.empty({R, F}, type);
+        o = Rows(out, "out", type, call, R, F);
+    }
+    const float *s1, *o1, *s2, *o2;
+    const int64_t na = params(call, tensor(a[8], "a_scale"), tensor(a[9], "a_offset"), T, "a", s1, o1);
+    const int64_t nw = params(call, tensor(a[10], "w_scale"), tensor(a[11], "w_offset"), E * N, "w", s2, o2);
+    if (bias != nullptr && bias->numel() != E * N) refuse("bias: expected " + std::to_string(E * N) + " values, got " + text(*bias));
+    check(f_experts(call.dense(&ap, "a_packed", at::kByte), call.dense<int32_t>(&as, "a_sum", at::kInt), T,
+                    call.dense<int32_t>(tokens, "tokens", at::kInt), call.dense<int32_t>(&start, "start", at::kInt), R, call.dense(&wp, "w_packed", at::kByte),
+                    call.dense<int32_t>(&ws, "w_sum", at::kInt), E, N, K, s1, o1, na, s2, o2, nw, call.dense<float>(bias, "bias", at::kFloat),
+                    (rtn_activation)whole(a[13], "activation"), gated, o.p, o.stride, dtype, codes.lo, codes.hi, codes.n, codes.p, codes.s, call.stream),
+          "rtn_ternary_experts");
+    if (!codes.packed.defined()) return given != nullptr ? Py_NewRef(a[15]) : THPVariable_Wrap(out);
+    return tuple_of({&codes.packed, &codes.sums});
+}
+
+// branch, residual, place, weights, post_weight, gate, gate_kind, scale, norm_weight, eps, out, normed, t_lo, t_hi, out_packed, out_sum, dtype, stream
+PyObject* block_norm(PyObject* const* a)
+{
+    const at::Tensor *branch = tensor_or_none(a[0], "branch"), *residual = tensor_or_none(a[1], "residual"), *place = tensor_or_none(a[2], "place");
+    const at::Tensor *weights = tensor_or_none(a[3], "weights"), *gate = tensor_or_none(a[5], "gate"), *scale = tensor_or_none(a[7], "scale");
+    const at::Tensor *given = tensor_or_none(a[10], "out"), *given_n = PyBool_Check(a[11]) ? nullptr : tensor_or_none(a[11], "normed");
+    if (branch == nullptr && residual == nullptr) refuse("branch and residual: one of them is required");
+    const at::Tensor& first = branch != nullptr ? *branch : *residual;
+    const Call call(first, a[17]);
+    if (first.dim() != 2) refuse("expected [rows, width], got " + text(first));
+    const int64_t W = first.size(1), R = branch != nullptr ? branch->size(0) : 0;
+    if (place != nullptr && place->dim() != 2) refuse("place: expected [tokens, choices], got " + text(*place));
+    const int64_t T = place != nullptr ? place->size(0) : first.size(0), k = place != nullptr ? place->size(1) : 0;
+    const at::ScalarType stream_type = residual != nullptr ? residual->scalar_type() : given != nullptr ? given->scalar_type() : dtype_of(a[16], first.scalar_type());
+    const at::ScalarType type = branch != nullptr ? branch->scalar_type() : given_n != nullptr ? given_n->scalar_type() : dtype_of(a[16], stream_type);
+    const rtn_dtype dtype = type_of(type), stream_dtype = type_of(stream_type);
+    Rows b, r, z, h, n;
+    if (branch != nullptr) b = Rows(*branch, "branch", type, call, place != nullptr ? -1 : T, W);
+    if (residual != nullptr) r = Rows(*residual, "residual", stream_type, call, T, W);
+    if (gate != nullptr) z = Rows(*gate, "gate", type, call, T, W);
+    const at::Tensor out = given != nullptr ? *given : call.empty({T, W}, stream_type);
+    h = Rows(out, "out", stream_type, call, T, W);
+    at::Tensor normed;
+    if (given_n != nullptr || a[11] == Py_True) {
+        normed = given_n != nullptr ? *given_n : call.empty({T, W}, type);
+        n = Rows(normed, "normed", type, call, T, W);
+    }
+    const Codes codes(call, a[12], a[13], a[14], a[15], T, W, W);
+    if (scale != nullptr && scale->numel() != 1 && scale->numel() != W) refuse("scale: expected 1 or " + std::to_string(W) + " values, got " + text(*scale));
+    check(f_norm(b.p, b.stride, R, call.dense<int32_t>(place, "place", at::kInt), call.dense<float>(weights, "weights", at::kFloat, {T, k}), k,
+                 call.dense<float>(tensor_or_none(a[4], "post_weight"), "post_weight", at::kFloat, {W}), z.p, z.stride, (rtn_gate)whole(a[6], "gate_kind"),
+                 call.dense<float>(scale, "scale", at::kFloat), scale != nullptr ? scale->numel() : 1, r.p, r.stride,
+                 call.dense<float>(tensor_or_none(a[8], "norm_weight"), "norm_weight", at::kFloat, {W}), (float)real(a[9]), T, W, h.p, h.stride,
+                 n.p, n.stride, codes.lo, codes.hi, codes.n, codes.p, codes.s, dtype, stream_dtype, call.stream), "rtn_block_norm");
+    return tuple_of({&out, &normed, &codes.packed, &codes.sums});
+}
+
 template <PyObject* (*F)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -316,13 +486,16 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     try {
-        expect_args(n, 6);
+        expect_args(n, 9);
         f_linear = reinterpret_cast<decltype(f_linear)>(whole(args[0], ""));
         f_rotary = reinterpret_cast<decltype(f_rotary)>(whole(args[1], ""));
         f_decay = reinterpret_cast<decltype(f_decay)>(whole(args[2], ""));
         f_step = reinterpret_cast<decltype(f_step)>(whole(args[3], ""));
         f_row_bytes = reinterpret_cast<decltype(f_row_bytes)>(whole(args[4], ""));
-        rtn_error = Py_NewRef(args[5]);
+        f_route = reinterpret_cast<decltype(f_route)>(whole(args[5], ""));
+        f_experts = reinterpret_cast<decltype(f_experts)>(whole(args[6], ""));
+        f_norm = reinterpret_cast<decltype(f_norm)>(whole(args[7], ""));
+        rtn_error = Py_NewRef(args[8]);
     } catch (const Raised&) {
         return nullptr;
     }
@@ -331,7 +504,8 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
 
 #define RTN_METHOD(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(static_cast<PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t)>(fn))), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RTN_METHOD("bind", bind), RTN_METHOD("linear", (entry<linear, 17>)), RTN_METHOD("rotary", (entry<rotary, 11>)),
-                         RTN_METHOD("decay", (entry<decay, 12>)), RTN_METHOD("step", (entry<step, 10>)), {nullptr, nullptr, 0, nullptr}};
+                         RTN_METHOD("decay", (entry<decay, 12>)), RTN_METHOD("step", (entry<step, 10>)), RTN_METHOD("route", (entry<route, 11>)), RTN_METHOD("experts", (entry<experts, 22>)),
+                         RTN_METHOD("block_norm", (entry<block_norm, 18>)), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rtn_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
