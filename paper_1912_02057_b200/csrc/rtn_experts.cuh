@@ -5,6 +5,8 @@
 
 namespace rtn {
 
+cudaError_t launch_experts_tiles(const ExpertsArgs& g, cudaStream_t s);        // on the tensor cores
+
 #ifdef __CUDACC__
 
 // Tile `index` of the experts' rows, each expert's in tiles of `height`: expert (-1: there are not so many tiles), first row and rows.
