@@ -153,7 +153,7 @@ cudaError_t launch_rows(const ExpertsArgs& g, cudaStream_t s)
 
 cudaError_t launch_ternary_experts(const ExpertsArgs& g, cudaStream_t s)
 {
-    if (g.R > 32) return launch_experts_tiles(g, s);
+    if (g.R > 32 && experts_tiles_supported(g)) return launch_experts_tiles(g, s);
     return g.R <= g.E ? launch_rows<1>(g, s) : launch_rows<4>(g, s);
 }
 

@@ -6,6 +6,7 @@
 namespace rtn {
 
 cudaError_t launch_experts_tiles(const ExpertsArgs& g, cudaStream_t s);        // on the tensor cores
+bool experts_tiles_supported(const ExpertsArgs& g);
 
 #ifdef __CUDACC__
 
@@ -74,16 +75,19 @@ __device__ __forceinline__ ColParams col_params(const ExpertsArgs& g, int64_t e,
     return p;
 }
 
-// y = a_s (w_s S + w_o S_x) + (a_o p3 + bias): at most five roundings to a term.
+// y = w_s (a_s S) + (w_o (a_s S_x) + (p3 a_o + bias)): at most five roundings to a term, the same in both forms of the product.
 __device__ __forceinline__ float affine(const RowParams& r, const ColParams& c, float S)
 {
-    return fmaf(r.as, fmaf(c.ws, S, c.wo * r.sx), fmaf(r.ao, c.p3, c.bias));
+    return fmaf(c.ws, r.as * S, fmaf(c.wo, r.as * r.sx, fmaf(c.p3, r.ao, c.bias)));
 }
 // What the terms add up to in magnitude.
 __device__ __forceinline__ float affine_size(const RowParams& r, const ColParams& c, float S)
 {
-    return fmaf(fabsf(r.as), fmaf(fabsf(c.ws), fabsf(S), fabsf(c.wo * r.sx)), fmaf(fabsf(r.ao), fabsf(c.p3), fabsf(c.bias)));
+    return fmaf(fabsf(c.ws), fabsf(r.as * S), fmaf(fabsf(c.wo), fabsf(r.as * r.sx), fmaf(fabsf(r.ao), fabsf(c.p3), fabsf(c.bias))));
 }
+// y / (1 + e^-y) by the approximate exponential and reciprocal: within 6 units of |y| (the exponent's rounding, up to 1.5 |y| units of e^-y, comes
+// with a factor e^-y / (1 + e^-y)^2).
+__device__ __forceinline__ float fast_silu(float y) { return __fdividef(y, 1.f + __expf(-y)); }
 
 __device__ __forceinline__ double exact_activation(double y, int act)
 {
@@ -120,7 +124,8 @@ __device__ __forceinline__ float output_of(const ExpertsArgs& g, const RowParams
 {
     float a = affine(r, c, S), y2 = 1.f;
     const float y1 = a;
-    if (g.act != RTN_ACT_NONE) a = activation(a, g.act);
+    if (g.act == RTN_ACT_SILU) a = fast_silu(a);
+    else if (g.act != RTN_ACT_NONE) a = activation(a, g.act);
     float v = a;
     if (g.gated) { y2 = affine(r, c2, S2); v = a * y2; }
     if constexpr (kCodes) {
@@ -129,7 +134,7 @@ __device__ __forceinline__ float output_of(const ExpertsArgs& g, const RowParams
         up = v > hi;
         down = !up && v < lo;
         const float d = fminf(fabsf(v - lo), fabsf(v - hi));
-        if (!(d > 1.25f * kUnit * err) || !(fabsf(v) < 1e37f)) {
+        if (!(d > 1.25f * kUnit * err)) {                       // (what overflowed or is NaN has such a bound)
             up = down = false;
             if (r.token >= 0) {
                 const double x = exact_value(g, r.token, e, n, S, S2);
