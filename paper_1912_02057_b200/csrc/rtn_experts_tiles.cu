@@ -29,11 +29,19 @@ struct TilesPlan {
 
 struct Bars {
     uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
+    uint32_t most[3][2];        // the largest |a_s S_x| and |a_o| of a tile, the next and the one after it, as bit patterns
     uint32_t tmem_slot;
     int dead;
 };
 
-struct TokenParams { float as[kMaxRows], asx[kMaxRows], ao[kMaxRows]; int token[kMaxRows]; };     // a_s, a_s S_x, a_o, input row (-1: out of range)
+// What the epilogue of a tile needs: a_s, a_s S_x, a_o and input row (-1: out of range) of its tokens, w_s, w_o, p3 and bias of its weight rows by
+// TMEM lane; the votes of each 16 tokens and quarter of the lanes.
+struct TileParams {
+    float as[kMaxRows], asx[kMaxRows], ao[kMaxRows];
+    int token[kMaxRows];
+    float4 col[128];
+    uint4 votes[4][kMaxRows / 4][2];
+};
 
 struct Tile { int e, row, rows, height; };
 
@@ -98,9 +106,8 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     Bars& bar = *reinterpret_cast<Bars*>(smem);
-    TokenParams* token = reinterpret_cast<TokenParams*>(smem + 256);             // [2]
-    int* sums = reinterpret_cast<int*>(token + 2);                               // [2][kMaxRows]
-    int* before = sums + 2 * kMaxRows;                                           // [E + 1] tiles before an expert's
+    TileParams* params = reinterpret_cast<TileParams*>(smem + 256);              // [2]
+    int* before = reinterpret_cast<int*>(params + 2);                            // [E + 1] tiles before an expert's
     int* first = before + g.E + 1;                                               // [E] its first row
     int* count = first + g.E;                                                    // [E] its rows
     int* height = count + g.E;                                                   // [E] rows of its tiles
@@ -143,7 +150,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         }
         if (lane == 0) before[g.E] = sum;
     }
-    if (threadIdx.x < 2 * kMaxRows) sums[threadIdx.x] = 0;
+    if (threadIdx.x < 6) bar.most[threadIdx.x / 2][threadIdx.x % 2] = 0;
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
@@ -187,8 +194,11 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
     const int quad = warp & 3;
     const int64_t nblk = (g.K + kBlockCodes - 1) / kBlockCodes;
     constexpr int kTileOuts = kGated ? 64 : 128;
-    // The weight row of a lane: 32 adjacent ones to a warp; gated, 16 and the 16 that they are multiplied with.
-    auto output_at = [&](uint32_t t) { return (int64_t)(t % cols) * kTileOuts + (kGated ? quad * 16 + (lane & 15) : quad * 32 + lane); };
+    // The output that TMEM lane 32 q + l belongs to, so that the lanes r, r + 8, ... which one thread of the epilogue reads are adjacent outputs; gated,
+    // lanes l >= 16 are the rows that those of l - 16 are multiplied with.
+    auto output_at = [&](uint32_t t, int q, int l) {
+        return (int64_t)(t % cols) * kTileOuts + (kGated ? q * 16 + 2 * (l & 7) + (l >> 3 & 1) : q * 32 + 4 * (l & 7) + (l >> 3));
+    };
     bool alive = true;
 
     if (warp < kExpandWarps) {
@@ -202,7 +212,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             bool moved = src == nullptr;
             while (k >= p.k_stages && t < total) { k -= p.k_stages; t += gridDim.x; moved = true; }
             if (moved && t < total) {
-                const int64_t f = output_at(t), e = find(t).e;
+                const int64_t f = output_at(t, quad, lane), e = find(t).e;
                 src = W;
                 left = 0;
                 if (f < g.F) {
@@ -223,21 +233,22 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         int s = warp >> 2;
         uint32_t phase = 0;
         while (t < total) {
-            uint4 w[4];
+            // expanded before the slot is free: what follows the wait is the store alone
+            uint32_t o[2][16];
             #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = next[i];
+            for (int i = 0; i < 2; ++i) {
+                const uint4 c0 = expand_weight(next[2 * i].x, next[2 * i + 1].x), c1 = expand_weight(next[2 * i].y, next[2 * i + 1].y);
+                const uint4 c2 = expand_weight(next[2 * i].z, next[2 * i + 1].z), c3 = expand_weight(next[2 * i].w, next[2 * i + 1].w);
+                o[i][0] = c0.x; o[i][1] = c0.y; o[i][2] = c0.z; o[i][3] = c0.w; o[i][4] = c1.x; o[i][5] = c1.y; o[i][6] = c1.z; o[i][7] = c1.w;
+                o[i][8] = c2.x; o[i][9] = c2.y; o[i][10] = c2.z; o[i][11] = c2.w; o[i][12] = c3.x; o[i][13] = c3.y; o[i][14] = c3.z; o[i][15] = c3.w;
+            }
             k += 2; src += 8; left -= 4;
             enter();
             if (t < total) fetch();
             if (!warp_wait(&bar.empty[s], phase + 1)) break;
             const uint32_t at = a_tmem + (uint32_t)(s * 32) + ((uint32_t)(quad * 32) << 16);
-            #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint4 c0 = expand_weight(w[2 * i].x, w[2 * i + 1].x), c1 = expand_weight(w[2 * i].y, w[2 * i + 1].y);
-                const uint4 c2 = expand_weight(w[2 * i].z, w[2 * i + 1].z), c3 = expand_weight(w[2 * i].w, w[2 * i + 1].w);
-                const uint32_t o[16] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w, c2.x, c2.y, c2.z, c2.w, c3.x, c3.y, c3.z, c3.w};
-                tc::tmem_st16(at + (uint32_t)(i * 16), o);
-            }
+            tc::tmem_st16(at, o[0]);
+            tc::tmem_st16(at + 16u, o[1]);
             tc::tmem_st_wait();
             tc::tc_fence_before_sync();
             __syncwarp();
@@ -291,176 +302,206 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             __syncwarp();
         }
     } else {
-        // ------------------------------------------------------------ write out: a warp has 32 lanes (weight rows) of every other 32 tokens
-        const int mine = threadIdx.x - kExpandWarps * 32, half = (warp - kExpandWarps) >> 2;
-        struct Own { Tile tile; float as, asx, ao; int token; ColParams col; };
-        auto fetch = [&](uint32_t t) {
-            Own o{};
-            o.token = -1;
-            if (t >= total) return o;
-            o.tile = find(t);
-            if (mine < o.tile.rows) {
-                const RowParams r = row_params(g, o.tile.row + mine);
-                o.as = r.as; o.asx = r.as * r.sx; o.ao = r.ao; o.token = r.token;
-                if (r.token < 0 && t % cols == 0) atomicOr(g.status, kStatusBadIndex);
+        // ------------------------------------------------------------ write out: a warp has a quarter of the lanes and every other 16 tokens; a thread
+        // kOwn adjacent outputs of two tokens in each 8.
+        constexpr int kOwn = kGated ? 2 : 4;
+        const int mine = threadIdx.x - kExpandWarps * 32, half = (warp - kExpandWarps) >> 2, r8 = lane >> 2, q4 = lane & 3;
+        // Parameters of the tile after this one, asked for as they are and looked at when this one is done: of token `mine`, of TMEM lane `mine`.
+        struct Raw { int token; float as, ao, ws, wo, bias; int sx, sw; bool col; };
+        Raw raw{};
+        int token_ahead = -1;
+        Tile tile_ahead{};
+        auto ask_token = [&](uint32_t t) {                                        // input row of token `mine` of tile t, a tile ahead of its parameters
+            token_ahead = -1;
+            if (t >= total) return;
+            tile_ahead = find(t);
+            if (mine < tile_ahead.rows) token_ahead = g.tokens != nullptr ? g.tokens[tile_ahead.row + mine] : tile_ahead.row + mine;
+        };
+        auto ask_params = [&](uint32_t t) {                                       // after ask_token(t)
+            raw.token = -1; raw.col = false;
+            if (t >= total) return;
+            if (mine < tile_ahead.rows) {
+                const int64_t m = token_ahead;
+                if (m >= 0 && m < g.T) {
+                    const int64_t i = g.ep.n_aparam == 1 ? 0 : m;
+                    raw.token = (int)m; raw.as = g.ep.a_scale[i]; raw.ao = g.ep.a_offset[i]; raw.sx = g.a_sum[m];
+                } else if (t % cols == 0) atomicOr(g.status, kStatusBadIndex);
             }
-            const int64_t f = output_at(t);
-            if (f < g.F) o.col = col_params(g, o.tile.e, kGated && lane >= 16 ? g.F + f : f);
-            return o;
+            if (mine < 128) {
+                const int64_t f = output_at(t, mine >> 5, mine & 31);
+                if (f < g.F) {
+                    const int64_t at = (int64_t)tile_ahead.e * g.N + (kGated && (mine & 16) ? g.F + f : f), i = g.ep.n_wparam == 1 ? 0 : at;
+                    raw.col = true; raw.ws = g.ep.w_scale[i]; raw.wo = g.ep.w_offset[i]; raw.sw = g.w_sum[at];
+                    raw.bias = g.bias != nullptr ? g.bias[at] : 0.f;
+                }
+            }
         };
-        auto keep = [&](const Own& o, uint32_t at) {
-            if (mine < kMaxRows) { token[at].as[mine] = o.as; token[at].asx[mine] = o.asx; token[at].ao[mine] = o.ao; token[at].token[mine] = o.token; }
+        auto keep = [&](TileParams& q, uint32_t (&most)[2], int rows) {
+            if (mine < kMaxRows) {
+                const float nan = __int_as_float(0x7fffffff);
+                float as = 0.f, asx = 0.f, ao = 0.f;
+                if (mine < rows) {
+                    as = raw.token >= 0 ? raw.as : nan; ao = raw.token >= 0 ? raw.ao : nan;
+                    asx = raw.token >= 0 ? raw.as * (float)raw.sx : nan;
+                }
+                q.as[mine] = as; q.asx[mine] = asx; q.ao[mine] = ao; q.token[mine] = raw.token;
+                if constexpr (kCodes) {
+                    const uint32_t a = __reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(asx))), b = __reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(ao)));
+                    if (lane == 0) { atomicMax(&most[0], a); atomicMax(&most[1], b); }
+                }
+            }
+            if (mine < 128) {
+                ColParams c{0.f, 0.f, 0.f, 0.f};
+                if (raw.col) c = ColParams{raw.ws, raw.wo, (float)((double)raw.ws * (double)raw.sw + (double)g.K * (double)raw.wo), raw.bias};
+                q.col[mine] = make_float4(c.ws, c.wo, c.p3, c.bias);
+            }
         };
-        Own next = fetch(blockIdx.x);
-        keep(next, 0);
+        ask_token(blockIdx.x);
+        ask_params(blockIdx.x);
+        Tile tile = tile_ahead;
+        keep(params[0], bar.most[0], tile.rows);
+        ask_token(blockIdx.x + gridDim.x);
         asm volatile("bar.sync 1, %0;" ::"n"(kEpilogueWarps * 32) : "memory");
         tc::pdl_wait();
         const int64_t width = (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes;
-        uint32_t ti = 0;
+        const bool vec = kCodes || ((reinterpret_cast<uintptr_t>(g.out) % (kOwn * sizeof(T))) == 0 && g.out_stride % kOwn == 0);
+        uint32_t ti = 0, m3 = 0;
         for (uint32_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
-            const Tile tile = next.tile;
-            const ColParams col = next.col;
-            const int64_t f = output_at(t);
-            const TokenParams& rows = token[ti & 1];
-            int* sum = sums + (ti & 1) * kMaxRows;
-            next = fetch(t + gridDim.x);
-            const pair_t ws = make_pair(col.ws, col.ws), wo = make_pair(col.wo, col.wo), p3 = make_pair(col.p3, col.p3), bias = make_pair(col.bias, col.bias);
-            float lo = 0.f, hi = 0.f, off = 0.f, off2 = 0.f;
-            if constexpr (kCodes) {
-                lo = g.t_lo[g.n_thr == 1 ? 0 : tile.e]; hi = g.t_hi[g.n_thr == 1 ? 0 : tile.e];
+            const uint32_t(&most)[2] = bar.most[m3];
+            TileParams& here = params[ti & 1];
+            const Tile next_tile = tile_ahead;
+            if (mine < 2) bar.most[m3 == 0 ? 2 : m3 - 1][mine] = 0;                 // the last tile's, for the one after the next
+            ask_params(t + gridDim.x);
+            ask_token(t + 2 * gridDim.x);
+            // this thread's weight rows: kOwn outputs, or kOwn and the kOwn that they are multiplied with
+            pair_t ws[4], wo[4], p3[4], bias[4];
+            float off = 0.f, lo = 0.f, hi = 0.f;
+            #pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 c = here.col[quad * 32 + r8 + 8 * j];
+                ws[j] = make_pair(c.x, c.x); wo[j] = make_pair(c.y, c.y); p3[j] = make_pair(c.z, c.z); bias[j] = make_pair(c.w, c.w);
                 // what the terms of the affine form other than the product add up to at most, twice (they may cancel)
-                float asx = 0.f, ao = 0.f;
-                for (int r = lane; r < tile.rows; r += 32) { asx = fmaxf(asx, fabsf(rows.asx[r])); ao = fmaxf(ao, fabsf(rows.ao[r])); }
-                #pragma unroll
-                for (int d = 16; d > 0; d >>= 1) { asx = fmaxf(asx, __shfl_xor_sync(0xffffffffu, asx, d)); ao = fmaxf(ao, __shfl_xor_sync(0xffffffffu, ao, d)); }
-                off = 2.f * (asx * fabsf(col.wo) + ao * fabsf(col.p3) + fabsf(col.bias));
-                if constexpr (kGated) {
-                    off2 = __shfl_xor_sync(0xffffffffu, off, 16);
-                    if (lane >= 16) { const float x = off; off = off2; off2 = x; }
+                if constexpr (kCodes) {
+                    const float x = __uint_as_float(most[0]) * fabsf(c.y) + __uint_as_float(most[1]) * fabsf(c.z) + fabsf(c.w);
+                    off = !(x <= off) ? x : off;                                   // (a NaN stays)
                 }
-                off *= 6.8f * 1.25f * kUnit;
-                off2 *= 6.f * 1.25f * kUnit;
             }
+            if constexpr (kCodes) { lo = g.t_lo[g.n_thr == 1 ? 0 : tile.e]; hi = g.t_hi[g.n_thr == 1 ? 0 : tile.e]; off *= 2.f; }
+            const int64_t f = output_at(t, quad, r8);                              // the first of this thread's outputs
             alive = warp_wait(&bar.acc_full[ti & 1], ti >> 1);
             tc::tc_fence_after_sync();
             const uint32_t acc = tmem + (ti & 1) * acc_cols + ((uint32_t)(quad * 32) << 16);
-            for (int c0 = half * 32; alive && c0 < tile.rows; c0 += 64) {
-                constexpr int kOwn = kGated ? 8 : 16;                             // outputs of a lane in 16 tokens
-                uint32_t my_nz = 0, my_up = 0;                                    // lane x: the warp's bits of output x
-                T* out = static_cast<T*>(g.out) + (int64_t)(tile.row + c0 + (kGated ? lane >> 4 : 0)) * g.out_stride + f;
-                #pragma unroll 1
-                for (int part = 0; part < 2; ++part) {
-                    const int c = c0 + part * 16;
-                    if (c >= tile.rows) break;
-                    uint32_t v[16];
-                    tc::tmem_ld16(acc + (uint32_t)c, v);
-                    tc::tmem_ld_wait();
-                    bool near = false;
+            #pragma unroll 1
+            for (int c = half * 16; alive && c < tile.rows; c += 32) {
+                uint32_t v[2][8];                                                  // TMEM lanes r8, r8 + 8 and r8 + 16, r8 + 24
+                tc::tmem_ld_16x16(acc + (uint32_t)c, v[0]);
+                tc::tmem_ld_16x16(acc + (uint32_t)c + (16u << 16), v[1]);
+                tc::tmem_ld_wait();
+                bool near = false;
+                #pragma unroll
+                for (int a = 0; a < 2; ++a) {
+                    const int at = c + 8 * a + 2 * q4;                             // tokens at and at + 1
+                    const float2 as = *reinterpret_cast<const float2*>(&here.as[at]), sx = *reinterpret_cast<const float2*>(&here.asx[at]);
+                    const float2 ao = *reinterpret_cast<const float2*>(&here.ao[at]);
+                    const pair_t as2 = make_pair(as.x, as.y), sx2 = make_pair(sx.x, sx.y), ao2 = make_pair(ao.x, ao.y);
+                    float y[4][2];                                                 // by weight row and token
                     #pragma unroll
-                    for (int x0 = 0; x0 < kOwn; x0 += 4) {
-                        float y1[4], y2[4];
-                        auto two = [&](int i, float& a, float& b) {               // tokens c + i and c + i + 1 (i even)
-                            const float2 as = *reinterpret_cast<const float2*>(&rows.as[c + i]), sx = *reinterpret_cast<const float2*>(&rows.asx[c + i]);
-                            const float2 ao = *reinterpret_cast<const float2*>(&rows.ao[c + i]);
-                            const pair_t S = mul_pair(make_pair(as.x, as.y), make_pair(__uint_as_float(v[i]), __uint_as_float(v[i + 1])));
-                            take_pair(fma_pair(ws, S, fma_pair(wo, make_pair(sx.x, sx.y), fma_pair(p3, make_pair(ao.x, ao.y), bias))), a, b);
-                        };
-                        if constexpr (kGated) {
-                            #pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                float a, b;
-                                two(2 * (x0 + x), a, b);
-                                // lanes 0-15 take the first token of the two, 16-31 the second
-                                const float own = lane < 16 ? a : b, other = __shfl_xor_sync(0xffffffffu, lane < 16 ? b : a, 16);
-                                y1[x] = lane < 16 ? own : other;
-                                y2[x] = lane < 16 ? other : own;
-                            }
-                        } else {
-                            two(x0, y1[0], y1[1]);
-                            two(x0 + 2, y1[2], y1[3]);
-                        }
-                        float o[4] = {y1[0], y1[1], y1[2], y1[3]};
-                        if (g.act == RTN_ACT_SILU) {
-                            #pragma unroll
-                            for (int x = 0; x < 4; ++x) o[x] = fast_silu(o[x]);
-                        } else if (g.act != RTN_ACT_NONE) {
-                            const float4 a = activation4(make_float4(o[0], o[1], o[2], o[3]), g.act);
-                            o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w;
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t* S = &v[j >> 1][4 * a + 2 * (j & 1)];
+                        take_pair(fma_pair(ws[j], mul_pair(as2, make_pair(__uint_as_float(S[0]), __uint_as_float(S[1]))),
+                                           fma_pair(wo[j], sx2, fma_pair(p3[j], ao2, bias[j]))), y[j][0], y[j][1]);
+                    }
+                    float o[kOwn][2];
+                    if (g.act == RTN_ACT_SILU) {
                         #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            if constexpr (kGated) o[x] *= y2[x];
-                            if constexpr (kCodes) {
-                                // (the bound of output_of, with |y| and the other terms for what the terms add up to)
-                                constexpr float u = 1.25f * kUnit;
-                                float err = fmaf(25.f * u, fabsf(y1[x]), off);
-                                if constexpr (kGated) err = fmaf(fabsf(y2[x]), fmaf(32.f * u, fabsf(y1[x]), off), off2 * fabsf(y1[x]));
-                                const bool up = o[x] > hi, nz = up || o[x] < lo;
-                                near = near || !(fminf(fabsf(o[x] - lo), fabsf(o[x] - hi)) > err);
-                                const uint32_t a = __ballot_sync(0xffffffffu, nz), b = __ballot_sync(0xffffffffu, up);
-                                if (lane == part * kOwn + x0 + x) { my_nz = a; my_up = b; }
-                            }
-                            if (!kCodes || g.out != nullptr) {
-                                const int r = kGated ? c + 2 * (x0 + x) + (lane >> 4) : c + x0 + x;
-                                if (r < tile.rows && f < g.F) *out = from_f32<T>(o[x]);
-                                out += kGated ? 2 * g.out_stride : g.out_stride;
-                            }
+                        for (int j = 0; j < kOwn; ++j) { o[j][0] = fast_silu(y[j][0]); o[j][1] = fast_silu(y[j][1]); }
+                    } else if (g.act == RTN_ACT_NONE) {
+                        #pragma unroll
+                        for (int j = 0; j < kOwn; ++j) { o[j][0] = y[j][0]; o[j][1] = y[j][1]; }
+                    } else {
+                        #pragma unroll
+                        for (int j = 0; j < kOwn; j += 2) {
+                            const float4 x = activation4(make_float4(y[j][0], y[j][1], y[j + 1][0], y[j + 1][1]), g.act);
+                            o[j][0] = x.x; o[j][1] = x.y; o[j + 1][0] = x.z; o[j + 1][1] = x.w;
                         }
                     }
+                    if constexpr (kGated) {
+                        #pragma unroll
+                        for (int j = 0; j < kOwn; ++j) { o[j][0] *= y[kOwn + j][0]; o[j][1] *= y[kOwn + j][1]; }
+                    }
                     if constexpr (kCodes) {
-                        if (__any_sync(0xffffffffu, near && f < g.F)) {           // all of them again, in double
-                            #pragma unroll 1
-                            for (int x = 0; x < kOwn; ++x) {
-                                float S, S2 = 0.f;
-                                uint32_t q[4];
-                                tc::tmem_ld4(acc + (uint32_t)(c + (kGated ? (x & ~1) * 2 : x & ~3)), q);
-                                tc::tmem_ld_wait();
-                                int r;
-                                if constexpr (kGated) {
-                                    const float a = __uint_as_float(x & 1 ? q[2] : q[0]), b = __uint_as_float(x & 1 ? q[3] : q[1]);
-                                    const float own = lane < 16 ? a : b, other = __shfl_xor_sync(0xffffffffu, lane < 16 ? b : a, 16);
-                                    S = lane < 16 ? own : other;
-                                    S2 = lane < 16 ? other : own;
-                                    r = c + 2 * x + (lane >> 4);
+                        uint32_t nz[2][kOwn], up[2][kOwn];
+                        #pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            #pragma unroll
+                            for (int j = 0; j < kOwn; ++j) {
+                                // (the bound of output_of: |y| and the other terms for what the terms add up to; gated,
+                                // |y2| (25 |y1| + 6.8 off) + |y1| (7 |y2| + 6 off) <= (32 |y1| + 6.8 off)(|y2| + off))
+                                constexpr float u = 1.25f * kUnit;
+                                const float e = fmaf(32.f * u, fabsf(y[j][i]), 6.8f * u * off), x = o[j][i];
+                                const float err = kGated ? e * (fabsf(y[kGated ? kOwn + j : j][i]) + off) : e;
+                                const bool p = x > hi, n = p || x < lo;
+                                near = near || !(fminf(fabsf(x - lo), fabsf(x - hi)) > err);
+                                nz[i][j] = __ballot_sync(0xffffffffu, n);
+                                up[i][j] = __ballot_sync(0xffffffffu, p);
+                            }
+                        if (lane == 0) {
+                            #pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                #pragma unroll
+                                for (int j = 0; j < kOwn; j += 2) here.votes[quad][c / 4 + 2 * a + i][j / 2] = make_uint4(nz[i][j], up[i][j], nz[i][j + 1], up[i][j + 1]);
+                        }
+                    }
+                    if (!kCodes || g.out != nullptr) {
+                        #pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            if (at + i >= tile.rows) continue;
+                            T* out = static_cast<T*>(g.out) + (int64_t)(tile.row + at + i) * g.out_stride + f;
+                            if (!kCodes && vec && f + kOwn <= g.F) {
+                                if constexpr (sizeof(T) == 2) {
+                                    if constexpr (kOwn == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(o[0][i], o[1][i]), pack2<T>(o[2][i], o[3][i]));
+                                    else *reinterpret_cast<uint32_t*>(out) = pack2<T>(o[0][i], o[1][i]);
                                 } else {
-                                    S = __uint_as_float(x & 2 ? (x & 1 ? q[3] : q[2]) : (x & 1 ? q[1] : q[0]));
-                                    r = c + x;
+                                    if constexpr (kOwn == 4) *reinterpret_cast<float4*>(out) = make_float4(o[0][i], o[1][i], o[2][i], o[3][i]);
+                                    else *reinterpret_cast<float2*>(out) = make_float2(o[0][i], o[1][i]);
                                 }
-                                bool up = false, down = false;
-                                const int m = r < tile.rows ? rows.token[r] : -1;
-                                if (m >= 0 && f < g.F) {
-                                    const double e = exact_value(g, m, tile.e, f, S, S2);
-                                    up = e > (double)hi;
-                                    down = !up && e < (double)lo;
-                                }
-                                __syncwarp();
-                                const uint32_t a = __ballot_sync(0xffffffffu, up || down), b = __ballot_sync(0xffffffffu, up);
-                                if (lane == part * kOwn + x) { my_nz = a; my_up = b; }
+                            } else {
+                                #pragma unroll
+                                for (int j = 0; j < kOwn; ++j) if (f + j < g.F) out[j] = from_f32<T>(o[j][i]);
                             }
                         }
                     }
                 }
                 if constexpr (kCodes) {
-                    const int64_t f0 = (int64_t)(t % cols) * kTileOuts + quad * (kGated ? 16 : 32);
-                    const uint32_t real = g.F - f0 >= (kGated ? 16 : 32) ? 0xffffffffu : g.F <= f0 ? 0u : (1u << (uint32_t)(g.F - f0)) - 1u;     // (padding: zeros)
-                    if (lane < 2 * kOwn && f0 < width) {
-                        uint8_t* at = g.out_packed + (int64_t)(tile.row + c0) * (width / 4) + f0 / kBlockCodes * kBlockBytes + f0 % kBlockCodes / 8;
-                        #pragma unroll
-                        for (int x = 0; x < (kGated ? 2 : 1); ++x) {
-                            const int r = kGated ? 2 * lane + x : lane;
-                            if (c0 + r >= tile.rows) continue;
-                            uint8_t* w = at + (int64_t)r * (width / 4);
-                            uint32_t nz = my_nz, up = my_up;
-                            if constexpr (kGated) {
-                                nz = nz >> (16 * x) & 0xffffu & real; up = up >> (16 * x) & 0xffffu & real;
-                                *reinterpret_cast<uint16_t*>(w) = (uint16_t)nz;
-                                *reinterpret_cast<uint16_t*>(w + 16) = (uint16_t)up;
-                            } else {
-                                nz &= real; up &= real;
-                                *reinterpret_cast<uint32_t*>(w) = nz;
-                                *reinterpret_cast<uint32_t*>(w + 16) = up;
+                    if (__any_sync(0xffffffffu, near)) {                           // the 16 tokens again, in double
+                        #pragma unroll 1
+                        for (int a = 0; a < 2; ++a) {
+                            uint32_t w[2][4];
+                            tc::tmem_ld_16x8(acc + (uint32_t)(c + 8 * a), w[0]);
+                            tc::tmem_ld_16x8(acc + (uint32_t)(c + 8 * a) + (16u << 16), w[1]);
+                            tc::tmem_ld_wait();
+                            #pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int at = c + 8 * a + 2 * q4 + i, m = at < tile.rows ? here.token[at] : -1;
+                                uint32_t nz[kOwn], up[kOwn];
+                                #pragma unroll
+                                for (int j = 0; j < kOwn; ++j) {
+                                    bool p = false, n = false;
+                                    if (m >= 0 && f + j < g.F) {
+                                        const double x = exact_value(g, m, tile.e, f + j, __uint_as_float(w[j >> 1][2 * (j & 1) + i]),
+                                                                     __uint_as_float(w[1][2 * (j & 1) + i]));
+                                        p = x > (double)hi;
+                                        n = p || x < (double)lo;
+                                    }
+                                    __syncwarp();
+                                    nz[j] = __ballot_sync(0xffffffffu, n);
+                                    up[j] = __ballot_sync(0xffffffffu, p);
+                                }
+                                if (lane == 0) {
+                                    #pragma unroll
+                                    for (int j = 0; j < kOwn; j += 2) here.votes[quad][c / 4 + 2 * a + i][j / 2] = make_uint4(nz[j], up[j], nz[j + 1], up[j + 1]);
+                                }
                             }
-                            atomicAdd(&sum[c0 + r], 2 * __popc(up) - __popc(nz));
                         }
                     }
                 }
@@ -468,15 +509,50 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             tc::tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&bar.acc_empty[ti & 1]);
-            keep(next, (ti + 1) & 1);
+            m3 = m3 == 2 ? 0 : m3 + 1;
+            keep(params[(ti + 1) & 1], bar.most[m3], next_tile.rows);
             asm volatile("bar.sync 1, %0;" ::"n"(kEpilogueWarps * 32) : "memory");
             if (*dead) break;                                                     // (all of them, whichever gave up)
             if constexpr (kCodes) {
+                // a token's codes of this tile, from the votes: bit 4 r + q of vote j is output kOwn r + j of a quarter, for token 2 q + i
                 if (mine < tile.rows) {
-                    if (sum[mine] != 0) atomicAdd(&g.out_sum[tile.row + mine], sum[mine]);          // (whole numbers: any order gives the same)
-                    sum[mine] = 0;
+                    const int q = mine >> 1 & 3, slot = mine / 16 * 4 + (mine >> 3 & 1) * 2 + (mine & 1);
+                    const int64_t f0 = (int64_t)(t % cols) * kTileOuts;
+                    uint32_t nz[4], up[4];
+                    #pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint4 b0 = here.votes[w][slot][0];
+                        nz[w] = (b0.x >> q & 0x11111111u) | (b0.z >> q & 0x11111111u) << 1;
+                        up[w] = (b0.y >> q & 0x11111111u) | (b0.w >> q & 0x11111111u) << 1;
+                        if constexpr (kGated) {
+                            auto squeeze = [](uint32_t x) {                        // two bits of every four
+                                x = (x | x >> 2) & 0x0f0f0f0fu;
+                                x = (x | x >> 4) & 0x00ff00ffu;
+                                return (x | x >> 8) & 0x0000ffffu;
+                            };
+                            nz[w] = squeeze(nz[w]); up[w] = squeeze(up[w]);
+                        } else {
+                            const uint4 b1 = here.votes[w][slot][1];
+                            nz[w] |= (b1.x >> q & 0x11111111u) << 2 | (b1.z >> q & 0x11111111u) << 3;
+                            up[w] |= (b1.y >> q & 0x11111111u) << 2 | (b1.w >> q & 0x11111111u) << 3;
+                        }
+                        constexpr int kBits = kGated ? 16 : 32;                    // (padding: zeros)
+                        const int64_t n = g.F - f0 - w * kBits;
+                        if (n < kBits) { const uint32_t real = n <= 0 ? 0u : (1u << (uint32_t)n) - 1u; nz[w] &= real; up[w] &= real; }
+                    }
+                    uint8_t* to = g.out_packed + (int64_t)(tile.row + mine) * (width / 4) + f0 / kBlockCodes * kBlockBytes + f0 % kBlockCodes / 8;
+                    if constexpr (kGated) {
+                        *reinterpret_cast<uint2*>(to) = make_uint2(nz[0] | nz[1] << 16, nz[2] | nz[3] << 16);
+                        *reinterpret_cast<uint2*>(to + 16) = make_uint2(up[0] | up[1] << 16, up[2] | up[3] << 16);
+                    } else {
+                        *reinterpret_cast<uint4*>(to) = make_uint4(nz[0], nz[1], nz[2], nz[3]);
+                        *reinterpret_cast<uint4*>(to + 16) = make_uint4(up[0], up[1], up[2], up[3]);
+                    }
+                    const int sum = 2 * (__popc(up[0]) + __popc(up[1]) + __popc(up[2]) + __popc(up[3])) - (__popc(nz[0]) + __popc(nz[1]) + __popc(nz[2]) + __popc(nz[3]));
+                    if (sum != 0) atomicAdd(&g.out_sum[tile.row + mine], sum);     // (whole numbers: any order gives the same)
                 }
             }
+            tile = next_tile;
         }
     }
 
@@ -498,7 +574,7 @@ TilesPlan make_plan(const ExpertsArgs& g)
     p.k_stages = (int)((g.K + kStageCodes - 1) / kStageCodes);
     const double used = (double)(g.R < g.E ? g.R : g.E), each = (double)g.R / used, sms = device_sm_count();
     double best = 0.0;
-    for (int h = 16; h <= kMaxRows; h += 16) {
+    for (int h = 16; h <= 160; h += 16) {
         const double per = (double)(int64_t)((each + h - 1) / h), tiles = used * per * p.col_tiles, height = each / per < 16 ? 16 : each / per;
         const double stage = 2.6 * height > 350.0 ? 2.6 * height : 350.0, loop = stage * p.k_stages, out = 20.0 * height + 500.0;
         const double rounds = tiles / sms < 1.0 ? 1.0 : (double)(int64_t)((tiles + sms - 1) / sms);
@@ -506,7 +582,7 @@ TilesPlan make_plan(const ExpertsArgs& g)
         if (p.max_rows == 0 || cost < best) { best = cost; p.max_rows = h; }
     }
     p.stage_bytes = (uint32_t)p.max_rows * 128u;
-    p.ring = (uint32_t)((256 + 2 * sizeof(TokenParams) + 2 * kMaxRows * 4 + (4 * g.E + 1) * 4 + 1023) / 1024 * 1024);
+    p.ring = (uint32_t)((256 + 2 * sizeof(TileParams) + (4 * g.E + 1) * 4 + 1023) / 1024 * 1024);
     const int by_smem = (int)((227u * 1024u - p.ring) / p.stage_bytes), by_tmem = (512 - 2 * p.max_rows - (int)kScaleCols) / 32;
     p.stages = by_smem < by_tmem ? by_smem : by_tmem;
     if (p.stages > kMaxStages) p.stages = kMaxStages;

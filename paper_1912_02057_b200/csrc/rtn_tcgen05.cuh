@@ -277,6 +277,22 @@ __device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t (&v)[4])
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(taddr) : "memory");
 }
 
+// 16 TMEM lanes (taddr's: the first or the second half of a warp's 32) x 16 columns: lane l of the warp reads TMEM lanes l / 4 and l / 4 + 8,
+// columns 2 (l mod 4) and the next, of each 8 columns: v[4 a + 2 j + i] is lane l / 4 + 8 j, column 8 a + 2 (l mod 4) + i.
+__device__ __forceinline__ void tmem_ld_16x16(uint32_t taddr, uint32_t (&v)[8])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+        : "r"(taddr) : "memory");
+}
+// The same for 8 columns.
+__device__ __forceinline__ void tmem_ld_16x8(uint32_t taddr, uint32_t (&v)[4])
+{
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(taddr) : "memory");
+}
+
 // Each lane writes 8 consecutive 32-bit columns of its own TMEM lane.
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8])
 {
