@@ -3,33 +3,36 @@
 #include "rtn_tcgen05.cuh"
 #include "rtn_tensormap.cuh"
 
+#include <float.h>
+
 namespace rtn {
 
 namespace {
 
 constexpr int kExpandWarps = 8, kEpilogueWarps = 8;             // two of each for every quarter of the lanes
-constexpr int kLoadWarp = kExpandWarps + kEpilogueWarps, kMmaWarp = kLoadWarp + 1;
-constexpr int kThreads = (kMmaWarp + 1) * 32;
-constexpr int kStageCodes = 256;                                // codes of K in a stage: a 128-byte row of 4-bit values, 32 columns
+constexpr int kLoadWarp = kExpandWarps + kEpilogueWarps, kMmaWarp = kLoadWarp + 1, kParamWarp = kMmaWarp + 1, kCodeWarp = kParamWarp + 1;
+constexpr int kThreads = (kCodeWarp + 1) * 32;
+// A stage holds 256 codes of K: a 128-byte row of 4-bit values to an input, 32 columns of tensor memory to a weight row.
 constexpr int kMaxRows = 192;                                   // of a tile
-constexpr int kMaxStages = 6;
-constexpr int kBoxRows = 16;                                    // of a copy
+constexpr int kMaxStages = 6, kMaxSpans = 8;
+constexpr uint32_t kSpanBytes = 128 * 128;                       // 512 codes of 128 weight rows, as planes
 constexpr uint32_t kTries = 1u << 20;
+constexpr uint32_t kSmemBytes = 227 * 1024;
 constexpr uint32_t kScaleCols = 16;
 
 struct TilesPlan {
     int max_rows;               // of a tile, a multiple of 16
-    int stages;
+    int stages, spans;          // slots of the two rings
     int col_tiles;
     int k_stages;
-    uint32_t ring;              // offset of the ring in shared memory
+    int box_rows;               // of a copy
+    uint32_t ring, planes;      // offsets of the rings in shared memory
     uint32_t stage_bytes;
     uint32_t smem;
 };
 
 struct Bars {
-    uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
-    uint32_t most[3][2];        // the largest |a_s S_x| and |a_o| of a tile, the next and the one after it, as bit patterns
+    uint64_t full[kMaxStages], empty[kMaxStages], planes_full[kMaxSpans], planes_empty[kMaxSpans], acc_full[2], acc_empty[2], params_full[2], params_empty[2], votes_full[2];
     uint32_t tmem_slot;
     int dead;
 };
@@ -40,6 +43,7 @@ struct TileParams {
     float as[kMaxRows], asx[kMaxRows], ao[kMaxRows];
     int token[kMaxRows];
     float4 col[128];
+    float most_asx, most_ao, pad[2];                            // the largest |a_s S_x| and |a_o|
     uint4 votes[4][kMaxRows / 4][2];
 };
 
@@ -75,43 +79,57 @@ __device__ __forceinline__ void mma_mxf4(uint32_t elected, uint32_t d, uint32_t 
         ::"r"(d), "r"(a), "l"(b_desc), "r"(idesc), "r"(scales), "r"((uint32_t)accumulate), "r"(elected) : "memory");
 }
 
-// kBoxRows rows of a [rows][pitch bytes] tensor from row r on, 128 bytes of each from byte x on, under the 128-byte swizzle.
+// box_rows rows of a [rows][pitch bytes] tensor from row r on, 128 bytes of each from byte x on, under the 128-byte swizzle.
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int x, int r, uint64_t* bar)
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(r), "r"(tc::smem_addr(bar)) : "memory");
 }
 
+// Order of a row's codes in K, the same for both operands: what lets four lanes that read a row's planes side by side (16 bytes of each plane
+// to a lane) hold whole fragments of a store to tensor memory.  A span is four blocks of 128 codes, or the last two; it is expanded in stages of 32 words (256 codes).
+// A lane q has 8 words w of a stage, and word w is at 8 (w / 2) + 2 q + w % 2.
+//   four blocks: lane q has block q; words 0-3 and 4-7 of stage h come from the block's plane words 2 h and 2 h + 1
+//   two blocks:  lane q has plane words 2 (q % 2) and the next of block q / 2
+__host__ __device__ __forceinline__ int stages_of(int nblk) { return nblk / 4 * 2 + (nblk % 4 + 1) / 2; }
+
 // The experts' rows one after the other as 4-bit values, `pitch` bytes each (a row's end is zeros); and the sums of their codes begin at 0.
 __global__ void __launch_bounds__(256)
-expand_inputs_kernel(const __grid_constant__ ExpertsArgs g, int nblk, int chunks, uint4* __restrict__ out)
+expand_inputs_kernel(const __grid_constant__ ExpertsArgs g, int nblk, int chunks, uint2* __restrict__ out)
 {
     tc::pdl_trigger();
     const uint32_t i = blockIdx.x * 256u + threadIdx.x;
-    const uint32_t row = i / (uint32_t)chunks, c = i % (uint32_t)chunks;
+    const uint32_t row = i / (uint32_t)chunks, c = i % (uint32_t)chunks;          // a chunk: 32 codes, four words
     if (row >= g.R || row < (uint32_t)g.start[0] || row >= (uint32_t)g.start[g.E]) return;
     if (c == 0 && g.out_sum != nullptr) g.out_sum[row] = 0;
     const int64_t m = g.tokens != nullptr ? g.tokens[row] : row;
+    const int stage = (int)(c / 8), q = (int)(c % 4), part = (int)(c % 8) / 4;    // this lane's words 4 part .. 4 part + 3 of the stage
+    const bool four = stage / 2 * 4 + 2 < nblk;
+    const int block = stage / 2 * 4 + (four ? q : q / 2), word = four ? stage % 2 * 2 + part : q % 2 * 2 + part;
     uint32_t nz = 0, pos = 0;
-    if ((int)(c / 4) < nblk && m >= 0 && m < g.T) {
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(g.a_packed) + (m * nblk + c / 4) * 8 + c % 4;
+    if (block < nblk && m >= 0 && m < g.T) {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(g.a_packed) + (m * nblk + block) * 8 + word;
         nz = p[0]; pos = p[4];
     }
-    out[(int64_t)row * chunks + c] = expand_input(nz, pos);
+    const uint4 w = expand_input(nz, pos);
+    uint2* to = out + ((int64_t)row * chunks + stage * 8) * 2 + part * 8 + q;
+    to[0] = make_uint2(w.x, w.y);
+    to[4] = make_uint2(w.z, w.w);
 }
 
 template <typename T, bool kGated, bool kCodes>
 __global__ void __launch_bounds__(kThreads, 1)
-experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constant__ CUtensorMap map, const __grid_constant__ TilesPlan p)
+experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap weight_map,
+                     const __grid_constant__ TilesPlan p)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     Bars& bar = *reinterpret_cast<Bars*>(smem);
-    TileParams* params = reinterpret_cast<TileParams*>(smem + 256);              // [2]
+    TileParams* params = reinterpret_cast<TileParams*>(smem + 512);              // [2]
     int* before = reinterpret_cast<int*>(params + 2);                            // [E + 1] tiles before an expert's
     int* first = before + g.E + 1;                                               // [E] its first row
     int* count = first + g.E;                                                    // [E] its rows
     int* height = count + g.E;                                                   // [E] rows of its tiles
-    static_assert(sizeof(Bars) <= 256, "barriers");
+    static_assert(sizeof(Bars) <= 512, "barriers");
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     volatile int* dead = &bar.dead;
     const uint32_t ring = tc::smem_addr(smem) + p.ring;
@@ -119,7 +137,11 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
     if (warp == kMmaWarp) tc::tmem_alloc(&bar.tmem_slot, 512);
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.stages; ++i) { tc::mbar_init(&bar.full[i], 5); tc::mbar_init(&bar.empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { tc::mbar_init(&bar.acc_full[i], 1); tc::mbar_init(&bar.acc_empty[i], kEpilogueWarps); }
+        for (int i = 0; i < p.spans; ++i) { tc::mbar_init(&bar.planes_full[i], 1); tc::mbar_init(&bar.planes_empty[i], 4); }
+        for (int i = 0; i < 2; ++i) {
+            tc::mbar_init(&bar.acc_full[i], 1); tc::mbar_init(&bar.acc_empty[i], kEpilogueWarps);
+            tc::mbar_init(&bar.params_full[i], 1); tc::mbar_init(&bar.params_empty[i], 1); tc::mbar_init(&bar.votes_full[i], kEpilogueWarps);
+        }
         tc::mbar_init_fence();
         bar.dead = 0;
     }
@@ -150,7 +172,6 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         }
         if (lane == 0) before[g.E] = sum;
     }
-    if (threadIdx.x < 6) bar.most[threadIdx.x / 2][threadIdx.x % 2] = 0;
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
@@ -169,30 +190,33 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
 
     // Tiles go round the CTAs with the columns fastest: those at work at a time share their rows.
     const uint32_t cols = (uint32_t)p.col_tiles, total = (uint32_t)before[g.E] * cols;
-    auto find = [&](uint32_t t) {                                                 // whole warp
+    int seen = 0;                                                                 // this warp's last expert: tiles only go up
+    auto find_from = [&](uint32_t t, int& seen) {                                 // whole warp
         const int rt = (int)(t / cols);
         Tile r{0, 0, 0, 16};
-        for (int e0 = 0; e0 < g.E; e0 += 32) {
-            const int e = e0 + lane;
-            const uint32_t who = __ballot_sync(0xffffffffu, e < g.E && before[e] <= rt && rt < before[e + 1]);
-            if (who != 0) {
-                r.e = e0 + __ffs(who) - 1;
-                r.height = height[r.e];
-                const int at = (rt - before[r.e]) * r.height, left = count[r.e] - at;
-                r.row = first[r.e] + at;
-                r.rows = left < r.height ? left : r.height;
-                break;
-            }
+        for (; seen < g.E; seen += 32) {
+            const int e = seen + lane;
+            const uint32_t who = __ballot_sync(0xffffffffu, e < g.E && rt < before[e + 1]);
+            if (who != 0) { seen += __ffs(who) - 1; break; }
         }
+        if (seen >= g.E) return r;
+        r.e = seen;
+        r.height = height[seen];
+        const int at = (rt - before[seen]) * r.height, left = count[seen] - at;
+        r.row = first[seen] + at;
+        r.rows = left < r.height ? left : r.height;
         return r;
     };
+    auto find = [&](uint32_t t) { return find_from(t, seen); };
     auto warp_wait = [&](uint64_t* m, uint32_t parity) {
         const bool ok = __all_sync(0xffffffffu, tc::mbar_wait_tries(m, parity & 1u, kTries)) != 0;
         if (!ok) *dead = 1;
         return ok;
     };
     const int quad = warp & 3;
-    const int64_t nblk = (g.K + kBlockCodes - 1) / kBlockCodes;
+    const int nblk = (int)((g.K + kBlockCodes - 1) / kBlockCodes), spans = (nblk + 3) / 4;
+    const bool short_last = nblk % 4 == 1 || nblk % 4 == 2;
+    auto stages_in = [&](int span) { return span == spans - 1 && short_last ? 1 : 2; };
     constexpr int kTileOuts = kGated ? 64 : 128;
     // The output that TMEM lane 32 q + l belongs to, so that the lanes r, r + 8, ... which one thread of the epilogue reads are adjacent outputs; gated,
     // lanes l >= 16 are the rows that those of l - 16 are multiplied with.
@@ -202,80 +226,111 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
     bool alive = true;
 
     if (warp < kExpandWarps) {
-        // ------------------------------------------------------------ weights: a team of four warps has every other stage
-        const uint4* __restrict__ W = reinterpret_cast<const uint4*>(g.w_packed);
-        uint4 next[4];
-        uint32_t t = blockIdx.x;                                                  // the stage that `next` is of
-        int k = warp >> 2, left = 0;                                              // blocks of the row from this stage on
-        const uint4* src = nullptr;
-        auto enter = [&]() {                                                      // stage k of tile t, or k - k_stages of the next, ...
-            bool moved = src == nullptr;
-            while (k >= p.k_stages && t < total) { k -= p.k_stages; t += gridDim.x; moved = true; }
-            if (moved && t < total) {
-                const int64_t f = output_at(t, quad, lane), e = find(t).e;
-                src = W;
-                left = 0;
-                if (f < g.F) {
-                    src = W + ((e * g.N + (kGated && lane >= 16 ? g.F + f : f)) * nblk + 2 * k) * 2;
-                    left = (int)nblk - 2 * k;
+        // ------------------------------------------------------------ weights: two teams of four warps have the spans in turn
+        const int row4 = lane >> 2, q4 = lane & 3;
+        const uint32_t mine = blockIdx.x < total ? (total - 1 - blockIdx.x) / gridDim.x + 1 : 0, n_spans = mine * (uint32_t)spans;
+        int k = warp >> 2, sp = k;                                                // span of a tile, its slot
+        while (k >= spans) k -= spans;
+        if (sp >= p.spans) sp -= p.spans;
+        uint32_t planes_phase = 0, phase = 0;
+        // Slots of the expanded codes go round as well; a span takes two, the last of a row perhaps one.
+        int s = 0;
+        auto skip = [&](int n) { s += n; if (s >= p.stages) { s -= p.stages; phase ^= 1; } };
+        if (warp >= 4) skip(stages_in(0));
+        for (uint32_t n = (uint32_t)warp >> 2; n < n_spans && alive; n += 2) {
+            const int stages = stages_in(k);
+            if (!(alive = warp_wait(&bar.planes_full[sp], planes_phase))) break;
+            uint4 nz[4], pos[4];                                                  // TMEM lanes row4 + 8 j of the quarter, this lane's part of the span
+            const uint8_t* from = smem + p.planes + (uint32_t)sp * kSpanBytes;
+            const int block = 4 * k + 2 < nblk ? q4 : q4 >> 1;
+            #pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = kGated ? (j >> 1) * 64 + quad * 16 + 2 * row4 + (j & 1) : quad * 32 + 4 * row4 + j;
+                nz[j] = *reinterpret_cast<const uint4*>(from + row * 128 + (((2 * block) ^ (row & 7)) << 4));
+                pos[j] = *reinterpret_cast<const uint4*>(from + row * 128 + (((2 * block + 1) ^ (row & 7)) << 4));
+            }
+            if (stages == 1) {                                                    // the last two blocks: this lane's half of one
+                #pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (q4 & 1) { nz[j].x = nz[j].z; nz[j].y = nz[j].w; pos[j].x = pos[j].z; pos[j].y = pos[j].w; }
+            }
+            #pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (h >= stages) break;
+                uint32_t o[2][16];
+                #pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint4 a = h == 0 ? expand_weight(nz[j].x, pos[j].x) : expand_weight(nz[j].z, pos[j].z);
+                    const uint4 b = h == 0 ? expand_weight(nz[j].y, pos[j].y) : expand_weight(nz[j].w, pos[j].w);
+                    uint32_t* to = o[j >> 1] + 2 * (j & 1);
+                    to[0] = a.x; to[1] = a.y; to[4] = a.z; to[5] = a.w; to[8] = b.x; to[9] = b.y; to[12] = b.z; to[13] = b.w;
                 }
+                if (h == 0) {                                                     // (the planes are in registers)
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&bar.planes_empty[sp]);
+                }
+                if (!(alive = warp_wait(&bar.empty[s], phase + 1))) break;
+                const uint32_t at = a_tmem + (uint32_t)(s * 32) + ((uint32_t)(quad * 32) << 16);
+                tc::tmem_st_16x32(at, o[0]);
+                tc::tmem_st_16x32(at + (16u << 16), o[1]);
+                tc::tmem_st_wait();
+                tc::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&bar.full[s]);
+                skip(1);
             }
-        };
-        auto fetch = [&]() {
-            #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                next[2 * i] = next[2 * i + 1] = make_uint4(0, 0, 0, 0);
-                if (i < left) { next[2 * i] = __ldg(src + 2 * i); next[2 * i + 1] = __ldg(src + 2 * i + 1); }
-            }
-        };
-        enter();
-        if (t < total) fetch();
-        int s = warp >> 2;
-        uint32_t phase = 0;
-        while (t < total) {
-            // expanded before the slot is free: what follows the wait is the store alone
-            uint32_t o[2][16];
-            #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint4 c0 = expand_weight(next[2 * i].x, next[2 * i + 1].x), c1 = expand_weight(next[2 * i].y, next[2 * i + 1].y);
-                const uint4 c2 = expand_weight(next[2 * i].z, next[2 * i + 1].z), c3 = expand_weight(next[2 * i].w, next[2 * i + 1].w);
-                o[i][0] = c0.x; o[i][1] = c0.y; o[i][2] = c0.z; o[i][3] = c0.w; o[i][4] = c1.x; o[i][5] = c1.y; o[i][6] = c1.z; o[i][7] = c1.w;
-                o[i][8] = c2.x; o[i][9] = c2.y; o[i][10] = c2.z; o[i][11] = c2.w; o[i][12] = c3.x; o[i][13] = c3.y; o[i][14] = c3.z; o[i][15] = c3.w;
-            }
-            k += 2; src += 8; left -= 4;
-            enter();
-            if (t < total) fetch();
-            if (!warp_wait(&bar.empty[s], phase + 1)) break;
-            const uint32_t at = a_tmem + (uint32_t)(s * 32) + ((uint32_t)(quad * 32) << 16);
-            tc::tmem_st16(at, o[0]);
-            tc::tmem_st16(at + 16u, o[1]);
-            tc::tmem_st_wait();
-            tc::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&bar.full[s]);
-            s += 2;
-            if (s >= p.stages) { s -= p.stages; phase ^= 1; }
+            skip(stages_in(k + 1 == spans ? 0 : k + 1));
+            k += 2;
+            while (k >= spans) k -= spans;
+            sp += 2;
+            if (sp >= p.spans) { sp -= p.spans; planes_phase ^= 1; }
         }
     } else if (warp == kLoadWarp) {
-        // ------------------------------------------------------------ input rows: a lane has 16 of them
+        // ------------------------------------------------------------ copies of planes, and of input rows (a copy takes some 60 clocks to issue: few large ones)
+        int seen_planes = 0, kp = 0, sp = 0;
+        uint32_t tp = blockIdx.x, planes_phase = 0;
+        int64_t weight_row = -1;
+        auto copy_planes = [&]() {                                                // the next span's
+            if (tp >= total) return true;
+            if (weight_row < 0) weight_row = (int64_t)find_from(tp, seen_planes).e * g.N + (int64_t)(tp % cols) * kTileOuts;
+            if (!warp_wait(&bar.planes_empty[sp], planes_phase + 1)) return false;
+            if (lane == 0) tc::mbar_arrive_expect_tx(&bar.planes_full[sp], kSpanBytes);
+            __syncwarp();
+            const uint32_t dst = ring - p.ring + p.planes + (uint32_t)sp * kSpanBytes;
+            if (lane < (kGated ? 2 : 1))                                          // (rows of other outputs behind the last, zeros behind the last row)
+                load_box(dst + (uint32_t)lane * (kSpanBytes / 2), &weight_map, kp * 128, (int)(weight_row + (lane ? g.F : 0)), &bar.planes_full[sp]);
+            if (++kp == spans) { kp = 0; tp += gridDim.x; weight_row = -1; }
+            if (++sp == p.spans) { sp = 0; planes_phase ^= 1; }
+            return true;
+        };
+        for (int i = 0; i < p.spans - 2; ++i) copy_planes();
         tc::pdl_wait();
+        const uint32_t box_bytes = (uint32_t)p.box_rows * 128u;
         int s = 0;
         uint32_t phase = 0;
         for (uint32_t t = blockIdx.x; t < total && alive; t += gridDim.x) {
             const Tile tile = find(t);
-            for (int k = 0; k < p.k_stages; ++k) {
-                if (!(alive = warp_wait(&bar.empty[s], phase + 1))) break;
-                if (lane == 0) tc::mbar_arrive_expect_tx(&bar.full[s], (uint32_t)tile.height * 128u);
-                __syncwarp();
-                if (lane * kBoxRows < tile.height)
-                    load_box(ring + (uint32_t)s * p.stage_bytes + (uint32_t)lane * (kBoxRows * 128u), &map, k * 128, tile.row + lane * kBoxRows, &bar.full[s]);
-                if (++s == p.stages) { s = 0; phase ^= 1; }
+            const int boxes = (tile.height + p.box_rows - 1) / p.box_rows;        // (what lies behind the tile's rows belongs to no output)
+            int x = 0;
+            for (int k = 0; k < spans && alive; ++k) {
+                if (!(alive = copy_planes())) break;
+                for (int h = stages_in(k); h > 0; --h, x += 128) {
+                    if (!(alive = warp_wait(&bar.empty[s], phase + 1))) break;
+                    if (lane == 0) tc::mbar_arrive_expect_tx(&bar.full[s], (uint32_t)boxes * box_bytes);
+                    __syncwarp();
+                    if (lane < boxes) load_box(ring + (uint32_t)s * p.stage_bytes + (uint32_t)lane * box_bytes, &map, x, tile.row + lane * p.box_rows, &bar.full[s]);
+                    if (++s == p.stages) { s = 0; phase ^= 1; }
+                }
             }
         }
-        // nobody leaves while copies are on their way: the last of each stage
+        // nobody leaves while copies are on their way: the last of each slot
         for (int i = 0; i < p.stages; ++i) {
-            const uint32_t uses = i < s ? phase + 1 : phase;                      // parity of the number of copies to this stage
+            const uint32_t uses = i < s ? phase + 1 : phase;                      // parity of the number of copies to this slot
             tc::mbar_wait_tries(&bar.full[i], (uses + 1) & 1u, kTries);
+        }
+        for (int i = 0; i < p.spans; ++i) {
+            const uint32_t uses = i < sp ? planes_phase + 1 : planes_phase;
+            tc::mbar_wait_tries(&bar.planes_full[i], (uses + 1) & 1u, kTries);
         }
     } else if (warp == kMmaWarp) {
         // ------------------------------------------------------------ products
@@ -301,78 +356,129 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             if (elected && alive) tc::mma_commit(&bar.acc_full[ti & 1]);
             __syncwarp();
         }
+    } else if (warp == kParamWarp) {
+        // ------------------------------------------------------------ parameters of a tile's tokens and weight rows
+        uint32_t ti = 0;
+        for (uint32_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
+            constexpr int kEach = kMaxRows / 32;
+            const Tile tile = find(t);
+            int64_t m[kEach];
+            #pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int r = lane + 32 * i;
+                m[i] = r >= tile.rows ? -1 : g.tokens != nullptr ? g.tokens[tile.row + r] : tile.row + r;
+            }
+            float ws[4], wo[4], bias[4];
+            int sw[4];
+            bool real[4];
+            #pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t f = output_at(t, i, lane), at = (int64_t)tile.e * g.N + (kGated && lane >= 16 ? g.F + f : f), w = g.ep.n_wparam == 1 ? 0 : at;
+                real[i] = f < g.F;
+                ws[i] = wo[i] = bias[i] = 0.f; sw[i] = 0;
+                if (real[i]) { ws[i] = g.ep.w_scale[w]; wo[i] = g.ep.w_offset[w]; sw[i] = g.w_sum[at]; if (g.bias != nullptr) bias[i] = g.bias[at]; }
+            }
+            float as[kEach], ao[kEach];
+            int sx[kEach];
+            bool bad = false;
+            #pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                as[i] = ao[i] = 0.f; sx[i] = 0;
+                if (lane + 32 * i < tile.rows) {
+                    if (m[i] >= 0 && m[i] < g.T) {
+                        const int64_t at = g.ep.n_aparam == 1 ? 0 : m[i];
+                        as[i] = g.ep.a_scale[at]; ao[i] = g.ep.a_offset[at]; sx[i] = g.a_sum[m[i]];
+                    } else { as[i] = ao[i] = __int_as_float(0x7fffffff); m[i] = -1; bad = true; }
+                }
+            }
+            if (bad && t % cols == 0) atomicOr(g.status, kStatusBadIndex);
+            if (!(alive = warp_wait(&bar.params_empty[ti & 1], (ti >> 1) + 1))) break;
+            TileParams& here = params[ti & 1];
+            uint32_t most_asx = 0, most_ao = 0;                                   // bit patterns: a NaN is the largest
+            #pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int r = lane + 32 * i;
+                const float asx = as[i] * (float)sx[i];
+                here.as[r] = as[i]; here.asx[r] = asx; here.ao[r] = ao[i]; here.token[r] = (int)m[i];
+                most_asx = max(most_asx, __float_as_uint(fabsf(asx))); most_ao = max(most_ao, __float_as_uint(fabsf(ao[i])));
+            }
+            #pragma unroll
+            for (int i = 0; i < 4; ++i)
+                here.col[i * 32 + lane] = make_float4(ws[i], wo[i], real[i] ? (float)((double)ws[i] * (double)sw[i] + (double)g.K * (double)wo[i]) : 0.f, bias[i]);
+            most_asx = __reduce_max_sync(0xffffffffu, most_asx); most_ao = __reduce_max_sync(0xffffffffu, most_ao);
+            if (lane == 0) { here.most_asx = __uint_as_float(most_asx); here.most_ao = __uint_as_float(most_ao); }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&bar.params_full[ti & 1]);
+        }
+    } else if (warp == kCodeWarp) {
+        // ------------------------------------------------------------ a token's codes of a tile, put together from the votes
+        tc::pdl_wait();
+        uint32_t ti = 0;
+        for (uint32_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
+            const Tile tile = find(t);
+            if (!(alive = warp_wait(&bar.votes_full[ti & 1], ti >> 1))) break;
+            if constexpr (kCodes) {
+                const TileParams& here = params[ti & 1];
+                const int64_t f0 = (int64_t)(t % cols) * kTileOuts, width = (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes;
+                #pragma unroll 2
+                for (int r = lane; r < tile.rows; r += 32) {
+                    // bit 4 i + q of vote j is output kOwn i + j of a quarter, for token 2 q or the one after it
+                    const int q = r >> 1 & 3, slot = r / 16 * 4 + (r >> 3 & 1) * 2 + (r & 1);
+                    uint32_t nz[4], up[4];
+                    #pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint4 b0 = here.votes[w][slot][0];
+                        nz[w] = (b0.x >> q & 0x11111111u) | (b0.z >> q & 0x11111111u) << 1;
+                        up[w] = (b0.y >> q & 0x11111111u) | (b0.w >> q & 0x11111111u) << 1;
+                        if constexpr (kGated) {
+                            auto squeeze = [](uint32_t x) {                        // two bits of every four
+                                x = (x | x >> 2) & 0x0f0f0f0fu;
+                                x = (x | x >> 4) & 0x00ff00ffu;
+                                return (x | x >> 8) & 0x0000ffffu;
+                            };
+                            nz[w] = squeeze(nz[w]); up[w] = squeeze(up[w]);
+                        } else {
+                            const uint4 b1 = here.votes[w][slot][1];
+                            nz[w] |= (b1.x >> q & 0x11111111u) << 2 | (b1.z >> q & 0x11111111u) << 3;
+                            up[w] |= (b1.y >> q & 0x11111111u) << 2 | (b1.w >> q & 0x11111111u) << 3;
+                        }
+                        constexpr int kBits = kGated ? 16 : 32;                    // (padding: zeros)
+                        const int64_t n = g.F - f0 - w * kBits;
+                        if (n < kBits) { const uint32_t real = n <= 0 ? 0u : (1u << (uint32_t)n) - 1u; nz[w] &= real; up[w] &= real; }
+                    }
+                    uint8_t* to = g.out_packed + (int64_t)(tile.row + r) * (width / 4) + f0 / kBlockCodes * kBlockBytes + f0 % kBlockCodes / 8;
+                    if constexpr (kGated) {
+                        *reinterpret_cast<uint2*>(to) = make_uint2(nz[0] | nz[1] << 16, nz[2] | nz[3] << 16);
+                        *reinterpret_cast<uint2*>(to + 16) = make_uint2(up[0] | up[1] << 16, up[2] | up[3] << 16);
+                    } else {
+                        *reinterpret_cast<uint4*>(to) = make_uint4(nz[0], nz[1], nz[2], nz[3]);
+                        *reinterpret_cast<uint4*>(to + 16) = make_uint4(up[0], up[1], up[2], up[3]);
+                    }
+                    const int sum = 2 * (__popc(up[0]) + __popc(up[1]) + __popc(up[2]) + __popc(up[3])) - (__popc(nz[0]) + __popc(nz[1]) + __popc(nz[2]) + __popc(nz[3]));
+                    if (sum != 0) atomicAdd(&g.out_sum[tile.row + r], sum);        // (whole numbers: any order gives the same)
+                }
+                __syncwarp();
+            }
+            if (lane == 0) tc::mbar_arrive(&bar.params_empty[ti & 1]);
+        }
     } else {
         // ------------------------------------------------------------ write out: a warp has a quarter of the lanes and every other 16 tokens; a thread
         // kOwn adjacent outputs of two tokens in each 8.
         constexpr int kOwn = kGated ? 2 : 4;
-        const int mine = threadIdx.x - kExpandWarps * 32, half = (warp - kExpandWarps) >> 2, r8 = lane >> 2, q4 = lane & 3;
-        // Parameters of the tile after this one, asked for as they are and looked at when this one is done: of token `mine`, of TMEM lane `mine`.
-        struct Raw { int token; float as, ao, ws, wo, bias; int sx, sw; bool col; };
-        Raw raw{};
-        int token_ahead = -1;
-        Tile tile_ahead{};
-        auto ask_token = [&](uint32_t t) {                                        // input row of token `mine` of tile t, a tile ahead of its parameters
-            token_ahead = -1;
-            if (t >= total) return;
-            tile_ahead = find(t);
-            if (mine < tile_ahead.rows) token_ahead = g.tokens != nullptr ? g.tokens[tile_ahead.row + mine] : tile_ahead.row + mine;
-        };
-        auto ask_params = [&](uint32_t t) {                                       // after ask_token(t)
-            raw.token = -1; raw.col = false;
-            if (t >= total) return;
-            if (mine < tile_ahead.rows) {
-                const int64_t m = token_ahead;
-                if (m >= 0 && m < g.T) {
-                    const int64_t i = g.ep.n_aparam == 1 ? 0 : m;
-                    raw.token = (int)m; raw.as = g.ep.a_scale[i]; raw.ao = g.ep.a_offset[i]; raw.sx = g.a_sum[m];
-                } else if (t % cols == 0) atomicOr(g.status, kStatusBadIndex);
-            }
-            if (mine < 128) {
-                const int64_t f = output_at(t, mine >> 5, mine & 31);
-                if (f < g.F) {
-                    const int64_t at = (int64_t)tile_ahead.e * g.N + (kGated && (mine & 16) ? g.F + f : f), i = g.ep.n_wparam == 1 ? 0 : at;
-                    raw.col = true; raw.ws = g.ep.w_scale[i]; raw.wo = g.ep.w_offset[i]; raw.sw = g.w_sum[at];
-                    raw.bias = g.bias != nullptr ? g.bias[at] : 0.f;
-                }
-            }
-        };
-        auto keep = [&](TileParams& q, uint32_t (&most)[2], int rows) {
-            if (mine < kMaxRows) {
-                const float nan = __int_as_float(0x7fffffff);
-                float as = 0.f, asx = 0.f, ao = 0.f;
-                if (mine < rows) {
-                    as = raw.token >= 0 ? raw.as : nan; ao = raw.token >= 0 ? raw.ao : nan;
-                    asx = raw.token >= 0 ? raw.as * (float)raw.sx : nan;
-                }
-                q.as[mine] = as; q.asx[mine] = asx; q.ao[mine] = ao; q.token[mine] = raw.token;
-                if constexpr (kCodes) {
-                    const uint32_t a = __reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(asx))), b = __reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(ao)));
-                    if (lane == 0) { atomicMax(&most[0], a); atomicMax(&most[1], b); }
-                }
-            }
-            if (mine < 128) {
-                ColParams c{0.f, 0.f, 0.f, 0.f};
-                if (raw.col) c = ColParams{raw.ws, raw.wo, (float)((double)raw.ws * (double)raw.sw + (double)g.K * (double)raw.wo), raw.bias};
-                q.col[mine] = make_float4(c.ws, c.wo, c.p3, c.bias);
-            }
-        };
-        ask_token(blockIdx.x);
-        ask_params(blockIdx.x);
-        Tile tile = tile_ahead;
-        keep(params[0], bar.most[0], tile.rows);
-        ask_token(blockIdx.x + gridDim.x);
-        asm volatile("bar.sync 1, %0;" ::"n"(kEpilogueWarps * 32) : "memory");
+        const int half = (warp - kExpandWarps) >> 2, r8 = lane >> 2, q4 = lane & 3;
         tc::pdl_wait();
-        const int64_t width = (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes;
         const bool vec = kCodes || ((reinterpret_cast<uintptr_t>(g.out) % (kOwn * sizeof(T))) == 0 && g.out_stride % kOwn == 0);
-        uint32_t ti = 0, m3 = 0;
+        // Units of an output's error for its value before the activation: the affine form's own (below), passed on with a slope of at most
+        // 1.13, and the activation's.
+        const float units = g.act == RTN_ACT_SILU ? 8.3f : g.act == RTN_ACT_NONE || g.act == RTN_ACT_RELU ? 2.f : 18.3f;
+        const float c1 = (units + (kGated ? 3.f : 0.f)) * 1.1f * kUnit;
+        uint32_t ti = 0;
+        Tile next{};
+        if (blockIdx.x < total) next = find(blockIdx.x);
         for (uint32_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
-            const uint32_t(&most)[2] = bar.most[m3];
+            const Tile tile = next;
             TileParams& here = params[ti & 1];
-            const Tile next_tile = tile_ahead;
-            if (mine < 2) bar.most[m3 == 0 ? 2 : m3 - 1][mine] = 0;                 // the last tile's, for the one after the next
-            ask_params(t + gridDim.x);
-            ask_token(t + 2 * gridDim.x);
+            if (!(alive = warp_wait(&bar.params_full[ti & 1], ti >> 1))) break;
             // this thread's weight rows: kOwn outputs, or kOwn and the kOwn that they are multiplied with
             pair_t ws[4], wo[4], p3[4], bias[4];
             float off = 0.f, lo = 0.f, hi = 0.f;
@@ -380,19 +486,25 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             for (int j = 0; j < 4; ++j) {
                 const float4 c = here.col[quad * 32 + r8 + 8 * j];
                 ws[j] = make_pair(c.x, c.x); wo[j] = make_pair(c.y, c.y); p3[j] = make_pair(c.z, c.z); bias[j] = make_pair(c.w, c.w);
-                // what the terms of the affine form other than the product add up to at most, twice (they may cancel)
+                // what the terms of the affine form other than the product add up to at most
                 if constexpr (kCodes) {
-                    const float x = __uint_as_float(most[0]) * fabsf(c.y) + __uint_as_float(most[1]) * fabsf(c.z) + fabsf(c.w);
+                    const float x = here.most_asx * fabsf(c.y) + here.most_ao * fabsf(c.z) + fabsf(c.w);
                     off = !(x <= off) ? x : off;                                   // (a NaN stays)
                 }
             }
-            if constexpr (kCodes) { lo = g.t_lo[g.n_thr == 1 ? 0 : tile.e]; hi = g.t_hi[g.n_thr == 1 ? 0 : tile.e]; off *= 2.f; }
+            // y = w_s (a_s S) + P with P = w_o a_s S_x + (p3 a_o + bias): u (2 |y| + 4 off) covers its roundings (those of a_s S, a_s S_x and p3, and
+            // three sums).  Gated, with |activation| <= |y1|:
+            //   |y2| (units |y1| + 4.6 off) + |y1| (2 |y2| + 4 off) + |y1 y2| <= ((units + 3) |y1| + 4.6 off) (|y2| + 0.8 off)
+            float c0 = 0.f, c2 = 0.f;
+            if constexpr (kCodes) { lo = g.t_lo[g.n_thr == 1 ? 0 : tile.e]; hi = g.t_hi[g.n_thr == 1 ? 0 : tile.e]; c0 = 4.6f * 1.1f * kUnit * off; c2 = 0.8f * off; }
+            if (!kGated && g.act == RTN_ACT_RELU && lo <= 0.f) lo = -FLT_MAX;        // (never below it: a threshold of 0 is not near)
             const int64_t f = output_at(t, quad, r8);                              // the first of this thread's outputs
-            alive = warp_wait(&bar.acc_full[ti & 1], ti >> 1);
+            if (t + gridDim.x < total) next = find(t + gridDim.x);
+            if (!(alive = warp_wait(&bar.acc_full[ti & 1], ti >> 1))) break;
             tc::tc_fence_after_sync();
             const uint32_t acc = tmem + (ti & 1) * acc_cols + ((uint32_t)(quad * 32) << 16);
             #pragma unroll 1
-            for (int c = half * 16; alive && c < tile.rows; c += 32) {
+            for (int c = half * 16; c < tile.rows; c += 32) {
                 uint32_t v[2][8];                                                  // TMEM lanes r8, r8 + 8 and r8 + 16, r8 + 24
                 tc::tmem_ld_16x16(acc + (uint32_t)c, v[0]);
                 tc::tmem_ld_16x16(acc + (uint32_t)c + (16u << 16), v[1]);
@@ -435,11 +547,8 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                         for (int i = 0; i < 2; ++i)
                             #pragma unroll
                             for (int j = 0; j < kOwn; ++j) {
-                                // (the bound of output_of: |y| and the other terms for what the terms add up to; gated,
-                                // |y2| (25 |y1| + 6.8 off) + |y1| (7 |y2| + 6 off) <= (32 |y1| + 6.8 off)(|y2| + off))
-                                constexpr float u = 1.25f * kUnit;
-                                const float e = fmaf(32.f * u, fabsf(y[j][i]), 6.8f * u * off), x = o[j][i];
-                                const float err = kGated ? e * (fabsf(y[kGated ? kOwn + j : j][i]) + off) : e;
+                                const float e = fmaf(c1, fabsf(y[j][i]), c0), x = o[j][i];
+                                const float err = kGated ? e * (fabsf(y[kGated ? kOwn + j : j][i]) + c2) : e;
                                 const bool p = x > hi, n = p || x < lo;
                                 near = near || !(fminf(fabsf(x - lo), fabsf(x - hi)) > err);
                                 nz[i][j] = __ballot_sync(0xffffffffu, n);
@@ -473,25 +582,38 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                     }
                 }
                 if constexpr (kCodes) {
-                    if (__any_sync(0xffffffffu, near)) {                           // the 16 tokens again, in double
+                    if (__any_sync(0xffffffffu, near)) {                           // the 16 tokens again, those too near in double
                         #pragma unroll 1
                         for (int a = 0; a < 2; ++a) {
                             uint32_t w[2][4];
                             tc::tmem_ld_16x8(acc + (uint32_t)(c + 8 * a), w[0]);
                             tc::tmem_ld_16x8(acc + (uint32_t)(c + 8 * a) + (16u << 16), w[1]);
                             tc::tmem_ld_wait();
-                            #pragma unroll
+                            #pragma unroll 1
                             for (int i = 0; i < 2; ++i) {
                                 const int at = c + 8 * a + 2 * q4 + i, m = at < tile.rows ? here.token[at] : -1;
+                                const RowParams row{here.as[at], here.ao[at], 0.f, m};
                                 uint32_t nz[kOwn], up[kOwn];
                                 #pragma unroll
                                 for (int j = 0; j < kOwn; ++j) {
-                                    bool p = false, n = false;
-                                    if (m >= 0 && f + j < g.F) {
-                                        const double x = exact_value(g, m, tile.e, f + j, __uint_as_float(w[j >> 1][2 * (j & 1) + i]),
-                                                                     __uint_as_float(w[1][2 * (j & 1) + i]));
-                                        p = x > (double)hi;
-                                        n = p || x < (double)lo;
+                                    const float S = __uint_as_float(i ? w[j >> 1][2 * (j & 1) + 1] : w[j >> 1][2 * (j & 1)]);
+                                    const float S2 = __uint_as_float(i ? w[1][2 * (j & 1) + 1] : w[1][2 * (j & 1)]);
+                                    const float asx = here.asx[at];
+                                    auto value = [&](int k, float sum) {
+                                        const float4 q = here.col[quad * 32 + r8 + 8 * k];
+                                        return fmaf(q.x, row.as * sum, fmaf(q.y, asx, fmaf(q.z, row.ao, q.w)));
+                                    };
+                                    const float y1 = value(j, S), y2 = kGated ? value(kGated ? kOwn + j : j, S2) : 1.f;
+                                    const float act = g.act == RTN_ACT_SILU ? fast_silu(y1) : g.act == RTN_ACT_NONE ? y1 : activation(y1, g.act);
+                                    const float x = kGated ? act * y2 : act, e = fmaf(c1, fabsf(y1), c0), err = kGated ? e * (fabsf(y2) + c2) : e;
+                                    bool p = x > hi, n = p || x < lo;
+                                    if (!(fminf(fabsf(x - lo), fabsf(x - hi)) > err)) {
+                                        p = n = false;
+                                        if (m >= 0 && f + j < g.F) {
+                                            const double d = exact_value(g, m, tile.e, f + j, S, S2);
+                                            p = d > (double)hi;
+                                            n = p || d < (double)lo;
+                                        }
                                     }
                                     __syncwarp();
                                     nz[j] = __ballot_sync(0xffffffffu, n);
@@ -508,55 +630,10 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             }
             tc::tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&bar.acc_empty[ti & 1]);
-            m3 = m3 == 2 ? 0 : m3 + 1;
-            keep(params[(ti + 1) & 1], bar.most[m3], next_tile.rows);
-            asm volatile("bar.sync 1, %0;" ::"n"(kEpilogueWarps * 32) : "memory");
-            if (*dead) break;                                                     // (all of them, whichever gave up)
-            if constexpr (kCodes) {
-                // a token's codes of this tile, from the votes: bit 4 r + q of vote j is output kOwn r + j of a quarter, for token 2 q + i
-                if (mine < tile.rows) {
-                    const int q = mine >> 1 & 3, slot = mine / 16 * 4 + (mine >> 3 & 1) * 2 + (mine & 1);
-                    const int64_t f0 = (int64_t)(t % cols) * kTileOuts;
-                    uint32_t nz[4], up[4];
-                    #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const uint4 b0 = here.votes[w][slot][0];
-                        nz[w] = (b0.x >> q & 0x11111111u) | (b0.z >> q & 0x11111111u) << 1;
-                        up[w] = (b0.y >> q & 0x11111111u) | (b0.w >> q & 0x11111111u) << 1;
-                        if constexpr (kGated) {
-                            auto squeeze = [](uint32_t x) {                        // two bits of every four
-                                x = (x | x >> 2) & 0x0f0f0f0fu;
-                                x = (x | x >> 4) & 0x00ff00ffu;
-                                return (x | x >> 8) & 0x0000ffffu;
-                            };
-                            nz[w] = squeeze(nz[w]); up[w] = squeeze(up[w]);
-                        } else {
-                            const uint4 b1 = here.votes[w][slot][1];
-                            nz[w] |= (b1.x >> q & 0x11111111u) << 2 | (b1.z >> q & 0x11111111u) << 3;
-                            up[w] |= (b1.y >> q & 0x11111111u) << 2 | (b1.w >> q & 0x11111111u) << 3;
-                        }
-                        constexpr int kBits = kGated ? 16 : 32;                    // (padding: zeros)
-                        const int64_t n = g.F - f0 - w * kBits;
-                        if (n < kBits) { const uint32_t real = n <= 0 ? 0u : (1u << (uint32_t)n) - 1u; nz[w] &= real; up[w] &= real; }
-                    }
-                    uint8_t* to = g.out_packed + (int64_t)(tile.row + mine) * (width / 4) + f0 / kBlockCodes * kBlockBytes + f0 % kBlockCodes / 8;
-                    if constexpr (kGated) {
-                        *reinterpret_cast<uint2*>(to) = make_uint2(nz[0] | nz[1] << 16, nz[2] | nz[3] << 16);
-                        *reinterpret_cast<uint2*>(to + 16) = make_uint2(up[0] | up[1] << 16, up[2] | up[3] << 16);
-                    } else {
-                        *reinterpret_cast<uint4*>(to) = make_uint4(nz[0], nz[1], nz[2], nz[3]);
-                        *reinterpret_cast<uint4*>(to + 16) = make_uint4(up[0], up[1], up[2], up[3]);
-                    }
-                    const int sum = 2 * (__popc(up[0]) + __popc(up[1]) + __popc(up[2]) + __popc(up[3])) - (__popc(nz[0]) + __popc(nz[1]) + __popc(nz[2]) + __popc(nz[3]));
-                    if (sum != 0) atomicAdd(&g.out_sum[tile.row + mine], sum);     // (whole numbers: any order gives the same)
-                }
-            }
-            tile = next_tile;
+            if (lane == 0) { tc::mbar_arrive(&bar.acc_empty[ti & 1]); tc::mbar_arrive(&bar.votes_full[ti & 1]); }
         }
     }
 
-    if (!alive) *dead = 1;
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
@@ -571,7 +648,7 @@ TilesPlan make_plan(const ExpertsArgs& g)
     const int outs = g.gated ? 64 : 128;
     const int64_t width = g.out_packed != nullptr ? (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes : g.F;
     p.col_tiles = (int)((width + outs - 1) / outs);
-    p.k_stages = (int)((g.K + kStageCodes - 1) / kStageCodes);
+    p.k_stages = stages_of((int)((g.K + kBlockCodes - 1) / kBlockCodes));
     const double used = (double)(g.R < g.E ? g.R : g.E), each = (double)g.R / used, sms = device_sm_count();
     double best = 0.0;
     for (int h = 16; h <= 160; h += 16) {
@@ -581,12 +658,16 @@ TilesPlan make_plan(const ExpertsArgs& g)
         const double cost = rounds * (loop > out ? loop : out) + (loop > out ? out : loop);
         if (p.max_rows == 0 || cost < best) { best = cost; p.max_rows = h; }
     }
-    p.stage_bytes = (uint32_t)p.max_rows * 128u;
-    p.ring = (uint32_t)((256 + 2 * sizeof(TileParams) + (4 * g.E + 1) * 4 + 1023) / 1024 * 1024);
-    const int by_smem = (int)((227u * 1024u - p.ring) / p.stage_bytes), by_tmem = (512 - 2 * p.max_rows - (int)kScaleCols) / 32;
-    p.stages = by_smem < by_tmem ? by_smem : by_tmem;
-    if (p.stages > kMaxStages) p.stages = kMaxStages;
-    p.smem = p.ring + (uint32_t)p.stages * p.stage_bytes;
+    p.box_rows = p.max_rows > 64 ? (p.max_rows + 31) / 32 * 16 : p.max_rows;          // two to a tile, or one
+    p.stage_bytes = (uint32_t)((p.max_rows + p.box_rows - 1) / p.box_rows * p.box_rows) * 128u;
+    p.ring = (uint32_t)((512 + 2 * sizeof(TileParams) + (4 * g.E + 1) * 4 + 1023) / 1024 * 1024);
+    const int by_tmem = (512 - 2 * p.max_rows - (int)kScaleCols) / 32;
+    p.stages = by_tmem < kMaxStages ? by_tmem : kMaxStages;
+    while (p.stages > 3 && p.ring + (uint32_t)p.stages * p.stage_bytes + 4 * kSpanBytes > kSmemBytes) --p.stages;
+    p.planes = p.ring + (uint32_t)p.stages * p.stage_bytes;                      // (a multiple of 1024: stages are multiples of 2048 bytes)
+    p.spans = (int)((kSmemBytes - p.planes) / kSpanBytes);
+    if (p.spans > kMaxSpans) p.spans = kMaxSpans;
+    p.smem = p.planes + (uint32_t)p.spans * kSpanBytes;
     return p;
 }
 
@@ -601,14 +682,18 @@ cudaError_t launch_experts_tiles(const ExpertsArgs& g, cudaStream_t s)
     void* scratch = nullptr;
     cudaError_t e = scratch_alloc(&scratch, (size_t)g.R * pitch, s);
     if (e != cudaSuccess) return e;
-    CUtensorMap map;
+    CUtensorMap map, weight_map;
     const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)g.R}, strides[1] = {(cuuint64_t)pitch};
-    const cuuint32_t box[2] = {128, kBoxRows}, unit[2] = {1, 1};
+    const cuuint32_t box[2] = {128, (cuuint32_t)p.box_rows}, unit[2] = {1, 1};
     if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, scratch, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) e = cudaErrorInvalidValue;
+    const cuuint64_t wdims[2] = {(cuuint64_t)nblk * kBlockBytes, (cuuint64_t)g.E * (cuuint64_t)g.N}, wstrides[1] = {(cuuint64_t)nblk * kBlockBytes};
+    const cuuint32_t wbox[2] = {128, g.gated ? 64u : 128u};
+    if (encode(&weight_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(g.w_packed), wdims, wstrides, wbox, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) e = cudaErrorInvalidValue;
     if (e == cudaSuccess) {
         const int64_t threads = g.R * (pitch / 16);
-        expand_inputs_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(g, nblk, pitch / 16, static_cast<uint4*>(scratch));
+        expand_inputs_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(g, nblk, pitch / 16, static_cast<uint2*>(scratch));
         e = cudaGetLastError();
     }
     if (e == cudaSuccess) {
@@ -617,7 +702,7 @@ cudaError_t launch_experts_tiles(const ExpertsArgs& g, cudaStream_t s)
             auto run = [&](auto kernel) {
                 cudaError_t x = allow_shared_memory(kernel);
                 if (x != cudaSuccess) return x;
-                return launch_pdl(kernel, dim3((unsigned)device_sm_count()), dim3(kThreads), p.smem, s, g, map, p);
+                return launch_pdl(kernel, dim3((unsigned)device_sm_count()), dim3(kThreads), p.smem, s, g, map, weight_map, p);
             };
             if (g.out_packed != nullptr) return g.gated ? run(experts_tiles_kernel<T, true, true>) : run(experts_tiles_kernel<T, false, true>);
             return g.gated ? run(experts_tiles_kernel<T, true, false>) : run(experts_tiles_kernel<T, false, false>);
@@ -630,7 +715,7 @@ cudaError_t launch_experts_tiles(const ExpertsArgs& g, cudaStream_t s)
 // What the tensor-core form counts in 32 bits.
 bool experts_tiles_supported(const ExpertsArgs& g)
 {
-    const int64_t pitch = (g.K + kStageCodes - 1) / kStageCodes * 8, cols = (g.F + 191) / 64 + 1;
+    const int64_t pitch = (g.K + 255) / 256 * 8, cols = (g.F + 191) / 64 + 1;
     return g.R * pitch < (int64_t(1) << 32) - 256 && (g.R / 16 + g.E) * cols < (int64_t(1) << 31);
 }
 
