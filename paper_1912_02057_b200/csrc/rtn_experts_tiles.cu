@@ -9,9 +9,15 @@ namespace rtn {
 
 namespace {
 
-constexpr int kExpandWarps = 8, kEpilogueWarps = 8;             // two of each for every quarter of the lanes
-constexpr int kLoadWarp = kExpandWarps + kEpilogueWarps, kMmaWarp = kLoadWarp + 1, kParamWarp = kMmaWarp + 1, kCodeWarp = kParamWarp + 1;
-constexpr int kThreads = (kCodeWarp + 1) * 32;
+// Warps: two groups of four expand weights, two write out (a warp of each for every quarter of the lanes), the fifth copies and issues the products, the
+// sixth has what a tile begins and ends with.  Registers a thread by group; what they add up to is what the block is launched with.
+constexpr int kExpandWarps = 8, kEpilogueWarps = 8, kEdgeWarps = 4;
+constexpr int kLoadWarp = kExpandWarps + kEpilogueWarps, kPlanesWarp = kLoadWarp + 1, kMmaWarp = kLoadWarp + 2, kEdgeWarp = kLoadWarp + 4;
+constexpr int kThreads = (kEdgeWarp + kEdgeWarps) * 32;
+constexpr int kLaunchRegs = 80, kExpandRegs = 88, kEpilogueRegs = 112, kIssueRegs = 24, kEdgeRegs = 56;
+static_assert(kThreads == 768 && 2 * kExpandRegs + 2 * kEpilogueRegs + kIssueRegs + kEdgeRegs <= 6 * kLaunchRegs, "registers");
+template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
 // A stage holds 256 codes of K: a 128-byte row of 4-bit values to an input, 32 columns of tensor memory to a weight row.
 constexpr int kMaxRows = 192;                                   // of a tile
 constexpr int kMaxStages = 6, kMaxSpans = 8;
@@ -32,7 +38,7 @@ struct TilesPlan {
 };
 
 struct Bars {
-    uint64_t full[kMaxStages], empty[kMaxStages], planes_full[kMaxSpans], planes_empty[kMaxSpans], acc_full[2], acc_empty[2], params_full[2], params_empty[2], votes_full[2];
+    uint64_t full[kMaxStages], empty[kMaxStages], planes_full[kMaxSpans], planes_empty[kMaxSpans], acc_full[2], acc_empty[2], params_full[2], votes_full[2];
     uint32_t tmem_slot;
     int dead;
 };
@@ -43,7 +49,7 @@ struct TileParams {
     float as[kMaxRows], asx[kMaxRows], ao[kMaxRows];
     int token[kMaxRows];
     float4 col[128];
-    float most_asx, most_ao, pad[2];                            // the largest |a_s S_x| and |a_o|
+    uint4 most_asx, most_ao;                                    // the largest |a_s S_x| and |a_o|, in four parts, as bit patterns (a NaN is the largest)
     uint4 votes[4][kMaxRows / 4][2];
 };
 
@@ -140,7 +146,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         for (int i = 0; i < p.spans; ++i) { tc::mbar_init(&bar.planes_full[i], 1); tc::mbar_init(&bar.planes_empty[i], 4); }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&bar.acc_full[i], 1); tc::mbar_init(&bar.acc_empty[i], kEpilogueWarps);
-            tc::mbar_init(&bar.params_full[i], 1); tc::mbar_init(&bar.params_empty[i], 1); tc::mbar_init(&bar.votes_full[i], kEpilogueWarps);
+            tc::mbar_init(&bar.params_full[i], kEdgeWarps); tc::mbar_init(&bar.votes_full[i], kEpilogueWarps);
         }
         tc::mbar_init_fence();
         bar.dead = 0;
@@ -227,6 +233,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
 
     if (warp < kExpandWarps) {
         // ------------------------------------------------------------ weights: two teams of four warps have the spans in turn
+        more_registers<kExpandRegs>();
         const int row4 = lane >> 2, q4 = lane & 3;
         const uint32_t mine = blockIdx.x < total ? (total - 1 - blockIdx.x) / gridDim.x + 1 : 0, n_spans = mine * (uint32_t)spans;
         int k = warp >> 2, sp = k;                                                // span of a tile, its slot
@@ -285,54 +292,67 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             sp += 2;
             if (sp >= p.spans) { sp -= p.spans; planes_phase ^= 1; }
         }
-    } else if (warp == kLoadWarp) {
-        // ------------------------------------------------------------ copies of planes, and of input rows (a copy takes some 60 clocks to issue: few large ones)
-        int seen_planes = 0, kp = 0, sp = 0;
-        uint32_t tp = blockIdx.x, planes_phase = 0;
-        int64_t weight_row = -1;
-        auto copy_planes = [&]() {                                                // the next span's
-            if (tp >= total) return true;
-            if (weight_row < 0) weight_row = (int64_t)find_from(tp, seen_planes).e * g.N + (int64_t)(tp % cols) * kTileOuts;
-            if (!warp_wait(&bar.planes_empty[sp], planes_phase + 1)) return false;
-            if (lane == 0) tc::mbar_arrive_expect_tx(&bar.planes_full[sp], kSpanBytes);
-            __syncwarp();
-            const uint32_t dst = ring - p.ring + p.planes + (uint32_t)sp * kSpanBytes;
-            if (lane < (kGated ? 2 : 1))                                          // (rows of other outputs behind the last, zeros behind the last row)
-                load_box(dst + (uint32_t)lane * (kSpanBytes / 2), &weight_map, kp * 128, (int)(weight_row + (lane ? g.F : 0)), &bar.planes_full[sp]);
-            if (++kp == spans) { kp = 0; tp += gridDim.x; weight_row = -1; }
-            if (++sp == p.spans) { sp = 0; planes_phase ^= 1; }
-            return true;
-        };
-        for (int i = 0; i < p.spans - 2; ++i) copy_planes();
-        tc::pdl_wait();
-        const uint32_t box_bytes = (uint32_t)p.box_rows * 128u;
-        int s = 0;
-        uint32_t phase = 0;
-        for (uint32_t t = blockIdx.x; t < total && alive; t += gridDim.x) {
-            const Tile tile = find(t);
-            const int boxes = (tile.height + p.box_rows - 1) / p.box_rows;        // (what lies behind the tile's rows belongs to no output)
-            int x = 0;
-            for (int k = 0; k < spans && alive; ++k) {
-                if (!(alive = copy_planes())) break;
-                for (int h = stages_in(k); h > 0; --h, x += 128) {
-                    if (!(alive = warp_wait(&bar.empty[s], phase + 1))) break;
-                    if (lane == 0) tc::mbar_arrive_expect_tx(&bar.full[s], (uint32_t)boxes * box_bytes);
-                    __syncwarp();
-                    if (lane < boxes) load_box(ring + (uint32_t)s * p.stage_bytes + (uint32_t)lane * box_bytes, &map, x, tile.row + lane * p.box_rows, &bar.full[s]);
+    } else if (warp >= kLoadWarp && warp < kEdgeWarp) {
+      fewer_registers<kIssueRegs>();
+      // Tile t's row tile for one thread.
+      auto find_one = [&](uint32_t t) {
+          const int rt = (int)(t / cols);
+          while (rt >= before[seen + 1]) ++seen;
+          return rt - before[seen];
+      };
+      auto wait = [&](uint64_t* m, uint32_t parity) {
+          if (tc::mbar_wait_tries(m, parity & 1u, kTries)) return true;
+          *dead = 1;
+          return false;
+      };
+      if (warp == kLoadWarp) {
+        // ------------------------------------------------------------ copies of input rows (one takes some 60 clocks to issue: few and large)
+        if (lane == 0) {
+            tc::pdl_wait();
+            const uint32_t box_bytes = (uint32_t)p.box_rows * 128u;
+            int s = 0;
+            uint32_t phase = 0;
+            for (uint32_t t = blockIdx.x; t < total && alive; t += gridDim.x) {
+                const int at = find_one(t), h = height[seen], row = first[seen] + at * h;
+                const int boxes = (h + p.box_rows - 1) / p.box_rows;              // (what lies behind the tile's rows belongs to no output)
+                for (int k = 0; k < p.k_stages; ++k) {
+                    if (!(alive = wait(&bar.empty[s], phase + 1))) break;
+                    tc::mbar_arrive_expect_tx(&bar.full[s], (uint32_t)boxes * box_bytes);
+                    const uint32_t dst = ring + (uint32_t)s * p.stage_bytes;
+                    load_box(dst, &map, k * 128, row, &bar.full[s]);
+                    if (boxes > 1) load_box(dst + box_bytes, &map, k * 128, row + p.box_rows, &bar.full[s]);
                     if (++s == p.stages) { s = 0; phase ^= 1; }
                 }
             }
+            // nobody leaves while copies are on their way: the last of each slot
+            for (int i = 0; i < p.stages; ++i) {
+                const uint32_t uses = i < s ? phase + 1 : phase;                  // parity of the number of copies to this slot
+                tc::mbar_wait_tries(&bar.full[i], (uses + 1) & 1u, kTries);
+            }
         }
-        // nobody leaves while copies are on their way: the last of each slot
-        for (int i = 0; i < p.stages; ++i) {
-            const uint32_t uses = i < s ? phase + 1 : phase;                      // parity of the number of copies to this slot
-            tc::mbar_wait_tries(&bar.full[i], (uses + 1) & 1u, kTries);
+      } else if (warp == kPlanesWarp) {
+        // ------------------------------------------------------------ copies of planes
+        if (lane == 0) {
+            int s = 0;
+            uint32_t phase = 0;
+            for (uint32_t t = blockIdx.x; t < total && alive; t += gridDim.x) {
+                find_one(t);
+                const int row = (int)((int64_t)seen * g.N + (int64_t)(t % cols) * kTileOuts);
+                for (int k = 0; k < spans; ++k) {
+                    if (!(alive = wait(&bar.planes_empty[s], phase + 1))) break;
+                    tc::mbar_arrive_expect_tx(&bar.planes_full[s], kSpanBytes);
+                    const uint32_t dst = ring - p.ring + p.planes + (uint32_t)s * kSpanBytes;
+                    load_box(dst, &weight_map, k * 128, row, &bar.planes_full[s]);                          // (rows of other outputs behind the last,
+                    if (kGated) load_box(dst + kSpanBytes / 2, &weight_map, k * 128, row + (int)g.F, &bar.planes_full[s]);          // zeros behind the last row)
+                    if (++s == p.spans) { s = 0; phase ^= 1; }
+                }
+            }
+            for (int i = 0; i < p.spans; ++i) {
+                const uint32_t uses = i < s ? phase + 1 : phase;
+                tc::mbar_wait_tries(&bar.planes_full[i], (uses + 1) & 1u, kTries);
+            }
         }
-        for (int i = 0; i < p.spans; ++i) {
-            const uint32_t uses = i < sp ? planes_phase + 1 : planes_phase;
-            tc::mbar_wait_tries(&bar.planes_full[i], (uses + 1) & 1u, kTries);
-        }
-    } else if (warp == kMmaWarp) {
+      } else if (warp == kMmaWarp) {
         // ------------------------------------------------------------ products
         const uint32_t elected = tc::elect_one();
         const uint64_t desc = tc::smem_desc_sw128(ring, 0);
@@ -356,72 +376,84 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             if (elected && alive) tc::mma_commit(&bar.acc_full[ti & 1]);
             __syncwarp();
         }
-    } else if (warp == kParamWarp) {
-        // ------------------------------------------------------------ parameters of a tile's tokens and weight rows
-        uint32_t ti = 0;
-        for (uint32_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
-            constexpr int kEach = kMaxRows / 32;
+      }
+      __syncwarp();
+    } else if (warp >= kEdgeWarp) {
+        // ------------------------------------------------------------ what a tile begins with, parameters of its tokens and weight rows, and ends with, its
+        // codes put together from the votes: a quarter of each to a warp.  Parameters are asked for a tile ahead, input rows two ahead (with
+        // both asked for and waited for in a tile's turn, that took 4000 clocks, longer than its products).
+        fewer_registers<kEdgeRegs>();
+        constexpr int kEach = (kMaxRows + 127) / 128;
+        const int part = warp - kEdgeWarp;
+        int m[kEach], m_next[kEach];                                              // -1: out of range, -2: no such row
+        float ws = 0.f, wo = 0.f, bias = 0.f, as[kEach], ao[kEach];
+        int sw = 0, sx[kEach], seen_params = 0;
+        auto row_of = [&](int i) { return lane + 32 * (part + 4 * i); };
+        auto ask_rows = [&](uint32_t t) {
+            #pragma unroll
+            for (int i = 0; i < kEach; ++i) m_next[i] = -2;
+            if (t >= total) return;
             const Tile tile = find(t);
-            int64_t m[kEach];
+            #pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (row_of(i) < tile.rows) m_next[i] = g.tokens != nullptr ? __ldg(g.tokens + tile.row + row_of(i)) : tile.row + row_of(i);
+        };
+        auto ask_params = [&](uint32_t t) {
+            if (t >= total) return;
+            const int64_t first_row = (int64_t)find_from(t, seen_params).e * g.N;
             #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const int r = lane + 32 * i;
-                m[i] = r >= tile.rows ? -1 : g.tokens != nullptr ? g.tokens[tile.row + r] : tile.row + r;
+                m[i] = m_next[i];
+                as[i] = ao[i] = 0.f; sx[i] = 0;
+                if (m[i] != -2) {
+                    const bool ok = m[i] >= 0 && m[i] < g.T;
+                    const int64_t in = ok ? m[i] : 0, at = g.ep.n_aparam == 1 ? 0 : in;
+                    as[i] = __ldg(g.ep.a_scale + at); ao[i] = __ldg(g.ep.a_offset + at); sx[i] = __ldg(g.a_sum + in);
+                    if (!ok) m[i] = -1;
+                }
             }
-            float ws[4], wo[4], bias[4];
-            int sw[4];
-            bool real[4];
-            #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t f = output_at(t, i, lane), at = (int64_t)tile.e * g.N + (kGated && lane >= 16 ? g.F + f : f), w = g.ep.n_wparam == 1 ? 0 : at;
-                real[i] = f < g.F;
-                ws[i] = wo[i] = bias[i] = 0.f; sw[i] = 0;
-                if (real[i]) { ws[i] = g.ep.w_scale[w]; wo[i] = g.ep.w_offset[w]; sw[i] = g.w_sum[at]; if (g.bias != nullptr) bias[i] = g.bias[at]; }
-            }
-            float as[kEach], ao[kEach];
-            int sx[kEach];
+            const int64_t f = output_at(t, part, lane), at = first_row + (kGated && lane >= 16 ? g.F + f : f), w = g.ep.n_wparam == 1 ? 0 : at;
+            ws = wo = bias = 0.f; sw = 0;
+            if (f < g.F) { ws = __ldg(g.ep.w_scale + w); wo = __ldg(g.ep.w_offset + w); sw = __ldg(g.w_sum + at); if (g.bias != nullptr) bias = __ldg(g.bias + at); }
+        };
+        auto tell = [&](uint32_t t, uint32_t at) {                                // the parameters of tile t, and asks for those of the next
+            if (t >= total) return;
+            TileParams& here = params[at];
+            uint32_t most_asx = 0, most_ao = 0;
             bool bad = false;
             #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                as[i] = ao[i] = 0.f; sx[i] = 0;
-                if (lane + 32 * i < tile.rows) {
-                    if (m[i] >= 0 && m[i] < g.T) {
-                        const int64_t at = g.ep.n_aparam == 1 ? 0 : m[i];
-                        as[i] = g.ep.a_scale[at]; ao[i] = g.ep.a_offset[at]; sx[i] = g.a_sum[m[i]];
-                    } else { as[i] = ao[i] = __int_as_float(0x7fffffff); m[i] = -1; bad = true; }
-                }
-            }
-            if (bad && t % cols == 0) atomicOr(g.status, kStatusBadIndex);
-            if (!(alive = warp_wait(&bar.params_empty[ti & 1], (ti >> 1) + 1))) break;
-            TileParams& here = params[ti & 1];
-            uint32_t most_asx = 0, most_ao = 0;                                   // bit patterns: a NaN is the largest
-            #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const int r = lane + 32 * i;
+                const int r = row_of(i);
+                if (m[i] == -1) { as[i] = ao[i] = __int_as_float(0x7fffffff); bad = true; }
                 const float asx = as[i] * (float)sx[i];
-                here.as[r] = as[i]; here.asx[r] = asx; here.ao[r] = ao[i]; here.token[r] = (int)m[i];
+                if (r < kMaxRows) { here.as[r] = as[i]; here.asx[r] = asx; here.ao[r] = ao[i]; here.token[r] = m[i]; }
                 most_asx = max(most_asx, __float_as_uint(fabsf(asx))); most_ao = max(most_ao, __float_as_uint(fabsf(ao[i])));
             }
-            #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                here.col[i * 32 + lane] = make_float4(ws[i], wo[i], real[i] ? (float)((double)ws[i] * (double)sw[i] + (double)g.K * (double)wo[i]) : 0.f, bias[i]);
+            here.col[part * 32 + lane] = make_float4(ws, wo, (float)((double)ws * (double)sw + (double)g.K * (double)wo), bias);
             most_asx = __reduce_max_sync(0xffffffffu, most_asx); most_ao = __reduce_max_sync(0xffffffffu, most_ao);
-            if (lane == 0) { here.most_asx = __uint_as_float(most_asx); here.most_ao = __uint_as_float(most_ao); }
+            if (lane == 0) { (&here.most_asx.x)[part] = most_asx; (&here.most_ao.x)[part] = most_ao; }
+            if (bad && t % cols == 0) atomicOr(g.status, kStatusBadIndex);
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&bar.params_full[ti & 1]);
-        }
-    } else if (warp == kCodeWarp) {
-        // ------------------------------------------------------------ a token's codes of a tile, put together from the votes
+            if (lane == 0) tc::mbar_arrive(&bar.params_full[at]);
+            ask_params(t + gridDim.x);
+            ask_rows(t + 2 * gridDim.x);
+        };
+        ask_rows(blockIdx.x);
+        ask_params(blockIdx.x);
+        ask_rows(blockIdx.x + gridDim.x);
+        tell(blockIdx.x, 0);
+        tell(blockIdx.x + gridDim.x, 1);
         tc::pdl_wait();
         uint32_t ti = 0;
+        int seen_codes = 0;
         for (uint32_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
-            const Tile tile = find(t);
+            const Tile tile = find_from(t, seen_codes);
             if (!(alive = warp_wait(&bar.votes_full[ti & 1], ti >> 1))) break;
             if constexpr (kCodes) {
                 const TileParams& here = params[ti & 1];
                 const int64_t f0 = (int64_t)(t % cols) * kTileOuts, width = (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes;
-                #pragma unroll 2
-                for (int r = lane; r < tile.rows; r += 32) {
+                #pragma unroll 1
+                for (int r = lane + 32 * part; r < tile.rows; r += 32 * kEdgeWarps) {
                     // bit 4 i + q of vote j is output kOwn i + j of a quarter, for token 2 q or the one after it
                     const int q = r >> 1 & 3, slot = r / 16 * 4 + (r >> 3 & 1) * 2 + (r & 1);
                     uint32_t nz[4], up[4];
@@ -459,11 +491,12 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                 }
                 __syncwarp();
             }
-            if (lane == 0) tc::mbar_arrive(&bar.params_empty[ti & 1]);
+            tell(t + 2 * gridDim.x, ti & 1);                                      // (the votes have been read, and so have the parameters, before they were cast)
         }
     } else {
         // ------------------------------------------------------------ write out: a warp has a quarter of the lanes and every other 16 tokens; a thread
         // kOwn adjacent outputs of two tokens in each 8.
+        more_registers<kEpilogueRegs>();
         constexpr int kOwn = kGated ? 2 : 4;
         const int half = (warp - kExpandWarps) >> 2, r8 = lane >> 2, q4 = lane & 3;
         tc::pdl_wait();
@@ -481,14 +514,19 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             if (!(alive = warp_wait(&bar.params_full[ti & 1], ti >> 1))) break;
             // this thread's weight rows: kOwn outputs, or kOwn and the kOwn that they are multiplied with
             pair_t ws[4], wo[4], p3[4], bias[4];
-            float off = 0.f, lo = 0.f, hi = 0.f;
+            float off = 0.f, lo = 0.f, hi = 0.f, most_asx = 0.f, most_ao = 0.f;
+            if constexpr (kCodes) {
+                const uint4 a = here.most_asx, b = here.most_ao;
+                most_asx = __uint_as_float(max(max(a.x, a.y), max(a.z, a.w)));
+                most_ao = __uint_as_float(max(max(b.x, b.y), max(b.z, b.w)));
+            }
             #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float4 c = here.col[quad * 32 + r8 + 8 * j];
                 ws[j] = make_pair(c.x, c.x); wo[j] = make_pair(c.y, c.y); p3[j] = make_pair(c.z, c.z); bias[j] = make_pair(c.w, c.w);
                 // what the terms of the affine form other than the product add up to at most
                 if constexpr (kCodes) {
-                    const float x = here.most_asx * fabsf(c.y) + here.most_ao * fabsf(c.z) + fabsf(c.w);
+                    const float x = most_asx * fabsf(c.y) + most_ao * fabsf(c.z) + fabsf(c.w);
                     off = !(x <= off) ? x : off;                                   // (a NaN stays)
                 }
             }
@@ -509,37 +547,42 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                 tc::tmem_ld_16x16(acc + (uint32_t)c, v[0]);
                 tc::tmem_ld_16x16(acc + (uint32_t)c + (16u << 16), v[1]);
                 tc::tmem_ld_wait();
+                // the 16 tokens in steps of their own, so that each has many independent values: affine forms, activations, codes
                 bool near = false;
+                float y[2][4][2], o[2][kOwn][2];                                   // by group of 8 tokens, weight row and token
                 #pragma unroll
                 for (int a = 0; a < 2; ++a) {
                     const int at = c + 8 * a + 2 * q4;                             // tokens at and at + 1
                     const float2 as = *reinterpret_cast<const float2*>(&here.as[at]), sx = *reinterpret_cast<const float2*>(&here.asx[at]);
                     const float2 ao = *reinterpret_cast<const float2*>(&here.ao[at]);
                     const pair_t as2 = make_pair(as.x, as.y), sx2 = make_pair(sx.x, sx.y), ao2 = make_pair(ao.x, ao.y);
-                    float y[4][2];                                                 // by weight row and token
                     #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const uint32_t* S = &v[j >> 1][4 * a + 2 * (j & 1)];
                         take_pair(fma_pair(ws[j], mul_pair(as2, make_pair(__uint_as_float(S[0]), __uint_as_float(S[1]))),
-                                           fma_pair(wo[j], sx2, fma_pair(p3[j], ao2, bias[j]))), y[j][0], y[j][1]);
+                                           fma_pair(wo[j], sx2, fma_pair(p3[j], ao2, bias[j]))), y[a][j][0], y[a][j][1]);
                     }
-                    float o[kOwn][2];
-                    if (g.act == RTN_ACT_SILU) {
+                }
+                if (g.act == RTN_ACT_SILU) {
+                    #pragma unroll
+                    for (int a = 0; a < 2; ++a)
                         #pragma unroll
-                        for (int j = 0; j < kOwn; ++j) { o[j][0] = fast_silu(y[j][0]); o[j][1] = fast_silu(y[j][1]); }
-                    } else if (g.act == RTN_ACT_NONE) {
-                        #pragma unroll
-                        for (int j = 0; j < kOwn; ++j) { o[j][0] = y[j][0]; o[j][1] = y[j][1]; }
-                    } else {
+                        for (int j = 0; j < kOwn; ++j) { o[a][j][0] = fast_silu(y[a][j][0]); o[a][j][1] = fast_silu(y[a][j][1]); }
+                } else {
+                    #pragma unroll
+                    for (int a = 0; a < 2; ++a)
                         #pragma unroll
                         for (int j = 0; j < kOwn; j += 2) {
-                            const float4 x = activation4(make_float4(y[j][0], y[j][1], y[j + 1][0], y[j + 1][1]), g.act);
-                            o[j][0] = x.x; o[j][1] = x.y; o[j + 1][0] = x.z; o[j + 1][1] = x.w;
+                            float4 x = make_float4(y[a][j][0], y[a][j][1], y[a][j + 1][0], y[a][j + 1][1]);
+                            if (g.act != RTN_ACT_NONE) x = activation4(x, g.act);
+                            o[a][j][0] = x.x; o[a][j][1] = x.y; o[a][j + 1][0] = x.z; o[a][j + 1][1] = x.w;
                         }
-                    }
+                }
+                #pragma unroll
+                for (int a = 0; a < 2; ++a) {
                     if constexpr (kGated) {
                         #pragma unroll
-                        for (int j = 0; j < kOwn; ++j) { o[j][0] *= y[kOwn + j][0]; o[j][1] *= y[kOwn + j][1]; }
+                        for (int j = 0; j < kOwn; ++j) { o[a][j][0] *= y[a][kOwn + j][0]; o[a][j][1] *= y[a][kOwn + j][1]; }
                     }
                     if constexpr (kCodes) {
                         uint32_t nz[2][kOwn], up[2][kOwn];
@@ -547,8 +590,8 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                         for (int i = 0; i < 2; ++i)
                             #pragma unroll
                             for (int j = 0; j < kOwn; ++j) {
-                                const float e = fmaf(c1, fabsf(y[j][i]), c0), x = o[j][i];
-                                const float err = kGated ? e * (fabsf(y[kGated ? kOwn + j : j][i]) + c2) : e;
+                                const float e = fmaf(c1, fabsf(y[a][j][i]), c0), x = o[a][j][i];
+                                const float err = kGated ? e * (fabsf(y[a][kGated ? kOwn + j : j][i]) + c2) : e;
                                 const bool p = x > hi, n = p || x < lo;
                                 near = near || !(fminf(fabsf(x - lo), fabsf(x - hi)) > err);
                                 nz[i][j] = __ballot_sync(0xffffffffu, n);
@@ -564,19 +607,21 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                     if (!kCodes || g.out != nullptr) {
                         #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            if (at + i >= tile.rows) continue;
-                            T* out = static_cast<T*>(g.out) + (int64_t)(tile.row + at + i) * g.out_stride + f;
+                            const int at = c + 8 * a + 2 * q4 + i;
+                            if (at >= tile.rows) continue;
+                            T* out = static_cast<T*>(g.out) + (int64_t)(tile.row + at) * g.out_stride + f;
+                            const auto& w = o[a];
                             if (!kCodes && vec && f + kOwn <= g.F) {
                                 if constexpr (sizeof(T) == 2) {
-                                    if constexpr (kOwn == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(o[0][i], o[1][i]), pack2<T>(o[2][i], o[3][i]));
-                                    else *reinterpret_cast<uint32_t*>(out) = pack2<T>(o[0][i], o[1][i]);
+                                    if constexpr (kOwn == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(w[0][i], w[1][i]), pack2<T>(w[2][i], w[3][i]));
+                                    else *reinterpret_cast<uint32_t*>(out) = pack2<T>(w[0][i], w[1][i]);
                                 } else {
-                                    if constexpr (kOwn == 4) *reinterpret_cast<float4*>(out) = make_float4(o[0][i], o[1][i], o[2][i], o[3][i]);
-                                    else *reinterpret_cast<float2*>(out) = make_float2(o[0][i], o[1][i]);
+                                    if constexpr (kOwn == 4) *reinterpret_cast<float4*>(out) = make_float4(w[0][i], w[1][i], w[2][i], w[3][i]);
+                                    else *reinterpret_cast<float2*>(out) = make_float2(w[0][i], w[1][i]);
                                 }
                             } else {
                                 #pragma unroll
-                                for (int j = 0; j < kOwn; ++j) if (f + j < g.F) out[j] = from_f32<T>(o[j][i]);
+                                for (int j = 0; j < kOwn; ++j) if (f + j < g.F) out[j] = from_f32<T>(w[j][i]);
                             }
                         }
                     }
