@@ -500,7 +500,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         constexpr int kOwn = kGated ? 2 : 4;
         const int half = (warp - kExpandWarps) >> 2, r8 = lane >> 2, q4 = lane & 3;
         tc::pdl_wait();
-        const bool vec = kCodes || ((reinterpret_cast<uintptr_t>(g.out) % (kOwn * sizeof(T))) == 0 && g.out_stride % kOwn == 0);
+        const bool whole = kCodes || ((reinterpret_cast<uintptr_t>(g.out) % (kOwn * sizeof(T))) == 0 && g.out_stride % kOwn == 0);
         // Units of an output's error for its value before the activation: the affine form's own (below), passed on with a slope of at most
         // 1.13, and the activation's.
         const float units = g.act == RTN_ACT_SILU ? 8.3f : g.act == RTN_ACT_NONE || g.act == RTN_ACT_RELU ? 2.f : 18.3f;
@@ -541,15 +541,17 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             if (!(alive = warp_wait(&bar.acc_full[ti & 1], ti >> 1))) break;
             tc::tc_fence_after_sync();
             const uint32_t acc = tmem + (ti & 1) * acc_cols + ((uint32_t)(quad * 32) << 16);
+            T* out = static_cast<T*>(g.out) + (int64_t)(tile.row + half * 16 + 2 * q4) * g.out_stride + f;
+            const bool vec = whole && f + kOwn <= g.F;
             #pragma unroll 1
-            for (int c = half * 16; c < tile.rows; c += 32) {
+            for (int c = half * 16; c < tile.rows; c += 32, out += 32 * g.out_stride) {
                 uint32_t v[2][8];                                                  // TMEM lanes r8, r8 + 8 and r8 + 16, r8 + 24
                 tc::tmem_ld_16x16(acc + (uint32_t)c, v[0]);
                 tc::tmem_ld_16x16(acc + (uint32_t)c + (16u << 16), v[1]);
                 tc::tmem_ld_wait();
                 // the 16 tokens in steps of their own, so that each has many independent values: affine forms, activations, codes
                 bool near = false;
-                float y[2][4][2], o[2][kOwn][2];                                   // by group of 8 tokens, weight row and token
+                float y[2][4][2], err[2][kOwn][2];                                 // by group of 8 tokens, weight row and token
                 #pragma unroll
                 for (int a = 0; a < 2; ++a) {
                     const int at = c + 8 * a + 2 * q4;                             // tokens at and at + 1
@@ -562,66 +564,71 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                         take_pair(fma_pair(ws[j], mul_pair(as2, make_pair(__uint_as_float(S[0]), __uint_as_float(S[1]))),
                                            fma_pair(wo[j], sx2, fma_pair(p3[j], ao2, bias[j]))), y[a][j][0], y[a][j][1]);
                     }
+                    if constexpr (kCodes) {
+                        #pragma unroll
+                        for (int j = 0; j < kOwn; ++j)
+                            #pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                err[a][j][i] = fmaf(c1, fabsf(y[a][j][i]), c0);
+                                if constexpr (kGated) err[a][j][i] *= fabsf(y[a][kGated ? kOwn + j : j][i]) + c2;
+                            }
+                    }
                 }
                 if (g.act == RTN_ACT_SILU) {
                     #pragma unroll
                     for (int a = 0; a < 2; ++a)
                         #pragma unroll
-                        for (int j = 0; j < kOwn; ++j) { o[a][j][0] = fast_silu(y[a][j][0]); o[a][j][1] = fast_silu(y[a][j][1]); }
-                } else {
+                        for (int j = 0; j < kOwn; ++j) { y[a][j][0] = fast_silu(y[a][j][0]); y[a][j][1] = fast_silu(y[a][j][1]); }
+                } else if (g.act != RTN_ACT_NONE) {
                     #pragma unroll
                     for (int a = 0; a < 2; ++a)
                         #pragma unroll
                         for (int j = 0; j < kOwn; j += 2) {
-                            float4 x = make_float4(y[a][j][0], y[a][j][1], y[a][j + 1][0], y[a][j + 1][1]);
-                            if (g.act != RTN_ACT_NONE) x = activation4(x, g.act);
-                            o[a][j][0] = x.x; o[a][j][1] = x.y; o[a][j + 1][0] = x.z; o[a][j + 1][1] = x.w;
+                            const float4 x = activation4(make_float4(y[a][j][0], y[a][j][1], y[a][j + 1][0], y[a][j + 1][1]), g.act);
+                            y[a][j][0] = x.x; y[a][j][1] = x.y; y[a][j + 1][0] = x.z; y[a][j + 1][1] = x.w;
                         }
                 }
                 #pragma unroll
                 for (int a = 0; a < 2; ++a) {
                     if constexpr (kGated) {
                         #pragma unroll
-                        for (int j = 0; j < kOwn; ++j) { o[a][j][0] *= y[a][kOwn + j][0]; o[a][j][1] *= y[a][kOwn + j][1]; }
+                        for (int j = 0; j < kOwn; ++j) { y[a][j][0] *= y[a][kOwn + j][0]; y[a][j][1] *= y[a][kOwn + j][1]; }
                     }
                     if constexpr (kCodes) {
-                        uint32_t nz[2][kOwn], up[2][kOwn];
                         #pragma unroll
-                        for (int i = 0; i < 2; ++i)
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t nz[kOwn], up[kOwn];
                             #pragma unroll
                             for (int j = 0; j < kOwn; ++j) {
-                                const float e = fmaf(c1, fabsf(y[a][j][i]), c0), x = o[a][j][i];
-                                const float err = kGated ? e * (fabsf(y[a][kGated ? kOwn + j : j][i]) + c2) : e;
+                                const float x = y[a][j][i];
                                 const bool p = x > hi, n = p || x < lo;
-                                near = near || !(fminf(fabsf(x - lo), fabsf(x - hi)) > err);
-                                nz[i][j] = __ballot_sync(0xffffffffu, n);
-                                up[i][j] = __ballot_sync(0xffffffffu, p);
+                                near = near || !(fminf(fabsf(x - lo), fabsf(x - hi)) > err[a][j][i]);
+                                nz[j] = __ballot_sync(0xffffffffu, n);
+                                up[j] = __ballot_sync(0xffffffffu, p);
                             }
-                        if (lane == 0) {
-                            #pragma unroll
-                            for (int i = 0; i < 2; ++i)
+                            if (lane == 0) {
                                 #pragma unroll
-                                for (int j = 0; j < kOwn; j += 2) here.votes[quad][c / 4 + 2 * a + i][j / 2] = make_uint4(nz[i][j], up[i][j], nz[i][j + 1], up[i][j + 1]);
+                                for (int j = 0; j < kOwn; j += 2) here.votes[quad][c / 4 + 2 * a + i][j / 2] = make_uint4(nz[j], up[j], nz[j + 1], up[j + 1]);
+                            }
                         }
                     }
                     if (!kCodes || g.out != nullptr) {
                         #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const int at = c + 8 * a + 2 * q4 + i;
-                            if (at >= tile.rows) continue;
-                            T* out = static_cast<T*>(g.out) + (int64_t)(tile.row + at) * g.out_stride + f;
-                            const auto& w = o[a];
-                            if (!kCodes && vec && f + kOwn <= g.F) {
+                            if (c + 8 * a + 2 * q4 + i >= tile.rows) continue;
+                            T* to = out + (8 * a + i) * g.out_stride;
+                            const auto& w = y[a];
+                            if (!kCodes && vec) {
                                 if constexpr (sizeof(T) == 2) {
-                                    if constexpr (kOwn == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(w[0][i], w[1][i]), pack2<T>(w[2][i], w[3][i]));
-                                    else *reinterpret_cast<uint32_t*>(out) = pack2<T>(w[0][i], w[1][i]);
+                                    if constexpr (kOwn == 4) *reinterpret_cast<uint2*>(to) = make_uint2(pack2<T>(w[0][i], w[1][i]), pack2<T>(w[2][i], w[3][i]));
+                                    else *reinterpret_cast<uint32_t*>(to) = pack2<T>(w[0][i], w[1][i]);
                                 } else {
-                                    if constexpr (kOwn == 4) *reinterpret_cast<float4*>(out) = make_float4(w[0][i], w[1][i], w[2][i], w[3][i]);
-                                    else *reinterpret_cast<float2*>(out) = make_float2(w[0][i], w[1][i]);
+                                    if constexpr (kOwn == 4) *reinterpret_cast<float4*>(to) = make_float4(w[0][i], w[1][i], w[2][i], w[3][i]);
+                                    else *reinterpret_cast<float2*>(to) = make_float2(w[0][i], w[1][i]);
                                 }
                             } else {
                                 #pragma unroll
-                                for (int j = 0; j < kOwn; ++j) if (f + j < g.F) out[j] = from_f32<T>(w[j][i]);
+                                for (int j = 0; j < kOwn; ++j) if (f + j < g.F) to[j] = from_f32<T>(w[j][i]);
                             }
                         }
                     }
