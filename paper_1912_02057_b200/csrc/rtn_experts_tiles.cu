@@ -14,13 +14,14 @@ namespace {
 constexpr int kExpandWarps = 8, kEpilogueWarps = 8, kEdgeWarps = 4;
 constexpr int kLoadWarp = kExpandWarps + kEpilogueWarps, kPlanesWarp = kLoadWarp + 1, kMmaWarp = kLoadWarp + 2, kEdgeWarp = kLoadWarp + 4;
 constexpr int kThreads = (kEdgeWarp + kEdgeWarps) * 32;
-constexpr int kLaunchRegs = 80, kExpandRegs = 88, kEpilogueRegs = 112, kIssueRegs = 24, kEdgeRegs = 56;
+constexpr int kLaunchRegs = 80, kExpandRegs = 80, kEpilogueRegs = 112, kIssueRegs = 40, kEdgeRegs = 56;
 static_assert(kThreads == 768 && 2 * kExpandRegs + 2 * kEpilogueRegs + kIssueRegs + kEdgeRegs <= 6 * kLaunchRegs, "registers");
 template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
 template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
-// A stage holds 256 codes of K: a 128-byte row of 4-bit values to an input, 32 columns of tensor memory to a weight row.
+// A slot holds a span of K, 512 codes (or the last 256): two 128-byte rows of 4-bit values to an input, 64 columns of tensor memory to a weight row.
+// (Slots of 256 codes: twice the barriers, which a small tile's time is made of.)
 constexpr int kMaxRows = 192;                                   // of a tile
-constexpr int kMaxStages = 6, kMaxSpans = 8;
+constexpr int kMaxStages = 6, kMaxSpans = 8;                    // slots of the rings
 constexpr uint32_t kSpanBytes = 128 * 128;                       // 512 codes of 128 weight rows, as planes
 constexpr uint32_t kTries = 1u << 20;
 constexpr uint32_t kSmemBytes = 227 * 1024;
@@ -30,10 +31,10 @@ struct TilesPlan {
     int max_rows;               // of a tile, a multiple of 16
     int stages, spans;          // slots of the two rings
     int col_tiles;
-    int k_stages;
+    int k_halves;               // 256 codes each
     int box_rows;               // of a copy
     uint32_t ring, planes;      // offsets of the rings in shared memory
-    uint32_t stage_bytes;
+    uint32_t half_bytes;        // of a slot: the inputs' rows of 256 codes
     uint32_t smem;
 };
 
@@ -97,7 +98,7 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
 // A lane q has 8 words w of a stage, and word w is at 8 (w / 2) + 2 q + w % 2.
 //   four blocks: lane q has block q; words 0-3 and 4-7 of stage h come from the block's plane words 2 h and 2 h + 1
 //   two blocks:  lane q has plane words 2 (q % 2) and the next of block q / 2
-__host__ __device__ __forceinline__ int stages_of(int nblk) { return nblk / 4 * 2 + (nblk % 4 + 1) / 2; }
+__host__ __device__ __forceinline__ int halves_of(int nblk) { return nblk / 4 * 2 + (nblk % 4 + 1) / 2; }
 
 // The experts' rows one after the other as 4-bit values, `pitch` bytes each (a row's end is zeros); and the sums of their codes begin at 0.
 __global__ void __launch_bounds__(256)
@@ -222,7 +223,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
     const int quad = warp & 3;
     const int nblk = (int)((g.K + kBlockCodes - 1) / kBlockCodes), spans = (nblk + 3) / 4;
     const bool short_last = nblk % 4 == 1 || nblk % 4 == 2;
-    auto stages_in = [&](int span) { return span == spans - 1 && short_last ? 1 : 2; };
+    auto halves_in = [&](int span) { return span == spans - 1 && short_last ? 1 : 2; };
     constexpr int kTileOuts = kGated ? 64 : 128;
     // The output that TMEM lane 32 q + l belongs to, so that the lanes r, r + 8, ... which one thread of the epilogue reads are adjacent outputs; gated,
     // lanes l >= 16 are the rows that those of l - 16 are multiplied with.
@@ -233,19 +234,16 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
 
     if (warp < kExpandWarps) {
         // ------------------------------------------------------------ weights: two teams of four warps have the spans in turn
-        more_registers<kExpandRegs>();
         const int row4 = lane >> 2, q4 = lane & 3;
         const uint32_t mine = blockIdx.x < total ? (total - 1 - blockIdx.x) / gridDim.x + 1 : 0, n_spans = mine * (uint32_t)spans;
         int k = warp >> 2, sp = k;                                                // span of a tile, its slot
         while (k >= spans) k -= spans;
         if (sp >= p.spans) sp -= p.spans;
         uint32_t planes_phase = 0, phase = 0;
-        // Slots of the expanded codes go round as well; a span takes two, the last of a row perhaps one.
-        int s = 0;
-        auto skip = [&](int n) { s += n; if (s >= p.stages) { s -= p.stages; phase ^= 1; } };
-        if (warp >= 4) skip(stages_in(0));
+        int s = warp >> 2;                                                        // slot of the expanded codes
+        if (s >= p.stages) s -= p.stages;
         for (uint32_t n = (uint32_t)warp >> 2; n < n_spans && alive; n += 2) {
-            const int stages = stages_in(k);
+            const int halves = halves_in(k);
             if (!(alive = warp_wait(&bar.planes_full[sp], planes_phase))) break;
             uint4 nz[4], pos[4];                                                  // TMEM lanes row4 + 8 j of the quarter, this lane's part of the span
             const uint8_t* from = smem + p.planes + (uint32_t)sp * kSpanBytes;
@@ -256,14 +254,17 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                 nz[j] = *reinterpret_cast<const uint4*>(from + row * 128 + (((2 * block) ^ (row & 7)) << 4));
                 pos[j] = *reinterpret_cast<const uint4*>(from + row * 128 + (((2 * block + 1) ^ (row & 7)) << 4));
             }
-            if (stages == 1) {                                                    // the last two blocks: this lane's half of one
+            if (halves == 1) {                                                    // the last two blocks: this lane's half of one
                 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (q4 & 1) { nz[j].x = nz[j].z; nz[j].y = nz[j].w; pos[j].x = pos[j].z; pos[j].y = pos[j].w; }
             }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&bar.planes_empty[sp]);                // (the planes are in registers)
+            const uint32_t at = a_tmem + (uint32_t)(s * 64) + ((uint32_t)(quad * 32) << 16);
             #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (h >= stages) break;
+                if (h >= halves) break;
                 uint32_t o[2][16];
                 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -272,21 +273,16 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                     uint32_t* to = o[j >> 1] + 2 * (j & 1);
                     to[0] = a.x; to[1] = a.y; to[4] = a.z; to[5] = a.w; to[8] = b.x; to[9] = b.y; to[12] = b.z; to[13] = b.w;
                 }
-                if (h == 0) {                                                     // (the planes are in registers)
-                    __syncwarp();
-                    if (lane == 0) tc::mbar_arrive(&bar.planes_empty[sp]);
-                }
-                if (!(alive = warp_wait(&bar.empty[s], phase + 1))) break;
-                const uint32_t at = a_tmem + (uint32_t)(s * 32) + ((uint32_t)(quad * 32) << 16);
-                tc::tmem_st_16x32(at, o[0]);
-                tc::tmem_st_16x32(at + (16u << 16), o[1]);
-                tc::tmem_st_wait();
-                tc::tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&bar.full[s]);
-                skip(1);
+                if (h == 0 && !(alive = warp_wait(&bar.empty[s], phase + 1))) break;
+                tc::tmem_st_16x32(at + (uint32_t)(h * 32), o[0]);
+                tc::tmem_st_16x32(at + (uint32_t)(h * 32) + (16u << 16), o[1]);
             }
-            skip(stages_in(k + 1 == spans ? 0 : k + 1));
+            tc::tmem_st_wait();
+            tc::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&bar.full[s]);
+            s += 2;
+            while (s >= p.stages) { s -= p.stages; phase ^= 1; }
             k += 2;
             while (k >= spans) k -= spans;
             sp += 2;
@@ -315,12 +311,15 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             for (uint32_t t = blockIdx.x; t < total && alive; t += gridDim.x) {
                 const int at = find_one(t), h = height[seen], row = first[seen] + at * h;
                 const int boxes = (h + p.box_rows - 1) / p.box_rows;              // (what lies behind the tile's rows belongs to no output)
-                for (int k = 0; k < p.k_stages; ++k) {
+                for (int k = 0; k < spans; ++k) {
                     if (!(alive = wait(&bar.empty[s], phase + 1))) break;
-                    tc::mbar_arrive_expect_tx(&bar.full[s], (uint32_t)boxes * box_bytes);
-                    const uint32_t dst = ring + (uint32_t)s * p.stage_bytes;
-                    load_box(dst, &map, k * 128, row, &bar.full[s]);
-                    if (boxes > 1) load_box(dst + box_bytes, &map, k * 128, row + p.box_rows, &bar.full[s]);
+                    const int halves = halves_in(k);
+                    tc::mbar_arrive_expect_tx(&bar.full[s], (uint32_t)(halves * boxes) * box_bytes);
+                    uint32_t dst = ring + (uint32_t)s * 2 * p.half_bytes;
+                    for (int h = 0; h < halves; ++h, dst += p.half_bytes) {
+                        load_box(dst, &map, k * 256 + h * 128, row, &bar.full[s]);
+                        if (boxes > 1) load_box(dst + box_bytes, &map, k * 256 + h * 128, row + p.box_rows, &bar.full[s]);
+                    }
                     if (++s == p.stages) { s = 0; phase ^= 1; }
                 }
             }
@@ -361,14 +360,16 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         for (uint32_t t = blockIdx.x; t < total && alive; t += gridDim.x, ++ti) {
             const uint32_t idesc = idesc_mxf4(128, (uint32_t)__shfl_sync(0xffffffffu, find(t).height, 0)), d = tmem + (ti & 1) * acc_cols;
             if (!(alive = warp_wait(&bar.acc_empty[ti & 1], (ti >> 1) + 1))) break;
-            for (int k = 0; k < p.k_stages; ++k) {
+            for (int k = 0; k < spans; ++k) {
                 if (!(alive = warp_wait(&bar.full[s], phase))) break;
                 tc::tc_fence_after_sync();
-                const uint64_t b = desc + (uint64_t)((uint32_t)s * (p.stage_bytes >> 4));
-                const uint32_t a = a_tmem + (uint32_t)(s * 32);
-                #pragma unroll
-                for (int j = 0; j < 4; ++j)                                       // K = 64: 32 bytes, eight columns
-                    mma_mxf4(elected, d, a + (uint32_t)(j * 8), b + (uint64_t)(j * 2), idesc, scales, k > 0 || j > 0);
+                uint64_t b = desc + (uint64_t)((uint32_t)s * (p.half_bytes >> 3));
+                uint32_t a = a_tmem + (uint32_t)(s * 64);
+                for (int h = halves_in(k); h > 0; --h, a += 32u, b += (uint64_t)(p.half_bytes >> 4)) {
+                    #pragma unroll
+                    for (int j = 0; j < 4; ++j)                                   // K = 64: 32 bytes, eight columns
+                        mma_mxf4(elected, d, a + (uint32_t)(j * 8), b + (uint64_t)(j * 2), idesc, scales, k > 0 || j > 0 || h == 1 && halves_in(k) == 2);
+                }
                 if (elected) tc::mma_commit(&bar.empty[s]);
                 __syncwarp();
                 if (++s == p.stages) { s = 0; phase ^= 1; }
@@ -700,23 +701,23 @@ TilesPlan make_plan(const ExpertsArgs& g)
     const int outs = g.gated ? 64 : 128;
     const int64_t width = g.out_packed != nullptr ? (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes : g.F;
     p.col_tiles = (int)((width + outs - 1) / outs);
-    p.k_stages = stages_of((int)((g.K + kBlockCodes - 1) / kBlockCodes));
+    p.k_halves = halves_of((int)((g.K + kBlockCodes - 1) / kBlockCodes));
     const double used = (double)(g.R < g.E ? g.R : g.E), each = (double)g.R / used, sms = device_sm_count();
     double best = 0.0;
     for (int h = 16; h <= 160; h += 16) {
         const double per = (double)(int64_t)((each + h - 1) / h), tiles = used * per * p.col_tiles, height = each / per < 16 ? 16 : each / per;
-        const double stage = 2.6 * height > 350.0 ? 2.6 * height : 350.0, loop = stage * p.k_stages, out = 20.0 * height + 500.0;
+        const double stage = 2.6 * height > 350.0 ? 2.6 * height : 350.0, loop = stage * p.k_halves, out = 20.0 * height + 500.0;
         const double rounds = tiles / sms < 1.0 ? 1.0 : (double)(int64_t)((tiles + sms - 1) / sms);
         const double cost = rounds * (loop > out ? loop : out) + (loop > out ? out : loop);
         if (p.max_rows == 0 || cost < best) { best = cost; p.max_rows = h; }
     }
     p.box_rows = p.max_rows > 64 ? (p.max_rows + 31) / 32 * 16 : p.max_rows;          // two to a tile, or one
-    p.stage_bytes = (uint32_t)((p.max_rows + p.box_rows - 1) / p.box_rows * p.box_rows) * 128u;
+    p.half_bytes = (uint32_t)((p.max_rows + p.box_rows - 1) / p.box_rows * p.box_rows) * 128u;
     p.ring = (uint32_t)((512 + 2 * sizeof(TileParams) + (4 * g.E + 1) * 4 + 1023) / 1024 * 1024);
-    const int by_tmem = (512 - 2 * p.max_rows - (int)kScaleCols) / 32;
+    const int by_tmem = (512 - 2 * p.max_rows - (int)kScaleCols) / 64;
     p.stages = by_tmem < kMaxStages ? by_tmem : kMaxStages;
-    while (p.stages > 3 && p.ring + (uint32_t)p.stages * p.stage_bytes + 4 * kSpanBytes > kSmemBytes) --p.stages;
-    p.planes = p.ring + (uint32_t)p.stages * p.stage_bytes;                      // (a multiple of 1024: stages are multiples of 2048 bytes)
+    while (p.stages > 2 && p.ring + (uint32_t)p.stages * 2 * p.half_bytes + 4 * kSpanBytes > kSmemBytes) --p.stages;
+    p.planes = p.ring + (uint32_t)p.stages * 2 * p.half_bytes;                   // (a multiple of 1024: halves are multiples of 2048 bytes)
     p.spans = (int)((kSmemBytes - p.planes) / kSpanBytes);
     if (p.spans > kMaxSpans) p.spans = kMaxSpans;
     p.smem = p.planes + (uint32_t)p.spans * kSpanBytes;
@@ -730,7 +731,7 @@ cudaError_t launch_experts_tiles(const ExpertsArgs& g, cudaStream_t s)
     const TilesPlan p = make_plan(g);
     const EncodeTiledFn encode = encode_tiled_fn();
     if (encode == nullptr) return cudaErrorNotSupported;
-    const int nblk = (int)((g.K + kBlockCodes - 1) / kBlockCodes), pitch = p.k_stages * 128;
+    const int nblk = (int)((g.K + kBlockCodes - 1) / kBlockCodes), pitch = p.k_halves * 128;
     void* scratch = nullptr;
     cudaError_t e = scratch_alloc(&scratch, (size_t)g.R * pitch, s);
     if (e != cudaSuccess) return e;
