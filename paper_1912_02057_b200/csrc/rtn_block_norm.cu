@@ -18,19 +18,34 @@ namespace {
 constexpr float kUnit = 5.9604644775390625e-8f;                // 2^-24
 constexpr int kMaxWarps = 32;
 
-// EV adjacent elements as fp32: 16-byte loads where EV > 1 (the launcher saw to the alignment).
+// EV adjacent elements: 16-byte accesses where EV > 1 (the launcher saw to the alignment).  `Held` is what they are until they are looked at,
+// so that many are on their way at a time.
+template <typename T, int EV> struct Held { uint4 u[EV * sizeof(T) / 16]; };
+template <typename T> struct Held<T, 1> { T u; };
+
 template <typename T, int EV>
-__device__ __forceinline__ void load_values(const void* base, int64_t at, float (&f)[EV])
+__device__ __forceinline__ Held<T, EV> ask(const void* base, int64_t at)
 {
+    Held<T, EV> h;
     const T* p = static_cast<const T*>(base) + at;
-    if constexpr (EV == 1) f[0] = to_f32(*p);
+    if constexpr (EV == 1) h.u = *p;
+    else {
+        #pragma unroll
+        for (int i = 0; i < EV * (int)sizeof(T) / 16; ++i) h.u[i] = reinterpret_cast<const uint4*>(p)[i];
+    }
+    return h;
+}
+template <typename T, int EV>
+__device__ __forceinline__ void take(const Held<T, EV>& h, bool ok, float (&f)[EV])       // zeros where not ok
+{
+    if constexpr (EV == 1) f[0] = ok ? to_f32(h.u) : 0.f;
     else {
         constexpr int N = Vec16<T>::N;
         static_assert(EV % N == 0, "whole vectors");
         #pragma unroll
         for (int i = 0; i < EV / N; ++i) {
             float part[N];
-            Vec16<T>::unpack(reinterpret_cast<const uint4*>(p)[i], part);
+            Vec16<T>::unpack(ok ? h.u[i] : make_uint4(0, 0, 0, 0), part);
             #pragma unroll
             for (int j = 0; j < N; ++j) f[i * N + j] = part[j];
         }
@@ -53,10 +68,9 @@ __device__ __forceinline__ void store_values(void* base, int64_t at, const float
     }
 }
 template <int EV>
-__device__ __forceinline__ void load_params(const float* p, int at, float (&f)[EV])     // (of W values, 4-byte aligned)
+__device__ __forceinline__ void load_params(const float* p, int at, float (&f)[EV])
 {
-    #pragma unroll
-    for (int i = 0; i < EV; ++i) f[i] = p[at + i];
+    take<float, EV>(ask<float, EV>(p, at), true, f);
 }
 
 // Sums of a pair over the block; every thread has them.
@@ -86,130 +100,167 @@ __device__ __forceinline__ float gate_of(float z, int kind)
 // Roundings of a sum of squares: per thread, two shuffle trees, and the mean, root and quotient after it.
 template <int NV, int EV> constexpr float kRootUnits = 0.5f * (NV * EV + 10) + 5.f;
 
-// h and n of token t.  slack receives the bound on n's error, where kTrack asks for it.
+// h and n of token t.  slack receives the bound on n's error, where kTrack asks for it.  Loads are not in branches (a value behind the row's end is
+// read from its beginning and put to zero): the compiler waited for one after the other there.
 template <typename TB, typename TS, int EV, int NV, bool kTrack>
 __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* red, float (&h)[NV][EV], float (&n)[NV][EV], float (&slack)[NV][EV])
 {
     const int W = g.W, step = blockDim.x * EV, first = threadIdx.x * EV;
     const float k_units = g.place != nullptr ? (float)g.k : 0.f;
     float zero = 0.f, ss = 0.f, sm = 0.f;
+    int at[NV];                                                 // a value's column, or 0 behind the row's end
+    bool in[NV];
+    #pragma unroll
+    for (int v = 0; v < NV; ++v) { in[v] = first + v * step < W; at[v] = in[v] ? first + v * step : 0; }
+    Held<TS, EV> res[NV];
+    if (g.residual != nullptr) {
+        #pragma unroll
+        for (int v = 0; v < NV; ++v) res[v] = ask<TS, EV>(g.residual, t * g.residual_stride + at[v]);
+    }
+    // y in h, the sum of its terms' magnitudes in slack
     #pragma unroll
     for (int v = 0; v < NV; ++v)
         #pragma unroll
         for (int i = 0; i < EV; ++i) h[v][i] = slack[v][i] = 0.f;
-    // y in h, the sum of its terms' magnitudes in slack
-    if (g.branch != nullptr) {
-        #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c = first + v * step;
-            if (c >= W) continue;
-            if (g.place == nullptr) {
-                load_values<TB, EV>(g.branch, t * g.branch_stride + c, h[v]);
-            } else {
-                #pragma unroll 4
-                for (int j = 0; j < g.k; ++j) {
-                    const int64_t row = g.place[t * g.k + j];
-                    float w = g.weights != nullptr ? g.weights[t * g.k + j] : 1.f;
-                    if (row < 0) continue;
-                    float x[EV];
-                    if (row < g.R) load_values<TB, EV>(g.branch, row * g.branch_stride + c, x);
-                    else {
-                        w = __int_as_float(0x7fffffff);
-                        #pragma unroll
-                        for (int i = 0; i < EV; ++i) x[i] = w;
-                    }
+    if (g.place != nullptr) {
+        constexpr int kAhead = NV * EV <= 8 ? 4 : 1;            // rows on their way
+        #pragma unroll 1
+        for (int j0 = 0; j0 < g.k; j0 += kAhead) {
+            Held<TB, EV> x[kAhead][NV];
+            float w[kAhead];
+            bool ok[kAhead];
+            #pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int j = j0 + i < g.k ? j0 + i : 0;
+                const int64_t row = g.place[t * g.k + j];
+                w[i] = g.weights != nullptr ? g.weights[t * g.k + j] : 1.f;
+                ok[i] = j0 + i < g.k && row >= 0 && row < g.R;
+                if (!ok[i]) w[i] = j0 + i < g.k && row >= g.R ? __int_as_float(0x7fffffff) : 0.f;
+                #pragma unroll
+                for (int v = 0; v < NV; ++v) x[i][v] = ask<TB, EV>(g.branch, (ok[i] ? row : 0) * g.branch_stride + at[v]);
+            }
+            #pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                #pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    float f[EV];
+                    take<TB, EV>(x[i][v], ok[i], f);
                     #pragma unroll
-                    for (int i = 0; i < EV; ++i) {
-                        h[v][i] = fmaf(w, x[i], h[v][i]);
-                        if constexpr (kTrack) slack[v][i] = fmaf(fabsf(w), fabsf(x[i]), slack[v][i]);
+                    for (int e = 0; e < EV; ++e) {
+                        h[v][e] = fmaf(w[i], f[e], h[v][e]);
+                        if constexpr (kTrack) slack[v][e] = fmaf(fabsf(w[i]), fabsf(f[e]), slack[v][e]);
                     }
                 }
+        }
+        #pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (!in[v]) {
+                #pragma unroll
+                for (int e = 0; e < EV; ++e) h[v][e] = slack[v][e] = 0.f;
+            }
+    } else if (g.branch != nullptr) {
+        Held<TB, EV> x[NV];
+        #pragma unroll
+        for (int v = 0; v < NV; ++v) x[v] = ask<TB, EV>(g.branch, t * g.branch_stride + at[v]);
+        #pragma unroll
+        for (int v = 0; v < NV; ++v) take<TB, EV>(x[v], in[v], h[v]);
+    }
+    // what y is multiplied with, apart from its norm
+    float f[NV][EV];
+    float units = g.post_weight != nullptr ? 2.f : 0.f;         // roundings of the factor and its product
+    #pragma unroll
+    for (int v = 0; v < NV; ++v)
+        #pragma unroll
+        for (int i = 0; i < EV; ++i) f[v][i] = 1.f;
+    if (g.gate != nullptr) {
+        Held<TB, EV> z[NV];
+        #pragma unroll
+        for (int v = 0; v < NV; ++v) z[v] = ask<TB, EV>(g.gate, t * g.gate_stride + at[v]);
+        #pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            take<TB, EV>(z[v], true, f[v]);
+            #pragma unroll
+            for (int i = 0; i < EV; ++i) f[v][i] = gate_of(f[v][i], g.gate_kind);
+        }
+        units += 12.f;
+    }
+    if (g.scale != nullptr) {
+        units += 1.f;
+        if (g.n_scale == 1) {
+            #pragma unroll
+            for (int v = 0; v < NV; ++v)
+                #pragma unroll
+                for (int i = 0; i < EV; ++i) f[v][i] *= g.scale[0];
+        } else {
+            #pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                float p[EV];
+                load_params<EV>(g.scale, at[v], p);
+                #pragma unroll
+                for (int i = 0; i < EV; ++i) f[v][i] *= p[i];
             }
         }
     }
-    float post = 1.f, post_units = 0.f;
+    float post_units = 0.f;
     if (g.post_weight != nullptr) {
         #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v) {
+            float p[EV];
+            load_params<EV>(g.post_weight, at[v], p);
             #pragma unroll
             for (int i = 0; i < EV; ++i) {
+                f[v][i] *= p[i];
                 ss = fmaf(h[v][i], h[v][i], ss);
                 if constexpr (kTrack) sm = fmaf(slack[v][i], slack[v][i], sm);
             }
+        }
         block_sums(ss, kTrack ? sm : zero, red);
-        post = 1.f / sqrtf(ss / (float)W + g.eps);
+        const float post = 1.f / sqrtf(ss / (float)W + g.eps);
         if constexpr (kTrack) post_units = kRootUnits<NV, EV> + 2.f + (ss > 0.f ? k_units * sqrtf(sm / ss) : 0.f);
+        #pragma unroll
+        for (int v = 0; v < NV; ++v)
+            #pragma unroll
+            for (int i = 0; i < EV; ++i) f[v][i] *= post;
+        ss = sm = 0.f;
     }
-    ss = sm = 0.f;
     #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int c = first + v * step;
-        if (c >= W) continue;
-        float f[EV];
-        #pragma unroll
-        for (int i = 0; i < EV; ++i) f[i] = 1.f;
-        float units = 0.f;                                      // roundings of the factor and its product
-        if (g.branch != nullptr) {
-            float p[EV];
-            if (g.post_weight != nullptr) {
-                load_params<EV>(g.post_weight, c, p);
-                #pragma unroll
-                for (int i = 0; i < EV; ++i) f[i] = post * p[i];
-                units = 2.f;
-            }
-            if (g.gate != nullptr) {
-                load_values<TB, EV>(g.gate, t * g.gate_stride + c, p);
-                #pragma unroll
-                for (int i = 0; i < EV; ++i) f[i] *= gate_of(p[i], g.gate_kind);
-                units += 12.f;
-            }
-            if (g.scale != nullptr) {
-                if (g.n_scale == 1) {
-                    #pragma unroll
-                    for (int i = 0; i < EV; ++i) f[i] *= g.scale[0];
-                } else {
-                    load_params<EV>(g.scale, c, p);
-                    #pragma unroll
-                    for (int i = 0; i < EV; ++i) f[i] *= p[i];
-                }
-                units += 1.f;
-            }
-        }
         float r[EV];
         #pragma unroll
         for (int i = 0; i < EV; ++i) r[i] = 0.f;
-        if (g.residual != nullptr) load_values<TS, EV>(g.residual, t * g.residual_stride + c, r);
+        if (g.residual != nullptr) take<TS, EV>(res[v], in[v], r);
         #pragma unroll
         for (int i = 0; i < EV; ++i) {
-            const float y = h[v][i];
-            h[v][i] = fmaf(f[i], y, r[i]);
+            const float y = h[v][i], m = slack[v][i];
+            h[v][i] = in[v] ? fmaf(f[v][i], y, r[i]) : 0.f;
             if constexpr (kTrack) {
-                slack[v][i] = fmaf(fabsf(f[i]), fmaf(k_units, slack[v][i], (post_units + units) * fabsf(y)), fabsf(h[v][i]));
+                slack[v][i] = in[v] ? fmaf(fabsf(f[v][i]), fmaf(k_units, m, (post_units + units) * fabsf(y)), fabsf(h[v][i])) : 0.f;
                 sm = fmaf(slack[v][i], slack[v][i], sm);
             }
             ss = fmaf(h[v][i], h[v][i], ss);
         }
     }
-    float pre = 1.f, pre_units = 0.f;
+    float pre_units = 0.f;
     if (g.norm_weight != nullptr) {
+        float p[NV][EV];
+        #pragma unroll
+        for (int v = 0; v < NV; ++v) load_params<EV>(g.norm_weight, at[v], p[v]);
         block_sums(ss, kTrack ? sm : zero, red);
-        pre = 1.f / sqrtf(ss / (float)W + g.eps);
+        const float pre = 1.f / sqrtf(ss / (float)W + g.eps);
         if constexpr (kTrack) pre_units = kRootUnits<NV, EV> + 4.f + (ss > 0.f ? sqrtf(sm / ss) : 0.f);
-    }
-    #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int c = first + v * step;
         #pragma unroll
-        for (int i = 0; i < EV; ++i) n[v][i] = h[v][i];
-        if (c >= W || g.norm_weight == nullptr) continue;
-        float p[EV];
-        load_params<EV>(g.norm_weight, c, p);
+        for (int v = 0; v < NV; ++v)
+            #pragma unroll
+            for (int i = 0; i < EV; ++i) {
+                const float q = pre * p[v][i];
+                n[v][i] = q * h[v][i];
+                if constexpr (kTrack) slack[v][i] = fmaf(fabsf(q), slack[v][i], pre_units * fabsf(n[v][i]));
+            }
+    } else {
         #pragma unroll
-        for (int i = 0; i < EV; ++i) {
-            const float f = pre * p[i];
-            n[v][i] = f * h[v][i];
-            if constexpr (kTrack) slack[v][i] = fmaf(fabsf(f), slack[v][i], pre_units * fabsf(n[v][i]));
-        }
+        for (int v = 0; v < NV; ++v)
+            #pragma unroll
+            for (int i = 0; i < EV; ++i) n[v][i] = h[v][i];
     }
 }
 
@@ -244,58 +295,68 @@ __device__ __forceinline__ bool code_row(const NormArgs& g, const float (&n)[NV]
     return near;
 }
 
-// The codes of one token in double, whatever the types: the inputs are read again in each pass.
+// The codes of one token in double, whatever the types: thread by thread the columns threadIdx.x, threadIdx.x + blockDim.x, ...
+constexpr int kExactEach = 16;                                  // of a thread at most
 __device__ __forceinline__ double exact_y(const NormArgs& g, int64_t t, int c)
 {
     if (g.branch == nullptr) return 0.0;
     if (g.place == nullptr) return (double)load_as_f32(g.branch, t * g.branch_stride + c, g.dtype);
     double y = 0.0;
-    for (int j = 0; j < g.k; ++j) {
-        const int64_t row = g.place[t * g.k + j];
-        if (row < 0) continue;
-        if (row >= g.R) return __longlong_as_double(0x7fffffffffffffffll);
-        y = fma(g.weights != nullptr ? (double)g.weights[t * g.k + j] : 1.0, (double)load_as_f32(g.branch, row * g.branch_stride + c, g.dtype), y);
+    #pragma unroll 1
+    for (int j0 = 0; j0 < g.k; j0 += 8) {
+        float x[8], w[8];
+        #pragma unroll
+        for (int i = 0; i < 8; ++i) {                           // (all of them on their way)
+            const int j = j0 + i < g.k ? j0 + i : 0;
+            const int64_t row = g.place[t * g.k + j];
+            const bool ok = j0 + i < g.k && row >= 0;
+            w[i] = !ok ? 0.f : row >= g.R ? __int_as_float(0x7fffffff) : g.weights != nullptr ? g.weights[t * g.k + j] : 1.f;
+            x[i] = load_as_f32(g.branch, (ok && row < g.R ? row : 0) * g.branch_stride + c, g.dtype);
+            if (!ok) x[i] = 0.f;
+        }
+        #pragma unroll
+        for (int i = 0; i < 8; ++i) y = fma((double)w[i], (double)x[i], y);
     }
     return y;
 }
-__device__ __forceinline__ double exact_h(const NormArgs& g, int64_t t, int c, double post)
-{
-    double y = exact_y(g, t, c);
-    if (g.post_weight != nullptr) y *= post * (double)g.post_weight[c];
-    if (g.gate != nullptr) {
-        const double z = (double)load_as_f32(g.gate, t * g.gate_stride + c, g.dtype), s = 1.0 / (1.0 + exp(-z));
-        y *= g.gate_kind == RTN_GATE_LINEAR ? z : g.gate_kind == RTN_GATE_SIGMOID ? s : z * s;
-    }
-    if (g.scale != nullptr) y *= (double)g.scale[g.n_scale == 1 ? 0 : c];
-    return g.residual != nullptr ? (double)load_as_f32(g.residual, t * g.residual_stride + c, g.stream_dtype) + y : y;
-}
 static __device__ __noinline__ int exact_codes(const NormArgs& g, int64_t t, double* red, uint8_t* row)
 {
-    double post = 1.0, pre = 1.0, none = 0.0;
+    double h[kExactEach], post = 1.0, pre = 1.0, none = 0.0, ss = 0.0;
+    #pragma unroll 1
+    for (int i = 0, c = threadIdx.x; c < g.W; ++i, c += blockDim.x) { h[i] = exact_y(g, t, c); ss = fma(h[i], h[i], ss); }
     if (g.post_weight != nullptr) {
-        double ss = 0.0;
-        for (int c = threadIdx.x; c < g.W; c += blockDim.x) { const double y = exact_y(g, t, c); ss = fma(y, y, ss); }
         block_sums(ss, none, red);
         post = 1.0 / sqrt(ss / (double)g.W + (double)g.eps);
     }
+    ss = none = 0.0;
+    #pragma unroll 1
+    for (int i = 0, c = threadIdx.x; c < g.W; ++i, c += blockDim.x) {
+        double y = h[i];
+        if (g.post_weight != nullptr) y *= post * (double)g.post_weight[c];
+        if (g.gate != nullptr) {
+            const double z = (double)load_as_f32(g.gate, t * g.gate_stride + c, g.dtype), s = 1.0 / (1.0 + exp(-z));
+            y *= g.gate_kind == RTN_GATE_LINEAR ? z : g.gate_kind == RTN_GATE_SIGMOID ? s : z * s;
+        }
+        if (g.scale != nullptr) y *= (double)g.scale[g.n_scale == 1 ? 0 : c];
+        if (g.residual != nullptr) y += (double)load_as_f32(g.residual, t * g.residual_stride + c, g.stream_dtype);
+        h[i] = y;
+        ss = fma(y, y, ss);
+    }
     if (g.norm_weight != nullptr) {
-        double ss = 0.0;
-        for (int c = threadIdx.x; c < g.W; c += blockDim.x) { const double h = exact_h(g, t, c, post); ss = fma(h, h, ss); }
-        none = 0.0;
         block_sums(ss, none, red);
         pre = 1.0 / sqrt(ss / (double)g.W + (double)g.eps);
     }
     int sum = 0;
     const int width = (g.W + kBlockCodes - 1) / kBlockCodes * kBlockCodes;
-    for (int c0 = threadIdx.x & ~31; c0 < width; c0 += blockDim.x) {
+    #pragma unroll 1
+    for (int i = 0, c0 = threadIdx.x & ~31; c0 < width; ++i, c0 += blockDim.x) {
         const int c = c0 + (threadIdx.x & 31);
         bool up = false, down = false;
         if (c < g.W) {
-            double n = exact_h(g, t, c, post);
-            if (g.norm_weight != nullptr) n *= pre * (double)g.norm_weight[c];
-            const int i = g.n_thr == 1 ? 0 : c;
-            up = n > (double)g.t_hi[i];
-            down = !up && n < (double)g.t_lo[i];
+            const double n = g.norm_weight != nullptr ? h[i] * (pre * (double)g.norm_weight[c]) : h[i];
+            const int k = g.n_thr == 1 ? 0 : c;
+            up = n > (double)g.t_hi[k];
+            down = !up && n < (double)g.t_lo[k];
         }
         const uint32_t a = __ballot_sync(0xffffffffu, up), b = __ballot_sync(0xffffffffu, down);
         if ((threadIdx.x & 31) == 0) {
@@ -308,8 +369,8 @@ static __device__ __noinline__ int exact_codes(const NormArgs& g, int64_t t, dou
     return sum;
 }
 
-template <typename TB, typename TS, int EV, int NV, bool kCodes>
-__global__ void __launch_bounds__(1024)
+template <typename TB, typename TS, int EV, int NV, int kMaxThreads, bool kCodes>
+__global__ void __launch_bounds__(kMaxThreads, kMaxThreads == 256 ? 4 : 1)
 block_norm_kernel(const __grid_constant__ NormArgs g)
 {
     __shared__ double red[2 * kMaxWarps];
@@ -355,20 +416,16 @@ block_norm_kernel(const __grid_constant__ NormArgs g)
         if (g.stream_out != nullptr) store_values<TS, EV>(g.stream_out, t * g.stream_stride + c, h[v]);
         if (g.normed != nullptr) store_values<TB, EV>(g.normed, t * g.normed_stride + c, n[v]);
     }
-    if (threadIdx.x == 0 && g.place != nullptr) {
-        bool bad = false;
-        for (int j = 0; j < g.k; ++j) bad |= g.place[t * g.k + j] >= g.R;
-        if (bad) atomicOr(g.status, kStatusBadIndex);
-    }
+    if (g.place != nullptr && threadIdx.x < g.k && g.place[t * g.k + threadIdx.x] >= g.R) atomicOr(g.status, kStatusBadIndex);
 }
 
-template <typename TB, typename TS, int EV, int NV>
+template <typename TB, typename TS, int EV, int NV, int kMaxThreads>
 cudaError_t launch_values(const NormArgs& g, cudaStream_t s)
 {
     const int width = (g.W + kBlockCodes - 1) / kBlockCodes * kBlockCodes;         // (the padding of a packed row is written too)
     const int threads = ((width + EV * NV - 1) / (EV * NV) + 31) / 32 * 32;
-    if (g.out_packed != nullptr) block_norm_kernel<TB, TS, EV, NV, true><<<(unsigned)g.T, threads, 0, s>>>(g);
-    else block_norm_kernel<TB, TS, EV, NV, false><<<(unsigned)g.T, threads, 0, s>>>(g);
+    if (g.out_packed != nullptr) block_norm_kernel<TB, TS, EV, NV, kMaxThreads, true><<<(unsigned)g.T, threads, 0, s>>>(g);
+    else block_norm_kernel<TB, TS, EV, NV, kMaxThreads, false><<<(unsigned)g.T, threads, 0, s>>>(g);
     return cudaGetLastError();
 }
 
@@ -380,10 +437,12 @@ cudaError_t launch_types(const NormArgs& g, cudaStream_t s)
     };
     const bool wide = g.W % 8 == 0 && vec(g.branch, g.branch_stride, sizeof(TB)) && vec(g.gate, g.gate_stride, sizeof(TB)) &&
                       vec(g.normed, g.normed_stride, sizeof(TB)) && vec(g.residual, g.residual_stride, sizeof(TS)) &&
-                      vec(g.stream_out, g.stream_stride, sizeof(TS));
-    if (wide) return g.W <= 8192 ? launch_values<TB, TS, 8, 1>(g, s) : launch_values<TB, TS, 8, 2>(g, s);
-    if (g.W <= 4096) return launch_values<TB, TS, 1, 4>(g, s);
-    return launch_values<TB, TS, 1, 16>(g, s);
+                      vec(g.stream_out, g.stream_stride, sizeof(TS)) && vec(g.post_weight, 0, 4) && vec(g.norm_weight, 0, 4) &&
+                      (g.n_scale == 1 || vec(g.scale, 0, 4)) && (g.n_thr == 1 || (vec(g.t_lo, 0, 4) && vec(g.t_hi, 0, 4)));
+    if (wide && g.W <= 2048) return launch_values<TB, TS, 8, 1, 256>(g, s);
+    if (wide) return g.W <= 8192 ? launch_values<TB, TS, 8, 1, 1024>(g, s) : launch_values<TB, TS, 8, 2, 1024>(g, s);
+    if (g.W <= 2048) return launch_values<TB, TS, 1, 8, 256>(g, s);
+    return g.W <= 8192 ? launch_values<TB, TS, 1, 8, 1024>(g, s) : launch_values<TB, TS, 1, 16, 1024>(g, s);
 }
 
 }  // namespace
