@@ -97,8 +97,16 @@ __device__ __forceinline__ float gate_of(float z, int kind)
     return kind == RTN_GATE_SIGMOID ? s : z * s;
 }
 
-// Roundings of a sum of squares: per thread, two shuffle trees, and the mean, root and quotient after it.
-template <int NV, int EV> constexpr float kRootUnits = 0.5f * (NV * EV + 10) + 5.f;
+// Roundings of a sum of squares, per thread and over two trees, of the mean and of the root (approximate: two units in the last place of 2^-23).
+template <int NV, int EV> constexpr float kRootUnits = 0.5f * (NV * EV + 10) + 6.f;
+
+// Square root of a quotient, for bounds only.
+__device__ __forceinline__ float root_of_ratio(float a, float b)
+{
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(__fdividef(a, b)));
+    return r;
+}
 
 // h and n of token t.  slack receives the bound on n's error, where kTrack asks for it.  Loads are not in branches (a value behind the row's end is
 // read from its beginning and put to zero): the compiler waited for one after the other there.
@@ -106,7 +114,7 @@ template <typename TB, typename TS, int EV, int NV, bool kTrack>
 __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* red, float (&h)[NV][EV], float (&n)[NV][EV], float (&slack)[NV][EV])
 {
     const int W = g.W, step = blockDim.x * EV, first = threadIdx.x * EV;
-    const float k_units = g.place != nullptr ? (float)g.k : 0.f;
+    const float k_units = g.place != nullptr ? (float)g.k : 0.f, mean = 1.f / (float)W;
     float zero = 0.f, ss = 0.f, sm = 0.f;
     int at[NV];                                                 // a value's column, or 0 behind the row's end
     bool in[NV];
@@ -215,14 +223,15 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
             }
         }
         block_sums(ss, kTrack ? sm : zero, red);
-        const float post = 1.f / sqrtf(ss / (float)W + g.eps);
-        if constexpr (kTrack) post_units = kRootUnits<NV, EV> + 2.f + (ss > 0.f ? k_units * sqrtf(sm / ss) : 0.f);
+        const float post = rsqrtf(fmaf(ss, mean, g.eps));
+        if constexpr (kTrack) post_units = kRootUnits<NV, EV> + 2.f + (ss > 0.f ? k_units * root_of_ratio(sm, ss) : 0.f);
         #pragma unroll
         for (int v = 0; v < NV; ++v)
             #pragma unroll
             for (int i = 0; i < EV; ++i) f[v][i] *= post;
         ss = sm = 0.f;
     }
+    const float y_units = post_units + units;
     #pragma unroll
     for (int v = 0; v < NV; ++v) {
         float r[EV];
@@ -231,10 +240,10 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
         if (g.residual != nullptr) take<TS, EV>(res[v], in[v], r);
         #pragma unroll
         for (int i = 0; i < EV; ++i) {
-            const float y = h[v][i], m = slack[v][i];
-            h[v][i] = in[v] ? fmaf(f[v][i], y, r[i]) : 0.f;
+            const float y = h[v][i], m = slack[v][i], q = in[v] ? f[v][i] : 0.f;       // (behind the row's end y, its terms and r are zeros)
+            h[v][i] = fmaf(q, y, r[i]);
             if constexpr (kTrack) {
-                slack[v][i] = in[v] ? fmaf(fabsf(f[v][i]), fmaf(k_units, m, (post_units + units) * fabsf(y)), fabsf(h[v][i])) : 0.f;
+                slack[v][i] = fmaf(fabsf(q), fmaf(k_units, m, y_units * fabsf(y)), fabsf(h[v][i]));
                 sm = fmaf(slack[v][i], slack[v][i], sm);
             }
             ss = fmaf(h[v][i], h[v][i], ss);
@@ -246,15 +255,15 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
         #pragma unroll
         for (int v = 0; v < NV; ++v) load_params<EV>(g.norm_weight, at[v], p[v]);
         block_sums(ss, kTrack ? sm : zero, red);
-        const float pre = 1.f / sqrtf(ss / (float)W + g.eps);
-        if constexpr (kTrack) pre_units = kRootUnits<NV, EV> + 4.f + (ss > 0.f ? sqrtf(sm / ss) : 0.f);
+        const float pre = rsqrtf(fmaf(ss, mean, g.eps));
+        if constexpr (kTrack) pre_units = kRootUnits<NV, EV> + 4.f + (ss > 0.f ? root_of_ratio(sm, ss) : 0.f);
         #pragma unroll
         for (int v = 0; v < NV; ++v)
             #pragma unroll
             for (int i = 0; i < EV; ++i) {
                 const float q = pre * p[v][i];
                 n[v][i] = q * h[v][i];
-                if constexpr (kTrack) slack[v][i] = fmaf(fabsf(q), slack[v][i], pre_units * fabsf(n[v][i]));
+                if constexpr (kTrack) slack[v][i] = fabsf(q) * fmaf(pre_units, fabsf(h[v][i]), slack[v][i]);
             }
     } else {
         #pragma unroll
@@ -289,7 +298,7 @@ __device__ __forceinline__ bool code_row(const NormArgs& g, const float (&n)[NV]
             up |= (uint32_t)a << (v * EV + i);
             down |= (uint32_t)b << (v * EV + i);
             const float d = fminf(fabsf(x - lo[i]), fabsf(x - hi[i]));        // (a difference that small is exact but for its own rounding)
-            near |= !(d > 1.25f * kUnit * slack[v][i]) || !(fabsf(x) < 1e37f);
+            near = near || !(d > 1.25f * kUnit * slack[v][i]);                       // (of a NaN, and of what overflowed)
         }
     }
     return near;
@@ -370,7 +379,7 @@ static __device__ __noinline__ int exact_codes(const NormArgs& g, int64_t t, dou
 }
 
 template <typename TB, typename TS, int EV, int NV, int kMaxThreads, bool kCodes>
-__global__ void __launch_bounds__(kMaxThreads, kMaxThreads == 256 ? 4 : 1)
+__global__ void __launch_bounds__(kMaxThreads, 1024 / kMaxThreads)
 block_norm_kernel(const __grid_constant__ NormArgs g)
 {
     __shared__ double red[2 * kMaxWarps];
@@ -405,9 +414,15 @@ block_norm_kernel(const __grid_constant__ NormArgs g)
                 }
             }
         }
-        float sum = (float)own, none = 0.f;                     // (whole numbers below 2^24)
-        block_sums(sum, none, reinterpret_cast<float*>(red));
-        if (threadIdx.x == 0) g.out_sum[t] = (int)sum;
+        own = __reduce_add_sync(0xffffffffu, own);
+        int* sums = reinterpret_cast<int*>(red);
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = own;
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            own = __reduce_add_sync(0xffffffffu, (int)threadIdx.x < (int)(blockDim.x >> 5) ? sums[threadIdx.x] : 0);
+            if (threadIdx.x == 0) g.out_sum[t] = own;
+        }
     }
     #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -442,7 +457,7 @@ cudaError_t launch_types(const NormArgs& g, cudaStream_t s)
     if (wide && g.W <= 2048) return launch_values<TB, TS, 8, 1, 256>(g, s);
     if (wide) return g.W <= 8192 ? launch_values<TB, TS, 8, 1, 1024>(g, s) : launch_values<TB, TS, 8, 2, 1024>(g, s);
     if (g.W <= 2048) return launch_values<TB, TS, 1, 8, 256>(g, s);
-    return g.W <= 8192 ? launch_values<TB, TS, 1, 8, 1024>(g, s) : launch_values<TB, TS, 1, 16, 1024>(g, s);
+    return g.W <= 8192 ? launch_values<TB, TS, 1, 16, 512>(g, s) : launch_values<TB, TS, 1, 16, 1024>(g, s);
 }
 
 }  // namespace

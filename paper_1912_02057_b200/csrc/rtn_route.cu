@@ -1,12 +1,15 @@
 // Choice of experts and the plan of their rows.
 //
-// route_choose_kernel: a warp takes one token at a time, lane i holding the logits of experts i, i + 32, ...  A choice is compared by a key, an
-//   unsigned number of the same order (0: not to be chosen): of the logit itself where no bias and no sum of scores is involved (softmax and
-//   sigmoid keep the order, so nothing is rounded), else of score + bias in double.  A pick is two or four warp
-//   reductions: the largest key, then the lowest expert that has it.
-//   A block takes kTokens tokens and notes who chose what in a bit per (expert, token), so that a pair's place among its expert's
-//   rows is a count of bits whatever order the warps finish in, and so are the block's counts.
-// route_plan_kernel: adds what lies before: the rows of lower experts, and of the expert's earlier blocks.  One block does both.
+// route_choose_kernel: a warp takes one token at a time, a lane VPL experts side by side.  A choice is compared by a key, an unsigned number
+//   of the same order (0: not to be chosen): of the logit itself where no bias and no sum of scores is involved (softmax and sigmoid keep the
+//   order, so nothing is rounded), else of score + bias in fp32.  There two neighbours in the order that are nearer to each other than their
+//   rounding errors make the warp choose this token's experts again in double (of ordinary tokens a few in a thousand).
+//   A pick is one warp reduction and one vote: the largest key, and the first lane that has it.  Groups are looked at all at once, a group's
+//   lanes side by side, where their sizes let them be, else one after the other.
+//   A block notes who chose what in a bit per (expert, token), so that a pair's place among its expert's rows is a count of bits
+//   whatever order the warps finish in, and so are the block's counts.
+// route_plan_kernel adds what lies before: the rows of lower experts, and of the expert's earlier blocks.  One block does both.
+// Bound: latency (a chain of about 40 clocks per pick) for few tokens, issue slots for many.
 #include "rtn_internal.cuh"
 #include "rtn_types.cuh"
 #include "rtn_tcgen05.cuh"
@@ -19,8 +22,9 @@ namespace {
 
 constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
-constexpr int kTokens = 128;                // of a block
-constexpr int kWords = kTokens / 32;
+constexpr int kMaxTokens = 128;             // of a block
+constexpr int kScanBlocks = 32;             // more: the counts are added up ahead (each block by itself reads them all)
+constexpr float kUnit = 5.9604644775390625e-8f;                // 2^-24
 
 // Numbers as unsigned of the same order, above 0.
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -28,6 +32,7 @@ __device__ __forceinline__ uint32_t key_of(float x)
     const uint32_t u = __float_as_uint(x + 0.f);               // (-0 is 0)
     return u >> 31 ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ uint64_t key_of(double x)
 {
     const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
@@ -41,33 +46,133 @@ __device__ __forceinline__ uint64_t warp_max(uint64_t k)
     const uint32_t hi = (uint32_t)(k >> 32), top = __reduce_max_sync(0xffffffffu, hi);
     return (uint64_t)top << 32 | __reduce_max_sync(0xffffffffu, hi == top ? (uint32_t)k : 0u);
 }
+__device__ __forceinline__ float warp_max(float x) { return value_of(warp_max(key_of(x))); }
 
-// The largest of the warp's keys that `mine` lets take part, and the lowest index that has it (index i * 32 + lane).
-template <int VPL, typename Key, typename Mine>
-__device__ __forceinline__ Key best_of(const Key (&key)[VPL], int lane, int& at, Mine&& mine)
+template <typename F>
+__device__ __forceinline__ F warp_sum(F x)
 {
-    Key top = 0;
+    #pragma unroll
+    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    return x;
+}
+
+// The logits of a lane's experts: NaN as -inf, +inf as the largest number.
+template <typename T, int VPL>
+__device__ __forceinline__ void read_logits(const RouteArgs& g, int64_t t, int lane, float (&x)[VPL])
+{
+    const T* row = static_cast<const T*>(g.logits) + t * g.stride + lane * VPL;
+    T raw[VPL];
+    bool vector = false;
+    if constexpr (VPL * sizeof(T) % 16 == 0) {
+        vector = g.E % VPL == 0 && (reinterpret_cast<uintptr_t>(row) & 15) == 0;
+        if (vector && lane * VPL < g.E) {
+            #pragma unroll
+            for (int i = 0; i < VPL * (int)sizeof(T) / 16; ++i) *reinterpret_cast<uint4*>(raw + i * 16 / sizeof(T)) = reinterpret_cast<const uint4*>(row)[i];
+        }
+    }
+    if (!vector) {
+        #pragma unroll
+        for (int i = 0; i < VPL; ++i) raw[i] = lane * VPL + i < g.E ? row[i] : from_f32<T>(0.f);
+    }
+    #pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        const float v = to_f32(raw[i]);
+        x[i] = lane * VPL + i < g.E && v > -INFINITY ? fminf(v, FLT_MAX) : -INFINITY;
+    }
+}
+
+// Lane j: choice j and its logit.
+struct Choice { int pick; float logit; };
+
+// The largest of the warp's keys that `mine` lets take part, and the lowest index that has it.
+template <int VPL, typename Mine>
+__device__ __forceinline__ uint64_t best_of(const uint64_t (&key)[VPL], int lane, int& at, Mine&& mine)
+{
+    uint64_t top = 0;
     #pragma unroll
     for (int i = 0; i < VPL; ++i) if (mine(i) && key[i] > top) top = key[i];
     top = warp_max(top);
     int low = 0x7fffffff;
     #pragma unroll
-    for (int i = VPL - 1; i >= 0; --i) if (mine(i) && key[i] == top) low = i * 32 + lane;
+    for (int i = VPL - 1; i >= 0; --i) if (mine(i) && key[i] == top) low = lane * VPL + i;
     at = (int)__reduce_min_sync(0xffffffffu, (unsigned)low);
     return top;
 }
 
-__device__ __forceinline__ double warp_sum(double x)
+// One token's choices in double, for any groups.
+template <typename T, int VPL>
+__device__ __noinline__ Choice choose_exact(const RouteArgs& g, int64_t t)
 {
+    const int lane = threadIdx.x & 31;
+    float x[VPL];
+    read_logits<T, VPL>(g, t, lane, x);
+    float most = -INFINITY;
     #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    return x;
-}
-__device__ __forceinline__ float warp_sum(float x)
-{
+    for (int i = 0; i < VPL; ++i) most = fmaxf(most, x[i]);
+    const double top = warp_max(most);
+    uint64_t key[VPL];
+    double s[VPL], all = 0.0;
     #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    return x;
+    for (int i = 0; i < VPL; ++i) {
+        s[i] = g.score == RTN_SCORE_SIGMOID ? 1.0 / (1.0 + exp(-(double)x[i])) : x[i] == -INFINITY ? 0.0 : exp((double)x[i] - top);
+        all += s[i];
+    }
+    all = g.score == RTN_SCORE_SIGMOID ? 1.0 : warp_sum(all);
+    const bool by_logit = g.bias == nullptr && (g.groups == 1 || g.group_top == 1);
+    #pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        const float b = g.bias != nullptr && lane * VPL + i < g.E ? g.bias[lane * VPL + i] : 0.f;
+        key[i] = x[i] > -INFINITY && b > -INFINITY ? key_of(by_logit ? (double)x[i] : s[i] / all + (double)b) : 0;
+    }
+    if (g.groups > 1) {
+        const int per_group = g.E / g.groups;
+        uint64_t value_key[1] = {0};                            // lane i: the value of group i
+        for (int gr = 0; gr < g.groups; ++gr) {
+            const int lo = gr * per_group, hi = lo + per_group;
+            int at = 0;
+            uint64_t best = best_of(key, lane, at, [&](int i) { return lane * VPL + i >= lo && lane * VPL + i < hi; });
+            if (g.group_top > 1 && best != 0) {
+                double value = value_of(best);
+                uint64_t limit = best;
+                int last = at;                                  // the picks go down by (key, index)
+                for (int n = 1; n < g.group_top; ++n) {
+                    const uint64_t next = best_of(key, lane, at, [&](int i) {
+                        const int e = lane * VPL + i;
+                        return e >= lo && e < hi && (key[i] < limit || (key[i] == limit && e > last));
+                    });
+                    if (next == 0) break;
+                    value += value_of(next);
+                    limit = next; last = at;
+                }
+                best = key_of(value);
+            }
+            if (lane == gr) value_key[0] = best;
+        }
+        uint32_t kept = 0;
+        for (int n = 0; n < g.kept; ++n) {
+            int at = 0;
+            if (best_of(value_key, lane, at, [&](int) { return true; }) == 0) break;
+            kept |= 1u << at;
+            if (lane == at) value_key[0] = 0;
+        }
+        #pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            const int e = lane * VPL + i;
+            if (e < g.E && !(kept >> (e / per_group) & 1u)) key[i] = 0;
+        }
+    }
+    Choice c{-1, -INFINITY};
+    for (int j = 0; j < g.top_k; ++j) {
+        int at = 0;
+        if (best_of(key, lane, at, [&](int) { return true; }) == 0) break;
+        float v = 0.f;
+        #pragma unroll
+        for (int i = 0; i < VPL; ++i)
+            if (lane * VPL + i == at) { v = x[i]; key[i] = 0; }
+        v = __shfl_sync(0xffffffffu, v, at / VPL);
+        if (lane == j) { c.pick = at; c.logit = v; }
+    }
+    return c;
 }
 
 // Exclusive sums of n <= kMaxExperts counts in shared memory, by one warp; the total goes to sum[n].
@@ -88,142 +193,164 @@ __device__ __forceinline__ void scan_counts(const int* count, int* sum, int n, i
     if (lane == 0) sum[n] = before;
 }
 
-// counts: [blocks][E], or NULL: no plan, or one block, which finishes it.
-template <typename T, int VPL, bool kWide>
+// What a launch is told: tokens of a block, experts of a group; whether the groups' lanes are side by side, a power of two of them (else 1).
+struct RoutePlan { int tokens, group_size, group_lanes; bool side_by_side; };
+
+// counts: [blocks][E], or NULL: no plan, or one block, which finishes it.  kScored: a bias or sums of scores.
+template <typename T, int VPL, bool kScored>
 __global__ void __launch_bounds__(kThreads)
-route_choose_kernel(const RouteArgs g, int* counts)
+route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int* counts)
 {
-    using Key = typename std::conditional<kWide, uint64_t, uint32_t>::type;
-    extern __shared__ uint32_t chosen[];                       // [E][kWords]; then count and start, [E + 1] each
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t t0 = (int64_t)blockIdx.x * kTokens;
-    const int n_tok = g.T - t0 < kTokens ? (int)(g.T - t0) : kTokens;
+    extern __shared__ uint32_t chosen[];                       // [E][words]; then count and start, [E + 1] each
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, words = (p.tokens + 31) / 32;
+    const int64_t t0 = (int64_t)blockIdx.x * p.tokens;
+    const int n_tok = g.T - t0 < p.tokens ? (int)(g.T - t0) : p.tokens;
     const bool plan = g.start != nullptr;
     const int k = g.top_k;
+    float bias[VPL];
+    #pragma unroll
+    for (int i = 0; i < VPL; ++i) bias[i] = kScored && g.bias != nullptr && lane * VPL + i < g.E ? g.bias[lane * VPL + i] : 0.f;
     if (plan) {
-        for (int i = threadIdx.x; i < g.E * kWords; i += kThreads) chosen[i] = 0;
+        for (int i = threadIdx.x; i < g.E * words; i += kThreads) chosen[i] = 0;
         __syncthreads();
     }
-    const int per_group = g.E / g.groups;
     for (int t = warp; t < n_tok; t += kWarps) {
-        const T* row = static_cast<const T*>(g.logits) + (t0 + t) * g.stride;
         float x[VPL];
-        Key key[VPL];
-        #pragma unroll
-        for (int i = 0; i < VPL; ++i) x[i] = i * 32 + lane < g.E ? to_f32(row[i * 32 + lane]) : -INFINITY;
-        float top = -INFINITY;
-        #pragma unroll
-        for (int i = 0; i < VPL; ++i) {
-            if (!(x[i] > -INFINITY)) x[i] = -INFINITY;         // NaN
-            x[i] = fminf(x[i], FLT_MAX);
-            top = fmaxf(top, x[i]);
+        read_logits<T, VPL>(g, t0 + t, lane, x);
+        float top = -INFINITY, sum = 1.f;                       // of a softmax over all experts
+        uint32_t key[VPL];
+        float slack = 0.f;                                      // how far a c (of this lane's) may be off
+        if (g.score == RTN_SCORE_SOFTMAX && (kScored || !g.renormalise)) {
+            #pragma unroll
+            for (int i = 0; i < VPL; ++i) top = fmaxf(top, x[i]);
+            top = warp_max(top);
+            float all = 0.f;
+            #pragma unroll
+            for (int i = 0; i < VPL; ++i) all += x[i] > -INFINITY ? __expf(x[i] - top) : 0.f;
+            sum = warp_sum(all);
         }
-        {
-            const uint32_t u = warp_max(key_of(top));
-            top = __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u);
-        }
-        float sum = 1.f;                                        // of a softmax over all experts
-        if constexpr (kWide) {
-            double s[VPL], all = 0.0;
+        if constexpr (kScored) {
+            // A score's error in units of 2^-24.  Sigmoid: (2 |x| + 4) (1 - s) s for the exponential, 4 s for sum and reciprocal.  Softmax with
+            // d = top - x: (2 d + 4) s <= 5, the sum's (VPL + 5 adds of terms with as much) and the quotient's 4.
+            const float units = g.score == RTN_SCORE_SIGMOID ? 8.f : (float)VPL + 24.f;
+            const float inverse = 1.f / sum;
             #pragma unroll
             for (int i = 0; i < VPL; ++i) {
-                s[i] = g.score == RTN_SCORE_SIGMOID ? 1.0 / (1.0 + exp(-(double)x[i])) : x[i] == -INFINITY ? 0.0 : exp((double)x[i] - (double)top);
-                all += s[i];
+                const float s = g.score == RTN_SCORE_SIGMOID ? __fdividef(1.f, 1.f + __expf(-x[i])) : __expf(x[i] - top) * inverse;
+                key[i] = x[i] > -INFINITY && bias[i] > -INFINITY ? key_of(s + bias[i]) : 0;
+                if (key[i] != 0) slack = fmaxf(slack, fabsf(bias[i]));
             }
-            all = g.score == RTN_SCORE_SIGMOID ? 1.0 : warp_sum(all);
-            sum = (float)all;
-            #pragma unroll
-            for (int i = 0; i < VPL; ++i) {
-                const float b = g.bias != nullptr && i * 32 + lane < g.E ? g.bias[i * 32 + lane] : 0.f;
-                key[i] = x[i] > -INFINITY && b > -INFINITY ? key_of(s[i] / all + (double)b) : 0;
-            }
+            slack = kUnit * (units + 2.f) * 1.25f * (1.f + warp_max(slack));
         } else {
             #pragma unroll
             for (int i = 0; i < VPL; ++i) key[i] = x[i] > -INFINITY ? key_of(x[i]) : 0;
-            if (g.score == RTN_SCORE_SOFTMAX && !g.renormalise) {
-                float all = 0.f;
+        }
+        bool unsure = g.groups > 1 && g.group_top > 2;
+        if (g.groups > 1 && !unsure) {
+            uint32_t a = 0, b = 0;                              // the largest and second largest of this lane's group
+            int mine = lane / p.group_lanes;
+            if (p.side_by_side) {
                 #pragma unroll
-                for (int i = 0; i < VPL; ++i) all += x[i] > -INFINITY ? expf(x[i] - top) : 0.f;
-                sum = warp_sum(all);
-            }
-        }
-        if (g.groups > 1) {
-            Key mine[1] = {0};                                  // lane i: the value of group i
-            for (int gr = 0; gr < g.groups; ++gr) {
-                const int lo = gr * per_group, hi = lo + per_group;
-                int at = 0;
-                Key best = best_of(key, lane, at, [&](int i) { return i * 32 + lane >= lo && i * 32 + lane < hi; });
-                if constexpr (kWide) {
-                    if (g.group_top > 1 && best != 0) {
-                        double value = value_of(best);
-                        uint64_t limit = best;
-                        int last = at;                          // the picks go down by (key, index)
-                        for (int n = 1; n < g.group_top; ++n) {
-                            const uint64_t next = best_of(key, lane, at, [&](int i) {
-                                const int e = i * 32 + lane;
-                                return e >= lo && e < hi && (key[i] < limit || (key[i] == limit && e > last));
-                            });
-                            if (next == 0) break;
-                            value += value_of(next);
-                            limit = next; last = at;
-                        }
-                        best = key_of(value);
-                    }
+                for (int i = 0; i < VPL; ++i) {
+                    b = max(b, min(a, key[i]));
+                    a = max(a, key[i]);
                 }
-                if (lane == gr) mine[0] = best;
+                for (int d = 1; d < p.group_lanes; d <<= 1) {
+                    const uint32_t c = __shfl_xor_sync(0xffffffffu, a, d), e = __shfl_xor_sync(0xffffffffu, b, d);
+                    b = max(max(b, e), min(a, c));
+                    a = max(a, c);
+                }
+            } else {                                            // one group after the other; lane i has group i
+                mine = lane;
+                for (int gr = 0, lo = -lane * VPL; gr < g.groups; ++gr, lo += p.group_size) {
+                    uint32_t c = 0, e = 0;
+                    #pragma unroll
+                    for (int i = 0; i < VPL; ++i)
+                        if (i >= lo && i < lo + p.group_size) { e = max(e, min(c, key[i])); c = max(c, key[i]); }
+                    const uint32_t first = warp_max(c);
+                    const int from = __ffs(__ballot_sync(0xffffffffu, c == first)) - 1;
+                    const uint32_t second = warp_max(lane == from ? e : c);
+                    if (lane == gr) { a = first; b = second; }
+                }
             }
-            uint32_t kept = 0;
+            if (g.group_top == 2 && b != 0) a = key_of(value_of(a) + value_of(b));
+            if (mine >= g.groups) a = 0;
+            uint32_t last = 0, kept = 0;                        // a bit per group
             for (int n = 0; n < g.kept; ++n) {
-                int at = 0;
-                if (best_of(mine, lane, at, [&](int) { return true; }) == 0) break;
-                kept |= 1u << at;
-                if (lane == at) mine[0] = 0;
+                last = warp_max(a);
+                if (last == 0) break;
+                const int first = (__ffs(__ballot_sync(0xffffffffu, a == last)) - 1) / p.group_lanes;
+                kept |= 1u << first;
+                if (first == mine) a = 0;
             }
-            #pragma unroll
-            for (int i = 0; i < VPL; ++i) {
-                const int e = i * 32 + lane;
-                if (e < g.E && !(kept >> (e / per_group) & 1u)) key[i] = 0;
+            if constexpr (kScored) {
+                const uint32_t next = warp_max(a);              // the best that was left
+                if (last != 0 && next != 0) unsure = !(value_of(last) - value_of(next) > 6.f * slack + 2.f * kUnit * fabsf(value_of(last)));
             }
-        }
-        int pick = -1;                                          // lane j: choice j and its logit
-        float logit = -INFINITY;
-        for (int j = 0; j < k; ++j) {
-            int at = 0;
-            if (best_of(key, lane, at, [&](int) { return true; }) == 0) break;
-            float v = 0.f;
             #pragma unroll
             for (int i = 0; i < VPL; ++i)
-                if (i * 32 + lane == at) { v = x[i]; key[i] = 0; }
-            v = __shfl_sync(0xffffffffu, v, at & 31);
-            if (lane == j) { pick = at; logit = v; }
+                if (!(kept >> (p.side_by_side ? mine & 31 : (lane * VPL + i) / p.group_size & 31) & 1u)) key[i] = 0;
         }
+        Choice c{-1, -INFINITY};
+        if (!unsure) {
+            uint32_t best = 0, last = 0;
+            #pragma unroll
+            for (int i = 0; i < VPL; ++i) best = max(best, key[i]);
+            for (int j = 0; j < k; ++j) {
+                const uint32_t now = warp_max(best);
+                if (now == 0) { last = 0; break; }
+                if constexpr (kScored) {
+                    if (j > 0) unsure = unsure || !(value_of(last) - value_of(now) > 2.f * slack);
+                    last = now;
+                }
+                const int from = __ffs(__ballot_sync(0xffffffffu, best == now)) - 1;      // the lowest index is the first lane's first
+                int at = 0;
+                float v = 0.f;
+                if (lane == from) {
+                    best = 0;
+                    bool found = false;
+                    #pragma unroll
+                    for (int i = 0; i < VPL; ++i) {
+                        if (!found && key[i] == now) { found = true; at = lane * VPL + i; v = x[i]; key[i] = 0; }
+                        best = max(best, key[i]);
+                    }
+                }
+                at = __shfl_sync(0xffffffffu, at, from);
+                v = __shfl_sync(0xffffffffu, v, from);
+                if (lane == j) { c.pick = at; c.logit = v; }
+            }
+            if constexpr (kScored) {
+                const uint32_t next = warp_max(best);
+                if (last != 0 && next != 0) unsure = unsure || !(value_of(last) - value_of(next) > 2.f * slack);
+            }
+        }
+        if (unsure) c = choose_exact<T, VPL>(g, t0 + t);
         float w = 0.f;
         if (g.renormalise) {
             // s up to a factor that all choices share, so that scores too small for fp32 still have their ratios
-            const uint32_t u = warp_max(key_of(logit));
-            const float best = __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u);
-            if (pick >= 0)
-                w = g.score == RTN_SCORE_SOFTMAX ? expf(logit - best) : expf(fminf(logit, 0.f) - fminf(best, 0.f)) / (1.f + expf(-fabsf(logit)));
+            const float best = warp_max(c.logit);
+            if (c.pick >= 0)
+                w = g.score == RTN_SCORE_SOFTMAX ? expf(c.logit - best) : expf(fminf(c.logit, 0.f) - fminf(best, 0.f)) / (1.f + expf(-fabsf(c.logit)));
             const float all = warp_sum(w);
-            if (pick >= 0) w /= all;
-        } else if (pick >= 0) {
-            w = g.score == RTN_SCORE_SOFTMAX ? expf(logit - top) / sum : 1.f / (1.f + expf(-logit));
+            if (c.pick >= 0) w /= all;
+        } else if (c.pick >= 0) {
+            w = g.score == RTN_SCORE_SOFTMAX ? expf(c.logit - top) / sum : 1.f / (1.f + expf(-c.logit));
         }
         if (lane < k) {
-            g.experts[(t0 + t) * k + lane] = pick;
+            g.experts[(t0 + t) * k + lane] = c.pick;
             g.weights[(t0 + t) * k + lane] = w * g.scale;
-            if (plan && pick >= 0) atomicOr(&chosen[pick * kWords + (t >> 5)], 1u << (t & 31));
+            if (plan && c.pick >= 0) atomicOr(&chosen[c.pick * words + (t >> 5)], 1u << (t & 31));
         }
     }
     if (!plan) return;
-    int* count = reinterpret_cast<int*>(chosen + g.E * kWords);
+    tc::pdl_trigger();
+    int* count = reinterpret_cast<int*>(chosen + g.E * words);
     int* start = count + g.E + 1;
     __syncthreads();
     const bool alone = counts == nullptr;
     for (int e = threadIdx.x; e < g.E; e += kThreads) {
         int n = 0;
-        #pragma unroll
-        for (int i = 0; i < kWords; ++i) n += __popc(chosen[e * kWords + i]);
+        for (int i = 0; i < words; ++i) n += __popc(chosen[e * words + i]);
         count[e] = n;
         if (!alone) counts[(int64_t)blockIdx.x * g.E + e] = n;
     }
@@ -238,43 +365,76 @@ route_choose_kernel(const RouteArgs g, int* counts)
         int at = -1;
         if (e >= 0) {
             at = 0;
-            for (int j = 0; j < (t >> 5); ++j) at += __popc(chosen[e * kWords + j]);
-            at += __popc(chosen[e * kWords + (t >> 5)] & ((1u << (t & 31)) - 1u));
+            for (int j = 0; j < (t >> 5); ++j) at += __popc(chosen[e * words + j]);
+            at += __popc(chosen[e * words + (t >> 5)] & ((1u << (t & 31)) - 1u));
             if (alone) { at += start[e]; g.tokens[at] = (int)(t0 + t); }
         }
         g.place[t0 * k + i] = at;
     }
-    tc::pdl_trigger();
 }
 
+// One expert's counts of all blocks as sums of those before; the total goes behind the last block's.
+__global__ void __launch_bounds__(256)
+route_scan_kernel(int E, int* counts, int64_t blocks)
+{
+    __shared__ int part[8];
+    const int e = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    tc::pdl_wait();
+    int before = 0;
+    for (int64_t b0 = 0; b0 < blocks; b0 += 256) {
+        const int64_t b = b0 + threadIdx.x;
+        const int c = b < blocks ? counts[b * E + e] : 0;
+        int x = c;
+        #pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
+        }
+        if (lane == 31) part[warp] = x;
+        __syncthreads();
+        int own = 0, all = 0;
+        #pragma unroll
+        for (int i = 0; i < 8; ++i) { own += i < warp ? part[i] : 0; all += part[i]; }
+        if (b < blocks) counts[b * E + e] = before + own + x - c;
+        before += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) counts[blocks * E + e] = before;
+}
+
+// scanned: counts are route_scan_kernel's.
 __global__ void __launch_bounds__(kThreads)
-route_plan_kernel(const RouteArgs g, const int* counts, int blocks)
+route_plan_kernel(const RouteArgs g, const int* counts, int64_t blocks, int tokens, bool scanned)
 {
     extern __shared__ int sums[];                               // total, before, start: [E + 1] each
     int *total = sums, *before = sums + g.E + 1, *start = before + g.E + 1;
     for (int e = threadIdx.x; e < g.E; e += kThreads) total[e] = before[e] = 0;
     tc::pdl_wait();
     __syncthreads();
-    const int parts = g.E < kThreads ? kThreads / g.E : 1;
-    for (int i = threadIdx.x; i < g.E * parts; i += kThreads) {
-        const int e = i % g.E, p = i / g.E;
-        int a = 0, b = 0;
-        #pragma unroll 8
-        for (int j = p; j < blocks; j += parts) {
-            const int c = counts[(int64_t)j * g.E + e];
-            a += c;
-            b += j < (int)blockIdx.x ? c : 0;
+    if (scanned) {
+        for (int e = threadIdx.x; e < g.E; e += kThreads) { total[e] = counts[blocks * g.E + e]; before[e] = counts[(int64_t)blockIdx.x * g.E + e]; }
+    } else {
+        const int parts = g.E < kThreads ? kThreads / g.E : 1;
+        for (int i = threadIdx.x; i < g.E * parts; i += kThreads) {
+            const int e = i % g.E, p = i / g.E;
+            int a = 0, b = 0;
+            #pragma unroll 16
+            for (int j = p; j < (int)blocks; j += parts) {
+                const int c = counts[(int64_t)j * g.E + e];
+                a += c;
+                b += j < (int)blockIdx.x ? c : 0;
+            }
+            atomicAdd(&total[e], a);
+            atomicAdd(&before[e], b);
         }
-        atomicAdd(&total[e], a);
-        atomicAdd(&before[e], b);
     }
     __syncthreads();
     if (threadIdx.x < 32) scan_counts(total, start, g.E, threadIdx.x);
     __syncthreads();
     if (blockIdx.x == 0)
         for (int e = threadIdx.x; e <= g.E; e += kThreads) g.start[e] = start[e];
-    const int64_t t0 = (int64_t)blockIdx.x * kTokens;
-    const int k = g.top_k, n = (int)((g.T - t0 < kTokens ? g.T - t0 : kTokens) * k);
+    const int64_t t0 = (int64_t)blockIdx.x * tokens;
+    const int k = g.top_k, n = (int)((g.T - t0 < tokens ? g.T - t0 : tokens) * k);
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const int e = g.experts[t0 * k + i];
         if (e < 0) continue;
@@ -285,12 +445,16 @@ route_plan_kernel(const RouteArgs g, const int* counts, int blocks)
 }
 
 template <typename T, int VPL>
-cudaError_t launch_choose(const RouteArgs& g, int* counts, unsigned blocks, cudaStream_t s)
+cudaError_t launch_choose(const RouteArgs& g, RoutePlan p, int* counts, unsigned blocks, cudaStream_t s)
 {
-    const size_t smem = g.start != nullptr ? (size_t)g.E * kWords * 4 + 2 * (g.E + 1) * 4 : 0;
+    p.group_size = g.E / g.groups;
+    const int lanes = p.group_size / VPL;
+    p.side_by_side = p.group_size % VPL == 0 && (lanes & (lanes - 1)) == 0;
+    p.group_lanes = p.side_by_side ? lanes : 1;
+    const size_t smem = g.start != nullptr ? (size_t)g.E * ((p.tokens + 31) / 32) * 4 + 2 * (g.E + 1) * 4 : 0;
     // scores have to be computed where a bias or a sum of them is compared
-    if (g.bias != nullptr || (g.groups > 1 && g.group_top > 1)) route_choose_kernel<T, VPL, true><<<blocks, kThreads, smem, s>>>(g, counts);
-    else route_choose_kernel<T, VPL, false><<<blocks, kThreads, smem, s>>>(g, counts);
+    if (g.bias != nullptr || (g.groups > 1 && g.group_top > 1)) route_choose_kernel<T, VPL, true><<<blocks, kThreads, smem, s>>>(g, p, counts);
+    else route_choose_kernel<T, VPL, false><<<blocks, kThreads, smem, s>>>(g, p, counts);
     return cudaGetLastError();
 }
 
@@ -299,24 +463,39 @@ cudaError_t launch_choose(const RouteArgs& g, int* counts, unsigned blocks, cuda
 cudaError_t launch_route_experts(const RouteArgs& g, cudaStream_t s)
 {
     if (g.T == 0) return cudaMemsetAsync(g.start, 0, (size_t)(g.E + 1) * sizeof(int32_t), s);
-    const int64_t blocks = (g.T + kTokens - 1) / kTokens;
+    // A token to each warp while there are few (a token's chain is what counts), more with more, so that about two blocks to an SM hold them
+    RoutePlan p{kWarps, 0, 1, false};
+    while (p.tokens < kMaxTokens && g.T > (int64_t)2 * device_sm_count() * p.tokens) p.tokens *= 2;
+    const int64_t blocks = (g.T + p.tokens - 1) / p.tokens;
+    const bool scanned = blocks > kScanBlocks;
     void* counts = nullptr;
     if (g.start != nullptr && blocks > 1) {
-        const cudaError_t e = scratch_alloc(&counts, (size_t)blocks * g.E * sizeof(int), s);
+        const cudaError_t e = scratch_alloc(&counts, (size_t)(blocks + 1) * g.E * sizeof(int), s);
         if (e != cudaSuccess) return e;
     }
     int* c = static_cast<int*>(counts);
     cudaError_t e = with_dtype(g.dtype, [&](auto t) {
         using T = decltype(t);
-        if (g.E <= 32) return launch_choose<T, 1>(g, c, (unsigned)blocks, s);
-        if (g.E <= 64) return launch_choose<T, 2>(g, c, (unsigned)blocks, s);
-        if (g.E <= 128) return launch_choose<T, 4>(g, c, (unsigned)blocks, s);
-        if (g.E <= 256) return launch_choose<T, 8>(g, c, (unsigned)blocks, s);
-        if (g.E <= 512) return launch_choose<T, 16>(g, c, (unsigned)blocks, s);
-        return launch_choose<T, 32>(g, c, (unsigned)blocks, s);
+        if (g.E <= 32) return launch_choose<T, 1>(g, p, c, (unsigned)blocks, s);
+        if (g.E <= 64) return launch_choose<T, 2>(g, p, c, (unsigned)blocks, s);
+        if (g.E <= 128) return launch_choose<T, 4>(g, p, c, (unsigned)blocks, s);
+        if (g.E <= 256) return launch_choose<T, 8>(g, p, c, (unsigned)blocks, s);
+        if (g.E <= 512) return launch_choose<T, 16>(g, p, c, (unsigned)blocks, s);
+        return launch_choose<T, 32>(g, p, c, (unsigned)blocks, s);
     });
-    if (e == cudaSuccess && counts != nullptr)
-        e = launch_pdl(route_plan_kernel, dim3((unsigned)blocks), dim3(kThreads), (size_t)3 * (g.E + 1) * sizeof(int), s, g, (const int*)counts, (int)blocks);
+    if (e == cudaSuccess && counts != nullptr) {
+        const size_t smem = (size_t)3 * (g.E + 1) * sizeof(int);
+        if (scanned) {
+            e = launch_pdl(route_scan_kernel, dim3((unsigned)g.E), dim3(256), 0, s, g.E, c, blocks);
+            // (not overlapped: it reads what the kernel before the last one has written)
+            if (e == cudaSuccess) {
+                route_plan_kernel<<<(unsigned)blocks, kThreads, smem, s>>>(g, c, blocks, p.tokens, true);
+                e = cudaGetLastError();
+            }
+        } else {
+            e = launch_pdl(route_plan_kernel, dim3((unsigned)blocks), dim3(kThreads), smem, s, g, (const int*)counts, blocks, p.tokens, false);
+        }
+    }
     if (counts != nullptr) {
         const cudaError_t e2 = cudaFreeAsync(counts, s);
         if (e == cudaSuccess) e = e2;

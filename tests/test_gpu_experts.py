@@ -544,3 +544,35 @@ def test_block_norm_refusals():
     want, got = f(**a), f(**a, stream=s)
     s.synchronize()
     assert torch.equal(want.stream, got.stream)
+
+
+@pytest.mark.parametrize("W", [136, 1003], ids=ids)
+def test_block_norm_infinite_parameters_stay_in_their_column(W):
+    """What the first column is multiplied with reaches no other one, whatever stands behind the row's end."""
+    a = norm_case(3, W, 0, 4, torch.float32, torch.float32)
+    a["scale"][0] = float("inf")
+    a["norm_weight"] = None
+    r = rtn.rtn_block_norm(**a)
+    assert bool(r.stream[:, 0].isinf().all()) and bool(r.stream[:, 1:].isfinite().all())
+    a["norm_weight"] = torch.ones(W, device="cuda")
+    n = rtn.rtn_block_norm(**a, normed=True).normed
+    assert bool(n[:, 0].isnan().all()) and bool((n[:, 1:] == 0).all())
+
+
+def test_route_many_tokens():
+    """More blocks than one launch adds up, tokens of a block up to the most, and the choices of a few rows."""
+    T, E, k = 80000, 32, 2
+    x = torch.randn(T, E, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    x[::7, :3] = float("-inf")
+    r = rtn.rtn_route_experts(x, k)
+    order = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(r.experts.long(), order)
+    flat = order.flatten()
+    at = torch.sort(flat, stable=True).indices
+    assert torch.equal(r.tokens.long(), at // k) and torch.equal(r.place.flatten()[at].long(), torch.arange(T * k, device="cuda"))
+    assert torch.equal(r.start[1:].long(), torch.bincount(flat, minlength=E).cumsum(0)) and int(r.start[0]) == 0
+    for T in (16, 17, 4000, 10000, 40000):
+        s = rtn.rtn_route_experts(x[:T], k)
+        assert torch.equal(s.experts, r.experts[:T]) and torch.equal(s.start[1:].long(), torch.bincount(flat[:T * k], minlength=E).cumsum(0))
+        at = torch.sort(flat[:T * k], stable=True).indices
+        assert torch.equal(s.tokens.long(), at // k)
