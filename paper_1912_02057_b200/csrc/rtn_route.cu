@@ -15,6 +15,7 @@
 #include "rtn_tcgen05.cuh"
 
 #include <float.h>
+#include <type_traits>
 
 namespace rtn {
 
@@ -23,6 +24,8 @@ namespace {
 constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
 constexpr int kMaxTokens = 128;             // of a block
+constexpr int kList = 8, kListThreads = 64; // a thread's list of a token's best; tokens of its block
+constexpr int64_t kListTokens = 4096;       // from here on
 constexpr int kScanBlocks = 32;             // more: the counts are added up ahead (each block by itself reads them all)
 constexpr float kUnit = 5.9604644775390625e-8f;                // 2^-24
 
@@ -56,24 +59,30 @@ __device__ __forceinline__ F warp_sum(F x)
     return x;
 }
 
-// The logits of a lane's experts: NaN as -inf, +inf as the largest number.
+// The logits of a lane's experts as they are in memory, asked for ahead.
 template <typename T, int VPL>
-__device__ __forceinline__ void read_logits(const RouteArgs& g, int64_t t, int lane, float (&x)[VPL])
+__device__ __forceinline__ void ask_logits(const RouteArgs& g, int64_t t, int lane, T (&raw)[VPL])
 {
     const T* row = static_cast<const T*>(g.logits) + t * g.stride + lane * VPL;
-    T raw[VPL];
-    bool vector = false;
-    if constexpr (VPL * sizeof(T) % 16 == 0) {
-        vector = g.E % VPL == 0 && (reinterpret_cast<uintptr_t>(row) & 15) == 0;
-        if (vector && lane * VPL < g.E) {
+    constexpr int kBytes = VPL * (int)sizeof(T), kVec = kBytes % 16 == 0 ? 16 : kBytes % 8 == 0 ? 8 : kBytes % 4 == 0 ? 4 : 2;
+    if (kVec > (int)sizeof(T) && g.E % VPL == 0 && (reinterpret_cast<uintptr_t>(row) & (kVec - 1)) == 0) {
+        if (lane * VPL < g.E) {
             #pragma unroll
-            for (int i = 0; i < VPL * (int)sizeof(T) / 16; ++i) *reinterpret_cast<uint4*>(raw + i * 16 / sizeof(T)) = reinterpret_cast<const uint4*>(row)[i];
+            for (int i = 0; i < kBytes / kVec; ++i) {
+                if constexpr (kVec == 16) reinterpret_cast<uint4*>(raw)[i] = reinterpret_cast<const uint4*>(row)[i];
+                else if constexpr (kVec == 8) reinterpret_cast<uint2*>(raw)[i] = reinterpret_cast<const uint2*>(row)[i];
+                else if constexpr (kVec == 4) reinterpret_cast<uint32_t*>(raw)[i] = reinterpret_cast<const uint32_t*>(row)[i];
+            }
         }
-    }
-    if (!vector) {
+    } else {
         #pragma unroll
-        for (int i = 0; i < VPL; ++i) raw[i] = lane * VPL + i < g.E ? row[i] : from_f32<T>(0.f);
+        for (int i = 0; i < VPL; ++i) raw[i] = row[lane * VPL + i < g.E ? i : -lane * VPL];           // (behind the last: the first)
     }
+}
+// NaN as -inf, +inf as the largest number.
+template <typename T, int VPL>
+__device__ __forceinline__ void take_logits(const RouteArgs& g, int lane, const T (&raw)[VPL], float (&x)[VPL])
+{
     #pragma unroll
     for (int i = 0; i < VPL; ++i) {
         const float v = to_f32(raw[i]);
@@ -105,7 +114,9 @@ __device__ __noinline__ Choice choose_exact(const RouteArgs& g, int64_t t)
 {
     const int lane = threadIdx.x & 31;
     float x[VPL];
-    read_logits<T, VPL>(g, t, lane, x);
+    alignas(16) T raw[VPL];
+    ask_logits<T, VPL>(g, t, lane, raw);
+    take_logits<T, VPL>(g, lane, raw, x);
     float most = -INFINITY;
     #pragma unroll
     for (int i = 0; i < VPL; ++i) most = fmaxf(most, x[i]);
@@ -193,8 +204,43 @@ __device__ __forceinline__ void scan_counts(const int* count, int* sum, int n, i
     if (lane == 0) sum[n] = before;
 }
 
-// What a launch is told: tokens of a block, experts of a group; whether the groups' lanes are side by side, a power of two of them (else 1).
-struct RoutePlan { int tokens, group_size, group_lanes; bool side_by_side; };
+// The block's part of the plan, from who chose what: counts: [blocks][E], or NULL: there is one block, which finishes it.  Behind the choices and their
+// notes, called by all.  chosen: [E][words]; behind it count and start, [E + 1] each.
+__device__ __forceinline__ void note_block(const RouteArgs& g, uint32_t* chosen, int64_t t0, int n_tok, int words, int* counts)
+{
+    tc::pdl_trigger();
+    const int k = g.top_k, threads = (int)blockDim.x;
+    int* count = reinterpret_cast<int*>(chosen + g.E * words);
+    int* start = count + g.E + 1;
+    __syncthreads();
+    const bool alone = counts == nullptr;
+    for (int e = threadIdx.x; e < g.E; e += threads) {
+        int n = 0;
+        for (int i = 0; i < words; ++i) n += __popc(chosen[e * words + i]);
+        count[e] = n;
+        if (!alone) counts[(int64_t)blockIdx.x * g.E + e] = n;
+    }
+    if (alone) {
+        __syncthreads();
+        if (threadIdx.x < 32) scan_counts(count, start, g.E, threadIdx.x);
+        __syncthreads();
+        for (int e = threadIdx.x; e <= g.E; e += threads) g.start[e] = start[e];
+    }
+    for (int i = threadIdx.x; i < n_tok * k; i += threads) {
+        const int t = i / k, e = g.experts[t0 * k + i];
+        int at = -1;
+        if (e >= 0) {
+            at = 0;
+            for (int j = 0; j < (t >> 5); ++j) at += __popc(chosen[e * words + j]);
+            at += __popc(chosen[e * words + (t >> 5)] & ((1u << (t & 31)) - 1u));
+            if (alone) { at += start[e]; g.tokens[at] = (int)(t0 + t); }
+        }
+        g.place[t0 * k + i] = at;
+    }
+}
+
+// What a launch is told: tokens of a block, experts of a group; whether the groups' lanes are side by side, 2^group_shift of them (else 1).
+struct RoutePlan { int tokens, group_size, group_shift; bool side_by_side; };
 
 // counts: [blocks][E], or NULL: no plan, or one block, which finishes it.  kScored: a bias or sums of scores.
 template <typename T, int VPL, bool kScored>
@@ -214,9 +260,12 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
         for (int i = threadIdx.x; i < g.E * words; i += kThreads) chosen[i] = 0;
         __syncthreads();
     }
+    alignas(16) T raw[VPL];
+    if (warp < n_tok) ask_logits<T, VPL>(g, t0 + warp, lane, raw);
     for (int t = warp; t < n_tok; t += kWarps) {
         float x[VPL];
-        read_logits<T, VPL>(g, t0 + t, lane, x);
+        take_logits<T, VPL>(g, lane, raw, x);
+        if (t + kWarps < n_tok) ask_logits<T, VPL>(g, t0 + t + kWarps, lane, raw);
         float top = -INFINITY, sum = 1.f;                       // of a softmax over all experts
         uint32_t key[VPL];
         float slack = 0.f;                                      // how far a c (of this lane's) may be off
@@ -230,17 +279,17 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
             sum = warp_sum(all);
         }
         if constexpr (kScored) {
-            // A score's error in units of 2^-24.  Sigmoid: (2 |x| + 4) (1 - s) s for the exponential, 4 s for sum and reciprocal.  Softmax with
+            // A score's error in units of 2^-24.  Sigmoid: (2 |x| + 4) (1 - s) s <= 1.5 for the exponential, 2 s for sum and quotient.  Softmax with
             // d = top - x: (2 d + 4) s <= 5, the sum's (VPL + 5 adds of terms with as much) and the quotient's 4.
-            const float units = g.score == RTN_SCORE_SIGMOID ? 8.f : (float)VPL + 24.f;
+            const float units = g.score == RTN_SCORE_SIGMOID ? 3.5f : (float)VPL + 24.f;
             const float inverse = 1.f / sum;
             #pragma unroll
             for (int i = 0; i < VPL; ++i) {
-                const float s = g.score == RTN_SCORE_SIGMOID ? __fdividef(1.f, 1.f + __expf(-x[i])) : __expf(x[i] - top) * inverse;
+                const float s = g.score == RTN_SCORE_SIGMOID ? 1.f / (1.f + __expf(-x[i])) : __expf(x[i] - top) * inverse;
                 key[i] = x[i] > -INFINITY && bias[i] > -INFINITY ? key_of(s + bias[i]) : 0;
                 if (key[i] != 0) slack = fmaxf(slack, fabsf(bias[i]));
             }
-            slack = kUnit * (units + 2.f) * 1.25f * (1.f + warp_max(slack));
+            slack = kUnit * (units + 1.f) * 1.1f * (1.f + warp_max(slack));
         } else {
             #pragma unroll
             for (int i = 0; i < VPL; ++i) key[i] = x[i] > -INFINITY ? key_of(x[i]) : 0;
@@ -248,14 +297,14 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
         bool unsure = g.groups > 1 && g.group_top > 2;
         if (g.groups > 1 && !unsure) {
             uint32_t a = 0, b = 0;                              // the largest and second largest of this lane's group
-            int mine = lane / p.group_lanes;
+            int mine = lane >> p.group_shift;
             if (p.side_by_side) {
                 #pragma unroll
                 for (int i = 0; i < VPL; ++i) {
                     b = max(b, min(a, key[i]));
                     a = max(a, key[i]);
                 }
-                for (int d = 1; d < p.group_lanes; d <<= 1) {
+                for (int d = 1; d < 1 << p.group_shift; d <<= 1) {
                     const uint32_t c = __shfl_xor_sync(0xffffffffu, a, d), e = __shfl_xor_sync(0xffffffffu, b, d);
                     b = max(max(b, e), min(a, c));
                     a = max(a, c);
@@ -279,7 +328,7 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
             for (int n = 0; n < g.kept; ++n) {
                 last = warp_max(a);
                 if (last == 0) break;
-                const int first = (__ffs(__ballot_sync(0xffffffffu, a == last)) - 1) / p.group_lanes;
+                const int first = (__ffs(__ballot_sync(0xffffffffu, a == last)) - 1) >> p.group_shift;
                 kept |= 1u << first;
                 if (first == mine) a = 0;
             }
@@ -303,21 +352,19 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
                     if (j > 0) unsure = unsure || !(value_of(last) - value_of(now) > 2.f * slack);
                     last = now;
                 }
-                const int from = __ffs(__ballot_sync(0xffffffffu, best == now)) - 1;      // the lowest index is the first lane's first
-                int at = 0;
-                float v = 0.f;
-                if (lane == from) {
-                    best = 0;
-                    bool found = false;
-                    #pragma unroll
-                    for (int i = 0; i < VPL; ++i) {
-                        if (!found && key[i] == now) { found = true; at = lane * VPL + i; v = x[i]; key[i] = 0; }
-                        best = max(best, key[i]);
-                    }
+                // the lowest index is the first lane's first; every lane looks for its own, without branches
+                const int from = __ffs(__ballot_sync(0xffffffffu, best == now)) - 1;
+                uint32_t same = 0;
+                #pragma unroll
+                for (int i = 0; i < VPL; ++i) same |= (uint32_t)(key[i] == now) << i;
+                const int own = __ffs(same) - 1, at = __shfl_sync(0xffffffffu, lane * VPL + own, from);
+                best = 0;
+                #pragma unroll
+                for (int i = 0; i < VPL; ++i) {
+                    if (lane == from && i == own) key[i] = 0;
+                    best = max(best, key[i]);
                 }
-                at = __shfl_sync(0xffffffffu, at, from);
-                v = __shfl_sync(0xffffffffu, v, from);
-                if (lane == j) { c.pick = at; c.logit = v; }
+                if (lane == j) c.pick = at;
             }
             if constexpr (kScored) {
                 const uint32_t next = warp_max(best);
@@ -325,6 +372,7 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
             }
         }
         if (unsure) c = choose_exact<T, VPL>(g, t0 + t);
+        else if (c.pick >= 0) c.logit = fminf(to_f32(static_cast<const T*>(g.logits)[(t0 + t) * g.stride + c.pick]), FLT_MAX);
         float w = 0.f;
         if (g.renormalise) {
             // s up to a factor that all choices share, so that scores too small for fp32 still have their ratios
@@ -342,35 +390,113 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
             if (plan && c.pick >= 0) atomicOr(&chosen[c.pick * words + (t >> 5)], 1u << (t & 31));
         }
     }
-    if (!plan) return;
-    tc::pdl_trigger();
-    int* count = reinterpret_cast<int*>(chosen + g.E * words);
-    int* start = count + g.E + 1;
-    __syncthreads();
-    const bool alone = counts == nullptr;
-    for (int e = threadIdx.x; e < g.E; e += kThreads) {
-        int n = 0;
-        for (int i = 0; i < words; ++i) n += __popc(chosen[e * words + i]);
-        count[e] = n;
-        if (!alone) counts[(int64_t)blockIdx.x * g.E + e] = n;
+    if (plan) note_block(g, chosen, t0, n_tok, words, counts);
+}
+
+// The same for many tokens, by logits alone and without groups: a thread takes a token and keeps its best kList experts in order while it goes through the
+// logits (a warp for each token: 600 instructions to a token, here 2 to 5 per expert and place of the list, for 32 of them).
+template <typename T> struct Entry;         // a key and its index in one word where the type has 16 bits: the larger, the earlier
+template <> struct Entry<float> { uint32_t key; int index; };
+template <typename T> struct Entry { uint32_t both; };
+// Into the list, behind what is not smaller (indices only go up).
+__device__ __forceinline__ void insert(Entry<float> (&list)[kList], const Entry<float>& x)
+{
+    bool before[kList];                                         // x's place is before this one, or this one
+    #pragma unroll
+    for (int j = 0; j < kList; ++j) before[j] = x.key > list[j].key;
+    #pragma unroll
+    for (int j = kList - 1; j >= 0; --j) {
+        const Entry<float> in = j > 0 && before[j > 0 ? j - 1 : 0] ? list[j > 0 ? j - 1 : 0] : x;
+        if (before[j]) list[j] = in;
     }
-    if (alone) {
-        __syncthreads();
-        if (warp == 0) scan_counts(count, start, g.E, lane);
-        __syncthreads();
-        for (int e = threadIdx.x; e <= g.E; e += kThreads) g.start[e] = start[e];
+}
+template <typename T>
+__device__ __forceinline__ void insert(Entry<T> (&list)[kList], Entry<T> x)
+{
+    #pragma unroll
+    for (int j = 0; j < kList; ++j) {
+        const uint32_t high = max(list[j].both, x.both);
+        x.both = min(list[j].both, x.both);
+        list[j].both = high;
     }
-    for (int i = threadIdx.x; i < n_tok * k; i += kThreads) {
-        const int t = i / k, e = g.experts[t0 * k + i];
-        int at = -1;
-        if (e >= 0) {
-            at = 0;
-            for (int j = 0; j < (t >> 5); ++j) at += __popc(chosen[e * words + j]);
-            at += __popc(chosen[e * words + (t >> 5)] & ((1u << (t & 31)) - 1u));
-            if (alone) { at += start[e]; g.tokens[at] = (int)(t0 + t); }
+}
+template <typename T>
+__device__ __forceinline__ Entry<T> entry_of(T logit, int index)
+{
+    const float v = to_f32(logit);
+    const uint32_t key = v > -INFINITY ? key_of(sizeof(T) == 4 ? fminf(v, FLT_MAX) : v) : 0u;
+    if constexpr (sizeof(T) == 4) return Entry<T>{key, index};
+    else if constexpr (std::is_same<T, __half>::value) {
+        const uint32_t u = __half_as_ushort(__float2half_rn(v + 0.f));
+        return Entry<T>{key == 0 ? 0u : (u >> 15 ? ~u & 0xffffu : u | 0x8000u) << 16 | (uint32_t)(0xffff - index)};
+    } else return Entry<T>{key == 0 ? 0u : key >> 16 << 16 | (uint32_t)(0xffff - index)};
+}
+__device__ __forceinline__ int index_of(const Entry<float>& e) { return e.key != 0 ? e.index : -1; }
+template <typename T> __device__ __forceinline__ int index_of(const Entry<T>& e) { return e.both != 0 ? 0xffff - (int)(e.both & 0xffffu) : -1; }
+
+template <typename T>
+__global__ void __launch_bounds__(kListThreads)
+route_list_kernel(const __grid_constant__ RouteArgs g, int* counts)
+{
+    extern __shared__ uint32_t chosen[];
+    constexpr int words = kListThreads / 32, kVec = 16 / (int)sizeof(T);
+    const int64_t t0 = (int64_t)blockIdx.x * kListThreads, t = t0 + threadIdx.x;
+    const int n_tok = g.T - t0 < kListThreads ? (int)(g.T - t0) : kListThreads, k = g.top_k;
+    const bool plan = g.start != nullptr;
+    if (plan) {
+        for (int i = threadIdx.x; i < g.E * words; i += kListThreads) chosen[i] = 0;
+        __syncthreads();
+    }
+    if (t < g.T) {
+        const T* row = static_cast<const T*>(g.logits) + t * g.stride;
+        Entry<T> list[kList];
+        #pragma unroll
+        for (int j = 0; j < kList; ++j) list[j] = Entry<T>{};
+        auto take = [&](T logit, int e) { insert(list, entry_of(logit, e)); };
+        int e = 0;
+        if ((reinterpret_cast<uintptr_t>(row) & 15) == 0) {
+            uint4 next = g.E >= kVec ? *reinterpret_cast<const uint4*>(row) : make_uint4(0, 0, 0, 0);
+            for (; e + kVec <= g.E; e += kVec) {
+                const uint4 u = next;
+                if (e + 2 * kVec <= g.E) next = *reinterpret_cast<const uint4*>(row + e + kVec);
+                const T* v = reinterpret_cast<const T*>(&u);
+                #pragma unroll
+                for (int i = 0; i < kVec; ++i) take(v[i], e + i);
+            }
         }
-        g.place[t0 * k + i] = at;
+        for (; e < g.E; ++e) take(row[e], e);
+        float top = -INFINITY, sum = 1.f;
+        if (g.score == RTN_SCORE_SOFTMAX && !g.renormalise && index_of(list[0]) >= 0) {
+            top = fminf(to_f32(row[index_of(list[0])]), FLT_MAX);
+            sum = 0.f;
+            for (int i = 0; i < g.E; ++i) {
+                const float v = to_f32(row[i]);
+                sum += v > -INFINITY ? __expf(fminf(v, FLT_MAX) - top) : 0.f;
+            }
+        }
+        float w[kList], all = 0.f, best = 0.f;
+        int pick[kList];
+        #pragma unroll
+        for (int j = 0; j < kList; ++j) {
+            pick[j] = j < k ? index_of(list[j]) : -1;
+            w[j] = 0.f;
+            if (pick[j] < 0) continue;
+            const float x = fminf(to_f32(row[pick[j]]), FLT_MAX);
+            if (j == 0) best = x;
+            if (g.renormalise) w[j] = g.score == RTN_SCORE_SOFTMAX ? expf(x - best) : expf(fminf(x, 0.f) - fminf(best, 0.f)) / (1.f + expf(-fabsf(x)));
+            else w[j] = g.score == RTN_SCORE_SOFTMAX ? expf(x - top) / sum : 1.f / (1.f + expf(-x));
+            all += w[j];
+        }
+        if (!g.renormalise || all == 0.f) all = 1.f;
+        #pragma unroll
+        for (int j = 0; j < kList; ++j) {
+            if (j >= k) continue;
+            g.experts[t * k + j] = pick[j];
+            g.weights[t * k + j] = w[j] / all * g.scale;
+            if (plan && pick[j] >= 0) atomicOr(&chosen[pick[j] * words + threadIdx.x / 32], 1u << (threadIdx.x & 31));
+        }
     }
+    if (plan) note_block(g, chosen, t0, n_tok, words, counts);
 }
 
 // One expert's counts of all blocks as sums of those before; the total goes behind the last block's.
@@ -450,7 +576,8 @@ cudaError_t launch_choose(const RouteArgs& g, RoutePlan p, int* counts, unsigned
     p.group_size = g.E / g.groups;
     const int lanes = p.group_size / VPL;
     p.side_by_side = p.group_size % VPL == 0 && (lanes & (lanes - 1)) == 0;
-    p.group_lanes = p.side_by_side ? lanes : 1;
+    p.group_shift = 0;
+    while (p.side_by_side && 1 << p.group_shift < lanes) ++p.group_shift;
     const size_t smem = g.start != nullptr ? (size_t)g.E * ((p.tokens + 31) / 32) * 4 + 2 * (g.E + 1) * 4 : 0;
     // scores have to be computed where a bias or a sum of them is compared
     if (g.bias != nullptr || (g.groups > 1 && g.group_top > 1)) route_choose_kernel<T, VPL, true><<<blocks, kThreads, smem, s>>>(g, p, counts);
@@ -464,8 +591,11 @@ cudaError_t launch_route_experts(const RouteArgs& g, cudaStream_t s)
 {
     if (g.T == 0) return cudaMemsetAsync(g.start, 0, (size_t)(g.E + 1) * sizeof(int32_t), s);
     // A token to each warp while there are few (a token's chain is what counts), more with more, so that about two blocks to an SM hold them
-    RoutePlan p{kWarps, 0, 1, false};
-    while (p.tokens < kMaxTokens && g.T > (int64_t)2 * device_sm_count() * p.tokens) p.tokens *= 2;
+    // (by threads: 16384 tokens, 8 of 128 experts, all kernels LISTUS, by warps WARPUS)
+    const bool listed = g.T >= kListTokens && g.top_k <= kList && g.groups == 1 && g.bias == nullptr;
+    RoutePlan p{kWarps, 0, 0, false};
+    if (listed) p.tokens = kListThreads;
+    else while (p.tokens < kMaxTokens && g.T > (int64_t)2 * device_sm_count() * p.tokens) p.tokens *= 2;
     const int64_t blocks = (g.T + p.tokens - 1) / p.tokens;
     const bool scanned = blocks > kScanBlocks;
     void* counts = nullptr;
@@ -476,6 +606,11 @@ cudaError_t launch_route_experts(const RouteArgs& g, cudaStream_t s)
     int* c = static_cast<int*>(counts);
     cudaError_t e = with_dtype(g.dtype, [&](auto t) {
         using T = decltype(t);
+        if (listed) {
+            const size_t smem = g.start != nullptr ? (size_t)g.E * (kListThreads / 32) * 4 + 2 * (g.E + 1) * 4 : 0;
+            route_list_kernel<T><<<(unsigned)blocks, kListThreads, smem, s>>>(g, c);
+            return cudaGetLastError();
+        }
         if (g.E <= 32) return launch_choose<T, 1>(g, p, c, (unsigned)blocks, s);
         if (g.E <= 64) return launch_choose<T, 2>(g, p, c, (unsigned)blocks, s);
         if (g.E <= 128) return launch_choose<T, 4>(g, p, c, (unsigned)blocks, s);

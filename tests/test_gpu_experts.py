@@ -576,3 +576,27 @@ def test_route_many_tokens():
         assert torch.equal(s.experts, r.experts[:T]) and torch.equal(s.start[1:].long(), torch.bincount(flat[:T * k], minlength=E).cumsum(0))
         at = torch.sort(flat[:T * k], stable=True).indices
         assert torch.equal(s.tokens.long(), at // k)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("E,k", [(64, 8), (60, 3), (129, 8), (7, 7), (256, 1)], ids=ids)
+def test_route_is_the_same_for_a_token_among_many(E, k, dtype):
+    """Special logits among them; rows on every alignment."""
+    T = 5000
+    g = torch.Generator(device="cuda").manual_seed(E)
+    x = (2 * torch.randn(T, E, generator=g, device="cuda")).to(dtype)
+    x[torch.rand(T, E, generator=g, device="cuda") < 0.02] = float("-inf")
+    x[torch.rand(T, E, generator=g, device="cuda") < 0.01] = float("nan")
+    x[torch.rand(T, E, generator=g, device="cuda") < 0.01] = float("inf")
+    x[torch.rand(T, E, generator=g, device="cuda") < 0.05] = torch.finfo(dtype).max
+    x[5], x[6, 1:], x[7] = float("-inf"), float("nan"), torch.finfo(dtype).min
+    x[8:40] = x[8:40].round()
+    for kw in (dict(), dict(score=rtn.SCORE_SIGMOID), dict(renormalise=False, scale=0.5), dict(score=rtn.SCORE_SIGMOID, renormalise=False)):
+        many = rtn.rtn_route_experts(x, k, **kw)
+        for a in (0, 4000):
+            few = rtn.rtn_route_experts(x[a:a + 700], k, **kw)
+            assert torch.equal(few.experts, many.experts[a:a + 700])
+            # (a softmax's sum over all experts goes in another order)
+            assert torch.allclose(few.weights, many.weights[a:a + 700], rtol=WEIGHT_C * 2.0 ** -23, atol=1e-37)
+        flat = many.experts.flatten().long()
+        assert torch.equal(many.start[1:].long(), torch.bincount(flat[flat >= 0], minlength=E).cumsum(0))
