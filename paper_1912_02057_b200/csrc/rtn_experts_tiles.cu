@@ -259,8 +259,6 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                 for (int j = 0; j < 4; ++j)
                     if (q4 & 1) { nz[j].x = nz[j].z; nz[j].y = nz[j].w; pos[j].x = pos[j].z; pos[j].y = pos[j].w; }
             }
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&bar.planes_empty[sp]);                // (the planes are in registers)
             const uint32_t at = a_tmem + (uint32_t)(s * 64) + ((uint32_t)(quad * 32) << 16);
             #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -274,13 +272,16 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                     to[0] = a.x; to[1] = a.y; to[4] = a.z; to[5] = a.w; to[8] = b.x; to[9] = b.y; to[12] = b.z; to[13] = b.w;
                 }
                 if (h == 0 && !(alive = warp_wait(&bar.empty[s], phase + 1))) break;
+                if (h == 0) tc::tc_fence_after_sync();
                 tc::tmem_st_16x32(at + (uint32_t)(h * 32), o[0]);
                 tc::tmem_st_16x32(at + (uint32_t)(h * 32) + (16u << 16), o[1]);
             }
             tc::tmem_st_wait();
             tc::tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&bar.full[s]);
+            // (The planes' slot is given back here and not behind the loads: an arrival that nothing waits for data with went ahead of loads under way, and the
+            // next planes came into what they were still to read.)
+            if (lane == 0) { tc::mbar_arrive(&bar.planes_empty[sp]); tc::mbar_arrive(&bar.full[s]); }
             s += 2;
             while (s >= p.stages) { s -= p.stages; phase ^= 1; }
             k += 2;
@@ -434,6 +435,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             most_asx = __reduce_max_sync(0xffffffffu, most_asx); most_ao = __reduce_max_sync(0xffffffffu, most_ao);
             if (lane == 0) { (&here.most_asx.x)[part] = most_asx; (&here.most_ao.x)[part] = most_ao; }
             if (bad && t % cols == 0) atomicOr(g.status, kStatusBadIndex);
+            __threadfence_block();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&bar.params_full[at]);
             ask_params(t + gridDim.x);
@@ -682,6 +684,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                 }
             }
             tc::tc_fence_before_sync();
+            __threadfence_block();
             __syncwarp();
             if (lane == 0) { tc::mbar_arrive(&bar.acc_empty[ti & 1]); tc::mbar_arrive(&bar.votes_full[ti & 1]); }
         }

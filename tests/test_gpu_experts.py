@@ -242,6 +242,30 @@ def test_experts_whole_sums_are_exact(counts):
         assert np.array_equal(ref.f64(rtn.rtn_ternary_experts(*call_args(d))), want)
 
 
+@pytest.mark.parametrize("R,E,N,K", [(20000, 12, 1024, 2048), (30000, 7, 520, 1100), (9000, 60, 2048, 600), (300, 64, 4096, 4096)], ids=ids)
+def test_experts_many_tiles_are_exact_every_time(R, E, N, K):
+    """Every CTA goes through many tiles, its rings round and round: whole sums against a product in fp32, which is exact, and codes against them; three times."""
+    g = torch.Generator(device="cuda").manual_seed(R)
+    code = lambda *s: torch.randint(-1, 2, s, generator=g, device="cuda", dtype=torch.int8)  # noqa: E731
+    x, w = code(R, K), code(E, N, K)
+    counts = torch.multinomial(torch.rand(E, generator=g, device="cuda") + 0.2, R, replacement=True, generator=g).bincount(minlength=E)
+    start = torch.cat([counts.new_zeros(1), counts.cumsum(0)]).int()
+    want = torch.cat([x[a:b].float() @ w[e].float().t() for e, (a, b) in enumerate(zip(start[:-1].tolist(), start[1:].tolist()))])
+    half, one, zero = (torch.tensor([v], device="cuda") for v in (0.5, 1.0, 0.0))
+    xp, xs = rtn.rtn_ternarize_pack_act(x.float(), -half, half)
+    wp, ws = rtn.rtn_pack_weights(w.view(E * N, K))
+    args = (xp, xs, None, start, wp, ws[0].contiguous(), N, K, one, zero, one, zero)
+    t = torch.tensor([20.5], device="cuda")
+    gated = want[:, :N // 2] * want[:, N // 2:]
+    codes, sums = rtn.rtn_ternarize_pack_act(gated, -t, t)
+    for _ in range(3):
+        assert torch.equal(rtn.rtn_ternary_experts(*args), want)
+        assert torch.equal(rtn.rtn_ternary_experts(*args, gated=True), gated)
+        got = rtn.rtn_ternary_experts(*args, gated=True, t_lo=-t, t_hi=t)
+        assert torch.equal(got[0], codes) and torch.equal(got[1], sums)
+    assert rtn.rtn_last_device_status() == 0
+
+
 @pytest.mark.parametrize("counts", [[2, 0, 3, 1], [40, 9, 0, 90]], ids=ids)
 @pytest.mark.parametrize("dtype", DTYPES, ids=ids)
 def test_experts_rows_behind_the_last_and_strides(counts, dtype):
