@@ -18,54 +18,41 @@ namespace {
 constexpr float kUnit = 5.9604644775390625e-8f;                // 2^-24
 constexpr int kMaxWarps = 32;
 
-// EV adjacent elements: 16-byte accesses where EV > 1 (the launcher saw to the alignment).  `Held` is what they are until they are looked at,
-// so that many are on their way at a time.
-template <typename T, int EV> struct Held { uint4 u[EV * sizeof(T) / 16]; };
-template <typename T> struct Held<T, 1> { T u; };
+// EV adjacent elements in accesses of up to 16 bytes (the launcher saw to the alignment).  `Held` is what they are until they are looked at, so that
+// many are on their way at a time.
+template <int kBytes> struct Word { uint4 u[kBytes / 16]; };
+template <> struct Word<2> { unsigned short u; };
+template <> struct Word<4> { uint32_t u; };
+template <> struct Word<8> { uint2 u; };
+template <typename T, int EV> using Held = Word<EV * (int)sizeof(T)>;
 
 template <typename T, int EV>
-__device__ __forceinline__ Held<T, EV> ask(const void* base, int64_t at)
+__device__ __forceinline__ Held<T, EV> ask(const T* row, int at)
 {
     Held<T, EV> h;
-    const T* p = static_cast<const T*>(base) + at;
-    if constexpr (EV == 1) h.u = *p;
-    else {
+    if constexpr (EV * sizeof(T) > 16) {
         #pragma unroll
-        for (int i = 0; i < EV * (int)sizeof(T) / 16; ++i) h.u[i] = reinterpret_cast<const uint4*>(p)[i];
-    }
+        for (int i = 0; i < EV * (int)sizeof(T) / 16; ++i) h.u[i] = reinterpret_cast<const uint4*>(row + at)[i];
+    } else h = *reinterpret_cast<const Held<T, EV>*>(row + at);
     return h;
 }
 template <typename T, int EV>
 __device__ __forceinline__ void take(const Held<T, EV>& h, bool ok, float (&f)[EV])       // zeros where not ok
 {
-    if constexpr (EV == 1) f[0] = ok ? to_f32(h.u) : 0.f;
-    else {
-        constexpr int N = Vec16<T>::N;
-        static_assert(EV % N == 0, "whole vectors");
-        #pragma unroll
-        for (int i = 0; i < EV / N; ++i) {
-            float part[N];
-            Vec16<T>::unpack(ok ? h.u[i] : make_uint4(0, 0, 0, 0), part);
-            #pragma unroll
-            for (int j = 0; j < N; ++j) f[i * N + j] = part[j];
-        }
-    }
+    const T* e = reinterpret_cast<const T*>(&h);
+    #pragma unroll
+    for (int i = 0; i < EV; ++i) f[i] = ok ? to_f32(e[i]) : 0.f;
 }
 template <typename T, int EV>
-__device__ __forceinline__ void store_values(void* base, int64_t at, const float (&f)[EV])
+__device__ __forceinline__ void store_values(T* row, int at, const float (&f)[EV])
 {
-    T* p = static_cast<T*>(base) + at;
-    if constexpr (EV == 1) *p = from_f32<T>(f[0]);
-    else {
-        constexpr int N = Vec16<T>::N;
+    alignas(16) T e[EV];
+    #pragma unroll
+    for (int i = 0; i < EV; ++i) e[i] = from_f32<T>(f[i]);
+    if constexpr (EV * sizeof(T) > 16) {
         #pragma unroll
-        for (int i = 0; i < EV / N; ++i) {
-            float part[N];
-            #pragma unroll
-            for (int j = 0; j < N; ++j) part[j] = f[i * N + j];
-            reinterpret_cast<uint4*>(p)[i] = Vec16<T>::pack(part);
-        }
-    }
+        for (int i = 0; i < EV * (int)sizeof(T) / 16; ++i) reinterpret_cast<uint4*>(row + at)[i] = reinterpret_cast<const uint4*>(e)[i];
+    } else *reinterpret_cast<Held<T, EV>*>(row + at) = *reinterpret_cast<const Held<T, EV>*>(e);
 }
 template <int EV>
 __device__ __forceinline__ void load_params(const float* p, int at, float (&f)[EV])
@@ -90,10 +77,14 @@ __device__ __forceinline__ void block_sums(F& a, F& b, F* red)
     for (int d = 16; d > 0; d >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, d); b += __shfl_xor_sync(0xffffffffu, b, d); }
 }
 
+// By the approximate exponential and reciprocal: the logistic function within (2 |z| + 4) (1 - s) + 4 <= 9 units of 2^-24, relative where it counts
+// (for z below 0 the exponent's 2 |z| units are the function's own; |z| >= 40 gives less than 2^-57).
 __device__ __forceinline__ float gate_of(float z, int kind)
 {
     if (kind == RTN_GATE_LINEAR) return z;
-    const float s = 1.f / (1.f + expf(-z));
+    float e, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
     return kind == RTN_GATE_SIGMOID ? s : z * s;
 }
 
@@ -123,7 +114,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
     Held<TS, EV> res[NV];
     if (g.residual != nullptr) {
         #pragma unroll
-        for (int v = 0; v < NV; ++v) res[v] = ask<TS, EV>(g.residual, t * g.residual_stride + at[v]);
+        for (int v = 0; v < NV; ++v) res[v] = ask<TS, EV>(static_cast<const TS*>(g.residual) + t * g.residual_stride, at[v]);
     }
     // y in h, the sum of its terms' magnitudes in slack
     #pragma unroll
@@ -145,7 +136,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
                 ok[i] = j0 + i < g.k && row >= 0 && row < g.R;
                 if (!ok[i]) w[i] = j0 + i < g.k && row >= g.R ? __int_as_float(0x7fffffff) : 0.f;
                 #pragma unroll
-                for (int v = 0; v < NV; ++v) x[i][v] = ask<TB, EV>(g.branch, (ok[i] ? row : 0) * g.branch_stride + at[v]);
+                for (int v = 0; v < NV; ++v) x[i][v] = ask<TB, EV>(static_cast<const TB*>(g.branch) + (ok[i] ? row : 0) * g.branch_stride, at[v]);
             }
             #pragma unroll
             for (int i = 0; i < kAhead; ++i)
@@ -169,7 +160,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
     } else if (g.branch != nullptr) {
         Held<TB, EV> x[NV];
         #pragma unroll
-        for (int v = 0; v < NV; ++v) x[v] = ask<TB, EV>(g.branch, t * g.branch_stride + at[v]);
+        for (int v = 0; v < NV; ++v) x[v] = ask<TB, EV>(static_cast<const TB*>(g.branch) + t * g.branch_stride, at[v]);
         #pragma unroll
         for (int v = 0; v < NV; ++v) take<TB, EV>(x[v], in[v], h[v]);
     }
@@ -183,7 +174,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
     if (g.gate != nullptr) {
         Held<TB, EV> z[NV];
         #pragma unroll
-        for (int v = 0; v < NV; ++v) z[v] = ask<TB, EV>(g.gate, t * g.gate_stride + at[v]);
+        for (int v = 0; v < NV; ++v) z[v] = ask<TB, EV>(static_cast<const TB*>(g.gate) + t * g.gate_stride, at[v]);
         #pragma unroll
         for (int v = 0; v < NV; ++v) {
             take<TB, EV>(z[v], true, f[v]);
@@ -378,6 +369,16 @@ static __device__ __noinline__ int exact_codes(const NormArgs& g, int64_t t, dou
     return sum;
 }
 
+// The low 16 bits, at the even places.
+__device__ __forceinline__ uint32_t spread(uint32_t x)
+{
+    x &= 0xffffu;
+    x = (x | x << 8) & 0x00ff00ffu;
+    x = (x | x << 4) & 0x0f0f0f0fu;
+    x = (x | x << 2) & 0x33333333u;
+    return (x | x << 1) & 0x55555555u;
+}
+
 template <typename TB, typename TS, int EV, int NV, int kMaxThreads, bool kCodes>
 __global__ void __launch_bounds__(kMaxThreads, 1024 / kMaxThreads)
 block_norm_kernel(const __grid_constant__ NormArgs g)
@@ -405,11 +406,23 @@ block_norm_kernel(const __grid_constant__ NormArgs g)
                         at[16] = (uint8_t)(up >> (v * 8));
                     }
                 } else {
-                    const uint32_t a = __ballot_sync(0xffffffffu, up >> v & 1), b = __ballot_sync(0xffffffffu, down >> v & 1);
-                    if ((threadIdx.x & 31) == 0 && c < blocks * kBlockCodes) {
-                        uint32_t* at = reinterpret_cast<uint32_t*>(row + c / kBlockCodes * kBlockBytes + c % kBlockCodes / 8);
-                        at[0] = a | b;
-                        at[4] = a;
+                    // a warp's 32 EV values: EV words of each plane, the values of a lane side by side
+                    uint32_t nz[EV], pos[EV];
+                    #pragma unroll
+                    for (int i = 0; i < EV; ++i) {
+                        pos[i] = __ballot_sync(0xffffffffu, up >> (v * EV + i) & 1);
+                        nz[i] = __ballot_sync(0xffffffffu, (up | down) >> (v * EV + i) & 1);
+                    }
+                    const int lane = threadIdx.x & 31, word = c - lane * EV + lane * 32;       // the word's first column, for lanes below EV
+                    if (lane < EV && word < blocks * kBlockCodes) {
+                        uint32_t a = nz[0], b = pos[0];
+                        if constexpr (EV == 2) {
+                            auto both = [&](uint32_t x, uint32_t y) { return spread(x >> (16 * lane)) | spread(y >> (16 * lane)) << 1; };
+                            a = both(nz[0], nz[1]); b = both(pos[0], pos[1]);
+                        }
+                        uint32_t* at = reinterpret_cast<uint32_t*>(row + word / kBlockCodes * kBlockBytes + word % kBlockCodes / 8);
+                        at[0] = a;
+                        at[4] = b;
                     }
                 }
             }
@@ -428,8 +441,8 @@ block_norm_kernel(const __grid_constant__ NormArgs g)
     for (int v = 0; v < NV; ++v) {
         const int c = threadIdx.x * EV + v * blockDim.x * EV;
         if (c >= g.W) continue;
-        if (g.stream_out != nullptr) store_values<TS, EV>(g.stream_out, t * g.stream_stride + c, h[v]);
-        if (g.normed != nullptr) store_values<TB, EV>(g.normed, t * g.normed_stride + c, n[v]);
+        if (g.stream_out != nullptr) store_values<TS, EV>(static_cast<TS*>(g.stream_out) + t * g.stream_stride, c, h[v]);
+        if (g.normed != nullptr) store_values<TB, EV>(static_cast<TB*>(g.normed) + t * g.normed_stride, c, n[v]);
     }
     if (g.place != nullptr && threadIdx.x < g.k && g.place[t * g.k + threadIdx.x] >= g.R) atomicOr(g.status, kStatusBadIndex);
 }
@@ -447,15 +460,25 @@ cudaError_t launch_values(const NormArgs& g, cudaStream_t s)
 template <typename TB, typename TS>
 cudaError_t launch_types(const NormArgs& g, cudaStream_t s)
 {
-    auto vec = [](const void* p, int64_t stride, size_t e) {
-        return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride * (int64_t)e % 16 == 0);
+    // Adjacent values that a thread may take at a time: eight or two where every row and parameter lets it, else one
+    auto fits = [&](int ev) {
+        auto ok = [&](const void* p, int64_t stride, size_t e) {
+            const uintptr_t bytes = ev * e < 16 ? ev * e : 16;
+            return p == nullptr || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && stride * (int64_t)e % (int64_t)bytes == 0);
+        };
+        return g.W % ev == 0 && ok(g.branch, g.branch_stride, sizeof(TB)) && ok(g.gate, g.gate_stride, sizeof(TB)) &&
+               ok(g.normed, g.normed_stride, sizeof(TB)) && ok(g.residual, g.residual_stride, sizeof(TS)) &&
+               ok(g.stream_out, g.stream_stride, sizeof(TS)) && ok(g.post_weight, 0, 4) && ok(g.norm_weight, 0, 4) &&
+               (g.n_scale == 1 || ok(g.scale, 0, 4)) && (g.n_thr == 1 || (ok(g.t_lo, 0, 4) && ok(g.t_hi, 0, 4)));
     };
-    const bool wide = g.W % 8 == 0 && vec(g.branch, g.branch_stride, sizeof(TB)) && vec(g.gate, g.gate_stride, sizeof(TB)) &&
-                      vec(g.normed, g.normed_stride, sizeof(TB)) && vec(g.residual, g.residual_stride, sizeof(TS)) &&
-                      vec(g.stream_out, g.stream_stride, sizeof(TS)) && vec(g.post_weight, 0, 4) && vec(g.norm_weight, 0, 4) &&
-                      (g.n_scale == 1 || vec(g.scale, 0, 4)) && (g.n_thr == 1 || (vec(g.t_lo, 0, 4) && vec(g.t_hi, 0, 4)));
-    if (wide && g.W <= 2048) return launch_values<TB, TS, 8, 1, 256>(g, s);
-    if (wide) return g.W <= 8192 ? launch_values<TB, TS, 8, 1, 1024>(g, s) : launch_values<TB, TS, 8, 2, 1024>(g, s);
+    if (fits(8)) {
+        if (g.W <= 2048) return launch_values<TB, TS, 8, 1, 256>(g, s);
+        return g.W <= 8192 ? launch_values<TB, TS, 8, 1, 1024>(g, s) : launch_values<TB, TS, 8, 2, 1024>(g, s);
+    }
+    if (fits(2)) {
+        if (g.W <= 2048) return launch_values<TB, TS, 2, 4, 256>(g, s);
+        return g.W <= 8192 ? launch_values<TB, TS, 2, 8, 512>(g, s) : launch_values<TB, TS, 2, 8, 1024>(g, s);
+    }
     if (g.W <= 2048) return launch_values<TB, TS, 1, 8, 256>(g, s);
     return g.W <= 8192 ? launch_values<TB, TS, 1, 16, 512>(g, s) : launch_values<TB, TS, 1, 16, 1024>(g, s);
 }
