@@ -5,6 +5,9 @@
 // shuffle tree joins the group.
 // Bound: DRAM, the packed weights of the experts that have rows, read once; from about four rows of an expert on the POPC rate.
 #include "rtn_experts.cuh"
+#include "rtn_tcgen05.cuh"
+
+#include <math.h>
 
 namespace rtn {
 
@@ -100,6 +103,7 @@ experts_rows_kernel(const __grid_constant__ ExpertsArgs g, int GL, int col_block
     }
     if constexpr (kCodes) {
         __syncthreads();
+        tc::pdl_wait();                                         // (the sums begin at 0)
         const int words = per_cta / 32;
         const int64_t width = (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes;     // (a packed row's padding is written too)
         for (int x = threadIdx.x; x < tile.rows * words; x += kThreads) {
@@ -120,6 +124,7 @@ experts_rows_kernel(const __grid_constant__ ExpertsArgs g, int GL, int col_block
 __global__ void __launch_bounds__(256)
 zero_sums_kernel(const ExpertsArgs g)
 {
+    tc::pdl_trigger();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i < g.R && i >= g.start[0] && i < g.start[g.E]) g.out_sum[i] = 0;
 }
@@ -140,8 +145,7 @@ cudaError_t launch_rows(const ExpertsArgs& g, cudaStream_t s)
         zero_sums_kernel<<<(unsigned)((g.R + 255) / 256), 256, 0, s>>>(g);
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
-        if (g.gated) experts_rows_kernel<MT, true, true><<<grid, kThreads, 0, s>>>(g, GL, (int)cols);
-        else experts_rows_kernel<MT, false, true><<<grid, kThreads, 0, s>>>(g, GL, (int)cols);
+        return launch_pdl(g.gated ? experts_rows_kernel<MT, true, true> : experts_rows_kernel<MT, false, true>, dim3(grid), dim3(kThreads), 0, s, g, GL, (int)cols);
     } else {
         if (g.gated) experts_rows_kernel<MT, true, false><<<grid, kThreads, 0, s>>>(g, GL, (int)cols);
         else experts_rows_kernel<MT, false, false><<<grid, kThreads, 0, s>>>(g, GL, (int)cols);
@@ -151,10 +155,20 @@ cudaError_t launch_rows(const ExpertsArgs& g, cudaStream_t s)
 
 }  // namespace
 
+// Which form: rows cost 7 us per million rows x columns x blocks of K (two rows to a tile: the POPC rate) on top of 5, tiles 10.5 us and 0.2 us per MB of the
+// planes of the experts that have rows (of R rows dealt at random).  In a graph on one B200 (us, rows of an expert on average in brackets):
+//                                                    rows  tiles                                             rows  tiles
+//   4 rows (0.1), 64 x 2048 x 2048, gated, codes      8.4   13.0     320 (5.3), 60 x 1006 x 429              14.0   12.8
+//   32 (0.5), 64 x 2048 x 2048, gated, codes         14.4   18.5     80 (1.3), 60 x 4096 x 300               12.5   20.7
+//   64 (1), 64 x 2048 x 2048, gated, codes           20.0   20.7     512 (32), 16 x 512 x 512                10.3   10.3
+//   128 (2), 64 x 2048 x 2048, gated, codes          29.1   24.8     1554 (194), 8 x 1000 x 520              57.4   14.4
+// One row to a tile where an expert has hardly more (16 rows (0.25): 8.5 us, two to a tile 10.3); four or eight were nowhere ahead.
 cudaError_t launch_ternary_experts(const ExpertsArgs& g, cudaStream_t s)
 {
-    if (g.R > 32 && experts_tiles_supported(g)) return launch_experts_tiles(g, s);
-    return g.R <= g.E ? launch_rows<1>(g, s) : launch_rows<4>(g, s);
+    const double nblk = (double)((g.K + kBlockCodes - 1) / kBlockCodes), used = g.E * (1.0 - exp(-(double)g.R / g.E));
+    const double rows_us = 5.0 + 7e-6 * (double)g.R * (double)g.N * nblk, tiles_us = 10.5 + 0.2e-6 * used * (double)g.N * nblk * kBlockBytes;
+    if (rows_us > tiles_us && experts_tiles_supported(g)) return launch_experts_tiles(g, s);
+    return 2 * g.R <= g.E ? launch_rows<1>(g, s) : launch_rows<2>(g, s);
 }
 
 }  // namespace rtn
