@@ -295,75 +295,123 @@ __device__ __forceinline__ bool code_row(const NormArgs& g, const float (&n)[NV]
     return near;
 }
 
-// The codes of one token in double, whatever the types: thread by thread the columns threadIdx.x, threadIdx.x + blockDim.x, ...
-constexpr int kExactEach = 16;                                  // of a thread at most
-__device__ __forceinline__ double exact_y(const NormArgs& g, int64_t t, int c)
-{
-    if (g.branch == nullptr) return 0.0;
-    if (g.place == nullptr) return (double)load_as_f32(g.branch, t * g.branch_stride + c, g.dtype);
-    double y = 0.0;
-    #pragma unroll 1
-    for (int j0 = 0; j0 < g.k; j0 += 8) {
-        float x[8], w[8];
-        #pragma unroll
-        for (int i = 0; i < 8; ++i) {                           // (all of them on their way)
-            const int j = j0 + i < g.k ? j0 + i : 0;
-            const int64_t row = g.place[t * g.k + j];
-            const bool ok = j0 + i < g.k && row >= 0;
-            w[i] = !ok ? 0.f : row >= g.R ? __int_as_float(0x7fffffff) : g.weights != nullptr ? g.weights[t * g.k + j] : 1.f;
-            x[i] = load_as_f32(g.branch, (ok && row < g.R ? row : 0) * g.branch_stride + c, g.dtype);
-            if (!ok) x[i] = 0.f;
-        }
-        #pragma unroll
-        for (int i = 0; i < 8; ++i) y = fma((double)w[i], (double)x[i], y);
-    }
-    return y;
-}
+// The codes of one token in double: thread by thread the columns threadIdx.x, threadIdx.x + blockDim.x, ..., kTogether of them with their loads on
+// their way together (a row's turn is some ten latencies; one column and one kind of load after the other took four times as long, and the last of
+// a launch's rows that needed it was what the launch waited for).
+constexpr int kExactEach = 16, kTogether = 4;                   // columns of a thread at most
+template <typename TB, typename TS>
 static __device__ __noinline__ int exact_codes(const NormArgs& g, int64_t t, double* red, uint8_t* row)
 {
+    const int W = g.W, step = blockDim.x;
     double h[kExactEach], post = 1.0, pre = 1.0, none = 0.0, ss = 0.0;
+    const TB* branch = static_cast<const TB*>(g.branch);
     #pragma unroll 1
-    for (int i = 0, c = threadIdx.x; c < g.W; ++i, c += blockDim.x) { h[i] = exact_y(g, t, c); ss = fma(h[i], h[i], ss); }
+    for (int i0 = 0, c0 = threadIdx.x; c0 < W; i0 += kTogether, c0 += kTogether * step) {
+        double y[kTogether];
+        #pragma unroll
+        for (int u = 0; u < kTogether; ++u) y[u] = 0.0;
+        if (g.place != nullptr) {
+            #pragma unroll 1
+            for (int j0 = 0; j0 < g.k; j0 += 4) {
+                TB x[4][kTogether];
+                float w[4];
+                bool ok[4];
+                #pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = j0 + i < g.k ? j0 + i : 0;
+                    const int64_t r = g.place[t * g.k + j];
+                    w[i] = g.weights != nullptr ? g.weights[t * g.k + j] : 1.f;
+                    ok[i] = j0 + i < g.k && r >= 0;
+                    if (ok[i] && r >= g.R) w[i] = __int_as_float(0x7fffffff);
+                    const TB* from = branch + (ok[i] && r < g.R ? r : 0) * g.branch_stride;
+                    #pragma unroll
+                    for (int u = 0; u < kTogether; ++u) x[i][u] = from[c0 + u * step < W ? c0 + u * step : 0];
+                }
+                #pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    #pragma unroll
+                    for (int u = 0; u < kTogether; ++u)
+                        if (ok[i]) y[u] = fma((double)w[i], (double)to_f32(x[i][u]), y[u]);
+            }
+        } else if (branch != nullptr) {
+            TB x[kTogether];
+            #pragma unroll
+            for (int u = 0; u < kTogether; ++u) x[u] = branch[t * g.branch_stride + (c0 + u * step < W ? c0 + u * step : 0)];
+            #pragma unroll
+            for (int u = 0; u < kTogether; ++u) y[u] = (double)to_f32(x[u]);
+        }
+        #pragma unroll
+        for (int u = 0; u < kTogether; ++u)
+            if (c0 + u * step < W) { h[i0 + u] = y[u]; ss = fma(y[u], y[u], ss); }
+    }
     if (g.post_weight != nullptr) {
         block_sums(ss, none, red);
-        post = 1.0 / sqrt(ss / (double)g.W + (double)g.eps);
+        post = 1.0 / sqrt(ss / (double)W + (double)g.eps);
     }
     ss = none = 0.0;
+    const TB* gate = static_cast<const TB*>(g.gate) + t * g.gate_stride;
+    const TS* residual = static_cast<const TS*>(g.residual) + t * g.residual_stride;
+    const double scale = g.scale != nullptr && g.n_scale == 1 ? (double)g.scale[0] : 1.0;
     #pragma unroll 1
-    for (int i = 0, c = threadIdx.x; c < g.W; ++i, c += blockDim.x) {
-        double y = h[i];
-        if (g.post_weight != nullptr) y *= post * (double)g.post_weight[c];
-        if (g.gate != nullptr) {
-            const double z = (double)load_as_f32(g.gate, t * g.gate_stride + c, g.dtype), s = 1.0 / (1.0 + exp(-z));
-            y *= g.gate_kind == RTN_GATE_LINEAR ? z : g.gate_kind == RTN_GATE_SIGMOID ? s : z * s;
+    for (int i0 = 0, c0 = threadIdx.x; c0 < W; i0 += kTogether, c0 += kTogether * step) {
+        float r[kTogether], z[kTogether], p[kTogether], q[kTogether];
+        #pragma unroll
+        for (int u = 0; u < kTogether; ++u) { r[u] = 0.f; z[u] = p[u] = q[u] = 1.f; }
+        #pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            const int c = c0 + u * step < W ? c0 + u * step : 0;
+            if (g.residual != nullptr) r[u] = to_f32(residual[c]);
+            if (g.gate != nullptr) z[u] = to_f32(gate[c]);
+            if (g.post_weight != nullptr) p[u] = g.post_weight[c];
+            if (g.scale != nullptr && g.n_scale != 1) q[u] = g.scale[c];
         }
-        if (g.scale != nullptr) y *= (double)g.scale[g.n_scale == 1 ? 0 : c];
-        if (g.residual != nullptr) y += (double)load_as_f32(g.residual, t * g.residual_stride + c, g.stream_dtype);
-        h[i] = y;
-        ss = fma(y, y, ss);
+        #pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            if (c0 + u * step >= W) continue;
+            double f = scale * (double)q[u] * (post * (double)p[u]);
+            if (g.gate != nullptr) {
+                if (g.gate_kind != RTN_GATE_SIGMOID) f *= (double)z[u];
+                if (g.gate_kind != RTN_GATE_LINEAR) f *= 1.0 / (1.0 + exp(-(double)z[u]));
+            }
+            const double y = branch != nullptr ? fma(f, h[i0 + u], (double)r[u]) : (double)r[u];
+            h[i0 + u] = y;
+            ss = fma(y, y, ss);
+        }
     }
     if (g.norm_weight != nullptr) {
         block_sums(ss, none, red);
-        pre = 1.0 / sqrt(ss / (double)g.W + (double)g.eps);
+        pre = 1.0 / sqrt(ss / (double)W + (double)g.eps);
     }
     int sum = 0;
-    const int width = (g.W + kBlockCodes - 1) / kBlockCodes * kBlockCodes;
+    const int width = (W + kBlockCodes - 1) / kBlockCodes * kBlockCodes, lane = threadIdx.x & 31;
     #pragma unroll 1
-    for (int i = 0, c0 = threadIdx.x & ~31; c0 < width; ++i, c0 += blockDim.x) {
-        const int c = c0 + (threadIdx.x & 31);
-        bool up = false, down = false;
-        if (c < g.W) {
-            const double n = g.norm_weight != nullptr ? h[i] * (pre * (double)g.norm_weight[c]) : h[i];
-            const int k = g.n_thr == 1 ? 0 : c;
-            up = n > (double)g.t_hi[k];
-            down = !up && n < (double)g.t_lo[k];
+    for (int i0 = 0, c0 = threadIdx.x & ~31; c0 < width; i0 += kTogether, c0 += kTogether * step) {
+        float p[kTogether], lo[kTogether], hi[kTogether];
+        #pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            const int c = c0 + lane + u * step < W ? c0 + lane + u * step : 0, k = g.n_thr == 1 ? 0 : c;
+            p[u] = 1.f;
+            if (g.norm_weight != nullptr) p[u] = g.norm_weight[c];
+            lo[u] = g.t_lo[k];
+            hi[u] = g.t_hi[k];
         }
-        const uint32_t a = __ballot_sync(0xffffffffu, up), b = __ballot_sync(0xffffffffu, down);
-        if ((threadIdx.x & 31) == 0) {
-            uint32_t* at = reinterpret_cast<uint32_t*>(row + c0 / kBlockCodes * kBlockBytes + c0 % kBlockCodes / 8);
-            at[0] = a | b;
-            at[4] = a;
-            sum += __popc(a) - __popc(b);
+        #pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            const int first = c0 + u * step;
+            if (first >= width) continue;
+            bool up = false, down = false;
+            if (first + lane < W) {
+                const double n = h[i0 + u] * (pre * (double)p[u]);
+                up = n > (double)hi[u];
+                down = !up && n < (double)lo[u];
+            }
+            const uint32_t a = __ballot_sync(0xffffffffu, up), b = __ballot_sync(0xffffffffu, down);
+            if (lane == 0) {
+                uint32_t* at = reinterpret_cast<uint32_t*>(row + first / kBlockCodes * kBlockBytes + first % kBlockCodes / 8);
+                at[0] = a | b;
+                at[4] = a;
+                sum += __popc(a) - __popc(b);
+            }
         }
     }
     return sum;
@@ -394,7 +442,7 @@ block_norm_kernel(const __grid_constant__ NormArgs g)
         uint8_t* row = g.out_packed + t * blocks * kBlockBytes;
         int own = __popc(up) - __popc(down);
         if (__syncthreads_or(near)) {
-            own = exact_codes(g, t, red, row);
+            own = exact_codes<TB, TS>(g, t, red, row);
         } else {
             #pragma unroll
             for (int v = 0; v < NV; ++v) {
