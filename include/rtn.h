@@ -360,9 +360,10 @@ rtn_status rtn_route_experts(const void* logits, int64_t logits_stride, int64_t 
  *   out_packed, out_sum   NULL (both), or the codes of the outputs against thresholds, R packed rows of F codes and their sums, as
  *               rtn_ternarize_pack_act gives them: what the next product reads.  t_lo, t_hi: n_thr 1 or E.  They are the codes of the exact
  *               output (one that fp32 cannot tell from a threshold is computed in double); out and out_packed may both be given
- * Few rows run on a bit-plane kernel that streams the weights, others on the tensor cores.  Bounds that do not fit (a decreasing
- * start, or one outside 0 .. R) leave the expert's rows as they were, a token out of range makes its row NaN (codes 0), and
- * rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once. */
+ * Few rows run on a bit-plane kernel that streams the weights, others on the tensor cores (with scratch of R * K / 2 bytes, K rounded up to
+ * 256).  Bounds that do not fit (a decreasing start, or one outside 0 .. R) leave the expert's outputs as they were, a token out of
+ * range makes its row NaN (codes 0), and rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once.  After such bounds the sums, and
+ * rows outside start[0] .. start[E], are not to be relied on. */
 rtn_status rtn_ternary_experts(const void* a_packed, const int32_t* a_sum, int64_t T, const int32_t* tokens, const int32_t* start, int64_t R,
                                const void* w_packed, const int32_t* w_sum, int64_t E, int64_t N, int64_t K,
                                const float* a_scale, const float* a_offset, int64_t n_aparam,

@@ -1,4 +1,18 @@
 // The experts' ternary products on the tensor cores: codes as 4-bit floating point.
+//
+// A product of codes is -1, 0 or 1, and so is one of e2m1 values of reciprocal magnitudes; with every block scale 1 the fp32 accumulators hold
+// S = sum_k x_k w_k exactly (|S| <= K <= 2^24).  kind::mxf4 runs at four times the bf16 rate (8.8 PFLOP/s measured; int8 twice).
+//   y = w_s (a_s S) + w_o a_s S_x + (w_s S_w + K w_o) a_o + bias, then act, gate, codes, all in the epilogue.
+// A tile: 128 weight rows (gated: 64 outputs' two rows each) times 16 .. 160 rows of one expert.  The weights are the operand of 128 rows, out of tensor
+// memory: planes come by TMA, warps expand them in registers straight into it (no shared memory in between, whose bandwidth both operands
+// would share), and a product of 32 inputs runs at the full rate (of 16 at two thirds).  Inputs are expanded once, ahead, into the experts' order
+// (K / 2 bytes a row of scratch): a row meets every column tile.  A persistent CTA per SM; two accumulators, so that a tile's outputs are written during the
+// next one's products; parameters are fetched two tiles ahead by warps of their own, which also put a token's codes together from the votes.
+// Codes are those of the exact output: a value nearer to a threshold than its error bound is worked out again in double, of 16 tokens at a time.
+// Bound: for long prompts the instructions of the epilogue (50 to 65 per output) and of the expansion (some 200 per 32 rows x 256 codes), the tensor
+// pipe idles two thirds of the time; for few rows of an expert its start (2.6 us) and the first planes' way (2.6 us).
+// Measured (one B200): 65536 rows, 64 experts of 2048 x 2048, gated, codes 269 us (2.0 PFLOP/s; the matrix instructions alone 63); of 2048 x 1024, bf16
+// values 156 us (268 MB written); 384 rows, 64 experts of 2048 x 2048, gated, codes 29.5 us (67 MB of planes at 2.3 TB/s).
 #include "rtn_experts.cuh"
 #include "rtn_tcgen05.cuh"
 #include "rtn_tensormap.cuh"
@@ -20,7 +34,7 @@ template <int kRegs> __device__ __forceinline__ void more_registers() { asm vola
 template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
 // A slot holds a span of K, 512 codes (or the last 256): two 128-byte rows of 4-bit values to an input, 64 columns of tensor memory to a weight row.
 // (Slots of 256 codes: twice the barriers, which a small tile's time is made of.)
-constexpr int kMaxRows = 192;                                   // of a tile
+constexpr int kMaxRows = 160;                                   // of a tile
 constexpr int kMaxStages = 6, kMaxSpans = 8;                    // slots of the rings
 constexpr uint32_t kSpanBytes = 128 * 128;                       // 512 codes of 128 weight rows, as planes
 constexpr uint32_t kTries = 1u << 20;
@@ -154,7 +168,8 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
     }
     // Tiles of each expert: as few as hold its rows, and of about the same height, so that little of the last one is empty.
     if (warp == 0) {
-        int sum = 0;
+        const uint32_t most = 0x7fffffffu / (uint32_t)p.col_tiles;               // (bounds that overlap can add up to any number of tiles)
+        uint32_t sum = 0;
         for (int e0 = 0; e0 < g.E; e0 += 32) {
             const int e = e0 + lane;
             int s = 0, n = 0;
@@ -164,20 +179,20 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
                 if (s >= 0 && len >= 0 && s + len <= g.R) n = (int)len;
                 else if (blockIdx.x == 0) atomicOr(g.status, kStatusBadIndex);
             }
-            const int tiles = (n + p.max_rows - 1) / p.max_rows;
-            int x = tiles;
+            const uint32_t tiles = ((uint32_t)n + (uint32_t)p.max_rows - 1) / (uint32_t)p.max_rows;
+            uint32_t x = min(tiles, most);
             #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, d);
-                if (lane >= d) x += y;
+                const uint32_t y = __shfl_up_sync(0xffffffffu, x, d);
+                if (lane >= d) x = min(x + y, most);
             }
             if (e < g.E) {
-                before[e] = sum + x - tiles; first[e] = s; count[e] = n;
-                height[e] = tiles > 0 ? ((n + tiles - 1) / tiles + 15) / 16 * 16 : 0;
+                before[e + 1] = (int)min(sum + x, most); first[e] = s; count[e] = n;
+                height[e] = tiles > 0 ? ((n + (int)tiles - 1) / (int)tiles + 15) / 16 * 16 : 0;
             }
-            sum += __shfl_sync(0xffffffffu, x, 31);
+            sum = min(sum + __shfl_sync(0xffffffffu, x, 31), most);
         }
-        if (lane == 0) before[g.E] = sum;
+        if (lane == 0) before[0] = 0;
     }
     tc::tc_fence_before_sync();
     __syncthreads();
@@ -697,7 +712,10 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
     if (warp == kMmaWarp) tc::tmem_dealloc(tmem, 512);
 }
 
-// Rows of a tile at most, from the rows that an expert has on average: what makes rounds of tiles times a tile's time least.
+// Rows of a tile at most, from the rows that an expert has on average: what makes rounds of tiles times a tile's time least.  A tile's time in clocks is the
+// longer of its expansion and products (350 for 256 codes, from 135 rows on 2.6 a row) and its outputs (500 and 20 a row; fitted to
+// measured times), and the shorter once more at the end.  65536 rows of 64 experts, 2048 x 2048 gated with codes, and 2048 x 1024 to bf16: 160 rows 271 and
+// 153 us, 144 280 and 162, 128 279 and 164, 112 304 and 179; more than 160 do not leave enough tensor memory for three slots of weights.
 TilesPlan make_plan(const ExpertsArgs& g)
 {
     TilesPlan p{};

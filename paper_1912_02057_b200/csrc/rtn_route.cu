@@ -24,8 +24,9 @@ namespace {
 constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
 constexpr int kMaxTokens = 128;             // of a block
-constexpr int kList = 8, kListThreads = 64; // a thread's list of a token's best; tokens of its block
-constexpr int64_t kListTokens = 4096;       // from here on
+constexpr int kList = 8, kShare = 4;        // a thread's list of a token's best; threads that share a token
+constexpr int kListTokens = 64, kListThreads = kListTokens * kShare;       // of a block
+constexpr int64_t kListFrom = 4096;         // tokens
 constexpr int kScanBlocks = 32;             // more: the counts are added up ahead (each block by itself reads them all)
 constexpr float kUnit = 5.9604644775390625e-8f;                // 2^-24
 
@@ -393,8 +394,10 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
     if (plan) note_block(g, chosen, t0, n_tok, words, counts);
 }
 
-// The same for many tokens, by logits alone and without groups: a thread takes a token and keeps its best kList experts in order while it goes through the
-// logits (a warp for each token: 600 instructions to a token, here 2 to 5 per expert and place of the list, for 32 of them).
+// The same for many tokens, by logits alone and without groups: kShare threads side by side take a token, every fourth 16 bytes of its logits each, and
+// keep the best kList experts of theirs in order; then the best of the four lists' heads is taken, top_k times, thread j % kShare has choice j.
+// (A warp for each token: 600 instructions to a token; here 2 to 5 per expert and place of the list, for 8 of them.  A thread for each token by
+// itself: one chain of the same length for all 128 experts, 110 threads to an SM.)
 template <typename T> struct Entry;         // a key and its index in one word where the type has 16 bits: the larger, the earlier
 template <> struct Entry<float> { uint32_t key; int index; };
 template <typename T> struct Entry { uint32_t both; };
@@ -434,67 +437,124 @@ __device__ __forceinline__ Entry<T> entry_of(T logit, int index)
 __device__ __forceinline__ int index_of(const Entry<float>& e) { return e.key != 0 ? e.index : -1; }
 template <typename T> __device__ __forceinline__ int index_of(const Entry<T>& e) { return e.both != 0 ? 0xffff - (int)(e.both & 0xffffu) : -1; }
 
+// The best of the heads of the lists of kShare threads, which its thread takes off its list.
+__device__ __forceinline__ Entry<float> take_best(Entry<float> (&list)[kList])
+{
+    uint32_t key = list[0].key;
+    #pragma unroll
+    for (int d = 1; d < kShare; d *= 2) key = max(key, __shfl_xor_sync(0xffffffffu, key, d));
+    int at = list[0].key == key ? list[0].index : 0x7fffffff;
+    const int own = at;
+    #pragma unroll
+    for (int d = 1; d < kShare; d *= 2) at = min(at, __shfl_xor_sync(0xffffffffu, at, d));
+    if (key != 0 && own == at) {
+        #pragma unroll
+        for (int j = 0; j + 1 < kList; ++j) list[j] = list[j + 1];
+        list[kList - 1] = Entry<float>{};
+    }
+    return Entry<float>{key, at};
+}
+template <typename T>
+__device__ __forceinline__ Entry<T> take_best(Entry<T> (&list)[kList])
+{
+    uint32_t both = list[0].both;
+    #pragma unroll
+    for (int d = 1; d < kShare; d *= 2) both = max(both, __shfl_xor_sync(0xffffffffu, both, d));
+    if (list[0].both == both) {                                 // (one thread, or nobody has any)
+        #pragma unroll
+        for (int j = 0; j + 1 < kList; ++j) list[j] = list[j + 1];
+        list[kList - 1] = Entry<T>{};
+    }
+    return Entry<T>{both};
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kListThreads)
 route_list_kernel(const __grid_constant__ RouteArgs g, int* counts)
 {
     extern __shared__ uint32_t chosen[];
-    constexpr int words = kListThreads / 32, kVec = 16 / (int)sizeof(T);
-    const int64_t t0 = (int64_t)blockIdx.x * kListThreads, t = t0 + threadIdx.x;
-    const int n_tok = g.T - t0 < kListThreads ? (int)(g.T - t0) : kListThreads, k = g.top_k;
+    constexpr int words = kListTokens / 32, kVec = 16 / (int)sizeof(T), kAhead = 4, kOwn = kList / kShare;
+    const int64_t t0 = (int64_t)blockIdx.x * kListTokens;
+    const int token = threadIdx.x / kShare, q = threadIdx.x % kShare;
+    const int n_tok = g.T - t0 < kListTokens ? (int)(g.T - t0) : kListTokens, k = g.top_k;
+    const int64_t t = t0 + (token < n_tok ? token : 0);         // (whoever has no token does another's, and writes nothing)
     const bool plan = g.start != nullptr;
     if (plan) {
         for (int i = threadIdx.x; i < g.E * words; i += kListThreads) chosen[i] = 0;
         __syncthreads();
     }
-    if (t < g.T) {
-        const T* row = static_cast<const T*>(g.logits) + t * g.stride;
-        Entry<T> list[kList];
+    const T* row = static_cast<const T*>(g.logits) + t * g.stride;
+    Entry<T> list[kList];
+    #pragma unroll
+    for (int j = 0; j < kList; ++j) list[j] = Entry<T>{};
+    const int vecs = (reinterpret_cast<uintptr_t>(row) & 15) == 0 ? g.E / kVec : 0;
+    #pragma unroll 1
+    for (int v0 = q; v0 < vecs; v0 += kShare * kAhead) {
+        uint4 u[kAhead];
         #pragma unroll
-        for (int j = 0; j < kList; ++j) list[j] = Entry<T>{};
-        auto take = [&](T logit, int e) { insert(list, entry_of(logit, e)); };
-        int e = 0;
-        if ((reinterpret_cast<uintptr_t>(row) & 15) == 0) {
-            uint4 next = g.E >= kVec ? *reinterpret_cast<const uint4*>(row) : make_uint4(0, 0, 0, 0);
-            for (; e + kVec <= g.E; e += kVec) {
-                const uint4 u = next;
-                if (e + 2 * kVec <= g.E) next = *reinterpret_cast<const uint4*>(row + e + kVec);
-                const T* v = reinterpret_cast<const T*>(&u);
-                #pragma unroll
-                for (int i = 0; i < kVec; ++i) take(v[i], e + i);
-            }
-        }
-        for (; e < g.E; ++e) take(row[e], e);
-        float top = -INFINITY, sum = 1.f;
-        if (g.score == RTN_SCORE_SOFTMAX && !g.renormalise && index_of(list[0]) >= 0) {
-            top = fminf(to_f32(row[index_of(list[0])]), FLT_MAX);
-            sum = 0.f;
-            for (int i = 0; i < g.E; ++i) {
-                const float v = to_f32(row[i]);
-                sum += v > -INFINITY ? __expf(fminf(v, FLT_MAX) - top) : 0.f;
-            }
-        }
-        float w[kList], all = 0.f, best = 0.f;
-        int pick[kList];
+        for (int i = 0; i < kAhead; ++i) u[i] = reinterpret_cast<const uint4*>(row)[v0 + i * kShare < vecs ? v0 + i * kShare : 0];
         #pragma unroll
-        for (int j = 0; j < kList; ++j) {
-            pick[j] = j < k ? index_of(list[j]) : -1;
-            w[j] = 0.f;
-            if (pick[j] < 0) continue;
-            const float x = fminf(to_f32(row[pick[j]]), FLT_MAX);
-            if (j == 0) best = x;
-            if (g.renormalise) w[j] = g.score == RTN_SCORE_SOFTMAX ? expf(x - best) : expf(fminf(x, 0.f) - fminf(best, 0.f)) / (1.f + expf(-fabsf(x)));
-            else w[j] = g.score == RTN_SCORE_SOFTMAX ? expf(x - top) / sum : 1.f / (1.f + expf(-x));
-            all += w[j];
+        for (int i = 0; i < kAhead; ++i) {
+            const int v = v0 + i * kShare;
+            if (v >= vecs) break;
+            const T* x = reinterpret_cast<const T*>(&u[i]);
+            #pragma unroll
+            for (int j = 0; j < kVec; ++j) insert(list, entry_of(x[j], v * kVec + j));
         }
-        if (!g.renormalise || all == 0.f) all = 1.f;
+    }
+    #pragma unroll 1
+    for (int e0 = vecs * kVec + q; e0 < g.E; e0 += kShare * kAhead) {
+        T x[kAhead];
         #pragma unroll
-        for (int j = 0; j < kList; ++j) {
-            if (j >= k) continue;
-            g.experts[t * k + j] = pick[j];
-            g.weights[t * k + j] = w[j] / all * g.scale;
-            if (plan && pick[j] >= 0) atomicOr(&chosen[pick[j] * words + threadIdx.x / 32], 1u << (threadIdx.x & 31));
+        for (int i = 0; i < kAhead; ++i) x[i] = row[e0 + i * kShare < g.E ? e0 + i * kShare : 0];
+        #pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (e0 + i * kShare < g.E) insert(list, entry_of(x[i], e0 + i * kShare));
+    }
+    __syncwarp();
+    int pick[kOwn], first = -1;
+    #pragma unroll
+    for (int j = 0; j < kList; ++j) {
+        const int at = index_of(take_best(list));
+        if (j == 0) first = at;
+        if (j % kShare == q) pick[j / kShare] = j < k ? at : -1;
+    }
+    const float best = first >= 0 ? fminf(to_f32(row[first]), FLT_MAX) : 0.f;
+    auto shared_sum = [](float x) {
+        #pragma unroll
+        for (int d = 1; d < kShare; d *= 2) x += __shfl_xor_sync(0xffffffffu, x, d);
+        return x;
+    };
+    float sum = 0.f, w[kOwn];
+    if (g.score == RTN_SCORE_SOFTMAX && !g.renormalise) {
+        #pragma unroll 4
+        for (int e = q; e < g.E; e += kShare) {
+            const float v = to_f32(row[e]);
+            sum += v > -INFINITY ? __expf(fminf(v, FLT_MAX) - best) : 0.f;
         }
+        sum = shared_sum(sum);
+    }
+    #pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        w[i] = 0.f;
+        if (pick[i] < 0) continue;
+        const float x = fminf(to_f32(row[pick[i]]), FLT_MAX);
+        if (g.score == RTN_SCORE_SOFTMAX) w[i] = expf(x - best);
+        else if (g.renormalise) w[i] = expf(fminf(x, 0.f) - fminf(best, 0.f)) / (1.f + expf(-fabsf(x)));
+        else w[i] = 1.f / (1.f + expf(-x));
+    }
+    if (g.renormalise) {
+        #pragma unroll
+        for (int i = 0; i < kOwn; ++i) sum += w[i];
+        sum = shared_sum(sum);
+    } else if (g.score == RTN_SCORE_SIGMOID) sum = 1.f;
+    #pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        const int j = i * kShare + q;
+        if (j >= k || token >= n_tok) continue;
+        g.experts[t * k + j] = pick[i];
+        g.weights[t * k + j] = pick[i] >= 0 ? w[i] / sum * g.scale : 0.f;
+        if (plan && pick[i] >= 0) atomicOr(&chosen[pick[i] * words + token / 32], 1u << (token & 31));
     }
     if (plan) note_block(g, chosen, t0, n_tok, words, counts);
 }
@@ -591,10 +651,10 @@ cudaError_t launch_route_experts(const RouteArgs& g, cudaStream_t s)
 {
     if (g.T == 0) return cudaMemsetAsync(g.start, 0, (size_t)(g.E + 1) * sizeof(int32_t), s);
     // A token to each warp while there are few (a token's chain is what counts), more with more, so that about two blocks to an SM hold them
-    // (by threads: 16384 tokens, 8 of 128 experts, all kernels LISTUS, by warps WARPUS)
-    const bool listed = g.T >= kListTokens && g.top_k <= kList && g.groups == 1 && g.bias == nullptr;
+    // (by threads: 16384 tokens, 8 of 128 experts of bf16, all kernels LISTUS, by warps WARPUS)
+    const bool listed = g.T >= kListFrom && g.top_k <= kList && g.groups == 1 && g.bias == nullptr;
     RoutePlan p{kWarps, 0, 0, false};
-    if (listed) p.tokens = kListThreads;
+    if (listed) p.tokens = kListTokens;
     else while (p.tokens < kMaxTokens && g.T > (int64_t)2 * device_sm_count() * p.tokens) p.tokens *= 2;
     const int64_t blocks = (g.T + p.tokens - 1) / p.tokens;
     const bool scanned = blocks > kScanBlocks;
@@ -607,7 +667,7 @@ cudaError_t launch_route_experts(const RouteArgs& g, cudaStream_t s)
     cudaError_t e = with_dtype(g.dtype, [&](auto t) {
         using T = decltype(t);
         if (listed) {
-            const size_t smem = g.start != nullptr ? (size_t)g.E * (kListThreads / 32) * 4 + 2 * (g.E + 1) * 4 : 0;
+            const size_t smem = g.start != nullptr ? (size_t)g.E * (kListTokens / 32) * 4 + 2 * (g.E + 1) * 4 : 0;
             route_list_kernel<T><<<(unsigned)blocks, kListThreads, smem, s>>>(g, c);
             return cudaGetLastError();
         }

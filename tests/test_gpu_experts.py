@@ -129,6 +129,29 @@ def test_route_rows_of_a_wider_tensor_no_tokens_and_no_plan():
     assert all(torch.equal(a, b) for a, b in zip(r, full))
 
 
+@pytest.mark.parametrize("T,E,k,dtype", [(4096, 8, 2, torch.bfloat16), (4133, 100, 8, torch.float16), (5000, 37, 7, torch.float32), (4100, 1024, 8, torch.bfloat16),
+                                         (4097, 3, 3, torch.float32), (6000, 132, 1, torch.float32)], ids=ids)
+def test_route_of_many_tokens(T, E, k, dtype):
+    """Few different values (ties everywhere) and some that are never chosen, rows that begin on and off 16 bytes."""
+    g = torch.Generator().manual_seed(T + E)
+    x = (torch.randint(-40, 41, (T, E + 3), generator=g).float() / 16)
+    x[torch.rand(T, E + 3, generator=g) < 0.05] = -float("inf")
+    x[torch.rand(T, E + 3, generator=g) < 0.02] = float("nan")
+    x[::97] = -float("inf")
+    wide = x.to(dtype).cuda()
+    for y in (wide[:, :E].contiguous(), wide[:, 1:E + 1]):
+        for score in (rtn.SCORE_SOFTMAX, rtn.SCORE_SIGMOID):
+            for renormalise in (True, False):
+                r = rtn.rtn_route_experts(y, k, score=score, renormalise=renormalise)
+                want = xref.route(ref.f64(y), k, kind=score, renormalise=renormalise)
+                for got, exact in zip((r.experts, r.start, r.place), (want[0], want[2], want[4])):
+                    assert np.array_equal(got.cpu().numpy(), exact), (score, renormalise)
+                rows = int(want[2][-1])
+                assert np.array_equal(r.tokens[:rows].cpu().numpy(), want[3][:rows])
+                # two exponentials of differences up to 5 (2.5 units each and their argument's rounding), E terms of a sum, a quotient
+                ref.assert_close(r.weights, want[1], np.abs(want[1]) + 2.0 ** -100, 40 + E / 2, "weights")
+
+
 def test_route_refusals():
     x = torch.randn(4, 12, device="cuda")
     for bad in (dict(top_k=0), dict(top_k=33), dict(top_k=2, bias=torch.zeros(11, device="cuda"))):
