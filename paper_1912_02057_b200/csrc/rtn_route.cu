@@ -9,7 +9,10 @@
 //   A block notes who chose what in a bit per (expert, token), so that a pair's place among its expert's rows is a count of bits
 //   whatever order the warps finish in, and so are the block's counts.
 // route_plan_kernel adds what lies before: the rows of lower experts, and of the expert's earlier blocks.  One block does both.
-// Bound: latency (a chain of about 40 clocks per pick) for few tokens, issue slots for many.
+// route_list_kernel does the first kernel's work for many tokens.
+// Bound: latency (two launches, a chain of about 40 clocks per pick) for few tokens, issue slots for many.
+// Measured (one B200): one token, 4 of 64 experts 8.5 us; 96 tokens, 8 of 256 in 4 of 8 groups, with a bias 14.3 us (most of it the chain of picks: 8
+// experts, 4 groups and the sums of 2 in each); 16384 tokens, 8 of 128 13.2 us (4.2 MB of logits: 0.6 us at the copy rate).
 #include "rtn_internal.cuh"
 #include "rtn_types.cuh"
 #include "rtn_tcgen05.cuh"
@@ -651,7 +654,9 @@ cudaError_t launch_route_experts(const RouteArgs& g, cudaStream_t s)
 {
     if (g.T == 0) return cudaMemsetAsync(g.start, 0, (size_t)(g.E + 1) * sizeof(int32_t), s);
     // A token to each warp while there are few (a token's chain is what counts), more with more, so that about two blocks to an SM hold them
-    // (by threads: 16384 tokens, 8 of 128 experts of bf16, all kernels LISTUS, by warps WARPUS)
+    // Lists from 4096 tokens on (in a graph on one B200, all kernels, us, lists and warps): 8 of 128 experts, bf16: 2048 tokens 10.6 and 9.2, 4096 10.6 and
+    // 11.1, 16384 13.2 and 22.8, 65536 31.6 and 70.2; 8 of 256, fp32: 2048 17.0 and 11.6, 4096 16.6 and 16.3, 16384 22.1 and 34.6.  Eight
+    // threads to a token, 64 tokens to a block: 12.7 at 16384 and 35.6 at 65536; four and 128: 12.8 and 30.8, but 12.3 for 10.9 at 8192.
     const bool listed = g.T >= kListFrom && g.top_k <= kList && g.groups == 1 && g.bias == nullptr;
     RoutePlan p{kWarps, 0, 0, false};
     if (listed) p.tokens = kListTokens;
