@@ -7,7 +7,10 @@
 //   y = sum_j w_j x_j, one rounding per term           E_y <= k sum_j |w_j x_j|   (0 without weights)
 //   1/sqrt(mean + eps) of a sum of squares over a tree  relative: (half of the tree's depth) + |E| / |.| (of the vector norms)
 // and so on through gate, scale and residual.  A value nearer to a threshold than its bound, or one that is not finite, makes the CTA work
-// the token's codes out again in double; of tokens of 2048 normal values about one in a hundred.
+// the token's codes out again in double; of tokens of 2048 normal values about one in a hundred.  That pass takes 10 us, which is what the last of a
+// launch's rows that needs it adds (with thresholds that nothing is near, the 129 us below are 117).
+// Measured (one B200): 8192 tokens of 2048, bf16, 8 experts' rows each, both norms, codes 129 us (407 MB: 62 at the copy rate; the rest is issue slots, some
+// 1100 instructions per 256 values); one token of 2048, 4 rows, codes 6.7 us; 48 of 4096, gated 5.8 us; 1111 of 5003, fp32, one value to an access 32.7 us.
 #include "rtn_internal.cuh"
 #include "rtn_epilogue.cuh"
 
@@ -428,7 +431,7 @@ __device__ __forceinline__ uint32_t spread(uint32_t x)
 }
 
 template <typename TB, typename TS, int EV, int NV, int kMaxThreads, bool kCodes>
-__global__ void __launch_bounds__(kMaxThreads, 1024 / kMaxThreads)
+__global__ void __launch_bounds__(kMaxThreads, kMaxThreads == 640 ? 2 : 1024 / kMaxThreads)
 block_norm_kernel(const __grid_constant__ NormArgs g)
 {
     __shared__ double red[2 * kMaxWarps];
@@ -519,15 +522,20 @@ cudaError_t launch_types(const NormArgs& g, cudaStream_t s)
                ok(g.stream_out, g.stream_stride, sizeof(TS)) && ok(g.post_weight, 0, 4) && ok(g.norm_weight, 0, 4) &&
                (g.n_scale == 1 || ok(g.scale, 0, 4)) && (g.n_thr == 1 || (ok(g.t_lo, 0, 4) && ok(g.t_hi, 0, 4)));
     };
+    // A thread has 8 values, whose arrays fit its registers, and only above 5120 16.  Rows of up to 5120 values in one or two to an access, two blocks of up to
+    // 640 threads to an SM instead of 16 values a thread, 1111 tokens, fp32, normed and codes: 5003 33.1 and 77.3 -> 32.7 and 63.6 us, 5002 33.9 and
+    // 69.4 -> 29.7 and 58.2, 2500 16.4 and 40.8 -> 11.5 and 32.1.
     if (fits(8)) {
         if (g.W <= 2048) return launch_values<TB, TS, 8, 1, 256>(g, s);
         return g.W <= 8192 ? launch_values<TB, TS, 8, 1, 1024>(g, s) : launch_values<TB, TS, 8, 2, 1024>(g, s);
     }
     if (fits(2)) {
         if (g.W <= 2048) return launch_values<TB, TS, 2, 4, 256>(g, s);
+        if (g.W <= 5120) return launch_values<TB, TS, 2, 4, 640>(g, s);
         return g.W <= 8192 ? launch_values<TB, TS, 2, 8, 512>(g, s) : launch_values<TB, TS, 2, 8, 1024>(g, s);
     }
     if (g.W <= 2048) return launch_values<TB, TS, 1, 8, 256>(g, s);
+    if (g.W <= 5120) return launch_values<TB, TS, 1, 8, 640>(g, s);
     return g.W <= 8192 ? launch_values<TB, TS, 1, 16, 512>(g, s) : launch_values<TB, TS, 1, 16, 1024>(g, s);
 }
 
