@@ -4,13 +4,13 @@
 // Bound: HBM, every input and output once.
 //
 // Codes are those of the exact value.  Beside each value runs a bound on its rounding error in units of u = 2^-24 (to first order):
-//   y = sum_j w_j x_j, one rounding per term           E_y <= k sum_j |w_j x_j|   (0 without weights)
+//   y = sum_j w_j x_j, one rounding per term           E_y <= the sum of the partial sums' magnitudes   (0 without experts)
 //   1/sqrt(mean + eps) of a sum of squares over a tree  relative: (half of the tree's depth) + |E| / |.| (of the vector norms)
 // and so on through gate, scale and residual.  A value nearer to a threshold than its bound, or one that is not finite, makes the CTA work
 // the token's codes out again in double; of tokens of 2048 normal values about one in a hundred.  That pass takes 10 us, which is what the last of a
-// launch's rows that needs it adds (with thresholds that nothing is near, the 129 us below are 117).
-// Measured (one B200): 8192 tokens of 2048, bf16, 8 experts' rows each, both norms, codes 129 us (407 MB: 62 at the copy rate; the rest is issue slots, some
-// 1100 instructions per 256 values); one token of 2048, 4 rows, codes 6.7 us; 48 of 4096, gated 5.8 us; 1111 of 5003, fp32, one value to an access 32.7 us.
+// launch's rows that needs it adds (with thresholds that nothing is near, the 123 us below are 112).
+// Measured (one B200): 8192 tokens of 2048, bf16, 8 experts' rows each, both norms, codes 123 us (407 MB: 62 at the copy rate; the rest is issue slots, some
+// 1200 instructions per 256 values); one token of 2048, 4 rows, codes 6.7 us; 48 of 4096, gated 5.8 us; 1111 of 5003, fp32, one value to an access 32.7 us.
 #include "rtn_internal.cuh"
 #include "rtn_epilogue.cuh"
 
@@ -108,7 +108,7 @@ template <typename TB, typename TS, int EV, int NV, bool kTrack>
 __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* red, float (&h)[NV][EV], float (&n)[NV][EV], float (&slack)[NV][EV])
 {
     const int W = g.W, step = blockDim.x * EV, first = threadIdx.x * EV;
-    const float k_units = g.place != nullptr ? (float)g.k : 0.f, mean = 1.f / (float)W;
+    const float mean = 1.f / (float)W;
     float zero = 0.f, ss = 0.f, sm = 0.f;
     int at[NV];                                                 // a value's column, or 0 behind the row's end
     bool in[NV];
@@ -119,7 +119,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
         #pragma unroll
         for (int v = 0; v < NV; ++v) res[v] = ask<TS, EV>(static_cast<const TS*>(g.residual) + t * g.residual_stride, at[v]);
     }
-    // y in h, the sum of its terms' magnitudes in slack
+    // y in h, the sum of its partial sums' magnitudes in slack
     #pragma unroll
     for (int v = 0; v < NV; ++v)
         #pragma unroll
@@ -147,10 +147,14 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
                 for (int v = 0; v < NV; ++v) {
                     float f[EV];
                     take<TB, EV>(x[i][v], ok[i], f);
-                    #pragma unroll
-                    for (int e = 0; e < EV; ++e) {
-                        h[v][e] = fmaf(w[i], f[e], h[v][e]);
-                        if constexpr (kTrack) slack[v][e] = fmaf(fabsf(w[i]), fabsf(f[e]), slack[v][e]);
+                    if constexpr (EV > 1) {                                      // (two products to an instruction)
+                        #pragma unroll
+                        for (int e = 0; e < EV; e += 2)
+                            take_pair(fma_pair(make_pair(w[i], w[i]), make_pair(f[e], f[e + 1]), make_pair(h[v][e], h[v][e + 1])), h[v][e], h[v][e + 1]);
+                    } else h[v][0] = fmaf(w[i], f[0], h[v][0]);
+                    if constexpr (kTrack) {
+                        #pragma unroll
+                        for (int e = 0; e < EV; ++e) slack[v][e] += fabsf(h[v][e]);
                     }
                 }
         }
@@ -218,7 +222,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
         }
         block_sums(ss, kTrack ? sm : zero, red);
         const float post = rsqrtf(fmaf(ss, mean, g.eps));
-        if constexpr (kTrack) post_units = kRootUnits<NV, EV> + 2.f + (ss > 0.f ? k_units * root_of_ratio(sm, ss) : 0.f);
+        if constexpr (kTrack) post_units = kRootUnits<NV, EV> + 2.f + (ss > 0.f ? root_of_ratio(sm, ss) : 0.f);
         #pragma unroll
         for (int v = 0; v < NV; ++v)
             #pragma unroll
@@ -237,7 +241,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
             const float y = h[v][i], m = slack[v][i], q = in[v] ? f[v][i] : 0.f;       // (behind the row's end y, its terms and r are zeros)
             h[v][i] = fmaf(q, y, r[i]);
             if constexpr (kTrack) {
-                slack[v][i] = fmaf(fabsf(q), fmaf(k_units, m, y_units * fabsf(y)), fabsf(h[v][i]));
+                slack[v][i] = fmaf(fabsf(q), fmaf(y_units, fabsf(y), m), fabsf(h[v][i]));
                 sm = fmaf(slack[v][i], slack[v][i], sm);
             }
             ss = fmaf(h[v][i], h[v][i], ss);
@@ -292,7 +296,7 @@ __device__ __forceinline__ bool code_row(const NormArgs& g, const float (&n)[NV]
             up |= (uint32_t)a << (v * EV + i);
             down |= (uint32_t)b << (v * EV + i);
             const float d = fminf(fabsf(x - lo[i]), fabsf(x - hi[i]));        // (a difference that small is exact but for its own rounding)
-            near = near || !(d > 1.25f * kUnit * slack[v][i]);                       // (of a NaN, and of what overflowed)
+            near = near || !(d > fmaf(1.25f * kUnit, slack[v][i], 1e-37f));          // (of a NaN, and of what over- or underflowed)
         }
     }
     return near;
