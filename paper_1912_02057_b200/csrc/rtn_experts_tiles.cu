@@ -10,7 +10,7 @@
 // next one's products; parameters are fetched two tiles ahead by warps of their own, which also put a token's codes together from the votes.
 // Codes are those of the exact output: a value nearer to a threshold than its error bound is worked out again in double, of 16 tokens at a time.
 // Bound: for long prompts the instructions of the epilogue (50 to 65 per output) and of the expansion (some 200 per 32 rows x 256 codes), the tensor
-// pipe idles two thirds of the time; for few rows of an expert its start (2.6 us) and the first planes' way (2.6 us).
+// pipe idles three quarters of the time; for few rows of an expert its start (2.6 us) and the first planes' way (2.6 us).
 // Measured (one B200): 65536 rows, 64 experts of 2048 x 2048, gated, codes 269 us (2.0 PFLOP/s; the matrix instructions alone 63); of 2048 x 1024, bf16
 // values 156 us (268 MB written); 384 rows, 64 experts of 2048 x 2048, gated, codes 29.5 us (67 MB of planes at 2.3 TB/s).
 #include "rtn_experts.cuh"
