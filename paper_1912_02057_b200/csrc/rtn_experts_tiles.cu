@@ -306,66 +306,58 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         }
     } else if (warp >= kLoadWarp && warp < kEdgeWarp) {
       fewer_registers<kIssueRegs>();
-      // Tile t's row tile for one thread.
-      auto find_one = [&](uint32_t t) {
-          const int rt = (int)(t / cols);
-          while (rt >= before[seen + 1]) ++seen;
-          return rt - before[seen];
-      };
-      auto wait = [&](uint64_t* m, uint32_t parity) {
-          if (tc::mbar_wait_tries(m, parity & 1u, kTries)) return true;
-          *dead = 1;
-          return false;
-      };
+      // (Tiles are looked up by whole warps: one thread that went on expert by expert took 2000 clocks where tiles are few to an expert.)
       if (warp == kLoadWarp) {
         // ------------------------------------------------------------ copies of input rows (one takes some 60 clocks to issue: few and large)
-        if (lane == 0) {
-            tc::pdl_wait();
-            const uint32_t box_bytes = (uint32_t)p.box_rows * 128u;
-            int s = 0;
-            uint32_t phase = 0;
-            for (uint32_t t = blockIdx.x; t < total && alive; t += gridDim.x) {
-                const int at = find_one(t), h = height[seen], row = first[seen] + at * h;
-                const int boxes = (h + p.box_rows - 1) / p.box_rows;              // (what lies behind the tile's rows belongs to no output)
-                for (int k = 0; k < spans; ++k) {
-                    if (!(alive = wait(&bar.empty[s], phase + 1))) break;
-                    const int halves = halves_in(k);
+        tc::pdl_wait();
+        const uint32_t elected = tc::elect_one(), box_bytes = (uint32_t)p.box_rows * 128u;
+        int s = 0;
+        uint32_t phase = 0;
+        for (uint32_t t = blockIdx.x; t < total && alive; t += gridDim.x) {
+            const Tile tile = find(t);
+            const int boxes = (tile.height + p.box_rows - 1) / p.box_rows;        // (what lies behind the tile's rows belongs to no output)
+            for (int k = 0; k < spans; ++k) {
+                if (!(alive = warp_wait(&bar.empty[s], phase + 1))) break;
+                const int halves = halves_in(k);
+                if (elected) {
                     tc::mbar_arrive_expect_tx(&bar.full[s], (uint32_t)(halves * boxes) * box_bytes);
                     uint32_t dst = ring + (uint32_t)s * 2 * p.half_bytes;
                     for (int h = 0; h < halves; ++h, dst += p.half_bytes) {
-                        load_box(dst, &map, k * 256 + h * 128, row, &bar.full[s]);
-                        if (boxes > 1) load_box(dst + box_bytes, &map, k * 256 + h * 128, row + p.box_rows, &bar.full[s]);
+                        load_box(dst, &map, k * 256 + h * 128, tile.row, &bar.full[s]);
+                        if (boxes > 1) load_box(dst + box_bytes, &map, k * 256 + h * 128, tile.row + p.box_rows, &bar.full[s]);
                     }
-                    if (++s == p.stages) { s = 0; phase ^= 1; }
                 }
+                __syncwarp();
+                if (++s == p.stages) { s = 0; phase ^= 1; }
             }
-            // nobody leaves while copies are on their way: the last of each slot
-            for (int i = 0; i < p.stages; ++i) {
-                const uint32_t uses = i < s ? phase + 1 : phase;                  // parity of the number of copies to this slot
-                tc::mbar_wait_tries(&bar.full[i], (uses + 1) & 1u, kTries);
-            }
+        }
+        // nobody leaves while copies are on their way: the last of each slot
+        for (int i = 0; i < p.stages; ++i) {
+            const uint32_t uses = i < s ? phase + 1 : phase;                      // parity of the number of copies to this slot
+            tc::mbar_wait_tries(&bar.full[i], (uses + 1) & 1u, kTries);
         }
       } else if (warp == kPlanesWarp) {
         // ------------------------------------------------------------ copies of planes
-        if (lane == 0) {
-            int s = 0;
-            uint32_t phase = 0;
-            for (uint32_t t = blockIdx.x; t < total && alive; t += gridDim.x) {
-                find_one(t);
-                const int row = (int)((int64_t)seen * g.N + (int64_t)(t % cols) * kTileOuts);
-                for (int k = 0; k < spans; ++k) {
-                    if (!(alive = wait(&bar.planes_empty[s], phase + 1))) break;
+        const uint32_t elected = tc::elect_one();
+        int s = 0;
+        uint32_t phase = 0;
+        for (uint32_t t = blockIdx.x; t < total && alive; t += gridDim.x) {
+            const int row = (int)((int64_t)find(t).e * g.N + (int64_t)(t % cols) * kTileOuts);
+            for (int k = 0; k < spans; ++k) {
+                if (!(alive = warp_wait(&bar.planes_empty[s], phase + 1))) break;
+                if (elected) {
                     tc::mbar_arrive_expect_tx(&bar.planes_full[s], kSpanBytes);
                     const uint32_t dst = ring - p.ring + p.planes + (uint32_t)s * kSpanBytes;
                     load_box(dst, &weight_map, k * 128, row, &bar.planes_full[s]);                          // (rows of other outputs behind the last,
                     if (kGated) load_box(dst + kSpanBytes / 2, &weight_map, k * 128, row + (int)g.F, &bar.planes_full[s]);          // zeros behind the last row)
-                    if (++s == p.spans) { s = 0; phase ^= 1; }
                 }
+                __syncwarp();
+                if (++s == p.spans) { s = 0; phase ^= 1; }
             }
-            for (int i = 0; i < p.spans; ++i) {
-                const uint32_t uses = i < s ? phase + 1 : phase;
-                tc::mbar_wait_tries(&bar.planes_full[i], (uses + 1) & 1u, kTries);
-            }
+        }
+        for (int i = 0; i < p.spans; ++i) {
+            const uint32_t uses = i < s ? phase + 1 : phase;
+            tc::mbar_wait_tries(&bar.planes_full[i], (uses + 1) & 1u, kTries);
         }
       } else if (warp == kMmaWarp) {
         // ------------------------------------------------------------ products
