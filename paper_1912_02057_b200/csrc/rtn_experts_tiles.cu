@@ -58,17 +58,18 @@ struct Bars {
     int dead;
 };
 
-// What the epilogue of a tile needs: a_s, a_s S_x, a_o and input row (-1: out of range) of its tokens, w_s, w_o, p3 and bias of its weight rows by
+// What the epilogue of a tile needs (looking the tile up itself, it lost 700 of a tile's 4000 clocks): a_s, a_s S_x, a_o and input row (-1: out of range) of its tokens, w_s, w_o, p3 and bias of its weight rows by
 // TMEM lane; the votes of each 16 tokens and quarter of the lanes.
+struct Tile { int e, row, rows, height; };
+
 struct TileParams {
     float as[kMaxRows], asx[kMaxRows], ao[kMaxRows];
     int token[kMaxRows];
     float4 col[128];
     uint4 most_asx, most_ao;                                    // the largest |a_s S_x| and |a_o|, in four parts, as bit patterns (a NaN is the largest)
     uint4 votes[4][kMaxRows / 4][2];
+    Tile tile;
 };
-
-struct Tile { int e, row, rows, height; };
 
 // 32 codes (a word of each plane) as four words of 4-bit values; nibble i of word r is code 4 i + r.  The magnitude of a nonzero weight is
 // 1/2, 1, 2, 1 by r, so that the plane's bits are used where they are, and an input's its reciprocal: their product is 1.
@@ -213,7 +214,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
     // Tiles go round the CTAs with the columns fastest: those at work at a time share their rows.
     const uint32_t cols = (uint32_t)p.col_tiles, total = (uint32_t)before[g.E] * cols;
     int seen = 0;                                                                 // this warp's last expert: tiles only go up
-    auto find_from = [&](uint32_t t, int& seen) {                                 // whole warp
+    auto find = [&](uint32_t t) {                                                 // whole warp
         const int rt = (int)(t / cols);
         Tile r{0, 0, 0, 16};
         for (; seen < g.E; seen += 32) {
@@ -229,7 +230,6 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         r.rows = left < r.height ? left : r.height;
         return r;
     };
-    auto find = [&](uint32_t t) { return find_from(t, seen); };
     auto warp_wait = [&](uint64_t* m, uint32_t parity) {
         const bool ok = __all_sync(0xffffffffu, tc::mbar_wait_tries(m, parity & 1u, kTries)) != 0;
         if (!ok) *dead = 1;
@@ -396,20 +396,22 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         const int part = warp - kEdgeWarp;
         int m[kEach], m_next[kEach];                                              // -1: out of range, -2: no such row
         float ws = 0.f, wo = 0.f, bias = 0.f, as[kEach], ao[kEach];
-        int sw = 0, sx[kEach], seen_params = 0;
+        int sw = 0, sx[kEach];
+        Tile asked{}, tile{};                                                     // whose rows, and whose parameters, have been asked for last
         auto row_of = [&](int i) { return lane + 32 * (part + 4 * i); };
         auto ask_rows = [&](uint32_t t) {
             #pragma unroll
             for (int i = 0; i < kEach; ++i) m_next[i] = -2;
             if (t >= total) return;
-            const Tile tile = find(t);
+            asked = find(t);
             #pragma unroll
             for (int i = 0; i < kEach; ++i)
-                if (row_of(i) < tile.rows) m_next[i] = g.tokens != nullptr ? __ldg(g.tokens + tile.row + row_of(i)) : tile.row + row_of(i);
+                if (row_of(i) < asked.rows) m_next[i] = g.tokens != nullptr ? __ldg(g.tokens + asked.row + row_of(i)) : asked.row + row_of(i);
         };
         auto ask_params = [&](uint32_t t) {
             if (t >= total) return;
-            const int64_t first_row = (int64_t)find_from(t, seen_params).e * g.N;
+            tile = asked;
+            const int64_t first_row = (int64_t)tile.e * g.N;
             #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 m[i] = m_next[i];
@@ -440,7 +442,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             }
             here.col[part * 32 + lane] = make_float4(ws, wo, (float)((double)ws * (double)sw + (double)g.K * (double)wo), bias);
             most_asx = __reduce_max_sync(0xffffffffu, most_asx); most_ao = __reduce_max_sync(0xffffffffu, most_ao);
-            if (lane == 0) { (&here.most_asx.x)[part] = most_asx; (&here.most_ao.x)[part] = most_ao; }
+            if (lane == 0) { (&here.most_asx.x)[part] = most_asx; (&here.most_ao.x)[part] = most_ao; if (part == 0) here.tile = tile; }
             if (bad && t % cols == 0) atomicOr(g.status, kStatusBadIndex);
             __threadfence_block();
             __syncwarp();
@@ -455,12 +457,11 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         tell(blockIdx.x + gridDim.x, 1);
         tc::pdl_wait();
         uint32_t ti = 0;
-        int seen_codes = 0;
         for (uint32_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
-            const Tile tile = find_from(t, seen_codes);
             if (!(alive = warp_wait(&bar.votes_full[ti & 1], ti >> 1))) break;
             if constexpr (kCodes) {
                 const TileParams& here = params[ti & 1];
+                const Tile tile = here.tile;
                 const int64_t f0 = (int64_t)(t % cols) * kTileOuts, width = (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes;
                 #pragma unroll 1
                 for (int r = lane + 32 * part; r < tile.rows; r += 32 * kEdgeWarps) {
@@ -516,12 +517,10 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         const float units = g.act == RTN_ACT_SILU ? 8.3f : g.act == RTN_ACT_NONE || g.act == RTN_ACT_RELU ? 2.f : 18.3f;
         const float c1 = (units + (kGated ? 3.f : 0.f)) * 1.1f * kUnit;
         uint32_t ti = 0;
-        Tile next{};
-        if (blockIdx.x < total) next = find(blockIdx.x);
         for (uint32_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
-            const Tile tile = next;
             TileParams& here = params[ti & 1];
             if (!(alive = warp_wait(&bar.params_full[ti & 1], ti >> 1))) break;
+            const Tile tile = here.tile;
             // this thread's weight rows: kOwn outputs, or kOwn and the kOwn that they are multiplied with
             pair_t ws[4], wo[4], p3[4], bias[4];
             float off = 0.f, lo = 0.f, hi = 0.f, most_asx = 0.f, most_ao = 0.f;
@@ -547,7 +546,6 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             if constexpr (kCodes) { lo = g.t_lo[g.n_thr == 1 ? 0 : tile.e]; hi = g.t_hi[g.n_thr == 1 ? 0 : tile.e]; c0 = 4.6f * 1.1f * kUnit * off; c2 = 0.8f * off; }
             if (!kGated && g.act == RTN_ACT_RELU && lo <= 0.f) lo = -FLT_MAX;        // (never below it: a threshold of 0 is not near)
             const int64_t f = output_at(t, quad, r8);                              // the first of this thread's outputs
-            if (t + gridDim.x < total) next = find(t + gridDim.x);
             if (!(alive = warp_wait(&bar.acc_full[ti & 1], ti >> 1))) break;
             tc::tc_fence_after_sync();
             const uint32_t acc = tmem + (ti & 1) * acc_cols + ((uint32_t)(quad * 32) << 16);
