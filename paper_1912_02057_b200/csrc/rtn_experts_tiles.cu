@@ -28,7 +28,7 @@ namespace {
 constexpr int kExpandWarps = 8, kEpilogueWarps = 8, kEdgeWarps = 4;
 constexpr int kLoadWarp = kExpandWarps + kEpilogueWarps, kPlanesWarp = kLoadWarp + 1, kMmaWarp = kLoadWarp + 2, kEdgeWarp = kLoadWarp + 4;
 constexpr int kThreads = (kEdgeWarp + kEdgeWarps) * 32;
-constexpr int kLaunchRegs = 80, kExpandRegs = 80, kEpilogueRegs = 112, kIssueRegs = 40, kEdgeRegs = 56;
+constexpr int kLaunchRegs = 80, kExpandRegs = 80, kEpilogueRegs = 104, kIssueRegs = 40, kEdgeRegs = 72;
 static_assert(kThreads == 768 && 2 * kExpandRegs + 2 * kEpilogueRegs + kIssueRegs + kEdgeRegs <= 6 * kLaunchRegs, "registers");
 template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
 template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
@@ -171,27 +171,36 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
     if (warp == 0) {
         const uint32_t most = 0x7fffffffu / (uint32_t)p.col_tiles;               // (bounds that overlap can add up to any number of tiles)
         uint32_t sum = 0;
-        for (int e0 = 0; e0 < g.E; e0 += 32) {
-            const int e = e0 + lane;
-            int s = 0, n = 0;
-            if (e < g.E) {
-                s = g.start[e];
-                const int64_t len = (int64_t)g.start[e + 1] - s;
-                if (s >= 0 && len >= 0 && s + len <= g.R) n = (int)len;
-                else if (blockIdx.x == 0) atomicOr(g.status, kStatusBadIndex);
-            }
-            const uint32_t tiles = ((uint32_t)n + (uint32_t)p.max_rows - 1) / (uint32_t)p.max_rows;
-            uint32_t x = min(tiles, most);
+        constexpr int kTogether = 4;                                              // bounds of 32 experts on their way
+        #pragma unroll 1
+        for (int e0 = 0; e0 < g.E; e0 += 32 * kTogether) {
+            int from[kTogether], to[kTogether];
             #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const uint32_t y = __shfl_up_sync(0xffffffffu, x, d);
-                if (lane >= d) x = min(x + y, most);
+            for (int i = 0; i < kTogether; ++i) {
+                const int e = e0 + 32 * i + lane < g.E ? e0 + 32 * i + lane : 0;
+                from[i] = g.start[e]; to[i] = g.start[e + 1];
             }
-            if (e < g.E) {
-                before[e + 1] = (int)min(sum + x, most); first[e] = s; count[e] = n;
-                height[e] = tiles > 0 ? ((n + (int)tiles - 1) / (int)tiles + 15) / 16 * 16 : 0;
+            #pragma unroll
+            for (int i = 0; i < kTogether; ++i) {
+                const int e = e0 + 32 * i + lane;
+                if (e0 + 32 * i >= g.E) break;
+                int n = 0;
+                const int64_t len = (int64_t)to[i] - from[i];
+                if (from[i] >= 0 && len >= 0 && from[i] + len <= g.R) n = e < g.E ? (int)len : 0;
+                else if (e < g.E && blockIdx.x == 0) atomicOr(g.status, kStatusBadIndex);
+                const uint32_t tiles = ((uint32_t)n + (uint32_t)p.max_rows - 1) / (uint32_t)p.max_rows;
+                uint32_t x = min(tiles, most);
+                #pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const uint32_t y = __shfl_up_sync(0xffffffffu, x, d);
+                    if (lane >= d) x = min(x + y, most);
+                }
+                if (e < g.E) {
+                    before[e + 1] = (int)min(sum + x, most); first[e] = from[i]; count[e] = n;
+                    height[e] = tiles > 0 ? ((n + (int)tiles - 1) / (int)tiles + 15) / 16 * 16 : 0;
+                }
+                sum = min(sum + __shfl_sync(0xffffffffu, x, 31), most);
             }
-            sum = min(sum + __shfl_sync(0xffffffffu, x, 31), most);
         }
         if (lane == 0) before[0] = 0;
     }
