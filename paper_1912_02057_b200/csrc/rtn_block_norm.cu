@@ -13,6 +13,7 @@
 // 1200 instructions per 256 values); one token of 2048, 4 rows, codes 6.7 us; 48 of 4096, gated 5.8 us; 1111 of 5003, fp32, one value to an access 32.7 us.
 #include "rtn_internal.cuh"
 #include "rtn_epilogue.cuh"
+#include "rtn_tcgen05.cuh"
 
 namespace rtn {
 
@@ -440,6 +441,7 @@ block_norm_kernel(const __grid_constant__ NormArgs g)
 {
     __shared__ double red[2 * kMaxWarps];
     const int64_t t = blockIdx.x;
+    tc::pdl_wait();
     float h[NV][EV], n[NV][EV], slack[NV][EV];
     norm_row<TB, TS, EV, NV, kCodes>(g, t, reinterpret_cast<float*>(red), h, n, slack);
     if constexpr (kCodes) {
@@ -507,9 +509,8 @@ cudaError_t launch_values(const NormArgs& g, cudaStream_t s)
 {
     const int width = (g.W + kBlockCodes - 1) / kBlockCodes * kBlockCodes;         // (the padding of a packed row is written too)
     const int threads = ((width + EV * NV - 1) / (EV * NV) + 31) / 32 * 32;
-    if (g.out_packed != nullptr) block_norm_kernel<TB, TS, EV, NV, kMaxThreads, true><<<(unsigned)g.T, threads, 0, s>>>(g);
-    else block_norm_kernel<TB, TS, EV, NV, kMaxThreads, false><<<(unsigned)g.T, threads, 0, s>>>(g);
-    return cudaGetLastError();
+    const bool coded = g.out_packed != nullptr;
+    return launch_pdl(coded ? block_norm_kernel<TB, TS, EV, NV, kMaxThreads, true> : block_norm_kernel<TB, TS, EV, NV, kMaxThreads, false>, dim3((unsigned)g.T), dim3(threads), 0, s, g);
 }
 
 template <typename TB, typename TS>

@@ -129,6 +129,7 @@ experts_rows_kernel(const __grid_constant__ ExpertsArgs g, int GL, int col_block
 __global__ void __launch_bounds__(256)
 zero_sums_kernel(const ExpertsArgs g)
 {
+    tc::pdl_wait();
     tc::pdl_trigger();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i < g.R && i >= g.start[0] && i < g.start[g.E]) g.out_sum[i] = 0;
@@ -147,8 +148,7 @@ cudaError_t launch_rows(const ExpertsArgs& g, cudaStream_t s)
     if (cols * tiles > 0x7fffffff) return cudaErrorInvalidConfiguration;
     const unsigned grid = (unsigned)(cols * tiles);
     if (g.out_packed != nullptr) {
-        zero_sums_kernel<<<(unsigned)((g.R + 255) / 256), 256, 0, s>>>(g);
-        const cudaError_t e = cudaGetLastError();
+        const cudaError_t e = launch_pdl(zero_sums_kernel, dim3((unsigned)((g.R + 255) / 256)), dim3(256), 0, s, g);
         if (e != cudaSuccess) return e;
         return launch_pdl(g.gated ? experts_rows_kernel<MT, true, true> : experts_rows_kernel<MT, false, true>, dim3(grid), dim3(kThreads), 0, s, g, GL, (int)cols);
     } else {

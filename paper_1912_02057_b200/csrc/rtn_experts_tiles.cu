@@ -119,7 +119,8 @@ __host__ __device__ __forceinline__ int halves_of(int nblk) { return nblk / 4 * 
 __global__ void __launch_bounds__(256)
 expand_inputs_kernel(const __grid_constant__ ExpertsArgs g, int nblk, int chunks, uint2* __restrict__ out)
 {
-    tc::pdl_trigger();
+    tc::pdl_wait();
+    tc::pdl_trigger();                                          // (now that what the products read ahead of their own wait is there)
     const uint32_t i = blockIdx.x * 256u + threadIdx.x;
     const uint32_t row = i / (uint32_t)chunks, c = i % (uint32_t)chunks;          // a chunk: 32 codes, four words
     if (row >= g.R || row < (uint32_t)g.start[0] || row >= (uint32_t)g.start[g.E]) return;
@@ -766,8 +767,8 @@ cudaError_t launch_experts_tiles(const ExpertsArgs& g, cudaStream_t s)
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) e = cudaErrorInvalidValue;
     if (e == cudaSuccess) {
         const int64_t threads = g.R * (pitch / 16);
-        expand_inputs_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(g, nblk, pitch / 16, static_cast<uint2*>(scratch));
-        e = cudaGetLastError();
+        // (its launch under the end of what ran before, too: calls one after the other 24.6 -> 21.6 us for 384 rows of 2048 x 2048)
+        e = launch_pdl(expand_inputs_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, g, nblk, pitch / 16, static_cast<uint2*>(scratch));
     }
     if (e == cudaSuccess) {
         e = with_dtype(g.dtype, [&](auto t) {

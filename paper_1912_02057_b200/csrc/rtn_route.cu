@@ -257,6 +257,7 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
     const int n_tok = g.T - t0 < p.tokens ? (int)(g.T - t0) : p.tokens;
     const bool plan = g.start != nullptr;
     const int k = g.top_k;
+    tc::pdl_wait();
     float bias[VPL];
     #pragma unroll
     for (int i = 0; i < VPL; ++i) bias[i] = kScored && g.bias != nullptr && lane * VPL + i < g.E ? g.bias[lane * VPL + i] : 0.f;
@@ -486,6 +487,7 @@ route_list_kernel(const __grid_constant__ RouteArgs g, int* counts)
         for (int i = threadIdx.x; i < g.E * words; i += kListThreads) chosen[i] = 0;
         __syncthreads();
     }
+    tc::pdl_wait();
     const T* row = static_cast<const T*>(g.logits) + t * g.stride;
     Entry<T> list[kList];
     #pragma unroll
@@ -643,9 +645,8 @@ cudaError_t launch_choose(const RouteArgs& g, RoutePlan p, int* counts, unsigned
     while (p.side_by_side && 1 << p.group_shift < lanes) ++p.group_shift;
     const size_t smem = g.start != nullptr ? (size_t)g.E * ((p.tokens + 31) / 32) * 4 + 2 * (g.E + 1) * 4 : 0;
     // scores have to be computed where a bias or a sum of them is compared
-    if (g.bias != nullptr || (g.groups > 1 && g.group_top > 1)) route_choose_kernel<T, VPL, true><<<blocks, kThreads, smem, s>>>(g, p, counts);
-    else route_choose_kernel<T, VPL, false><<<blocks, kThreads, smem, s>>>(g, p, counts);
-    return cudaGetLastError();
+    const bool scored = g.bias != nullptr || (g.groups > 1 && g.group_top > 1);
+    return launch_pdl(scored ? route_choose_kernel<T, VPL, true> : route_choose_kernel<T, VPL, false>, dim3(blocks), dim3(kThreads), smem, s, g, p, counts);
 }
 
 }  // namespace
@@ -673,8 +674,7 @@ cudaError_t launch_route_experts(const RouteArgs& g, cudaStream_t s)
         using T = decltype(t);
         if (listed) {
             const size_t smem = g.start != nullptr ? (size_t)g.E * (kListTokens / 32) * 4 + 2 * (g.E + 1) * 4 : 0;
-            route_list_kernel<T><<<(unsigned)blocks, kListThreads, smem, s>>>(g, c);
-            return cudaGetLastError();
+            return launch_pdl(route_list_kernel<T>, dim3((unsigned)blocks), dim3(kListThreads), smem, s, g, c);
         }
         if (g.E <= 32) return launch_choose<T, 1>(g, p, c, (unsigned)blocks, s);
         if (g.E <= 64) return launch_choose<T, 2>(g, p, c, (unsigned)blocks, s);
@@ -687,11 +687,8 @@ cudaError_t launch_route_experts(const RouteArgs& g, cudaStream_t s)
         const size_t smem = (size_t)3 * (g.E + 1) * sizeof(int);
         if (scanned) {
             e = launch_pdl(route_scan_kernel, dim3((unsigned)g.E), dim3(256), 0, s, g.E, c, blocks);
-            // (not overlapped: it reads what the kernel before the last one has written)
-            if (e == cudaSuccess) {
-                route_plan_kernel<<<(unsigned)blocks, kThreads, smem, s>>>(g, c, blocks, p.tokens, true);
-                e = cudaGetLastError();
-            }
+            // (it reads what the kernel before the last one has written, which the last one has waited for)
+            if (e == cudaSuccess) e = launch_pdl(route_plan_kernel, dim3((unsigned)blocks), dim3(kThreads), smem, s, g, (const int*)counts, blocks, p.tokens, true);
         } else {
             e = launch_pdl(route_plan_kernel, dim3((unsigned)blocks), dim3(kThreads), smem, s, g, (const int*)counts, blocks, p.tokens, false);
         }

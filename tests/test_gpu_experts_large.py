@@ -170,3 +170,69 @@ def test_the_longest_rows(R):
     want = torch.stack([(first, second)[i % 2] for i in range(R)])
     assert torch.equal(got.double().cpu(), want)
     assert rtn.rtn_last_device_status() == 0
+
+
+def joined(T, W, E):
+    """Inputs that two streams make, each at the end of long work of its own, then the operators at once."""
+    g = gen(T)
+    base = torch.randn(T, W, generator=g, device="cuda")
+    big = torch.randn(2048, 2048, generator=g, device="cuda")
+    up, us = rtn.rtn_pack_weights(codes(g, E * W, W))
+    us = us[0].contiguous()
+    one, zero, t = (torch.tensor([v], device="cuda") for v in (1.0, 0.0, 0.4))
+    side = torch.cuda.Stream()
+    x, r, logits = torch.empty_like(base), torch.empty_like(base), torch.empty(T, E, device="cuda")
+    scale = torch.ones((), device="cuda")
+
+    def slow(v, out):
+        y = big
+        for _ in range(6):
+            y = (y @ big) * 1e-2
+        torch.mul(v, scale + 0 * y[0, 0], out=out)
+
+    def run():
+        main = torch.cuda.current_stream()
+        for t_ in (x, r, logits):
+            t_.fill_(float("nan"))
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            slow(base.flip(0), r)
+        slow(base, x)
+        torch.mul(x[:, :E], 2.0, out=logits)
+        main.wait_stream(side)
+        n = rtn.rtn_block_norm(x, r, norm_weight=torch.ones(W, device="cuda"), t_lo=-t, t_hi=t)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            slow(base[:, :E], logits)
+        main.wait_stream(side)
+        route = rtn.rtn_route_experts(logits, 2)
+        main.wait_stream(side)
+        y = rtn.rtn_ternary_experts(n.codes, n.sums, route.tokens, route.start, up, us, W, W, one, zero, one, zero, t_lo=-t, t_hi=t)
+        return [n.stream, n.codes, n.sums, *route, *y]
+    return scale, run
+
+
+@pytest.mark.parametrize("T", [3, 1500])
+def test_inputs_of_two_streams_eager_and_captured(T):
+    scale, run = joined(T, 256, 16)
+    want = [t.clone() for t in run()]
+    torch.cuda.synchronize()
+    assert not bool(torch.isnan(want[0]).any())
+    for _ in range(5):
+        got = run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for factor in (1.0, -0.5, 1.0):
+        scale.fill_(factor)
+        want = [t.clone() for t in run()]
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for t in out:
+                t.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+    assert rtn.rtn_last_device_status() == 0
