@@ -10,7 +10,7 @@
 // the token's codes out again in double; of tokens of 2048 normal values about one in a hundred.  That pass takes 10 us, which is what the last of a
 // launch's rows that needs it adds (with thresholds that nothing is near, the 123 us below are 112).
 // Measured (one B200): 8192 tokens of 2048, bf16, 8 experts' rows each, both norms, codes 123 us (407 MB: 62 at the copy rate; the rest is issue slots, some
-// 1200 instructions per 256 values); one token of 2048, 4 rows, codes 6.7 us; 48 of 4096, gated 5.8 us; 1111 of 5003, fp32, one value to an access 32.7 us.
+// 1200 instructions per 256 values); one token of 2048, 4 rows, codes 3.5 us in a graph; 48 of 4096, gated 3.3 us; 1111 of 5003, fp32, one value to an access 30.5 us.
 #include "rtn_internal.cuh"
 #include "rtn_epilogue.cuh"
 #include "rtn_tcgen05.cuh"

@@ -11,8 +11,8 @@
 // Codes are those of the exact output: a value nearer to a threshold than its error bound is worked out again in double, of 16 tokens at a time.
 // Bound: for long prompts the instructions of the epilogue (50 to 65 per output) and of the expansion (some 200 per 32 rows x 256 codes), the tensor
 // pipe idles three quarters of the time; for few rows of an expert its start (2.6 us) and the first planes' way (2.6 us).
-// Measured (one B200): 65536 rows, 64 experts of 2048 x 2048, gated, codes 269 us (2.0 PFLOP/s; the matrix instructions alone 63); of 2048 x 1024, bf16
-// values 156 us (268 MB written); 384 rows, 64 experts of 2048 x 2048, gated, codes 29.5 us (67 MB of planes at 2.3 TB/s).
+// Measured (one B200, in a graph): 65536 rows, 64 experts of 2048 x 2048, gated, codes 243 us (2.3 PFLOP/s; the matrix instructions alone 63); of 2048 x 1024,
+// bf16 values 133 us (268 MB written); 384 rows, 64 experts of 2048 x 2048, gated, codes 22.2 us (67 MB of planes at 3.0 TB/s).
 #include "rtn_experts.cuh"
 #include "rtn_tcgen05.cuh"
 #include "rtn_tensormap.cuh"
@@ -714,8 +714,8 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
 
 // Rows of a tile at most, from the rows that an expert has on average: what makes rounds of tiles times a tile's time least.  A tile's time in clocks is the
 // longer of its expansion and products (350 for 256 codes, from 135 rows on 2.6 a row) and its outputs (500 and 20 a row; fitted to
-// measured times), and the shorter once more at the end.  65536 rows of 64 experts, 2048 x 2048 gated with codes, and 2048 x 1024 to bf16: 160 rows 271 and
-// 153 us, 144 280 and 162, 128 279 and 164, 112 304 and 179; more than 160 do not leave enough tensor memory for three slots of weights.
+// measured times), and the shorter once more at the end.  65536 rows of 64 experts, 2048 x 2048 gated with codes, and 2048 x 1024 to bf16 (before later
+// steps took 26 and 20 us off): 160 rows 271 and 153 us, 144 280 and 162, 128 279 and 164, 112 304 and 179; more than 160 do not leave enough tensor memory for three slots of weights.
 TilesPlan make_plan(const ExpertsArgs& g)
 {
     TilesPlan p{};

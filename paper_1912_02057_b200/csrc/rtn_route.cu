@@ -11,8 +11,8 @@
 // route_plan_kernel adds what lies before: the rows of lower experts, and of the expert's earlier blocks.  One block does both.
 // route_list_kernel does the first kernel's work for many tokens.
 // Bound: latency (two launches, a chain of about 40 clocks per pick) for few tokens, issue slots for many.
-// Measured (one B200): one token, 4 of 64 experts 8.5 us; 96 tokens, 8 of 256 in 4 of 8 groups, with a bias 14.3 us (most of it the chain of picks: 8
-// experts, 4 groups and the sums of 2 in each); 16384 tokens, 8 of 128 13.2 us (4.2 MB of logits: 0.6 us at the copy rate).
+// Measured (one B200): one token, 4 of 64 experts 3.5 us in a graph; 96 tokens, 8 of 256 in 4 of 8 groups, with a bias 11.0 us (most of it the chain of picks: 8
+// experts, 4 groups and the sums of 2 in each); 16384 tokens, 8 of 128 12.6 us (4.2 MB of logits: 0.6 us at the copy rate).
 #include "rtn_internal.cuh"
 #include "rtn_types.cuh"
 #include "rtn_tcgen05.cuh"
