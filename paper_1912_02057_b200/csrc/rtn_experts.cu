@@ -160,18 +160,19 @@ cudaError_t launch_rows(const ExpertsArgs& g, cudaStream_t s)
 
 }  // namespace
 
-// Which form: rows cost 7 us per million rows x columns x blocks of K (two rows to a tile: the POPC rate) on top of 5, tiles 10.5 us and 0.2 us per MB of the
-// planes of the experts that have rows (of R rows dealt at random).  In a graph on one B200 (us, rows of an expert on average in brackets):
+// Which form: rows cost 6.2 us per million rows x columns x blocks of K (two rows to a tile: the POPC rate) on top of 4; tiles 8 us and, a round of one to every SM,
+// 0.45 us per 512 codes of K or 1.4, whichever is more (of R rows dealt at random).  In a graph on one B200 (us, rows of an expert on average in brackets):
 //                                                    rows  tiles                                             rows  tiles
-//   4 rows (0.1), 64 x 2048 x 2048, gated, codes      8.4   13.0     320 (5.3), 60 x 1006 x 429              14.0   12.8
-//   32 (0.5), 64 x 2048 x 2048, gated, codes         14.4   18.5     80 (1.3), 60 x 4096 x 300               12.5   20.7
-//   64 (1), 64 x 2048 x 2048, gated, codes           20.0   20.7     512 (32), 16 x 512 x 512                10.3   10.3
-//   128 (2), 64 x 2048 x 2048, gated, codes          29.1   24.8     1554 (194), 8 x 1000 x 520              57.4   14.4
-// One row to a tile where an expert has hardly more (16 rows (0.25): 8.5 us, two to a tile 10.3); four or eight were nowhere ahead.
+//   4 rows (0.1), 64 x 2048 x 2048, gated, codes      5.8    9.7     320 (5.3), 60 x 1006 x 429              11.1   13.1
+//   32 (0.5), 64 x 2048 x 2048, gated, codes         11.3   14.0     80 (1.3), 60 x 4096 x 300               12.0   23.1
+//   64 (1), 64 x 2048 x 2048, gated, codes           17.3   16.1     512 (32), 16 x 512 x 512                 9.5    9.4
+//   128 (2), 64 x 2048 x 2048, gated, codes          27.5   19.8     1554 (194), 8 x 1000 x 520              57.4   13.7
+// One row to a tile where an expert has hardly more (16 rows (0.25): 6.7 us, two to a tile 7.2; 32: 11.3 and 12.5); four or eight were nowhere ahead.
 cudaError_t launch_ternary_experts(const ExpertsArgs& g, cudaStream_t s)
 {
-    const double nblk = (double)((g.K + kBlockCodes - 1) / kBlockCodes), used = g.E * (1.0 - exp(-(double)g.R / g.E));
-    const double rows_us = 5.0 + 7e-6 * (double)g.R * (double)g.N * nblk, tiles_us = 10.5 + 0.2e-6 * used * (double)g.N * nblk * kBlockBytes;
+    const double nblk = (double)((g.K + kBlockCodes - 1) / kBlockCodes), used = g.E * (1.0 - exp(-(double)g.R / g.E)), sms = device_sm_count();
+    const double high = (double)g.R / used / 160.0, rounds = used * (high > 1.0 ? high : 1.0) * (double)((g.N + 127) / 128) / sms, each = 0.1125 * nblk;
+    const double rows_us = 4.0 + 6.2e-6 * (double)g.R * (double)g.N * nblk, tiles_us = 8.0 + (rounds > 1.0 ? rounds : 1.0) * (each > 1.4 ? each : 1.4);
     if (rows_us > tiles_us && experts_tiles_supported(g)) return launch_experts_tiles(g, s);
     return 2 * g.R <= g.E ? launch_rows<1>(g, s) : launch_rows<2>(g, s);
 }
