@@ -68,7 +68,7 @@ struct TileParams {
     float4 col[128];
     uint4 most_asx, most_ao;                                    // the largest |a_s S_x| and |a_o|, in four parts, as bit patterns (a NaN is the largest)
     uint4 votes[4][kMaxRows / 4][2];
-    Tile tile;
+    Tile tile[kEdgeWarps];                                      // the same place four times: each edge warp writes and reads its own
 };
 
 // 32 codes (a word of each plane) as four words of 4-bit values; nibble i of word r is code 4 i + r.  The magnitude of a nonzero weight is
@@ -452,7 +452,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             }
             here.col[part * 32 + lane] = make_float4(ws, wo, (float)((double)ws * (double)sw + (double)g.K * (double)wo), bias);
             most_asx = __reduce_max_sync(0xffffffffu, most_asx); most_ao = __reduce_max_sync(0xffffffffu, most_ao);
-            if (lane == 0) { (&here.most_asx.x)[part] = most_asx; (&here.most_ao.x)[part] = most_ao; if (part == 0) here.tile = tile; }
+            if (lane == 0) { (&here.most_asx.x)[part] = most_asx; (&here.most_ao.x)[part] = most_ao; here.tile[part] = tile; }
             if (bad && t % cols == 0) atomicOr(g.status, kStatusBadIndex);
             __threadfence_block();
             __syncwarp();
@@ -471,7 +471,9 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
             if (!(alive = warp_wait(&bar.votes_full[ti & 1], ti >> 1))) break;
             if constexpr (kCodes) {
                 const TileParams& here = params[ti & 1];
-                const Tile tile = here.tile;
+                // (A place of this warp's own: nothing orders the edge warps among each other, so the first of them may be a tile ahead and have put the
+                // place of the one two rounds on where the others are still to read.)
+                const Tile tile = here.tile[part];
                 const int64_t f0 = (int64_t)(t % cols) * kTileOuts, width = (g.F + kBlockCodes - 1) / kBlockCodes * kBlockCodes;
                 #pragma unroll 1
                 for (int r = lane + 32 * part; r < tile.rows; r += 32 * kEdgeWarps) {
@@ -530,7 +532,7 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
         for (uint32_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
             TileParams& here = params[ti & 1];
             if (!(alive = warp_wait(&bar.params_full[ti & 1], ti >> 1))) break;
-            const Tile tile = here.tile;
+            const Tile tile = here.tile[0];
             // this thread's weight rows: kOwn outputs, or kOwn and the kOwn that they are multiplied with
             pair_t ws[4], wo[4], p3[4], bias[4];
             float off = 0.f, lo = 0.f, hi = 0.f, most_asx = 0.f, most_ao = 0.f;
