@@ -81,8 +81,10 @@ __device__ __forceinline__ void block_sums(F& a, F& b, F* red)
     for (int d = 16; d > 0; d >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, d); b += __shfl_xor_sync(0xffffffffu, b, d); }
 }
 
-// By the approximate exponential and reciprocal: the logistic function within (2 |z| + 4) (1 - s) + 4 <= 9 units of 2^-24, relative where it counts
-// (for z below 0 the exponent's 2 |z| units are the function's own; |z| >= 40 gives less than 2^-57).
+// By the approximate exponential (4 units of 2^-24) and reciprocal (2).  Rounded, the exponent is off by |z| units, its constant by another 0.22 |z|, so the
+// logistic function is within (1.25 |z| + 4) (1 - s) + 3 units, relative: below 8 for z >= 0, but growing with how far a gate is closed.  Below -87
+// it leaves fp32's normal range and is 0.
+constexpr float kShut = -746.f;             // the logistic function is 0 in double, too
 __device__ __forceinline__ float gate_of(float z, int kind)
 {
     if (kind == RTN_GATE_LINEAR) return z;
@@ -110,7 +112,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
 {
     const int W = g.W, step = blockDim.x * EV, first = threadIdx.x * EV;
     const float mean = 1.f / (float)W;
-    float zero = 0.f, ss = 0.f, sm = 0.f;
+    float zero = 0.f, ss = 0.f, sm = 0.f, closed = 0.f;
     int at[NV];                                                 // a value's column, or 0 behind the row's end
     bool in[NV];
     #pragma unroll
@@ -186,10 +188,17 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
         #pragma unroll
         for (int v = 0; v < NV; ++v) {
             take<TB, EV>(z[v], true, f[v]);
+            if constexpr (kTrack) {
+                if (g.gate_kind != RTN_GATE_LINEAR) {
+                    #pragma unroll
+                    for (int i = 0; i < EV; ++i) closed = fmaxf(closed, f[v][i] > kShut ? -f[v][i] : 0.f);
+                }
+            }
             #pragma unroll
             for (int i = 0; i < EV; ++i) f[v][i] = gate_of(f[v][i], g.gate_kind);
         }
-        units += 12.f;
+        // (one bound for all of a thread's values, by its most closed gate; none where that is 0 in fp32 only)
+        units += closed < 87.f ? fmaf(1.25f, closed, 12.f) : INFINITY;
     }
     if (g.scale != nullptr) {
         units += 1.f;
@@ -379,7 +388,10 @@ static __device__ __noinline__ int exact_codes(const NormArgs& g, int64_t t, dou
             double f = scale * (double)q[u] * (post * (double)p[u]);
             if (g.gate != nullptr) {
                 if (g.gate_kind != RTN_GATE_SIGMOID) f *= (double)z[u];
-                if (g.gate_kind != RTN_GATE_LINEAR) f *= 1.0 / (1.0 + exp(-(double)z[u]));
+                if (g.gate_kind != RTN_GATE_LINEAR) {
+                    const double e = exp(-fabs((double)z[u]));                     // (of -z it would leave the range at 710)
+                    f *= (z[u] < 0.f ? e : 1.0) / (1.0 + e);
+                }
             }
             const double y = branch != nullptr ? fma(f, h[i0 + u], (double)r[u]) : (double)r[u];
             h[i0 + u] = y;

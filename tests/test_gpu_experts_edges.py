@@ -40,3 +40,42 @@ def test_experts_of_few_and_of_many_rows_in_turn(E, N, K, gated):
         wrong += (places[0] != want[0]).sum() + (places[1] != want[1]).sum()
     assert int(wrong) == 0
     assert rtn.rtn_last_device_status() == 0
+
+
+# ---------------------------------------------------------------------------------------------- closed gates
+
+@pytest.mark.parametrize("kind", [rtn.GATE_SIGMOID, rtn.GATE_SILU])
+@pytest.mark.parametrize("low,high,hi", [(-2.0, 2.0, 1.0), (-12.0, -4.0, 0.01), (-40.0, -20.0, 1e-9), (-80.0, -40.0, 1e-20), (-87.2, -80.0, 1e-25), (-100.0, -86.0, 1e-12),
+                                         (-110.0, -104.0, 1e-8)], ids=ids)
+def test_block_norm_codes_of_closed_gates(low, high, hi, kind):
+    """Tokens of one value each (one that is too near for fp32 sends a whole token to the exact form), within a hundred steps of a threshold: the
+    code is that of the exact value however far the gate is closed."""
+    T = 20000
+    r = np.random.default_rng(int(-10 * low) + kind)
+    hi = float(np.float32(hi))
+    z = r.uniform(low, high, T).astype(np.float32)
+    z64 = z.astype(np.float64)
+    f = np.exp(z64) / (1.0 + np.exp(z64)) * (z64 if kind == rtn.GATE_SILU else 1.0)
+    y = (hi / f * (1.0 + r.integers(-100, 101, T) * 2.0 ** -24)).astype(np.float32)
+    y = np.where(np.isfinite(y), y, np.float32(1.0))                        # (SiLU: about z = 0)
+    n = y.astype(np.float64) * f                                           # off by some 2^-51
+    sure = np.abs(n / hi - 1.0) > 1e-14
+    assert sure.mean() > 0.99 and 0.2 < (n > hi).mean() < 0.8
+    dev = lambda a: torch.from_numpy(a).cuda()[:, None]  # noqa: E731
+    for sign in (1.0, -1.0):
+        t = torch.tensor([hi], device="cuda")
+        lo, up = (-torch.full_like(t, np.inf), t) if sign > 0 else (-t, torch.full_like(t, np.inf))
+        got = rtn.rtn_block_norm(sign * dev(y), gate=dev(z), gate_kind=kind, t_lo=lo, t_hi=up)
+        assert np.array_equal(got.sums.cpu().numpy()[sure], (sign * (n > hi)).astype(np.int32)[sure])
+    assert rtn.rtn_last_device_status() == 0
+
+
+def test_block_norm_gates_that_are_shut():
+    """Gates whose logistic function is 0 in double too: what is left is the residual, and no token is NaN."""
+    for z in (-746.0, -1e4, -3e38):
+        y, r = torch.randn(3, 500, device="cuda"), torch.randn(3, 500, device="cuda")
+        t = torch.tensor([0.25], device="cuda")
+        for kind in (rtn.GATE_SIGMOID, rtn.GATE_SILU):
+            got = rtn.rtn_block_norm(y, r, gate=torch.full_like(y, z), gate_kind=kind, t_lo=-t, t_hi=t)
+            want = rtn.rtn_ternarize_pack_act(r, -t, t)
+            assert torch.equal(got.stream, r) and torch.equal(got.codes, want[0]) and torch.equal(got.sums, want[1])
