@@ -385,7 +385,7 @@ rtn_status rtn_ternary_experts(const void* a_packed, const int32_t* a_sum, int64
  *   out_packed, out_sum   NULL (both), or n's codes, T packed rows of W codes and their sums (t_lo, t_hi: n_thr 1 or W); they are the codes of
  *               the exact n
  * Rows of every tensor are `*_stride` elements apart (0 repeats a row of an input).  W <= 16384.  A place >= R makes the token's row NaN
- * (codes 0), and rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once. */
+ * (codes 0), and rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once.  With places, R may be 0 (branch is not read, and may be NULL). */
 rtn_status rtn_block_norm(const void* branch, int64_t branch_stride, int64_t R, const int32_t* place, const float* weights, int64_t k,
                           const float* post_weight, const void* gate, int64_t gate_stride, rtn_gate gate_kind,
                           const float* scale, int64_t n_scale, const void* residual, int64_t residual_stride,

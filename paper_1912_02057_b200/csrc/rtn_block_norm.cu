@@ -127,7 +127,14 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
     for (int v = 0; v < NV; ++v)
         #pragma unroll
         for (int i = 0; i < EV; ++i) h[v][i] = slack[v][i] = 0.f;
-    if (g.place != nullptr) {
+    if (g.place != nullptr && g.R == 0) {                       // no rows to read, not even for a place that is out of range
+        bool bad = false;
+        for (int j = 0; j < g.k; ++j) bad = bad || g.place[t * g.k + j] >= 0;
+        #pragma unroll
+        for (int v = 0; v < NV; ++v)
+            #pragma unroll
+            for (int i = 0; i < EV; ++i) h[v][i] = bad ? __int_as_float(0x7fffffff) : 0.f;
+    } else if (g.place != nullptr) {
         constexpr int kAhead = NV * EV <= 8 ? 4 : 1;            // rows on their way
         #pragma unroll 1
         for (int j0 = 0; j0 < g.k; j0 += kAhead) {
@@ -327,7 +334,12 @@ static __device__ __noinline__ int exact_codes(const NormArgs& g, int64_t t, dou
         double y[kTogether];
         #pragma unroll
         for (int u = 0; u < kTogether; ++u) y[u] = 0.0;
-        if (g.place != nullptr) {
+        if (g.place != nullptr && g.R == 0) {
+            bool bad = false;
+            for (int j = 0; j < g.k; ++j) bad = bad || g.place[t * g.k + j] >= 0;
+            #pragma unroll
+            for (int u = 0; u < kTogether; ++u) y[u] = bad ? __longlong_as_double(0x7fffffffffffffffll) : 0.0;
+        } else if (g.place != nullptr) {
             #pragma unroll 1
             for (int j0 = 0; j0 < g.k; j0 += 4) {
                 TB x[4][kTogether];
@@ -393,7 +405,7 @@ static __device__ __noinline__ int exact_codes(const NormArgs& g, int64_t t, dou
                     f *= (z[u] < 0.f ? e : 1.0) / (1.0 + e);
                 }
             }
-            const double y = branch != nullptr ? fma(f, h[i0 + u], (double)r[u]) : (double)r[u];
+            const double y = branch != nullptr || g.place != nullptr ? fma(f, h[i0 + u], (double)r[u]) : (double)r[u];
             h[i0 + u] = y;
             ss = fma(y, y, ss);
         }

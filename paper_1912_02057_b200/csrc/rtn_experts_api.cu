@@ -93,8 +93,9 @@ rtn_status rtn_block_norm(const void* branch, int64_t branch_stride, int64_t R, 
     if (T < 0 || T >= kMaxDim || W <= 0 || W > rtn::kNormMaxWidth || R < 0 || R >= kMaxDim || k < 0 || k > rtn::kMaxChoices) return RTN_ERR_SHAPE;
     if ((place != nullptr) != (k > 0) && T > 0) return RTN_ERR_SHAPE;
     if (branch != nullptr && place == nullptr && R < T) return RTN_ERR_SHAPE;
-    if (T > 0 && branch == nullptr && residual == nullptr) return RTN_ERR_NULL;
-    if (T > 0 && branch == nullptr && (place != nullptr || post_weight != nullptr || gate != nullptr || scale != nullptr)) return RTN_ERR_NULL;
+    const bool none = branch == nullptr && !(place != nullptr && R == 0);           // (no rows: nothing to point at)
+    if (T > 0 && none && residual == nullptr) return RTN_ERR_NULL;
+    if (T > 0 && none && (place != nullptr || post_weight != nullptr || gate != nullptr || scale != nullptr)) return RTN_ERR_NULL;
     if (weights != nullptr && place == nullptr && T > 0) return RTN_ERR_NULL;
     const bool coded = out_packed != nullptr;
     if (coded ? out_sum == nullptr || t_lo == nullptr || t_hi == nullptr : out_sum != nullptr) return RTN_ERR_NULL;

@@ -79,3 +79,31 @@ def test_block_norm_gates_that_are_shut():
             got = rtn.rtn_block_norm(y, r, gate=torch.full_like(y, z), gate_kind=kind, t_lo=-t, t_hi=t)
             want = rtn.rtn_ternarize_pack_act(r, -t, t)
             assert torch.equal(got.stream, r) and torch.equal(got.codes, want[0]) and torch.equal(got.sums, want[1])
+
+
+# ---------------------------------------------------------------------------------------------- rows of nobody
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids)
+@pytest.mark.parametrize("W", [256, 130, 1003])
+def test_block_norm_without_any_rows(W, dtype):
+    """No expert has a row: the sum is 0, whatever stands (or does not) where rows would begin; a place that is not negative is out of range."""
+    x = torch.randn(5, W, device="cuda")
+    weight = 1 + 0.2 * torch.randn(W, device="cuda")
+    t = torch.tensor([0.25], device="cuda")
+    kw = dict(place=torch.full((5, 3), -1, dtype=torch.int32, device="cuda"), weights=torch.full((5, 3), float("nan"), device="cuda"), post_weight=weight,
+              gate=torch.randn(5, W, device="cuda").to(dtype), gate_kind=rtn.GATE_SILU, norm_weight=weight, t_lo=-t, t_hi=t, normed=True)
+    want = rtn.rtn_block_norm(None, x, norm_weight=weight, t_lo=-t, t_hi=t, normed=True)
+    # an empty tensor of its own, and what is behind the last row of one
+    for rows in (torch.empty(0, W, dtype=dtype, device="cuda"), torch.full((1, W), float("nan"), dtype=dtype, device="cuda")[1:]):
+        got = rtn.rtn_block_norm(rows, x, **kw)
+        assert torch.equal(got.stream, want.stream) and torch.equal(got.normed, want.normed.to(dtype))
+        assert torch.equal(got.codes, want.codes) and torch.equal(got.sums, want.sums)
+    alone = rtn.rtn_block_norm(torch.empty(0, W, dtype=dtype, device="cuda"), None, place=kw["place"])
+    assert alone.stream.dtype == dtype and alone.stream.shape == (5, W) and not bool(alone.stream.any())
+    assert rtn.rtn_last_device_status() == 0
+    kw["place"][2, 1] = 0
+    got = rtn.rtn_block_norm(torch.empty(0, W, dtype=dtype, device="cuda"), x, **kw)
+    assert rtn.rtn_last_device_status() == 8 and rtn.rtn_last_device_status() == 0
+    keep = [0, 1, 3, 4]
+    assert bool(got.stream[2].isnan().all()) and not bool(got.codes[2].any()) and torch.equal(got.stream[keep], want.stream[keep])
+    assert torch.equal(got.codes[keep], want.codes[keep])
