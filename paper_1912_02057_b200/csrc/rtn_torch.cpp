@@ -444,7 +444,8 @@ PyObject* block_norm(PyObject* const* a)
     const Call call(first, a[17]);
     if (first.dim() != 2) refuse("expected [rows, width], got " + text(first));
     const int64_t W = first.size(1), R = branch != nullptr ? branch->size(0) : 0;
-    if (place != nullptr && place->dim() != 2) refuse("place: expected [tokens, choices], got " + text(*place));
+    // (no choices: without this an empty place, which has no address, would be none, and row t what token t has)
+    if (place != nullptr && (place->dim() != 2 || place->size(1) < 1)) refuse("place: expected [tokens, choices], got " + text(*place));
     const int64_t T = place != nullptr ? place->size(0) : first.size(0), k = place != nullptr ? place->size(1) : 0;
     const at::ScalarType stream_type = residual != nullptr ? residual->scalar_type() : given != nullptr ? given->scalar_type() : dtype_of(a[16], first.scalar_type());
     const at::ScalarType type = branch != nullptr ? branch->scalar_type() : given_n != nullptr ? given_n->scalar_type() : dtype_of(a[16], stream_type);

@@ -107,3 +107,11 @@ def test_block_norm_without_any_rows(W, dtype):
     keep = [0, 1, 3, 4]
     assert bool(got.stream[2].isnan().all()) and not bool(got.codes[2].any()) and torch.equal(got.stream[keep], want.stream[keep])
     assert torch.equal(got.codes[keep], want.codes[keep])
+
+
+def test_block_norm_refuses_places_without_choices():
+    rows = torch.randn(5, 64, device="cuda")
+    for k in (dict(place=torch.empty(5, 0, dtype=torch.int32, device="cuda")), dict(place=torch.empty(5, 0, dtype=torch.int32, device="cuda"),
+                                                                                    weights=torch.empty(5, 0, device="cuda"))):
+        with pytest.raises(ValueError):
+            rtn.rtn_block_norm(rows, rows, **k)
