@@ -94,15 +94,21 @@ __device__ __forceinline__ float gate_of(float z, int kind)
     return kind == RTN_GATE_SIGMOID ? s : z * s;
 }
 
-// Roundings of a sum of squares, per thread and over two trees, of the mean and of the root (approximate: two units in the last place of 2^-23).
-template <int NV, int EV> constexpr float kRootUnits = 0.5f * (NV * EV + 10) + 6.f;
-
 // Square root of a quotient, for bounds only.
 __device__ __forceinline__ float root_of_ratio(float a, float b)
 {
     float r;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(__fdividef(a, b)));
     return r;
+}
+// Units of a root's error: roundings of the sum of squares `ss`, per thread and over two trees, of the mean and of the root (approximate: two units in the last
+// place of 2^-23), and the values' own errors, whose squares add up to `sm`.  No bound where squares leave fp32: what
+// falls below its normal range is less than 2^-149 each, nothing beside a mean (with eps: `square`) of 1e-30; above 2^126 the quotient is 0.
+template <int NV, int EV>
+__device__ __forceinline__ float root_units(float square, float ss, float sm)
+{
+    const float units = 0.5f * (NV * EV + 10) + 6.f + (ss > 0.f ? root_of_ratio(sm, ss) : 0.f);
+    return square > 1e-30f && ss < 8e37f ? units : INFINITY;
 }
 
 // h and n of token t.  slack receives the bound on n's error, where kTrack asks for it.  Loads are not in branches (a value behind the row's end is
@@ -238,8 +244,8 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
             }
         }
         block_sums(ss, kTrack ? sm : zero, red);
-        const float post = rsqrtf(fmaf(ss, mean, g.eps));
-        if constexpr (kTrack) post_units = kRootUnits<NV, EV> + 2.f + (ss > 0.f ? root_of_ratio(sm, ss) : 0.f);
+        const float square = fmaf(ss, mean, g.eps), post = rsqrtf(square);
+        if constexpr (kTrack) post_units = root_units<NV, EV>(square, ss, sm) + 2.f;
         #pragma unroll
         for (int v = 0; v < NV; ++v)
             #pragma unroll
@@ -270,8 +276,8 @@ __device__ __forceinline__ void norm_row(const NormArgs& g, int64_t t, float* re
         #pragma unroll
         for (int v = 0; v < NV; ++v) load_params<EV>(g.norm_weight, at[v], p[v]);
         block_sums(ss, kTrack ? sm : zero, red);
-        const float pre = rsqrtf(fmaf(ss, mean, g.eps));
-        if constexpr (kTrack) pre_units = kRootUnits<NV, EV> + 4.f + (ss > 0.f ? root_of_ratio(sm, ss) : 0.f);
+        const float square = fmaf(ss, mean, g.eps), pre = rsqrtf(square);
+        if constexpr (kTrack) pre_units = root_units<NV, EV>(square, ss, sm) + 4.f;
         #pragma unroll
         for (int v = 0; v < NV; ++v)
             #pragma unroll

@@ -115,3 +115,32 @@ def test_block_norm_refuses_places_without_choices():
                                                                                     weights=torch.empty(5, 0, device="cuda"))):
         with pytest.raises(ValueError):
             rtn.rtn_block_norm(rows, rows, **k)
+
+
+# ---------------------------------------------------------------------------------------------- squares at the ends of fp32
+
+def as_codes(n, lo, hi):
+    return np.where(n > hi, 1, np.where(n < lo, -1, 0))
+
+
+@pytest.mark.parametrize("size", [1e-22, 1e-20, 1e-18, 1e-15, 1e17, 3e17, 1e19])
+@pytest.mark.parametrize("W", [256, 131])
+def test_block_norm_codes_where_squares_leave_fp32(W, size):
+    """Without an epsilon a row's size does not count: the codes are those of the same row at any size, for both norms."""
+    T = 3000
+    r = np.random.default_rng(W)
+    x = (r.standard_normal((T, W)) * size).astype(np.float32)
+    x64, weight = x.astype(np.float64), r.uniform(0.8, 1.2, W).astype(np.float32)
+    n = x64 / np.sqrt((x64 * x64).mean(1, keepdims=True)) * weight
+    dev = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    for hi in (0.5, 1.0):
+        t = torch.tensor([hi], device="cuda")
+        want = as_codes(n, -hi, hi)
+        assert np.abs(np.abs(n) - hi).min() > 1e-10              # (no value is nearer than double tells)
+        for kw in (dict(branch=None, residual=dev(x), norm_weight=dev(weight)), dict(branch=dev(x), post_weight=dev(weight))):
+            got = rtn.rtn_block_norm(**kw, eps=0.0, t_lo=-t, t_hi=t)
+            assert np.array_equal(got.sums.cpu().numpy(), want.sum(1))
+            p = got.codes.cpu().numpy().reshape(T, -1, 2, 16)
+            bits = np.unpackbits(p, axis=3, bitorder="little").transpose(2, 0, 1, 3).reshape(2, T, -1)[:, :, :W]
+            assert np.array_equal(bits[0], want != 0) and np.array_equal(bits[1], want > 0)
+    assert rtn.rtn_last_device_status() == 0
