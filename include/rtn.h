@@ -338,8 +338,9 @@ typedef enum { RTN_GATE_LINEAR = 0, RTN_GATE_SIGMOID = 1, RTN_GATE_SILU = 2 } rt
  *   start, tokens, place   NULL (all three), or the plan: the T*top_k (token, choice) pairs as rows sorted by expert, within an expert by
  *               token.  Expert e has rows start[e] .. start[e+1]-1 (int32 [E+1]); row r is of token tokens[r] (int32 [T*top_k]); choice j of
  *               token t is row place[t][j] (int32 [T][top_k])
- * Choices are those of exact arithmetic (a c that fp32 cannot tell from another is computed in double); of equal ones the lowest index
- * comes first, for groups too.  A logit of -inf or NaN (or a bias of it) is never chosen, and +inf counts as the largest finite
+ * Choices are those of exact arithmetic (a c that fp32 cannot tell from another is computed in double, and what that leaves open in pairs of
+ * doubles, where a score keeps 47 bits of its distance to 0 and to 1; what is equal there goes by the logit); of equal ones the lowest
+ * index comes first, for groups too.  A logit of -inf or NaN (or a bias of it) is never chosen, and +inf counts as the largest finite
  * value; a token with fewer experts to choose has -1, weight 0 and place -1 in the rest, and the rows from start[E] on are not written.
  * E <= 1024, groups <= 32 and a divisor of E, top_k <= 32 and <= the experts in the kept groups. */
 rtn_status rtn_route_experts(const void* logits, int64_t logits_stride, int64_t T, int64_t E, rtn_dtype dtype, rtn_score score,

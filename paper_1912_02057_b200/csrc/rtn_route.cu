@@ -3,7 +3,9 @@
 // route_choose_kernel: a warp takes one token at a time, a lane VPL experts side by side.  A choice is compared by a key, an unsigned number
 //   of the same order (0: not to be chosen): of the logit itself where no bias and no sum of scores is involved (softmax and sigmoid keep the
 //   order, so nothing is rounded), else of score + bias in fp32.  There two neighbours in the order that are nearer to each other than their
-//   rounding errors make the warp choose this token's experts again in double (of ordinary tokens a few in a thousand).
+//   rounding errors make the warp choose this token's experts again in double (of ordinary tokens a few in a thousand), and what double leaves
+//   open, scores next to 1 or under large biases, in pairs of doubles when the block's other tokens are done (16384 tokens, 8 of 128, bias: 30.7
+//   us without that, 32.7 with it).
 //   A pick is one warp reduction and one vote: the largest key, and the first lane that has it.  Groups are looked at all at once, a group's
 //   lanes side by side, where their sizes let them be, else one after the other.
 //   A block notes who chose what in a bit per (expert, token), so that a pair's place among its expert's rows is a count of bits
@@ -96,6 +98,7 @@ __device__ __forceinline__ void take_logits(const RouteArgs& g, int lane, const 
 
 // Lane j: choice j and its logit.
 struct Choice { int pick; float logit; };
+constexpr int kOpen = -2;                   // (of all lanes) not decided
 
 // The largest of the warp's keys that `mine` lets take part, and the lowest index that has it.
 template <int VPL, typename Mine>
@@ -112,11 +115,153 @@ __device__ __forceinline__ uint64_t best_of(const uint64_t (&key)[VPL], int lane
     return top;
 }
 
-// One token's choices in double, for any groups.
+// Weights of a token's choices (top and sum: of a softmax over all experts, where it is not renormalised), and the note of who chose what.
+__device__ __forceinline__ void finish_token(const RouteArgs& g, int64_t t, const Choice& c, float top, float sum, uint32_t* chosen, int words, int bit)
+{
+    const int lane = threadIdx.x & 31;
+    float w = 0.f;
+    if (g.renormalise) {
+        // s up to a factor that all choices share, so that scores too small for fp32 still have their ratios
+        const float best = warp_max(c.logit);
+        if (c.pick >= 0)
+            w = g.score == RTN_SCORE_SOFTMAX ? expf(c.logit - best) : expf(fminf(c.logit, 0.f) - fminf(best, 0.f)) / (1.f + expf(-fabsf(c.logit)));
+        const float all = warp_sum(w);
+        if (c.pick >= 0) w /= all;
+    } else if (c.pick >= 0) {
+        w = g.score == RTN_SCORE_SOFTMAX ? expf(c.logit - top) / sum : 1.f / (1.f + expf(-c.logit));
+    }
+    if (lane < g.top_k) {
+        g.experts[t * g.top_k + lane] = c.pick;
+        g.weights[t * g.top_k + lane] = w * g.scale;
+        if (chosen != nullptr && c.pick >= 0) atomicOr(&chosen[c.pick * words + (bit >> 5)], 1u << (bit & 31));
+    }
+}
+
+// A sum of two doubles as a pair: the rounded sum, and what it left out (0 beside an infinity).
+struct Pair { double hi, lo; };
+__device__ __forceinline__ Pair pair_sum(double a, double b)
+{
+    const double s = a + b, t = s - a;
+    return Pair{s, isinf(s) ? 0.0 : (a - (s - t)) + (b - t)};
+}
+__device__ __forceinline__ Pair pair_sum(Pair a, Pair b)
+{
+    const Pair s = pair_sum(a.hi, b.hi);
+    return pair_sum(s.hi, s.lo + (a.lo + b.lo));
+}
+// Places in the order of choices: by c, as a pair, by the logit, which a score grows with where c does not tell any more, and by the index, lowest first.  Of
+// infinities nothing but the index counts.
+struct Place { uint64_t hi, lo; uint32_t logit; int at; };
+__device__ __forceinline__ bool ahead(const Place& a, const Place& b)
+{
+    if (a.hi != b.hi) return a.hi > b.hi;
+    if (a.lo != b.lo) return a.lo > b.lo;
+    return a.logit != b.logit ? a.logit > b.logit : a.at < b.at;
+}
+// The first of the lanes' places (at -1: there is none).
+__device__ __forceinline__ Place first_of(Place p)
+{
+    const uint64_t hi = warp_max(p.at >= 0 ? p.hi : 0);
+    bool same = p.at >= 0 && p.hi == hi;
+    const uint64_t lo = warp_max(same ? p.lo : 0);
+    same = same && p.lo == lo;
+    const uint32_t logit = warp_max(same ? p.logit : 0u);
+    same = same && p.logit == logit;
+    return Place{hi, lo, logit, (int)__reduce_min_sync(0xffffffffu, same ? (unsigned)p.at : 0xffffffffu)};
+}
+// Expert e's place (0 for hi: not to be chosen).  top, all: the largest logit and the sum of exponentials of a softmax.  A sigmoid next to 1 is 1 less what it
+// lacks, so that neither end hides a difference.
+template <typename T>
+__device__ __noinline__ Place place_of(const RouteArgs& g, int64_t t, int e, double top, double all)
+{
+    const float v = to_f32(static_cast<const T*>(g.logits)[t * g.stride + e]), x = v > -INFINITY ? fminf(v, FLT_MAX) : -INFINITY;
+    const float b = g.bias != nullptr ? g.bias[e] : 0.f;
+    if (!(x > -INFINITY && b > -INFINITY)) return Place{0, 0, 0, e};
+    Pair c{(double)b, 0.0};
+    if (g.score == RTN_SCORE_SIGMOID) {
+        const double r = exp(-fabs((double)x)), s = r / (1.0 + r);
+        c = x > 0.f ? pair_sum(pair_sum(c.hi, 1.0), Pair{-s, 0.0}) : pair_sum(c.hi, s);
+    } else c = pair_sum(c.hi, exp((double)x - top) / all);
+    return Place{key_of(c.hi), key_of(c.lo), isinf(c.hi) ? 0u : key_of(x), e};
+}
+// The first place behind `last` of experts lo .. hi - 1 (of the groups in `kept`).  Rolled up and worked out again each time: it is to need no more registers than the
+// kernel has, and hardly a token comes here.
+template <typename T>
+__device__ __noinline__ Place next_place(const RouteArgs& g, int64_t t, int lo, int hi, uint32_t kept, const Place& last, double top, double all)
+{
+    Place best{0, 0, 0, -1};
+    #pragma unroll 1
+    for (int e = lo + (threadIdx.x & 31); e < hi; e += 32) {
+        if (!(kept >> (e / (g.E / g.groups)) & 1u)) continue;
+        const Place p = place_of<T>(g, t, e, top, all);
+        if (p.hi != 0 && ahead(last, p) && (best.at < 0 || ahead(p, best))) best = p;
+    }
+    __syncwarp();
+    return first_of(best);
+}
+
+// One token, for any groups, where double does not tell two choices apart.  (A softmax's sum is off by up to 2^-48, for all scores alike.)
+template <typename T>
+__device__ __noinline__ void choose_by_pairs(const RouteArgs& g, int64_t t, uint32_t* chosen, int words, int bit)
+{
+    const int lane = threadIdx.x & 31, per_group = g.E / g.groups;
+    const T* row = static_cast<const T*>(g.logits) + t * g.stride;
+    float most = -INFINITY;
+    #pragma unroll 1
+    for (int e = lane; e < g.E; e += 32) most = fmaxf(most, to_f32(row[e]));       // (a NaN is never the larger)
+    const float top = fminf(warp_max(most), FLT_MAX);
+    double all = 0.0;
+    #pragma unroll 1
+    for (int e = lane; e < g.E; e += 32) {
+        const float x = to_f32(row[e]);
+        if (x > -INFINITY) all += exp((double)fminf(x, FLT_MAX) - (double)top);
+    }
+    all = warp_sum(all);
+    const Place before{~0ull, ~0ull, ~0u, -1};
+    uint32_t kept = 0xffffffffu;
+    if (g.groups > 1) {
+        Place value{0, 0, 0, -1};                               // lane i: of group i
+        #pragma unroll 1
+        for (int gr = 0; gr < g.groups; ++gr) {
+            Place last = before;
+            Pair sum{0.0, 0.0};
+            int n = 0;
+            #pragma unroll 1
+            for (; n < g.group_top; ++n) {
+                last = next_place<T>(g, t, gr * per_group, (gr + 1) * per_group, kept, last, top, all);
+                if (last.at < 0) break;
+                const Pair c{value_of(last.hi), value_of(last.lo)};
+                sum = n == 0 ? c : pair_sum(sum, c);
+            }
+            if (lane == gr && n > 0) value = Place{key_of(sum.hi), key_of(sum.lo), 0u, gr};
+        }
+        kept = 0;
+        #pragma unroll 1
+        for (int n = 0; n < g.kept; ++n) {
+            const Place best = first_of(value);
+            if (best.at < 0) break;
+            kept |= 1u << best.at;
+            if (lane == best.at) value.at = -1;
+        }
+    }
+    Choice c{-1, -INFINITY};
+    Place last = before;
+    #pragma unroll 1
+    for (int j = 0; j < g.top_k; ++j) {
+        last = next_place<T>(g, t, 0, g.E, kept, last, top, all);
+        if (last.at < 0) break;
+        if (lane == j) { c.pick = last.at; c.logit = fminf(to_f32(row[last.at]), FLT_MAX); }
+    }
+    finish_token(g, t, c, top, (float)all, chosen, words, bit);
+}
+
+// One token's choices in double, for any groups.  Its own errors are below 2^-50 of score and c; two neighbours in the order that are nearer than a few of
+// those, and not the same logit and bias, are left to the form above (kOpen): scores next to 1, or under a large bias.
 template <typename T, int VPL>
 __device__ __noinline__ Choice choose_exact(const RouteArgs& g, int64_t t)
 {
     const int lane = threadIdx.x & 31;
+    constexpr double kNear = 0x1p-47;
     float x[VPL];
     alignas(16) T raw[VPL];
     ask_logits<T, VPL>(g, t, lane, raw);
@@ -133,12 +278,15 @@ __device__ __noinline__ Choice choose_exact(const RouteArgs& g, int64_t t)
         all += s[i];
     }
     all = g.score == RTN_SCORE_SIGMOID ? 1.0 : warp_sum(all);
-    const bool by_logit = g.bias == nullptr && (g.groups == 1 || g.group_top == 1);
+    float most_bias = 0.f;
     #pragma unroll
     for (int i = 0; i < VPL; ++i) {
         const float b = g.bias != nullptr && lane * VPL + i < g.E ? g.bias[lane * VPL + i] : 0.f;
-        key[i] = x[i] > -INFINITY && b > -INFINITY ? key_of(by_logit ? (double)x[i] : s[i] / all + (double)b) : 0;
+        key[i] = x[i] > -INFINITY && b > -INFINITY ? key_of(s[i] / all + (double)b) : 0;
+        if (key[i] != 0 && b < INFINITY) most_bias = fmaxf(most_bias, fabsf(b));
     }
+    const double reach = warp_max(most_bias);
+    bool unsure = false;
     if (g.groups > 1) {
         const int per_group = g.E / g.groups;
         uint64_t value_key[1] = {0};                            // lane i: the value of group i
@@ -164,12 +312,18 @@ __device__ __noinline__ Choice choose_exact(const RouteArgs& g, int64_t t)
             if (lane == gr) value_key[0] = best;
         }
         uint32_t kept = 0;
+        double last = INFINITY;
         for (int n = 0; n < g.kept; ++n) {
             int at = 0;
-            if (best_of(value_key, lane, at, [&](int) { return true; }) == 0) break;
+            const uint64_t best = best_of(value_key, lane, at, [&](int) { return true; });
+            if (best == 0) break;
             kept |= 1u << at;
+            last = value_of(best);
             if (lane == at) value_key[0] = 0;
         }
+        // the last that is kept and those that are not (a sum's terms are no larger than it and twice their biases)
+        const double size = 2.0 * fabs(last) + 4.0 * g.group_top * reach;
+        unsure = __any_sync(0xffffffffu, value_key[0] != 0 && !(last - value_of(value_key[0]) > kNear * size));
         #pragma unroll
         for (int i = 0; i < VPL; ++i) {
             const int e = lane * VPL + i;
@@ -177,16 +331,47 @@ __device__ __noinline__ Choice choose_exact(const RouteArgs& g, int64_t t)
         }
     }
     Choice c{-1, -INFINITY};
-    for (int j = 0; j < g.top_k; ++j) {
-        int at = 0;
-        if (best_of(key, lane, at, [&](int) { return true; }) == 0) break;
-        float v = 0.f;
+    uint64_t before = 0;                                        // the last choice
+    float before_logit = 0.f;
+    int before_at = 0;
+    auto near = [&](uint64_t next, double size) {
+        const double a = value_of(before), b = value_of(next);
+        return !(a - b > kNear * (fabs(a) + fabs(b) + size));
+    };
+    auto look = [&](uint64_t next, int at, float logit) {
+        if (before == 0 || !near(next, 4.0 * reach)) return;
+        const float b = g.bias != nullptr ? g.bias[at] : 0.f, before_b = g.bias != nullptr ? g.bias[before_at] : 0.f;
+        unsure = unsure || ((logit != before_logit || b != before_b) && near(next, 2.0 * (fabs((double)b) + fabs((double)before_b))));
+    };
+    auto take = [&](float& logit, int& at) {                    // the best that is left
+        const uint64_t best = best_of(key, lane, at, [&](int) { return true; });
+        if (best == 0) return best;
         #pragma unroll
         for (int i = 0; i < VPL; ++i)
-            if (lane * VPL + i == at) { v = x[i]; key[i] = 0; }
-        v = __shfl_sync(0xffffffffu, v, at / VPL);
-        if (lane == j) { c.pick = at; c.logit = v; }
+            if (lane * VPL + i == at) { logit = x[i]; key[i] = 0; }
+        logit = __shfl_sync(0xffffffffu, logit, at / VPL);
+        look(best, at, logit);
+        return best;
+    };
+    #pragma unroll 1
+    for (int j = 0; j < g.top_k; ++j) {
+        int at = 0;
+        float logit = 0.f;
+        const uint64_t best = take(logit, at);
+        if (best == 0) break;
+        if (lane == j) { c.pick = at; c.logit = logit; }
+        before = best; before_logit = logit; before_at = at;
     }
+    uint64_t left = 0;
+    #pragma unroll
+    for (int i = 0; i < VPL; ++i) left = key[i] > left ? key[i] : left;
+    left = warp_max(left);
+    if (before != 0 && left != 0 && near(left, 4.0 * reach)) {
+        int at = 0;
+        float logit = 0.f;
+        take(logit, at);
+    }
+    if (unsure) c.pick = kOpen;
     return c;
 }
 
@@ -246,9 +431,10 @@ __device__ __forceinline__ void note_block(const RouteArgs& g, uint32_t* chosen,
 // What a launch is told: tokens of a block, experts of a group; whether the groups' lanes are side by side, 2^group_shift of them (else 1).
 struct RoutePlan { int tokens, group_size, group_shift; bool side_by_side; };
 
-// counts: [blocks][E], or NULL: no plan, or one block, which finishes it.  kScored: a bias or sums of scores.
+// counts: [blocks][E], or NULL: no plan, or one block, which finishes it.  kScored: a bias or sums of scores.  (Two blocks to an SM, and tokens
+// that double leaves open only when the others are done: what is called for one in a thousand is not to take the others' registers.)
 template <typename T, int VPL, bool kScored>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kScored && VPL <= 4 ? 2 : 1)
 route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int* counts)
 {
     extern __shared__ uint32_t chosen[];                       // [E][words]; then count and start, [E + 1] each
@@ -267,6 +453,7 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
     }
     alignas(16) T raw[VPL];
     if (warp < n_tok) ask_logits<T, VPL>(g, t0 + warp, lane, raw);
+    uint32_t open = 0;                                          // this warp's tokens that double leaves open
     for (int t = warp; t < n_tok; t += kWarps) {
         float x[VPL];
         take_logits<T, VPL>(g, lane, raw, x);
@@ -299,7 +486,7 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
             #pragma unroll
             for (int i = 0; i < VPL; ++i) key[i] = x[i] > -INFINITY ? key_of(x[i]) : 0;
         }
-        bool unsure = g.groups > 1 && g.group_top > 2;
+        bool unsure = g.groups > 1 && g.group_top > 2;             // (scored)
         if (g.groups > 1 && !unsure) {
             uint32_t a = 0, b = 0;                              // the largest and second largest of this lane's group
             int mine = lane >> p.group_shift;
@@ -376,23 +563,18 @@ route_choose_kernel(const __grid_constant__ RouteArgs g, const RoutePlan p, int*
                 if (last != 0 && next != 0) unsure = unsure || !(value_of(last) - value_of(next) > 2.f * slack);
             }
         }
-        if (unsure) c = choose_exact<T, VPL>(g, t0 + t);
-        else if (c.pick >= 0) c.logit = fminf(to_f32(static_cast<const T*>(g.logits)[(t0 + t) * g.stride + c.pick]), FLT_MAX);
-        float w = 0.f;
-        if (g.renormalise) {
-            // s up to a factor that all choices share, so that scores too small for fp32 still have their ratios
-            const float best = warp_max(c.logit);
-            if (c.pick >= 0)
-                w = g.score == RTN_SCORE_SOFTMAX ? expf(c.logit - best) : expf(fminf(c.logit, 0.f) - fminf(best, 0.f)) / (1.f + expf(-fabsf(c.logit)));
-            const float all = warp_sum(w);
-            if (c.pick >= 0) w /= all;
-        } else if (c.pick >= 0) {
-            w = g.score == RTN_SCORE_SOFTMAX ? expf(c.logit - top) / sum : 1.f / (1.f + expf(-c.logit));
-        }
-        if (lane < k) {
-            g.experts[(t0 + t) * k + lane] = c.pick;
-            g.weights[(t0 + t) * k + lane] = w * g.scale;
-            if (plan && c.pick >= 0) atomicOr(&chosen[c.pick * words + (t >> 5)], 1u << (t & 31));
+        if (kScored && unsure) {
+            if constexpr (kScored) {
+                c = choose_exact<T, VPL>(g, t0 + t);
+                if (c.pick == kOpen) { open |= 1u << (t / kWarps); continue; }
+            }
+        } else if (c.pick >= 0) c.logit = fminf(to_f32(static_cast<const T*>(g.logits)[(t0 + t) * g.stride + c.pick]), FLT_MAX);
+        finish_token(g, t0 + t, c, top, sum, plan ? chosen : nullptr, words, t);
+    }
+    if constexpr (kScored) {
+        for (; open != 0; open &= open - 1) {
+            const int t = warp + (__ffs(open) - 1) * kWarps;
+            choose_by_pairs<T>(g, t0 + t, plan ? chosen : nullptr, words, t);
         }
     }
     if (plan) note_block(g, chosen, t0, n_tok, words, counts);
