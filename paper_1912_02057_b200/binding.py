@@ -5,7 +5,8 @@ the path runs in the library's CUDA kernels.  There is no fallback: if the share
 missing, the first call raises.
 
 ``stream=S`` stands for ``with torch.cuda.stream(S)`` around the call: the results a call makes belong to S, and as there the
-caller sees to it that inputs made on another stream are complete, and stay, until S has used them.
+caller sees to it that inputs made on another stream are complete, and stay, until S has used them.  (The layer operators keep the memory
+of their tensors until then by themselves, temporaries among them, where S is one of torch's own streams.)
 """
 import collections
 import contextlib
@@ -431,7 +432,8 @@ def _load_torch_side():
     at = lambda f: C.cast(f, C.c_void_p).value
     L = lib()
     native.bind(at(L.rtn_ternary_linear), at(L.rtn_qk_norm_rotary), at(L.rtn_decay_attention), at(L.rtn_decay_attention_step),
-                at(L.rtn_packed_row_bytes), at(L.rtn_route_experts), at(L.rtn_ternary_experts), at(L.rtn_block_norm), RtnError)
+                at(L.rtn_packed_row_bytes), at(L.rtn_route_experts), at(L.rtn_ternary_experts), at(L.rtn_block_norm), RtnError,
+                torch.cuda.Stream)
     _torch_side = native
     return native
 
@@ -441,7 +443,7 @@ def rtn_ternary_linear(a_packed, a_sum, w_packed, w_sum, M, N, K, a_scale, a_off
     """act(packed ternary product + affine form + bias) + residual -> [M,N] of ``dtype`` (default: the type of ``out`` or
     ``residual``, else fp32).  ``out`` may be ``residual``; rows of either may be strided."""
     return (_torch_side or _load_torch_side()).linear(a_packed, a_sum, w_packed, w_sum, M, N, K, a_scale, a_offset, w_scale, w_offset,
-                                                      bias, activation, residual, out, dtype, stream and stream.cuda_stream)
+                                                      bias, activation, residual, out, dtype, stream)
 
 
 def rtn_rotary_table(rows, R, base=10000.0, scaling=ROTARY_SCALE_NONE, factor=1.0, original_context=0.0, low=1.0, high=32.0,
@@ -460,7 +462,7 @@ def rtn_qk_norm_rotary(q, k, positions, table, q_weight=None, k_weight=None, eps
     """Norms (where weights are given) and rotation of q [T,Hq,D] and k [T,Hk,D] (or None) by the rows ``positions`` (int64 [T],
     or None: 0, 1, ...) of ``table`` [P,R] (or None: no rotation).  ``out_q`` / ``out_k`` may be the inputs.  Returns both."""
     return (_torch_side or _load_torch_side()).rotary(q, k, positions, table, q_weight, k_weight, eps, layout, out_q, out_k,
-                                                      stream and stream.cuda_stream)
+                                                      stream)
 
 
 def rtn_decay_attention(q, k, v, log_decay, start, max_len, state=None, state_out=None, slots=None, scale=None, out=None, stream=None):
@@ -470,13 +472,13 @@ def rtn_decay_attention(q, k, v, log_decay, start, max_len, state=None, state_ou
     run on the tensor cores, with scores and the state's part in an output held to 16 bits; states keep fp32's precision.  Returns
     (out [total,H,Dv], state_out)."""
     return (_torch_side or _load_torch_side()).decay(q, k, v, log_decay, start, max_len, state, state_out, slots, scale, out,
-                                                     stream and stream.cuda_stream)
+                                                     stream)
 
 
 def rtn_decay_attention_step(q, k, v, log_decay, state, state_out=None, slots=None, scale=None, out=None, stream=None):
     """One new token for each of B sequences: q [B,H,Dk], k [B,Hk,Dk], v [B,Hk,Dv]; ``state`` (None: zero) and ``state_out``
     (default: in place) fp32 [slots,H,Dk,Dv], ``slots`` int32 [B] (negative: a padding entry).  Returns (out [B,H,Dv], state_out)."""
-    return (_torch_side or _load_torch_side()).step(q, k, v, log_decay, state, state_out, slots, scale, out, stream and stream.cuda_stream)
+    return (_torch_side or _load_torch_side()).step(q, k, v, log_decay, state, state_out, slots, scale, out, stream)
 
 
 Routing = collections.namedtuple("Routing", "experts weights start tokens place")
@@ -490,7 +492,7 @@ def rtn_route_experts(logits, top_k, score=SCORE_SOFTMAX, bias=None, groups=1, k
     weights fp32 [T,top_k], start int32 [E+1], tokens int32 [T*top_k], place int32 [T,top_k]); the last three are the plan of the rows
     that rtn_ternary_experts works on (``plan=False``: None).  Logits of -inf or NaN are never chosen (-1 where too few are left)."""
     return Routing(*(_torch_side or _load_torch_side()).route(logits, top_k, score, bias, groups, kept_groups, group_top, renormalise, scale, plan,
-                                                              stream and stream.cuda_stream))
+                                                              stream))
 
 
 def rtn_ternary_experts(a_packed, a_sum, tokens, start, w_packed, w_sum, N, K, a_scale, a_offset, w_scale, w_offset, bias=None,
@@ -501,7 +503,7 @@ def rtn_ternary_experts(a_packed, a_sum, tokens, start, w_packed, w_sum, N, K, a
     (packed rows, sums); an ``out`` given with thresholds is written too.  Rows outside every expert are left as they were."""
     return (_torch_side or _load_torch_side()).experts(a_packed, a_sum, tokens, start, w_packed, w_sum, N, K, a_scale, a_offset, w_scale, w_offset,
                                                        bias, activation, gated, out, dtype, t_lo, t_hi, out_packed, out_sum,
-                                                       stream and stream.cuda_stream)
+                                                       stream)
 
 
 def rtn_block_norm(branch, residual=None, place=None, weights=None, post_weight=None, gate=None, gate_kind=GATE_LINEAR, scale=None,
@@ -513,4 +515,4 @@ def rtn_block_norm(branch, residual=None, place=None, weights=None, post_weight=
     ``normed``, else ``dtype``, else h's)."""
     return Normed(*(_torch_side or _load_torch_side()).block_norm(branch, residual, place, weights, post_weight, gate, gate_kind, scale, norm_weight,
                                                                   eps, out, normed, t_lo, t_hi, out_packed, out_sum, dtype,
-                                                                  stream and stream.cuda_stream))
+                                                                  stream))

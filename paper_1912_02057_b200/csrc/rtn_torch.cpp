@@ -9,6 +9,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -26,6 +27,7 @@ decltype(&rtn_route_experts) f_route;
 decltype(&rtn_ternary_experts) f_experts;
 decltype(&rtn_block_norm) f_norm;
 PyObject* rtn_error;                // class RtnError(code, where)
+PyObject* torch_stream;             // class torch.cuda.Stream
 
 // Thrown with the Python error already set.
 struct Raised {};
@@ -82,12 +84,29 @@ struct Call {
     c10::Device device;
     void* stream;
     bool given;                 // a stream of the caller's, not the current one
+    bool lasting = false;       // one of torch's own, which are there as long as any tensor
     Call(const at::Tensor& first, PyObject* stream_or_none) : device(first.device()), given(stream_or_none != Py_None)
     {
         if (!first.is_cuda()) refuse("expected a CUDA tensor");
         const auto current = c10::cuda::current_device();
         if (device.index() != current) refuse("tensors on " + device.str() + ", but the current device is cuda:" + std::to_string(current));
-        stream = given ? reinterpret_cast<void*>(whole(stream_or_none, "stream")) : c10::cuda::getCurrentCUDAStream(current).stream();
+        stream = c10::cuda::getCurrentCUDAStream(current).stream();
+        if (!given) return;
+        PyObject* handle = PyObject_GetAttrString(stream_or_none, "cuda_stream");
+        if (handle == nullptr) throw Raised{};
+        void* own = PyLong_AsVoidPtr(handle);
+        Py_DECREF(handle);
+        if (own == nullptr && PyErr_Occurred()) throw Raised{};
+        lasting = own != stream && reinterpret_cast<PyObject*>(Py_TYPE(stream_or_none)) == torch_stream;
+        stream = own;
+    }
+    // Memory that the call uses stays until its stream has: a temporary of the current stream, let go of when the call returns, would be given to the next
+    // tensor there at once, and written while this stream is still to read it.  (An outside stream may be gone when a tensor is: its memory is the
+    // caller's to keep.)
+    void* use(const at::Tensor& t) const
+    {
+        if (lasting) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), device.index()));
+        return t.data_ptr();
     }
     // A contiguous tensor of this type; None is NULL.
     template <typename T = void>
@@ -99,7 +118,7 @@ struct Call {
             if (!shape.empty()) { want += " ["; for (size_t i = 0; i < shape.size(); ++i) want += (i ? ", " : "") + std::to_string(shape[i]); want += "]"; }
             refuse(std::string(name) + ": expected contiguous " + want + " on " + device.str() + ", got " + text(*t));
         }
-        return static_cast<T*>(t->data_ptr());
+        return static_cast<T*>(use(*t));
     }
     // A result of the stream that writes it: on the current one's memory it could take the place of a tensor whose last use there
     // is still to come.
@@ -122,7 +141,7 @@ struct Heads {
             refuse(std::string(name) + ": expected " + c10::toString(type) + " [" + std::to_string(T) + ", " + std::to_string(H) + ", " +
                    std::to_string(D) + "] on " + call.device.str() + ", got " + text(t));
         if (t.stride(2) != 1 && D > 1 && t.numel() > 0) refuse(std::string(name) + ": the elements of a head have to be adjacent");
-        p = t.data_ptr(); token = t.stride(0); head = t.stride(1);
+        p = call.use(t); token = t.stride(0); head = t.stride(1);
     }
 };
 
@@ -194,7 +213,7 @@ PyObject* linear(PyObject* const* a)
         if (t->dim() != 2 || t->size(0) != M || t->size(1) != N || t->scalar_type() != type || t->device() != call.device || (t->stride(1) != 1 && N > 1))
             refuse(std::string(i ? "out" : "residual") + ": expected " + c10::toString(type) + " [" + std::to_string(M) + ", " + std::to_string(N) +
                    "] with adjacent columns on " + call.device.str() + ", got " + text(*t));
-        at_[i] = t->data_ptr();
+        at_[i] = call.use(*t);
         stride[i] = M > 1 ? t->stride(0) : std::max(N, t->stride(0));
     }
     const float *s1, *o1, *s2, *o2;
@@ -314,7 +333,7 @@ struct Rows {
             (t.stride(1) != 1 && width > 1 && t.size(0) > 0))
             refuse(std::string(name) + ": expected " + c10::toString(type) + " [" + (rows >= 0 ? std::to_string(rows) : "rows") + ", " +
                    std::to_string(width) + "] with adjacent columns on " + call.device.str() + ", got " + text(t));
-        p = t.data_ptr();
+        p = call.use(t);
         stride = t.size(0) > 1 ? t.stride(0) : std::max(width, t.stride(0));
     }
 };
@@ -487,7 +506,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     try {
-        expect_args(n, 9);
+        expect_args(n, 10);
         f_linear = reinterpret_cast<decltype(f_linear)>(whole(args[0], ""));
         f_rotary = reinterpret_cast<decltype(f_rotary)>(whole(args[1], ""));
         f_decay = reinterpret_cast<decltype(f_decay)>(whole(args[2], ""));
@@ -497,6 +516,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
         f_experts = reinterpret_cast<decltype(f_experts)>(whole(args[6], ""));
         f_norm = reinterpret_cast<decltype(f_norm)>(whole(args[7], ""));
         rtn_error = Py_NewRef(args[8]);
+        torch_stream = Py_NewRef(args[9]);
     } catch (const Raised&) {
         return nullptr;
     }

@@ -144,3 +144,104 @@ def test_block_norm_codes_where_squares_leave_fp32(W, size):
             bits = np.unpackbits(p, axis=3, bitorder="little").transpose(2, 0, 1, 3).reshape(2, T, -1)[:, :, :W]
             assert np.array_equal(bits[0], want != 0) and np.array_equal(bits[1], want > 0)
     assert rtn.rtn_last_device_status() == 0
+
+
+# ---------------------------------------------------------------------------------------------- other streams
+
+def layer(seed, T, E=12, W=256, H=128, k=3):
+    """A chain of the operators, whose inputs are all there before its first call."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    x, logits = randn(T, W), randn(T, E)
+    up, us = rtn.rtn_pack_weights(codes(g, E * 2 * H, W))
+    down, ds = rtn.rtn_pack_weights(codes(g, E * W, H))
+    us, ds = us[0].contiguous(), ds[0].contiguous()
+    one, zero, small, lo, hi, low, high = (torch.tensor([v], device="cuda") for v in (1.0, 0.0, 0.05, -0.4, 0.4, -0.1, 0.1))
+    weight = 1 + 0.1 * randn(W)
+
+    def run(stream=None):
+        n = rtn.rtn_block_norm(None, x, norm_weight=weight, t_lo=lo, t_hi=hi, stream=stream)
+        r = rtn.rtn_route_experts(logits, k, stream=stream)
+        h = rtn.rtn_ternary_experts(n.codes, n.sums, r.tokens, r.start, up, us, 2 * H, W, one, zero, small, zero, activation=rtn.ACT_SILU, gated=True,
+                                    t_lo=low, t_hi=high, stream=stream)
+        y = rtn.rtn_ternary_experts(h[0], h[1], None, r.start, down, ds, W, H, one, zero, small, zero, dtype=torch.bfloat16, stream=stream)
+        z = rtn.rtn_block_norm(y, x, place=r.place, weights=r.weights, post_weight=weight, norm_weight=weight, normed=True, t_lo=lo, t_hi=hi, stream=stream)
+        return [n.codes, n.sums, *r, *h, y, *z]
+    return run
+
+
+@pytest.mark.parametrize("sizes", [(1, 5), (700, 900), (2, 5000), (100, 16000)], ids=str)
+def test_two_streams_at_a_time_in_memory_of_earlier_results(sizes):
+    """Twenty layers on each of two streams, four times; in between the results' memory is filled with something else."""
+    chains = [layer(i, T) for i, T in enumerate(sizes)]
+    want = [[t.clone() for t in run()] for run in chains]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in chains]
+    for fill in (0x11, 0xa5, 0x11, 0xff):
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        got = [[run(stream=s) for run, s in zip(chains, streams)] for _ in range(20)]
+        torch.cuda.synchronize()
+        for both in got:
+            for a, b in zip(both, want):
+                assert all(torch.equal(p, q) for p, q in zip(a, b))
+        for t in (t for both in got for a in both for t in a):
+            t.view(torch.uint8).fill_(fill)
+        torch.cuda.synchronize()
+        del got, both, a
+    assert rtn.rtn_last_device_status() == 0
+
+
+def calls_with_temporaries():
+    """Name and call of each layer operator, on tensors that are made for the call and let go of behind it."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    T, W, E, D = 70, 256, 8, 64
+    x, logits, half, zero = randn(T, W), randn(T, E), torch.tensor([0.5], device="cuda"), torch.zeros(1, device="cuda")
+    xp, xs = rtn.rtn_ternarize_pack_act(x, -half, half)
+    wp, ws = rtn.rtn_pack_weights(codes(g, E * W, W))
+    ws = ws[0].contiguous()
+    table, q, kv, decay, weight = rtn.rtn_rotary_table(300, D), randn(T, 4, D), randn(T, 2, D), -0.1 * torch.ones(4, device="cuda"), randn(W)
+    route = rtn.rtn_route_experts(logits, 2)
+    rows = randn(2 * T, W)
+    states = randn(T, 4, D, D)
+    one = half + half
+    return [("linear", lambda on: [rtn.rtn_ternary_linear(xp + 0, xs + 0, wp[:W] + 0, ws[:W] + 0, T, W, W, one + 0, zero + 0, one + 0, zero + 0, bias=weight + 0, residual=x + 0,
+                                                          stream=on)]),
+            ("rotary", lambda on: [t for t in rtn.rtn_qk_norm_rotary(q + 0, kv + 0, torch.arange(T, device="cuda"), table + 0, weight[:D] + 0, weight[:D] + 0, stream=on)]),
+            ("prompt", lambda on: rtn.rtn_decay_attention(q + 0, kv + 0, kv + 0, decay + 0, torch.tensor([0, 30, T], dtype=torch.int32).cuda(), 40, stream=on)),
+            ("step", lambda on: rtn.rtn_decay_attention_step(q + 0, kv + 0, kv + 0, decay + 0, states + 0, stream=on)),
+            ("route", lambda on: rtn.rtn_route_experts(logits + 0, 3, score=rtn.SCORE_SIGMOID, bias=logits[0] + 0, stream=on)),
+            ("experts", lambda on: rtn.rtn_ternary_experts(xp + 0, xs + 0, route.tokens + 0, route.start + 0, wp + 0, ws + 0, W, W, one + 0, zero + 0, one + 0, zero + 0,
+                                                           t_lo=-half, t_hi=half + 0, stream=on)),
+            ("norm", lambda on: rtn.rtn_block_norm(rows + 0, x + 0, place=route.place + 0, weights=route.weights + 0, post_weight=weight + 0, gate=x + 0, scale=weight + 0,
+                                                   norm_weight=weight + 0, t_lo=-half, t_hi=half + 0, stream=on))]
+
+
+def test_temporaries_stay_until_the_given_stream_has_used_them():
+    side = torch.cuda.Stream()
+    for name, call in calls_with_temporaries():
+        want = [t.clone() for t in call(None) if t is not None]
+        torch.cuda.synchronize()
+        for _ in range(2):
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(20_000_000)
+            got = [t for t in call(side) if t is not None]
+            # what the temporaries left behind, if anything, goes to these
+            junk = [torch.full((n,), 0x7f, dtype=torch.uint8, device="cuda") for n in [1 << b for b in range(2, 23)] + [280, 560, 32, 36, 64, 1024] + [8] * 20]
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, got)), name
+            del junk
+    # with a stream of the caller's that torch does not own, and with the current one
+    held = torch.cuda.ExternalStream(side.cuda_stream)
+    for name, call in calls_with_temporaries():
+        want = [t.clone() for t in call(None) if t is not None]
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.default_stream())
+            for on in (side, held, None):
+                got = [t for t in call(on) if t is not None]
+                side.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(want, got)), name
+    with pytest.raises(AttributeError):
+        rtn.rtn_route_experts(torch.zeros(2, 4, device="cuda"), 1, stream=7)
+    assert rtn.rtn_last_device_status() == 0
