@@ -146,6 +146,52 @@ def test_block_norm_codes_where_squares_leave_fp32(W, size):
     assert rtn.rtn_last_device_status() == 0
 
 
+# ---------------------------------------------------------------------------------------------- thresholds the other way round
+
+def plus_first(v, lo, hi):
+    """1 above hi, else -1 below lo, else 0, for any lo and hi."""
+    return as_codes(v, lo, hi).astype(np.int8)
+
+
+def packed_of(c):
+    rows, n = c.shape
+    p = np.zeros((rows, -(-n // 128) * 128), np.int8)
+    p[:, :n] = c
+    p = p.reshape(rows, -1, 128)
+    return np.concatenate([np.packbits(p != 0, axis=2, bitorder="little"), np.packbits(p > 0, axis=2, bitorder="little")], 2).reshape(rows, -1)
+
+
+@pytest.mark.parametrize("lo,hi", [(0.5, -0.5), (-0.25, -0.75), (0.75, 0.25), (0.5, 0.5), (float("inf"), float("-inf")), (0.0, 0.0)], ids=ids)
+@pytest.mark.parametrize("R", [5, 600])
+def test_codes_of_thresholds_that_overlap(R, lo, hi):
+    """Few rows and many through the experts, every activation that leaves whole sums exact; and the norms."""
+    g = torch.Generator(device="cuda").manual_seed(R)
+    E, N, K = 3, 200, 90
+    x, w = codes(g, R, K), codes(g, E, N, K)
+    start = torch.tensor([0, R // 3, R // 3, R], dtype=torch.int32, device="cuda")
+    half, one, zero, step = (torch.tensor([v], device="cuda") for v in (0.5, 1.0, 0.0, 0.25))
+    xp, xs = rtn.rtn_ternarize_pack_act(x.float(), -half, half)
+    wp, ws = rtn.rtn_pack_weights(w.view(E * N, K))
+    of = np.repeat([0, 2], [R // 3, R - R // 3])
+    y = 0.25 * np.stack([w[e].cpu().numpy().astype(np.float64) @ v for e, v in zip(of, x.cpu().numpy().astype(np.float64))])    # (multiples of 1/4: exact)
+    t = dict(t_lo=torch.tensor([lo], device="cuda"), t_hi=torch.tensor([hi], device="cuda"))
+    for act in (rtn.ACT_NONE, rtn.ACT_RELU):
+        z = y if act == rtn.ACT_NONE else np.maximum(y, 0.0)
+        first = np.maximum(y[:, :N // 2], 0.0) if act == rtn.ACT_RELU else y[:, :N // 2]
+        for gated in (False, True):
+            want = plus_first(first * y[:, N // 2:] if gated else z, lo, hi)
+            got = rtn.rtn_ternary_experts(xp, xs, None, start, wp, ws[0].contiguous(), N, K, one, zero, step, zero, activation=act, gated=gated, **t)
+            assert np.array_equal(got[0].cpu().numpy(), packed_of(want)) and np.array_equal(got[1].cpu().numpy(), want.sum(1))
+    for W in (256, 130, 131):
+        v = 0.25 * torch.randint(-6, 7, (R, W), generator=g, device="cuda").float()
+        want = plus_first(v.cpu().numpy(), lo, hi)
+        got = rtn.rtn_block_norm(None, v, **t)
+        assert np.array_equal(got.codes.cpu().numpy(), packed_of(want)) and np.array_equal(got.sums.cpu().numpy(), want.sum(1))
+        per = rtn.rtn_block_norm(None, v, t_lo=t["t_lo"].expand(W).contiguous(), t_hi=t["t_hi"].expand(W).contiguous())
+        assert torch.equal(got.codes, per.codes) and torch.equal(got.sums, per.sums)
+    assert rtn.rtn_last_device_status() == 0
+
+
 # ---------------------------------------------------------------------------------------------- other streams
 
 def layer(seed, T, E=12, W=256, H=128, k=3):
