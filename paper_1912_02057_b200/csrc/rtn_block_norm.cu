@@ -103,12 +103,13 @@ __device__ __forceinline__ float root_of_ratio(float a, float b)
 }
 // Units of a root's error: roundings of the sum of squares `ss`, per thread and over two trees, of the mean and of the root (approximate: two units in the last
 // place of 2^-23), and the values' own errors, whose squares add up to `sm`.  No bound where squares leave fp32: what
-// falls below its normal range is less than 2^-149 each, nothing beside a mean (with eps: `square`) of 1e-30; above 2^126 the quotient is 0.
+// falls below its normal range is less than 2^-149 each, nothing beside a mean (with eps: `square`) of 1e-30; above 2^126 the quotient is 0.  And none
+// where the values' errors are more than a 64th of them (sums that cancel): bounds are to first order.
 template <int NV, int EV>
 __device__ __forceinline__ float root_units(float square, float ss, float sm)
 {
     const float units = 0.5f * (NV * EV + 10) + 6.f + (ss > 0.f ? root_of_ratio(sm, ss) : 0.f);
-    return square > 1e-30f && ss < 8e37f ? units : INFINITY;
+    return square > 1e-30f && ss < 8e37f && units < 262144.f ? units : INFINITY;
 }
 
 // h and n of token t.  slack receives the bound on n's error, where kTrack asks for it.  Loads are not in branches (a value behind the row's end is

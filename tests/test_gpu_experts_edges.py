@@ -146,6 +146,30 @@ def test_block_norm_codes_where_squares_leave_fp32(W, size):
     assert rtn.rtn_last_device_status() == 0
 
 
+@pytest.mark.parametrize("apart", [2.0 ** -23, 2.0 ** -21, 2.0 ** -18, 2.0 ** -12])
+@pytest.mark.parametrize("eps", [0.0, 1e-16])
+def test_block_norm_codes_of_sums_that_cancel(apart, eps):
+    """Two experts' rows that all but cancel: what fp32 leaves of their sum is mostly rounding, and the codes are those of the exact sum all the same."""
+    T, W = 2000, 256
+    r = np.random.default_rng(5)
+    a = r.standard_normal((T, W)).astype(np.float32)
+    rows = np.concatenate([a, a * (1.0 + apart * r.integers(-3, 4, (T, W)))]).astype(np.float32)
+    w = np.tile(np.float32([0.3, -0.3]), (T, 1)) * r.uniform(1.0, 2.0, (T, 1)).astype(np.float32)
+    y = w[:, :1].astype(np.float64) * rows[:T] + w[:, 1:].astype(np.float64) * rows[T:]
+    n = y / np.sqrt((y * y).mean(1, keepdims=True) + eps)
+    dev = lambda v: torch.from_numpy(np.ascontiguousarray(v)).cuda()  # noqa: E731
+    place, ones = dev(np.stack([np.arange(T), np.arange(T, 2 * T)], 1).astype(np.int32)), torch.ones(W, device="cuda")
+    for hi in (0.05, 0.7, 3.0):
+        want = as_codes(n, -float(np.float32(hi)), float(np.float32(hi)))
+        t = torch.tensor([hi], device="cuda")
+        for norm in ("post_weight", "norm_weight"):
+            got = rtn.rtn_block_norm(dev(rows), place=place, weights=dev(w), eps=eps, t_lo=-t, t_hi=t, **{norm: ones})
+            assert np.array_equal(got.sums.cpu().numpy(), want.sum(1))
+            p = got.codes.cpu().numpy().reshape(T, -1, 2, 16)
+            bits = np.unpackbits(p, axis=3, bitorder="little").transpose(2, 0, 1, 3).reshape(2, T, -1)[:, :, :W]
+            assert np.array_equal(bits[0], want != 0) and np.array_equal(bits[1], want > 0)
+
+
 # ---------------------------------------------------------------------------------------------- thresholds the other way round
 
 def plus_first(v, lo, hi):
