@@ -360,7 +360,9 @@ rtn_status rtn_route_experts(const void* logits, int64_t logits_stride, int64_t 
  *   out         NULL, or [R][F] of `dtype`, rows out_stride >= F elements apart
  *   out_packed, out_sum   NULL (both), or the codes of the outputs against thresholds, R packed rows of F codes and their sums, as
  *               rtn_ternarize_pack_act gives them: what the next product reads.  t_lo, t_hi: n_thr 1 or E.  They are the codes of the exact
- *               output (one that fp32 cannot tell from a threshold is computed in double); out and out_packed may both be given
+ *               output (one that fp32 cannot tell from a threshold is computed in double; products of parameters that fall below fp32's normal
+ *               range keep what it keeps of them); out and out_packed may both be given
+ * Values are worked out in fp32 and rounded to `dtype` once; RTN_ACT_SILU by approximations, within 6 units of 2^-24 |y|.
  * Few rows run on a bit-plane kernel that streams the weights, others on the tensor cores (with scratch of R * K / 2 bytes, K rounded up to
  * 256).  Bounds that do not fit (a decreasing start, or one outside 0 .. R) leave the expert's outputs as they were, a token out of
  * range makes its row NaN (codes 0), and rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once.  After such bounds the sums, and
@@ -384,7 +386,10 @@ rtn_status rtn_ternary_experts(const void* a_packed, const int32_t* a_sum, int64
  *   stream_out  NULL, or h in `stream_dtype`; may be `residual` (same stride), no other overlap
  *   normed      NULL, or n in `dtype` (n is computed from h before its rounding)
  *   out_packed, out_sum   NULL (both), or n's codes, T packed rows of W codes and their sums (t_lo, t_hi: n_thr 1 or W); they are the codes of
- *               the exact n
+ *               the exact n (of double: a logistic function below its range is 0; factors whose product falls below fp32's normal range keep
+ *               what it keeps of them)
+ * h and n as values are worked out in fp32, squares too: behind post_weight or norm_weight a row is 0 where the mean of its squares is beyond fp32 (values
+ * above 1.8e19), and without an eps to speak of it loses digits where that is below 1e-30.  Their codes are not touched by this.
  * Rows of every tensor are `*_stride` elements apart (0 repeats a row of an input).  W <= 16384.  A place >= R makes the token's row NaN
  * (codes 0), and rtn_last_device_status reports RTN_ERR_DEVICE_INDEX once.  With places, R may be 0 (branch is not read, and may be NULL). */
 rtn_status rtn_block_norm(const void* branch, int64_t branch_stride, int64_t R, const int32_t* place, const float* weights, int64_t k,

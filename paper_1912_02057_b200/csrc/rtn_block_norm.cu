@@ -1,5 +1,5 @@
 // The norms after one block and before the next, with the block's gate, its residual and the experts' weighted sum, and the codes of the
-// result: a CTA per token, the token's values in registers between the passes.
+// result: a CTA per token, the token's values in registers between the passes (what of them does not fit is with the launcher's rule).
 //
 // Bound: HBM, every input and output once.
 //
@@ -8,9 +8,12 @@
 //   1/sqrt(mean + eps) of a sum of squares over a tree  relative: (half of the tree's depth) + |E| / |.| (of the vector norms)
 // and so on through gate, scale and residual.  A value nearer to a threshold than its bound, or one that is not finite, makes the CTA work
 // the token's codes out again in double; of tokens of 2048 normal values about one in a hundred.  That pass takes 10 us, which is what the last of a
-// launch's rows that needs it adds (with thresholds that nothing is near, the 123 us below are 112).
-// Measured (one B200): 8192 tokens of 2048, bf16, 8 experts' rows each, both norms, codes 123 us (407 MB: 62 at the copy rate; the rest is issue slots, some
-// 1200 instructions per 256 values); one token of 2048, 4 rows, codes 3.5 us in a graph; 48 of 4096, gated 3.3 us; 1111 of 5003, fp32, one value to an access 30.5 us.
+// launch's rows that needs it adds (with thresholds that nothing is near, the 124 us below are 112).  A value that equals its threshold is always too near:
+// rows without a norm in 16 bits lie on values of their type, and with a threshold that is one of these nearly every token is worked out
+// again (8192 x 2048, bf16 135 us, with a threshold between two of them 37).
+// Measured (one B200): 8192 tokens of 2048, bf16, 8 experts' rows each, both norms, codes 124 us (407 MB: 62 at the copy rate; the rest is issue slots, some
+// 1200 instructions per 256 values, at half the occupancy), values in place of codes 84 us; without experts 83 and 49 us; one token of 2048, 4 rows, codes 3.4 us
+// in a graph; 48 of 4096, gated 3.4 us; 1111 of 5003, fp32, one value to an access 30.3 us.
 #include "rtn_internal.cuh"
 #include "rtn_epilogue.cuh"
 #include "rtn_tcgen05.cuh"
@@ -558,8 +561,10 @@ cudaError_t launch_types(const NormArgs& g, cudaStream_t s)
                ok(g.stream_out, g.stream_stride, sizeof(TS)) && ok(g.post_weight, 0, 4) && ok(g.norm_weight, 0, 4) &&
                (g.n_scale == 1 || ok(g.scale, 0, 4)) && (g.n_thr == 1 || (ok(g.t_lo, 0, 4) && ok(g.t_hi, 0, 4)));
     };
-    // A thread has 8 values, whose arrays fit its registers, and only above 5120 16.  Rows of up to 5120 values in one or two to an access, two blocks of up to
-    // 640 threads to an SM instead of 16 values a thread, 1111 tokens, fp32, normed and codes: 5003 33.1 and 77.3 -> 32.7 and 63.6 us, 5002 33.9 and
+    // A thread has 8 values, and only above 5120 16 where they do not come eight to an access.  Eight to an access and without codes all of them stay in its
+    // 56 to 64 registers (up to 8192 wide); in the other forms without codes up to 204 bytes a thread go to local memory, and the bounds beside the values
+    // make that 120 to 152 bytes with codes, eight to an access, and 180 to 512 in the others (of -Xptxas -v).  Rows of up to 5120 values in one or two to an access, two blocks of up to
+    // 640 threads to an SM, which leaves a thread 48 registers, instead of 16 values a thread, 1111 tokens, fp32, normed and codes: 5003 33.1 and 77.3 -> 32.7 and 63.6 us, 5002 33.9 and
     // 69.4 -> 29.7 and 58.2, 2500 16.4 and 40.8 -> 11.5 and 32.1.
     if (fits(8)) {
         if (g.W <= 2048) return launch_values<TB, TS, 8, 1, 256>(g, s);

@@ -5,7 +5,7 @@
 // shuffle tree joins the group.
 // Bound: latency for a token (a launch, one trip to DRAM for the planes, the epilogue), then DRAM, the packed weights of the experts that have rows,
 // read once; from about two rows of an expert on the POPC rate.
-// Measured (one B200): a token's 4 of 64 experts of 2048 x 2048, gated, codes 5.7 us in a graph (4.2 MB of planes: 0.7 us at the copy rate).
+// Measured (one B200): a token's 4 of 64 experts of 2048 x 2048, gated, codes 5.8 us in a graph (4.2 MB of planes: 0.7 us at the copy rate).
 #include "rtn_experts.cuh"
 #include "rtn_tcgen05.cuh"
 

@@ -8,11 +8,14 @@
 // would share), and a product of 32 inputs runs at the full rate (of 16 at two thirds).  Inputs are expanded once, ahead, into the experts' order
 // (K / 2 bytes a row of scratch): a row meets every column tile.  A persistent CTA per SM; two accumulators, so that a tile's outputs are written during the
 // next one's products; parameters are fetched two tiles ahead by warps of their own, which also put a token's codes together from the votes.
-// Codes are those of the exact output: a value nearer to a threshold than its error bound is worked out again in double, of 16 tokens at a time.
+// Codes are those of the exact output: a value nearer to a threshold than its error bound is worked out again in double, of 16 tokens at a time.  One that equals
+// it always is: an upper threshold of 0 behind a ReLU, or one of 0 behind a gated one, whose outputs are 0 half of the time, sends nearly everything there (65536
+// rows, 64 experts of 2048 x 2048, gated ReLU 1800 us in place of 273, of 2048 x 1024, ReLU 1440 in place of 208), and so do a last tile's padding columns
+// (zeros) with a threshold of 0, though not on to double.
 // Bound: for long prompts the instructions of the epilogue (50 to 65 per output) and of the expansion (some 200 per 32 rows x 256 codes), the tensor
 // pipe idles three quarters of the time; for few rows of an expert its start (2.6 us) and the first planes' way (2.6 us).
-// Measured (one B200, in a graph): 65536 rows, 64 experts of 2048 x 2048, gated, codes 243 us (2.3 PFLOP/s; the matrix instructions alone 63); of 2048 x 1024,
-// bf16 values 133 us (268 MB written); 384 rows, 64 experts of 2048 x 2048, gated, codes 22.2 us (67 MB of planes at 3.0 TB/s).
+// Measured (one B200, in a graph): 65536 rows, 64 experts of 2048 x 2048, gated, codes 242 us (2.3 PFLOP/s; the matrix instructions alone 63); of 2048 x 1024,
+// bf16 values 133 us (268 MB written); 384 rows, 64 experts of 2048 x 2048, gated, codes 22.4 us (67 MB of planes at 3.0 TB/s).
 #include "rtn_experts.cuh"
 #include "rtn_tcgen05.cuh"
 #include "rtn_tensormap.cuh"
@@ -34,7 +37,7 @@ template <int kRegs> __device__ __forceinline__ void more_registers() { asm vola
 template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
 // A slot holds a span of K, 512 codes (or the last 256): two 128-byte rows of 4-bit values to an input, 64 columns of tensor memory to a weight row.
 // (Slots of 256 codes: twice the barriers, which a small tile's time is made of.)
-constexpr int kMaxRows = 160;                                   // of a tile
+constexpr int kMaxRows = 160;                                   // of a tile (with what tells them apart: make_plan)
 constexpr int kMaxStages = 6, kMaxSpans = 8;                    // slots of the rings
 constexpr uint32_t kSpanBytes = 128 * 128;                       // 512 codes of 128 weight rows, as planes
 constexpr uint32_t kTries = 1u << 20;
@@ -717,7 +720,8 @@ experts_tiles_kernel(const __grid_constant__ ExpertsArgs g, const __grid_constan
 // Rows of a tile at most, from the rows that an expert has on average: what makes rounds of tiles times a tile's time least.  A tile's time in clocks is the
 // longer of its expansion and products (350 for 256 codes, from 135 rows on 2.6 a row) and its outputs (500 and 20 a row; fitted to
 // measured times), and the shorter once more at the end.  65536 rows of 64 experts, 2048 x 2048 gated with codes, and 2048 x 1024 to bf16 (before later
-// steps took 26 and 20 us off): 160 rows 271 and 153 us, 144 280 and 162, 128 279 and 164, 112 304 and 179; more than 160 do not leave enough tensor memory for three slots of weights.
+// steps took 26 and 20 us off): 160 rows 271 and 153 us, 144 280 and 162, 128 279 and 164, 112 304 and 179.  (512 - 16 - 2 h) / 64 slots of weights fit
+// tensor memory beside two accumulators of h rows: two from 160 on, three from 144 down.  Above kMaxRows nothing was measured; 176 would have two slots, too.
 TilesPlan make_plan(const ExpertsArgs& g)
 {
     TilesPlan p{};
@@ -727,7 +731,7 @@ TilesPlan make_plan(const ExpertsArgs& g)
     p.k_halves = halves_of((int)((g.K + kBlockCodes - 1) / kBlockCodes));
     const double used = (double)(g.R < g.E ? g.R : g.E), each = (double)g.R / used, sms = device_sm_count();
     double best = 0.0;
-    for (int h = 16; h <= 160; h += 16) {
+    for (int h = 16; h <= kMaxRows; h += 16) {
         const double per = (double)(int64_t)((each + h - 1) / h), tiles = used * per * p.col_tiles, height = each / per < 16 ? 16 : each / per;
         const double stage = 2.6 * height > 350.0 ? 2.6 * height : 350.0, loop = stage * p.k_halves, out = 20.0 * height + 500.0;
         const double rounds = tiles / sms < 1.0 ? 1.0 : (double)(int64_t)((tiles + sms - 1) / sms);

@@ -12,9 +12,14 @@
 //   whatever order the warps finish in, and so are the block's counts.
 // route_plan_kernel adds what lies before: the rows of lower experts, and of the expert's earlier blocks.  One block does both.
 // route_list_kernel does the first kernel's work for many tokens.
-// Bound: latency (two launches, a chain of about 40 clocks per pick) for few tokens, issue slots for many.
-// Measured (one B200): one token, 4 of 64 experts 3.5 us in a graph; 96 tokens, 8 of 256 in 4 of 8 groups, with a bias 11.0 us (most of it the chain of picks: 8
-// experts, 4 groups and the sums of 2 in each); 16384 tokens, 8 of 128 12.6 us (4.2 MB of logits: 0.6 us at the copy rate).
+// Bound: latency (a launch and dependent loads) for a token.  For a batch the instructions of a token and where they run: 96 tokens, 8 of 256 in 4 of 8 groups, with a
+// bias take 1660 warp instructions each, on six blocks of 16 warps, so that four warps share a scheduler of six SMs (0.44 of its issue slots) and the other SMs
+// have nothing to do.  For many tokens the places of the lists, each of which every logit goes through, and a round of blocks that comes out uneven (256 on 148
+// SMs; 0.44 of the issue slots).
+// Measured (one B200, in a graph): one token, 4 of 64 experts 3.4 us; 96 tokens as above 10.9 us; 16384 tokens, 8 of 128 12.6 us (4.2 MB of logits: 0.6 us at
+// the copy rate).  What leaves the lists: a bias or sums of scores, whose fp32 values need the bound and the exact form, groups, and more than
+// eight choices, the places that a list has; 16384 tokens take, a warp to each, 8 of 128 with a bias 32.7 us, 12 of 128 28.2, 8 of 256 with a bias 51.6, in 4 of 8
+// groups by sums of two 64.1, of three (all in double) 251.
 #include "rtn_internal.cuh"
 #include "rtn_types.cuh"
 #include "rtn_tcgen05.cuh"
